@@ -181,18 +181,17 @@ def _sizes(case):
     return [max(1, int(case["total"] * x / sum(part))) for x in part]
 
 
-def _stands(x, power, levels, scale):
-    """What an 8-bit moment's levels stand for."""
-    y = x * (1.0 / levels)
-    y = y * y.abs() if power == 2 else (y * y) * (y * y)
-    return (y.view(-1, _BLOCK) * scale[:, None]).view(-1)
+def _stands(q, power, levels, scale):
+    """What an 8-bit moment's levels stand for: (q / levels)^power of the block's scale."""
+    q = q * q.abs() if power == 2 else (q * q) * (q * q)
+    return (q.view(-1, _BLOCK) * (scale * (1.0 / levels ** power))[:, None]).view(-1)
 
 
 def _levels(x, power, levels):
     """An 8-bit moment's levels (whole numbers) and the scale of each block."""
     x = x.view(-1, _BLOCK)
     scale = x.abs().amax(1)
-    scale = torch.where(scale < 2.0 ** -100, torch.zeros_like(scale), scale)
+    scale = torch.where(scale < 2.0 ** -90, torch.zeros_like(scale), scale)
     inv = torch.where(scale > 0, 1.0 / scale, torch.zeros_like(scale))
     y = (x.abs() * inv[:, None]).sqrt()
     if power == 4:
