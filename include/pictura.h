@@ -410,6 +410,165 @@ pictura_status pictura_encode_views(const pictura_encoder* enc, const uint8_t* c
                                     int32_t height, int32_t width, void* workspace, uint64_t workspace_bytes,
                                     float* out, void* stream);
 
+/* ---- the policy: acting, learning, stepping the weights ---------------------
+ * What follows the encoder in the training process the renderer belongs to
+ * (paper Sec. 3.3 and App. A.3: categorical actions, clipped policy optimisation
+ * with normalised advantages, AdamW).  Like pictura_encode_views these calls take
+ * no context: they run on `stream` of the current device, allocate nothing and
+ * do not synchronise, so they can be captured in a graph.  Errors are found on
+ * the host before anything is launched. */
+
+#define PICTURA_F32  0
+#define PICTURA_BF16 1
+#define PICTURA_F16  2
+
+#define PICTURA_MAX_ACTIONS (1 << 20)
+
+/* Logits of a head: row n, one decision, has `actions` values of `dtype` from
+ * data + n * stride (in elements; stride >= actions) on.  mask (or NULL): byte
+ * mask[n * mask_stride + i] is 0 where action i is not allowed in row n
+ * (mask_stride 0: the same for every row); what stands at such a place is not
+ * looked at.  A logit of -inf is an action of probability zero as well. */
+typedef struct {
+    const void* data;
+    int32_t dtype;        /* PICTURA_F32, PICTURA_BF16 or PICTURA_F16 */
+    int32_t actions;      /* 1..PICTURA_MAX_ACTIONS */
+    int64_t rows;         /* 0..2^31 - 1 */
+    int64_t stride;
+    const uint8_t* mask;
+    int64_t mask_stride;
+} pictura_logits;
+
+/* How actions are drawn.  A pointer, where not NULL, holds a value for each row
+ * in place of the scalar before it.  temperature >= 0 (0: the largest logit);
+ * top_k <= 0, top_p >= 1 and min_p <= 0 are off, a NaN among top_ps or min_ps too. */
+typedef struct {
+    float temperature;
+    int32_t top_k;
+    float top_p;
+    float min_p;
+    const float* temperatures;
+    const int32_t* top_ks;
+    const float* top_ps;
+    const float* min_ps;
+} pictura_sampling;
+
+/* Draw one action per row from the random numbers uniform[rows] in [0, 1).
+ * With l the allowed logits of a row, d = (l - max l) / temperature and the
+ * weights w = rint(2^31 exp(d)) as whole numbers (fp32 up to the rounding, so
+ * that no sum below depends on its order): order the actions by logit, largest
+ * first, equal ones by index.  top_k keeps the first top_k of them; top_p of
+ * those the shortest prefix whose weights reach max(1, floor(top_p * their sum));
+ * min_p (1 at most) drops what weighs less than min_p * 2^31.  With W the sum that is left
+ * and t = floor(u * W) (u and top_p cut to 31 bits), out_action[n] is the first
+ * index whose running sum, by index, exceeds t, and out_logp[n] = log(w / W), the
+ * logarithm of the probability it was drawn with.  temperature 0 takes the first
+ * of the largest logits, with out_logp 0.  A row that allows no action, that holds
+ * a NaN or +inf at an allowed place, or whose temperature is negative or NaN gets
+ * -1 and NaN.  uniform is taken as 0 below 0 and as the largest number below 1
+ * from 1 on. */
+pictura_status pictura_sample_actions(const pictura_logits* logits, const pictura_sampling* how, const float* uniform,
+                                      int64_t* out_action, float* out_logp, void* stream);
+
+/* The decisions a policy loss is taken over, device arrays of `rows` values
+ * (values with `values_stride` elements between them).  weights NULL: all 1.  A row
+ * with weight 0 or an action outside 0..actions - 1 (what pictura_sample_actions
+ * gives a row without actions) counts nothing: its numbers are not looked at and
+ * its gradients are 0. */
+typedef struct {
+    const float* values;
+    int64_t values_stride;
+    const int64_t* actions;
+    const float* old_logp;       /* log-probability the action was drawn with */
+    const float* advantages;
+    const float* returns;
+    const float* old_values;     /* read where value_clip > 0 */
+    const float* weights;
+    float temperature;           /* > 0: the one the actions were drawn with */
+    float clip;                  /* >= 0 */
+    float value_clip;            /* > 0: clipped value loss */
+    float value_coef, entropy_coef;
+    float denominator;           /* 0: the sum of the weights; else what sums are divided by */
+    int32_t normalize;           /* 1: advantages - mean over (standard deviation + 1e-8), weighted, over the rows */
+} pictura_policy_batch;
+
+#define PICTURA_POLICY_STATS 6   /* loss, policy loss, value loss, entropy, approximate KL, clipped fraction */
+
+/* Bytes of workspace pictura_policy_loss takes for this many rows. */
+pictura_status pictura_policy_loss_workspace(int64_t rows, int32_t actions, uint64_t* bytes);
+
+/* Clipped policy loss and its gradient.  Per row, with p the softmax of the allowed
+ * logits over temperature, H = -sum p log p, r = exp(log p[action] - old_logp), A the
+ * advantage, v the value, R the return:
+ *   policy = -min(r A, clamp(r, 1 - clip, 1 + clip) A)
+ *   value  = (v - R)^2 / 2; where value_clip > 0 and |v - old| > value_clip, that of
+ *            v clamped to old +- value_clip if it is larger (and then constant)
+ *   loss   = policy + value_coef value - entropy_coef H
+ * and the means of those over the rows, by weight, are out_stats[0..3]; [4] is the
+ * mean of (r - 1) - log r, [5] the weight of rows with r outside 1 +- clip.
+ * dlogits (the logits' type, dlogits_stride elements between rows) and dvalues
+ * [rows] receive the gradient of the mean loss; it is 0 at actions of probability
+ * zero.  If no row counts, all are 0.  Sums are taken in a fixed order.
+ * workspace: device memory, 256-byte aligned, in use until the call's work on the
+ * stream is done.  dlogits may be the logits' own memory (same stride).  EINVAL: a null or
+ * misaligned pointer, a value out of range, or a workspace too small. */
+pictura_status pictura_policy_loss(const pictura_logits* logits, const pictura_policy_batch* batch, void* workspace,
+                                   uint64_t workspace_bytes, float* out_stats, void* dlogits, int64_t dlogits_stride,
+                                   float* dvalues, void* stream);
+
+#define PICTURA_ADAMW_BLOCK 256   /* elements that share a scale of an 8-bit moment */
+
+/* One tensor of an optimizer step: n elements each, contiguous.  With 32 bits
+ * the moments are fp32 and the scales NULL.  With 8 bits exp_avg holds int8 codes
+ * c in -127..127 and exp_avg_sq uint8 codes, with one fp32 scale s for each block
+ * of PICTURA_ADAMW_BLOCK elements (the last one may be shorter): they stand for
+ * c |c| / 127^2 * s and (c / 255)^4 * s. */
+typedef struct {
+    void* param;
+    const void* grad;
+    void* exp_avg;
+    void* exp_avg_sq;
+    float* exp_avg_scale;
+    float* exp_avg_sq_scale;
+    int64_t n;
+    int32_t param_dtype;   /* PICTURA_F32, PICTURA_BF16 or PICTURA_F16 */
+    int32_t grad_dtype;
+} pictura_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;             /* this step's number, from 1 on */
+    int32_t bits;             /* of the moments: 32 or 8 */
+    const float* grad_factor; /* device: what gradients are multiplied by first, or NULL */
+} pictura_adamw;
+
+/* Bytes of workspace pictura_grad_norm takes for these tensors (reads n alone). */
+pictura_status pictura_grad_norm_workspace(const pictura_adamw_tensor* tensors, int32_t count, uint64_t* bytes);
+
+/* Norm of all gradients together: out[0] = sqrt(sum g^2), out[1] = min(1, max_norm /
+ * (out[0] + 1e-6)), the factor that clips them (a NaN norm gives NaN).  Squares are
+ * summed in fp64, in a fixed order.  out: two floats on the device. */
+pictura_status pictura_grad_norm(const pictura_adamw_tensor* tensors, int32_t count, float max_norm, void* workspace,
+                                 uint64_t workspace_bytes, float* out, void* stream);
+
+/* One AdamW step (weight decay apart from the gradient) of `count` tensors, fp32
+ * without contraction: g = grad * grad_factor, m = beta1 m + (1 - beta1) g,
+ * v = beta2 v + ((1 - beta2) g) g, param = param (1 - lr weight_decay)
+ * - lr / (1 - beta1^step) (m / (sqrt(v) / sqrt(1 - beta2^step) + eps)), rounded once to
+ * the parameter's type.  The factors are taken in fp64 and rounded.  With 8 bits
+ * the update uses m and v before they are cut: a block's scale is its largest
+ * magnitude (0 if that is below 2^-90), m's code the sign and rint(127 sqrt(|m| / s)),
+ * v's rint(255 (v / s)^(1/4)), at least 1 where v > 0.  A NaN makes its block's scale
+ * NaN.  EINVAL: a null pointer where n > 0, a pointer not aligned to its elements,
+ * n < 0, step < 1, betas outside [0, 1), or bits other than 32 and 8. */
+pictura_status pictura_adamw_step(const pictura_adamw* how, const pictura_adamw_tensor* tensors, int32_t count,
+                                  void* stream);
+
+/* What 8-bit moments stand for, in fp32: param and grad are not read; exp_avg_out[k]
+ * and exp_avg_sq_out[k] (host arrays of device pointers) receive tensor k's n values. */
+pictura_status pictura_adamw_moments(const pictura_adamw_tensor* tensors, int32_t count, float* const* exp_avg_out,
+                                     float* const* exp_avg_sq_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

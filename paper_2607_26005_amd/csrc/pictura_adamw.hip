@@ -1,0 +1,411 @@
+// AdamW over many tensors at once, with moments in fp32 or in 8 bits, and the
+// norm of all gradients together.
+//
+// The tensors' pointers travel in the kernel's arguments, kTensors to a launch,
+// so a step copies nothing to the device and can be captured in a graph.  A
+// workgroup takes kChunk elements of one tensor.
+#include <cmath>
+
+#include "pictura.h"
+#include "pictura_internal.h"
+
+#pragma clang fp contract(off)
+
+namespace pictura {
+
+constexpr int kTensors = 56;                     // of one launch: 56 * 64 B and the factors stay below 4 KB
+constexpr int kThreads = 256;
+constexpr int kChunk = 4096;                     // elements of one workgroup
+constexpr int kBlk = PICTURA_ADAMW_BLOCK;
+constexpr float kTiny = 0x1p-90f;                // below it a block's moments count as zero: 1 / scale stays finite
+static_assert(kChunk % kBlk == 0, "blocks do not straddle workgroups");
+
+struct TensorArg {
+    void* param;
+    const void* grad;
+    void* m;
+    void* v;
+    float* ms;
+    float* vs;
+    int64_t n;
+    int32_t first;      // workgroup of its first chunk
+    uint8_t pt, gt;     // PICTURA_F32 ..
+};
+
+struct TensorArgs {
+    TensorArg t[kTensors];
+    int32_t count;
+};
+
+struct StepFactors {
+    float b1, c1, b2, c2, rbc2, eps, keep, rate;
+    const float* grad_factor;
+};
+
+// Tensor of workgroup b: the last whose first workgroup is not beyond b.
+__device__ __forceinline__ int tensor_of(const TensorArgs& a, int b)
+{
+    int lo = 0, hi = a.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.t[mid].first <= b) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ float load_as(const void* p, int type, int64_t i)
+{
+    if (type == PICTURA_F32) return ((const float*)p)[i];
+    if (type == PICTURA_BF16) return (float)((const __bf16*)p)[i];
+    return (float)((const _Float16*)p)[i];
+}
+
+__device__ __forceinline__ void store_as(void* p, int type, int64_t i, float x)
+{
+    if (type == PICTURA_F32) ((float*)p)[i] = x;
+    else if (type == PICTURA_BF16) ((__bf16*)p)[i] = (__bf16)x;
+    else ((_Float16*)p)[i] = (_Float16)x;
+}
+
+// m and v after the gradient g, and the parameter.
+__device__ __forceinline__ float adamw(const StepFactors& f, float p, float g, float& m, float& v)
+{
+    m = f.b1 * m + f.c1 * g;
+    v = f.b2 * v + (f.c2 * g) * g;
+    const float den = sqrtf(v) * f.rbc2 + f.eps;
+    return p * f.keep - f.rate * (m / den);
+}
+
+// c |c| and c^2 are whole numbers below 2^24: a value takes three roundings (four
+// for v), and those of the scale are shared by its block.
+__device__ __forceinline__ float m_unit(float s) { return s * (float)(1.0 / 16129.0); }
+
+__device__ __forceinline__ float v_unit(float s) { return s * (float)(1.0 / 4228250625.0); }
+
+__device__ __forceinline__ float m_value(int c, float unit)
+{
+    const float x = (float)c;
+    return x * fabsf(x) * unit;
+}
+
+__device__ __forceinline__ float v_value(uint32_t c, float unit)
+{
+    const float x = (float)c, x2 = x * x;
+    return x2 * x2 * unit;
+}
+
+// The codes of m and v, with inv = 1 / scale (0 for a scale of zero or NaN; a
+// NaN comes out as 0: its scale says it).
+__device__ __forceinline__ int m_code(float m, float inv)
+{
+    const float q = fminf(fmaxf(rintf(sqrtf(fabsf(m) * inv) * 127.0f), 0.0f), 127.0f);
+    return m < 0.0f ? -(int)q : (int)q;
+}
+
+__device__ __forceinline__ uint32_t v_code(float v, float inv)
+{
+    float q = fminf(fmaxf(rintf(sqrtf(sqrtf(v * inv)) * 255.0f), 0.0f), 255.0f);
+    if (v > 0.0f && inv > 0.0f) q = fmaxf(q, 1.0f);
+    return (uint32_t)q;
+}
+
+__global__ __launch_bounds__(kThreads) void adamw32_kernel(const TensorArgs a, const StepFactors f)
+{
+    const TensorArg& t = a.t[tensor_of(a, (int)blockIdx.x)];
+    const float gf = f.grad_factor ? *f.grad_factor : 1.0f;
+    const int64_t at = (int64_t)((int)blockIdx.x - t.first) * kChunk;
+    const int n = (int)min((int64_t)kChunk, t.n - at);
+    float* m = (float*)t.m + at;
+    float* v = (float*)t.v + at;
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        float mi = m[i], vi = v[i];
+        const float p = adamw(f, load_as(t.param, t.pt, at + i), load_as(t.grad, t.gt, at + i) * gf, mi, vi);
+        m[i] = mi;
+        v[i] = vi;
+        store_as(t.param, t.pt, at + i, p);
+    }
+}
+
+// A wave takes a block of 256 elements, four to a lane.
+__global__ __launch_bounds__(kThreads) void adamw8_kernel(const TensorArgs a, const StepFactors f)
+{
+    const TensorArg& t = a.t[tensor_of(a, (int)blockIdx.x)];
+    const float gf = f.grad_factor ? *f.grad_factor : 1.0f;
+    const int64_t at = (int64_t)((int)blockIdx.x - t.first) * kChunk;
+    const int lane = threadIdx.x & 63;
+    for (int b = threadIdx.x >> 6; b < kChunk / kBlk; b += kThreads / 64) {
+        const int64_t i0 = at + (int64_t)b * kBlk;
+        if (i0 >= t.n) break;
+        const int n = (int)min((int64_t)kBlk, t.n - i0);
+        const float ms = m_unit(t.ms[i0 / kBlk]), vs = v_unit(t.vs[i0 / kBlk]);
+        int8_t* cm = (int8_t*)t.m + i0;
+        uint8_t* cv = (uint8_t*)t.v + i0;
+        float m[4], v[4];
+        // largest magnitudes by their bits: a NaN is larger than any number
+        uint32_t mm = 0, vm = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = lane + 64 * k;
+            m[k] = v[k] = 0.0f;
+            if (i < n) {
+                m[k] = m_value(cm[i], ms);
+                v[k] = v_value(cv[i], vs);
+                const float p = adamw(f, load_as(t.param, t.pt, i0 + i), load_as(t.grad, t.gt, i0 + i) * gf, m[k], v[k]);
+                store_as(t.param, t.pt, i0 + i, p);
+            }
+            mm = max(mm, __float_as_uint(fabsf(m[k])));
+            vm = max(vm, __float_as_uint(fabsf(v[k])));
+        }
+        for (int d = 32; d; d >>= 1) {
+            mm = max(mm, (uint32_t)__shfl_xor((int)mm, d));
+            vm = max(vm, (uint32_t)__shfl_xor((int)vm, d));
+        }
+        float nms = __uint_as_float(mm), nvs = __uint_as_float(vm);
+        if (nms < kTiny) nms = 0.0f;
+        if (nvs < kTiny) nvs = 0.0f;
+        const float im = nms > 0.0f ? 1.0f / nms : 0.0f, iv = nvs > 0.0f ? 1.0f / nvs : 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = lane + 64 * k;
+            if (i < n) {
+                cm[i] = (int8_t)m_code(m[k], im);
+                cv[i] = (uint8_t)v_code(v[k], iv);
+            }
+        }
+        if (lane == 0) {
+            t.ms[i0 / kBlk] = nms;
+            t.vs[i0 / kBlk] = nvs;
+        }
+    }
+}
+
+// What 8-bit moments stand for: param and grad hold the fp32 outputs.
+__global__ __launch_bounds__(kThreads) void moments_kernel(const TensorArgs a)
+{
+    const TensorArg& t = a.t[tensor_of(a, (int)blockIdx.x)];
+    const int64_t at = (int64_t)((int)blockIdx.x - t.first) * kChunk;
+    const int n = (int)min((int64_t)kChunk, t.n - at);
+    for (int j = threadIdx.x; j < n; j += kThreads) {
+        const int64_t i = at + j;
+        ((float*)t.param)[i] = m_value(((const int8_t*)t.m)[i], m_unit(t.ms[i / kBlk]));
+        ((float*)t.grad)[i] = v_value(((const uint8_t*)t.v)[i], v_unit(t.vs[i / kBlk]));
+    }
+}
+
+// Sum of a workgroup's values, in a fixed order.
+__device__ __forceinline__ double block_sum(double x, double* lds)
+{
+    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0.0;
+    for (int w = 0; w < kThreads / 64; ++w) x += lds[w];
+    return x;
+}
+
+__global__ __launch_bounds__(kThreads) void norm_part_kernel(const TensorArgs a, double* __restrict__ part)
+{
+    __shared__ double lds[kThreads / 64];
+    const TensorArg& t = a.t[tensor_of(a, (int)blockIdx.x)];
+    const int64_t at = (int64_t)((int)blockIdx.x - t.first) * kChunk;
+    const int n = (int)min((int64_t)kChunk, t.n - at);
+    double s = 0.0;
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        const double g = (double)load_as(t.grad, t.gt, at + i);
+        s = fma(g, g, s);
+    }
+    s = block_sum(s, lds);
+    if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(kThreads) void norm_kernel(const double* __restrict__ part, int64_t n, float max_norm,
+                                                        float* __restrict__ out)
+{
+    __shared__ double lds[kThreads / 64];
+    double s = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += kThreads) s += part[i];
+    s = block_sum(s, lds);
+    if (threadIdx.x == 0) {
+        const float norm = (float)sqrt(s);
+        const float c = max_norm / (norm + 1e-6f);
+        out[0] = norm;
+        out[1] = c > 1.0f ? 1.0f : c;
+    }
+}
+
+namespace {
+
+int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
+
+size_t size_of(int type) { return type == PICTURA_F32 ? 4 : 2; }
+
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+bool dtype_ok(int32_t t) { return t == PICTURA_F32 || t == PICTURA_BF16 || t == PICTURA_F16; }
+
+// Split the tensors over launches of at most kTensors tensors and 2^22
+// workgroups; a tensor beyond that is taken in parts.  launch(args, blocks).
+template <class Fill, class Launch>
+void for_launches(const pictura_adamw_tensor* ts, int32_t count, Fill fill, Launch launch)
+{
+    constexpr int64_t kMostBlocks = 1 << 22;
+    TensorArgs a;
+    a.count = 0;
+    int64_t blocks = 0;
+    auto flush = [&] {
+        if (a.count) launch(a, (unsigned)blocks);
+        a.count = 0;
+        blocks = 0;
+    };
+    for (int32_t k = 0; k < count; ++k) {
+        int64_t at = 0;
+        while (at < ts[k].n) {
+            const int64_t left = chunks_of(ts[k].n - at), room = kMostBlocks - blocks;
+            const int64_t take = left < room ? left : room;
+            TensorArg& t = a.t[a.count];
+            t.n = ts[k].n - at < take * kChunk ? ts[k].n - at : take * kChunk;
+            t.first = (int32_t)blocks;
+            fill(t, k, at);
+            ++a.count;
+            blocks += take;
+            at += take * kChunk;
+            if (a.count == kTensors || blocks == kMostBlocks) flush();
+        }
+    }
+    flush();
+}
+
+void fill_common(TensorArg& t, const pictura_adamw_tensor& s, int64_t at, int bits)
+{
+    t.param = (char*)s.param + at * size_of(s.param_dtype);
+    t.grad = (const char*)s.grad + at * size_of(s.grad_dtype);
+    const size_t b = bits == 8 ? 1 : 4;
+    t.m = (char*)s.exp_avg + at * b;
+    t.v = (char*)s.exp_avg_sq + at * b;
+    t.ms = bits == 8 ? s.exp_avg_scale + at / kBlk : nullptr;
+    t.vs = bits == 8 ? s.exp_avg_sq_scale + at / kBlk : nullptr;
+    t.pt = (uint8_t)s.param_dtype;
+    t.gt = (uint8_t)s.grad_dtype;
+}
+
+constexpr int64_t kMostElements = 1ll << 48;
+
+bool moments_ok(const pictura_adamw_tensor& t, int bits)
+{
+    if (!t.exp_avg || !t.exp_avg_sq) return false;
+    if (bits == 32) return aligned(t.exp_avg, 4) && aligned(t.exp_avg_sq, 4);
+    return t.exp_avg_scale && t.exp_avg_sq_scale && aligned(t.exp_avg_scale, 4) && aligned(t.exp_avg_sq_scale, 4);
+}
+
+bool grads_ok(const pictura_adamw_tensor* ts, int32_t count)
+{
+    if (count < 0 || (count > 0 && !ts)) return false;
+    for (int32_t k = 0; k < count; ++k) {
+        const pictura_adamw_tensor& t = ts[k];
+        if (t.n < 0 || t.n > kMostElements || !dtype_ok(t.grad_dtype)) return false;
+        if (t.n > 0 && (!t.grad || !aligned(t.grad, size_of(t.grad_dtype)))) return false;
+    }
+    return true;
+}
+
+pictura_status launched() { return hipGetLastError() == hipSuccess ? PICTURA_OK : PICTURA_EDEVICE; }
+
+}  // namespace
+}  // namespace pictura
+
+using namespace pictura;
+
+extern "C" {
+
+pictura_status pictura_grad_norm_workspace(const pictura_adamw_tensor* tensors, int32_t count, uint64_t* bytes)
+{
+    if (!bytes || count < 0 || (count > 0 && !tensors)) return PICTURA_EINVAL;
+    int64_t n = 0;
+    for (int32_t k = 0; k < count; ++k) {
+        if (tensors[k].n < 0 || tensors[k].n > kMostElements) return PICTURA_EINVAL;
+        n += chunks_of(tensors[k].n);
+    }
+    *bytes = (uint64_t)(n > 0 ? n : 1) * sizeof(double);
+    return PICTURA_OK;
+}
+
+pictura_status pictura_grad_norm(const pictura_adamw_tensor* tensors, int32_t count, float max_norm, void* workspace,
+                                 uint64_t workspace_bytes, float* out, void* stream)
+{
+    if (!grads_ok(tensors, count) || !out || !workspace || !aligned(out, 4) || !aligned(workspace, 256)) return PICTURA_EINVAL;
+    if (!(max_norm >= 0.0f)) return PICTURA_EINVAL;
+    uint64_t need = 0;
+    pictura_status st = pictura_grad_norm_workspace(tensors, count, &need);
+    if (st != PICTURA_OK) return st;
+    if (workspace_bytes < need) return PICTURA_EINVAL;
+    hipStream_t s = (hipStream_t)stream;
+    double* part = (double*)workspace;
+    int64_t n = 0;
+    for_launches(
+        tensors, count,
+        [&](TensorArg& t, int32_t k, int64_t at) {
+            t.grad = (const char*)tensors[k].grad + at * size_of(tensors[k].grad_dtype);
+            t.gt = (uint8_t)tensors[k].grad_dtype;
+        },
+        [&](const TensorArgs& a, unsigned blocks) {
+            hipLaunchKernelGGL(norm_part_kernel, dim3(blocks), dim3(kThreads), 0, s, a, part + n);
+            n += blocks;
+        });
+    hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, s, part, n, max_norm, out);
+    return launched();
+}
+
+pictura_status pictura_adamw_step(const pictura_adamw* how, const pictura_adamw_tensor* tensors, int32_t count,
+                                  void* stream)
+{
+    if (!how || !grads_ok(tensors, count)) return PICTURA_EINVAL;
+    if (how->bits != 32 && how->bits != 8) return PICTURA_EINVAL;
+    if (!(how->beta1 >= 0.0 && how->beta1 < 1.0 && how->beta2 >= 0.0 && how->beta2 < 1.0) || how->step < 1) return PICTURA_EINVAL;
+    if (!std::isfinite(how->lr) || !(how->eps >= 0.0) || !std::isfinite(how->weight_decay)) return PICTURA_EINVAL;
+    for (int32_t k = 0; k < count; ++k) {
+        const pictura_adamw_tensor& t = tensors[k];
+        if (!dtype_ok(t.param_dtype)) return PICTURA_EINVAL;
+        if (t.n > 0 && (!t.param || !aligned(t.param, size_of(t.param_dtype)) || !moments_ok(t, how->bits)))
+            return PICTURA_EINVAL;
+    }
+    hipStream_t s = (hipStream_t)stream;
+    const double bc1 = 1.0 - std::pow(how->beta1, (double)how->step), bc2 = 1.0 - std::pow(how->beta2, (double)how->step);
+    const StepFactors f{(float)how->beta1, (float)(1.0 - how->beta1), (float)how->beta2, (float)(1.0 - how->beta2),
+                        (float)(1.0 / std::sqrt(bc2)), (float)how->eps, (float)(1.0 - how->lr * how->weight_decay),
+                        (float)(how->lr / bc1), how->grad_factor};
+    for_launches(
+        tensors, count, [&](TensorArg& t, int32_t k, int64_t at) { fill_common(t, tensors[k], at, how->bits); },
+        [&](const TensorArgs& a, unsigned blocks) {
+            if (how->bits == 32) hipLaunchKernelGGL(adamw32_kernel, dim3(blocks), dim3(kThreads), 0, s, a, f);
+            else hipLaunchKernelGGL(adamw8_kernel, dim3(blocks), dim3(kThreads), 0, s, a, f);
+        });
+    return launched();
+}
+
+pictura_status pictura_adamw_moments(const pictura_adamw_tensor* tensors, int32_t count, float* const* exp_avg_out,
+                                     float* const* exp_avg_sq_out, void* stream)
+{
+    if (count < 0 || (count > 0 && (!tensors || !exp_avg_out || !exp_avg_sq_out))) return PICTURA_EINVAL;
+    for (int32_t k = 0; k < count; ++k) {
+        const pictura_adamw_tensor& t = tensors[k];
+        if (t.n < 0 || t.n > kMostElements) return PICTURA_EINVAL;
+        if (t.n > 0 && (!moments_ok(t, 8) || !exp_avg_out[k] || !exp_avg_sq_out[k] || !aligned(exp_avg_out[k], 4) ||
+                        !aligned(exp_avg_sq_out[k], 4)))
+            return PICTURA_EINVAL;
+    }
+    hipStream_t s = (hipStream_t)stream;
+    for_launches(
+        tensors, count,
+        [&](TensorArg& t, int32_t k, int64_t at) {
+            fill_common(t, tensors[k], at, 8);
+            t.param = exp_avg_out[k] + at;
+            t.grad = exp_avg_sq_out[k] + at;
+        },
+        [&](const TensorArgs& a, unsigned blocks) {
+            hipLaunchKernelGGL(moments_kernel, dim3(blocks), dim3(kThreads), 0, s, a);
+        });
+    return launched();
+}
+
+}  // extern "C"

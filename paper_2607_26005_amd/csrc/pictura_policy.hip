@@ -1,0 +1,599 @@
+// The policy's decisions: actions drawn from logits, and the clipped policy loss
+// over them with its gradient.
+#include <cmath>
+
+#include "pictura.h"
+#include "pictura_internal.h"
+
+#pragma clang fp contract(off)
+
+namespace pictura {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr float kOne = 0x1p31f;           // weight of a row's largest logit
+constexpr int kMaxBlocks = 1 << 20;       // workgroups of a launch, which then take rows in turn
+
+struct Rows {
+    const void* data;
+    int64_t stride;
+    const uint8_t* mask;
+    int64_t mask_stride;
+    int64_t rows;
+    int32_t actions;
+};
+
+struct Sampling {
+    float temperature, top_p, min_p;
+    int32_t top_k;
+    const float* temperatures;
+    const float* top_ps;
+    const float* min_ps;
+    const int32_t* top_ks;
+};
+
+// One row as the kernels read it: fp32, -inf at a place that is not allowed, and
+// no negative zero (the order by bits is then that of the values).
+template <class T>
+struct Row {
+    const T* x;
+    const uint8_t* mask;
+    __device__ __forceinline__ Row(const Rows& r, int64_t n)
+        : x((const T*)r.data + n * r.stride), mask(r.mask ? r.mask + n * r.mask_stride : nullptr) {}
+    __device__ __forceinline__ float operator()(int i) const
+    {
+        return mask && !mask[i] ? -INFINITY : (float)x[i] + 0.0f;
+    }
+};
+
+// Bits in the order of the values.
+__device__ __forceinline__ uint32_t order_key(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__device__ __forceinline__ float key_value(uint32_t k)
+{
+    return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
+}
+
+// Weight of a logit against the row's largest.
+__device__ __forceinline__ uint32_t weight_of(float x, float top, float temp)
+{
+    if (x == -INFINITY) return 0;
+    return (uint32_t)rintf(expf((x - top) / temp) * kOne);
+}
+
+// floor(total * m / 2^31) for m < 2^31
+__device__ __forceinline__ uint64_t share(uint64_t total, uint32_t m)
+{
+    return (total >> 32) * m * 2 + ((total & 0xFFFFFFFFull) * m >> 31);
+}
+
+// floor(2^31 x) of x cut to [0, 1)
+__device__ __forceinline__ uint32_t cut31(float x)
+{
+    return (uint32_t)(fminf(fmaxf(x, 0.0f), 1.0f - 0x1p-24f) * kOne);
+}
+
+template <class V>
+__device__ __forceinline__ V wave_sum(V x)
+{
+    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+    return x;
+}
+
+// Sum over the workgroup, the same in every thread; lds[kWaves] is free again after
+// the next barrier.
+template <class V>
+__device__ __forceinline__ V block_sum(V x, V* lds)
+{
+    x = wave_sum(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = lds[0];
+    for (int w = 1; w < kWaves; ++w) x += lds[w];
+    return x;
+}
+
+__device__ __forceinline__ float block_max(float x, float* lds)
+{
+    for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = lds[0];
+    for (int w = 1; w < kWaves; ++w) x = fmaxf(x, lds[w]);
+    return x;
+}
+
+// A prefix of the actions ordered by logit, then index: everything above `key`
+// and the first `ties` of those with it.
+struct Cut {
+    uint32_t key;
+    uint32_t ties;
+};
+
+// The shortest prefix whose sum of add(key) reaches `need` > 0, of the actions
+// above `floor_key`; `need` is at most the sum of all of those.  Most significant
+// byte first: a histogram of the sums by byte, from the largest byte down to where
+// `need` is reached.
+template <class T, class Add>
+__device__ Cut find_cut(const Row<T>& row, int A, uint32_t floor_key, uint64_t need, Add add, unsigned long long* hist,
+                        uint64_t* told)
+{
+    uint32_t prefix = 0;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        hist[threadIdx.x] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < A; i += kThreads) {
+            const float x = row(i);
+            const uint32_t k = order_key(x);
+            if (x == -INFINITY || k <= floor_key || (shift < 24 && (k >> (shift + 8)) != prefix)) continue;
+            atomicAdd(&hist[(k >> shift) & 255u], (unsigned long long)add(x));
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            uint64_t sum = 0;
+            int b = 255;
+            for (; b > 0 && sum + hist[b] < need; --b) sum += hist[b];
+            told[0] = (uint64_t)b;
+            told[1] = need - sum;
+        }
+        __syncthreads();
+        prefix = prefix << 8 | (uint32_t)told[0];
+        need = told[1];
+        __syncthreads();
+    }
+    const uint64_t one = add(key_value(prefix));
+    return Cut{prefix, (uint32_t)((need + one - 1) / one)};
+}
+
+// One workgroup per row, the row read again for every pass.
+template <class T>
+__global__ __launch_bounds__(kThreads) void sample_kernel(const Rows R, const Sampling S,
+                                                          const float* __restrict__ uniform,
+                                                          int64_t* __restrict__ out_action, float* __restrict__ out_logp)
+{
+    __shared__ unsigned long long hist[256];
+    __shared__ uint64_t told[2], lds64[kWaves];
+    __shared__ float ldsf[kWaves];
+    __shared__ uint32_t wties[kWaves];
+    const int A = R.actions;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int64_t n = blockIdx.x; n < R.rows; n += gridDim.x) {
+        const Row<T> row(R, n);
+        const float temp = S.temperatures ? S.temperatures[n] : S.temperature;
+        const int32_t k = S.top_ks ? S.top_ks[n] : S.top_k;
+        const float top_p = S.top_ps ? S.top_ps[n] : S.top_p, min_p = S.min_ps ? S.min_ps[n] : S.min_p;
+        // the largest logit; a NaN or +inf, or a temperature without meaning, makes no draw
+        float top = -INFINITY, bad = temp >= 0.0f ? 0.0f : 1.0f;
+        for (int i = threadIdx.x; i < A; i += kThreads) {
+            const float x = row(i);
+            top = fmaxf(top, x);
+            if (!(x < INFINITY)) bad = 1.0f;
+        }
+        top = block_max(top, ldsf);
+        bad = block_max(bad, ldsf);
+        if (bad != 0.0f || top == -INFINITY) {
+            if (threadIdx.x == 0) {
+                out_action[n] = -1;
+                out_logp[n] = NAN;
+            }
+            continue;
+        }
+        auto weight = [&](float x) { return temp > 0.0f ? weight_of(x, top, temp) : x == top ? 1u : 0u; };
+        Cut cut{0u, 0u};
+        if (temp == 0.0f) {
+            cut = Cut{order_key(top), 1u};
+        } else {
+            if (k > 0 && k < A) {
+                uint32_t some = 0;
+                for (int i = threadIdx.x; i < A; i += kThreads) some += row(i) != -INFINITY;
+                if (block_sum((uint64_t)some, lds64) > (uint64_t)k)
+                    cut = find_cut(row, A, 0u, (uint64_t)k, [](float) { return 1u; }, hist, told);
+            }
+            if (top_p < 1.0f) {
+                uint64_t above = 0;
+                for (int i = threadIdx.x; i < A; i += kThreads) {
+                    const float x = row(i);
+                    if (order_key(x) > cut.key) above += weight(x);
+                }
+                above = block_sum(above, lds64);
+                const uint64_t one = cut.ties ? weight(key_value(cut.key)) : 0;
+                uint64_t need = share(above + one * cut.ties, cut31(top_p));
+                if (need < 1) need = 1;
+                if (need <= above) cut = find_cut(row, A, cut.key, need, weight, hist, told);
+                else cut.ties = (uint32_t)((need - above + one - 1) / one);
+            }
+        }
+        const uint32_t least = temp > 0.0f ? (uint32_t)ceilf(fminf(fmaxf(min_p, 0.0f), 1.0f) * kOne) : 0u;
+        auto kept = [&](float x) {
+            const uint32_t w = weight(x);
+            return w < least ? 0u : w;
+        };
+        // each wave its part of the row; the ties belong to the first waves that have them
+        const int per = ((A + kThreads - 1) / kThreads) * 64, i0 = min(A, wave * per), i1 = min(A, i0 + per);
+        uint64_t sum = 0;
+        uint32_t ties = 0;
+        for (int i = i0 + lane; i < i1; i += 64) {
+            const float x = row(i);
+            const uint32_t key = order_key(x);
+            if (x == -INFINITY) continue;
+            if (key > cut.key) sum += kept(x);
+            ties += key == cut.key;
+        }
+        sum = wave_sum(sum);
+        ties = wave_sum(ties);
+        const uint32_t one = cut.ties ? kept(key_value(cut.key)) : 0u;
+        __syncthreads();
+        if (lane == 0) {
+            lds64[wave] = sum;
+            wties[wave] = ties;
+        }
+        __syncthreads();
+        uint64_t total = 0;
+        uint32_t quota = cut.ties;
+        uint64_t wsum[kWaves];
+        uint32_t wquota[kWaves];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            wquota[w] = min(quota, wties[w]);
+            quota -= wquota[w];
+            wsum[w] = lds64[w] + (uint64_t)wquota[w] * one;
+            total += wsum[w];
+        }
+        const uint64_t target = share(total, cut31(uniform[n]));
+        // the wave whose part holds the target walks through it
+        uint64_t base = 0;
+        uint32_t left = 0;
+        bool mine = false;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w == wave) {
+                mine = base <= target && target < base + wsum[w];
+                left = wquota[w];
+                if (mine) break;
+            }
+            base += wsum[w];
+        }
+        if (mine) {
+            for (int b = i0; b < i1; b += 64) {
+                const int i = b + lane;
+                const float x = i < i1 ? row(i) : -INFINITY;
+                const uint32_t key = order_key(x);
+                const bool tie = x != -INFINITY && key == cut.key;
+                const uint64_t same = __ballot(tie);
+                const uint32_t before = __popcll(same & ((1ull << lane) - 1ull));
+                const uint32_t w = x == -INFINITY ? 0u : key > cut.key || (tie && before < left) ? kept(x) : 0u;
+                uint64_t run = w;
+                for (int d = 1; d < 64; d <<= 1) {
+                    const uint64_t o = __shfl_up(run, d);
+                    if (lane >= d) run += o;
+                }
+                const uint64_t hit = __ballot(base + run > target);
+                if (hit) {
+                    if (lane == __ffsll((unsigned long long)hit) - 1) {
+                        out_action[n] = i;
+                        out_logp[n] = logf((float)w / (float)total);
+                    }
+                    break;
+                }
+                base += __shfl(run, 63);
+                left -= min(left, (uint32_t)__popcll(same));
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------
+// policy loss
+// ---------------------------------------------------------------------------
+
+struct Batch {
+    const float* values;
+    int64_t values_stride;
+    const int64_t* actions;
+    const float* old_logp;
+    const float* advantages;
+    const float* returns;
+    const float* old_values;
+    const float* weights;
+    float temperature, clip, value_clip, value_coef, entropy_coef, denominator;
+    int32_t normalize;
+    float* stats;
+    void* dlogits;
+    int64_t dstride;
+    float* dvalues;
+};
+
+constexpr int kMomentBlocks = 128;      // partial sums of the weights and advantages
+constexpr int kSums = 5;                // sums over the rows: policy, value, entropy, KL, clipped
+
+__device__ __forceinline__ double block_sum_d(double x, double* lds)
+{
+    return block_sum(x, lds);
+}
+
+// Weight of row n, 0 where it does not count.
+__device__ __forceinline__ float row_weight(const Batch& b, int64_t n, int32_t A)
+{
+    const int64_t a = b.actions[n];
+    if (a < 0 || a >= A) return 0.0f;
+    return b.weights ? b.weights[n] : 1.0f;
+}
+
+// Sums of the weights, and of the advantages and their squares by weight.
+__global__ __launch_bounds__(kThreads) void loss_moments_kernel(const Batch b, int64_t rows, int32_t A, double* __restrict__ part)
+{
+    __shared__ double lds[kWaves];
+    double w0 = 0.0, w1 = 0.0, w2 = 0.0;
+    for (int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x; n < rows; n += (int64_t)kMomentBlocks * kThreads) {
+        const double w = (double)row_weight(b, n, A);
+        if (w == 0.0) continue;
+        const double a = (double)b.advantages[n];
+        w0 += w;
+        w1 += w * a;
+        w2 += w * a * a;
+    }
+    w0 = block_sum_d(w0, lds);
+    w1 = block_sum_d(w1, lds);
+    w2 = block_sum_d(w2, lds);
+    if (threadIdx.x == 0) {
+        part[blockIdx.x * 3] = w0;
+        part[blockIdx.x * 3 + 1] = w1;
+        part[blockIdx.x * 3 + 2] = w2;
+    }
+}
+
+// What all rows share: 1 / denominator, mean of the advantages, 1 / deviation.
+struct Shared3 {
+    float inv, mean, rstd;
+};
+
+__device__ __forceinline__ Shared3 loss_shared(const Batch& b, const double* __restrict__ part, double* lds)
+{
+    double s[3];
+    for (int k = 0; k < 3; ++k) {
+        double x = 0.0;
+        for (int i = threadIdx.x; i < kMomentBlocks; i += kThreads) x += part[i * 3 + k];
+        s[k] = block_sum_d(x, lds);
+    }
+    Shared3 o;
+    const double den = b.denominator != 0.0f ? (double)b.denominator : s[0];
+    o.inv = s[0] != 0.0 ? (float)(1.0 / den) : 0.0f;
+    o.mean = 0.0f;
+    o.rstd = 1.0f;
+    if (b.normalize && s[0] != 0.0) {
+        const double mean = s[1] / s[0], var = s[2] / s[0] - mean * mean;
+        o.mean = (float)mean;
+        o.rstd = (float)(1.0 / (sqrt(var > 0.0 ? var : 0.0) + 1e-8));
+    }
+    return o;
+}
+
+// The terms of one row, given its log-probability and entropy: d loss / d log p[action]
+// and d loss / d v before weights, and what goes into the sums.
+struct RowTerms {
+    float g, dv, sums[kSums];
+};
+
+__device__ __forceinline__ RowTerms row_terms(const Batch& b, const Shared3& s, int64_t n, float logp, float entropy)
+{
+    RowTerms o;
+    const float adv = (b.advantages[n] - s.mean) * s.rstd;
+    const float diff = logp - b.old_logp[n];
+    const float r = expf(diff);
+    const float lo = 1.0f - b.clip, hi = 1.0f + b.clip;
+    const float un = r * adv, cl = fminf(fmaxf(r, lo), hi) * adv;
+    // (written so that a NaN stays one)
+    o.sums[0] = un <= cl ? -un : cl < un ? -cl : un + cl;
+    o.g = un <= cl ? -un : cl < un ? 0.0f : un + cl;
+    const float v = b.values[n * b.values_stride], R = b.returns[n];
+    float err = v - R, dv = err;
+    if (b.value_clip > 0.0f) {
+        const float old = b.old_values[n], move = v - old;
+        const float far = old + fminf(fmaxf(move, -b.value_clip), b.value_clip) - R;
+        if (fabsf(move) > b.value_clip && fabsf(far) > fabsf(err)) {
+            err = far;
+            dv = 0.0f;
+        }
+    }
+    o.dv = b.value_coef * dv;
+    o.sums[1] = 0.5f * err * err;
+    o.sums[2] = entropy;
+    o.sums[3] = expm1f(diff) - diff;
+    o.sums[4] = r < lo || r > hi ? 1.0f : 0.0f;
+    return o;
+}
+
+// One workgroup per row, the row read again for every pass.
+template <class T>
+__global__ __launch_bounds__(kThreads) void loss_kernel(const Rows R, const Batch b, const double* __restrict__ part,
+                                                        double* __restrict__ sums)
+{
+    __shared__ double ldsd[kWaves];
+    __shared__ float ldsf[kWaves];
+    const Shared3 s = loss_shared(b, part, ldsd);
+    const int A = R.actions;
+    double acc[kSums] = {};
+    for (int64_t n = blockIdx.x; n < R.rows; n += gridDim.x) {
+        const Row<T> row(R, n);
+        T* out = (T*)b.dlogits + n * b.dstride;
+        const float w = row_weight(b, n, A);
+        if (w == 0.0f) {
+            for (int i = threadIdx.x; i < A; i += kThreads) out[i] = (T)0.0f;
+            if (threadIdx.x == 0) b.dvalues[n] = 0.0f;
+            continue;
+        }
+        const int a = (int)b.actions[n];
+        float top = -INFINITY, xa = 0.0f;
+        for (int i = threadIdx.x; i < A; i += kThreads) {
+            const float x = row(i);
+            top = x > top || x != x ? x : top;
+        }
+        xa = row(a);
+        top = block_max(top, ldsf);
+        const float rt = b.temperature;
+        // d = (x - top) / T, sum of e = exp d, and of e d
+        auto dist = [&](float x) { return x == -INFINITY ? -INFINITY : (x - top) / rt; };
+        float e0 = 0.0f, e1 = 0.0f;
+        for (int i = threadIdx.x; i < A; i += kThreads) {
+            const float d = dist(row(i)), e = expf(d);
+            e0 += e;
+            if (e != 0.0f) e1 += e * d;
+        }
+        e0 = block_sum(e0, ldsf);
+        e1 = block_sum(e1, ldsf);
+        const float logs = logf(e0), rs = 1.0f / e0;
+        const float H = e0 > 0.0f ? logs - e1 * rs : e0 == 0.0f ? 0.0f : e0;
+        const float logp = e0 == 0.0f ? -INFINITY : dist(xa) - logs;
+        const RowTerms t = row_terms(b, s, n, logp, H);
+        const float scale = w * s.inv;
+        const float ce = b.entropy_coef;
+        for (int i = threadIdx.x; i < A; i += kThreads) {
+            const float d = dist(row(i)), e = expf(d), p = e * rs;
+            float y = e != 0.0f ? p * (ce * (d - logs + H) - t.g) : 0.0f;
+            if (i == a) y += t.g;
+            out[i] = (T)(y * scale / rt);
+        }
+        if (threadIdx.x == 0) {
+            b.dvalues[n] = t.dv * scale;
+            for (int k = 0; k < kSums; ++k) acc[k] += (double)w * (double)t.sums[k];
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x == 0)
+        for (int k = 0; k < kSums; ++k) sums[(int64_t)blockIdx.x * kSums + k] = acc[k];
+}
+
+__global__ __launch_bounds__(kThreads) void loss_stats_kernel(const Batch b, const double* __restrict__ part,
+                                                              const double* __restrict__ sums, int64_t blocks)
+{
+    __shared__ double lds[kWaves];
+    const Shared3 s = loss_shared(b, part, lds);
+    double x[kSums];
+    for (int k = 0; k < kSums; ++k) {
+        x[k] = 0.0;
+        for (int64_t i = threadIdx.x; i < blocks; i += kThreads) x[k] += sums[i * kSums + k];
+        x[k] = block_sum_d(x[k], lds) * (double)s.inv;
+    }
+    if (threadIdx.x == 0) {
+        b.stats[0] = (float)(x[0] + (double)b.value_coef * x[1] - (double)b.entropy_coef * x[2]);
+        for (int k = 0; k < kSums; ++k) b.stats[k + 1] = (float)x[k];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+
+namespace {
+
+size_t size_of(int32_t t) { return t == PICTURA_F32 ? 4 : 2; }
+
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+bool logits_ok(const pictura_logits* l)
+{
+    if (!l || (l->dtype != PICTURA_F32 && l->dtype != PICTURA_BF16 && l->dtype != PICTURA_F16)) return false;
+    if (l->actions < 1 || l->actions > PICTURA_MAX_ACTIONS || l->rows < 0 || l->rows > 0x7FFFFFFFll) return false;
+    if (l->rows == 0) return true;
+    if (l->stride < l->actions && l->rows > 1) return false;
+    if (l->mask && l->mask_stride != 0 && l->mask_stride < l->actions && l->rows > 1) return false;
+    return l->data && aligned(l->data, size_of(l->dtype));
+}
+
+Rows rows_of(const pictura_logits& l) { return Rows{l.data, l.stride, l.mask, l.mask_stride, l.rows, l.actions}; }
+
+unsigned blocks_for(int64_t rows) { return (unsigned)(rows < kMaxBlocks ? rows : kMaxBlocks); }
+
+// Row blocks of the loss: each leaves one set of partial sums.
+int64_t loss_blocks(int64_t rows) { return rows < 65536 ? rows : 65536; }
+
+uint64_t loss_bytes(int64_t rows) { return sizeof(double) * (uint64_t)(kMomentBlocks * 3 + loss_blocks(rows) * kSums); }
+
+pictura_status launched() { return hipGetLastError() == hipSuccess ? PICTURA_OK : PICTURA_EDEVICE; }
+
+}  // namespace
+}  // namespace pictura
+
+using namespace pictura;
+
+extern "C" {
+
+pictura_status pictura_sample_actions(const pictura_logits* logits, const pictura_sampling* how, const float* uniform,
+                                      int64_t* out_action, float* out_logp, void* stream)
+{
+    if (!logits_ok(logits) || !how) return PICTURA_EINVAL;
+    if (logits->rows == 0) return PICTURA_OK;
+    if (!uniform || !out_action || !out_logp || !aligned(uniform, 4) || !aligned(out_action, 8) || !aligned(out_logp, 4))
+        return PICTURA_EINVAL;
+    if (!aligned(how->temperatures, 4) || !aligned(how->top_ks, 4) || !aligned(how->top_ps, 4) || !aligned(how->min_ps, 4))
+        return PICTURA_EINVAL;
+    if (!how->temperatures && !(how->temperature >= 0.0f)) return PICTURA_EINVAL;
+    if ((!how->top_ps && std::isnan(how->top_p)) || (!how->min_ps && std::isnan(how->min_p))) return PICTURA_EINVAL;
+    const Sampling S{how->temperature, how->top_p, how->min_p, how->top_k,
+                     how->temperatures, how->top_ps, how->min_ps, how->top_ks};
+    const Rows R = rows_of(*logits);
+    hipStream_t s = (hipStream_t)stream;
+    const dim3 grid(blocks_for(R.rows)), block(kThreads);
+    if (logits->dtype == PICTURA_F32)
+        hipLaunchKernelGGL(sample_kernel<float>, grid, block, 0, s, R, S, uniform, out_action, out_logp);
+    else if (logits->dtype == PICTURA_BF16)
+        hipLaunchKernelGGL(sample_kernel<__bf16>, grid, block, 0, s, R, S, uniform, out_action, out_logp);
+    else
+        hipLaunchKernelGGL(sample_kernel<_Float16>, grid, block, 0, s, R, S, uniform, out_action, out_logp);
+    return launched();
+}
+
+pictura_status pictura_policy_loss_workspace(int64_t rows, int32_t actions, uint64_t* bytes)
+{
+    if (!bytes || rows < 0 || rows > 0x7FFFFFFFll || actions < 1 || actions > PICTURA_MAX_ACTIONS) return PICTURA_EINVAL;
+    *bytes = loss_bytes(rows);
+    return PICTURA_OK;
+}
+
+pictura_status pictura_policy_loss(const pictura_logits* logits, const pictura_policy_batch* q, void* workspace,
+                                   uint64_t workspace_bytes, float* out_stats, void* dlogits, int64_t dlogits_stride,
+                                   float* dvalues, void* stream)
+{
+    if (!logits_ok(logits) || !q || !out_stats || !aligned(out_stats, 4) || !workspace || !aligned(workspace, 256))
+        return PICTURA_EINVAL;
+    if (workspace_bytes < loss_bytes(logits->rows)) return PICTURA_EINVAL;
+    if (!(q->temperature > 0.0f) || !std::isfinite(q->temperature) || !(q->clip >= 0.0f) || std::isnan(q->value_clip) ||
+        !std::isfinite(q->value_coef) || !std::isfinite(q->entropy_coef) || !(q->denominator >= 0.0f))
+        return PICTURA_EINVAL;
+    if (logits->rows > 0) {
+        const size_t e = size_of(logits->dtype);
+        if (!dlogits || !dvalues || !aligned(dlogits, e) || !aligned(dvalues, 4)) return PICTURA_EINVAL;
+        if (dlogits_stride < logits->actions && logits->rows > 1) return PICTURA_EINVAL;
+        if (!q->values || !q->actions || !q->old_logp || !q->advantages || !q->returns) return PICTURA_EINVAL;
+        if (q->value_clip > 0.0f && !q->old_values) return PICTURA_EINVAL;
+        if (!aligned(q->values, 4) || !aligned(q->actions, 8) || !aligned(q->old_logp, 4) || !aligned(q->advantages, 4) ||
+            !aligned(q->returns, 4) || !aligned(q->old_values, 4) || !aligned(q->weights, 4))
+            return PICTURA_EINVAL;
+    }
+    const Rows R = rows_of(*logits);
+    const Batch b{q->values, q->values_stride, q->actions, q->old_logp, q->advantages, q->returns, q->old_values, q->weights,
+                  q->temperature, q->clip, q->value_clip, q->value_coef, q->entropy_coef, q->denominator,
+                  q->normalize ? 1 : 0, out_stats, dlogits, dlogits_stride, dvalues};
+    hipStream_t s = (hipStream_t)stream;
+    double* part = (double*)workspace;
+    double* sums = part + kMomentBlocks * 3;
+    const int64_t blocks = loss_blocks(R.rows);
+    hipLaunchKernelGGL(loss_moments_kernel, dim3(kMomentBlocks), dim3(kThreads), 0, s, b, R.rows, R.actions, part);
+    if (blocks > 0) {
+        const dim3 grid((unsigned)blocks), block(kThreads);
+        if (logits->dtype == PICTURA_F32) hipLaunchKernelGGL(loss_kernel<float>, grid, block, 0, s, R, b, part, sums);
+        else if (logits->dtype == PICTURA_BF16) hipLaunchKernelGGL(loss_kernel<__bf16>, grid, block, 0, s, R, b, part, sums);
+        else hipLaunchKernelGGL(loss_kernel<_Float16>, grid, block, 0, s, R, b, part, sums);
+    }
+    hipLaunchKernelGGL(loss_stats_kernel, dim3(1), dim3(kThreads), 0, s, b, part, sums, blocks);
+    return launched();
+}
+
+}  // extern "C"

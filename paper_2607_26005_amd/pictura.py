@@ -69,6 +69,39 @@ class _Encoder(ctypes.Structure):
                                                "proj_w", "proj_b")]
 
 
+class _Logits(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("actions", ctypes.c_int32),
+                ("rows", ctypes.c_int64), ("stride", ctypes.c_int64), ("mask", ctypes.c_void_p),
+                ("mask_stride", ctypes.c_int64)]
+
+
+class _Sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_k", ctypes.c_int32), ("top_p", ctypes.c_float),
+                ("min_p", ctypes.c_float)] + \
+               [(n, ctypes.c_void_p) for n in ("temperatures", "top_ks", "top_ps", "min_ps")]
+
+
+class _PolicyBatch(ctypes.Structure):
+    _fields_ = [("values", ctypes.c_void_p), ("values_stride", ctypes.c_int64)] + \
+               [(n, ctypes.c_void_p) for n in ("actions", "old_logp", "advantages", "returns", "old_values", "weights")] + \
+               [(n, ctypes.c_float) for n in ("temperature", "clip", "value_clip", "value_coef", "entropy_coef",
+                                              "denominator")] + [("normalize", ctypes.c_int32)]
+
+
+class _AdamW(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + \
+               [("step", ctypes.c_int64), ("bits", ctypes.c_int32), ("grad_factor", ctypes.c_void_p)]
+
+
+# pictura_adamw_tensor, as a row of a table: a step fills the columns
+ADAMW_TENSOR = np.dtype([(n, np.uint64) for n in ("param", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale",
+                                                  "exp_avg_sq_scale")] +
+                        [("n", np.int64), ("param_dtype", np.int32), ("grad_dtype", np.int32)], align=True)
+ADAMW_BLOCK = 256
+MAX_ACTIONS = 1 << 20
+POLICY_STATS = ("loss", "policy_loss", "value_loss", "entropy", "approx_kl", "clip_fraction")
+
+
 _P = ctypes.c_void_p
 _lib.pictura_create.argtypes = [ctypes.c_int32, ctypes.POINTER(_P)]
 _lib.pictura_create.restype = ctypes.c_int32
@@ -113,13 +146,30 @@ _lib.pictura_encoder_workspace.restype = ctypes.c_int32
 _lib.pictura_encode_views.argtypes = [ctypes.POINTER(_Encoder), _P, _P, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
                                       _P, ctypes.c_uint64, _P, _P]
 _lib.pictura_encode_views.restype = ctypes.c_int32
+_lib.pictura_sample_actions.argtypes = [ctypes.POINTER(_Logits), ctypes.POINTER(_Sampling), _P, _P, _P, _P]
+_lib.pictura_sample_actions.restype = ctypes.c_int32
+_lib.pictura_policy_loss_workspace.argtypes = [ctypes.c_int64, ctypes.c_int32, _P]
+_lib.pictura_policy_loss_workspace.restype = ctypes.c_int32
+_lib.pictura_policy_loss.argtypes = [ctypes.POINTER(_Logits), ctypes.POINTER(_PolicyBatch), _P, ctypes.c_uint64, _P, _P,
+                                     ctypes.c_int64, _P, _P]
+_lib.pictura_policy_loss.restype = ctypes.c_int32
+_lib.pictura_grad_norm_workspace.argtypes = [_P, ctypes.c_int32, _P]
+_lib.pictura_grad_norm_workspace.restype = ctypes.c_int32
+_lib.pictura_grad_norm.argtypes = [_P, ctypes.c_int32, ctypes.c_float, _P, ctypes.c_uint64, _P, _P]
+_lib.pictura_grad_norm.restype = ctypes.c_int32
+_lib.pictura_adamw_step.argtypes = [ctypes.POINTER(_AdamW), _P, ctypes.c_int32, _P]
+_lib.pictura_adamw_step.restype = ctypes.c_int32
+_lib.pictura_adamw_moments.argtypes = [_P, ctypes.c_int32, _P, _P, _P]
+_lib.pictura_adamw_moments.restype = ctypes.c_int32
 
 EXPORTED = ["pictura_create", "pictura_destroy", "pictura_last_error", "pictura_scene_upload",
             "pictura_bin_scene", "pictura_render_views", "pictura_agents_step", "pictura_bins_info",
             "pictura_bins_copy", "pictura_set_option", "pictura_stats_copy", "pictura_selftest_rcp",
             "pictura_set_lights", "pictura_render_instances", "pictura_render_rgb", "pictura_render_rgb_aa",
             "pictura_device_errors", "pictura_selftest_rcp_noalloc", "pictura_store_probe",
-            "pictura_encoder_workspace", "pictura_encode_views"]
+            "pictura_encoder_workspace", "pictura_encode_views", "pictura_sample_actions",
+            "pictura_policy_loss_workspace", "pictura_policy_loss", "pictura_grad_norm_workspace", "pictura_grad_norm",
+            "pictura_adamw_step", "pictura_adamw_moments"]
 DEVERR_RING_WAIT = 1
 
 STAT_NAMES = ["view_tiles", "cells_in_rect", "cells_prefiltered", "cells_visible", "cand_tris", "boxes_visible",
@@ -419,6 +469,219 @@ def pictura_encode_views(cams, num_classes, convs, queries, in_proj, out_proj, p
     st = _lib.pictura_encode_views(ctypes.byref(e), oc, od, V, H, W, ws.data_ptr(), int(need.value), oo, _stream(None))
     if st != OK:
         raise PicturaError(st, "encode_views failed")
+
+
+# --- the policy's operators -------------------------------------------------------
+
+def _codes():
+    import torch
+    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+_DTYPE_CODES = {}
+
+
+def _dtype_code(t, name: str) -> int:
+    if not _DTYPE_CODES:
+        _DTYPE_CODES.update(_codes())
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise PicturaError(EINVAL, f"{name}: dtype {t.dtype}, expected float32, bfloat16 or float16")
+    return code
+
+
+def _matrix(t, name: str, rows=None, cols=None) -> int:
+    """Address of a [rows, cols] tensor whose rows are contiguous and do not overlap."""
+    if t.dim() != 2 or (rows is not None and tuple(t.shape) != (rows, cols)):
+        raise PicturaError(EINVAL, f"{name}: shape {tuple(t.shape)}, expected " +
+                           ("[rows, actions]" if rows is None else f"[{rows}, {cols}]"))
+    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise PicturaError(EINVAL, f"{name}: strides {t.stride()}: a row has to be contiguous, and apart from the next")
+    if t.is_neg() or t.is_conj():
+        raise PicturaError(EINVAL, f"{name}: a lazily negated or conjugated tensor")
+    return t.data_ptr()
+
+
+def _tensor(t, name: str):
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise PicturaError(EINVAL, f"{name}: expected a torch tensor on the HIP device, got {type(t).__name__}")
+    _check_device(t, name, None)
+    return t
+
+
+def _one_device(ref, **others) -> None:
+    for name, t in others.items():
+        if t is not None and t.device != ref.device:
+            raise PicturaError(EINVAL, f"{name}: tensor on {t.device}, the logits are on {ref.device}")
+
+
+def _vector(t, name: str, kind, count: int) -> int:
+    """Address of a contiguous vector of exactly `count` elements of torch dtype `kind`."""
+    t = _tensor(t, name)
+    if t.dtype != kind:
+        raise PicturaError(EINVAL, f"{name}: dtype {t.dtype}, expected {str(kind).replace('torch.', '')}")
+    if tuple(t.shape) != (count,):
+        raise PicturaError(EINVAL, f"{name}: shape {tuple(t.shape)}, expected [{count}]")
+    if not t.is_contiguous() or t.is_neg():
+        raise PicturaError(EINVAL, f"{name}: tensor is not contiguous")
+    return t.data_ptr()
+
+
+def _logits(logits, mask) -> _Logits:
+    import torch
+    t = _tensor(logits, "logits")
+    ptr = _matrix(t, "logits")
+    N, A = t.shape
+    if not 1 <= A <= MAX_ACTIONS or N > 0x7FFFFFFF:
+        raise PicturaError(EINVAL, f"logits: shape {tuple(t.shape)}: 1 to {MAX_ACTIONS} actions, fewer than 2^31 rows")
+    l = _Logits(ptr, _dtype_code(t, "logits"), A, N, t.stride(0) if N > 1 else A)
+    if mask is not None:
+        m = _tensor(mask, "mask")
+        if m.dtype not in (torch.bool, torch.uint8):
+            raise PicturaError(EINVAL, f"mask: dtype {m.dtype}, expected bool or uint8")
+        if m.dim() == 1 or (m.dim() == 2 and m.shape[0] == 1) or (m.dim() == 2 and m.stride(0) == 0):
+            row = m if m.dim() == 1 else m[0]   # one row for all
+            if row.shape[0] != A or (A > 1 and row.stride(0) != 1) or (m.dim() == 2 and m.shape[0] not in (1, N)):
+                raise PicturaError(EINVAL, f"mask: shape {tuple(m.shape)}, strides {m.stride()}, expected contiguous "
+                                   f"rows of {A}")
+            l.mask, l.mask_stride = row.data_ptr(), 0
+        else:
+            l.mask, l.mask_stride = _matrix(m, "mask", N, A), m.stride(0)
+    return l
+
+
+def pictura_sample_actions(logits, uniform, out_action, out_logp, mask=None, temperature=1.0, top_k=0, top_p=1.0,
+                           min_p=0.0):
+    """Draw an action per row: logits [rows, actions] of float32, bfloat16 or
+    float16 (rows contiguous, any distance apart), mask bool or uint8 of the same
+    shape or one row for all, uniform float32 [rows]; temperature, top_k, top_p and
+    min_p each a number or a tensor [rows] (float32; top_k int32).  Writes
+    out_action int64 [rows] and out_logp float32 [rows], on the current stream."""
+    import torch
+    l = _logits(logits, mask)
+    N = l.rows
+    h = _Sampling(1.0, 0, 1.0, 0.0)
+    for name, v, kind in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                          ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if isinstance(v, torch.Tensor):
+            setattr(h, name + "s", _vector(v, name, kind, N))
+        elif isinstance(v, bool) or not isinstance(v, int if kind == torch.int32 else (int, float)):
+            raise PicturaError(EINVAL, f"{name}: {v!r}, expected a number or a tensor of one per row")
+        elif name == "top_k":
+            h.top_k = min(max(v, 0), MAX_ACTIONS)
+        elif not (0.0 <= v if name == "temperature" else v == v):
+            raise PicturaError(EINVAL, f"{name}: {v!r}")
+        else:
+            setattr(h, name, v)
+    iu = _vector(uniform, "uniform", torch.float32, N)
+    oa, ol = _vector(out_action, "out_action", torch.int64, N), _vector(out_logp, "out_logp", torch.float32, N)
+    per_row = {n: v for n, v in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p))
+               if isinstance(v, torch.Tensor)}
+    _one_device(logits, mask=mask, uniform=uniform, out_action=out_action, out_logp=out_logp, **per_row)
+    with torch.cuda.device(logits.device):
+        st = _lib.pictura_sample_actions(ctypes.byref(l), ctypes.byref(h), iu, oa, ol, _stream(None))
+    if st != OK:
+        raise PicturaError(st, "sample_actions failed")
+
+
+def pictura_policy_loss(logits, values, actions, old_logp, advantages, returns, out_stats, dlogits, dvalues,
+                        old_values=None, weights=None, mask=None, temperature=1.0, clip=0.2, value_clip=0.0,
+                        value_coef=0.5, entropy_coef=0.01, normalize=False, denominator=0.0):
+    """Clipped policy loss and its gradient: logits and mask as in
+    pictura_sample_actions, values float32 [rows] (any stride), actions int64, the
+    other vectors float32 [rows].  Writes out_stats float32 [6] (POLICY_STATS),
+    dlogits (the logits' type and shape, rows contiguous) and dvalues float32
+    [rows], on the current stream in a workspace of the caching allocator."""
+    import torch
+    l = _logits(logits, mask)
+    N, A = l.rows, l.actions
+    f32 = torch.float32
+    v = _tensor(values, "values")
+    if v.dtype != f32 or tuple(v.shape) != (N,) or v.is_neg():
+        raise PicturaError(EINVAL, f"values: {v.dtype} {tuple(v.shape)}, expected float32 [{N}]")
+    b = _PolicyBatch(v.data_ptr(), v.stride(0))
+    b.actions = _vector(actions, "actions", torch.int64, N)
+    b.old_logp = _vector(old_logp, "old_logp", f32, N)
+    b.advantages = _vector(advantages, "advantages", f32, N)
+    b.returns = _vector(returns, "returns", f32, N)
+    if value_clip > 0 and old_values is None:
+        raise PicturaError(EINVAL, "old_values: needed where value_clip > 0")
+    b.old_values = None if old_values is None else _vector(old_values, "old_values", f32, N)
+    b.weights = None if weights is None else _vector(weights, "weights", f32, N)
+    b.temperature, b.clip, b.value_clip = float(temperature), float(clip), float(value_clip)
+    b.value_coef, b.entropy_coef = float(value_coef), float(entropy_coef)
+    b.denominator, b.normalize = float(denominator), int(bool(normalize))
+    os_ = _vector(out_stats, "out_stats", f32, len(POLICY_STATS))
+    dl = _matrix(_tensor(dlogits, "dlogits"), "dlogits", N, A)
+    if dlogits.dtype != logits.dtype:
+        raise PicturaError(EINVAL, f"dlogits: dtype {dlogits.dtype}, the logits have {logits.dtype}")
+    dv = _vector(dvalues, "dvalues", f32, N)
+    _one_device(logits, values=values, actions=actions, old_logp=old_logp, advantages=advantages, returns=returns,
+                old_values=old_values, weights=weights, mask=mask, out_stats=out_stats, dlogits=dlogits, dvalues=dvalues)
+    need = ctypes.c_uint64()
+    st = _lib.pictura_policy_loss_workspace(N, A, ctypes.addressof(need))
+    if st != OK:
+        raise PicturaError(st, "policy_loss_workspace: sizes out of range")
+    with torch.cuda.device(logits.device):
+        ws = torch.empty(int(need.value), dtype=torch.uint8, device=logits.device)
+        st = _lib.pictura_policy_loss(ctypes.byref(l), ctypes.byref(b), ws.data_ptr(), int(need.value), os_, dl,
+                                      dlogits.stride(0) if N > 1 else A, dv, _stream(None))
+    if st != OK:
+        raise PicturaError(st, "policy_loss: a value out of range")
+
+
+def _table(table, name="tensors") -> int:
+    if not isinstance(table, np.ndarray) or table.dtype != ADAMW_TENSOR or not table.flags.c_contiguous:
+        raise PicturaError(EINVAL, f"{name}: expected a contiguous array of ADAMW_TENSOR")
+    return table.ctypes.data
+
+
+def pictura_grad_norm(table, max_norm: float, out, device):
+    """Norm of the gradients of a table (NumPy array of ADAMW_TENSOR holding device
+    addresses of tensors on `device`) and the factor that clips them to max_norm,
+    into out float32 [2], on the current stream in a workspace of the caching
+    allocator."""
+    import torch
+    at, n = _table(table), len(table)
+    oo = _vector(out, "out", torch.float32, 2)
+    need = ctypes.c_uint64()
+    st = _lib.pictura_grad_norm_workspace(at, n, ctypes.addressof(need))
+    if st != OK:
+        raise PicturaError(st, "grad_norm_workspace: sizes out of range")
+    with torch.cuda.device(device):
+        ws = torch.empty(int(need.value), dtype=torch.uint8, device=device)
+        st = _lib.pictura_grad_norm(at, n, float(max_norm), ws.data_ptr(), int(need.value), oo, _stream(None))
+    if st != OK:
+        raise PicturaError(st, "grad_norm: a value out of range")
+
+
+def pictura_adamw_step(table, device, lr, betas, eps, weight_decay, step, bits=32, grad_factor=None):
+    """One AdamW step of the tensors of a table (see pictura_grad_norm), on the
+    current stream.  grad_factor: float32 tensor of one element on the device."""
+    import torch
+    at = _table(table)
+    gf = None if grad_factor is None else _vector(grad_factor, "grad_factor", torch.float32, 1)
+    h = _AdamW(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), int(step), int(bits), gf)
+    with torch.cuda.device(device):
+        st = _lib.pictura_adamw_step(ctypes.byref(h), at, len(table), _stream(None))
+    if st != OK:
+        raise PicturaError(st, "adamw_step: a value out of range")
+
+
+def pictura_adamw_moments(table, exp_avg_out, exp_avg_sq_out, device):
+    """What the 8-bit moments of a table stand for: exp_avg_out and exp_avg_sq_out
+    are contiguous uint64 arrays of the outputs' device addresses (float32)."""
+    import torch
+    at = _table(table)
+    for a in (exp_avg_out, exp_avg_sq_out):
+        if a.dtype != np.uint64 or a.shape != (len(table),) or not a.flags.c_contiguous:
+            raise PicturaError(EINVAL, "moments: expected one uint64 address per tensor")
+    with torch.cuda.device(device):
+        st = _lib.pictura_adamw_moments(at, len(table), exp_avg_out.ctypes.data, exp_avg_sq_out.ctypes.data,
+                                        _stream(None))
+    if st != OK:
+        raise PicturaError(st, "adamw_moments: a value out of range")
 
 
 # --- device-resident agents ------------------------------------------------------

@@ -1,0 +1,371 @@
+"""Actions drawn from logits, and the clipped policy loss with its gradient, against
+64-bit implementations (tests/policy_oracle.py)."""
+import numpy as np
+import pytest
+
+from tests import policy_oracle as PO
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = ("float32", "bfloat16", "float16")
+
+
+@pytest.fixture(scope="module")
+def mods():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no HIP device")
+    from paper_2607_26005_amd import policy
+    return torch, policy
+
+
+def _logits(torch, N, A, dtype, seed, pad=0, spread=2.0):
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn(N, A + pad, generator=g) * spread).to(getattr(torch, dtype)).cuda()
+    return x[:, :A], torch.rand(N, generator=g)
+
+
+def _check_draws(torch, policy, logits, u, mask=None, **how):
+    """Every row against the 64-bit distribution.  The kernel's weights are fp32
+    exponentials of (x - max) / T, relative error at most 2^-23 |x - max| / T (the
+    division) + 2^-23 (exp), cut to 2^-32 of the largest: the cumulative
+    distribution is off by less than 2e-5 for the ranges used here (|d| <= 88),
+    so a row may differ only where u or a filter's sum is that near an edge."""
+    tol = 2e-5
+    act, logp = policy.sample_actions(logits, u.cuda(), mask=mask, **{
+        k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in how.items()})
+    act, logp = act.cpu().numpy(), logp.cpu().numpy()
+    x = logits.float().cpu().numpy()
+    m = None if mask is None else np.broadcast_to(mask.cpu().numpy(), x.shape)
+    sure = 0
+    for n in range(len(x)):
+        at = {k: v[n].item() if isinstance(v, torch.Tensor) else v for k, v in how.items()}
+        p, near = PO.kept_weights(x[n], None if m is None else m[n], **at)
+        if p is None:
+            assert act[n] == -1 and np.isnan(logp[n]), (n, act[n], logp[n])
+            sure += 1
+            continue
+        assert 0 <= act[n] < x.shape[1], (n, act[n])
+        if near < tol:
+            continue
+        a, edge = PO.draw(p, float(u[n]))
+        assert p[act[n]] > 0, (n, act[n], a)
+        if edge > tol:
+            assert act[n] == a, (n, act[n], a, edge)
+            sure += 1
+        assert abs(logp[n] - np.log(p[act[n]])) < 4e-5 + 1e-6 * abs(logp[n]), (n, logp[n], np.log(p[act[n]]))
+    return act, logp, sure
+
+
+FILTERS = [dict(), dict(temperature=0.7), dict(top_k=5), dict(top_p=0.8), dict(min_p=0.1), dict(temperature=0.0),
+           dict(temperature=1.3, top_k=40, top_p=0.9, min_p=0.02), dict(top_k=1), dict(top_p=0.0), dict(top_k=7, top_p=0.999)]
+
+
+@pytest.mark.parametrize("how", FILTERS, ids=str)
+@pytest.mark.parametrize("N, A", [(1, 1), (33, 2), (70, 12), (5, 63), (5, 64), (6, 65), (9, 130), (7, 257), (5, 1000),
+                                  (3, 4099), (2, 16385), (2, 65537)])
+def test_draws_match_float64(mods, N, A, how):
+    torch, policy = mods
+    dtype = DTYPES[(N + A) % 3]
+    logits, u = _logits(torch, N, A, dtype, N * 7 + A, pad=A % 3)
+    _, _, sure = _check_draws(torch, policy, logits, u, **how)
+    assert sure * 2 >= N or A > 4000
+
+
+@pytest.mark.parametrize("A", [3, 12, 40, 300, 5000, 70000])
+def test_draws_with_masks_and_settings_per_row(mods, A):
+    torch, policy = mods
+    N = 24 if A < 1000 else 6
+    logits, u = _logits(torch, N, A, "float32", A, pad=1)
+    g = torch.Generator().manual_seed(A)
+    mask = torch.rand(N, A, generator=g) < 0.6
+    mask[1] = False                        # a row that allows nothing
+    mask[2] = False
+    mask[2, A - 1] = True                  # one that allows the last action alone
+    logits = logits.clone()
+    logits[~mask.cuda()] = float("nan")    # what is masked is not looked at
+    logits[3, mask[3].nonzero()[0, 0]] = -float("inf")
+    how = dict(temperature=torch.rand(N, generator=g) + 0.5, top_k=torch.randint(0, 9, (N,), generator=g, dtype=torch.int32),
+               top_p=torch.rand(N, generator=g) * 0.5 + 0.6, min_p=torch.rand(N, generator=g) * 0.05)
+    how["temperature"][4] = 0.0
+    how["temperature"][5] = -1.0
+    act, logp, _ = _check_draws(torch, policy, logits, u, mask=mask.cuda(), **how)
+    assert act[1] == -1 and act[2] == A - 1 and logp[2] == 0.0 and act[5] == -1 and logp[4] == 0.0
+    assert all(a < 0 or mask[n, a] for n, a in enumerate(act))
+    # one row of the mask for all
+    if A >= 12:
+        some = mask[0].cuda()
+        act2, _, _ = _check_draws(torch, policy, torch.nan_to_num(logits, 0.0, 0.0, -3.0), u, mask=some, top_p=0.9)
+        assert all(some[a] for a in act2)
+
+
+@pytest.mark.parametrize("A", [12, 300, 5000, 70000])
+def test_rows_that_make_no_draw_or_a_certain_one(mods, A):
+    torch, policy = mods
+    low = torch.finfo(torch.float32).min
+    x = torch.zeros(8, A)
+    x[0] = -float("inf")
+    x[1, A // 2] = float("nan")
+    x[2, A // 2] = float("inf")
+    x[3] = low                             # all at the type's lowest value: all alike
+    x[4] = low
+    x[4, A - 2] = 1.0                      # one above it: certain
+    x[5] = -float("inf")
+    x[5, 1] = low
+    x[6, ::2] = -0.0                       # zeros of both signs are equal
+    x[7] = torch.linspace(1, -1, A) * 3e38   # differences that overflow
+    u = torch.full((8,), 0.999999)
+    for how in (dict(), dict(top_k=3), dict(top_p=0.5), dict(top_k=3, top_p=0.7, min_p=0.5), dict(temperature=0.0)):
+        act, logp = policy.sample_actions(x.cuda(), u.cuda(), **how)
+        act, logp = act.cpu().tolist(), logp.cpu()
+        assert act[:3] == [-1, -1, -1] and logp[:3].isnan().all()
+        assert act[4] == A - 2 and act[5] == 1 and act[7] == 0 and (logp[[4, 5, 7]] == 0).all()
+        for n in (3, 6):                   # equal logits: a filter keeps the lowest indices
+            p, _ = PO.kept_weights(np.zeros(A), **how)
+            count = int((p > 0).sum())
+            assert act[n] == count - 1, (how, n, act[n], count)
+            assert abs(logp[n].item() + np.log(count)) < 1e-5
+
+
+def test_random_numbers_at_the_ends(mods):
+    torch, policy = mods
+    x = torch.zeros(7, 6).cuda()
+    u = torch.tensor([0.0, 1.0 - 2.0 ** -24, 1.0, 2.0, -1.0, float("nan"), 2.0 ** -40]).cuda()
+    act, _ = policy.sample_actions(x, u)
+    assert act.cpu().tolist() == [0, 5, 5, 5, 0, 0, 0]
+
+
+@pytest.mark.parametrize("A", [12, 2000])
+def test_draws_follow_the_distribution(mods, A):
+    # 200,000 draws of one row: each of 12 cells' counts within 5 sigma of its share
+    torch, policy = mods
+    N = 200_000 if A == 12 else 20_000
+    row, _ = _logits(torch, 1, A, "float32", 5, spread=1.5)
+    u = torch.rand(N, generator=torch.Generator().manual_seed(9))
+    act, logp = policy.sample_actions(row.expand(N, A).contiguous(), u.cuda(), top_p=0.95)
+    p, _ = PO.kept_weights(row[0].cpu().numpy(), top_p=0.95)
+    cell = np.arange(A) * 12 // A
+    got = np.bincount(cell[act.cpu().numpy()], minlength=12)
+    want = np.bincount(cell, weights=p, minlength=12)
+    assert (np.abs(got - N * want) <= 5 * np.sqrt(N * want * (1 - want)) + 1e-9).all()
+
+
+def test_a_row_draws_alike_in_any_batch_and_on_any_stream(mods):
+    torch, policy = mods
+    for A in (12, 777, 9000):
+        logits, u = _logits(torch, 50, A, "float32", A)
+        u = u.cuda()
+        act, logp = policy.sample_actions(logits, u, top_p=0.9, temperature=0.9)
+        one = [policy.sample_actions(logits[n:n + 1], u[n:n + 1], top_p=0.9, temperature=0.9) for n in range(0, 50, 7)]
+        assert torch.equal(act[::7], torch.cat([a for a, _ in one])) and torch.equal(logp[::7], torch.cat([l for _, l in one]))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            again = policy.sample_actions(logits, u, top_p=0.9, temperature=0.9)
+        side.synchronize()
+        assert torch.equal(act, again[0]) and torch.equal(logp, again[1])
+
+
+def test_no_rows(mods):
+    torch, policy = mods
+    e = torch.empty(0, device="cuda")
+    act, logp = policy.sample_actions(torch.empty(0, 12, device="cuda"), e)
+    assert act.shape == (0,) and logp.shape == (0,)
+    out = policy.policy_gradient(torch.empty(0, 12, device="cuda"), e, torch.empty(0, dtype=torch.int64, device="cuda"), e, e, e)
+    assert (out.stats == 0).all() and out.dlogits.shape == (0, 12)
+
+
+# ---------------------------------------------------------------------------
+# policy loss
+# ---------------------------------------------------------------------------
+
+def _batch(torch, N, A, dtype, seed, pad=0, spread=1.5):
+    g = torch.Generator().manual_seed(seed)
+    head = (torch.randn(N, A + pad, generator=g) * spread).to(getattr(torch, dtype)).cuda()
+    z = head[:, :A].float().cpu().double()
+    b = dict(actions=torch.randint(0, A, (N,), generator=g), advantages=torch.randn(N, generator=g) + 0.2,
+             values=torch.randn(N, generator=g), old_values=torch.randn(N, generator=g) * 0.3,
+             weights=(torch.rand(N, generator=g) < 0.7).float())
+    b["old_values"] += b["values"]
+    b["returns"] = b["values"] + torch.randn(N, generator=g)
+    b["weights"][N // 2] = 1.0
+    # log-ratios spread over both sides of the clip, none within 1e-3 of its edges
+    diff = torch.randn(N, generator=g, dtype=torch.float64) * 0.3
+    r = diff.exp()
+    diff = torch.where(((r - 0.8).abs() < 1e-3) | ((r - 1.2).abs() < 1e-3), torch.tensor(0.01, dtype=torch.float64), diff)
+    b["diff"] = diff
+    return head[:, :A], z, b
+
+
+def _old_logp(torch, z, b, mask=None, temperature=1.0):
+    x = z if mask is None else z.masked_fill(~mask, -1e300)
+    lp = (x / temperature).log_softmax(1).gather(1, b["actions"][:, None])[:, 0]
+    return (lp - b["diff"]).float()
+
+
+def _run(torch, policy, logits, b, old_logp, mask=None, **kw):
+    c = {k: v.cuda() for k, v in b.items()}
+    out = policy.policy_gradient(logits, c["values"], c["actions"], old_logp.cuda(), c["advantages"], c["returns"],
+                                 old_values=c["old_values"], mask=mask, **{
+                                     k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in kw.items()})
+    ref = PO.policy_loss(logits.float().cpu().numpy(), b["values"].numpy(), b["actions"].numpy(), old_logp.numpy(),
+                         b["advantages"].numpy(), b["returns"].numpy(), old_values=b["old_values"].numpy(),
+                         mask=None if mask is None else mask.cpu().numpy(),
+                         **{k: v.numpy() if isinstance(v, torch.Tensor) else v for k, v in kw.items()})
+    return out, ref
+
+
+# a rounding to the logits' type, at most half a unit of it; the fp32 arithmetic before
+# it: sums of up to 2^17 terms in lanes and trees, logarithms of up to 2^4, exponents of
+# up to 88: well below 2^-16
+ROUND = {"float32": 2.0 ** -16, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}
+
+
+def _close(out, ref, dtype):
+    stats, dz, dv = ref
+    got = [out.stats.cpu().double().numpy(), out.dlogits.float().cpu().double().numpy(), out.dvalues.cpu().double().numpy()]
+    assert np.abs(got[0] - stats).max() <= 2.0 ** -16 * max(1.0, np.abs(stats).max()), (got[0], stats)
+    # (fp16's smallest steps: 2^-25 is half of one)
+    tol = (ROUND[dtype] + 2.0 ** -16) * np.abs(dz) + 2.0 ** -20 * np.abs(dz).max() + (2.0 ** -25 if dtype == "float16" else 0)
+    assert (np.abs(got[1] - dz) <= tol).all(), np.abs(got[1] - dz).max()
+    assert (np.abs(got[2] - dv) <= 2.0 ** -20 * np.abs(dv).max() + 1e-12).all()
+
+
+@pytest.mark.parametrize("N, A", [(1, 1), (1, 2), (40, 12), (300, 7), (9, 32), (9, 33), (9, 64), (9, 65), (8, 130), (5, 1000),
+                                  (3, 4099), (2, 16381), (2, 65537)])
+@pytest.mark.parametrize("options", [False, True])
+def test_loss_and_gradient_match_float64(mods, N, A, options):
+    torch, policy = mods
+    for dtype in DTYPES:
+        logits, z, b = _batch(torch, N, A, dtype, N + A, pad=A % 2)
+        kw = dict(weights=b["weights"], value_clip=0.2, normalize=N > 2, entropy_coef=0.05, value_coef=0.7) if options else {}
+        out, ref = _run(torch, policy, logits, b, _old_logp(torch, z, b), **kw)
+        _close(out, ref, dtype)
+
+
+@pytest.mark.parametrize("A", [5, 12, 48, 700, 5000, 70000])
+def test_loss_with_masks_and_rows_that_do_not_count(mods, A):
+    torch, policy = mods
+    N = 12
+    logits, z, b = _batch(torch, N, A, "float32", A, pad=1)
+    g = torch.Generator().manual_seed(A)
+    mask = torch.rand(N, A, generator=g) < 0.5
+    mask.scatter_(1, b["actions"][:, None], True)
+    mask[7] = False                                          # a row that allows nothing: no action was drawn
+    b["actions"][7] = -1
+    b["actions"][8] = A                                      # outside the head
+    old = _old_logp(torch, z, dict(b, actions=b["actions"].clamp(0, A - 1)), mask, temperature=0.8)
+    w = torch.rand(N, generator=g) + 0.5
+    w[3] = 0.0
+    logits = logits.clone()
+    logits[~mask.cuda()] = float("nan")
+    logits[3] = float("nan")                                 # nothing of such a row is looked at
+    for k in ("values", "advantages", "returns", "old_values"):
+        b[k][3] = float("nan")
+        b[k][7] = float("inf")
+    out, ref = _run(torch, policy, logits, b, old, mask=mask.cuda(), weights=w, temperature=0.8, normalize=True, value_clip=0.3)
+    _close(out, ref, "float32")
+    d = out.dlogits.cpu()
+    assert (d[~mask] == 0).all() and (d[[3, 7, 8]] == 0).all() and (out.dvalues.cpu()[[3, 7, 8]] == 0).all()
+
+
+def test_parts_of_a_minibatch_add_up(mods):
+    torch, policy = mods
+    logits, z, b = _batch(torch, 60, 12, "float32", 1)
+    old = _old_logp(torch, z, b)
+    c = {k: v.cuda() for k, v in b.items()}
+    args = lambda s: (logits[s], c["values"][s], c["actions"][s], old.cuda()[s], c["advantages"][s], c["returns"][s])
+    whole = policy.policy_gradient(*args(slice(None)))
+    parts = [policy.policy_gradient(*args(slice(i, i + 20)), denominator=60.0) for i in (0, 20, 40)]
+    assert torch.allclose(sum(p.stats for p in parts), whole.stats, rtol=1e-6, atol=1e-7)
+    assert torch.allclose(torch.cat([p.dlogits for p in parts]), whole.dlogits, rtol=1e-6, atol=0)
+    assert torch.equal(torch.cat([p.dvalues for p in parts]), whole.dvalues)
+
+
+def test_no_row_counts(mods):
+    torch, policy = mods
+    logits, z, b = _batch(torch, 5, 12, "float32", 2)
+    out, ref = _run(torch, policy, logits, b, _old_logp(torch, z, b), weights=torch.zeros(5), normalize=True)
+    assert (out.stats == 0).all() and (out.dlogits == 0).all() and (out.dvalues == 0).all()
+
+
+@pytest.mark.parametrize("A", [12, 900])
+def test_gradient_matches_differences(mods, A):
+    # central differences of the 64-bit loss: the gradient's own check, apart from the formula
+    torch, policy = mods
+    N, h = 6, 1e-5
+    logits, z, b = _batch(torch, N, A, "float32", 3 + A)
+    old = _old_logp(torch, z, b)
+    kw = dict(value_clip=0.2, entropy_coef=0.1, temperature=1.0)
+    out, _ = _run(torch, policy, logits, b, old, **kw)
+    base = [z.numpy(), b["values"].double().numpy(), b["actions"].numpy(), old.numpy(), b["advantages"].numpy(), b["returns"].numpy()]
+    loss = lambda x, v: PO.policy_loss(x, v, *base[2:], old_values=b["old_values"].numpy(), value_only=True, **kw)
+    rng = np.random.default_rng(0)
+    for _ in range(12):
+        n, i = int(rng.integers(N)), int(rng.integers(A))
+        for i in (i, int(b["actions"][n])):
+            e = np.zeros((N, A))
+            e[n, i] = h
+            num = (loss(base[0] + e, base[1]) - loss(base[0] - e, base[1])) / (2 * h)
+            # differences: h^2 of the third derivative (below 10) and 2^-52 / h of the loss
+            assert abs(num - out.dlogits[n, i].item()) < 1e-8 + 2.0 ** -18 * abs(num) + 2.0 ** -22, (n, i)
+        e = np.zeros(N)
+        e[n] = h
+        num = (loss(base[0], base[1] + e) - loss(base[0], base[1] - e)) / (2 * h)
+        assert abs(num - out.dvalues[n].item()) < 1e-7
+
+
+def test_loss_under_autograd(mods):
+    torch, policy = mods
+    logits, z, b = _batch(torch, 30, 12, "float32", 4)
+    old = _old_logp(torch, z, b).cuda()
+    c = {k: v.cuda() for k, v in b.items()}
+    x, v = logits.clone().requires_grad_(), c["values"].clone().requires_grad_()
+    loss, stats = policy.policy_loss(x, v, c["actions"], old, c["advantages"], c["returns"], normalize=True)
+    (3.0 * loss).backward()
+    out = policy.policy_gradient(logits, c["values"], c["actions"], old, c["advantages"], c["returns"], normalize=True)
+    assert torch.equal(loss.detach(), out.stats[0]) and torch.equal(stats, out.stats)
+    assert torch.allclose(x.grad, 3.0 * out.dlogits) and torch.allclose(v.grad, 3.0 * out.dvalues)
+
+
+def test_loss_repeats_to_the_bit_and_overwrites_its_logits(mods):
+    torch, policy = mods
+    from paper_2607_26005_amd import pictura
+    for A in (12, 100, 3000):
+        logits, z, b = _batch(torch, 200, A, "float32", 6)
+        old = _old_logp(torch, z, b).cuda()
+        c = {k: v.cuda() for k, v in b.items()}
+        a = policy.policy_gradient(logits, c["values"], c["actions"], old, c["advantages"], c["returns"], weights=c["weights"])
+        x = logits.clone()
+        stats, dv = torch.empty(6, device="cuda"), torch.empty(200, device="cuda")
+        pictura.pictura_policy_loss(x, c["values"], c["actions"], old, c["advantages"], c["returns"], stats, x, dv,
+                                    weights=c["weights"])
+        assert torch.equal(stats, a.stats) and torch.equal(x, a.dlogits) and torch.equal(dv, a.dvalues)
+
+
+def test_draw_and_loss_in_a_graph(mods):
+    torch, policy = mods
+    logits, z, b = _batch(torch, 64, 12, "float32", 8)
+    old = _old_logp(torch, z, b).cuda()
+    c = {k: v.cuda() for k, v in b.items()}
+    u = torch.rand(64, device="cuda")
+    run = lambda: (*policy.sample_actions(logits, u, top_p=0.9),
+                   *policy.policy_gradient(logits, c["values"], c["actions"], old, c["advantages"], c["returns"], normalize=True))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for k in range(4):
+        logits.copy_(torch.randn(64, 12, generator=torch.Generator().manual_seed(k)))
+        u.copy_(torch.rand(64, generator=torch.Generator().manual_seed(k)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got_now = [t.clone() for t in got]
+        want = run()
+        torch.cuda.synchronize()
+        for x, y in zip(got_now, want):
+            assert torch.equal(x, y), k
