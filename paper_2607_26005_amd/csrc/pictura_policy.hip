@@ -289,6 +289,91 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const Rows R, const Sa
     }
 }
 
+
+// ---------------------------------------------------------------------------
+// few actions: a row in a group of G lanes
+// ---------------------------------------------------------------------------
+
+template <int G>
+__device__ __forceinline__ float group_max(float x)
+{
+#pragma unroll
+    for (int d = G / 2; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+    return x;
+}
+
+template <int G, class V>
+__device__ __forceinline__ V group_sum(V x)
+{
+#pragma unroll
+    for (int d = G / 2; d; d >>= 1) x += __shfl_xor(x, d);
+    return x;
+}
+
+// Heads of up to 64 actions.  Each lane holds one action; where a filter is on, it
+// counts the actions and adds the weights that come before its own, A steps.
+template <class T, int G, bool kFilter>
+__global__ __launch_bounds__(kThreads) void sample_small_kernel(const Rows R, const Sampling S,
+                                                                const float* __restrict__ uniform,
+                                                                int64_t* __restrict__ out_action,
+                                                                float* __restrict__ out_logp)
+{
+    const int A = R.actions, j = threadIdx.x & (G - 1), lane = threadIdx.x & 63, first = lane & ~(G - 1);
+    const uint64_t group = (G == 64 ? ~0ull : (1ull << (G & 63)) - 1ull) << first;
+    const int64_t step = (int64_t)gridDim.x * (kThreads / G);
+    for (int64_t n0 = (int64_t)blockIdx.x * (kThreads / G); n0 < R.rows; n0 += step) {
+        const int64_t n = n0 + threadIdx.x / G;
+        const bool live = n < R.rows;
+        const int64_t m = live ? n : R.rows - 1;
+        const Row<T> row(R, m);
+        const float x = j < A ? row(j) : -INFINITY;
+        const float temp = S.temperatures ? S.temperatures[m] : S.temperature;
+        const float u = uniform[m];
+        const float top = group_max<G>(x);
+        const bool bad = (__ballot(!(x < INFINITY)) & group) != 0 || !(temp >= 0.0f) || top == -INFINITY;
+        uint32_t w;
+        if (temp > 0.0f) w = weight_of(x, top, temp);
+        else w = lane == __ffsll((unsigned long long)(__ballot(x == top) & group)) - 1 ? 1u : 0u;
+        if constexpr (kFilter) {
+            const int32_t k = S.top_ks ? S.top_ks[m] : S.top_k;
+            const float top_p = S.top_ps ? S.top_ps[m] : S.top_p, min_p = S.min_ps ? S.min_ps[m] : S.min_p;
+            int rank = 0;
+            uint64_t before = 0;
+            for (int i = 0; i < A; ++i) {
+                const float xi = __shfl(x, first + i);
+                const uint32_t wi = (uint32_t)__shfl((int)w, first + i);
+                const bool ahead = xi > x || (xi == x && i < j);
+                rank += ahead;
+                before += ahead ? wi : 0u;
+            }
+            if (temp > 0.0f) {
+                if (k > 0 && rank >= k) w = 0;
+                if (top_p < 1.0f) {
+                    const uint64_t need = share(group_sum<G>((uint64_t)w), cut31(top_p));
+                    if (before >= (need < 1 ? 1 : need)) w = 0;
+                }
+                if (w < (uint32_t)ceilf(fminf(fmaxf(min_p, 0.0f), 1.0f) * kOne)) w = 0;
+            }
+        }
+        uint64_t run = w;
+#pragma unroll
+        for (int d = 1; d < G; d <<= 1) {
+            const uint64_t o = __shfl_up(run, d);
+            if (j >= d) run += o;
+        }
+        const uint64_t total = __shfl(run, first + G - 1);
+        const uint64_t hit = __ballot(run > share(total, cut31(u))) & group;
+        if (live && !bad && lane == __ffsll((unsigned long long)hit) - 1) {
+            out_action[n] = j;
+            out_logp[n] = logf((float)w / (float)total);
+        }
+        if (live && bad && j == 0) {
+            out_action[n] = -1;
+            out_logp[n] = NAN;
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------
 // policy loss
 // ---------------------------------------------------------------------------
@@ -310,13 +395,9 @@ struct Batch {
     float* dvalues;
 };
 
-constexpr int kMomentBlocks = 128;      // partial sums of the weights and advantages
+constexpr int kMomentBlocks = 64;       // most partial sums of the weights and advantages: a lane each
+constexpr int kMomentRows = 1024;       // rows of a workgroup that sums them, at least
 constexpr int kSums = 5;                // sums over the rows: policy, value, entropy, KL, clipped
-
-__device__ __forceinline__ double block_sum_d(double x, double* lds)
-{
-    return block_sum(x, lds);
-}
 
 // Weight of row n, 0 where it does not count.
 __device__ __forceinline__ float row_weight(const Batch& b, int64_t n, int32_t A)
@@ -326,12 +407,14 @@ __device__ __forceinline__ float row_weight(const Batch& b, int64_t n, int32_t A
     return b.weights ? b.weights[n] : 1.0f;
 }
 
-// Sums of the weights, and of the advantages and their squares by weight.
-__global__ __launch_bounds__(kThreads) void loss_moments_kernel(const Batch b, int64_t rows, int32_t A, double* __restrict__ part)
+// Sums of the weights, and of the advantages and their squares by weight; clears the
+// count of finished workgroups that the loss kernel keeps.
+__global__ __launch_bounds__(kThreads) void loss_moments_kernel(const Batch b, int64_t rows, int32_t A,
+                                                                double* __restrict__ part, uint32_t* __restrict__ done)
 {
     __shared__ double lds[kWaves];
     double w0 = 0.0, w1 = 0.0, w2 = 0.0;
-    for (int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x; n < rows; n += (int64_t)kMomentBlocks * kThreads) {
+    for (int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x; n < rows; n += (int64_t)gridDim.x * kThreads) {
         const double w = (double)row_weight(b, n, A);
         if (w == 0.0) continue;
         const double a = (double)b.advantages[n];
@@ -339,13 +422,14 @@ __global__ __launch_bounds__(kThreads) void loss_moments_kernel(const Batch b, i
         w1 += w * a;
         w2 += w * a * a;
     }
-    w0 = block_sum_d(w0, lds);
-    w1 = block_sum_d(w1, lds);
-    w2 = block_sum_d(w2, lds);
+    w0 = block_sum(w0, lds);
+    w1 = block_sum(w1, lds);
+    w2 = block_sum(w2, lds);
     if (threadIdx.x == 0) {
-        part[blockIdx.x * 3] = w0;
-        part[blockIdx.x * 3 + 1] = w1;
-        part[blockIdx.x * 3 + 2] = w2;
+        part[blockIdx.x] = w0;
+        part[kMomentBlocks + blockIdx.x] = w1;
+        part[2 * kMomentBlocks + blockIdx.x] = w2;
+        if (blockIdx.x == 0) *done = 0;
     }
 }
 
@@ -354,14 +438,14 @@ struct Shared3 {
     float inv, mean, rstd;
 };
 
-__device__ __forceinline__ Shared3 loss_shared(const Batch& b, const double* __restrict__ part, double* lds)
+__device__ __forceinline__ Shared3 loss_shared(const Batch& b, const double* __restrict__ part, int parts)
 {
+    const int lane = threadIdx.x & 63;
     double s[3];
-    for (int k = 0; k < 3; ++k) {
-        double x = 0.0;
-        for (int i = threadIdx.x; i < kMomentBlocks; i += kThreads) x += part[i * 3 + k];
-        s[k] = block_sum_d(x, lds);
-    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) s[k] = lane < parts ? part[k * kMomentBlocks + lane] : 0.0;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) s[k] = wave_sum(s[k]);
     Shared3 o;
     const double den = b.denominator != 0.0f ? (double)b.denominator : s[0];
     o.inv = s[0] != 0.0 ? (float)(1.0 / den) : 0.0f;
@@ -410,14 +494,95 @@ __device__ __forceinline__ RowTerms row_terms(const Batch& b, const Shared3& s, 
     return o;
 }
 
+// Leave this workgroup's sums; the last workgroup to do so adds them all up, in the
+// order of the workgroups, and writes the statistics.
+__device__ void loss_finish(const Batch& b, const Shared3& s, const double* acc, double* __restrict__ sums,
+                            uint32_t* __restrict__ done, double* lds)
+{
+    __shared__ uint32_t last;
+    double total[kSums];
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) total[k] = block_sum(acc[k], lds);
+    if (threadIdx.x == 0) {
+        for (int k = 0; k < kSums; ++k) sums[(int64_t)blockIdx.x * kSums + k] = total[k];
+        __threadfence();
+        last = atomicAdd(done, 1u);
+    }
+    __syncthreads();
+    if (last != gridDim.x - 1) return;
+    __threadfence();
+    double x[kSums] = {};
+    for (unsigned i = threadIdx.x; i < gridDim.x; i += kThreads)
+#pragma unroll
+        for (int k = 0; k < kSums; ++k) x[k] += sums[(int64_t)i * kSums + k];
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) x[k] = block_sum(x[k], lds) * (double)s.inv;
+    if (threadIdx.x == 0) {
+        b.stats[0] = (float)(x[0] + (double)b.value_coef * x[1] - (double)b.entropy_coef * x[2]);
+        for (int k = 0; k < kSums; ++k) b.stats[k + 1] = (float)x[k];
+    }
+}
+
+struct Work {
+    const double* part;   // sums of loss_moments_kernel
+    int32_t parts;
+    double* sums;
+    uint32_t* done;
+};
+
+// Heads of up to 64 actions: a row in a group of G lanes, one action each.
+template <class T, int G>
+__global__ __launch_bounds__(kThreads) void loss_small_kernel(const Rows R, const Batch b, const Work k)
+{
+    __shared__ double lds[kWaves];
+    const Shared3 s = loss_shared(b, k.part, k.parts);
+    const int A = R.actions, j = threadIdx.x & (G - 1), first = threadIdx.x & 63 & ~(G - 1);
+    const int64_t step = (int64_t)gridDim.x * (kThreads / G);
+    const float ce = b.entropy_coef, rt = b.temperature;
+    double acc[kSums] = {};
+    for (int64_t n0 = (int64_t)blockIdx.x * (kThreads / G); n0 < R.rows; n0 += step) {
+        const int64_t n = n0 + threadIdx.x / G;
+        const bool live = n < R.rows;
+        const int64_t m = live ? n : R.rows - 1;
+        const float w = live ? row_weight(b, m, A) : 0.0f;
+        const bool on = w != 0.0f;
+        const Row<T> row(R, m);
+        const float x = on && j < A ? row(j) : -INFINITY;
+        const int a = on ? (int)b.actions[m] : 0;
+        const float top = group_max<G>(x);
+        const float d = x == -INFINITY ? -INFINITY : (x - top) / rt, e = expf(d);
+        const float e0 = group_sum<G>(e), e1 = group_sum<G>(e != 0.0f ? e * d : 0.0f);
+        const float da = __shfl(d, first + a);
+        if (!live) continue;
+        float y = 0.0f;
+        if (on) {
+            const float logs = logf(e0), rs = 1.0f / e0;
+            const float H = e0 > 0.0f ? logs - e1 * rs : e0 == 0.0f ? 0.0f : e0;
+            const RowTerms t = row_terms(b, s, m, e0 == 0.0f ? -INFINITY : da - logs, H);
+            const float scale = w * s.inv;
+            if (e != 0.0f) y = e * rs * (ce * (d - logs + H) - t.g);
+            if (j == a) y += t.g;
+            y = y * scale / rt;
+            if (j == 0) {
+                b.dvalues[n] = t.dv * scale;
+#pragma unroll
+                for (int q = 0; q < kSums; ++q) acc[q] += (double)w * (double)t.sums[q];
+            }
+        } else if (j == 0) {
+            b.dvalues[n] = 0.0f;
+        }
+        if (j < A) ((T*)b.dlogits)[n * b.dstride + j] = (T)y;
+    }
+    loss_finish(b, s, acc, k.sums, k.done, lds);
+}
+
 // One workgroup per row, the row read again for every pass.
 template <class T>
-__global__ __launch_bounds__(kThreads) void loss_kernel(const Rows R, const Batch b, const double* __restrict__ part,
-                                                        double* __restrict__ sums)
+__global__ __launch_bounds__(kThreads) void loss_kernel(const Rows R, const Batch b, const Work k)
 {
     __shared__ double ldsd[kWaves];
     __shared__ float ldsf[kWaves];
-    const Shared3 s = loss_shared(b, part, ldsd);
+    const Shared3 s = loss_shared(b, k.part, k.parts);
     const int A = R.actions;
     double acc[kSums] = {};
     for (int64_t n = blockIdx.x; n < R.rows; n += gridDim.x) {
@@ -430,12 +595,9 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(const Rows R, const Batc
             continue;
         }
         const int a = (int)b.actions[n];
-        float top = -INFINITY, xa = 0.0f;
-        for (int i = threadIdx.x; i < A; i += kThreads) {
-            const float x = row(i);
-            top = x > top || x != x ? x : top;
-        }
-        xa = row(a);
+        float top = -INFINITY;
+        for (int i = threadIdx.x; i < A; i += kThreads) top = fmaxf(top, row(i));
+        const float xa = row(a);
         top = block_max(top, ldsf);
         const float rt = b.temperature;
         // d = (x - top) / T, sum of e = exp d, and of e d
@@ -450,8 +612,7 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(const Rows R, const Batc
         e1 = block_sum(e1, ldsf);
         const float logs = logf(e0), rs = 1.0f / e0;
         const float H = e0 > 0.0f ? logs - e1 * rs : e0 == 0.0f ? 0.0f : e0;
-        const float logp = e0 == 0.0f ? -INFINITY : dist(xa) - logs;
-        const RowTerms t = row_terms(b, s, n, logp, H);
+        const RowTerms t = row_terms(b, s, n, e0 == 0.0f ? -INFINITY : dist(xa) - logs, H);
         const float scale = w * s.inv;
         const float ce = b.entropy_coef;
         for (int i = threadIdx.x; i < A; i += kThreads) {
@@ -462,29 +623,11 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(const Rows R, const Batc
         }
         if (threadIdx.x == 0) {
             b.dvalues[n] = t.dv * scale;
-            for (int k = 0; k < kSums; ++k) acc[k] += (double)w * (double)t.sums[k];
+            for (int q = 0; q < kSums; ++q) acc[q] += (double)w * (double)t.sums[q];
         }
         __syncthreads();
     }
-    if (threadIdx.x == 0)
-        for (int k = 0; k < kSums; ++k) sums[(int64_t)blockIdx.x * kSums + k] = acc[k];
-}
-
-__global__ __launch_bounds__(kThreads) void loss_stats_kernel(const Batch b, const double* __restrict__ part,
-                                                              const double* __restrict__ sums, int64_t blocks)
-{
-    __shared__ double lds[kWaves];
-    const Shared3 s = loss_shared(b, part, lds);
-    double x[kSums];
-    for (int k = 0; k < kSums; ++k) {
-        x[k] = 0.0;
-        for (int64_t i = threadIdx.x; i < blocks; i += kThreads) x[k] += sums[i * kSums + k];
-        x[k] = block_sum_d(x[k], lds) * (double)s.inv;
-    }
-    if (threadIdx.x == 0) {
-        b.stats[0] = (float)(x[0] + (double)b.value_coef * x[1] - (double)b.entropy_coef * x[2]);
-        for (int k = 0; k < kSums; ++k) b.stats[k + 1] = (float)x[k];
-    }
+    loss_finish(b, s, acc, k.sums, k.done, ldsd);
 }
 
 // ---------------------------------------------------------------------------
@@ -511,10 +654,59 @@ Rows rows_of(const pictura_logits& l) { return Rows{l.data, l.stride, l.mask, l.
 
 unsigned blocks_for(int64_t rows) { return (unsigned)(rows < kMaxBlocks ? rows : kMaxBlocks); }
 
-// Row blocks of the loss: each leaves one set of partial sums.
-int64_t loss_blocks(int64_t rows) { return rows < 65536 ? rows : 65536; }
+// Lanes that hold a row of up to 64 actions.
+int group_lanes(int32_t actions) { return actions <= 8 ? 8 : actions <= 16 ? 16 : actions <= 32 ? 32 : 64; }
 
-uint64_t loss_bytes(int64_t rows) { return sizeof(double) * (uint64_t)(kMomentBlocks * 3 + loss_blocks(rows) * kSums); }
+// Workgroups of the loss: each leaves one set of partial sums.
+constexpr int64_t kLossBlocks = 4096;
+
+int64_t loss_blocks(int64_t rows, int32_t actions)
+{
+    const int64_t per = actions <= 64 ? kThreads / group_lanes(actions) : 1;
+    const int64_t b = (rows + per - 1) / per;
+    return b < 1 ? 1 : b < kLossBlocks ? b : kLossBlocks;
+}
+
+uint64_t loss_bytes(int64_t rows, int32_t actions)
+{
+    return sizeof(double) * (uint64_t)(kMomentBlocks * 3 + loss_blocks(rows, actions) * kSums) + 256;
+}
+
+template <class T>
+void launch_sample(const Rows& R, const Sampling& S, const float* uniform, int64_t* action, float* logp, hipStream_t s)
+{
+    if (R.actions <= 64) {
+        const bool filter = S.top_ks || S.top_ps || S.min_ps || (S.top_k > 0 && S.top_k < R.actions) || S.top_p < 1.0f || S.min_p > 0.0f;
+        const int G = group_lanes(R.actions);
+        const dim3 grid(blocks_for((R.rows * G + kThreads - 1) / kThreads)), block(kThreads);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, R, S, uniform, action, logp); };
+        if (filter) {
+            if (G == 8) go(sample_small_kernel<T, 8, true>);
+            else if (G == 16) go(sample_small_kernel<T, 16, true>);
+            else if (G == 32) go(sample_small_kernel<T, 32, true>);
+            else go(sample_small_kernel<T, 64, true>);
+        } else {
+            if (G == 8) go(sample_small_kernel<T, 8, false>);
+            else if (G == 16) go(sample_small_kernel<T, 16, false>);
+            else if (G == 32) go(sample_small_kernel<T, 32, false>);
+            else go(sample_small_kernel<T, 64, false>);
+        }
+        return;
+    }
+    hipLaunchKernelGGL(sample_kernel<T>, dim3(blocks_for(R.rows)), dim3(kThreads), 0, s, R, S, uniform, action, logp);
+}
+
+template <class T>
+void launch_loss(const Rows& R, const Batch& b, const Work& k, hipStream_t s)
+{
+    const dim3 grid((unsigned)loss_blocks(R.rows, R.actions)), block(kThreads);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, R, b, k); };
+    if (R.actions > 64) go(loss_kernel<T>);
+    else if (group_lanes(R.actions) == 8) go(loss_small_kernel<T, 8>);
+    else if (group_lanes(R.actions) == 16) go(loss_small_kernel<T, 16>);
+    else if (group_lanes(R.actions) == 32) go(loss_small_kernel<T, 32>);
+    else go(loss_small_kernel<T, 64>);
+}
 
 pictura_status launched() { return hipGetLastError() == hipSuccess ? PICTURA_OK : PICTURA_EDEVICE; }
 
@@ -540,20 +732,16 @@ pictura_status pictura_sample_actions(const pictura_logits* logits, const pictur
                      how->temperatures, how->top_ps, how->min_ps, how->top_ks};
     const Rows R = rows_of(*logits);
     hipStream_t s = (hipStream_t)stream;
-    const dim3 grid(blocks_for(R.rows)), block(kThreads);
-    if (logits->dtype == PICTURA_F32)
-        hipLaunchKernelGGL(sample_kernel<float>, grid, block, 0, s, R, S, uniform, out_action, out_logp);
-    else if (logits->dtype == PICTURA_BF16)
-        hipLaunchKernelGGL(sample_kernel<__bf16>, grid, block, 0, s, R, S, uniform, out_action, out_logp);
-    else
-        hipLaunchKernelGGL(sample_kernel<_Float16>, grid, block, 0, s, R, S, uniform, out_action, out_logp);
+    if (logits->dtype == PICTURA_F32) launch_sample<float>(R, S, uniform, out_action, out_logp, s);
+    else if (logits->dtype == PICTURA_BF16) launch_sample<__bf16>(R, S, uniform, out_action, out_logp, s);
+    else launch_sample<_Float16>(R, S, uniform, out_action, out_logp, s);
     return launched();
 }
 
 pictura_status pictura_policy_loss_workspace(int64_t rows, int32_t actions, uint64_t* bytes)
 {
     if (!bytes || rows < 0 || rows > 0x7FFFFFFFll || actions < 1 || actions > PICTURA_MAX_ACTIONS) return PICTURA_EINVAL;
-    *bytes = loss_bytes(rows);
+    *bytes = loss_bytes(rows, actions);
     return PICTURA_OK;
 }
 
@@ -563,7 +751,7 @@ pictura_status pictura_policy_loss(const pictura_logits* logits, const pictura_p
 {
     if (!logits_ok(logits) || !q || !out_stats || !aligned(out_stats, 4) || !workspace || !aligned(workspace, 256))
         return PICTURA_EINVAL;
-    if (workspace_bytes < loss_bytes(logits->rows)) return PICTURA_EINVAL;
+    if (workspace_bytes < loss_bytes(logits->rows, logits->actions)) return PICTURA_EINVAL;
     if (!(q->temperature > 0.0f) || !std::isfinite(q->temperature) || !(q->clip >= 0.0f) || std::isnan(q->value_clip) ||
         !std::isfinite(q->value_coef) || !std::isfinite(q->entropy_coef) || !(q->denominator >= 0.0f))
         return PICTURA_EINVAL;
@@ -582,17 +770,14 @@ pictura_status pictura_policy_loss(const pictura_logits* logits, const pictura_p
                   q->temperature, q->clip, q->value_clip, q->value_coef, q->entropy_coef, q->denominator,
                   q->normalize ? 1 : 0, out_stats, dlogits, dlogits_stride, dvalues};
     hipStream_t s = (hipStream_t)stream;
-    double* part = (double*)workspace;
-    double* sums = part + kMomentBlocks * 3;
-    const int64_t blocks = loss_blocks(R.rows);
-    hipLaunchKernelGGL(loss_moments_kernel, dim3(kMomentBlocks), dim3(kThreads), 0, s, b, R.rows, R.actions, part);
-    if (blocks > 0) {
-        const dim3 grid((unsigned)blocks), block(kThreads);
-        if (logits->dtype == PICTURA_F32) hipLaunchKernelGGL(loss_kernel<float>, grid, block, 0, s, R, b, part, sums);
-        else if (logits->dtype == PICTURA_BF16) hipLaunchKernelGGL(loss_kernel<__bf16>, grid, block, 0, s, R, b, part, sums);
-        else hipLaunchKernelGGL(loss_kernel<_Float16>, grid, block, 0, s, R, b, part, sums);
-    }
-    hipLaunchKernelGGL(loss_stats_kernel, dim3(1), dim3(kThreads), 0, s, b, part, sums, blocks);
+    uint32_t* done = (uint32_t*)workspace;
+    double* part = (double*)((char*)workspace + 256);
+    const int64_t parts = R.rows / kMomentRows < 1 ? 1 : R.rows / kMomentRows < kMomentBlocks ? R.rows / kMomentRows : kMomentBlocks;
+    const Work k{part, (int32_t)parts, part + 3 * kMomentBlocks, done};
+    hipLaunchKernelGGL(loss_moments_kernel, dim3((unsigned)parts), dim3(kThreads), 0, s, b, R.rows, R.actions, part, done);
+    if (logits->dtype == PICTURA_F32) launch_loss<float>(R, b, k, s);
+    else if (logits->dtype == PICTURA_BF16) launch_loss<__bf16>(R, b, k, s);
+    else launch_loss<_Float16>(R, b, k, s);
     return launched();
 }
 
