@@ -1,6 +1,7 @@
 // The policy's decisions: actions drawn from logits, and the clipped policy loss
 // over them with its gradient.
 #include <cmath>
+#include <type_traits>
 
 #include "pictura.h"
 #include "pictura_internal.h"
@@ -84,28 +85,50 @@ __device__ __forceinline__ V wave_sum(V x)
     return x;
 }
 
-// Sum over the workgroup, the same in every thread; lds[kWaves] is free again after
-// the next barrier.
-template <class V>
-__device__ __forceinline__ V block_sum(V x, V* lds)
+__device__ __forceinline__ float wave_max(float x)
 {
-    x = wave_sum(x);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = lds[0];
-    for (int w = 1; w < kWaves; ++w) x += lds[w];
+    for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
     return x;
 }
 
-__device__ __forceinline__ float block_max(float x, float* lds)
+// Running sum over the wave's lanes, this one included.
+template <class V>
+__device__ __forceinline__ V wave_scan(V x)
 {
-    for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const V o = __shfl_up(x, d);
+        if (lane >= d) x += o;
+    }
+    return x;
+}
+
+// Sum or maximum over a workgroup of NW waves, the same in every thread;
+// lds[NW] is free again after the next barrier.
+template <int NW, class V>
+__device__ __forceinline__ V block_sum(V x, V* lds)
+{
+    x = wave_sum(x);
+    if constexpr (NW == 1) return x;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
     x = lds[0];
-    for (int w = 1; w < kWaves; ++w) x = fmaxf(x, lds[w]);
+    for (int w = 1; w < NW; ++w) x += lds[w];
+    return x;
+}
+
+template <int NW>
+__device__ __forceinline__ float block_max(float x, float* lds)
+{
+    x = wave_max(x);
+    if constexpr (NW == 1) return x;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = lds[0];
+    for (int w = 1; w < NW; ++w) x = fmaxf(x, lds[w]);
     return x;
 }
 
@@ -116,67 +139,108 @@ struct Cut {
     uint32_t ties;
 };
 
-// The shortest prefix whose sum of add(key) reaches `need` > 0, of the actions
-// above `floor_key`; `need` is at most the sum of all of those.  Most significant
-// byte first: a histogram of the sums by byte, from the largest byte down to where
-// `need` is reached.
-template <class T, class Add>
-__device__ Cut find_cut(const Row<T>& row, int A, uint32_t floor_key, uint64_t need, Add add, unsigned long long* hist,
-                        uint64_t* told)
+// Histogram of whole numbers, its bins padded apart so that a lane can walk
+// through consecutive ones.
+__device__ __forceinline__ int padded(int bin) { return bin + (bin >> 4); }
+
+// First bin of `bins` (a multiple of 64) up to which the sums reach need, by one
+// wave; told = {bin, need less the bins before it}.  need is at most the sum of all.
+__device__ __forceinline__ void find_bin(const unsigned long long* hist, int bins, uint64_t need, uint64_t* told)
+{
+    const int lane = threadIdx.x & 63, per = bins / 64;
+    uint64_t mine = 0;
+    for (int i = 0; i < per; ++i) mine += hist[padded(lane * per + i)];
+    const uint64_t run = wave_scan(mine);
+    const uint64_t hit = __ballot(run >= need);
+    if (lane == __ffsll((unsigned long long)hit) - 1) {
+        uint64_t left = need - (run - mine);
+        int i = 0;
+        for (; i < per - 1; ++i) {
+            const uint64_t h = hist[padded(lane * per + i)];
+            if (h >= left) break;
+            left -= h;
+        }
+        told[0] = (uint64_t)(lane * per + i);
+        told[1] = left;
+    }
+}
+
+// The shortest prefix whose sum of add(x) reaches `need` > 0, of the logits above
+// floor_key that each(f) hands to f, spread over the threads; need is at most the
+// sum of all of those.  By bytes of the key, from the highest: a histogram of the
+// sums, largest byte first, up to where need is reached.
+template <class Each, class Add>
+__device__ Cut find_cut(Each each, uint32_t floor_key, uint64_t need, Add add, unsigned long long* hist, uint64_t* told)
 {
     uint32_t prefix = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
-        hist[threadIdx.x] = 0;
         __syncthreads();
-        for (int i = threadIdx.x; i < A; i += kThreads) {
-            const float x = row(i);
+        for (int i = threadIdx.x; i < padded(256); i += blockDim.x) hist[i] = 0;
+        __syncthreads();
+        each([&](float x) {
             const uint32_t k = order_key(x);
-            if (x == -INFINITY || k <= floor_key || (shift < 24 && (k >> (shift + 8)) != prefix)) continue;
-            atomicAdd(&hist[(k >> shift) & 255u], (unsigned long long)add(x));
-        }
+            if (x == -INFINITY || k <= floor_key || (shift < 24 && (k >> (shift + 8)) != prefix)) return;
+            atomicAdd(&hist[padded(255 - ((k >> shift) & 255u))], (unsigned long long)add(x));
+        });
         __syncthreads();
-        if (threadIdx.x == 0) {
-            uint64_t sum = 0;
-            int b = 255;
-            for (; b > 0 && sum + hist[b] < need; --b) sum += hist[b];
-            told[0] = (uint64_t)b;
-            told[1] = need - sum;
-        }
+        if (threadIdx.x < 64) find_bin(hist, 256, need, told);
         __syncthreads();
-        prefix = prefix << 8 | (uint32_t)told[0];
+        prefix = prefix << 8 | (255u - (uint32_t)told[0]);
         need = told[1];
-        __syncthreads();
     }
     const uint64_t one = add(key_value(prefix));
+    __syncthreads();
     return Cut{prefix, (uint32_t)((need + one - 1) / one)};
 }
 
-// One workgroup per row, the row read again for every pass.
+// A row's settings.
+struct RowSampling {
+    float temp, top_p;
+    int32_t top_k;
+    uint32_t least;   // smallest weight that min_p keeps
+    __device__ __forceinline__ RowSampling(const Sampling& S, int64_t n)
+    {
+        temp = S.temperatures ? S.temperatures[n] : S.temperature;
+        top_k = S.top_ks ? S.top_ks[n] : S.top_k;
+        top_p = S.top_ps ? S.top_ps[n] : S.top_p;
+        const float min_p = S.min_ps ? S.min_ps[n] : S.min_p;
+        least = temp > 0.0f ? (uint32_t)ceilf(fminf(fmaxf(min_p, 0.0f), 1.0f) * kOne) : 0u;
+    }
+};
+
+// ---------------------------------------------------------------------------
+// rows of any length: read again for every pass
+// ---------------------------------------------------------------------------
+
+constexpr int kLongWaves = 16;
+
 template <class T>
-__global__ __launch_bounds__(kThreads) void sample_kernel(const Rows R, const Sampling S,
-                                                          const float* __restrict__ uniform,
-                                                          int64_t* __restrict__ out_action, float* __restrict__ out_logp)
+__global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows R, const Sampling S,
+                                                                      const float* __restrict__ uniform,
+                                                                      int64_t* __restrict__ out_action,
+                                                                      float* __restrict__ out_logp)
 {
-    __shared__ unsigned long long hist[256];
-    __shared__ uint64_t told[2], lds64[kWaves];
-    __shared__ float ldsf[kWaves];
-    __shared__ uint32_t wties[kWaves];
+    constexpr int NW = kLongWaves, NT = NW * 64;
+    __shared__ unsigned long long hist[256 + 16];
+    __shared__ uint64_t told[2], lds64[NW];
+    __shared__ float ldsf[NW];
+    __shared__ uint32_t wties[NW];
     const int A = R.actions;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int64_t n = blockIdx.x; n < R.rows; n += gridDim.x) {
         const Row<T> row(R, n);
-        const float temp = S.temperatures ? S.temperatures[n] : S.temperature;
-        const int32_t k = S.top_ks ? S.top_ks[n] : S.top_k;
-        const float top_p = S.top_ps ? S.top_ps[n] : S.top_p, min_p = S.min_ps ? S.min_ps[n] : S.min_p;
+        const RowSampling q(S, n);
+        auto each = [&](auto f) {
+            for (int i = threadIdx.x; i < A; i += NT) f(row(i));
+        };
         // the largest logit; a NaN or +inf, or a temperature without meaning, makes no draw
-        float top = -INFINITY, bad = temp >= 0.0f ? 0.0f : 1.0f;
-        for (int i = threadIdx.x; i < A; i += kThreads) {
-            const float x = row(i);
+        float top = -INFINITY, bad = q.temp >= 0.0f ? 0.0f : 1.0f;
+        each([&](float x) {
             top = fmaxf(top, x);
             if (!(x < INFINITY)) bad = 1.0f;
-        }
-        top = block_max(top, ldsf);
-        bad = block_max(bad, ldsf);
+        });
+        top = block_max<NW>(top, ldsf);
+        bad = block_max<NW>(bad, ldsf);
         if (bad != 0.0f || top == -INFINITY) {
             if (threadIdx.x == 0) {
                 out_action[n] = -1;
@@ -184,38 +248,36 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const Rows R, const Sa
             }
             continue;
         }
-        auto weight = [&](float x) { return temp > 0.0f ? weight_of(x, top, temp) : x == top ? 1u : 0u; };
+        auto weight = [&](float x) { return q.temp > 0.0f ? weight_of(x, top, q.temp) : x == top ? 1u : 0u; };
         Cut cut{0u, 0u};
-        if (temp == 0.0f) {
+        if (q.temp == 0.0f) {
             cut = Cut{order_key(top), 1u};
         } else {
-            if (k > 0 && k < A) {
-                uint32_t some = 0;
-                for (int i = threadIdx.x; i < A; i += kThreads) some += row(i) != -INFINITY;
-                if (block_sum((uint64_t)some, lds64) > (uint64_t)k)
-                    cut = find_cut(row, A, 0u, (uint64_t)k, [](float) { return 1u; }, hist, told);
+            if (q.top_k > 0 && q.top_k < A) {
+                uint64_t some = 0;
+                each([&](float x) { some += x != -INFINITY; });
+                if (block_sum<NW>(some, lds64) > (uint64_t)q.top_k)
+                    cut = find_cut(each, 0u, (uint64_t)q.top_k, [](float) { return 1u; }, hist, told);
             }
-            if (top_p < 1.0f) {
+            if (q.top_p < 1.0f) {
                 uint64_t above = 0;
-                for (int i = threadIdx.x; i < A; i += kThreads) {
-                    const float x = row(i);
+                each([&](float x) {
                     if (order_key(x) > cut.key) above += weight(x);
-                }
-                above = block_sum(above, lds64);
+                });
+                above = block_sum<NW>(above, lds64);
                 const uint64_t one = cut.ties ? weight(key_value(cut.key)) : 0;
-                uint64_t need = share(above + one * cut.ties, cut31(top_p));
+                uint64_t need = share(above + one * cut.ties, cut31(q.top_p));
                 if (need < 1) need = 1;
-                if (need <= above) cut = find_cut(row, A, cut.key, need, weight, hist, told);
+                if (need <= above) cut = find_cut(each, cut.key, need, weight, hist, told);
                 else cut.ties = (uint32_t)((need - above + one - 1) / one);
             }
         }
-        const uint32_t least = temp > 0.0f ? (uint32_t)ceilf(fminf(fmaxf(min_p, 0.0f), 1.0f) * kOne) : 0u;
         auto kept = [&](float x) {
             const uint32_t w = weight(x);
-            return w < least ? 0u : w;
+            return w < q.least ? 0u : w;
         };
         // each wave its part of the row; the ties belong to the first waves that have them
-        const int per = ((A + kThreads - 1) / kThreads) * 64, i0 = min(A, wave * per), i1 = min(A, i0 + per);
+        const int per = ((A + NT - 1) / NT) * 64, i0 = min(A, wave * per), i1 = min(A, i0 + per);
         uint64_t sum = 0;
         uint32_t ties = 0;
         for (int i = i0 + lane; i < i1; i += 64) {
@@ -234,32 +296,22 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const Rows R, const Sa
             wties[wave] = ties;
         }
         __syncthreads();
-        uint64_t total = 0;
-        uint32_t quota = cut.ties;
-        uint64_t wsum[kWaves];
-        uint32_t wquota[kWaves];
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            wquota[w] = min(quota, wties[w]);
-            quota -= wquota[w];
-            wsum[w] = lds64[w] + (uint64_t)wquota[w] * one;
-            total += wsum[w];
+        // where this wave's part of the running sum begins, and how many ties are left for it
+        uint64_t total = 0, base = 0, mine = 0;
+        uint32_t quota = cut.ties, left = 0;
+        for (int w = 0; w < NW; ++w) {
+            const uint32_t take = min(quota, wties[w]);
+            const uint64_t part = lds64[w] + (uint64_t)take * one;
+            if (w == wave) {
+                base = total;
+                mine = part;
+                left = take;
+            }
+            quota -= take;
+            total += part;
         }
         const uint64_t target = share(total, cut31(uniform[n]));
-        // the wave whose part holds the target walks through it
-        uint64_t base = 0;
-        uint32_t left = 0;
-        bool mine = false;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            if (w == wave) {
-                mine = base <= target && target < base + wsum[w];
-                left = wquota[w];
-                if (mine) break;
-            }
-            base += wsum[w];
-        }
-        if (mine) {
+        if (base <= target && target - base < mine) {   // one wave: it walks through its part
             for (int b = i0; b < i1; b += 64) {
                 const int i = b + lane;
                 const float x = i < i1 ? row(i) : -INFINITY;
@@ -268,11 +320,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const Rows R, const Sa
                 const uint64_t same = __ballot(tie);
                 const uint32_t before = __popcll(same & ((1ull << lane) - 1ull));
                 const uint32_t w = x == -INFINITY ? 0u : key > cut.key || (tie && before < left) ? kept(x) : 0u;
-                uint64_t run = w;
-                for (int d = 1; d < 64; d <<= 1) {
-                    const uint64_t o = __shfl_up(run, d);
-                    if (lane >= d) run += o;
-                }
+                const uint64_t run = wave_scan((uint64_t)w);
                 const uint64_t hit = __ballot(base + run > target);
                 if (hit) {
                     if (lane == __ffsll((unsigned long long)hit) - 1) {
@@ -289,6 +337,405 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const Rows R, const Sa
     }
 }
 
+// ---------------------------------------------------------------------------
+// rows that fit a workgroup's registers
+// ---------------------------------------------------------------------------
+
+// Bits of a number up to 2^31 as a float, which keeps the order.
+__device__ __forceinline__ uint32_t float_bits(uint32_t w) { return __float_as_uint((float)w); }
+
+constexpr uint32_t kOneBits = 0x4F000000u;   // of 2^31
+
+// A row of V-element vectors at 16-byte addresses: vector q covers the elements
+// from q V - shift on, the first and the last only in part.
+template <class T>
+struct VecRow {
+    static constexpr int V = 16 / sizeof(T);
+    Row<T> row;
+    int A, shift, vectors;
+    bool mask_vec;   // the mask's bytes of a vector lie at a V-byte address
+    __device__ __forceinline__ VecRow(const Rows& r, int64_t n) : row(r, n), A(r.actions)
+    {
+        shift = (int)(reinterpret_cast<uintptr_t>(row.x) / sizeof(T)) & (V - 1);
+        vectors = (A + shift + V - 1) / V;
+        mask_vec = ((reinterpret_cast<uintptr_t>(row.mask) - shift) & (V - 1)) == 0;
+    }
+    __device__ __forceinline__ int first(int q) const { return q * V - shift; }
+    __device__ __forceinline__ void load(int q, float* x) const
+    {
+        const int i0 = first(q);
+        if (q < vectors && i0 >= 0 && i0 + V <= A) {
+            struct alignas(16) Vec { T v[V]; };
+            const Vec t = *reinterpret_cast<const Vec*>(row.x + i0);
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = (float)t.v[v] + 0.0f;
+            if (row.mask) {
+                if (mask_vec) {
+                    struct alignas(V) Bytes { uint8_t v[V]; };
+                    const Bytes k = *reinterpret_cast<const Bytes*>(row.mask + i0);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) x[v] = k.v[v] ? x[v] : -INFINITY;
+                } else {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) x[v] = row.mask[i0 + v] ? x[v] : -INFINITY;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = q < vectors && i0 + v >= 0 && i0 + v < A ? row(i0 + v) : -INFINITY;
+        }
+    }
+};
+
+// One workgroup of NW waves per row, ITEMS logits to a thread, read once.  Each
+// wave holds a stretch of the row, 64 vectors at a time, so that running sums by
+// index go wave by wave.
+template <class T, int NW, int ITEMS, bool kFilter>
+__global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const Sampling S,
+                                                             const float* __restrict__ uniform,
+                                                             int64_t* __restrict__ out_action,
+                                                             float* __restrict__ out_logp)
+{
+    constexpr int V = VecRow<T>::V, NV = ITEMS / V;
+    constexpr int kBins = NW == 1 ? 256 : 1024, kList = NW == 1 ? 1024 : 2048;
+    __shared__ unsigned long long hist[kFilter ? kBins + kBins / 16 : 1];
+    __shared__ uint32_t list[kFilter ? kList : NW];
+    __shared__ uint32_t listed;
+    __shared__ uint64_t told[2], lds64[NW];
+    __shared__ float ldsf[2 * NW];
+    __shared__ uint32_t wties[NW];
+    const int A = R.actions;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int64_t n = blockIdx.x; n < R.rows; n += gridDim.x) {
+        const VecRow<T> vr(R, n);
+        const Row<T>& row = vr.row;
+        const RowSampling q(S, n);
+        const float u = uniform[n];
+        const int per = (vr.vectors + NW * 64 - 1) / (NW * 64);   // vectors of a thread, at most NV
+        const int q0 = wave * per * 64 + lane;                    // its first one
+        float x[NV][V];
+        float top = -INFINITY;
+        bool odd = !(q.temp >= 0.0f);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (j < per) {
+                vr.load(q0 + j * 64, x[j]);
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; ++v) x[j][v] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (j < per) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    top = fmaxf(top, x[j][v]);
+                    odd |= !(x[j][v] < INFINITY);
+                }
+            }
+        // the largest logit; a NaN or +inf, or a temperature without meaning, makes no draw
+        top = block_max<NW>(top, ldsf);
+        const float bad = block_max<NW>(odd ? 1.0f : 0.0f, ldsf + NW);
+        if (bad != 0.0f || top == -INFINITY) {
+            if (threadIdx.x == 0) {
+                out_action[n] = -1;
+                out_logp[n] = NAN;
+            }
+            continue;
+        }
+        auto weight = [&](float y) { return weight_of(y, top, q.temp); };
+        // Above the cut: logits over `over` and the first `ties` of those equal to it.
+        // by_weight: the registers hold the weights (they keep the order of the logits, up
+        // to equal ones), of which those above `wover` are kept.
+        float over = -INFINITY;
+        uint32_t ties = 0, wover = 0;
+        bool by_weight = true;
+        uint32_t (&w)[NV][V] = reinterpret_cast<uint32_t (&)[NV][V]>(x);
+        if (q.temp == 0.0f) {
+            over = top;
+            ties = 1;
+            by_weight = false;
+        } else {
+            Cut cut{0u, 0u};
+            bool cut_k = false;
+            if constexpr (kFilter) {
+                uint64_t some = 0;
+                if (q.top_k > 0 && q.top_k < A) {
+#pragma unroll
+                    for (int j = 0; j < NV; ++j)
+                        if (j < per) {
+#pragma unroll
+                            for (int v = 0; v < V; ++v) some += x[j][v] != -INFINITY;
+                        }
+                    cut_k = block_sum<NW>(some, lds64) > (uint64_t)q.top_k;
+                }
+                if (cut_k) {
+                    by_weight = false;
+                    // The top_k-th largest of the vectors' maxima is no more than the top_k-th
+                    // largest logit: a histogram of them bounds the logits that can be kept
+                    // from below, and those few are listed.
+                    float low = INFINITY;
+                    float vmax[NV];
+#pragma unroll
+                    for (int j = 0; j < NV; ++j) {
+                        vmax[j] = x[j][0];
+#pragma unroll
+                        for (int v = 1; v < V; ++v) vmax[j] = fmaxf(vmax[j], x[j][v]);
+                        if (vmax[j] > -INFINITY) low = fminf(low, vmax[j]);
+                    }
+                    low = -block_max<NW>(-low, ldsf);
+                    const float scale = (float)kBins / (top - low);   // (no range: NaN, and all in bin 0)
+                    auto bin = [&](float y) { return (int)fminf(fmaxf((top - y) * scale, 0.0f), (float)(kBins - 1)); };
+                    for (int i = threadIdx.x; i < kBins + kBins / 16; i += NW * 64) hist[i] = 0;
+                    if (threadIdx.x == 0) listed = 0;
+                    __syncthreads();
+                    uint64_t vecs = 0;
+#pragma unroll
+                    for (int j = 0; j < NV; ++j)
+                        if (vmax[j] > -INFINITY) {
+                            ++vecs;
+                            atomicAdd(&hist[padded(bin(vmax[j]))], 1ull);
+                        }
+                    vecs = block_sum<NW>(vecs, lds64);
+                    int edge = kBins - 1;
+                    if (vecs >= (uint64_t)q.top_k) {
+                        if (NW == 1) __syncthreads();
+                        if (threadIdx.x < 64) find_bin(hist, kBins, (uint64_t)q.top_k, told);
+                        __syncthreads();
+                        edge = (int)told[0];
+                    }
+#pragma unroll
+                    for (int j = 0; j < NV; ++j)
+                        if (vmax[j] > -INFINITY && bin(vmax[j]) <= edge) {
+#pragma unroll
+                            for (int v = 0; v < V; ++v)
+                                if (x[j][v] > -INFINITY && bin(x[j][v]) <= edge) {
+                                    const uint32_t at = atomicAdd(&listed, 1u);
+                                    if (at < kList) list[at] = __float_as_uint(x[j][v]);
+                                }
+                        }
+                    __syncthreads();
+                    const uint32_t C = listed;
+                    auto from_list = [&](auto f) {
+                        for (uint32_t i = threadIdx.x; i < C; i += NW * 64) f(__uint_as_float(list[i]));
+                    };
+                    auto from_row = [&](auto f) {
+                        for (int i = threadIdx.x; i < A; i += NW * 64) f(row(i));
+                    };
+                    auto narrow = [&](auto each) {
+                        cut = find_cut(each, 0u, (uint64_t)q.top_k, [](float) { return 1u; }, hist, told);
+                        if (q.top_p < 1.0f) {
+                            uint64_t above = 0;
+                            each([&](float y) {
+                                if (order_key(y) > cut.key) above += weight(y);
+                            });
+                            above = block_sum<NW>(above, lds64);
+                            const uint64_t one = weight(key_value(cut.key));
+                            uint64_t need = share(above + one * cut.ties, cut31(q.top_p));
+                            if (need < 1) need = 1;
+                            if (need <= above) cut = find_cut(each, cut.key, need, weight, hist, told);
+                            else cut.ties = (uint32_t)((need - above + one - 1) / one);
+                        }
+                    };
+                    if (C <= kList) narrow(from_list);
+                    else narrow(from_row);
+                    over = key_value(cut.key);
+                    ties = cut.ties;
+                }
+            }
+            if (by_weight) {
+                uint64_t sum = 0;
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    if (j < per) {
+#pragma unroll
+                        for (int v = 0; v < V; ++v) {
+                            w[j][v] = weight(x[j][v]);
+                            sum += w[j][v];
+                        }
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < V; ++v) w[j][v] = 0;
+                    }
+                }
+                if constexpr (kFilter) {
+                    if (q.top_p < 1.0f) {
+                        sum = block_sum<NW>(sum, lds64);
+                        uint64_t need = share(sum, cut31(q.top_p));
+                        if (need < 1) need = 1;
+                        // All weights up to `small` together stay below sum - need, so the prefix
+                        // ends above it.
+                        const uint32_t small = (uint32_t)((float)(sum - need) / (float)A * 0.999f);
+                        const uint32_t range = kOneBits - float_bits(small + 1);
+                        constexpr int kLog = NW == 1 ? 8 : 10;
+                        const int drop = max(0, 32 - __clz((int)range) - kLog);
+                        auto bin = [&](uint32_t y) { return (int)((kOneBits - float_bits(y)) >> drop); };
+                        for (int i = threadIdx.x; i < kBins + kBins / 16; i += NW * 64) hist[i] = 0;
+                        if (threadIdx.x == 0) listed = 0;
+                        __syncthreads();
+#pragma unroll
+                        for (int j = 0; j < NV; ++j)
+                            if (j < per) {
+#pragma unroll
+                                for (int v = 0; v < V; ++v)
+                                    if (w[j][v] > small) atomicAdd(&hist[padded(bin(w[j][v]))], (unsigned long long)w[j][v]);
+                            }
+                        __syncthreads();
+                        if (threadIdx.x < 64) find_bin(hist, kBins, need, told);
+                        __syncthreads();
+                        const int edge = (int)told[0];
+                        const uint64_t rest = told[1];
+#pragma unroll
+                        for (int j = 0; j < NV; ++j)
+                            if (j < per) {
+#pragma unroll
+                                for (int v = 0; v < V; ++v)
+                                    if (w[j][v] > small && bin(w[j][v]) == edge) {
+                                        const uint32_t at = atomicAdd(&listed, 1u);
+                                        if (at < kList) list[at] = (uint32_t)(vr.first(q0 + j * 64) + v);
+                                    }
+                            }
+                        __syncthreads();
+                        const uint32_t C = listed;
+                        if (C <= kList) {
+                            for (uint32_t i = threadIdx.x; i < C; i += NW * 64) list[i] = __float_as_uint(row((int)list[i]));
+                            cut = find_cut(
+                                [&](auto f) {
+                                    for (uint32_t i = threadIdx.x; i < C; i += NW * 64) f(__uint_as_float(list[i]));
+                                },
+                                0u, rest, weight, hist, told);
+                        } else {
+                            cut = find_cut(
+                                [&](auto f) {
+                                    for (int i = threadIdx.x; i < A; i += NW * 64) f(row(i));
+                                },
+                                0u, need, weight, hist, told);
+                        }
+                        over = key_value(cut.key);
+                        ties = cut.ties;
+                        wover = weight(over);
+                    }
+                }
+            }
+        }
+        // What is kept of element (j, v): its weight, and whether it is one of the ties.
+        auto look = [&](int j, int v, uint32_t& wt, bool& tie) {
+            if (by_weight) {
+                const uint32_t y = w[j][v];
+                wt = y > wover ? y : 0u;
+                tie = false;
+                if (y == wover && ties) {
+                    const float z = row(vr.first(q0 + j * 64) + v);
+                    if (z >= over) wt = y;
+                    tie = z == over;
+                }
+            } else {
+                const float y = x[j][v];
+                tie = y == over;
+                wt = 0;
+                if (y >= over) wt = q.temp > 0.0f ? weight(y) : 1u;
+            }
+            if (wt < q.least) wt = 0;
+        };
+        uint64_t sum = 0;
+        uint32_t same = 0, one = 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (j < per) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    uint32_t wt;
+                    bool tie;
+                    look(j, v, wt, tie);
+                    if (tie) {
+                        ++same;
+                        one = wt;
+                    } else {
+                        sum += wt;
+                    }
+                }
+            }
+        sum = wave_sum(sum);
+        same = wave_sum(same);
+        // (of equal logits the weight is one: a wave with a tie knows it)
+        for (int d = 32; d; d >>= 1) one = max(one, (uint32_t)__shfl_xor((int)one, d));
+        uint64_t total = sum + (uint64_t)min(ties, same) * one, base = 0, mine = total;
+        uint32_t left = min(ties, same);
+        if constexpr (NW > 1) {
+            __syncthreads();
+            if (lane == 0) {
+                lds64[wave] = sum;
+                wties[wave] = same;
+                list[wave] = one;
+            }
+            __syncthreads();
+            total = 0;
+            uint32_t quota = ties;
+            for (int k = 0; k < NW; ++k) {
+                const uint32_t take = min(quota, wties[k]);
+                const uint64_t part = lds64[k] + (uint64_t)take * list[k];
+                if (k == wave) {
+                    base = total;
+                    mine = part;
+                    left = take;
+                }
+                quota -= take;
+                total += part;
+            }
+        }
+        const uint64_t target = share(total, cut31(u));
+        if (base <= target && target - base < mine) {   // one wave: it walks through its part
+            bool found = false;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (j < per && !found) {
+                    uint32_t wt[V], before = 0;
+                    bool tie[V];
+                    uint32_t held = 0;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        look(j, v, wt[v], tie[v]);
+                        held += tie[v];
+                    }
+                    uint32_t inside = 0;
+                    if (__any(held != 0)) {
+                        const uint32_t run = wave_scan(held);
+                        before = run - held;
+                        inside = (uint32_t)__shfl((int)run, 63);
+                    }
+                    uint64_t here = 0;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        if (tie[v] && before++ >= left) wt[v] = 0;
+                        here += wt[v];
+                    }
+                    const uint64_t run = wave_scan(here);
+                    const uint64_t hit = __ballot(base + run > target);
+                    if (hit) {
+                        if (lane == __ffsll((unsigned long long)hit) - 1) {
+                            uint64_t c = base + run - here;
+                            bool out = false;
+#pragma unroll
+                            for (int v = 0; v < V; ++v) {
+                                c += wt[v];
+                                if (!out && c > target) {
+                                    out = true;
+                                    out_action[n] = vr.first(q0 + j * 64) + v;
+                                    out_logp[n] = logf((float)wt[v] / (float)total);
+                                }
+                            }
+                        }
+                        found = true;
+                    }
+                    base += __shfl(run, 63);
+                    left -= min(left, inside);
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
 
 // ---------------------------------------------------------------------------
 // few actions: a row in a group of G lanes
@@ -422,9 +869,9 @@ __global__ __launch_bounds__(kThreads) void loss_moments_kernel(const Batch b, i
         w1 += w * a;
         w2 += w * a * a;
     }
-    w0 = block_sum(w0, lds);
-    w1 = block_sum(w1, lds);
-    w2 = block_sum(w2, lds);
+    w0 = block_sum<kWaves>(w0, lds);
+    w1 = block_sum<kWaves>(w1, lds);
+    w2 = block_sum<kWaves>(w2, lds);
     if (threadIdx.x == 0) {
         part[blockIdx.x] = w0;
         part[kMomentBlocks + blockIdx.x] = w1;
@@ -502,7 +949,7 @@ __device__ void loss_finish(const Batch& b, const Shared3& s, const double* acc,
     __shared__ uint32_t last;
     double total[kSums];
 #pragma unroll
-    for (int k = 0; k < kSums; ++k) total[k] = block_sum(acc[k], lds);
+    for (int k = 0; k < kSums; ++k) total[k] = block_sum<kWaves>(acc[k], lds);
     if (threadIdx.x == 0) {
         for (int k = 0; k < kSums; ++k) sums[(int64_t)blockIdx.x * kSums + k] = total[k];
         __threadfence();
@@ -516,7 +963,7 @@ __device__ void loss_finish(const Batch& b, const Shared3& s, const double* acc,
 #pragma unroll
         for (int k = 0; k < kSums; ++k) x[k] += sums[(int64_t)i * kSums + k];
 #pragma unroll
-    for (int k = 0; k < kSums; ++k) x[k] = block_sum(x[k], lds) * (double)s.inv;
+    for (int k = 0; k < kSums; ++k) x[k] = block_sum<kWaves>(x[k], lds) * (double)s.inv;
     if (threadIdx.x == 0) {
         b.stats[0] = (float)(x[0] + (double)b.value_coef * x[1] - (double)b.entropy_coef * x[2]);
         for (int k = 0; k < kSums; ++k) b.stats[k + 1] = (float)x[k];
@@ -598,7 +1045,7 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(const Rows R, const Batc
         float top = -INFINITY;
         for (int i = threadIdx.x; i < A; i += kThreads) top = fmaxf(top, row(i));
         const float xa = row(a);
-        top = block_max(top, ldsf);
+        top = block_max<kWaves>(top, ldsf);
         const float rt = b.temperature;
         // d = (x - top) / T, sum of e = exp d, and of e d
         auto dist = [&](float x) { return x == -INFINITY ? -INFINITY : (x - top) / rt; };
@@ -608,8 +1055,8 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(const Rows R, const Batc
             e0 += e;
             if (e != 0.0f) e1 += e * d;
         }
-        e0 = block_sum(e0, ldsf);
-        e1 = block_sum(e1, ldsf);
+        e0 = block_sum<kWaves>(e0, ldsf);
+        e1 = block_sum<kWaves>(e1, ldsf);
         const float logs = logf(e0), rs = 1.0f / e0;
         const float H = e0 > 0.0f ? logs - e1 * rs : e0 == 0.0f ? 0.0f : e0;
         const RowTerms t = row_terms(b, s, n, e0 == 0.0f ? -INFINITY : dist(xa) - logs, H);
@@ -693,7 +1140,27 @@ void launch_sample(const Rows& R, const Sampling& S, const float* uniform, int64
         }
         return;
     }
-    hipLaunchKernelGGL(sample_kernel<T>, dim3(blocks_for(R.rows)), dim3(kThreads), 0, s, R, S, uniform, action, logp);
+    const bool filter = S.top_ks || S.top_ps || (S.top_k > 0 && S.top_k < R.actions) || S.top_p < 1.0f;
+    // slots a row takes: rows that do not start at 16-byte addresses begin inside a vector
+    constexpr int V = 16 / sizeof(T);
+    const bool even = aligned(R.data, 16) && (R.rows == 1 || R.stride % V == 0);
+    const int slots = R.actions + (even ? 0 : V - 1);
+    const dim3 grid(blocks_for(R.rows));
+    auto go = [&](auto kernel, int waves) {
+        hipLaunchKernelGGL(kernel, grid, dim3(waves * 64), 0, s, R, S, uniform, action, logp);
+    };
+    auto pick = [&](auto f) {
+        constexpr bool F = decltype(f)::value;
+        if (slots <= 64 * 16) go(sample_row_kernel<T, 1, 16, F>, 1);
+        else if (slots <= 4 * 64 * 16) go(sample_row_kernel<T, 4, 16, F>, 4);
+        else if (slots <= 4 * 64 * 32) go(sample_row_kernel<T, 4, 32, F>, 4);
+        else if (slots <= 16 * 64 * 16) go(sample_row_kernel<T, 16, 16, F>, 16);
+        else if (slots <= 16 * 64 * 32) go(sample_row_kernel<T, 16, 32, F>, 16);
+        else if (slots <= 16 * 64 * 72) go(sample_row_kernel<T, 16, 72, F>, 16);
+        else go(sample_long_kernel<T>, kLongWaves);
+    };
+    if (filter) pick(std::true_type{});
+    else pick(std::false_type{});
 }
 
 template <class T>
