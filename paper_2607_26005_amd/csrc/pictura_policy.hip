@@ -59,12 +59,31 @@ __device__ __forceinline__ float key_value(uint32_t k)
     return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
 }
 
-// Weight of a logit against the row's largest.
-__device__ __forceinline__ uint32_t weight_of(float x, float top, float temp)
-{
-    if (x == -INFINITY) return 0;
-    return (uint32_t)rintf(expf((x - top) / temp) * kOne);
-}
+// Weight of a logit against the row's largest.  The quotient (x - top) / T is the
+// correctly rounded one, by a reciprocal and two corrections: with y = 1 / T rounded, q0 =
+// d y is within two units of d / T, q1 = q0 + (d - q0 T) y within one, and from there
+// one more step rounds correctly (Markstein, "Computation of elementary functions on
+// the IBM RISC System/6000 processor", 1990).  Powers of two keep T and d where nothing
+// underflows that could show, and quotients below -200 (an exponential of zero) are
+// cut there, so that -inf gives weight 0.
+struct Weights {
+    float top, scale, temp, y, least;
+    __device__ __forceinline__ Weights(float top_, float t) : top(top_)
+    {
+        scale = t < 0x1p-64f ? 0x1p100f : t > 0x1p64f ? 0x1p-64f : 1.0f;
+        temp = t * scale;
+        y = 1.0f / temp;
+        least = -200.0f * temp;
+    }
+    __device__ __forceinline__ uint32_t operator()(float x) const
+    {
+        const float d = fmaxf((x - top) * scale, least);
+        float q = d * y;
+        q = fmaf(fmaf(-q, temp, d), y, q);
+        q = fmaf(fmaf(-q, temp, d), y, q);
+        return (uint32_t)rintf(expf(q) * kOne);
+    }
+};
 
 // floor(total * m / 2^31) for m < 2^31
 __device__ __forceinline__ uint64_t share(uint64_t total, uint32_t m)
@@ -78,45 +97,98 @@ __device__ __forceinline__ uint32_t cut31(float x)
     return (uint32_t)(fminf(fmaxf(x, 0.0f), 1.0f - 0x1p-24f) * kOne);
 }
 
+// Lanes exchange through the vector unit's own data paths (row shifts and
+// broadcasts): some 60 cycles for a reduction over the wave, where six shuffles
+// through LDS take ten times that.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint32_t lanes(uint32_t old, uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)x, kCtrl, kRows, 0xf, false);
+}
+
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint64_t lanes(uint64_t old, uint64_t x)
+{
+    return (uint64_t)lanes<kCtrl, kRows>((uint32_t)(old >> 32), (uint32_t)(x >> 32)) << 32 |
+           lanes<kCtrl, kRows>((uint32_t)old, (uint32_t)x);
+}
+
+template <int kCtrl, int kRows>
+__device__ __forceinline__ float lanes(float old, float x)
+{
+    return __uint_as_float(lanes<kCtrl, kRows>(__float_as_uint(old), __float_as_uint(x)));
+}
+
+// x of this lane combined with those before it: within 16 lanes (L = 16), or
+// over the wave (L = 64).  `none` is what lanes that do not exist hold.
+template <int L, class V, class F>
+__device__ __forceinline__ V lane_scan(V x, V none, F f)
+{
+    x = f(x, lanes<0x111, 0xf>(none, x));
+    if constexpr (L > 2) x = f(x, lanes<0x112, 0xf>(none, x));
+    if constexpr (L > 4) x = f(x, lanes<0x114, 0xf>(none, x));
+    if constexpr (L > 8) x = f(x, lanes<0x118, 0xf>(none, x));
+    if constexpr (L > 16) x = f(x, lanes<0x142, 0xa>(none, x));
+    if constexpr (L > 32) x = f(x, lanes<0x143, 0xc>(none, x));
+    return x;
+}
+
+__device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
+
+__device__ __forceinline__ uint64_t from_lane(uint64_t x, int lane)
+{
+    return (uint64_t)from_lane((uint32_t)(x >> 32), lane) << 32 | from_lane((uint32_t)x, lane);
+}
+
+__device__ __forceinline__ float from_lane(float x, int lane) { return __uint_as_float(from_lane(__float_as_uint(x), lane)); }
+
+struct Add {
+    template <class V>
+    __device__ __forceinline__ V operator()(V a, V b) const { return a + b; }
+};
+
+struct Max {
+    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+
+// Running sum over the wave's lanes, this one included; and the whole sum or maximum.
 template <class V>
-__device__ __forceinline__ V wave_sum(V x)
+__device__ __forceinline__ V wave_scan(V x) { return lane_scan<64>(x, (V)0, Add{}); }
+
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) { return from_lane(wave_scan(x), 63); }
+
+__device__ __forceinline__ uint64_t wave_sum(uint64_t x) { return from_lane(wave_scan(x), 63); }
+
+__device__ __forceinline__ double wave_sum(double x)
 {
     for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
     return x;
 }
 
-__device__ __forceinline__ float wave_max(float x)
+__device__ __forceinline__ float wave_sum(float x)
 {
-    for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
-    return x;
+    return from_lane(lane_scan<64>(x, 0.0f, Add{}), 63);
 }
 
-// Running sum over the wave's lanes, this one included.
-template <class V>
-__device__ __forceinline__ V wave_scan(V x)
-{
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const V o = __shfl_up(x, d);
-        if (lane >= d) x += o;
-    }
-    return x;
-}
+__device__ __forceinline__ float wave_max(float x) { return from_lane(lane_scan<64>(x, -INFINITY, Max{}), 63); }
 
-// Sum or maximum over a workgroup of NW waves, the same in every thread;
-// lds[NW] is free again after the next barrier.
+// Sum or maximum over a workgroup of NW waves, the same in every thread.  lds[NW]
+// must not be in use by the threads before this call's barrier: two calls in a
+// row take two arrays.
 template <int NW, class V>
 __device__ __forceinline__ V block_sum(V x, V* lds)
 {
     x = wave_sum(x);
     if constexpr (NW == 1) return x;
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
-    x = lds[0];
-    for (int w = 1; w < NW; ++w) x += lds[w];
-    return x;
+    if constexpr (sizeof(V) == 8 && !std::is_integral<V>::value) {
+        x = lds[0];
+        for (int w = 1; w < NW; ++w) x += lds[w];
+        return x;
+    } else {
+        return from_lane(lane_scan<NW>(lds[threadIdx.x & (NW - 1)], (V)0, Add{}), NW - 1);
+    }
 }
 
 template <int NW>
@@ -124,12 +196,9 @@ __device__ __forceinline__ float block_max(float x, float* lds)
 {
     x = wave_max(x);
     if constexpr (NW == 1) return x;
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
-    x = lds[0];
-    for (int w = 1; w < NW; ++w) x = fmaxf(x, lds[w]);
-    return x;
+    return from_lane(lane_scan<NW>(lds[threadIdx.x & (NW - 1)], -INFINITY, Max{}), NW - 1);
 }
 
 // A prefix of the actions ordered by logit, then index: everything above `key`
@@ -143,26 +212,32 @@ struct Cut {
 // through consecutive ones.
 __device__ __forceinline__ int padded(int bin) { return bin + (bin >> 4); }
 
-// First bin of `bins` (a multiple of 64) up to which the sums reach need, by one
-// wave; told = {bin, need less the bins before it}.  need is at most the sum of all.
-__device__ __forceinline__ void find_bin(const unsigned long long* hist, int bins, uint64_t need, uint64_t* told)
+// First bin of `bins` (a multiple of 64, at most 4096) up to which the sums reach
+// need, by one wave; told = {bin, need less the bins before it}.  need is at most the
+// sum of all.
+template <class H>
+__device__ __forceinline__ void find_bin(const H* hist, int bins, uint64_t need, uint64_t* told)
 {
     const int lane = threadIdx.x & 63, per = bins / 64;
     uint64_t mine = 0;
     for (int i = 0; i < per; ++i) mine += hist[padded(lane * per + i)];
-    const uint64_t run = wave_scan(mine);
-    const uint64_t hit = __ballot(run >= need);
-    if (lane == __ffsll((unsigned long long)hit) - 1) {
-        uint64_t left = need - (run - mine);
-        int i = 0;
-        for (; i < per - 1; ++i) {
-            const uint64_t h = hist[padded(lane * per + i)];
-            if (h >= left) break;
-            left -= h;
-        }
-        told[0] = (uint64_t)(lane * per + i);
-        told[1] = left;
+    uint64_t run = wave_scan(mine);
+    const int at = __ffsll((unsigned long long)__ballot(run >= need)) - 1;
+    need -= from_lane(run - mine, at);
+    mine = lane < per ? hist[padded(at * per + lane)] : 0;   // that lane's bins, one each
+    run = wave_scan(mine);
+    const int in = __ffsll((unsigned long long)__ballot(run >= need)) - 1;
+    if (lane == in) {
+        told[0] = (uint64_t)(at * per + in);
+        told[1] = need - (run - mine);
     }
+}
+
+// Smallest count of weights `one` that reaches `need` (below 2^52, a quotient up
+// to 2^20): exact in fp64.
+__device__ __forceinline__ uint32_t ties_for(uint64_t need, uint64_t one)
+{
+    return (uint32_t)ceil((double)need / (double)one);
 }
 
 // The shortest prefix whose sum of add(x) reaches `need` > 0, of the logits above
@@ -188,9 +263,8 @@ __device__ Cut find_cut(Each each, uint32_t floor_key, uint64_t need, Add add, u
         prefix = prefix << 8 | (255u - (uint32_t)told[0]);
         need = told[1];
     }
-    const uint64_t one = add(key_value(prefix));
     __syncthreads();
-    return Cut{prefix, (uint32_t)((need + one - 1) / one)};
+    return Cut{prefix, ties_for(need, add(key_value(prefix)))};
 }
 
 // A row's settings.
@@ -222,8 +296,8 @@ __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows
 {
     constexpr int NW = kLongWaves, NT = NW * 64;
     __shared__ unsigned long long hist[256 + 16];
-    __shared__ uint64_t told[2], lds64[NW];
-    __shared__ float ldsf[NW];
+    __shared__ uint64_t told[2], lds64[3 * NW];
+    __shared__ float ldsf[2 * NW];
     __shared__ uint32_t wties[NW];
     const int A = R.actions;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -240,15 +314,17 @@ __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows
             if (!(x < INFINITY)) bad = 1.0f;
         });
         top = block_max<NW>(top, ldsf);
-        bad = block_max<NW>(bad, ldsf);
+        bad = block_max<NW>(bad, ldsf + NW);
         if (bad != 0.0f || top == -INFINITY) {
             if (threadIdx.x == 0) {
                 out_action[n] = -1;
                 out_logp[n] = NAN;
             }
+            __syncthreads();
             continue;
         }
-        auto weight = [&](float x) { return q.temp > 0.0f ? weight_of(x, top, q.temp) : x == top ? 1u : 0u; };
+        const Weights of(top, q.temp);
+        auto weight = [&](float x) { return q.temp > 0.0f ? of(x) : x == top ? 1u : 0u; };
         Cut cut{0u, 0u};
         if (q.temp == 0.0f) {
             cut = Cut{order_key(top), 1u};
@@ -264,12 +340,12 @@ __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows
                 each([&](float x) {
                     if (order_key(x) > cut.key) above += weight(x);
                 });
-                above = block_sum<NW>(above, lds64);
+                above = block_sum<NW>(above, lds64 + NW);
                 const uint64_t one = cut.ties ? weight(key_value(cut.key)) : 0;
                 uint64_t need = share(above + one * cut.ties, cut31(q.top_p));
                 if (need < 1) need = 1;
                 if (need <= above) cut = find_cut(each, cut.key, need, weight, hist, told);
-                else cut.ties = (uint32_t)((need - above + one - 1) / one);
+                else cut.ties = ties_for(need - above, one);
             }
         }
         auto kept = [&](float x) {
@@ -290,9 +366,8 @@ __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows
         sum = wave_sum(sum);
         ties = wave_sum(ties);
         const uint32_t one = cut.ties ? kept(key_value(cut.key)) : 0u;
-        __syncthreads();
         if (lane == 0) {
-            lds64[wave] = sum;
+            lds64[2 * NW + wave] = sum;
             wties[wave] = ties;
         }
         __syncthreads();
@@ -301,7 +376,7 @@ __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows
         uint32_t quota = cut.ties, left = 0;
         for (int w = 0; w < NW; ++w) {
             const uint32_t take = min(quota, wties[w]);
-            const uint64_t part = lds64[w] + (uint64_t)take * one;
+            const uint64_t part = lds64[2 * NW + w] + (uint64_t)take * one;
             if (w == wave) {
                 base = total;
                 mine = part;
@@ -387,302 +462,417 @@ struct VecRow {
     }
 };
 
+constexpr int kRank = 256;   // candidates that are ranked by counting
+
+// Shared memory of a row's workgroup.
+template <int NW, bool kFilter>
+struct RowLds {
+    static constexpr int kBins = NW == 1 ? 256 : 1024, kList = NW == 1 ? 1024 : 2048;
+    unsigned long long hist[kFilter ? kBins + kBins / 16 : 1];
+    uint64_t sums[4][NW], told[4];
+    uint64_t before[kFilter ? kRank : 1];       // weight of the candidates above each
+    float list[kFilter ? kList + 4 : 1];        // candidates
+    uint32_t weight[kFilter ? kRank + 4 : 1];   // theirs
+    uint32_t equal[kFilter ? kRank : 1];        // candidates equal to each
+    uint32_t listed;
+    float maxima[3][NW];
+    uint32_t ties[NW];
+};
+
+constexpr uint32_t kTie = 0xFFFFFFFFu;   // in a weight's place: equal to the cut
+
 // One workgroup of NW waves per row, ITEMS logits to a thread, read once.  Each
 // wave holds a stretch of the row, 64 vectors at a time, so that running sums by
-// index go wave by wave.
+// index go wave by wave.  A cut is found (the value that the kept prefix ends
+// with, and how many of the logits equal to it are kept), then the registers hold
+// the weights that are left, then the draw goes by their sums.
 template <class T, int NW, int ITEMS, bool kFilter>
 __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const Sampling S,
                                                              const float* __restrict__ uniform,
                                                              int64_t* __restrict__ out_action,
                                                              float* __restrict__ out_logp)
 {
-    constexpr int V = VecRow<T>::V, NV = ITEMS / V;
-    constexpr int kBins = NW == 1 ? 256 : 1024, kList = NW == 1 ? 1024 : 2048;
-    __shared__ unsigned long long hist[kFilter ? kBins + kBins / 16 : 1];
-    __shared__ uint32_t list[kFilter ? kList : NW];
-    __shared__ uint32_t listed;
-    __shared__ uint64_t told[2], lds64[NW];
-    __shared__ float ldsf[2 * NW];
-    __shared__ uint32_t wties[NW];
+    constexpr int V = VecRow<T>::V, NV = ITEMS / V, NT = NW * 64;
+    using Lds = RowLds<NW, kFilter>;
+    __shared__ alignas(16) Lds lds;
     const int A = R.actions;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int64_t n = blockIdx.x; n < R.rows; n += gridDim.x) {
         const VecRow<T> vr(R, n);
         const Row<T>& row = vr.row;
         const RowSampling q(S, n);
         const float u = uniform[n];
-        const int per = (vr.vectors + NW * 64 - 1) / (NW * 64);   // vectors of a thread, at most NV
-        const int q0 = wave * per * 64 + lane;                    // its first one
-        float x[NV][V];
+        const int per = (vr.vectors + NT - 1) / NT;   // vectors of a thread, at most NV
+        const int q0 = wave * per * 64 + lane;        // its first one
+        // bits of the logits, later the weights
+        uint32_t r[NV][V];
         float top = -INFINITY;
         bool odd = !(q.temp >= 0.0f);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            if (j < per) {
-                vr.load(q0 + j * 64, x[j]);
-            } else {
+            float x[V];
 #pragma unroll
-                for (int v = 0; v < V; ++v) x[j][v] = -INFINITY;
-            }
+            for (int v = 0; v < V; ++v) x[v] = -INFINITY;
+            if (j < per) vr.load(q0 + j * 64, x);
+#pragma unroll
+            for (int v = 0; v < V; ++v) r[j][v] = __float_as_uint(x[v]);
         }
+        auto x = [&](int j, int v) { return __uint_as_float(r[j][v]); };
+        auto vmax = [&](int j) {
+            float m = x(j, 0);
+#pragma unroll
+            for (int v = 1; v < V; ++v) m = fmaxf(m, x(j, v));
+            return m;
+        };
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if (j < per) {
+                top = fmaxf(top, vmax(j));
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    top = fmaxf(top, x[j][v]);
-                    odd |= !(x[j][v] < INFINITY);
-                }
+                for (int v = 0; v < V; ++v) odd |= !(x(j, v) < INFINITY);
             }
         // the largest logit; a NaN or +inf, or a temperature without meaning, makes no draw
-        top = block_max<NW>(top, ldsf);
-        const float bad = block_max<NW>(odd ? 1.0f : 0.0f, ldsf + NW);
-        if (bad != 0.0f || top == -INFINITY) {
+        top = block_max<NW>(odd ? INFINITY : top, lds.maxima[0]);
+        if (top == INFINITY || top == -INFINITY) {
             if (threadIdx.x == 0) {
                 out_action[n] = -1;
                 out_logp[n] = NAN;
             }
+            __syncthreads();
             continue;
         }
-        auto weight = [&](float y) { return weight_of(y, top, q.temp); };
-        // Above the cut: logits over `over` and the first `ties` of those equal to it.
-        // by_weight: the registers hold the weights (they keep the order of the logits, up
-        // to equal ones), of which those above `wover` are kept.
+        const Weights weight(top, q.temp);
+        // The cut: logits over `over` are kept, and the first `ties` of those equal to it.
         float over = -INFINITY;
-        uint32_t ties = 0, wover = 0;
-        bool by_weight = true;
-        uint32_t (&w)[NV][V] = reinterpret_cast<uint32_t (&)[NV][V]>(x);
+        uint32_t ties = 0;
+        bool by_logit = false;   // the cut comes from the logits, before any weight
         if (q.temp == 0.0f) {
             over = top;
             ties = 1;
-            by_weight = false;
-        } else {
-            Cut cut{0u, 0u};
+            by_logit = true;
+        }
+        // the cut among lds.list[0 .. C): by count, or by weight, up to `need`
+        auto rank_list = [&](uint32_t C, bool weigh) {
+            if (threadIdx.x < 4) {
+                lds.list[C + threadIdx.x] = -INFINITY;
+                lds.weight[C + threadIdx.x] = 0;
+            }
+            if (weigh)
+                for (uint32_t i = threadIdx.x; i < C; i += NT) lds.weight[i] = weight(lds.list[i]);
+            __syncthreads();
+        };
+        if constexpr (kFilter) {
             bool cut_k = false;
-            if constexpr (kFilter) {
-                uint64_t some = 0;
-                if (q.top_k > 0 && q.top_k < A) {
+            if (!by_logit && q.top_k > 0 && q.top_k < A) {
+                uint32_t some = 0;
 #pragma unroll
-                    for (int j = 0; j < NV; ++j)
-                        if (j < per) {
+                for (int j = 0; j < NV; ++j)
+                    if (j < per) {
 #pragma unroll
-                            for (int v = 0; v < V; ++v) some += x[j][v] != -INFINITY;
-                        }
-                    cut_k = block_sum<NW>(some, lds64) > (uint64_t)q.top_k;
-                }
-                if (cut_k) {
-                    by_weight = false;
-                    // The top_k-th largest of the vectors' maxima is no more than the top_k-th
-                    // largest logit: a histogram of them bounds the logits that can be kept
-                    // from below, and those few are listed.
-                    float low = INFINITY;
-                    float vmax[NV];
-#pragma unroll
-                    for (int j = 0; j < NV; ++j) {
-                        vmax[j] = x[j][0];
-#pragma unroll
-                        for (int v = 1; v < V; ++v) vmax[j] = fmaxf(vmax[j], x[j][v]);
-                        if (vmax[j] > -INFINITY) low = fminf(low, vmax[j]);
+                        for (int v = 0; v < V; ++v) some += x(j, v) != -INFINITY;
                     }
-                    low = -block_max<NW>(-low, ldsf);
-                    const float scale = (float)kBins / (top - low);   // (no range: NaN, and all in bin 0)
-                    auto bin = [&](float y) { return (int)fminf(fmaxf((top - y) * scale, 0.0f), (float)(kBins - 1)); };
-                    for (int i = threadIdx.x; i < kBins + kBins / 16; i += NW * 64) hist[i] = 0;
-                    if (threadIdx.x == 0) listed = 0;
-                    __syncthreads();
-                    uint64_t vecs = 0;
+                cut_k = block_sum<NW>((uint64_t)some, lds.sums[0]) > (uint64_t)q.top_k;
+            }
+            if (cut_k) {
+                by_logit = true;
+                // The top_k-th largest of the vectors' maxima is no more than the top_k-th
+                // largest logit: a histogram of them bounds the logits that can be kept
+                // from below, and those few are listed.
+                float low = INFINITY;
+                uint32_t vecs = 0;
 #pragma unroll
-                    for (int j = 0; j < NV; ++j)
-                        if (vmax[j] > -INFINITY) {
+                for (int j = 0; j < NV; ++j)
+                    if (j < per) {
+                        const float m = vmax(j);
+                        if (m > -INFINITY) {
+                            low = fminf(low, m);
                             ++vecs;
-                            atomicAdd(&hist[padded(bin(vmax[j]))], 1ull);
                         }
-                    vecs = block_sum<NW>(vecs, lds64);
-                    int edge = kBins - 1;
-                    if (vecs >= (uint64_t)q.top_k) {
-                        if (NW == 1) __syncthreads();
-                        if (threadIdx.x < 64) find_bin(hist, kBins, (uint64_t)q.top_k, told);
-                        __syncthreads();
-                        edge = (int)told[0];
                     }
+                for (int i = threadIdx.x; i < Lds::kBins + Lds::kBins / 16; i += NT) lds.hist[i] = 0;
+                if (threadIdx.x == 0) lds.listed = 0;
+                low = -block_max<NW>(-low, lds.maxima[1]);
+                if (NW == 1) __syncthreads();
+                const float scale = (float)Lds::kBins / (top - low);   // (no range: NaN, and all in bin 0)
+                auto bin = [&](float y) { return (int)fminf(fmaxf((top - y) * scale, 0.0f), (float)(Lds::kBins - 1)); };
 #pragma unroll
-                    for (int j = 0; j < NV; ++j)
-                        if (vmax[j] > -INFINITY && bin(vmax[j]) <= edge) {
+                for (int j = 0; j < NV; ++j)
+                    if (j < per) {
+                        const float m = vmax(j);
+                        if (m > -INFINITY) atomicAdd(&lds.hist[padded(bin(m))], 1ull);
+                    }
+                const bool enough = block_sum<NW>((uint64_t)vecs, lds.sums[1]) >= (uint64_t)q.top_k;
+                int edge = Lds::kBins - 1;
+                if (enough) {
+                    if (NW == 1) __syncthreads();
+                    if (wave == 0) find_bin(lds.hist, Lds::kBins, (uint64_t)q.top_k, lds.told);
+                    __syncthreads();
+                    edge = (int)lds.told[0];
+                }
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (j < per) {
+                        const float m = vmax(j);
+                        if (m > -INFINITY && bin(m) <= edge) {
 #pragma unroll
                             for (int v = 0; v < V; ++v)
-                                if (x[j][v] > -INFINITY && bin(x[j][v]) <= edge) {
-                                    const uint32_t at = atomicAdd(&listed, 1u);
-                                    if (at < kList) list[at] = __float_as_uint(x[j][v]);
+                                if (x(j, v) > -INFINITY && bin(x(j, v)) <= edge) {
+                                    const uint32_t at = atomicAdd(&lds.listed, 1u);
+                                    if (at < Lds::kList) lds.list[at] = x(j, v);
                                 }
                         }
+                    }
+                __syncthreads();
+                const uint32_t C = lds.listed;
+                if (C <= kRank) {
+                    // how many and how much is above each, and equal to it
+                    rank_list(C, q.top_p < 1.0f);
+                    for (uint32_t i = threadIdx.x; i < C; i += NT) {
+                        const float xi = lds.list[i];
+                        uint32_t above = 0, equal = 0;
+                        uint64_t before = 0;
+                        for (uint32_t k = 0; k < C; k += 4) {
+                            const float4 y = *reinterpret_cast<const float4*>(lds.list + k);
+                            const uint4 w = *reinterpret_cast<const uint4*>(lds.weight + k);
+                            above += (y.x > xi) + (y.y > xi) + (y.z > xi) + (y.w > xi);
+                            equal += (y.x == xi) + (y.y == xi) + (y.z == xi) + (y.w == xi);
+                            before += (uint64_t)(y.x > xi ? w.x : 0u) + (y.y > xi ? w.y : 0u);
+                            before += (uint64_t)(y.z > xi ? w.z : 0u) + (y.w > xi ? w.w : 0u);
+                        }
+                        lds.before[i] = before;
+                        lds.equal[i] = equal;
+                        if (above < (uint32_t)q.top_k && (uint32_t)q.top_k <= above + equal) {
+                            // (equal ones write the same)
+                            lds.told[0] = (uint64_t)__float_as_uint(xi);
+                            lds.told[1] = (uint64_t)((uint32_t)q.top_k - above);
+                            lds.told[2] = before + (uint64_t)((uint32_t)q.top_k - above) * lds.weight[i];
+                        }
+                    }
                     __syncthreads();
-                    const uint32_t C = listed;
-                    auto from_list = [&](auto f) {
-                        for (uint32_t i = threadIdx.x; i < C; i += NW * 64) f(__uint_as_float(list[i]));
-                    };
-                    auto from_row = [&](auto f) {
-                        for (int i = threadIdx.x; i < A; i += NW * 64) f(row(i));
-                    };
+                    over = __uint_as_float((uint32_t)lds.told[0]);
+                    ties = (uint32_t)lds.told[1];
+                    if (q.top_p < 1.0f) {
+                        uint64_t need = share(lds.told[2], cut31(q.top_p));
+                        if (need < 1) need = 1;
+                        __syncthreads();
+                        for (uint32_t i = threadIdx.x; i < C; i += NT) {
+                            const float xi = lds.list[i];
+                            const uint32_t equal = xi == over ? ties : lds.equal[i];
+                            const uint64_t before = lds.before[i];
+                            if (xi >= over && before < need && need <= before + (uint64_t)equal * lds.weight[i]) {
+                                lds.told[0] = (uint64_t)__float_as_uint(xi);
+                                lds.told[1] = ties_for(need - before, lds.weight[i]);
+                            }
+                        }
+                        __syncthreads();
+                        over = __uint_as_float((uint32_t)lds.told[0]);
+                        ties = (uint32_t)lds.told[1];
+                    }
+                } else {
                     auto narrow = [&](auto each) {
-                        cut = find_cut(each, 0u, (uint64_t)q.top_k, [](float) { return 1u; }, hist, told);
+                        Cut cut = find_cut(each, 0u, (uint64_t)q.top_k, [](float) { return 1u; }, lds.hist, lds.told);
                         if (q.top_p < 1.0f) {
                             uint64_t above = 0;
                             each([&](float y) {
                                 if (order_key(y) > cut.key) above += weight(y);
                             });
-                            above = block_sum<NW>(above, lds64);
+                            above = block_sum<NW>(above, lds.sums[2]);
                             const uint64_t one = weight(key_value(cut.key));
                             uint64_t need = share(above + one * cut.ties, cut31(q.top_p));
                             if (need < 1) need = 1;
-                            if (need <= above) cut = find_cut(each, cut.key, need, weight, hist, told);
-                            else cut.ties = (uint32_t)((need - above + one - 1) / one);
-                        }
-                    };
-                    if (C <= kList) narrow(from_list);
-                    else narrow(from_row);
-                    over = key_value(cut.key);
-                    ties = cut.ties;
-                }
-            }
-            if (by_weight) {
-                uint64_t sum = 0;
-#pragma unroll
-                for (int j = 0; j < NV; ++j) {
-                    if (j < per) {
-#pragma unroll
-                        for (int v = 0; v < V; ++v) {
-                            w[j][v] = weight(x[j][v]);
-                            sum += w[j][v];
-                        }
-                    } else {
-#pragma unroll
-                        for (int v = 0; v < V; ++v) w[j][v] = 0;
-                    }
-                }
-                if constexpr (kFilter) {
-                    if (q.top_p < 1.0f) {
-                        sum = block_sum<NW>(sum, lds64);
-                        uint64_t need = share(sum, cut31(q.top_p));
-                        if (need < 1) need = 1;
-                        // All weights up to `small` together stay below sum - need, so the prefix
-                        // ends above it.
-                        const uint32_t small = (uint32_t)((float)(sum - need) / (float)A * 0.999f);
-                        const uint32_t range = kOneBits - float_bits(small + 1);
-                        constexpr int kLog = NW == 1 ? 8 : 10;
-                        const int drop = max(0, 32 - __clz((int)range) - kLog);
-                        auto bin = [&](uint32_t y) { return (int)((kOneBits - float_bits(y)) >> drop); };
-                        for (int i = threadIdx.x; i < kBins + kBins / 16; i += NW * 64) hist[i] = 0;
-                        if (threadIdx.x == 0) listed = 0;
-                        __syncthreads();
-#pragma unroll
-                        for (int j = 0; j < NV; ++j)
-                            if (j < per) {
-#pragma unroll
-                                for (int v = 0; v < V; ++v)
-                                    if (w[j][v] > small) atomicAdd(&hist[padded(bin(w[j][v]))], (unsigned long long)w[j][v]);
-                            }
-                        __syncthreads();
-                        if (threadIdx.x < 64) find_bin(hist, kBins, need, told);
-                        __syncthreads();
-                        const int edge = (int)told[0];
-                        const uint64_t rest = told[1];
-#pragma unroll
-                        for (int j = 0; j < NV; ++j)
-                            if (j < per) {
-#pragma unroll
-                                for (int v = 0; v < V; ++v)
-                                    if (w[j][v] > small && bin(w[j][v]) == edge) {
-                                        const uint32_t at = atomicAdd(&listed, 1u);
-                                        if (at < kList) list[at] = (uint32_t)(vr.first(q0 + j * 64) + v);
-                                    }
-                            }
-                        __syncthreads();
-                        const uint32_t C = listed;
-                        if (C <= kList) {
-                            for (uint32_t i = threadIdx.x; i < C; i += NW * 64) list[i] = __float_as_uint(row((int)list[i]));
-                            cut = find_cut(
-                                [&](auto f) {
-                                    for (uint32_t i = threadIdx.x; i < C; i += NW * 64) f(__uint_as_float(list[i]));
-                                },
-                                0u, rest, weight, hist, told);
-                        } else {
-                            cut = find_cut(
-                                [&](auto f) {
-                                    for (int i = threadIdx.x; i < A; i += NW * 64) f(row(i));
-                                },
-                                0u, need, weight, hist, told);
+                            if (need <= above) cut = find_cut(each, cut.key, need, weight, lds.hist, lds.told);
+                            else cut.ties = ties_for(need - above, one);
                         }
                         over = key_value(cut.key);
                         ties = cut.ties;
-                        wover = weight(over);
-                    }
+                    };
+                    if (C <= Lds::kList)
+                        narrow([&](auto f) {
+                            for (uint32_t i = threadIdx.x; i < C; i += NT) f(lds.list[i]);
+                        });
+                    else
+                        narrow([&](auto f) {
+                            for (int i = threadIdx.x; i < A; i += NT) f(row(i));
+                        });
                 }
             }
         }
-        // What is kept of element (j, v): its weight, and whether it is one of the ties.
-        auto look = [&](int j, int v, uint32_t& wt, bool& tie) {
-            if (by_weight) {
-                const uint32_t y = w[j][v];
-                wt = y > wover ? y : 0u;
-                tie = false;
-                if (y == wover && ties) {
-                    const float z = row(vr.first(q0 + j * 64) + v);
-                    if (z >= over) wt = y;
-                    tie = z == over;
+        uint32_t one = 0;   // weight of a tie
+        if (by_logit) {
+            one = q.temp > 0.0f ? weight(over) : 1u;
+            if (one < q.least) one = 0;
+            // few vectors hold a kept logit
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j < per) {
+                    if (vmax(j) >= over) {
+#pragma unroll
+                        for (int v = 0; v < V; ++v) {
+                            const float y = x(j, v);
+                            const uint32_t w = y > over ? weight(y) : 0u;
+                            r[j][v] = y == over ? kTie : w < q.least ? 0u : w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < V; ++v) r[j][v] = 0u;
+                    }
                 }
-            } else {
-                const float y = x[j][v];
-                tie = y == over;
-                wt = 0;
-                if (y >= over) wt = q.temp > 0.0f ? weight(y) : 1u;
+        } else {
+            uint64_t sum = 0;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j < per) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        r[j][v] = weight(x(j, v));
+                        sum += r[j][v];
+                    }
+                }
+            uint32_t wover = 0;   // weights above it are kept, and some of those equal to it
+            if constexpr (kFilter) {
+                if (q.top_p < 1.0f) {
+                    for (int i = threadIdx.x; i < Lds::kBins + Lds::kBins / 16; i += NT) lds.hist[i] = 0;
+                    if (threadIdx.x == 0) lds.listed = 0;
+                    sum = block_sum<NW>(sum, lds.sums[1]);
+                    if (NW == 1) __syncthreads();
+                    uint64_t need = share(sum, cut31(q.top_p));
+                    if (need < 1) need = 1;
+                    // All weights up to `small` together stay below sum - need, so the prefix
+                    // ends above it.
+                    const uint32_t small = (uint32_t)((float)(sum - need) / (float)A * 0.999f);
+                    const uint32_t range = kOneBits - float_bits(small + 1);
+                    constexpr int kLog = NW == 1 ? 8 : 10;
+                    const int drop = max(0, 32 - __clz((int)range) - kLog);
+#pragma unroll
+                    for (int j = 0; j < NV; ++j)
+                        if (j < per) {
+#pragma unroll
+                            for (int v = 0; v < V; ++v)
+                                if (r[j][v] > small)
+                                    atomicAdd(&lds.hist[padded((int)((kOneBits - float_bits(r[j][v])) >> drop))],
+                                              (unsigned long long)r[j][v]);
+                        }
+                    __syncthreads();
+                    if (wave == 0) find_bin(lds.hist, Lds::kBins, need, lds.told);
+                    __syncthreads();
+                    const uint32_t edge = (uint32_t)lds.told[0];
+                    const uint64_t rest = lds.told[1];
+                    // the bin's logits (the order of logits and of weights is one, up to equal
+                    // weights of different logits)
+                    const uint32_t most = kOneBits - (edge << drop), least = most - ((1u << drop) - 1u);
+#pragma unroll
+                    for (int j = 0; j < NV; ++j)
+                        if (j < per) {
+#pragma unroll
+                            for (int v = 0; v < V; ++v) {
+                                const uint32_t f = float_bits(r[j][v]);
+                                if (r[j][v] > small && f <= most && f >= least) {
+                                    const uint32_t at = atomicAdd(&lds.listed, 1u);
+                                    if (at < Lds::kList) lds.list[at] = row(vr.first(q0 + j * 64) + v);
+                                }
+                            }
+                        }
+                    __syncthreads();
+                    const uint32_t C = lds.listed;
+                    if (C <= kRank) {
+                        rank_list(C, true);
+                        for (uint32_t i = threadIdx.x; i < C; i += NT) {
+                            const float xi = lds.list[i];
+                            uint32_t equal = 0;
+                            uint64_t before = 0;
+                            for (uint32_t k = 0; k < C; k += 4) {
+                                const float4 y = *reinterpret_cast<const float4*>(lds.list + k);
+                                const uint4 w = *reinterpret_cast<const uint4*>(lds.weight + k);
+                                equal += (y.x == xi) + (y.y == xi) + (y.z == xi) + (y.w == xi);
+                                before += (uint64_t)(y.x > xi ? w.x : 0u) + (y.y > xi ? w.y : 0u);
+                                before += (uint64_t)(y.z > xi ? w.z : 0u) + (y.w > xi ? w.w : 0u);
+                            }
+                            if (before < rest && rest <= before + (uint64_t)equal * lds.weight[i]) {
+                                lds.told[2] = (uint64_t)__float_as_uint(xi);
+                                lds.told[3] = ties_for(rest - before, lds.weight[i]);
+                            }
+                        }
+                        __syncthreads();
+                        over = __uint_as_float((uint32_t)lds.told[2]);
+                        ties = (uint32_t)lds.told[3];
+                    } else {
+                        Cut cut;
+                        if (C <= Lds::kList)
+                            cut = find_cut(
+                                [&](auto f) {
+                                    for (uint32_t i = threadIdx.x; i < C; i += NT) f(lds.list[i]);
+                                },
+                                0u, rest, weight, lds.hist, lds.told);
+                        else
+                            cut = find_cut(
+                                [&](auto f) {
+                                    for (int i = threadIdx.x; i < A; i += NT) f(row(i));
+                                },
+                                0u, need, weight, lds.hist, lds.told);
+                        over = key_value(cut.key);
+                        ties = cut.ties;
+                    }
+                    wover = weight(over);
+                }
             }
-            if (wt < q.least) wt = 0;
-        };
+            one = wover < q.least ? 0u : wover;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j < per) {
+                    bool look = false;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        look |= kFilter && r[j][v] == wover;
+                        r[j][v] = r[j][v] < q.least || r[j][v] < wover ? 0u : r[j][v];
+                    }
+                    if (kFilter && wover != 0 && look) {   // which of them the logits tell
+#pragma unroll
+                        for (int v = 0; v < V; ++v) {
+                            const int i = vr.first(q0 + j * 64) + v;
+                            if (r[j][v] == wover && i >= 0 && i < A) {
+                                const float y = row(i);
+                                if (y == over) r[j][v] = kTie;
+                                else if (y < over) r[j][v] = 0;
+                            }
+                        }
+                    }
+                }
+        }
         uint64_t sum = 0;
-        uint32_t same = 0, one = 0;
+        uint32_t same = 0;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if (j < per) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    uint32_t wt;
-                    bool tie;
-                    look(j, v, wt, tie);
-                    if (tie) {
-                        ++same;
-                        one = wt;
-                    } else {
-                        sum += wt;
-                    }
+                    const bool tie = kTie == r[j][v];
+                    same += tie;
+                    sum += tie ? 0u : r[j][v];
                 }
             }
         sum = wave_sum(sum);
         same = wave_sum(same);
-        // (of equal logits the weight is one: a wave with a tie knows it)
-        for (int d = 32; d; d >>= 1) one = max(one, (uint32_t)__shfl_xor((int)one, d));
-        uint64_t total = sum + (uint64_t)min(ties, same) * one, base = 0, mine = total;
-        uint32_t left = min(ties, same);
-        if constexpr (NW > 1) {
-            __syncthreads();
+        uint64_t total, base = 0, mine;
+        uint32_t left;
+        if constexpr (NW == 1) {
+            left = min(ties, same);
+            total = mine = sum + (uint64_t)left * one;
+        } else {
             if (lane == 0) {
-                lds64[wave] = sum;
-                wties[wave] = same;
-                list[wave] = one;
+                lds.sums[3][wave] = sum;
+                lds.ties[wave] = same;
             }
             __syncthreads();
-            total = 0;
-            uint32_t quota = ties;
-            for (int k = 0; k < NW; ++k) {
-                const uint32_t take = min(quota, wties[k]);
-                const uint64_t part = lds64[k] + (uint64_t)take * list[k];
-                if (k == wave) {
-                    base = total;
-                    mine = part;
-                    left = take;
-                }
-                quota -= take;
-                total += part;
-            }
+            // lane w: wave w; the ties belong to the first waves that have them
+            const uint32_t has = lds.ties[lane & (NW - 1)];
+            const uint32_t before = lane_scan<NW>(has, 0u, Add{}) - has;
+            const uint32_t take = before < ties ? min(ties - before, has) : 0u;
+            const uint64_t part = lds.sums[3][lane & (NW - 1)] + (uint64_t)take * one;
+            const uint64_t run = lane_scan<NW>(part, (uint64_t)0, Add{});
+            total = from_lane(run, NW - 1);
+            mine = from_lane(part, wave);
+            base = from_lane(run, wave) - mine;
+            left = from_lane(take, wave);
         }
         const uint64_t target = share(total, cut31(u));
         if (base <= target && target - base < mine) {   // one wave: it walks through its part
@@ -690,25 +880,20 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 if (j < per && !found) {
-                    uint32_t wt[V], before = 0;
-                    bool tie[V];
                     uint32_t held = 0;
 #pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        look(j, v, wt[v], tie[v]);
-                        held += tie[v];
-                    }
-                    uint32_t inside = 0;
+                    for (int v = 0; v < V; ++v) held += r[j][v] == kTie;
+                    uint32_t before = 0, inside = 0;
                     if (__any(held != 0)) {
                         const uint32_t run = wave_scan(held);
                         before = run - held;
-                        inside = (uint32_t)__shfl((int)run, 63);
+                        inside = from_lane(run, 63);
                     }
                     uint64_t here = 0;
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        if (tie[v] && before++ >= left) wt[v] = 0;
-                        here += wt[v];
+                        if (r[j][v] == kTie) r[j][v] = before++ < left ? one : 0u;
+                        here += r[j][v];
                     }
                     const uint64_t run = wave_scan(here);
                     const uint64_t hit = __ballot(base + run > target);
@@ -718,17 +903,17 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
                             bool out = false;
 #pragma unroll
                             for (int v = 0; v < V; ++v) {
-                                c += wt[v];
+                                c += r[j][v];
                                 if (!out && c > target) {
                                     out = true;
                                     out_action[n] = vr.first(q0 + j * 64) + v;
-                                    out_logp[n] = logf((float)wt[v] / (float)total);
+                                    out_logp[n] = logf((float)r[j][v] / (float)total);
                                 }
                             }
                         }
                         found = true;
                     }
-                    base += __shfl(run, 63);
+                    base += from_lane(run, 63);
                     left -= min(left, inside);
                 }
             }
@@ -779,7 +964,7 @@ __global__ __launch_bounds__(kThreads) void sample_small_kernel(const Rows R, co
         const float top = group_max<G>(x);
         const bool bad = (__ballot(!(x < INFINITY)) & group) != 0 || !(temp >= 0.0f) || top == -INFINITY;
         uint32_t w;
-        if (temp > 0.0f) w = weight_of(x, top, temp);
+        if (temp > 0.0f) w = Weights(top, temp)(x);
         else w = lane == __ffsll((unsigned long long)(__ballot(x == top) & group)) - 1 ? 1u : 0u;
         if constexpr (kFilter) {
             const int32_t k = S.top_ks ? S.top_ks[m] : S.top_k;
@@ -846,6 +1031,20 @@ constexpr int kMomentBlocks = 64;       // most partial sums of the weights and 
 constexpr int kMomentRows = 1024;       // rows of a workgroup that sums them, at least
 constexpr int kSums = 5;                // sums over the rows: policy, value, entropy, KL, clipped
 
+// Over the workgroup; the array may be in use before.
+template <class V>
+__device__ __forceinline__ V loss_sum(V x, V* lds)
+{
+    __syncthreads();
+    return block_sum<kWaves>(x, lds);
+}
+
+__device__ __forceinline__ float loss_max(float x, float* lds)
+{
+    __syncthreads();
+    return block_max<kWaves>(x, lds);
+}
+
 // Weight of row n, 0 where it does not count.
 __device__ __forceinline__ float row_weight(const Batch& b, int64_t n, int32_t A)
 {
@@ -869,9 +1068,9 @@ __global__ __launch_bounds__(kThreads) void loss_moments_kernel(const Batch b, i
         w1 += w * a;
         w2 += w * a * a;
     }
-    w0 = block_sum<kWaves>(w0, lds);
-    w1 = block_sum<kWaves>(w1, lds);
-    w2 = block_sum<kWaves>(w2, lds);
+    w0 = loss_sum(w0, lds);
+    w1 = loss_sum(w1, lds);
+    w2 = loss_sum(w2, lds);
     if (threadIdx.x == 0) {
         part[blockIdx.x] = w0;
         part[kMomentBlocks + blockIdx.x] = w1;
@@ -949,7 +1148,7 @@ __device__ void loss_finish(const Batch& b, const Shared3& s, const double* acc,
     __shared__ uint32_t last;
     double total[kSums];
 #pragma unroll
-    for (int k = 0; k < kSums; ++k) total[k] = block_sum<kWaves>(acc[k], lds);
+    for (int k = 0; k < kSums; ++k) total[k] = loss_sum(acc[k], lds);
     if (threadIdx.x == 0) {
         for (int k = 0; k < kSums; ++k) sums[(int64_t)blockIdx.x * kSums + k] = total[k];
         __threadfence();
@@ -963,7 +1162,7 @@ __device__ void loss_finish(const Batch& b, const Shared3& s, const double* acc,
 #pragma unroll
         for (int k = 0; k < kSums; ++k) x[k] += sums[(int64_t)i * kSums + k];
 #pragma unroll
-    for (int k = 0; k < kSums; ++k) x[k] = block_sum<kWaves>(x[k], lds) * (double)s.inv;
+    for (int k = 0; k < kSums; ++k) x[k] = loss_sum(x[k], lds) * (double)s.inv;
     if (threadIdx.x == 0) {
         b.stats[0] = (float)(x[0] + (double)b.value_coef * x[1] - (double)b.entropy_coef * x[2]);
         for (int k = 0; k < kSums; ++k) b.stats[k + 1] = (float)x[k];
@@ -1045,7 +1244,7 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(const Rows R, const Batc
         float top = -INFINITY;
         for (int i = threadIdx.x; i < A; i += kThreads) top = fmaxf(top, row(i));
         const float xa = row(a);
-        top = block_max<kWaves>(top, ldsf);
+        top = loss_max(top, ldsf);
         const float rt = b.temperature;
         // d = (x - top) / T, sum of e = exp d, and of e d
         auto dist = [&](float x) { return x == -INFINITY ? -INFINITY : (x - top) / rt; };
@@ -1055,8 +1254,8 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(const Rows R, const Batc
             e0 += e;
             if (e != 0.0f) e1 += e * d;
         }
-        e0 = block_sum<kWaves>(e0, ldsf);
-        e1 = block_sum<kWaves>(e1, ldsf);
+        e0 = loss_sum(e0, ldsf);
+        e1 = loss_sum(e1, ldsf);
         const float logs = logf(e0), rs = 1.0f / e0;
         const float H = e0 > 0.0f ? logs - e1 * rs : e0 == 0.0f ? 0.0f : e0;
         const RowTerms t = row_terms(b, s, n, e0 == 0.0f ? -INFINITY : dist(xa) - logs, H);
