@@ -33,8 +33,7 @@ struct Sampling {
     const int32_t* top_ks;
 };
 
-// One row as the kernels read it: fp32, -inf at a place that is not allowed, and
-// no negative zero (the order by bits is then that of the values).
+// One row as the kernels read it: fp32, -inf at a place that is not allowed.
 template <class T>
 struct Row {
     const T* x;
@@ -43,14 +42,14 @@ struct Row {
         : x((const T*)r.data + n * r.stride), mask(r.mask ? r.mask + n * r.mask_stride : nullptr) {}
     __device__ __forceinline__ float operator()(int i) const
     {
-        return mask && !mask[i] ? -INFINITY : (float)x[i] + 0.0f;
+        return mask && !mask[i] ? -INFINITY : (float)x[i];
     }
 };
 
-// Bits in the order of the values.
+// Bits in the order of the values (both zeros alike).
 __device__ __forceinline__ uint32_t order_key(float x)
 {
-    const uint32_t u = __float_as_uint(x);
+    const uint32_t u = __float_as_uint(x + 0.0f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
@@ -267,18 +266,40 @@ __device__ Cut find_cut(Each each, uint32_t floor_key, uint64_t need, Add add, u
     return Cut{prefix, ties_for(need, add(key_value(prefix)))};
 }
 
+// x as a value that is the same in every lane, which the compiler then knows.
+__device__ __forceinline__ uint32_t same_in_wave(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+
+__device__ __forceinline__ uint64_t same_in_wave(uint64_t x)
+{
+    return (uint64_t)same_in_wave((uint32_t)(x >> 32)) << 32 | same_in_wave((uint32_t)x);
+}
+
+__device__ __forceinline__ float same_in_wave(float x) { return __uint_as_float(same_in_wave(__float_as_uint(x))); }
+
 // A row's settings.
 struct RowSampling {
-    float temp, top_p;
+    float temp, top_p, u;
     int32_t top_k;
-    uint32_t least;   // smallest weight that min_p keeps
-    __device__ __forceinline__ RowSampling(const Sampling& S, int64_t n)
+    uint32_t least;   // smallest weight that is kept
+    bool greedy;
+    __device__ __forceinline__ RowSampling(const Sampling& S, const float* uniform, int64_t n)
     {
-        temp = S.temperatures ? S.temperatures[n] : S.temperature;
-        top_k = S.top_ks ? S.top_ks[n] : S.top_k;
-        top_p = S.top_ps ? S.top_ps[n] : S.top_p;
-        const float min_p = S.min_ps ? S.min_ps[n] : S.min_p;
-        least = temp > 0.0f ? (uint32_t)ceilf(fminf(fmaxf(min_p, 0.0f), 1.0f) * kOne) : 0u;
+        temp = same_in_wave(S.temperatures ? S.temperatures[n] : S.temperature);
+        top_k = (int32_t)same_in_wave((uint32_t)(S.top_ks ? S.top_ks[n] : S.top_k));
+        top_p = same_in_wave(S.top_ps ? S.top_ps[n] : S.top_p);
+        const float min_p = same_in_wave(S.min_ps ? S.min_ps[n] : S.min_p);
+        least = (uint32_t)ceilf(fminf(fmaxf(min_p, 0.0f), 1.0f) * kOne);
+        u = same_in_wave(uniform[n]);
+        // The first of the largest logits: at this temperature any smaller one weighs less
+        // than 2^31 (the least difference, 2^-149, makes it 2^31 - 2^8), and 0 draws the first.
+        greedy = temp == 0.0f;
+        if (greedy) {
+            temp = 0x1p-126f;
+            least = 1u << 31;
+            top_k = 0;
+            top_p = 1.0f;
+            u = 0.0f;
+        }
     }
 };
 
@@ -303,7 +324,7 @@ __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int64_t n = blockIdx.x; n < R.rows; n += gridDim.x) {
         const Row<T> row(R, n);
-        const RowSampling q(S, n);
+        const RowSampling q(S, uniform, n);
         auto each = [&](auto f) {
             for (int i = threadIdx.x; i < A; i += NT) f(row(i));
         };
@@ -323,30 +344,25 @@ __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows
             __syncthreads();
             continue;
         }
-        const Weights of(top, q.temp);
-        auto weight = [&](float x) { return q.temp > 0.0f ? of(x) : x == top ? 1u : 0u; };
+        const Weights weight(top, q.temp);
         Cut cut{0u, 0u};
-        if (q.temp == 0.0f) {
-            cut = Cut{order_key(top), 1u};
-        } else {
-            if (q.top_k > 0 && q.top_k < A) {
-                uint64_t some = 0;
-                each([&](float x) { some += x != -INFINITY; });
-                if (block_sum<NW>(some, lds64) > (uint64_t)q.top_k)
-                    cut = find_cut(each, 0u, (uint64_t)q.top_k, [](float) { return 1u; }, hist, told);
-            }
-            if (q.top_p < 1.0f) {
-                uint64_t above = 0;
-                each([&](float x) {
-                    if (order_key(x) > cut.key) above += weight(x);
-                });
-                above = block_sum<NW>(above, lds64 + NW);
-                const uint64_t one = cut.ties ? weight(key_value(cut.key)) : 0;
-                uint64_t need = share(above + one * cut.ties, cut31(q.top_p));
-                if (need < 1) need = 1;
-                if (need <= above) cut = find_cut(each, cut.key, need, weight, hist, told);
-                else cut.ties = ties_for(need - above, one);
-            }
+        if (q.top_k > 0 && q.top_k < A) {
+            uint64_t some = 0;
+            each([&](float x) { some += x != -INFINITY; });
+            if (block_sum<NW>(some, lds64) > (uint64_t)q.top_k)
+                cut = find_cut(each, 0u, (uint64_t)q.top_k, [](float) { return 1u; }, hist, told);
+        }
+        if (q.top_p < 1.0f) {
+            uint64_t above = 0;
+            each([&](float x) {
+                if (order_key(x) > cut.key) above += weight(x);
+            });
+            above = block_sum<NW>(above, lds64 + NW);
+            const uint64_t one = cut.ties ? weight(key_value(cut.key)) : 0;
+            uint64_t need = share(above + one * cut.ties, cut31(q.top_p));
+            if (need < 1) need = 1;
+            if (need <= above) cut = find_cut(each, cut.key, need, weight, hist, told);
+            else cut.ties = ties_for(need - above, one);
         }
         auto kept = [&](float x) {
             const uint32_t w = weight(x);
@@ -385,7 +401,7 @@ __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows
             quota -= take;
             total += part;
         }
-        const uint64_t target = share(total, cut31(uniform[n]));
+        const uint64_t target = share(total, cut31(q.u));
         if (base <= target && target - base < mine) {   // one wave: it walks through its part
             for (int b = i0; b < i1; b += 64) {
                 const int i = b + lane;
@@ -400,7 +416,7 @@ __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows
                 if (hit) {
                     if (lane == __ffsll((unsigned long long)hit) - 1) {
                         out_action[n] = i;
-                        out_logp[n] = logf((float)w / (float)total);
+                        out_logp[n] = q.greedy ? 0.0f : logf((float)w / (float)total);
                     }
                     break;
                 }
@@ -421,47 +437,94 @@ __device__ __forceinline__ uint32_t float_bits(uint32_t w) { return __float_as_u
 
 constexpr uint32_t kOneBits = 0x4F000000u;   // of 2^31
 
+// Says that x may be new from here on: what was computed from it in an earlier pass
+// over a thread's registers is not kept for this one (it would take as many
+// registers again).
+template <int V>
+__device__ __forceinline__ void renew(uint32_t (&x)[V])
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v) asm volatile("" : "+v"(x[v]));
+}
+
 // A row of V-element vectors at 16-byte addresses: vector q covers the elements
-// from q V - shift on, the first and the last only in part.
-template <class T>
+// from q V - shift on, the first and the last perhaps only in part.  A thread of
+// a workgroup of NW waves holds up to NV of them, 64 vectors apart, and a wave a
+// stretch of the row.
+template <class T, int NW, int NV>
 struct VecRow {
     static constexpr int V = 16 / sizeof(T);
     Row<T> row;
-    int A, shift, vectors;
-    bool mask_vec;   // the mask's bytes of a vector lie at a V-byte address
-    __device__ __forceinline__ VecRow(const Rows& r, int64_t n) : row(r, n), A(r.actions)
+    int A, shift, vectors, per, q0;
+    __device__ __forceinline__ VecRow(const Rows& r, int64_t n, int wave, int lane) : row(r, n), A(r.actions)
     {
         shift = (int)(reinterpret_cast<uintptr_t>(row.x) / sizeof(T)) & (V - 1);
         vectors = (A + shift + V - 1) / V;
-        mask_vec = ((reinterpret_cast<uintptr_t>(row.mask) - shift) & (V - 1)) == 0;
+        per = (vectors + NW * 64 - 1) / (NW * 64);   // vectors of a thread, at most NV
+        q0 = wave * per * 64 + lane;                 // its first one
     }
-    __device__ __forceinline__ int first(int q) const { return q * V - shift; }
-    __device__ __forceinline__ void load(int q, float* x) const
+    __device__ __forceinline__ int first(int j) const { return (q0 + j * 64) * V - shift; }
+    // whole vectors: q in [from, to)
+    __device__ __forceinline__ int from() const { return shift ? 1 : 0; }
+    __device__ __forceinline__ int to() const { return (A + shift) / V; }
+    __device__ __forceinline__ bool whole(int j) const { return q0 + j * 64 >= from() && q0 + j * 64 < to(); }
+
+    // The logits' bits, -inf where there is none.
+    __device__ __forceinline__ void load(uint32_t (&r)[NV][V]) const
     {
-        const int i0 = first(q);
-        if (q < vectors && i0 >= 0 && i0 + V <= A) {
-            struct alignas(16) Vec { T v[V]; };
-            const Vec t = *reinterpret_cast<const Vec*>(row.x + i0);
+        struct alignas(16) Vec { T v[V]; };
+        const Vec* at = reinterpret_cast<const Vec*>(row.x - shift) + q0;
+        const uint32_t none = __float_as_uint(-INFINITY);
 #pragma unroll
-            for (int v = 0; v < V; ++v) x[v] = (float)t.v[v] + 0.0f;
-            if (row.mask) {
-                if (mask_vec) {
-                    struct alignas(V) Bytes { uint8_t v[V]; };
-                    const Bytes k = *reinterpret_cast<const Bytes*>(row.mask + i0);
+        for (int j = 0; j < NV; ++j) {
 #pragma unroll
-                    for (int v = 0; v < V; ++v) x[v] = k.v[v] ? x[v] : -INFINITY;
-                } else {
+            for (int v = 0; v < V; ++v) r[j][v] = none;
+            if (j < per && whole(j)) {
+                const Vec t = at[j * 64];
 #pragma unroll
-                    for (int v = 0; v < V; ++v) x[v] = row.mask[i0 + v] ? x[v] : -INFINITY;
-                }
+                for (int v = 0; v < V; ++v) r[j][v] = __float_as_uint((float)t.v[v]);
             }
-        } else {
+        }
+        // the two ends, element by element
+        const int last = vectors - 1 - q0;
+        const int je = last >= 0 && !(last & 63) && to() < vectors && (last >> 6) < per ? last >> 6 : -1;
+        if (q0 == 0 && shift) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) x[v] = q < vectors && i0 + v >= 0 && i0 + v < A ? row(i0 + v) : -INFINITY;
+            for (int v = 0; v < V; ++v)
+                if (v >= shift && v - shift < A) r[0][v] = __float_as_uint((float)row.x[v - shift]);
+        }
+        if (je >= 0 && (je > 0 || q0 > 0 || !shift)) {
+            uint32_t t[V];
+            const int i0 = first(je);
+#pragma unroll
+            for (int v = 0; v < V; ++v) t[v] = i0 + v < A ? __float_as_uint((float)row.x[i0 + v]) : none;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v) r[j][v] = j == je ? t[v] : r[j][v];
+        }
+        if (row.mask) {
+            struct alignas(V) Bytes { uint8_t v[V]; };
+            const bool even = ((reinterpret_cast<uintptr_t>(row.mask) - shift) & (V - 1)) == 0;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j < per) {
+                    const int i0 = first(j);
+                    if (even && whole(j)) {
+                        const Bytes k = *reinterpret_cast<const Bytes*>(row.mask + i0);
+#pragma unroll
+                        for (int v = 0; v < V; ++v) r[j][v] = k.v[v] ? r[j][v] : none;
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < V; ++v)
+                            if (i0 + v >= 0 && i0 + v < A && !row.mask[i0 + v]) r[j][v] = none;
+                    }
+                }
         }
     }
 };
 
+constexpr int kMostSlots = 16 * 64 * 72;   // longest row that registers hold
 constexpr int kRank = 256;   // candidates that are ranked by counting
 
 // Shared memory of a row's workgroup.
@@ -492,433 +555,429 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
                                                              int64_t* __restrict__ out_action,
                                                              float* __restrict__ out_logp)
 {
-    constexpr int V = VecRow<T>::V, NV = ITEMS / V, NT = NW * 64;
+    constexpr int V = 16 / sizeof(T), NV = ITEMS / V, NT = NW * 64;
     using Lds = RowLds<NW, kFilter>;
     __shared__ alignas(16) Lds lds;
     const int A = R.actions;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for (int64_t n = blockIdx.x; n < R.rows; n += gridDim.x) {
-        const VecRow<T> vr(R, n);
-        const Row<T>& row = vr.row;
-        const RowSampling q(S, n);
-        const float u = uniform[n];
-        const int per = (vr.vectors + NT - 1) / NT;   // vectors of a thread, at most NV
-        const int q0 = wave * per * 64 + lane;        // its first one
-        // bits of the logits, later the weights
-        uint32_t r[NV][V];
-        float top = -INFINITY;
-        bool odd = !(q.temp >= 0.0f);
+    const int64_t n = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (n >= R.rows) return;
+    const VecRow<T, NW, NV> vr(R, n, wave, lane);
+    const Row<T>& row = vr.row;
+    const RowSampling q(S, uniform, n);
+    const int per = vr.per;
+    // bits of the logits, later the weights
+    uint32_t r[NV][V];
+    float top = -INFINITY;
+    bool odd = !(q.temp >= 0.0f);
+    vr.load(r);
+    auto x = [&](int j, int v) { return __uint_as_float(r[j][v]); };
+    auto vmax = [&](int j) {
+        float m = x(j, 0);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            float x[V];
+        for (int v = 1; v < V; ++v) m = fmaxf(m, x(j, v));
+        return m;
+    };
 #pragma unroll
-            for (int v = 0; v < V; ++v) x[v] = -INFINITY;
-            if (j < per) vr.load(q0 + j * 64, x);
+    for (int j = 0; j < NV; ++j)
+        if (j < per) {
+            renew(r[j]);
+            top = fmaxf(top, vmax(j));
 #pragma unroll
-            for (int v = 0; v < V; ++v) r[j][v] = __float_as_uint(x[v]);
+            for (int v = 0; v < V; ++v) odd |= !(x(j, v) < INFINITY);
         }
-        auto x = [&](int j, int v) { return __uint_as_float(r[j][v]); };
-        auto vmax = [&](int j) {
-            float m = x(j, 0);
-#pragma unroll
-            for (int v = 1; v < V; ++v) m = fmaxf(m, x(j, v));
-            return m;
-        };
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (j < per) {
-                top = fmaxf(top, vmax(j));
-#pragma unroll
-                for (int v = 0; v < V; ++v) odd |= !(x(j, v) < INFINITY);
-            }
-        // the largest logit; a NaN or +inf, or a temperature without meaning, makes no draw
-        top = block_max<NW>(odd ? INFINITY : top, lds.maxima[0]);
-        if (top == INFINITY || top == -INFINITY) {
-            if (threadIdx.x == 0) {
-                out_action[n] = -1;
-                out_logp[n] = NAN;
-            }
-            __syncthreads();
-            continue;
+    // the largest logit; a NaN or +inf, or a temperature without meaning, makes no draw
+    top = block_max<NW>(odd ? INFINITY : top, lds.maxima[0]);
+    if (top == INFINITY || top == -INFINITY) {
+        if (threadIdx.x == 0) {
+            out_action[n] = -1;
+            out_logp[n] = NAN;
         }
-        const Weights weight(top, q.temp);
-        // The cut: logits over `over` are kept, and the first `ties` of those equal to it.
-        float over = -INFINITY;
-        uint32_t ties = 0;
-        bool by_logit = false;   // the cut comes from the logits, before any weight
-        if (q.temp == 0.0f) {
-            over = top;
-            ties = 1;
-            by_logit = true;
+        return;
+    }
+    const Weights weight(top, q.temp);
+    // The cut: logits over `over` are kept, and the first `ties` of those equal to it.
+    float over = -INFINITY;
+    uint32_t ties = 0;
+    bool by_logit = false;   // the cut comes from the logits, before any weight
+    // the cut among lds.list[0 .. C): by count, or by weight, up to `need`
+    auto rank_list = [&](uint32_t C, bool weigh) {
+        if (threadIdx.x < 4) {
+            lds.list[C + threadIdx.x] = -INFINITY;
+            lds.weight[C + threadIdx.x] = 0;
         }
-        // the cut among lds.list[0 .. C): by count, or by weight, up to `need`
-        auto rank_list = [&](uint32_t C, bool weigh) {
-            if (threadIdx.x < 4) {
-                lds.list[C + threadIdx.x] = -INFINITY;
-                lds.weight[C + threadIdx.x] = 0;
-            }
-            if (weigh)
-                for (uint32_t i = threadIdx.x; i < C; i += NT) lds.weight[i] = weight(lds.list[i]);
-            __syncthreads();
-        };
-        if constexpr (kFilter) {
-            bool cut_k = false;
-            if (!by_logit && q.top_k > 0 && q.top_k < A) {
-                uint32_t some = 0;
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-                    if (j < per) {
-#pragma unroll
-                        for (int v = 0; v < V; ++v) some += x(j, v) != -INFINITY;
-                    }
-                cut_k = block_sum<NW>((uint64_t)some, lds.sums[0]) > (uint64_t)q.top_k;
-            }
-            if (cut_k) {
-                by_logit = true;
-                // The top_k-th largest of the vectors' maxima is no more than the top_k-th
-                // largest logit: a histogram of them bounds the logits that can be kept
-                // from below, and those few are listed.
-                float low = INFINITY;
-                uint32_t vecs = 0;
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-                    if (j < per) {
-                        const float m = vmax(j);
-                        if (m > -INFINITY) {
-                            low = fminf(low, m);
-                            ++vecs;
-                        }
-                    }
-                for (int i = threadIdx.x; i < Lds::kBins + Lds::kBins / 16; i += NT) lds.hist[i] = 0;
-                if (threadIdx.x == 0) lds.listed = 0;
-                low = -block_max<NW>(-low, lds.maxima[1]);
-                if (NW == 1) __syncthreads();
-                const float scale = (float)Lds::kBins / (top - low);   // (no range: NaN, and all in bin 0)
-                auto bin = [&](float y) { return (int)fminf(fmaxf((top - y) * scale, 0.0f), (float)(Lds::kBins - 1)); };
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-                    if (j < per) {
-                        const float m = vmax(j);
-                        if (m > -INFINITY) atomicAdd(&lds.hist[padded(bin(m))], 1ull);
-                    }
-                const bool enough = block_sum<NW>((uint64_t)vecs, lds.sums[1]) >= (uint64_t)q.top_k;
-                int edge = Lds::kBins - 1;
-                if (enough) {
-                    if (NW == 1) __syncthreads();
-                    if (wave == 0) find_bin(lds.hist, Lds::kBins, (uint64_t)q.top_k, lds.told);
-                    __syncthreads();
-                    edge = (int)lds.told[0];
-                }
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-                    if (j < per) {
-                        const float m = vmax(j);
-                        if (m > -INFINITY && bin(m) <= edge) {
-#pragma unroll
-                            for (int v = 0; v < V; ++v)
-                                if (x(j, v) > -INFINITY && bin(x(j, v)) <= edge) {
-                                    const uint32_t at = atomicAdd(&lds.listed, 1u);
-                                    if (at < Lds::kList) lds.list[at] = x(j, v);
-                                }
-                        }
-                    }
-                __syncthreads();
-                const uint32_t C = lds.listed;
-                if (C <= kRank) {
-                    // how many and how much is above each, and equal to it
-                    rank_list(C, q.top_p < 1.0f);
-                    for (uint32_t i = threadIdx.x; i < C; i += NT) {
-                        const float xi = lds.list[i];
-                        uint32_t above = 0, equal = 0;
-                        uint64_t before = 0;
-                        for (uint32_t k = 0; k < C; k += 4) {
-                            const float4 y = *reinterpret_cast<const float4*>(lds.list + k);
-                            const uint4 w = *reinterpret_cast<const uint4*>(lds.weight + k);
-                            above += (y.x > xi) + (y.y > xi) + (y.z > xi) + (y.w > xi);
-                            equal += (y.x == xi) + (y.y == xi) + (y.z == xi) + (y.w == xi);
-                            before += (uint64_t)(y.x > xi ? w.x : 0u) + (y.y > xi ? w.y : 0u);
-                            before += (uint64_t)(y.z > xi ? w.z : 0u) + (y.w > xi ? w.w : 0u);
-                        }
-                        lds.before[i] = before;
-                        lds.equal[i] = equal;
-                        if (above < (uint32_t)q.top_k && (uint32_t)q.top_k <= above + equal) {
-                            // (equal ones write the same)
-                            lds.told[0] = (uint64_t)__float_as_uint(xi);
-                            lds.told[1] = (uint64_t)((uint32_t)q.top_k - above);
-                            lds.told[2] = before + (uint64_t)((uint32_t)q.top_k - above) * lds.weight[i];
-                        }
-                    }
-                    __syncthreads();
-                    over = __uint_as_float((uint32_t)lds.told[0]);
-                    ties = (uint32_t)lds.told[1];
-                    if (q.top_p < 1.0f) {
-                        uint64_t need = share(lds.told[2], cut31(q.top_p));
-                        if (need < 1) need = 1;
-                        __syncthreads();
-                        for (uint32_t i = threadIdx.x; i < C; i += NT) {
-                            const float xi = lds.list[i];
-                            const uint32_t equal = xi == over ? ties : lds.equal[i];
-                            const uint64_t before = lds.before[i];
-                            if (xi >= over && before < need && need <= before + (uint64_t)equal * lds.weight[i]) {
-                                lds.told[0] = (uint64_t)__float_as_uint(xi);
-                                lds.told[1] = ties_for(need - before, lds.weight[i]);
-                            }
-                        }
-                        __syncthreads();
-                        over = __uint_as_float((uint32_t)lds.told[0]);
-                        ties = (uint32_t)lds.told[1];
-                    }
-                } else {
-                    auto narrow = [&](auto each) {
-                        Cut cut = find_cut(each, 0u, (uint64_t)q.top_k, [](float) { return 1u; }, lds.hist, lds.told);
-                        if (q.top_p < 1.0f) {
-                            uint64_t above = 0;
-                            each([&](float y) {
-                                if (order_key(y) > cut.key) above += weight(y);
-                            });
-                            above = block_sum<NW>(above, lds.sums[2]);
-                            const uint64_t one = weight(key_value(cut.key));
-                            uint64_t need = share(above + one * cut.ties, cut31(q.top_p));
-                            if (need < 1) need = 1;
-                            if (need <= above) cut = find_cut(each, cut.key, need, weight, lds.hist, lds.told);
-                            else cut.ties = ties_for(need - above, one);
-                        }
-                        over = key_value(cut.key);
-                        ties = cut.ties;
-                    };
-                    if (C <= Lds::kList)
-                        narrow([&](auto f) {
-                            for (uint32_t i = threadIdx.x; i < C; i += NT) f(lds.list[i]);
-                        });
-                    else
-                        narrow([&](auto f) {
-                            for (int i = threadIdx.x; i < A; i += NT) f(row(i));
-                        });
-                }
-            }
-        }
-        uint32_t one = 0;   // weight of a tie
-        if (by_logit) {
-            one = q.temp > 0.0f ? weight(over) : 1u;
-            if (one < q.least) one = 0;
-            // few vectors hold a kept logit
+        if (weigh)
+            for (uint32_t i = threadIdx.x; i < C; i += NT) lds.weight[i] = weight(lds.list[i]);
+        __syncthreads();
+    };
+    if constexpr (kFilter) {
+        bool cut_k = false;
+        if (q.top_k > 0 && q.top_k < A) {
+            uint32_t some = 0;
 #pragma unroll
             for (int j = 0; j < NV; ++j)
                 if (j < per) {
-                    if (vmax(j) >= over) {
+                    renew(r[j]);
 #pragma unroll
-                        for (int v = 0; v < V; ++v) {
-                            const float y = x(j, v);
-                            const uint32_t w = y > over ? weight(y) : 0u;
-                            r[j][v] = y == over ? kTie : w < q.least ? 0u : w;
-                        }
-                    } else {
+                    for (int v = 0; v < V; ++v) some += x(j, v) != -INFINITY;
+                }
+            cut_k = block_sum<NW>((uint64_t)some, lds.sums[0]) > (uint64_t)q.top_k;
+        }
+        if (cut_k) {
+            by_logit = true;
+            // The top_k-th largest of the vectors' maxima is no more than the top_k-th
+            // largest logit: a histogram of them bounds the logits that can be kept
+            // from below, and those few are listed.
+            float low = INFINITY;
+            uint32_t vecs = 0;
 #pragma unroll
-                        for (int v = 0; v < V; ++v) r[j][v] = 0u;
+            for (int j = 0; j < NV; ++j)
+                if (j < per) {
+                    renew(r[j]);
+                    const float m = vmax(j);
+                    if (m > -INFINITY) {
+                        low = fminf(low, m);
+                        ++vecs;
                     }
                 }
-        } else {
+            for (int i = threadIdx.x; i < Lds::kBins + Lds::kBins / 16; i += NT) lds.hist[i] = 0;
+            if (threadIdx.x == 0) lds.listed = 0;
+            low = -block_max<NW>(-low, lds.maxima[1]);
+            if (NW == 1) __syncthreads();
+            const float scale = (float)Lds::kBins / (top - low);   // (no range: NaN, and all in bin 0)
+            auto bin = [&](float y) { return (int)fminf(fmaxf((top - y) * scale, 0.0f), (float)(Lds::kBins - 1)); };
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j < per) {
+                    renew(r[j]);
+                    const float m = vmax(j);
+                    if (m > -INFINITY) atomicAdd(&lds.hist[padded(bin(m))], 1ull);
+                }
+            const bool enough = block_sum<NW>((uint64_t)vecs, lds.sums[1]) >= (uint64_t)q.top_k;
+            int edge = Lds::kBins - 1;
+            if (enough) {
+                if (NW == 1) __syncthreads();
+                if (wave == 0) find_bin(lds.hist, Lds::kBins, (uint64_t)q.top_k, lds.told);
+                __syncthreads();
+                edge = (int)same_in_wave((uint32_t)lds.told[0]);
+            }
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j < per) {
+                    renew(r[j]);
+                    const float m = vmax(j);
+                    if (m > -INFINITY && bin(m) <= edge) {
+#pragma unroll
+                        for (int v = 0; v < V; ++v)
+                            if (x(j, v) > -INFINITY && bin(x(j, v)) <= edge) {
+                                const uint32_t at = atomicAdd(&lds.listed, 1u);
+                                if (at < Lds::kList) lds.list[at] = x(j, v);
+                            }
+                    }
+                }
+            __syncthreads();
+            const uint32_t C = same_in_wave(lds.listed);
+            if (C <= kRank) {
+                // how many and how much is above each, and equal to it
+                rank_list(C, q.top_p < 1.0f);
+                for (uint32_t i = threadIdx.x; i < C; i += NT) {
+                    const float xi = lds.list[i];
+                    uint32_t above = 0, equal = 0;
+                    uint64_t before = 0;
+                    for (uint32_t k = 0; k < C; k += 4) {
+                        const float4 y = *reinterpret_cast<const float4*>(lds.list + k);
+                        const uint4 w = *reinterpret_cast<const uint4*>(lds.weight + k);
+                        above += (y.x > xi) + (y.y > xi) + (y.z > xi) + (y.w > xi);
+                        equal += (y.x == xi) + (y.y == xi) + (y.z == xi) + (y.w == xi);
+                        before += (uint64_t)(y.x > xi ? w.x : 0u) + (y.y > xi ? w.y : 0u);
+                        before += (uint64_t)(y.z > xi ? w.z : 0u) + (y.w > xi ? w.w : 0u);
+                    }
+                    lds.before[i] = before;
+                    lds.equal[i] = equal;
+                    if (above < (uint32_t)q.top_k && (uint32_t)q.top_k <= above + equal) {
+                        // (equal ones write the same)
+                        lds.told[0] = (uint64_t)__float_as_uint(xi);
+                        lds.told[1] = (uint64_t)((uint32_t)q.top_k - above);
+                        lds.told[2] = before + (uint64_t)((uint32_t)q.top_k - above) * lds.weight[i];
+                    }
+                }
+                __syncthreads();
+                over = __uint_as_float(same_in_wave((uint32_t)lds.told[0]));
+                ties = same_in_wave((uint32_t)lds.told[1]);
+                if (q.top_p < 1.0f) {
+                    uint64_t need = share(lds.told[2], cut31(q.top_p));
+                    if (need < 1) need = 1;
+                    __syncthreads();
+                    for (uint32_t i = threadIdx.x; i < C; i += NT) {
+                        const float xi = lds.list[i];
+                        const uint32_t equal = xi == over ? ties : lds.equal[i];
+                        const uint64_t before = lds.before[i];
+                        if (xi >= over && before < need && need <= before + (uint64_t)equal * lds.weight[i]) {
+                            lds.told[0] = (uint64_t)__float_as_uint(xi);
+                            lds.told[1] = ties_for(need - before, lds.weight[i]);
+                        }
+                    }
+                    __syncthreads();
+                    over = __uint_as_float(same_in_wave((uint32_t)lds.told[0]));
+                    ties = same_in_wave((uint32_t)lds.told[1]);
+                }
+            } else {
+                auto narrow = [&](auto each) {
+                    Cut cut = find_cut(each, 0u, (uint64_t)q.top_k, [](float) { return 1u; }, lds.hist, lds.told);
+                    if (q.top_p < 1.0f) {
+                        uint64_t above = 0;
+                        each([&](float y) {
+                            if (order_key(y) > cut.key) above += weight(y);
+                        });
+                        above = block_sum<NW>(above, lds.sums[2]);
+                        const uint64_t one = weight(key_value(cut.key));
+                        uint64_t need = share(above + one * cut.ties, cut31(q.top_p));
+                        if (need < 1) need = 1;
+                        if (need <= above) cut = find_cut(each, cut.key, need, weight, lds.hist, lds.told);
+                        else cut.ties = ties_for(need - above, one);
+                    }
+                    over = key_value(cut.key);
+                    ties = cut.ties;
+                };
+                if (C <= Lds::kList)
+                    narrow([&](auto f) {
+                        for (uint32_t i = threadIdx.x; i < C; i += NT) f(lds.list[i]);
+                    });
+                else
+                    narrow([&](auto f) {
+                        for (int i = threadIdx.x; i < A; i += NT) f(row(i));
+                    });
+            }
+        }
+    }
+    // The registers come to hold the weights that are left, kTie for one equal to the cut.
+    // (One pass for every kind of cut: alternatives over the registers double them.)
+    const uint32_t at_cut = kFilter && by_logit ? kTie : 0u;
+    uint32_t one = kFilter && by_logit ? weight(over) : 0u;   // weight of a tie
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (j < per) {
+            renew(r[j]);
+            if (!kFilter || vmax(j) >= over) {   // few vectors hold a logit that top_k keeps
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float y = x(j, v);
+                    r[j][v] = weight(y);
+                    if (kFilter) r[j][v] = y > over ? r[j][v] : y == over ? at_cut : 0u;
+                }
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; ++v) r[j][v] = 0u;
+            }
+        }
+    if constexpr (kFilter) {
+        if (!by_logit && q.top_p < 1.0f) {
             uint64_t sum = 0;
 #pragma unroll
             for (int j = 0; j < NV; ++j)
                 if (j < per) {
+                    renew(r[j]);
 #pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        r[j][v] = weight(x(j, v));
-                        sum += r[j][v];
-                    }
+                    for (int v = 0; v < V; ++v) sum += r[j][v];
                 }
-            uint32_t wover = 0;   // weights above it are kept, and some of those equal to it
-            if constexpr (kFilter) {
-                if (q.top_p < 1.0f) {
-                    for (int i = threadIdx.x; i < Lds::kBins + Lds::kBins / 16; i += NT) lds.hist[i] = 0;
-                    if (threadIdx.x == 0) lds.listed = 0;
-                    sum = block_sum<NW>(sum, lds.sums[1]);
-                    if (NW == 1) __syncthreads();
-                    uint64_t need = share(sum, cut31(q.top_p));
-                    if (need < 1) need = 1;
-                    // All weights up to `small` together stay below sum - need, so the prefix
-                    // ends above it.
-                    const uint32_t small = (uint32_t)((float)(sum - need) / (float)A * 0.999f);
-                    const uint32_t range = kOneBits - float_bits(small + 1);
-                    constexpr int kLog = NW == 1 ? 8 : 10;
-                    const int drop = max(0, 32 - __clz((int)range) - kLog);
-#pragma unroll
-                    for (int j = 0; j < NV; ++j)
-                        if (j < per) {
-#pragma unroll
-                            for (int v = 0; v < V; ++v)
-                                if (r[j][v] > small)
-                                    atomicAdd(&lds.hist[padded((int)((kOneBits - float_bits(r[j][v])) >> drop))],
-                                              (unsigned long long)r[j][v]);
-                        }
-                    __syncthreads();
-                    if (wave == 0) find_bin(lds.hist, Lds::kBins, need, lds.told);
-                    __syncthreads();
-                    const uint32_t edge = (uint32_t)lds.told[0];
-                    const uint64_t rest = lds.told[1];
-                    // the bin's logits (the order of logits and of weights is one, up to equal
-                    // weights of different logits)
-                    const uint32_t most = kOneBits - (edge << drop), least = most - ((1u << drop) - 1u);
-#pragma unroll
-                    for (int j = 0; j < NV; ++j)
-                        if (j < per) {
-#pragma unroll
-                            for (int v = 0; v < V; ++v) {
-                                const uint32_t f = float_bits(r[j][v]);
-                                if (r[j][v] > small && f <= most && f >= least) {
-                                    const uint32_t at = atomicAdd(&lds.listed, 1u);
-                                    if (at < Lds::kList) lds.list[at] = row(vr.first(q0 + j * 64) + v);
-                                }
-                            }
-                        }
-                    __syncthreads();
-                    const uint32_t C = lds.listed;
-                    if (C <= kRank) {
-                        rank_list(C, true);
-                        for (uint32_t i = threadIdx.x; i < C; i += NT) {
-                            const float xi = lds.list[i];
-                            uint32_t equal = 0;
-                            uint64_t before = 0;
-                            for (uint32_t k = 0; k < C; k += 4) {
-                                const float4 y = *reinterpret_cast<const float4*>(lds.list + k);
-                                const uint4 w = *reinterpret_cast<const uint4*>(lds.weight + k);
-                                equal += (y.x == xi) + (y.y == xi) + (y.z == xi) + (y.w == xi);
-                                before += (uint64_t)(y.x > xi ? w.x : 0u) + (y.y > xi ? w.y : 0u);
-                                before += (uint64_t)(y.z > xi ? w.z : 0u) + (y.w > xi ? w.w : 0u);
-                            }
-                            if (before < rest && rest <= before + (uint64_t)equal * lds.weight[i]) {
-                                lds.told[2] = (uint64_t)__float_as_uint(xi);
-                                lds.told[3] = ties_for(rest - before, lds.weight[i]);
-                            }
-                        }
-                        __syncthreads();
-                        over = __uint_as_float((uint32_t)lds.told[2]);
-                        ties = (uint32_t)lds.told[3];
-                    } else {
-                        Cut cut;
-                        if (C <= Lds::kList)
-                            cut = find_cut(
-                                [&](auto f) {
-                                    for (uint32_t i = threadIdx.x; i < C; i += NT) f(lds.list[i]);
-                                },
-                                0u, rest, weight, lds.hist, lds.told);
-                        else
-                            cut = find_cut(
-                                [&](auto f) {
-                                    for (int i = threadIdx.x; i < A; i += NT) f(row(i));
-                                },
-                                0u, need, weight, lds.hist, lds.told);
-                        over = key_value(cut.key);
-                        ties = cut.ties;
-                    }
-                    wover = weight(over);
-                }
-            }
-            one = wover < q.least ? 0u : wover;
+            for (int i = threadIdx.x; i < Lds::kBins + Lds::kBins / 16; i += NT) lds.hist[i] = 0;
+            if (threadIdx.x == 0) lds.listed = 0;
+            sum = block_sum<NW>(sum, lds.sums[1]);
+            if (NW == 1) __syncthreads();
+            uint64_t need = share(sum, cut31(q.top_p));
+            if (need < 1) need = 1;
+            // All weights up to `small` together stay below sum - need, so the prefix
+            // ends above it.
+            const uint32_t small = (uint32_t)((float)(sum - need) / (float)A * 0.999f);
+            const uint32_t range = kOneBits - float_bits(small + 1);
+            constexpr int kLog = NW == 1 ? 8 : 10;
+            const int drop = max(0, 32 - __clz((int)range) - kLog);
 #pragma unroll
             for (int j = 0; j < NV; ++j)
                 if (j < per) {
-                    bool look = false;
+                    renew(r[j]);
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        if (r[j][v] > small)
+                            atomicAdd(&lds.hist[padded((int)((kOneBits - float_bits(r[j][v])) >> drop))],
+                                      (unsigned long long)r[j][v]);
+                }
+            __syncthreads();
+            if (wave == 0) find_bin(lds.hist, Lds::kBins, need, lds.told);
+            __syncthreads();
+            const uint32_t edge = same_in_wave((uint32_t)lds.told[0]);
+            const uint64_t rest = same_in_wave(lds.told[1]);
+            // the bin's logits (the order of logits and of weights is one, up to equal
+            // weights of different logits)
+            const uint32_t most = kOneBits - (edge << drop), least = most - ((1u << drop) - 1u);
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j < per) {
+                    renew(r[j]);
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        look |= kFilter && r[j][v] == wover;
-                        r[j][v] = r[j][v] < q.least || r[j][v] < wover ? 0u : r[j][v];
-                    }
-                    if (kFilter && wover != 0 && look) {   // which of them the logits tell
-#pragma unroll
-                        for (int v = 0; v < V; ++v) {
-                            const int i = vr.first(q0 + j * 64) + v;
-                            if (r[j][v] == wover && i >= 0 && i < A) {
-                                const float y = row(i);
-                                if (y == over) r[j][v] = kTie;
-                                else if (y < over) r[j][v] = 0;
-                            }
+                        const uint32_t f = float_bits(r[j][v]);
+                        if (r[j][v] > small && f <= most && f >= least) {
+                            const uint32_t at = atomicAdd(&lds.listed, 1u);
+                            if (at < Lds::kList) lds.list[at] = row(vr.first(j) + v);
                         }
                     }
                 }
+            __syncthreads();
+            const uint32_t C = same_in_wave(lds.listed);
+            if (C <= kRank) {
+                rank_list(C, true);
+                for (uint32_t i = threadIdx.x; i < C; i += NT) {
+                    const float xi = lds.list[i];
+                    uint32_t equal = 0;
+                    uint64_t before = 0;
+                    for (uint32_t k = 0; k < C; k += 4) {
+                        const float4 y = *reinterpret_cast<const float4*>(lds.list + k);
+                        const uint4 w = *reinterpret_cast<const uint4*>(lds.weight + k);
+                        equal += (y.x == xi) + (y.y == xi) + (y.z == xi) + (y.w == xi);
+                        before += (uint64_t)(y.x > xi ? w.x : 0u) + (y.y > xi ? w.y : 0u);
+                        before += (uint64_t)(y.z > xi ? w.z : 0u) + (y.w > xi ? w.w : 0u);
+                    }
+                    if (before < rest && rest <= before + (uint64_t)equal * lds.weight[i]) {
+                        lds.told[2] = (uint64_t)__float_as_uint(xi);
+                        lds.told[3] = ties_for(rest - before, lds.weight[i]);
+                    }
+                }
+                __syncthreads();
+                over = __uint_as_float(same_in_wave((uint32_t)lds.told[2]));
+                ties = same_in_wave((uint32_t)lds.told[3]);
+            } else {
+                Cut cut;
+                if (C <= Lds::kList)
+                    cut = find_cut(
+                        [&](auto f) {
+                            for (uint32_t i = threadIdx.x; i < C; i += NT) f(lds.list[i]);
+                        },
+                        0u, rest, weight, lds.hist, lds.told);
+                else
+                    cut = find_cut(
+                        [&](auto f) {
+                            for (int i = threadIdx.x; i < A; i += NT) f(row(i));
+                        },
+                        0u, need, weight, lds.hist, lds.told);
+                over = key_value(cut.key);
+                ties = cut.ties;
+            }
+            one = weight(over);
+            // another logit of the same weight: then the logits tell which are kept
+            bool alike = false;
+            if (C <= Lds::kList)
+                for (uint32_t i = threadIdx.x; i < C; i += NT) alike |= lds.list[i] != over && weight(lds.list[i]) == one;
+            else
+                for (int i = threadIdx.x; i < A; i += NT) alike |= row(i) != over && weight(row(i)) == one;
+            const bool ask = block_max<NW>(alike ? 1.0f : 0.0f, lds.maxima[2]) != 0.0f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j < per) {
+                    renew(r[j]);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        uint32_t w = r[j][v] < one ? 0u : r[j][v];
+                        if (w == one) {
+                            const float y = ask ? row(vr.first(j) + v) : over;
+                            w = y == over ? kTie : y < over ? 0u : w;
+                        }
+                        r[j][v] = w;
+                    }
+                }
         }
-        uint64_t sum = 0;
-        uint32_t same = 0;
+    }
+    if (q.least > 0) {
+        if (one < q.least) one = 0;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if (j < per) {
+                renew(r[j]);
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const bool tie = kTie == r[j][v];
-                    same += tie;
-                    sum += tie ? 0u : r[j][v];
-                }
+                for (int v = 0; v < V; ++v) r[j][v] = r[j][v] < q.least ? 0u : r[j][v];
             }
-        sum = wave_sum(sum);
-        same = wave_sum(same);
-        uint64_t total, base = 0, mine;
-        uint32_t left;
-        if constexpr (NW == 1) {
-            left = min(ties, same);
-            total = mine = sum + (uint64_t)left * one;
-        } else {
-            if (lane == 0) {
-                lds.sums[3][wave] = sum;
-                lds.ties[wave] = same;
+    }
+    uint64_t sum = 0;
+    uint32_t same = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (j < per) {
+            renew(r[j]);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const bool tie = kTie == r[j][v];
+                same += tie;
+                sum += tie ? 0u : r[j][v];
             }
-            __syncthreads();
-            // lane w: wave w; the ties belong to the first waves that have them
-            const uint32_t has = lds.ties[lane & (NW - 1)];
-            const uint32_t before = lane_scan<NW>(has, 0u, Add{}) - has;
-            const uint32_t take = before < ties ? min(ties - before, has) : 0u;
-            const uint64_t part = lds.sums[3][lane & (NW - 1)] + (uint64_t)take * one;
-            const uint64_t run = lane_scan<NW>(part, (uint64_t)0, Add{});
-            total = from_lane(run, NW - 1);
-            mine = from_lane(part, wave);
-            base = from_lane(run, wave) - mine;
-            left = from_lane(take, wave);
         }
-        const uint64_t target = share(total, cut31(u));
-        if (base <= target && target - base < mine) {   // one wave: it walks through its part
-            bool found = false;
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                if (j < per && !found) {
-                    uint32_t held = 0;
-#pragma unroll
-                    for (int v = 0; v < V; ++v) held += r[j][v] == kTie;
-                    uint32_t before = 0, inside = 0;
-                    if (__any(held != 0)) {
-                        const uint32_t run = wave_scan(held);
-                        before = run - held;
-                        inside = from_lane(run, 63);
-                    }
-                    uint64_t here = 0;
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        if (r[j][v] == kTie) r[j][v] = before++ < left ? one : 0u;
-                        here += r[j][v];
-                    }
-                    const uint64_t run = wave_scan(here);
-                    const uint64_t hit = __ballot(base + run > target);
-                    if (hit) {
-                        if (lane == __ffsll((unsigned long long)hit) - 1) {
-                            uint64_t c = base + run - here;
-                            bool out = false;
-#pragma unroll
-                            for (int v = 0; v < V; ++v) {
-                                c += r[j][v];
-                                if (!out && c > target) {
-                                    out = true;
-                                    out_action[n] = vr.first(q0 + j * 64) + v;
-                                    out_logp[n] = logf((float)r[j][v] / (float)total);
-                                }
-                            }
-                        }
-                        found = true;
-                    }
-                    base += from_lane(run, 63);
-                    left -= min(left, inside);
-                }
-            }
+    sum = wave_sum(sum);
+    same = wave_sum(same);
+    uint64_t total, base = 0, mine;
+    uint32_t left;
+    if constexpr (NW == 1) {
+        left = min(ties, same);
+        total = mine = sum + (uint64_t)left * one;
+    } else {
+        if (lane == 0) {
+            lds.sums[3][wave] = sum;
+            lds.ties[wave] = same;
         }
         __syncthreads();
+        // lane w: wave w; the ties belong to the first waves that have them
+        const uint32_t has = lds.ties[lane & (NW - 1)];
+        const uint32_t before = lane_scan<NW>(has, 0u, Add{}) - has;
+        const uint32_t take = before < ties ? min(ties - before, has) : 0u;
+        const uint64_t part = lds.sums[3][lane & (NW - 1)] + (uint64_t)take * one;
+        const uint64_t run = lane_scan<NW>(part, (uint64_t)0, Add{});
+        total = from_lane(run, NW - 1);
+        mine = from_lane(part, wave);
+        base = from_lane(run, wave) - mine;
+        left = from_lane(take, wave);
+    }
+    const uint64_t target = share(total, cut31(q.u));
+    if (base <= target && target - base < mine) {   // one wave: it walks through its part
+        bool found = false;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (j < per && !found) {
+                renew(r[j]);
+                uint32_t held = 0;
+#pragma unroll
+                for (int v = 0; v < V; ++v) held += r[j][v] == kTie;
+                uint32_t before = 0, inside = 0;
+                if (__any(held != 0)) {
+                    const uint32_t run = wave_scan(held);
+                    before = run - held;
+                    inside = from_lane(run, 63);
+                }
+                uint64_t here = 0;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    if (r[j][v] == kTie) r[j][v] = before++ < left ? one : 0u;
+                    here += r[j][v];
+                }
+                const uint64_t run = wave_scan(here);
+                const uint64_t hit = __ballot(base + run > target);
+                if (hit) {
+                    if (lane == __ffsll((unsigned long long)hit) - 1) {
+                        uint64_t c = base + run - here;
+                        bool out = false;
+#pragma unroll
+                        for (int v = 0; v < V; ++v) {
+                            c += r[j][v];
+                            if (!out && c > target) {
+                                out = true;
+                                out_action[n] = vr.first(j) + v;
+                                out_logp[n] = q.greedy ? 0.0f : logf((float)r[j][v] / (float)total);
+                            }
+                        }
+                    }
+                    found = true;
+                }
+                base += from_lane(run, 63);
+                left -= min(left, inside);
+            }
+        }
     }
 }
 
@@ -963,9 +1022,8 @@ __global__ __launch_bounds__(kThreads) void sample_small_kernel(const Rows R, co
         const float u = uniform[m];
         const float top = group_max<G>(x);
         const bool bad = (__ballot(!(x < INFINITY)) & group) != 0 || !(temp >= 0.0f) || top == -INFINITY;
-        uint32_t w;
-        if (temp > 0.0f) w = Weights(top, temp)(x);
-        else w = lane == __ffsll((unsigned long long)(__ballot(x == top) & group)) - 1 ? 1u : 0u;
+        const bool greedy = temp == 0.0f;   // see RowSampling
+        uint32_t w = Weights(top, greedy ? 0x1p-126f : temp)(x);
         if constexpr (kFilter) {
             const int32_t k = S.top_ks ? S.top_ks[m] : S.top_k;
             const float top_p = S.top_ps ? S.top_ps[m] : S.top_p, min_p = S.min_ps ? S.min_ps[m] : S.min_p;
@@ -978,7 +1036,7 @@ __global__ __launch_bounds__(kThreads) void sample_small_kernel(const Rows R, co
                 rank += ahead;
                 before += ahead ? wi : 0u;
             }
-            if (temp > 0.0f) {
+            if (!greedy) {
                 if (k > 0 && rank >= k) w = 0;
                 if (top_p < 1.0f) {
                     const uint64_t need = share(group_sum<G>((uint64_t)w), cut31(top_p));
@@ -987,6 +1045,7 @@ __global__ __launch_bounds__(kThreads) void sample_small_kernel(const Rows R, co
                 if (w < (uint32_t)ceilf(fminf(fmaxf(min_p, 0.0f), 1.0f) * kOne)) w = 0;
             }
         }
+        if (greedy && w < 1u << 31) w = 0;
         uint64_t run = w;
 #pragma unroll
         for (int d = 1; d < G; d <<= 1) {
@@ -994,10 +1053,10 @@ __global__ __launch_bounds__(kThreads) void sample_small_kernel(const Rows R, co
             if (j >= d) run += o;
         }
         const uint64_t total = __shfl(run, first + G - 1);
-        const uint64_t hit = __ballot(run > share(total, cut31(u))) & group;
+        const uint64_t hit = __ballot(run > share(total, greedy ? 0u : cut31(u))) & group;
         if (live && !bad && lane == __ffsll((unsigned long long)hit) - 1) {
             out_action[n] = j;
-            out_logp[n] = logf((float)w / (float)total);
+            out_logp[n] = greedy ? 0.0f : logf((float)w / (float)total);
         }
         if (live && bad && j == 0) {
             out_action[n] = -1;
@@ -1344,7 +1403,8 @@ void launch_sample(const Rows& R, const Sampling& S, const float* uniform, int64
     constexpr int V = 16 / sizeof(T);
     const bool even = aligned(R.data, 16) && (R.rows == 1 || R.stride % V == 0);
     const int slots = R.actions + (even ? 0 : V - 1);
-    const dim3 grid(blocks_for(R.rows));
+    const unsigned gx = blocks_for(R.rows);
+    const dim3 grid(gx, slots <= kMostSlots ? (unsigned)((R.rows + gx - 1) / gx) : 1u);
     auto go = [&](auto kernel, int waves) {
         hipLaunchKernelGGL(kernel, grid, dim3(waves * 64), 0, s, R, S, uniform, action, logp);
     };
@@ -1355,7 +1415,7 @@ void launch_sample(const Rows& R, const Sampling& S, const float* uniform, int64
         else if (slots <= 4 * 64 * 32) go(sample_row_kernel<T, 4, 32, F>, 4);
         else if (slots <= 16 * 64 * 16) go(sample_row_kernel<T, 16, 16, F>, 16);
         else if (slots <= 16 * 64 * 32) go(sample_row_kernel<T, 16, 32, F>, 16);
-        else if (slots <= 16 * 64 * 72) go(sample_row_kernel<T, 16, 72, F>, 16);
+        else if (slots <= kMostSlots) go(sample_row_kernel<T, 16, 72, F>, 16);
         else go(sample_long_kernel<T>, kLongWaves);
     };
     if (filter) pick(std::true_type{});

@@ -127,6 +127,52 @@ def test_rows_that_make_no_draw_or_a_certain_one(mods, A):
             assert abs(logp[n].item() + np.log(count)) < 1e-5
 
 
+def _rule(torch, x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """The drawing rule in whole numbers, as the header states it."""
+    one = 1 << 31
+    share = lambda W, m: (W >> 32) * m * 2 + ((W & 0xFFFFFFFF) * m >> 31)
+    cut = lambda v: (v.clamp(0.0, 1.0 - 2.0 ** -24) * float(one)).to(torch.int64)
+    x = x.float()
+    col = torch.full_like(u, temperature)[:, None]
+    w = (((x - x.amax(1, keepdim=True)) / col).exp() * float(one)).round().to(torch.int64)
+    order = x.sort(dim=1, descending=True, stable=True).indices
+    ws = w.gather(1, order)
+    if top_k > 0:
+        ws[:, top_k:] = 0
+    if top_p < 1:
+        need = share(ws.sum(1, keepdim=True), cut(torch.tensor(top_p, dtype=torch.float32, device=x.device))).clamp_min(1)
+        ws = ws * (ws.cumsum(1) - ws < need)
+    ws = ws * (ws >= int(np.ceil(np.float32(min_p) * np.float32(one))))
+    w = torch.zeros_like(w).scatter_(1, order, ws)
+    c = w.cumsum(1)
+    act = (c <= share(c[:, -1:], cut(u)[:, None])).sum(1, keepdim=True)
+    return act[:, 0], (w.gather(1, act).float() / c[:, -1:].float()).log()[:, 0]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("A", [13, 64, 65, 999, 1025, 4090, 5000, 9000, 20000, 40001, 65536, 80000])
+def test_draws_follow_the_rule_to_the_bit(mods, A, dtype):
+    # Weights are whole numbers, so a draw is exact.  Rows of every kind a cut can
+    # fall into: spread ones, many equal logits, different logits of one weight (a
+    # long tail under a large logit), a tail that decides the sum, all equal.
+    torch, policy = mods
+    g = torch.Generator().manual_seed(A)
+    rnd = lambda *s: torch.randn(*s, generator=g)
+    x = torch.cat([rnd(4, A) * 2.5, rnd(2, A) * 0.5, (rnd(2, A) * 2).round(), rnd(4, A) * 1e-4 - 12.0, rnd(2, A) * 1e-6 - 18.0,
+                   rnd(1, A) * 8.0, torch.zeros(1, A)])
+    x[8:14, A // 3] = 0.0
+    x = x.to(getattr(torch, dtype)).cuda()
+    u = torch.rand(len(x), generator=g).cuda()
+    for how in (dict(), dict(top_p=0.9), dict(top_p=0.3, temperature=0.7), dict(top_p=0.02), dict(top_p=0.999, temperature=1.7),
+                dict(top_k=10), dict(top_k=300, top_p=0.8), dict(top_k=1500, top_p=0.5), dict(top_k=A // 2), dict(min_p=3e-6, top_p=0.95),
+                dict(min_p=0.05)):
+        act, logp = policy.sample_actions(x, u, **how)
+        want, wlogp = _rule(torch, x, u, **how)
+        assert torch.equal(act, want), (how, (act != want).nonzero().flatten().tolist())
+        # (the same whole numbers: their quotient's logarithm, a unit of it)
+        assert ((logp - wlogp).abs() <= 2.0 ** -22 * wlogp.abs() + 2.0 ** -23).all(), how
+
+
 def test_random_numbers_at_the_ends(mods):
     torch, policy = mods
     x = torch.zeros(7, 6).cuda()
