@@ -113,6 +113,13 @@ __device__ __forceinline__ uint64_t lanes(uint64_t old, uint64_t x)
 }
 
 template <int kCtrl, int kRows>
+__device__ __forceinline__ double lanes(double old, double x)
+{
+    return __longlong_as_double((long long)lanes<kCtrl, kRows>((uint64_t)__double_as_longlong(old),
+                                                               (uint64_t)__double_as_longlong(x)));
+}
+
+template <int kCtrl, int kRows>
 __device__ __forceinline__ float lanes(float old, float x)
 {
     return __uint_as_float(lanes<kCtrl, kRows>(__float_as_uint(old), __float_as_uint(x)));
@@ -139,6 +146,11 @@ __device__ __forceinline__ uint64_t from_lane(uint64_t x, int lane)
     return (uint64_t)from_lane((uint32_t)(x >> 32), lane) << 32 | from_lane((uint32_t)x, lane);
 }
 
+__device__ __forceinline__ double from_lane(double x, int lane)
+{
+    return __longlong_as_double((long long)from_lane((uint64_t)__double_as_longlong(x), lane));
+}
+
 __device__ __forceinline__ float from_lane(float x, int lane) { return __uint_as_float(from_lane(__float_as_uint(x), lane)); }
 
 struct Add {
@@ -154,20 +166,8 @@ struct Max {
 template <class V>
 __device__ __forceinline__ V wave_scan(V x) { return lane_scan<64>(x, (V)0, Add{}); }
 
-__device__ __forceinline__ uint32_t wave_sum(uint32_t x) { return from_lane(wave_scan(x), 63); }
-
-__device__ __forceinline__ uint64_t wave_sum(uint64_t x) { return from_lane(wave_scan(x), 63); }
-
-__device__ __forceinline__ double wave_sum(double x)
-{
-    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-    return x;
-}
-
-__device__ __forceinline__ float wave_sum(float x)
-{
-    return from_lane(lane_scan<64>(x, 0.0f, Add{}), 63);
-}
+template <class V>
+__device__ __forceinline__ V wave_sum(V x) { return from_lane(wave_scan(x), 63); }
 
 __device__ __forceinline__ float wave_max(float x) { return from_lane(lane_scan<64>(x, -INFINITY, Max{}), 63); }
 
@@ -181,13 +181,7 @@ __device__ __forceinline__ V block_sum(V x, V* lds)
     if constexpr (NW == 1) return x;
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
-    if constexpr (sizeof(V) == 8 && !std::is_integral<V>::value) {
-        x = lds[0];
-        for (int w = 1; w < NW; ++w) x += lds[w];
-        return x;
-    } else {
-        return from_lane(lane_scan<NW>(lds[threadIdx.x & (NW - 1)], (V)0, Add{}), NW - 1);
-    }
+    return from_lane(lane_scan<NW>(lds[threadIdx.x & (NW - 1)], (V)0, Add{}), NW - 1);
 }
 
 template <int NW>
@@ -1201,13 +1195,15 @@ __device__ __forceinline__ RowTerms row_terms(const Batch& b, const Shared3& s, 
 
 // Leave this workgroup's sums; the last workgroup to do so adds them all up, in the
 // order of the workgroups, and writes the statistics.
+template <int NW>
 __device__ void loss_finish(const Batch& b, const Shared3& s, const double* acc, double* __restrict__ sums,
-                            uint32_t* __restrict__ done, double* lds)
+                            uint32_t* __restrict__ done)
 {
     __shared__ uint32_t last;
+    __shared__ double lds[2][kSums][NW];
     double total[kSums];
 #pragma unroll
-    for (int k = 0; k < kSums; ++k) total[k] = loss_sum(acc[k], lds);
+    for (int k = 0; k < kSums; ++k) total[k] = block_sum<NW>(acc[k], lds[0][k]);
     if (threadIdx.x == 0) {
         for (int k = 0; k < kSums; ++k) sums[(int64_t)blockIdx.x * kSums + k] = total[k];
         __threadfence();
@@ -1217,11 +1213,11 @@ __device__ void loss_finish(const Batch& b, const Shared3& s, const double* acc,
     if (last != gridDim.x - 1) return;
     __threadfence();
     double x[kSums] = {};
-    for (unsigned i = threadIdx.x; i < gridDim.x; i += kThreads)
+    for (unsigned i = threadIdx.x; i < gridDim.x; i += NW * 64)
 #pragma unroll
         for (int k = 0; k < kSums; ++k) x[k] += sums[(int64_t)i * kSums + k];
 #pragma unroll
-    for (int k = 0; k < kSums; ++k) x[k] = loss_sum(x[k], lds) * (double)s.inv;
+    for (int k = 0; k < kSums; ++k) x[k] = block_sum<NW>(x[k], lds[1][k]) * (double)s.inv;
     if (threadIdx.x == 0) {
         b.stats[0] = (float)(x[0] + (double)b.value_coef * x[1] - (double)b.entropy_coef * x[2]);
         for (int k = 0; k < kSums; ++k) b.stats[k + 1] = (float)x[k];
@@ -1239,7 +1235,6 @@ struct Work {
 template <class T, int G>
 __global__ __launch_bounds__(kThreads) void loss_small_kernel(const Rows R, const Batch b, const Work k)
 {
-    __shared__ double lds[kWaves];
     const Shared3 s = loss_shared(b, k.part, k.parts);
     const int A = R.actions, j = threadIdx.x & (G - 1), first = threadIdx.x & 63 & ~(G - 1);
     const int64_t step = (int64_t)gridDim.x * (kThreads / G);
@@ -1278,14 +1273,139 @@ __global__ __launch_bounds__(kThreads) void loss_small_kernel(const Rows R, cons
         }
         if (j < A) ((T*)b.dlogits)[n * b.dstride + j] = (T)y;
     }
-    loss_finish(b, s, acc, k.sums, k.done, lds);
+    loss_finish<kWaves>(b, s, acc, k.sums, k.done);
+}
+
+// exp d for d <= 0.  d log2 e rounded once is off by up to 2^-24 of itself, which
+// the exponential of a large |d| shows; fp32 gradients take the rest of the product
+// along.
+template <class T>
+__device__ __forceinline__ float exp_of(float d)
+{
+    constexpr float kLog2e = 1.44269502f, kRest = 1.92596299e-8f;   // log2 e = their sum
+    const float h = d * kLog2e;
+    const float e = __builtin_amdgcn_exp2f(h);
+    if constexpr (sizeof(T) == 2) return e;
+    const float l = fmaf(d, kRest, fmaf(d, kLog2e, -h));
+    return fmaf(e, l * 0.693147182f, e);
+}
+
+// Rows held in registers, as in sample_row_kernel: the logits are read once and the
+// gradient written once.  With e = exp d and S its sum, d loss / d logit of action i is
+// e_i (k1 d_i + k0), plus g at the action taken.
+template <class T, int NW, int ITEMS>
+__global__ __launch_bounds__(NW * 64) void loss_row_kernel(const Rows R, const Batch b, const Work k)
+{
+    constexpr int V = 16 / sizeof(T), NV = ITEMS / V;
+    __shared__ float maxima[NW], sums[2][NW];
+    __shared__ double acc[kSums];
+    const Shared3 s = loss_shared(b, k.part, k.parts);
+    const int A = R.actions;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const float rt = 1.0f / b.temperature;
+    if (threadIdx.x == 0)
+        for (int q = 0; q < kSums; ++q) acc[q] = 0.0;
+    for (int64_t n = blockIdx.x; n < R.rows; n += gridDim.x) {
+        const VecRow<T, NW, NV> vr(R, n, wave, lane);
+        const int per = vr.per;
+        const float w = same_in_wave(row_weight(b, n, A));
+        const bool on = w != 0.0f;
+        const int a = on ? (int)same_in_wave((uint32_t)b.actions[n]) : 0;
+        uint32_t r[NV][V];
+        float k1 = 0.0f, k0 = 0.0f, ga = 0.0f;
+        if (on) {
+            const float xa = vr.row(a);
+            vr.load(r);
+            float top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j < per) {
+                    renew(r[j]);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) top = fmaxf(top, __uint_as_float(r[j][v]));
+                }
+            top = block_max<NW>(top, maxima);
+            if (top == -INFINITY) top = 0.0f;   // nothing is allowed
+            // (an exponential of zero is cut off there; a NaN stays one)
+            auto dist = [&](float x) {
+                const float d = (x - top) * rt;
+                return d < -1e4f ? -1e4f : d;
+            };
+            float e0 = 0.0f, e1 = 0.0f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j < per) {
+                    renew(r[j]);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const float d = dist(__uint_as_float(r[j][v])), e = exp_of<T>(d);
+                        e0 += e;
+                        e1 = fmaf(e, d, e1);
+                        r[j][v] = __float_as_uint(d);
+                    }
+                }
+            e0 = wave_sum(e0);
+            e1 = wave_sum(e1);
+            if constexpr (NW > 1) {
+                if (lane == 0) {
+                    sums[0][wave] = e0;
+                    sums[1][wave] = e1;
+                }
+                __syncthreads();
+                e0 = from_lane(lane_scan<NW>(sums[0][lane & (NW - 1)], 0.0f, Add{}), NW - 1);
+                e1 = from_lane(lane_scan<NW>(sums[1][lane & (NW - 1)], 0.0f, Add{}), NW - 1);
+            }
+            const float logs = logf(e0), rs = 1.0f / e0;
+            const float H = e0 > 0.0f ? logs - e1 * rs : e0 == 0.0f ? 0.0f : e0;
+            const RowTerms t = row_terms(b, s, n, e0 == 0.0f ? -INFINITY : (xa - top) * rt - logs, H);
+            const float scale = w * s.inv;
+            k1 = e0 == 0.0f ? 0.0f : b.entropy_coef * rs * scale * rt;
+            k0 = e0 == 0.0f ? 0.0f : (b.entropy_coef * (H - logs) - t.g) * rs * scale * rt;
+            ga = t.g * scale * rt;
+            if (threadIdx.x == 0) {
+                b.dvalues[n] = t.dv * scale;
+#pragma unroll
+                for (int q = 0; q < kSums; ++q) acc[q] += (double)w * (double)t.sums[q];
+            }
+        } else if (threadIdx.x == 0) {
+            b.dvalues[n] = 0.0f;
+        }
+        T* out = (T*)b.dlogits + n * b.dstride;
+        struct alignas(16) Vec { T v[V]; };
+        const bool even = ((reinterpret_cast<uintptr_t>(out) / sizeof(T) - vr.shift) & (V - 1)) == 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (j < per) {
+                renew(r[j]);
+                const int i0 = vr.first(j);
+                Vec y;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float d = __uint_as_float(r[j][v]);
+                    float z = on ? exp_of<T>(d) * fmaf(d, k1, k0) : 0.0f;
+                    if (on && i0 + v == a) z += ga;
+                    y.v[v] = (T)z;
+                }
+                if (even && vr.whole(j)) {
+                    *reinterpret_cast<Vec*>(out + i0) = y;
+                } else {
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        if (i0 + v >= 0 && i0 + v < A) out[i0 + v] = y.v[v];
+                }
+            }
+        if constexpr (NW > 1) __syncthreads();
+    }
+    __syncthreads();
+    double mine[kSums];
+    for (int q = 0; q < kSums; ++q) mine[q] = threadIdx.x == 0 ? acc[q] : 0.0;
+    loss_finish<NW>(b, s, mine, k.sums, k.done);
 }
 
 // One workgroup per row, the row read again for every pass.
 template <class T>
-__global__ __launch_bounds__(kThreads) void loss_kernel(const Rows R, const Batch b, const Work k)
+__global__ __launch_bounds__(kThreads) void loss_long_kernel(const Rows R, const Batch b, const Work k)
 {
-    __shared__ double ldsd[kWaves];
     __shared__ float ldsf[kWaves];
     const Shared3 s = loss_shared(b, k.part, k.parts);
     const int A = R.actions;
@@ -1332,7 +1452,7 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(const Rows R, const Batc
         }
         __syncthreads();
     }
-    loss_finish(b, s, acc, k.sums, k.done, ldsd);
+    loss_finish<kWaves>(b, s, acc, k.sums, k.done);
 }
 
 // ---------------------------------------------------------------------------
@@ -1362,19 +1482,33 @@ unsigned blocks_for(int64_t rows) { return (unsigned)(rows < kMaxBlocks ? rows :
 // Lanes that hold a row of up to 64 actions.
 int group_lanes(int32_t actions) { return actions <= 8 ? 8 : actions <= 16 ? 16 : actions <= 32 ? 32 : 64; }
 
-// Workgroups of the loss: each leaves one set of partial sums.
+// Waves of a workgroup that holds a row of so many slots in its registers.
+int row_waves(int slots) { return slots <= 64 * 16 ? 1 : slots <= 4 * 64 * 32 ? 4 : 16; }
+
+// Workgroups of the loss: each leaves one set of partial sums, so there are no more
+// than fill the card a few times.
 constexpr int64_t kLossBlocks = 4096;
 
 int64_t loss_blocks(int64_t rows, int32_t actions)
 {
     const int64_t per = actions <= 64 ? kThreads / group_lanes(actions) : 1;
+    const int64_t most = actions <= 64 ? 1024 : kLossBlocks / row_waves(actions);
     const int64_t b = (rows + per - 1) / per;
-    return b < 1 ? 1 : b < kLossBlocks ? b : kLossBlocks;
+    return b < 1 ? 1 : b < most ? b : most;
 }
 
 uint64_t loss_bytes(int64_t rows, int32_t actions)
 {
     return sizeof(double) * (uint64_t)(kMomentBlocks * 3 + loss_blocks(rows, actions) * kSums) + 256;
+}
+
+// Slots a row takes: rows that do not start at 16-byte addresses begin inside a vector.
+template <class T>
+int slots_of(const Rows& R)
+{
+    constexpr int V = 16 / sizeof(T);
+    const bool even = aligned(R.data, 16) && (R.rows == 1 || R.stride % V == 0);
+    return R.actions + (even ? 0 : V - 1);
 }
 
 template <class T>
@@ -1399,10 +1533,7 @@ void launch_sample(const Rows& R, const Sampling& S, const float* uniform, int64
         return;
     }
     const bool filter = S.top_ks || S.top_ps || (S.top_k > 0 && S.top_k < R.actions) || S.top_p < 1.0f;
-    // slots a row takes: rows that do not start at 16-byte addresses begin inside a vector
-    constexpr int V = 16 / sizeof(T);
-    const bool even = aligned(R.data, 16) && (R.rows == 1 || R.stride % V == 0);
-    const int slots = R.actions + (even ? 0 : V - 1);
+    const int slots = slots_of<T>(R);
     const unsigned gx = blocks_for(R.rows);
     const dim3 grid(gx, slots <= kMostSlots ? (unsigned)((R.rows + gx - 1) / gx) : 1u);
     auto go = [&](auto kernel, int waves) {
@@ -1427,8 +1558,17 @@ void launch_loss(const Rows& R, const Batch& b, const Work& k, hipStream_t s)
 {
     const dim3 grid((unsigned)loss_blocks(R.rows, R.actions)), block(kThreads);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, R, b, k); };
-    if (R.actions > 64) go(loss_kernel<T>);
-    else if (group_lanes(R.actions) == 8) go(loss_small_kernel<T, 8>);
+    if (R.actions > 64) {
+        const int slots = slots_of<T>(R);
+        auto row = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3(waves * 64), 0, s, R, b, k); };
+        if (slots <= 64 * 16) row(loss_row_kernel<T, 1, 16>, 1);
+        else if (slots <= 4 * 64 * 16) row(loss_row_kernel<T, 4, 16>, 4);
+        else if (slots <= 4 * 64 * 32) row(loss_row_kernel<T, 4, 32>, 4);
+        else if (slots <= 16 * 64 * 16) row(loss_row_kernel<T, 16, 16>, 16);
+        else if (slots <= 16 * 64 * 32) row(loss_row_kernel<T, 16, 32>, 16);
+        else if (slots <= kMostSlots) row(loss_row_kernel<T, 16, 72>, 16);
+        else go(loss_long_kernel<T>);
+    } else if (group_lanes(R.actions) == 8) go(loss_small_kernel<T, 8>);
     else if (group_lanes(R.actions) == 16) go(loss_small_kernel<T, 16>);
     else if (group_lanes(R.actions) == 32) go(loss_small_kernel<T, 32>);
     else go(loss_small_kernel<T, 64>);
