@@ -20,7 +20,7 @@ constexpr int kBlk = PICTURA_ADAMW_BLOCK;
 constexpr float kTiny = 0x1p-90f;                // below it a block's moments count as zero: 1 / scale stays finite
 static_assert(kChunk % kBlk == 0, "blocks do not straddle workgroups");
 
-struct TensorArg {
+struct alignas(8) TensorArg {
     void* param;
     const void* grad;
     void* m;
@@ -30,6 +30,7 @@ struct TensorArg {
     int64_t n;
     int32_t first;      // workgroup of its first chunk
     uint8_t pt, gt;     // PICTURA_F32 ..
+    uint8_t vec;        // 1: four elements at a time are aligned in every array
 };
 
 struct TensorArgs {
@@ -54,6 +55,11 @@ __device__ __forceinline__ int tensor_of(const TensorArgs& a, int b)
     return lo;
 }
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Elements of any of the types, in fp32; four from i on, or, without `vec`, those of
+// them below n.
 __device__ __forceinline__ float load_as(const void* p, int type, int64_t i)
 {
     if (type == PICTURA_F32) return ((const float*)p)[i];
@@ -66,6 +72,44 @@ __device__ __forceinline__ void store_as(void* p, int type, int64_t i, float x)
     if (type == PICTURA_F32) ((float*)p)[i] = x;
     else if (type == PICTURA_BF16) ((__bf16*)p)[i] = (__bf16)x;
     else ((_Float16*)p)[i] = (_Float16)x;
+}
+
+template <class T>
+struct Four {
+    T v[4];
+};
+
+__device__ __forceinline__ void load4(const void* p, int type, int64_t i, float* x)
+{
+    if (type == PICTURA_F32) {
+        const f32x4 t = *(const f32x4*)((const float*)p + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = t[k];
+        return;
+    }
+    const u32x2 t = *(const u32x2*)((const uint16_t*)p + i);
+    if (type == PICTURA_BF16) {
+        const Four<__bf16> h = __builtin_bit_cast(Four<__bf16>, t);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = (float)h.v[k];
+    } else {
+        const Four<_Float16> h = __builtin_bit_cast(Four<_Float16>, t);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = (float)h.v[k];
+    }
+}
+
+__device__ __forceinline__ void store4(void* p, int type, int64_t i, const float* x)
+{
+    if (type == PICTURA_F32) {
+        *(f32x4*)((float*)p + i) = f32x4{x[0], x[1], x[2], x[3]};
+    } else if (type == PICTURA_BF16) {
+        const Four<__bf16> h = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+        *(u32x2*)((uint16_t*)p + i) = __builtin_bit_cast(u32x2, h);
+    } else {
+        const Four<_Float16> h = {(_Float16)x[0], (_Float16)x[1], (_Float16)x[2], (_Float16)x[3]};
+        *(u32x2*)((uint16_t*)p + i) = __builtin_bit_cast(u32x2, h);
+    }
 }
 
 // m and v after the gradient g, and the parameter.
@@ -118,7 +162,39 @@ __global__ __launch_bounds__(kThreads) void adamw32_kernel(const TensorArgs a, c
     const int n = (int)min((int64_t)kChunk, t.n - at);
     float* m = (float*)t.m + at;
     float* v = (float*)t.v + at;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
+    const int n4 = t.vec ? n & ~3 : 0;
+    constexpr int kAhead = 2;   // groups of four in flight: more take registers and gain nothing
+    for (int i0 = threadIdx.x * 4; i0 < n4; i0 += kThreads * 4 * kAhead) {
+        float p[kAhead][4], g[kAhead][4];
+        f32x4 mi[kAhead], vi[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = i0 + u * kThreads * 4;
+            if (i < n4) {
+                load4(t.grad, t.gt, at + i, g[u]);
+                load4(t.param, t.pt, at + i, p[u]);
+                mi[u] = *(const f32x4*)(m + i);
+                vi[u] = *(const f32x4*)(v + i);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = i0 + u * kThreads * 4;
+            if (i < n4) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float mk = mi[u][k], vk = vi[u][k];
+                    p[u][k] = adamw(f, p[u][k], g[u][k] * gf, mk, vk);
+                    mi[u][k] = mk;
+                    vi[u][k] = vk;
+                }
+                *(f32x4*)(m + i) = mi[u];
+                *(f32x4*)(v + i) = vi[u];
+                store4(t.param, t.pt, at + i, p[u]);
+            }
+        }
+    }
+    for (int i = n4 + threadIdx.x; i < n; i += kThreads) {
         float mi = m[i], vi = v[i];
         const float p = adamw(f, load_as(t.param, t.pt, at + i), load_as(t.grad, t.gt, at + i) * gf, mi, vi);
         m[i] = mi;
@@ -127,7 +203,20 @@ __global__ __launch_bounds__(kThreads) void adamw32_kernel(const TensorArgs a, c
     }
 }
 
-// A wave takes a block of 256 elements, four to a lane.
+// Maximum over the wave's lanes (row shifts and broadcasts of the vector unit), the same in all.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x)
+{
+    auto with = [&](uint32_t y) { x = max(x, y); };
+    with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));
+    with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+    with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+    with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+    with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));
+    with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
+// A wave takes a block of 256 elements, four neighbours to a lane.
 __global__ __launch_bounds__(kThreads) void adamw8_kernel(const TensorArgs a, const StepFactors f)
 {
     const TensorArg& t = a.t[tensor_of(a, (int)blockIdx.x)];
@@ -138,40 +227,64 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const TensorArgs a, co
         const int64_t i0 = at + (int64_t)b * kBlk;
         if (i0 >= t.n) break;
         const int n = (int)min((int64_t)kBlk, t.n - i0);
-        const float ms = m_unit(t.ms[i0 / kBlk]), vs = v_unit(t.vs[i0 / kBlk]);
+        const int i = lane * 4;
+        const bool four = t.vec && i + 4 <= n;
         int8_t* cm = (int8_t*)t.m + i0;
         uint8_t* cv = (uint8_t*)t.v + i0;
+        float p[4] = {}, g[4] = {};
+        Four<int8_t> qm = {};
+        Four<uint8_t> qv = {};
+        if (four) {
+            load4(t.grad, t.gt, i0 + i, g);
+            load4(t.param, t.pt, i0 + i, p);
+            qm = __builtin_bit_cast(Four<int8_t>, *(const uint32_t*)(cm + i));
+            qv = __builtin_bit_cast(Four<uint8_t>, *(const uint32_t*)(cv + i));
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k < n) {
+                    g[k] = load_as(t.grad, t.gt, i0 + i + k);
+                    p[k] = load_as(t.param, t.pt, i0 + i + k);
+                    qm.v[k] = cm[i + k];
+                    qv.v[k] = cv[i + k];
+                }
+        }
+        const float ms = m_unit(t.ms[i0 / kBlk]), vs = v_unit(t.vs[i0 / kBlk]);
         float m[4], v[4];
         // largest magnitudes by their bits: a NaN is larger than any number
         uint32_t mm = 0, vm = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int i = lane + 64 * k;
             m[k] = v[k] = 0.0f;
-            if (i < n) {
-                m[k] = m_value(cm[i], ms);
-                v[k] = v_value(cv[i], vs);
-                const float p = adamw(f, load_as(t.param, t.pt, i0 + i), load_as(t.grad, t.gt, i0 + i) * gf, m[k], v[k]);
-                store_as(t.param, t.pt, i0 + i, p);
+            if (i + k < n) {
+                m[k] = m_value(qm.v[k], ms);
+                v[k] = v_value(qv.v[k], vs);
+                p[k] = adamw(f, p[k], g[k] * gf, m[k], v[k]);
             }
             mm = max(mm, __float_as_uint(fabsf(m[k])));
             vm = max(vm, __float_as_uint(fabsf(v[k])));
         }
-        for (int d = 32; d; d >>= 1) {
-            mm = max(mm, (uint32_t)__shfl_xor((int)mm, d));
-            vm = max(vm, (uint32_t)__shfl_xor((int)vm, d));
-        }
-        float nms = __uint_as_float(mm), nvs = __uint_as_float(vm);
+        float nms = __uint_as_float(wave_max(mm)), nvs = __uint_as_float(wave_max(vm));
         if (nms < kTiny) nms = 0.0f;
         if (nvs < kTiny) nvs = 0.0f;
         const float im = nms > 0.0f ? 1.0f / nms : 0.0f, iv = nvs > 0.0f ? 1.0f / nvs : 0.0f;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int i = lane + 64 * k;
-            if (i < n) {
-                cm[i] = (int8_t)m_code(m[k], im);
-                cv[i] = (uint8_t)v_code(v[k], iv);
-            }
+            qm.v[k] = (int8_t)m_code(m[k], im);
+            qv.v[k] = (uint8_t)v_code(v[k], iv);
+        }
+        if (four) {
+            store4(t.param, t.pt, i0 + i, p);
+            *(uint32_t*)(cm + i) = __builtin_bit_cast(uint32_t, qm);
+            *(uint32_t*)(cv + i) = __builtin_bit_cast(uint32_t, qv);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k < n) {
+                    store_as(t.param, t.pt, i0 + i + k, p[k]);
+                    cm[i + k] = qm.v[k];
+                    cv[i + k] = qv.v[k];
+                }
         }
         if (lane == 0) {
             t.ms[i0 / kBlk] = nms;
@@ -186,10 +299,29 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(const TensorArgs a)
     const TensorArg& t = a.t[tensor_of(a, (int)blockIdx.x)];
     const int64_t at = (int64_t)((int)blockIdx.x - t.first) * kChunk;
     const int n = (int)min((int64_t)kChunk, t.n - at);
-    for (int j = threadIdx.x; j < n; j += kThreads) {
-        const int64_t i = at + j;
-        ((float*)t.param)[i] = m_value(((const int8_t*)t.m)[i], m_unit(t.ms[i / kBlk]));
-        ((float*)t.grad)[i] = v_value(((const uint8_t*)t.v)[i], v_unit(t.vs[i / kBlk]));
+    const int8_t* cm = (const int8_t*)t.m + at;
+    const uint8_t* cv = (const uint8_t*)t.v + at;
+    float* om = (float*)t.param + at;
+    float* ov = (float*)t.grad + at;
+    const float* ms = t.ms + at / kBlk;
+    const float* vs = t.vs + at / kBlk;
+    const int n4 = t.vec ? n & ~3 : 0;
+    for (int i = threadIdx.x * 4; i < n4; i += kThreads * 4) {
+        const Four<int8_t> qm = __builtin_bit_cast(Four<int8_t>, *(const uint32_t*)(cm + i));
+        const Four<uint8_t> qv = __builtin_bit_cast(Four<uint8_t>, *(const uint32_t*)(cv + i));
+        const float um = m_unit(ms[i / kBlk]), uv = v_unit(vs[i / kBlk]);
+        f32x4 m, v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            m[k] = m_value(qm.v[k], um);
+            v[k] = v_value(qv.v[k], uv);
+        }
+        *(f32x4*)(om + i) = m;
+        *(f32x4*)(ov + i) = v;
+    }
+    for (int i = n4 + threadIdx.x; i < n; i += kThreads) {
+        om[i] = m_value(cm[i], m_unit(ms[i / kBlk]));
+        ov[i] = v_value(cv[i], v_unit(vs[i / kBlk]));
     }
 }
 
@@ -204,14 +336,24 @@ __device__ __forceinline__ double block_sum(double x, double* lds)
     return x;
 }
 
-__global__ __launch_bounds__(kThreads) void norm_part_kernel(const TensorArgs a, double* __restrict__ part)
+__global__ __launch_bounds__(kThreads) void norm_part_kernel(const TensorArgs a, int64_t chunk, double* __restrict__ part)
 {
     __shared__ double lds[kThreads / 64];
     const TensorArg& t = a.t[tensor_of(a, (int)blockIdx.x)];
-    const int64_t at = (int64_t)((int)blockIdx.x - t.first) * kChunk;
-    const int n = (int)min((int64_t)kChunk, t.n - at);
+    const int64_t at = (int64_t)((int)blockIdx.x - t.first) * chunk;
+    const int64_t n = min(chunk, t.n - at), n4 = t.vec ? n & ~(int64_t)3 : 0;
     double s = 0.0;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
+    for (int64_t i0 = threadIdx.x * 4; i0 < n4; i0 += kThreads * 16) {
+        float g[4][4] = {};
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i0 + u * kThreads * 4 < n4) load4(t.grad, t.gt, at + i0 + u * kThreads * 4, g[u]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s = fma((double)g[u][k], (double)g[u][k], s);
+    }
+    for (int64_t i = n4 + threadIdx.x; i < n; i += kThreads) {
         const double g = (double)load_as(t.grad, t.gt, at + i);
         s = fma(g, g, s);
     }
@@ -236,7 +378,7 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const double* __restrict
 
 namespace {
 
-int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
+int64_t chunks_of(int64_t n, int64_t chunk) { return (n + chunk - 1) / chunk; }
 
 size_t size_of(int type) { return type == PICTURA_F32 ? 4 : 2; }
 
@@ -245,9 +387,10 @@ bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) 
 bool dtype_ok(int32_t t) { return t == PICTURA_F32 || t == PICTURA_BF16 || t == PICTURA_F16; }
 
 // Split the tensors over launches of at most kTensors tensors and 2^22
-// workgroups; a tensor beyond that is taken in parts.  launch(args, blocks).
+// workgroups of `chunk` elements; a tensor beyond that is taken in parts.
+// launch(args, blocks).
 template <class Fill, class Launch>
-void for_launches(const pictura_adamw_tensor* ts, int32_t count, Fill fill, Launch launch)
+void for_launches(const pictura_adamw_tensor* ts, int32_t count, int64_t chunk, Fill fill, Launch launch)
 {
     constexpr int64_t kMostBlocks = 1 << 22;
     TensorArgs a;
@@ -261,15 +404,15 @@ void for_launches(const pictura_adamw_tensor* ts, int32_t count, Fill fill, Laun
     for (int32_t k = 0; k < count; ++k) {
         int64_t at = 0;
         while (at < ts[k].n) {
-            const int64_t left = chunks_of(ts[k].n - at), room = kMostBlocks - blocks;
+            const int64_t left = chunks_of(ts[k].n - at, chunk), room = kMostBlocks - blocks;
             const int64_t take = left < room ? left : room;
             TensorArg& t = a.t[a.count];
-            t.n = ts[k].n - at < take * kChunk ? ts[k].n - at : take * kChunk;
+            t.n = ts[k].n - at < take * chunk ? ts[k].n - at : take * chunk;
             t.first = (int32_t)blocks;
             fill(t, k, at);
             ++a.count;
             blocks += take;
-            at += take * kChunk;
+            at += take * chunk;
             if (a.count == kTensors || blocks == kMostBlocks) flush();
         }
     }
@@ -287,6 +430,17 @@ void fill_common(TensorArg& t, const pictura_adamw_tensor& s, int64_t at, int bi
     t.vs = bits == 8 ? s.exp_avg_sq_scale + at / kBlk : nullptr;
     t.pt = (uint8_t)s.param_dtype;
     t.gt = (uint8_t)s.grad_dtype;
+    t.vec = aligned(t.param, 4 * size_of(s.param_dtype)) && aligned(t.grad, 4 * size_of(s.grad_dtype)) &&
+            aligned(t.m, 4 * b) && aligned(t.v, 4 * b);
+}
+
+// Elements of a workgroup of the norm: some 1,024 workgroups, whose sums one more adds up.
+int64_t norm_chunk(const pictura_adamw_tensor* ts, int32_t count)
+{
+    int64_t n = 0;
+    for (int32_t k = 0; k < count; ++k) n += ts[k].n;
+    const int64_t c = chunks_of(n, 1024);
+    return c < kChunk ? kChunk : chunks_of(c, kChunk) * kChunk;
 }
 
 constexpr int64_t kMostElements = 1ll << 48;
@@ -321,11 +475,11 @@ extern "C" {
 pictura_status pictura_grad_norm_workspace(const pictura_adamw_tensor* tensors, int32_t count, uint64_t* bytes)
 {
     if (!bytes || count < 0 || (count > 0 && !tensors)) return PICTURA_EINVAL;
-    int64_t n = 0;
-    for (int32_t k = 0; k < count; ++k) {
+    for (int32_t k = 0; k < count; ++k)
         if (tensors[k].n < 0 || tensors[k].n > kMostElements) return PICTURA_EINVAL;
-        n += chunks_of(tensors[k].n);
-    }
+    const int64_t chunk = norm_chunk(tensors, count);
+    int64_t n = 0;
+    for (int32_t k = 0; k < count; ++k) n += chunks_of(tensors[k].n, chunk);
     *bytes = (uint64_t)(n > 0 ? n : 1) * sizeof(double);
     return PICTURA_OK;
 }
@@ -342,14 +496,16 @@ pictura_status pictura_grad_norm(const pictura_adamw_tensor* tensors, int32_t co
     hipStream_t s = (hipStream_t)stream;
     double* part = (double*)workspace;
     int64_t n = 0;
+    const int64_t chunk = norm_chunk(tensors, count);
     for_launches(
-        tensors, count,
+        tensors, count, chunk,
         [&](TensorArg& t, int32_t k, int64_t at) {
             t.grad = (const char*)tensors[k].grad + at * size_of(tensors[k].grad_dtype);
             t.gt = (uint8_t)tensors[k].grad_dtype;
+            t.vec = aligned(t.grad, 4 * size_of(tensors[k].grad_dtype));
         },
         [&](const TensorArgs& a, unsigned blocks) {
-            hipLaunchKernelGGL(norm_part_kernel, dim3(blocks), dim3(kThreads), 0, s, a, part + n);
+            hipLaunchKernelGGL(norm_part_kernel, dim3(blocks), dim3(kThreads), 0, s, a, chunk, part + n);
             n += blocks;
         });
     hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, s, part, n, max_norm, out);
@@ -375,7 +531,7 @@ pictura_status pictura_adamw_step(const pictura_adamw* how, const pictura_adamw_
                         (float)(1.0 / std::sqrt(bc2)), (float)how->eps, (float)(1.0 - how->lr * how->weight_decay),
                         (float)(how->lr / bc1), how->grad_factor};
     for_launches(
-        tensors, count, [&](TensorArg& t, int32_t k, int64_t at) { fill_common(t, tensors[k], at, how->bits); },
+        tensors, count, kChunk, [&](TensorArg& t, int32_t k, int64_t at) { fill_common(t, tensors[k], at, how->bits); },
         [&](const TensorArgs& a, unsigned blocks) {
             if (how->bits == 32) hipLaunchKernelGGL(adamw32_kernel, dim3(blocks), dim3(kThreads), 0, s, a, f);
             else hipLaunchKernelGGL(adamw8_kernel, dim3(blocks), dim3(kThreads), 0, s, a, f);
@@ -396,11 +552,12 @@ pictura_status pictura_adamw_moments(const pictura_adamw_tensor* tensors, int32_
     }
     hipStream_t s = (hipStream_t)stream;
     for_launches(
-        tensors, count,
+        tensors, count, kChunk,
         [&](TensorArg& t, int32_t k, int64_t at) {
             fill_common(t, tensors[k], at, 8);
             t.param = exp_avg_out[k] + at;
             t.grad = exp_avg_sq_out[k] + at;
+            t.vec = aligned(t.param, 16) && aligned(t.grad, 16) && aligned(t.m, 4) && aligned(t.v, 4);
         },
         [&](const TensorArgs& a, unsigned blocks) {
             hipLaunchKernelGGL(moments_kernel, dim3(blocks), dim3(kThreads), 0, s, a);
