@@ -1,4 +1,5 @@
-"""Builds the HIP library libpictura.so for gfx950 (in-tree)."""
+"""Builds the HIP library libpictura.so for gfx950 and the binding's helper
+_tensors.so (in-tree)."""
 import os
 import subprocess
 
@@ -6,6 +7,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libpictura.so")
+TENSORS = os.path.join(HERE, "_tensors.so")
 SOURCES = ["pictura_binner.hip", "pictura_render.hip", "pictura_encoder.hip", "pictura_policy.hip", "pictura_adamw.hip",
            "pictura_abi.hip"]
 # (source, object name, extra flags): the render source is compiled three
@@ -33,10 +35,27 @@ HIPCC_FLAGS = [
 ]
 
 
+def _tensors_command(out: str) -> list:
+    """The host compiler's command for the helper that reads lists of torch tensors."""
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    inc = os.path.join(root, "include")
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-isystem", inc, "-isystem",
+            os.path.join(inc, "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
+            os.path.join(CSRC, "pictura_tensors.cpp"), "-o", out, "-L", os.path.join(root, "lib"), "-ltorch_python",
+            "-ltorch", "-ltorch_cpu", "-lc10"]
+
+
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     objs = []
-    procs = []
+    tensors = _tensors_command(TENSORS + ".tmp")
+    if verbose:
+        print(" ".join(tensors))
+    procs = [subprocess.Popen(tensors)]
     for src, oname, extra in UNITS:
         obj = os.path.join(CSRC, oname)
         cmd = [hipcc, *HIPCC_FLAGS, *extra, "-I", INCLUDE, "-c", os.path.join(CSRC, src), "-o", obj]
@@ -46,7 +65,8 @@ def build(verbose: bool = False) -> str:
         objs.append(obj)
     for p in procs:
         if p.wait() != 0:
-            raise RuntimeError("hipcc failed")
+            raise RuntimeError(f"{p.args[0]} failed")
+    os.replace(TENSORS + ".tmp", TENSORS)
     tmp = LIB + ".tmp"
     subprocess.check_call([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-Wl,--no-undefined", "-o", tmp, *objs])
     os.replace(tmp, LIB)

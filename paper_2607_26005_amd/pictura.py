@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -93,6 +94,12 @@ class _AdamW(ctypes.Structure):
                [("step", ctypes.c_int64), ("bits", ctypes.c_int32), ("grad_factor", ctypes.c_void_p)]
 
 
+# The same structs packed: a tenth of the time of filling a ctypes one, in calls of a few microseconds
+_LOGITS_PACK, _SAMPLING_PACK = struct.Struct("@PiiqqPq"), struct.Struct("@fiffPPPP")
+_BATCH_PACK, _ADAMW_PACK = struct.Struct("@PqPPPPPPffffffi4x"), struct.Struct("@dddddqi4xP")
+assert [p.size for p in (_LOGITS_PACK, _SAMPLING_PACK, _BATCH_PACK, _ADAMW_PACK)] == \
+    [ctypes.sizeof(c) for c in (_Logits, _Sampling, _PolicyBatch, _AdamW)]
+
 # pictura_adamw_tensor, as a row of a table: a step fills the columns
 ADAMW_TENSOR = np.dtype([(n, np.uint64) for n in ("param", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale",
                                                   "exp_avg_sq_scale")] +
@@ -146,18 +153,17 @@ _lib.pictura_encoder_workspace.restype = ctypes.c_int32
 _lib.pictura_encode_views.argtypes = [ctypes.POINTER(_Encoder), _P, _P, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
                                       _P, ctypes.c_uint64, _P, _P]
 _lib.pictura_encode_views.restype = ctypes.c_int32
-_lib.pictura_sample_actions.argtypes = [ctypes.POINTER(_Logits), ctypes.POINTER(_Sampling), _P, _P, _P, _P]
+_lib.pictura_sample_actions.argtypes = [_P, _P, _P, _P, _P, _P]
 _lib.pictura_sample_actions.restype = ctypes.c_int32
 _lib.pictura_policy_loss_workspace.argtypes = [ctypes.c_int64, ctypes.c_int32, _P]
 _lib.pictura_policy_loss_workspace.restype = ctypes.c_int32
-_lib.pictura_policy_loss.argtypes = [ctypes.POINTER(_Logits), ctypes.POINTER(_PolicyBatch), _P, ctypes.c_uint64, _P, _P,
-                                     ctypes.c_int64, _P, _P]
+_lib.pictura_policy_loss.argtypes = [_P, _P, _P, ctypes.c_uint64, _P, _P, ctypes.c_int64, _P, _P]
 _lib.pictura_policy_loss.restype = ctypes.c_int32
 _lib.pictura_grad_norm_workspace.argtypes = [_P, ctypes.c_int32, _P]
 _lib.pictura_grad_norm_workspace.restype = ctypes.c_int32
 _lib.pictura_grad_norm.argtypes = [_P, ctypes.c_int32, ctypes.c_float, _P, ctypes.c_uint64, _P, _P]
 _lib.pictura_grad_norm.restype = ctypes.c_int32
-_lib.pictura_adamw_step.argtypes = [ctypes.POINTER(_AdamW), _P, ctypes.c_int32, _P]
+_lib.pictura_adamw_step.argtypes = [_P, _P, ctypes.c_int32, _P]
 _lib.pictura_adamw_step.restype = ctypes.c_int32
 _lib.pictura_adamw_moments.argtypes = [_P, ctypes.c_int32, _P, _P, _P]
 _lib.pictura_adamw_moments.restype = ctypes.c_int32
@@ -473,82 +479,90 @@ def pictura_encode_views(cams, num_classes, convs, queries, in_proj, out_proj, p
 
 # --- the policy's operators -------------------------------------------------------
 
-def _codes():
-    import torch
-    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-
-
 _DTYPE_CODES = {}
 
 
 def _dtype_code(t, name: str) -> int:
     if not _DTYPE_CODES:
-        _DTYPE_CODES.update(_codes())
+        import torch
+        _DTYPE_CODES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
     code = _DTYPE_CODES.get(t.dtype)
     if code is None:
         raise PicturaError(EINVAL, f"{name}: dtype {t.dtype}, expected float32, bfloat16 or float16")
     return code
 
 
-def _matrix(t, name: str, rows=None, cols=None) -> int:
-    """Address of a [rows, cols] tensor whose rows are contiguous and do not overlap."""
-    if t.dim() != 2 or (rows is not None and tuple(t.shape) != (rows, cols)):
-        raise PicturaError(EINVAL, f"{name}: shape {tuple(t.shape)}, expected " +
-                           ("[rows, actions]" if rows is None else f"[{rows}, {cols}]"))
-    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        raise PicturaError(EINVAL, f"{name}: strides {t.stride()}: a row has to be contiguous, and apart from the next")
-    if t.is_neg() or t.is_conj():
-        raise PicturaError(EINVAL, f"{name}: a lazily negated or conjugated tensor")
-    return t.data_ptr()
+def _call(device, fn, *args) -> int:
+    """fn(*args, stream) on the device's current stream, with the device current."""
+    import torch
+    i = device.index
+    if i == torch._C._cuda_getDevice():
+        return fn(*args, torch._C._cuda_getCurrentRawStream(i))
+    with torch.cuda.device(device):
+        return fn(*args, torch.cuda.current_stream().cuda_stream)
 
 
-def _tensor(t, name: str):
+def _tensor(t, name: str, device=None):
+    """t, a torch tensor on the HIP device (`device`, where given)."""
     import torch
     if not isinstance(t, torch.Tensor):
         raise PicturaError(EINVAL, f"{name}: expected a torch tensor on the HIP device, got {type(t).__name__}")
-    _check_device(t, name, None)
+    if not t.is_cuda:
+        _check_device(t, name, None)
+    if device is not None and t.device != device:
+        raise PicturaError(EINVAL, f"{name}: tensor on {t.device}, the logits are on {device}")
     return t
 
 
-def _one_device(ref, **others) -> None:
-    for name, t in others.items():
-        if t is not None and t.device != ref.device:
-            raise PicturaError(EINVAL, f"{name}: tensor on {t.device}, the logits are on {ref.device}")
+def _matrix(t, name: str, rows=None, cols=None):
+    """(address, rows, columns, elements between rows) of a [rows, cols] tensor whose
+    rows are contiguous and do not overlap."""
+    shape = t.shape
+    if len(shape) != 2 or (rows is not None and shape != (rows, cols)):
+        raise PicturaError(EINVAL, f"{name}: shape {tuple(shape)}, expected " +
+                           ("[rows, actions]" if rows is None else f"[{rows}, {cols}]"))
+    rows, cols = shape
+    s0, s1 = t.stride()
+    if (cols > 1 and s1 != 1) or (rows > 1 and s0 < cols):
+        raise PicturaError(EINVAL, f"{name}: strides {t.stride()}: a row has to be contiguous, and apart from the next")
+    if t.is_neg():
+        raise PicturaError(EINVAL, f"{name}: a lazily negated tensor")
+    return t.data_ptr(), rows, cols, s0 if rows > 1 else cols
 
 
-def _vector(t, name: str, kind, count: int) -> int:
+def _vector(t, name: str, kind, count: int, device=None) -> int:
     """Address of a contiguous vector of exactly `count` elements of torch dtype `kind`."""
-    t = _tensor(t, name)
+    t = _tensor(t, name, device)
     if t.dtype != kind:
         raise PicturaError(EINVAL, f"{name}: dtype {t.dtype}, expected {str(kind).replace('torch.', '')}")
-    if tuple(t.shape) != (count,):
+    if t.shape != (count,):
         raise PicturaError(EINVAL, f"{name}: shape {tuple(t.shape)}, expected [{count}]")
     if not t.is_contiguous() or t.is_neg():
         raise PicturaError(EINVAL, f"{name}: tensor is not contiguous")
     return t.data_ptr()
 
 
-def _logits(logits, mask) -> _Logits:
+def _logits(logits, mask):
+    """(packed pictura_logits, rows, actions)"""
     import torch
     t = _tensor(logits, "logits")
-    ptr = _matrix(t, "logits")
-    N, A = t.shape
+    ptr, N, A, stride = _matrix(t, "logits")
     if not 1 <= A <= MAX_ACTIONS or N > 0x7FFFFFFF:
         raise PicturaError(EINVAL, f"logits: shape {tuple(t.shape)}: 1 to {MAX_ACTIONS} actions, fewer than 2^31 rows")
-    l = _Logits(ptr, _dtype_code(t, "logits"), A, N, t.stride(0) if N > 1 else A)
+    mp = ms = 0
     if mask is not None:
-        m = _tensor(mask, "mask")
+        m = _tensor(mask, "mask", t.device)
         if m.dtype not in (torch.bool, torch.uint8):
             raise PicturaError(EINVAL, f"mask: dtype {m.dtype}, expected bool or uint8")
-        if m.dim() == 1 or (m.dim() == 2 and m.shape[0] == 1) or (m.dim() == 2 and m.stride(0) == 0):
+        if m.dim() == 1 or (m.dim() == 2 and (m.shape[0] == 1 or m.stride(0) == 0)):
             row = m if m.dim() == 1 else m[0]   # one row for all
             if row.shape[0] != A or (A > 1 and row.stride(0) != 1) or (m.dim() == 2 and m.shape[0] not in (1, N)):
                 raise PicturaError(EINVAL, f"mask: shape {tuple(m.shape)}, strides {m.stride()}, expected contiguous "
                                    f"rows of {A}")
-            l.mask, l.mask_stride = row.data_ptr(), 0
+            mp = row.data_ptr()
         else:
-            l.mask, l.mask_stride = _matrix(m, "mask", N, A), m.stride(0)
-    return l
+            mp, _, _, ms = _matrix(m, "mask", N, A)
+    return _LOGITS_PACK.pack(ptr, _dtype_code(t, "logits"), A, N, stride, mp, ms), N, A
 
 
 def pictura_sample_actions(logits, uniform, out_action, out_logp, mask=None, temperature=1.0, top_k=0, top_p=1.0,
@@ -559,28 +573,26 @@ def pictura_sample_actions(logits, uniform, out_action, out_logp, mask=None, tem
     min_p each a number or a tensor [rows] (float32; top_k int32).  Writes
     out_action int64 [rows] and out_logp float32 [rows], on the current stream."""
     import torch
-    l = _logits(logits, mask)
-    N = l.rows
-    h = _Sampling(1.0, 0, 1.0, 0.0)
-    for name, v, kind in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
-                          ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+    l, N, _ = _logits(logits, mask)
+    dev = logits.device
+    scalars, rows = [], []
+    for name, v, kind, off in (("temperature", temperature, torch.float32, 1.0), ("top_k", top_k, torch.int32, 0),
+                               ("top_p", top_p, torch.float32, 1.0), ("min_p", min_p, torch.float32, 0.0)):
         if isinstance(v, torch.Tensor):
-            setattr(h, name + "s", _vector(v, name, kind, N))
+            rows.append(_vector(v, name, kind, N, dev))
+            v = off
         elif isinstance(v, bool) or not isinstance(v, int if kind == torch.int32 else (int, float)):
             raise PicturaError(EINVAL, f"{name}: {v!r}, expected a number or a tensor of one per row")
-        elif name == "top_k":
-            h.top_k = min(max(v, 0), MAX_ACTIONS)
-        elif not (0.0 <= v if name == "temperature" else v == v):
-            raise PicturaError(EINVAL, f"{name}: {v!r}")
         else:
-            setattr(h, name, v)
-    iu = _vector(uniform, "uniform", torch.float32, N)
-    oa, ol = _vector(out_action, "out_action", torch.int64, N), _vector(out_logp, "out_logp", torch.float32, N)
-    per_row = {n: v for n, v in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p))
-               if isinstance(v, torch.Tensor)}
-    _one_device(logits, mask=mask, uniform=uniform, out_action=out_action, out_logp=out_logp, **per_row)
-    with torch.cuda.device(logits.device):
-        st = _lib.pictura_sample_actions(ctypes.byref(l), ctypes.byref(h), iu, oa, ol, _stream(None))
+            rows.append(0)
+            if name == "top_k":
+                v = min(max(v, 0), MAX_ACTIONS)
+            elif not (0.0 <= v if name == "temperature" else v == v):
+                raise PicturaError(EINVAL, f"{name}: {v!r}")
+        scalars.append(v)
+    iu = _vector(uniform, "uniform", torch.float32, N, dev)
+    oa, ol = _vector(out_action, "out_action", torch.int64, N, dev), _vector(out_logp, "out_logp", torch.float32, N, dev)
+    st = _call(dev, _lib.pictura_sample_actions, l, _SAMPLING_PACK.pack(*scalars, *rows), iu, oa, ol)
     if st != OK:
         raise PicturaError(st, "sample_actions failed")
 
@@ -594,39 +606,30 @@ def pictura_policy_loss(logits, values, actions, old_logp, advantages, returns, 
     dlogits (the logits' type and shape, rows contiguous) and dvalues float32
     [rows], on the current stream in a workspace of the caching allocator."""
     import torch
-    l = _logits(logits, mask)
-    N, A = l.rows, l.actions
-    f32 = torch.float32
-    v = _tensor(values, "values")
-    if v.dtype != f32 or tuple(v.shape) != (N,) or v.is_neg():
+    l, N, A = _logits(logits, mask)
+    dev, f32 = logits.device, torch.float32
+    v = _tensor(values, "values", dev)
+    if v.dtype != f32 or v.shape != (N,) or v.is_neg():
         raise PicturaError(EINVAL, f"values: {v.dtype} {tuple(v.shape)}, expected float32 [{N}]")
-    b = _PolicyBatch(v.data_ptr(), v.stride(0))
-    b.actions = _vector(actions, "actions", torch.int64, N)
-    b.old_logp = _vector(old_logp, "old_logp", f32, N)
-    b.advantages = _vector(advantages, "advantages", f32, N)
-    b.returns = _vector(returns, "returns", f32, N)
     if value_clip > 0 and old_values is None:
         raise PicturaError(EINVAL, "old_values: needed where value_clip > 0")
-    b.old_values = None if old_values is None else _vector(old_values, "old_values", f32, N)
-    b.weights = None if weights is None else _vector(weights, "weights", f32, N)
-    b.temperature, b.clip, b.value_clip = float(temperature), float(clip), float(value_clip)
-    b.value_coef, b.entropy_coef = float(value_coef), float(entropy_coef)
-    b.denominator, b.normalize = float(denominator), int(bool(normalize))
-    os_ = _vector(out_stats, "out_stats", f32, len(POLICY_STATS))
-    dl = _matrix(_tensor(dlogits, "dlogits"), "dlogits", N, A)
+    batch = _BATCH_PACK.pack(v.data_ptr(), v.stride(0), _vector(actions, "actions", torch.int64, N, dev),
+                        _vector(old_logp, "old_logp", f32, N, dev), _vector(advantages, "advantages", f32, N, dev),
+                        _vector(returns, "returns", f32, N, dev),
+                        0 if old_values is None else _vector(old_values, "old_values", f32, N, dev),
+                        0 if weights is None else _vector(weights, "weights", f32, N, dev),
+                        temperature, clip, value_clip, value_coef, entropy_coef, denominator, bool(normalize))
+    os_ = _vector(out_stats, "out_stats", f32, len(POLICY_STATS), dev)
+    dl, _, _, stride = _matrix(_tensor(dlogits, "dlogits", dev), "dlogits", N, A)
     if dlogits.dtype != logits.dtype:
         raise PicturaError(EINVAL, f"dlogits: dtype {dlogits.dtype}, the logits have {logits.dtype}")
-    dv = _vector(dvalues, "dvalues", f32, N)
-    _one_device(logits, values=values, actions=actions, old_logp=old_logp, advantages=advantages, returns=returns,
-                old_values=old_values, weights=weights, mask=mask, out_stats=out_stats, dlogits=dlogits, dvalues=dvalues)
+    dv = _vector(dvalues, "dvalues", f32, N, dev)
     need = ctypes.c_uint64()
     st = _lib.pictura_policy_loss_workspace(N, A, ctypes.addressof(need))
     if st != OK:
         raise PicturaError(st, "policy_loss_workspace: sizes out of range")
-    with torch.cuda.device(logits.device):
-        ws = torch.empty(int(need.value), dtype=torch.uint8, device=logits.device)
-        st = _lib.pictura_policy_loss(ctypes.byref(l), ctypes.byref(b), ws.data_ptr(), int(need.value), os_, dl,
-                                      dlogits.stride(0) if N > 1 else A, dv, _stream(None))
+    ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+    st = _call(dev, _lib.pictura_policy_loss, l, batch, ws.data_ptr(), need.value, os_, dl, stride, dv)
     if st != OK:
         raise PicturaError(st, "policy_loss: a value out of range")
 
@@ -649,9 +652,8 @@ def pictura_grad_norm(table, max_norm: float, out, device):
     st = _lib.pictura_grad_norm_workspace(at, n, ctypes.addressof(need))
     if st != OK:
         raise PicturaError(st, "grad_norm_workspace: sizes out of range")
-    with torch.cuda.device(device):
-        ws = torch.empty(int(need.value), dtype=torch.uint8, device=device)
-        st = _lib.pictura_grad_norm(at, n, float(max_norm), ws.data_ptr(), int(need.value), oo, _stream(None))
+    ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+    st = _call(device, _lib.pictura_grad_norm, at, n, max_norm, ws.data_ptr(), need.value, oo)
     if st != OK:
         raise PicturaError(st, "grad_norm: a value out of range")
 
@@ -661,10 +663,9 @@ def pictura_adamw_step(table, device, lr, betas, eps, weight_decay, step, bits=3
     current stream.  grad_factor: float32 tensor of one element on the device."""
     import torch
     at = _table(table)
-    gf = None if grad_factor is None else _vector(grad_factor, "grad_factor", torch.float32, 1)
-    h = _AdamW(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), int(step), int(bits), gf)
-    with torch.cuda.device(device):
-        st = _lib.pictura_adamw_step(ctypes.byref(h), at, len(table), _stream(None))
+    gf = 0 if grad_factor is None else _vector(grad_factor, "grad_factor", torch.float32, 1)
+    st = _call(device, _lib.pictura_adamw_step, _ADAMW_PACK.pack(lr, betas[0], betas[1], eps, weight_decay, step, bits, gf), at,
+               len(table))
     if st != OK:
         raise PicturaError(st, "adamw_step: a value out of range")
 
@@ -672,14 +673,11 @@ def pictura_adamw_step(table, device, lr, betas, eps, weight_decay, step, bits=3
 def pictura_adamw_moments(table, exp_avg_out, exp_avg_sq_out, device):
     """What the 8-bit moments of a table stand for: exp_avg_out and exp_avg_sq_out
     are contiguous uint64 arrays of the outputs' device addresses (float32)."""
-    import torch
     at = _table(table)
     for a in (exp_avg_out, exp_avg_sq_out):
         if a.dtype != np.uint64 or a.shape != (len(table),) or not a.flags.c_contiguous:
             raise PicturaError(EINVAL, "moments: expected one uint64 address per tensor")
-    with torch.cuda.device(device):
-        st = _lib.pictura_adamw_moments(at, len(table), exp_avg_out.ctypes.data, exp_avg_sq_out.ctypes.data,
-                                        _stream(None))
+    st = _call(device, _lib.pictura_adamw_moments, at, len(table), exp_avg_out.ctypes.data, exp_avg_sq_out.ctypes.data)
     if st != OK:
         raise PicturaError(st, "adamw_moments: a value out of range")
 

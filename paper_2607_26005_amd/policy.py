@@ -10,12 +10,13 @@ csrc/pictura_adamw.hip) on the current stream and never waits for the device.
 """
 from __future__ import annotations
 
+import operator
 from typing import NamedTuple, Optional
 
 import numpy as np
 import torch
 
-from paper_2607_26005_amd import pictura
+from paper_2607_26005_amd import _tensors, pictura
 from paper_2607_26005_amd.pictura import EINVAL, PicturaError
 
 POLICY_STATS = pictura.POLICY_STATS
@@ -115,7 +116,7 @@ class AdamW(torch.optim.Optimizer):
 
     def _state(self, p):
         s = self.state[p]
-        if not s:
+        if "step" not in s:
             flat = lambda dt, n: torch.zeros(n, dtype=dt, device=p.device)
             n = p.numel()
             s["step"] = 0
@@ -127,43 +128,30 @@ class AdamW(torch.optim.Optimizer):
                 s["exp_avg_scale"], s["exp_avg_sq_scale"] = flat(torch.float32, blocks), flat(torch.float32, blocks)
         return s
 
-    def _check(self, p, g, s, i):
-        """Refuse what the kernels could not use safely."""
-        dev = p.device
-        pictura._check_device(p, f"parameter {i}", None)
-        n = p.numel()
-        if not p.is_contiguous() or p.is_neg():
-            raise PicturaError(EINVAL, f"parameter {i}: tensor is not contiguous")
-        if g is not None and (g.device != dev or g.shape != p.shape or not g.is_contiguous() or g.is_neg()
-                              or g.is_sparse):
-            raise PicturaError(EINVAL, f"gradient {i}: {g.dtype} {tuple(g.shape)} on {g.device}, expected a contiguous "
-                               f"tensor of the parameter's shape {tuple(p.shape)} on {dev}")
-        m, v = s["exp_avg"], s["exp_avg_sq"]
-        kinds = (torch.float32, torch.float32) if self.bits == 32 else (torch.int8, torch.uint8)
-        held = [(m, kinds[0], n), (v, kinds[1], n)]
-        if self.bits == 8:
-            blocks = -(-n // pictura.ADAMW_BLOCK)
-            held += [(s["exp_avg_scale"], torch.float32, blocks), (s["exp_avg_sq_scale"], torch.float32, blocks)]
-        for t, kind, count in held:
-            if t.dtype != kind or t.numel() != count or t.device != dev or not t.is_contiguous():
-                raise PicturaError(EINVAL, f"state of parameter {i}: {t.dtype} of {t.numel()} elements on {t.device}, "
-                                   f"expected {kind} of {count} on {dev}")
+    def _in_order(self, params):
+        """Whether the states are those of these parameters, one by one (a lookup by
+        tensor costs ten times this)."""
+        return len(self.state) == len(params) and all(map(operator.is_, self.state, params))
 
-    def _table(self, entries):
-        """pictura_adamw_tensor of each (parameter, gradient or None, state)."""
-        t = np.zeros(len(entries), pictura.ADAMW_TENSOR)
-        t["param"] = [p.data_ptr() for p, _, _ in entries]
-        t["exp_avg"] = [s["exp_avg"].data_ptr() for _, _, s in entries]
-        t["exp_avg_sq"] = [s["exp_avg_sq"].data_ptr() for _, _, s in entries]
-        if self.bits == 8:
-            t["exp_avg_scale"] = [s["exp_avg_scale"].data_ptr() for _, _, s in entries]
-            t["exp_avg_sq_scale"] = [s["exp_avg_sq_scale"].data_ptr() for _, _, s in entries]
-        t["n"] = [p.numel() for p, _, _ in entries]
-        t["param_dtype"] = [pictura._dtype_code(p, "parameter") for p, _, _ in entries]
-        if entries and entries[0][1] is not None:
-            t["grad"] = [g.data_ptr() for _, g, _ in entries]
-            t["grad_dtype"] = [pictura._dtype_code(g, "gradient") for _, g, _ in entries]
-        return t
+    def _table(self, params, grads):
+        """(rows of pictura_adamw_tensor, their steps) of the parameters that have a
+        gradient (grads: a list, or True for the parameters' own; False: of all that have
+        a state), everything checked that the kernels rely on."""
+        table, steps = np.empty(len(params), pictura.ADAMW_TENSOR), np.empty(len(params), np.int64)
+        if self._in_order(params):
+            states = list(self.state.values())
+        elif grads is False:
+            states = [self.state[p] for p in params]
+        else:
+            states = [self._state(p) if (p.grad if grads is True else g) is not None else None
+                      for p, g in zip(params, params if grads is True else grads)]
+        if params:
+            pictura._check_device(params[0], "parameter 0", None)
+        try:
+            n = _tensors.fill(params, grads, states, self.bits, table, steps)
+        except ValueError as e:
+            raise PicturaError(EINVAL, str(e)) from None
+        return table[:n], steps[:n], states
 
     @torch.no_grad()
     def step(self, closure=None, grads=None):
@@ -171,40 +159,35 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
-        todo, i, dev = [], 0, None
-        for group in self.param_groups:
-            for p in group["params"]:
-                g = p.grad if grads is None else grads[i]
-                if g is not None:
-                    s = self._state(p)
-                    self._check(p, g, s, i)
-                    if dev is not None and p.device != dev:
-                        raise PicturaError(EINVAL, f"parameter {i}: on {p.device}, others on {dev}")
-                    dev = p.device
-                    todo.append((p, g, s, group))
-                i += 1
-        if grads is not None and len(grads) != i:
-            raise PicturaError(EINVAL, f"grads: {len(grads)} of them for {i} parameters")
-        if not todo:
+        params = [p for group in self.param_groups for p in group["params"]]
+        if grads is not None and len(grads) != len(params):
+            raise PicturaError(EINVAL, f"grads: {len(grads)} of them for {len(params)} parameters")
+        table, steps, states = self._table(params, True if grads is None else list(grads))
+        if not len(table):
             return loss
-        table = self._table([e[:3] for e in todo])
+        dev = params[0].device
         factor = None
         if self.max_norm is not None:
             norm = torch.empty(2, dtype=torch.float32, device=dev)
             pictura.pictura_grad_norm(table, self.max_norm, norm, dev)
             self.grad_norm, factor = norm[0], norm[1:]
-        # one call for the tensors of a group at the same step
-        at = 0
-        while at < len(todo):
-            group, step = todo[at][3], int(todo[at][2]["step"]) + 1
-            end = at
-            while end < len(todo) and todo[end][3] is group and int(todo[end][2]["step"]) + 1 == step:
-                end += 1
-            pictura.pictura_adamw_step(table[at:end], dev, group["lr"], group["betas"], group["eps"],
-                                       group["weight_decay"], step, self.bits, factor)
-            at = end
-        for _, _, s, _ in todo:
-            s["step"] = int(s["step"]) + 1
+        # one call for neighbours of a group at the same step
+        got = range(len(params)) if len(table) == len(params) else \
+            [i for i, p in enumerate(params) if (p.grad if grads is None else grads[i]) is not None]
+        ends, at = [], 0
+        for group in self.param_groups:
+            at += len(group["params"])
+            ends.append(sum(1 for i in got if i < at) if len(table) != len(params) else at)
+        begin = 0
+        for group, end in zip(self.param_groups, ends):
+            while begin < end:
+                same = steps[begin:end] != steps[begin]
+                stop = begin + int(same.argmax()) if same.any() else end
+                pictura.pictura_adamw_step(table[begin:stop], dev, group["lr"], group["betas"], group["eps"],
+                                           group["weight_decay"], int(steps[begin]) + 1, self.bits, factor)
+                begin = stop
+        for i in got:
+            states[i]["step"] += 1
         return loss
 
     @torch.no_grad()
@@ -212,24 +195,20 @@ class AdamW(torch.optim.Optimizer):
         """(first moments, second moments) of all parameters that have a state, two
         lists of float32 tensors; with bits=8 what the codes stand for, written to
         the two lists of contiguous float32 tensors `out` where that is given."""
-        entries = [(p, None, self.state[p]) for group in self.param_groups for p in group["params"] if self.state.get(p)]
+        params = [p for group in self.param_groups for p in group["params"]]
+        if not self._in_order(params) or not all(self.state.values()):
+            params = [p for p in params if self.state.get(p)]
         if self.bits == 32:
-            return [s["exp_avg"] for _, _, s in entries], [s["exp_avg_sq"] for _, _, s in entries]
-        for i, (p, _, s) in enumerate(entries):
-            self._check(p, None, s, i)
+            return [self.state[p]["exp_avg"] for p in params], [self.state[p]["exp_avg_sq"] for p in params]
+        table, _, _ = self._table(params, False)
         if out is None:
-            out = tuple([torch.empty(p.numel(), dtype=torch.float32, device=p.device) for p, _, _ in entries]
-                        for _ in range(2))
-        addresses = []
-        for ts in out:
-            if len(ts) != len(entries):
-                raise PicturaError(EINVAL, f"out: {len(ts)} tensors for {len(entries)} parameters")
-            for i, (t, (p, _, _)) in enumerate(zip(ts, entries)):
-                if t.dtype != torch.float32 or t.numel() != p.numel() or not t.is_contiguous() or t.device != p.device:
-                    raise PicturaError(EINVAL, f"out {i}: {t.dtype} of {t.numel()} elements, expected float32 of {p.numel()}")
-            addresses.append(np.array([t.data_ptr() for t in ts], np.uint64))
-        if entries:
-            pictura.pictura_adamw_moments(self._table(entries), *addresses, entries[0][0].device)
+            out = tuple([torch.empty(p.numel(), dtype=torch.float32, device=p.device) for p in params] for _ in range(2))
+        try:
+            addresses = [_tensors.outputs(list(ts), params) for ts in out]
+        except ValueError as e:
+            raise PicturaError(EINVAL, str(e)) from None
+        if params:
+            pictura.pictura_adamw_moments(table, *(np.frombuffer(a, np.uint64) for a in addresses), params[0].device)
         return list(out[0]), list(out[1])
 
     def load_state_dict(self, state_dict):
