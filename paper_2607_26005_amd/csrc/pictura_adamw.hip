@@ -1,8 +1,8 @@
 // AdamW over many tensors at once, with moments in fp32 or in 8 bits, and the
 // norm of all gradients together.
 //
-// The tensors' pointers travel in the kernel's arguments, kTensors to a launch,
-// so a step copies nothing to the device and can be captured in a graph.  A
+// The tensors' pointers travel in the kernel's arguments, up to 80 tensors to a
+// launch, so a step copies nothing to the device and can be captured in a graph.  A
 // workgroup takes kChunk elements of one tensor.
 #include <cmath>
 
@@ -13,28 +13,37 @@
 
 namespace pictura {
 
-constexpr int kTensors = 56;                     // of one launch: 56 * 64 B and the factors stay below 4 KB
 constexpr int kThreads = 256;
 constexpr int kChunk = 4096;                     // elements of one workgroup
 constexpr int kBlk = PICTURA_ADAMW_BLOCK;
 constexpr float kTiny = 0x1p-90f;                // below it a block's moments count as zero: 1 / scale stays finite
 static_assert(kChunk % kBlk == 0, "blocks do not straddle workgroups");
 
-struct alignas(8) TensorArg {
-    void* param;
+// A tensor, or a part of one, of a launch.  Fewer fields, more tensors to a launch:
+// the arguments of a kernel take 4 KB.
+struct GradArg {
     const void* grad;
-    void* m;
-    void* v;
-    float* ms;
-    float* vs;
     int64_t n;
     int32_t first;      // workgroup of its first chunk
     uint8_t pt, gt;     // PICTURA_F32 ..
     uint8_t vec;        // 1: four elements at a time are aligned in every array
 };
 
-struct TensorArgs {
-    TensorArg t[kTensors];
+struct StepArg : GradArg {
+    void* param;
+    void* m;
+    void* v;
+};
+
+struct Step8Arg : StepArg {
+    float* ms;
+    float* vs;
+};
+
+template <class Arg>
+struct Args {
+    static constexpr int kMost = 3840 / (int)sizeof(Arg);
+    Arg t[kMost];
     int32_t count;
 };
 
@@ -44,7 +53,8 @@ struct StepFactors {
 };
 
 // Tensor of workgroup b: the last whose first workgroup is not beyond b.
-__device__ __forceinline__ int tensor_of(const TensorArgs& a, int b)
+template <class A>
+__device__ __forceinline__ int tensor_of(const A& a, int b)
 {
     int lo = 0, hi = a.count - 1;
     while (lo < hi) {
@@ -154,9 +164,9 @@ __device__ __forceinline__ uint32_t v_code(float v, float inv)
     return (uint32_t)q;
 }
 
-__global__ __launch_bounds__(kThreads) void adamw32_kernel(const TensorArgs a, const StepFactors f)
+__global__ __launch_bounds__(kThreads) void adamw32_kernel(const Args<StepArg> a, const StepFactors f)
 {
-    const TensorArg& t = a.t[tensor_of(a, (int)blockIdx.x)];
+    const auto& t = a.t[tensor_of(a, (int)blockIdx.x)];
     const float gf = f.grad_factor ? *f.grad_factor : 1.0f;
     const int64_t at = (int64_t)((int)blockIdx.x - t.first) * kChunk;
     const int n = (int)min((int64_t)kChunk, t.n - at);
@@ -217,9 +227,9 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x)
 }
 
 // A wave takes a block of 256 elements, four neighbours to a lane.
-__global__ __launch_bounds__(kThreads) void adamw8_kernel(const TensorArgs a, const StepFactors f)
+__global__ __launch_bounds__(kThreads) void adamw8_kernel(const Args<Step8Arg> a, const StepFactors f)
 {
-    const TensorArg& t = a.t[tensor_of(a, (int)blockIdx.x)];
+    const auto& t = a.t[tensor_of(a, (int)blockIdx.x)];
     const float gf = f.grad_factor ? *f.grad_factor : 1.0f;
     const int64_t at = (int64_t)((int)blockIdx.x - t.first) * kChunk;
     const int lane = threadIdx.x & 63;
@@ -294,9 +304,9 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const TensorArgs a, co
 }
 
 // What 8-bit moments stand for: param and grad hold the fp32 outputs.
-__global__ __launch_bounds__(kThreads) void moments_kernel(const TensorArgs a)
+__global__ __launch_bounds__(kThreads) void moments_kernel(const Args<Step8Arg> a)
 {
-    const TensorArg& t = a.t[tensor_of(a, (int)blockIdx.x)];
+    const auto& t = a.t[tensor_of(a, (int)blockIdx.x)];
     const int64_t at = (int64_t)((int)blockIdx.x - t.first) * kChunk;
     const int n = (int)min((int64_t)kChunk, t.n - at);
     const int8_t* cm = (const int8_t*)t.m + at;
@@ -325,21 +335,22 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(const TensorArgs a)
     }
 }
 
-// Sum of a workgroup's values, in a fixed order.
+// Sum of the values of a workgroup of NW waves, in a fixed order.
+template <int NW>
 __device__ __forceinline__ double block_sum(double x, double* lds)
 {
     for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
     x = 0.0;
-    for (int w = 0; w < kThreads / 64; ++w) x += lds[w];
+    for (int w = 0; w < NW; ++w) x += lds[w];
     return x;
 }
 
-__global__ __launch_bounds__(kThreads) void norm_part_kernel(const TensorArgs a, int64_t chunk, double* __restrict__ part)
+__global__ __launch_bounds__(kThreads) void norm_part_kernel(const Args<GradArg> a, int64_t chunk, double* __restrict__ part)
 {
     __shared__ double lds[kThreads / 64];
-    const TensorArg& t = a.t[tensor_of(a, (int)blockIdx.x)];
+    const auto& t = a.t[tensor_of(a, (int)blockIdx.x)];
     const int64_t at = (int64_t)((int)blockIdx.x - t.first) * chunk;
     const int64_t n = min(chunk, t.n - at), n4 = t.vec ? n & ~(int64_t)3 : 0;
     double s = 0.0;
@@ -357,17 +368,19 @@ __global__ __launch_bounds__(kThreads) void norm_part_kernel(const TensorArgs a,
         const double g = (double)load_as(t.grad, t.gt, at + i);
         s = fma(g, g, s);
     }
-    s = block_sum(s, lds);
+    s = block_sum<kThreads / 64>(s, lds);
     if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-__global__ __launch_bounds__(kThreads) void norm_kernel(const double* __restrict__ part, int64_t n, float max_norm,
-                                                        float* __restrict__ out)
+constexpr int kNormThreads = 1024;
+
+__global__ __launch_bounds__(kNormThreads) void norm_kernel(const double* __restrict__ part, int64_t n, float max_norm,
+                                                            float* __restrict__ out)
 {
-    __shared__ double lds[kThreads / 64];
+    __shared__ double lds[kNormThreads / 64];
     double s = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += kThreads) s += part[i];
-    s = block_sum(s, lds);
+    for (int64_t i = threadIdx.x; i < n; i += kNormThreads) s += part[i];
+    s = block_sum<kNormThreads / 64>(s, lds);
     if (threadIdx.x == 0) {
         const float norm = (float)sqrt(s);
         const float c = max_norm / (norm + 1e-6f);
@@ -386,14 +399,14 @@ bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) 
 
 bool dtype_ok(int32_t t) { return t == PICTURA_F32 || t == PICTURA_BF16 || t == PICTURA_F16; }
 
-// Split the tensors over launches of at most kTensors tensors and 2^22
+// Split the tensors over launches of as many tensors as their arguments hold and 2^22
 // workgroups of `chunk` elements; a tensor beyond that is taken in parts.
 // launch(args, blocks).
-template <class Fill, class Launch>
+template <class Arg, class Fill, class Launch>
 void for_launches(const pictura_adamw_tensor* ts, int32_t count, int64_t chunk, Fill fill, Launch launch)
 {
     constexpr int64_t kMostBlocks = 1 << 22;
-    TensorArgs a;
+    Args<Arg> a;
     a.count = 0;
     int64_t blocks = 0;
     auto flush = [&] {
@@ -406,40 +419,45 @@ void for_launches(const pictura_adamw_tensor* ts, int32_t count, int64_t chunk, 
         while (at < ts[k].n) {
             const int64_t left = chunks_of(ts[k].n - at, chunk), room = kMostBlocks - blocks;
             const int64_t take = left < room ? left : room;
-            TensorArg& t = a.t[a.count];
+            Arg& t = a.t[a.count];
             t.n = ts[k].n - at < take * chunk ? ts[k].n - at : take * chunk;
             t.first = (int32_t)blocks;
             fill(t, k, at);
             ++a.count;
             blocks += take;
             at += take * chunk;
-            if (a.count == kTensors || blocks == kMostBlocks) flush();
+            if (a.count == Args<Arg>::kMost || blocks == kMostBlocks) flush();
         }
     }
     flush();
 }
 
-void fill_common(TensorArg& t, const pictura_adamw_tensor& s, int64_t at, int bits)
+void fill_step(StepArg& t, const pictura_adamw_tensor& s, int64_t at, int bits)
 {
     t.param = (char*)s.param + at * size_of(s.param_dtype);
     t.grad = (const char*)s.grad + at * size_of(s.grad_dtype);
     const size_t b = bits == 8 ? 1 : 4;
     t.m = (char*)s.exp_avg + at * b;
     t.v = (char*)s.exp_avg_sq + at * b;
-    t.ms = bits == 8 ? s.exp_avg_scale + at / kBlk : nullptr;
-    t.vs = bits == 8 ? s.exp_avg_sq_scale + at / kBlk : nullptr;
     t.pt = (uint8_t)s.param_dtype;
     t.gt = (uint8_t)s.grad_dtype;
     t.vec = aligned(t.param, 4 * size_of(s.param_dtype)) && aligned(t.grad, 4 * size_of(s.grad_dtype)) &&
             aligned(t.m, 4 * b) && aligned(t.v, 4 * b);
 }
 
-// Elements of a workgroup of the norm: some 1,024 workgroups, whose sums one more adds up.
+void fill_scales(Step8Arg& t, const pictura_adamw_tensor& s, int64_t at)
+{
+    t.ms = s.exp_avg_scale + at / kBlk;
+    t.vs = s.exp_avg_sq_scale + at / kBlk;
+}
+
+// Elements of a workgroup of the norm: at most some 8,192 workgroups, whose sums one
+// more adds up.
 int64_t norm_chunk(const pictura_adamw_tensor* ts, int32_t count)
 {
     int64_t n = 0;
     for (int32_t k = 0; k < count; ++k) n += ts[k].n;
-    const int64_t c = chunks_of(n, 1024);
+    const int64_t c = chunks_of(n, 8192);
     return c < kChunk ? kChunk : chunks_of(c, kChunk) * kChunk;
 }
 
@@ -497,18 +515,18 @@ pictura_status pictura_grad_norm(const pictura_adamw_tensor* tensors, int32_t co
     double* part = (double*)workspace;
     int64_t n = 0;
     const int64_t chunk = norm_chunk(tensors, count);
-    for_launches(
+    for_launches<GradArg>(
         tensors, count, chunk,
-        [&](TensorArg& t, int32_t k, int64_t at) {
+        [&](GradArg& t, int32_t k, int64_t at) {
             t.grad = (const char*)tensors[k].grad + at * size_of(tensors[k].grad_dtype);
             t.gt = (uint8_t)tensors[k].grad_dtype;
             t.vec = aligned(t.grad, 4 * size_of(tensors[k].grad_dtype));
         },
-        [&](const TensorArgs& a, unsigned blocks) {
+        [&](const Args<GradArg>& a, unsigned blocks) {
             hipLaunchKernelGGL(norm_part_kernel, dim3(blocks), dim3(kThreads), 0, s, a, chunk, part + n);
             n += blocks;
         });
-    hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, s, part, n, max_norm, out);
+    hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kNormThreads), 0, s, part, n, max_norm, out);
     return launched();
 }
 
@@ -530,12 +548,22 @@ pictura_status pictura_adamw_step(const pictura_adamw* how, const pictura_adamw_
     const StepFactors f{(float)how->beta1, (float)(1.0 - how->beta1), (float)how->beta2, (float)(1.0 - how->beta2),
                         (float)(1.0 / std::sqrt(bc2)), (float)how->eps, (float)(1.0 - how->lr * how->weight_decay),
                         (float)(how->lr / bc1), how->grad_factor};
-    for_launches(
-        tensors, count, kChunk, [&](TensorArg& t, int32_t k, int64_t at) { fill_common(t, tensors[k], at, how->bits); },
-        [&](const TensorArgs& a, unsigned blocks) {
-            if (how->bits == 32) hipLaunchKernelGGL(adamw32_kernel, dim3(blocks), dim3(kThreads), 0, s, a, f);
-            else hipLaunchKernelGGL(adamw8_kernel, dim3(blocks), dim3(kThreads), 0, s, a, f);
-        });
+    if (how->bits == 32)
+        for_launches<StepArg>(
+            tensors, count, kChunk, [&](StepArg& t, int32_t k, int64_t at) { fill_step(t, tensors[k], at, 32); },
+            [&](const Args<StepArg>& a, unsigned blocks) {
+                hipLaunchKernelGGL(adamw32_kernel, dim3(blocks), dim3(kThreads), 0, s, a, f);
+            });
+    else
+        for_launches<Step8Arg>(
+            tensors, count, kChunk,
+            [&](Step8Arg& t, int32_t k, int64_t at) {
+                fill_step(t, tensors[k], at, 8);
+                fill_scales(t, tensors[k], at);
+            },
+            [&](const Args<Step8Arg>& a, unsigned blocks) {
+                hipLaunchKernelGGL(adamw8_kernel, dim3(blocks), dim3(kThreads), 0, s, a, f);
+            });
     return launched();
 }
 
@@ -551,15 +579,17 @@ pictura_status pictura_adamw_moments(const pictura_adamw_tensor* tensors, int32_
             return PICTURA_EINVAL;
     }
     hipStream_t s = (hipStream_t)stream;
-    for_launches(
+    for_launches<Step8Arg>(
         tensors, count, kChunk,
-        [&](TensorArg& t, int32_t k, int64_t at) {
-            fill_common(t, tensors[k], at, 8);
+        [&](Step8Arg& t, int32_t k, int64_t at) {
             t.param = exp_avg_out[k] + at;
             t.grad = exp_avg_sq_out[k] + at;
+            t.m = (char*)tensors[k].exp_avg + at;
+            t.v = (char*)tensors[k].exp_avg_sq + at;
             t.vec = aligned(t.param, 16) && aligned(t.grad, 16) && aligned(t.m, 4) && aligned(t.v, 4);
+            fill_scales(t, tensors[k], at);
         },
-        [&](const TensorArgs& a, unsigned blocks) {
+        [&](const Args<Step8Arg>& a, unsigned blocks) {
             hipLaunchKernelGGL(moments_kernel, dim3(blocks), dim3(kThreads), 0, s, a);
         });
     return launched();

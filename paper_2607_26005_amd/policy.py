@@ -15,6 +15,7 @@ from typing import NamedTuple, Optional
 
 import numpy as np
 import torch
+from torch.optim import optimizer as _optimizer
 
 from paper_2607_26005_amd import _tensors, pictura
 from paper_2607_26005_amd.pictura import EINVAL, PicturaError
@@ -153,8 +154,15 @@ class AdamW(torch.optim.Optimizer):
             raise PicturaError(EINVAL, str(e)) from None
         return table[:n], steps[:n], states
 
-    @torch.no_grad()
     def step(self, closure=None, grads=None):
+        if (self._optimizer_step_pre_hooks or self._optimizer_step_post_hooks or _optimizer._global_optimizer_pre_hooks
+                or _optimizer._global_optimizer_post_hooks or torch.autograd._profiler_enabled()):
+            return self._hooked_step(closure, grads=grads)
+        return self._step(closure, grads)
+
+    step.hooked = True   # by _hooked_step: torch's wrapper takes 10 us also where there is nothing to call
+
+    def _step(self, closure=None, grads=None):
         loss = None
         if closure is not None:
             with torch.enable_grad():
@@ -189,6 +197,8 @@ class AdamW(torch.optim.Optimizer):
         for i in got:
             states[i]["step"] += 1
         return loss
+
+    _hooked_step = torch.optim.Optimizer.profile_hook_step(_step)
 
     @torch.no_grad()
     def moments(self, out=None):

@@ -240,3 +240,27 @@ def test_step_in_a_graph(mods):
         torch.cuda.synchronize()
         for p, q in zip(ps, qs):
             assert torch.equal(p, q), k
+
+
+def test_hooks_and_schedulers(mods):
+    # hooks around a step run, and a scheduler's rate is the one that is used
+    torch, policy = mods
+    p = torch.nn.Parameter(torch.ones(10).cuda())
+    opt = policy.AdamW([p], lr=1e-2, weight_decay=0.0)
+    sched = torch.optim.lr_scheduler.CosineAnnealingLR(opt, T_max=4)
+    seen = []
+    pre = opt.register_step_pre_hook(lambda o, a, k: seen.append("pre"))
+    opt.register_step_post_hook(lambda o, a, k: seen.append("post"))
+    rates = []
+    for _ in range(3):
+        p.grad = torch.ones(10).cuda()
+        before = p.detach().clone()
+        opt.step()
+        rates.append((before - p).mean().item())   # a constant gradient moves by the rate
+        sched.step()
+    assert seen == ["pre", "post"] * 3
+    want = [1e-2 * (1 + np.cos(np.pi * k / 4)) / 2 for k in range(3)]
+    assert np.allclose(rates, want, rtol=1e-4)
+    pre.remove()
+    opt.zero_grad()
+    assert p.grad is None
