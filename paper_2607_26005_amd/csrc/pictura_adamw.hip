@@ -66,10 +66,10 @@ __device__ __forceinline__ int tensor_of(const A& a, int b)
 }
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// Elements of any of the types, in fp32; four from i on, or, without `vec`, those of
-// them below n.
+// Elements of any of the types, one at a time.
 __device__ __forceinline__ float load_as(const void* p, int type, int64_t i)
 {
     if (type == PICTURA_F32) return ((const float*)p)[i];
@@ -89,21 +89,27 @@ struct Four {
     T v[4];
 };
 
-__device__ __forceinline__ void load4(const void* p, int type, int64_t i, float* x)
+// Four elements from i on: loaded as they are (so that several loads are under way
+// before the first is waited for), and made fp32.
+__device__ __forceinline__ u32x4 load4(const void* p, int type, int64_t i)
 {
-    if (type == PICTURA_F32) {
-        const f32x4 t = *(const f32x4*)((const float*)p + i);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = t[k];
-        return;
-    }
+    if (type == PICTURA_F32) return *(const u32x4*)((const float*)p + i);
     const u32x2 t = *(const u32x2*)((const uint16_t*)p + i);
-    if (type == PICTURA_BF16) {
-        const Four<__bf16> h = __builtin_bit_cast(Four<__bf16>, t);
+    return u32x4{t[0], t[1], 0u, 0u};
+}
+
+__device__ __forceinline__ void as_float(u32x4 t, int type, float* x)
+{
+    const u32x2 low = {t[0], t[1]};
+    if (type == PICTURA_F32) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = __uint_as_float(t[k]);
+    } else if (type == PICTURA_BF16) {
+        const Four<__bf16> h = __builtin_bit_cast(Four<__bf16>, low);
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[k] = (float)h.v[k];
     } else {
-        const Four<_Float16> h = __builtin_bit_cast(Four<_Float16>, t);
+        const Four<_Float16> h = __builtin_bit_cast(Four<_Float16>, low);
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[k] = (float)h.v[k];
     }
@@ -122,11 +128,18 @@ __device__ __forceinline__ void store4(void* p, int type, int64_t i, const float
     }
 }
 
-// m and v after the gradient g, and the parameter.
+// m and v after the gradient g, and the parameter.  kFast: with the hardware's root
+// and reciprocal (a unit off each, where the correctly rounded ones take some 25
+// instructions): the 8-bit step is bound by instructions, the 32-bit one by memory.
+template <bool kFast>
 __device__ __forceinline__ float adamw(const StepFactors& f, float p, float g, float& m, float& v)
 {
     m = f.b1 * m + f.c1 * g;
     v = f.b2 * v + (f.c2 * g) * g;
+    if constexpr (kFast) {
+        const float den = __builtin_amdgcn_sqrtf(v) * f.rbc2 + f.eps;
+        return p * f.keep - f.rate * (m * __builtin_amdgcn_rcpf(den));
+    }
     const float den = sqrtf(v) * f.rbc2 + f.eps;
     return p * f.keep - f.rate * (m / den);
 }
@@ -149,40 +162,59 @@ __device__ __forceinline__ float v_value(uint32_t c, float unit)
     return x2 * x2 * unit;
 }
 
+// rint(kLevels a^(1/2)), or a^(1/4), of the correctly rounded roots.  The hardware's
+// are a unit off, which with the product moves up to 255 steps by less than 1e-4; only
+// within 2e-4 of a half (one element in 2,500) are the exact ones taken.
+template <int kLevels, bool kFourth>
+__device__ __forceinline__ float steps_of(float a)
+{
+    float y = __builtin_amdgcn_sqrtf(a);
+    if (kFourth) y = __builtin_amdgcn_sqrtf(y);
+    y *= (float)kLevels;
+    float q = rintf(y);
+    if (__builtin_expect(fabsf(y - q) > 0.4998f, 0)) {
+        asm volatile("" : "+v"(a));   // (a branch: computed for all, the exact roots cost what they save)
+        y = sqrtf(a);
+        if (kFourth) y = sqrtf(y);
+        q = rintf(y * (float)kLevels);
+    }
+    return q;
+}
+
 // The codes of m and v, with inv = 1 / scale (0 for a scale of zero or NaN; a
 // NaN comes out as 0: its scale says it).
 __device__ __forceinline__ int m_code(float m, float inv)
 {
-    const float q = fminf(fmaxf(rintf(sqrtf(fabsf(m) * inv) * 127.0f), 0.0f), 127.0f);
+    const float q = fminf(fmaxf(steps_of<127, false>(fabsf(m) * inv), 0.0f), 127.0f);
     return m < 0.0f ? -(int)q : (int)q;
 }
 
 __device__ __forceinline__ uint32_t v_code(float v, float inv)
 {
-    float q = fminf(fmaxf(rintf(sqrtf(sqrtf(v * inv)) * 255.0f), 0.0f), 255.0f);
+    float q = fminf(fmaxf(steps_of<255, true>(v * inv), 0.0f), 255.0f);
     if (v > 0.0f && inv > 0.0f) q = fmaxf(q, 1.0f);
     return (uint32_t)q;
 }
 
 __global__ __launch_bounds__(kThreads) void adamw32_kernel(const Args<StepArg> a, const StepFactors f)
 {
-    const auto& t = a.t[tensor_of(a, (int)blockIdx.x)];
-    const float gf = f.grad_factor ? *f.grad_factor : 1.0f;
+    const StepArg t = a.t[tensor_of(a, (int)blockIdx.x)];
     const int64_t at = (int64_t)((int)blockIdx.x - t.first) * kChunk;
     const int n = (int)min((int64_t)kChunk, t.n - at);
     float* m = (float*)t.m + at;
     float* v = (float*)t.v + at;
     const int n4 = t.vec ? n & ~3 : 0;
+    const float gf = f.grad_factor ? *f.grad_factor : 1.0f;
     constexpr int kAhead = 2;   // groups of four in flight: more take registers and gain nothing
     for (int i0 = threadIdx.x * 4; i0 < n4; i0 += kThreads * 4 * kAhead) {
-        float p[kAhead][4], g[kAhead][4];
+        u32x4 pr[kAhead], gr[kAhead];
         f32x4 mi[kAhead], vi[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int i = i0 + u * kThreads * 4;
             if (i < n4) {
-                load4(t.grad, t.gt, at + i, g[u]);
-                load4(t.param, t.pt, at + i, p[u]);
+                gr[u] = load4(t.grad, t.gt, at + i);
+                pr[u] = load4(t.param, t.pt, at + i);
                 mi[u] = *(const f32x4*)(m + i);
                 vi[u] = *(const f32x4*)(v + i);
             }
@@ -191,22 +223,25 @@ __global__ __launch_bounds__(kThreads) void adamw32_kernel(const Args<StepArg> a
         for (int u = 0; u < kAhead; ++u) {
             const int i = i0 + u * kThreads * 4;
             if (i < n4) {
+                float p[4], g[4];
+                as_float(gr[u], t.gt, g);
+                as_float(pr[u], t.pt, p);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     float mk = mi[u][k], vk = vi[u][k];
-                    p[u][k] = adamw(f, p[u][k], g[u][k] * gf, mk, vk);
+                    p[k] = adamw<false>(f, p[k], g[k] * gf, mk, vk);
                     mi[u][k] = mk;
                     vi[u][k] = vk;
                 }
                 *(f32x4*)(m + i) = mi[u];
                 *(f32x4*)(v + i) = vi[u];
-                store4(t.param, t.pt, at + i, p[u]);
+                store4(t.param, t.pt, at + i, p);
             }
         }
     }
     for (int i = n4 + threadIdx.x; i < n; i += kThreads) {
         float mi = m[i], vi = v[i];
-        const float p = adamw(f, load_as(t.param, t.pt, at + i), load_as(t.grad, t.gt, at + i) * gf, mi, vi);
+        const float p = adamw<false>(f, load_as(t.param, t.pt, at + i), load_as(t.grad, t.gt, at + i) * gf, mi, vi);
         m[i] = mi;
         v[i] = vi;
         store_as(t.param, t.pt, at + i, p);
@@ -229,26 +264,31 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x)
 // A wave takes a block of 256 elements, four neighbours to a lane.
 __global__ __launch_bounds__(kThreads) void adamw8_kernel(const Args<Step8Arg> a, const StepFactors f)
 {
-    const auto& t = a.t[tensor_of(a, (int)blockIdx.x)];
-    const float gf = f.grad_factor ? *f.grad_factor : 1.0f;
+    const Step8Arg t = a.t[tensor_of(a, (int)blockIdx.x)];
     const int64_t at = (int64_t)((int)blockIdx.x - t.first) * kChunk;
-    const int lane = threadIdx.x & 63;
-    for (int b = threadIdx.x >> 6; b < kChunk / kBlk; b += kThreads / 64) {
+    const int lane = threadIdx.x & 63, i = lane * 4;
+    const int blocks = (int)min((int64_t)(kChunk / kBlk), (t.n - at + kBlk - 1) / kBlk);
+    const float gf = f.grad_factor ? *f.grad_factor : 1.0f;
+    for (int b = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); b < blocks; b += kThreads / 64) {
         const int64_t i0 = at + (int64_t)b * kBlk;
-        if (i0 >= t.n) break;
         const int n = (int)min((int64_t)kBlk, t.n - i0);
-        const int i = lane * 4;
         const bool four = t.vec && i + 4 <= n;
         int8_t* cm = (int8_t*)t.m + i0;
         uint8_t* cv = (uint8_t*)t.v + i0;
+        float* ms = t.ms + i0 / kBlk;
+        float* vs = t.vs + i0 / kBlk;
         float p[4] = {}, g[4] = {};
         Four<int8_t> qm = {};
         Four<uint8_t> qv = {};
+        float um, uv;
         if (four) {
-            load4(t.grad, t.gt, i0 + i, g);
-            load4(t.param, t.pt, i0 + i, p);
+            const u32x4 gr = load4(t.grad, t.gt, i0 + i), pr = load4(t.param, t.pt, i0 + i);
             qm = __builtin_bit_cast(Four<int8_t>, *(const uint32_t*)(cm + i));
             qv = __builtin_bit_cast(Four<uint8_t>, *(const uint32_t*)(cv + i));
+            um = *ms;
+            uv = *vs;
+            as_float(gr, t.gt, g);
+            as_float(pr, t.pt, p);
         } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -258,19 +298,20 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const Args<Step8Arg> a
                     qm.v[k] = cm[i + k];
                     qv.v[k] = cv[i + k];
                 }
+            um = *ms;
+            uv = *vs;
         }
-        const float ms = m_unit(t.ms[i0 / kBlk]), vs = v_unit(t.vs[i0 / kBlk]);
+        um = m_unit(um);
+        uv = v_unit(uv);
         float m[4], v[4];
-        // largest magnitudes by their bits: a NaN is larger than any number
+        // Largest magnitudes by their bits: a NaN is larger than any number.  (Past the end all
+        // is zero, and m and v stay so, unless the scale is no number.)
         uint32_t mm = 0, vm = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            m[k] = v[k] = 0.0f;
-            if (i + k < n) {
-                m[k] = m_value(qm.v[k], ms);
-                v[k] = v_value(qv.v[k], vs);
-                p[k] = adamw(f, p[k], g[k] * gf, m[k], v[k]);
-            }
+            m[k] = m_value(qm.v[k], um);
+            v[k] = v_value(qv.v[k], uv);
+            p[k] = adamw<true>(f, p[k], g[k] * gf, m[k], v[k]);
             mm = max(mm, __float_as_uint(fabsf(m[k])));
             vm = max(vm, __float_as_uint(fabsf(v[k])));
         }
@@ -297,8 +338,8 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const Args<Step8Arg> a
                 }
         }
         if (lane == 0) {
-            t.ms[i0 / kBlk] = nms;
-            t.vs[i0 / kBlk] = nvs;
+            *ms = nms;
+            *vs = nvs;
         }
     }
 }
@@ -350,19 +391,22 @@ __device__ __forceinline__ double block_sum(double x, double* lds)
 __global__ __launch_bounds__(kThreads) void norm_part_kernel(const Args<GradArg> a, int64_t chunk, double* __restrict__ part)
 {
     __shared__ double lds[kThreads / 64];
-    const auto& t = a.t[tensor_of(a, (int)blockIdx.x)];
+    const GradArg t = a.t[tensor_of(a, (int)blockIdx.x)];
     const int64_t at = (int64_t)((int)blockIdx.x - t.first) * chunk;
     const int64_t n = min(chunk, t.n - at), n4 = t.vec ? n & ~(int64_t)3 : 0;
     double s = 0.0;
     for (int64_t i0 = threadIdx.x * 4; i0 < n4; i0 += kThreads * 16) {
-        float g[4][4] = {};
+        u32x4 r[4] = {};
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            if (i0 + u * kThreads * 4 < n4) load4(t.grad, t.gt, at + i0 + u * kThreads * 4, g[u]);
+            if (i0 + u * kThreads * 4 < n4) r[u] = load4(t.grad, t.gt, at + i0 + u * kThreads * 4);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < 4; ++u) {
+            float g[4];
+            as_float(r[u], t.gt, g);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s = fma((double)g[u][k], (double)g[u][k], s);
+            for (int k = 0; k < 4; ++k) s = fma((double)g[k], (double)g[k], s);
+        }
     }
     for (int64_t i = n4 + threadIdx.x; i < n; i += kThreads) {
         const double g = (double)load_as(t.grad, t.gt, at + i);
