@@ -393,22 +393,32 @@ __global__ __launch_bounds__(kThreads) void norm_part_kernel(const Args<GradArg>
     __shared__ double lds[kThreads / 64];
     const GradArg t = a.t[tensor_of(a, (int)blockIdx.x)];
     const int64_t at = (int64_t)((int)blockIdx.x - t.first) * chunk;
-    const int64_t n = min(chunk, t.n - at), n4 = t.vec ? n & ~(int64_t)3 : 0;
+    // 16 bytes to a load, four of them under way
+    const int per = t.gt == PICTURA_F32 ? 4 : 8;
+    const int64_t n = min(chunk, t.n - at), nv = t.vec ? n / per : 0;
+    const u32x4* g4 = (const u32x4*)((const char*)t.grad + at * (16 / per));
     double s = 0.0;
-    for (int64_t i0 = threadIdx.x * 4; i0 < n4; i0 += kThreads * 16) {
+    auto add = [&](const float* g) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s = fma((double)g[k], (double)g[k], s);
+    };
+    for (int64_t i0 = threadIdx.x; i0 < nv; i0 += kThreads * 4) {
         u32x4 r[4] = {};
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            if (i0 + u * kThreads * 4 < n4) r[u] = load4(t.grad, t.gt, at + i0 + u * kThreads * 4);
+            if (i0 + u * kThreads < nv) r[u] = g4[i0 + u * kThreads];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             float g[4];
             as_float(r[u], t.gt, g);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) s = fma((double)g[k], (double)g[k], s);
+            add(g);
+            if (per == 8) {
+                as_float(u32x4{r[u][2], r[u][3], 0u, 0u}, t.gt, g);
+                add(g);
+            }
         }
     }
-    for (int64_t i = n4 + threadIdx.x; i < n; i += kThreads) {
+    for (int64_t i = nv * per + threadIdx.x; i < n; i += kThreads) {
         const double g = (double)load_as(t.grad, t.gt, at + i);
         s = fma(g, g, s);
     }
@@ -564,7 +574,7 @@ pictura_status pictura_grad_norm(const pictura_adamw_tensor* tensors, int32_t co
         [&](GradArg& t, int32_t k, int64_t at) {
             t.grad = (const char*)tensors[k].grad + at * size_of(tensors[k].grad_dtype);
             t.gt = (uint8_t)tensors[k].grad_dtype;
-            t.vec = aligned(t.grad, 4 * size_of(tensors[k].grad_dtype));
+            t.vec = aligned(t.grad, 16);
         },
         [&](const Args<GradArg>& a, unsigned blocks) {
             hipLaunchKernelGGL(norm_part_kernel, dim3(blocks), dim3(kThreads), 0, s, a, chunk, part + n);
