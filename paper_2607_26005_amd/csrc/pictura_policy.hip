@@ -1231,7 +1231,77 @@ struct Work {
     uint32_t* done;
 };
 
-// Heads of up to 64 actions: a row in a group of G lanes, one action each.
+// exp d for d <= 0.  d log2 e rounded once is off by up to 2^-24 of itself, which
+// the exponential of a large |d| shows; fp32 gradients take the rest of the product
+// along.
+template <class T>
+__device__ __forceinline__ float exp_of(float d)
+{
+    constexpr float kLog2e = 1.44269502f, kRest = 1.92596299e-8f;   // log2 e = their sum
+    const float h = d * kLog2e;
+    const float e = __builtin_amdgcn_exp2f(h);
+    if constexpr (sizeof(T) == 2) return e;
+    const float l = fmaf(d, kRest, fmaf(d, kLog2e, -h));
+    return fmaf(e, l * 0.693147182f, e);
+}
+
+// Heads of up to 16 actions: a row to a thread.  What a row takes apart from its
+// logits (the terms, two exponentials, a logarithm) is then done once for it, not by
+// every lane of a group.
+template <class T>
+__global__ __launch_bounds__(kThreads) void loss_thread_kernel(const Rows R, const Batch b, const Work k)
+{
+    constexpr int kMax = 16;
+    const Shared3 s = loss_shared(b, k.part, k.parts);
+    const int A = R.actions;
+    const float ce = b.entropy_coef, rt = 1.0f / b.temperature;
+    double acc[kSums] = {};
+    for (int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x; n < R.rows; n += (int64_t)gridDim.x * kThreads) {
+        const Row<T> row(R, n);
+        T* out = (T*)b.dlogits + n * b.dstride;
+        const float w = row_weight(b, n, A);
+        if (w == 0.0f) {
+            for (int i = 0; i < A; ++i) out[i] = (T)0.0f;
+            b.dvalues[n] = 0.0f;
+            continue;
+        }
+        const int a = (int)b.actions[n];
+        float x[kMax], top = -INFINITY, xa = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kMax; ++i) x[i] = i < A ? row(i) : -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kMax; ++i) {
+            top = fmaxf(top, x[i]);
+            xa = i == a ? x[i] : xa;
+        }
+        if (top == -INFINITY) top = 0.0f;   // nothing is allowed
+        float e0 = 0.0f, e1 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kMax; ++i) {
+            const float d = (x[i] - top) * rt;
+            x[i] = d < -1e4f ? -1e4f : d;   // (an exponential of zero; a NaN stays one)
+            const float e = exp_of<float>(x[i]);
+            e0 += e;
+            e1 = fmaf(e, x[i], e1);
+        }
+        const float logs = logf(e0), rs = 1.0f / e0;
+        const float H = e0 > 0.0f ? logs - e1 * rs : e0 == 0.0f ? 0.0f : e0;
+        const RowTerms t = row_terms(b, s, n, e0 == 0.0f ? -INFINITY : (xa - top) * rt - logs, H);
+        const float scale = w * s.inv;
+        const float k1 = e0 == 0.0f ? 0.0f : ce * rs * scale * rt;
+        const float k0 = e0 == 0.0f ? 0.0f : (ce * (H - logs) - t.g) * rs * scale * rt;
+        const float ga = t.g * scale * rt;
+#pragma unroll
+        for (int i = 0; i < kMax; ++i)
+            if (i < A) out[i] = (T)(exp_of<float>(x[i]) * fmaf(x[i], k1, k0) + (i == a ? ga : 0.0f));
+        b.dvalues[n] = t.dv * scale;
+#pragma unroll
+        for (int q = 0; q < kSums; ++q) acc[q] += (double)w * (double)t.sums[q];
+    }
+    loss_finish<kWaves>(b, s, acc, k.sums, k.done);
+}
+
+// Heads of 17 to 64 actions: a row in a group of G lanes, one action each.
 template <class T, int G>
 __global__ __launch_bounds__(kThreads) void loss_small_kernel(const Rows R, const Batch b, const Work k)
 {
@@ -1274,20 +1344,6 @@ __global__ __launch_bounds__(kThreads) void loss_small_kernel(const Rows R, cons
         if (j < A) ((T*)b.dlogits)[n * b.dstride + j] = (T)y;
     }
     loss_finish<kWaves>(b, s, acc, k.sums, k.done);
-}
-
-// exp d for d <= 0.  d log2 e rounded once is off by up to 2^-24 of itself, which
-// the exponential of a large |d| shows; fp32 gradients take the rest of the product
-// along.
-template <class T>
-__device__ __forceinline__ float exp_of(float d)
-{
-    constexpr float kLog2e = 1.44269502f, kRest = 1.92596299e-8f;   // log2 e = their sum
-    const float h = d * kLog2e;
-    const float e = __builtin_amdgcn_exp2f(h);
-    if constexpr (sizeof(T) == 2) return e;
-    const float l = fmaf(d, kRest, fmaf(d, kLog2e, -h));
-    return fmaf(e, l * 0.693147182f, e);
 }
 
 // Rows held in registers, as in sample_row_kernel: the logits are read once and the
@@ -1491,7 +1547,7 @@ constexpr int64_t kLossBlocks = 4096;
 
 int64_t loss_blocks(int64_t rows, int32_t actions)
 {
-    const int64_t per = actions <= 64 ? kThreads / group_lanes(actions) : 1;
+    const int64_t per = actions <= 16 ? kThreads : actions <= 64 ? kThreads / group_lanes(actions) : 1;
     const int64_t most = actions <= 64 ? 1024 : kLossBlocks / row_waves(actions);
     const int64_t b = (rows + per - 1) / per;
     return b < 1 ? 1 : b < most ? b : most;
@@ -1568,8 +1624,7 @@ void launch_loss(const Rows& R, const Batch& b, const Work& k, hipStream_t s)
         else if (slots <= 16 * 64 * 32) row(loss_row_kernel<T, 16, 32>, 16);
         else if (slots <= kMostSlots) row(loss_row_kernel<T, 16, 72>, 16);
         else go(loss_long_kernel<T>);
-    } else if (group_lanes(R.actions) == 8) go(loss_small_kernel<T, 8>);
-    else if (group_lanes(R.actions) == 16) go(loss_small_kernel<T, 16>);
+    } else if (R.actions <= 16) go(loss_thread_kernel<T>);
     else if (group_lanes(R.actions) == 32) go(loss_small_kernel<T, 32>);
     else go(loss_small_kernel<T, 64>);
 }

@@ -1,7 +1,7 @@
-// Fills the optimizer's table of device addresses from lists of tensors, with every
-// check that keeps a kernel inside its buffers.  In Python those checks are some
-// 4 us a tensor (29 tensors of the policy: 115 us a step, ten times the step's
-// kernels); here 0.1 us.
+// Reads torch tensors for the binding: their device addresses, after every check that
+// keeps a kernel inside its buffers.  In Python those checks take 0.5 us a vector and
+// some 4 us an optimizer's tensor (29 tensors of the policy: 115 us a step, ten times
+// the step's kernels); here 0.1 us.
 #include <Python.h>
 
 #include <torch/csrc/autograd/python_variable.h>
@@ -137,6 +137,53 @@ PyObject* fill(PyObject*, PyObject* args)
     return result;
 }
 
+const char* type_name(at::ScalarType k)
+{
+    return k == at::kFloat ? "float32" : k == at::kLong ? "int64" : "int32";
+}
+
+// vectors(like, count, (name, kind, tensor), ...) -> addresses.  Each tensor is a
+// contiguous vector of `count` elements on the device of `like`, kind "f" float32, "l"
+// int64 or "i" int32; None gives 0.
+PyObject* vectors(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (n < 2 || (n - 2) % 3 || !THPVariable_Check(args[0]) || !PyLong_Check(args[1])) {
+        PyErr_SetString(PyExc_TypeError, "vectors(like, count, name, kind, tensor, ...)");
+        return nullptr;
+    }
+    PyObject* result = PyTuple_New((n - 2) / 3);
+    if (!result) return nullptr;
+    try {
+        const at::Device dev = THPVariable_Unpack(args[0]).device();
+        const int64_t count = PyLong_AsLongLong(args[1]);
+        for (Py_ssize_t k = 2; k < n; k += 3) {
+            const char* name = PyUnicode_AsUTF8(args[k]);
+            const char* code = PyUnicode_AsUTF8(args[k + 1]);
+            if (!name || !code) refuse("a name is no text");
+            const at::ScalarType kind = *code == 'f' ? at::kFloat : *code == 'l' ? at::kLong : at::kInt;
+            uint64_t at = 0;
+            if (args[k + 2] != Py_None) {
+                if (!THPVariable_Check(args[k + 2]))
+                    refuse(name, ": expected a torch tensor on the HIP device, got ", Py_TYPE(args[k + 2])->tp_name);
+                const at::Tensor& t = THPVariable_Unpack(args[k + 2]);
+                if (t.device() != dev) refuse(name, ": tensor on ", t.device(), ", the logits are on ", dev);
+                if (t.scalar_type() != kind) refuse(name, ": dtype ", t.scalar_type(), ", expected ", type_name(kind));
+                if (t.dim() != 1 || t.size(0) != count) refuse(name, ": shape ", t.sizes(), ", expected [", count, "]");
+                if (t.layout() != at::kStrided || !t.is_contiguous() || t.is_neg()) refuse(name, ": tensor is not contiguous");
+                at = (uint64_t)(uintptr_t)t.data_ptr();
+            }
+            PyObject* o = PyLong_FromUnsignedLongLong(at);
+            if (!o) refuse("out of memory");
+            PyTuple_SET_ITEM(result, (k - 2) / 3, o);
+        }
+        return result;
+    } catch (const std::exception& e) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, e.what());
+    }
+    Py_DECREF(result);
+    return nullptr;
+}
+
 // outputs(tensors, params) -> bytes: the addresses of contiguous fp32 tensors of the
 // parameters' sizes.
 PyObject* outputs(PyObject*, PyObject* args)
@@ -166,6 +213,7 @@ PyObject* outputs(PyObject*, PyObject* args)
 }
 
 PyMethodDef methods[] = {{"outputs", outputs, METH_VARARGS, "Addresses of fp32 tensors of the parameters' sizes."},
+                         {"vectors", (PyCFunction)(void (*)())vectors, METH_FASTCALL, "Addresses of vectors of one length."},
                          {"fill", fill, METH_VARARGS, "Fill a table of pictura_adamw_tensor from lists of tensors."},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -530,16 +530,14 @@ def _matrix(t, name: str, rows=None, cols=None):
     return t.data_ptr(), rows, cols, s0 if rows > 1 else cols
 
 
-def _vector(t, name: str, kind, count: int, device=None) -> int:
-    """Address of a contiguous vector of exactly `count` elements of torch dtype `kind`."""
-    t = _tensor(t, name, device)
-    if t.dtype != kind:
-        raise PicturaError(EINVAL, f"{name}: dtype {t.dtype}, expected {str(kind).replace('torch.', '')}")
-    if t.shape != (count,):
-        raise PicturaError(EINVAL, f"{name}: shape {tuple(t.shape)}, expected [{count}]")
-    if not t.is_contiguous() or t.is_neg():
-        raise PicturaError(EINVAL, f"{name}: tensor is not contiguous")
-    return t.data_ptr()
+def _vectors(like, count: int, *named) -> tuple:
+    """Addresses of contiguous vectors of `count` elements on the device of `like`, from
+    name, kind ("f" float32, "l" int64, "i" int32), tensor (or None: 0) in turn."""
+    from paper_2607_26005_amd import _tensors
+    try:
+        return _tensors.vectors(like, count, *named)
+    except ValueError as e:
+        raise PicturaError(EINVAL, str(e)) from None
 
 
 def _logits(logits, mask):
@@ -574,25 +572,23 @@ def pictura_sample_actions(logits, uniform, out_action, out_logp, mask=None, tem
     out_action int64 [rows] and out_logp float32 [rows], on the current stream."""
     import torch
     l, N, _ = _logits(logits, mask)
-    dev = logits.device
-    scalars, rows = [], []
-    for name, v, kind, off in (("temperature", temperature, torch.float32, 1.0), ("top_k", top_k, torch.int32, 0),
-                               ("top_p", top_p, torch.float32, 1.0), ("min_p", min_p, torch.float32, 0.0)):
+    scalars, named = [], []
+    for name, v, kind, off in (("temperature", temperature, "f", 1.0), ("top_k", top_k, "i", 0),
+                               ("top_p", top_p, "f", 1.0), ("min_p", min_p, "f", 0.0)):
+        row = None
         if isinstance(v, torch.Tensor):
-            rows.append(_vector(v, name, kind, N, dev))
-            v = off
-        elif isinstance(v, bool) or not isinstance(v, int if kind == torch.int32 else (int, float)):
+            row, v = v, off
+        elif isinstance(v, bool) or not isinstance(v, int if kind == "i" else (int, float)):
             raise PicturaError(EINVAL, f"{name}: {v!r}, expected a number or a tensor of one per row")
-        else:
-            rows.append(0)
-            if name == "top_k":
-                v = min(max(v, 0), MAX_ACTIONS)
-            elif not (0.0 <= v if name == "temperature" else v == v):
-                raise PicturaError(EINVAL, f"{name}: {v!r}")
+        elif kind == "i":
+            v = min(max(v, 0), MAX_ACTIONS)
+        elif not (0.0 <= v if name == "temperature" else v == v):
+            raise PicturaError(EINVAL, f"{name}: {v!r}")
         scalars.append(v)
-    iu = _vector(uniform, "uniform", torch.float32, N, dev)
-    oa, ol = _vector(out_action, "out_action", torch.int64, N, dev), _vector(out_logp, "out_logp", torch.float32, N, dev)
-    st = _call(dev, _lib.pictura_sample_actions, l, _SAMPLING_PACK.pack(*scalars, *rows), iu, oa, ol)
+        named += (name, kind, row)
+    *rows, iu, oa, ol = _vectors(logits, N, *named, "uniform", "f", uniform, "out_action", "l", out_action, "out_logp", "f",
+                                 out_logp)
+    st = _call(logits.device, _lib.pictura_sample_actions, l, _SAMPLING_PACK.pack(*scalars, *rows), iu, oa, ol)
     if st != OK:
         raise PicturaError(st, "sample_actions failed")
 
@@ -607,23 +603,21 @@ def pictura_policy_loss(logits, values, actions, old_logp, advantages, returns, 
     [rows], on the current stream in a workspace of the caching allocator."""
     import torch
     l, N, A = _logits(logits, mask)
-    dev, f32 = logits.device, torch.float32
+    dev = logits.device
     v = _tensor(values, "values", dev)
-    if v.dtype != f32 or v.shape != (N,) or v.is_neg():
+    if v.dtype != torch.float32 or v.shape != (N,) or v.is_neg():
         raise PicturaError(EINVAL, f"values: {v.dtype} {tuple(v.shape)}, expected float32 [{N}]")
     if value_clip > 0 and old_values is None:
         raise PicturaError(EINVAL, "old_values: needed where value_clip > 0")
-    batch = _BATCH_PACK.pack(v.data_ptr(), v.stride(0), _vector(actions, "actions", torch.int64, N, dev),
-                        _vector(old_logp, "old_logp", f32, N, dev), _vector(advantages, "advantages", f32, N, dev),
-                        _vector(returns, "returns", f32, N, dev),
-                        0 if old_values is None else _vector(old_values, "old_values", f32, N, dev),
-                        0 if weights is None else _vector(weights, "weights", f32, N, dev),
-                        temperature, clip, value_clip, value_coef, entropy_coef, denominator, bool(normalize))
-    os_ = _vector(out_stats, "out_stats", f32, len(POLICY_STATS), dev)
+    *rows, dv = _vectors(logits, N, "actions", "l", actions, "old_logp", "f", old_logp, "advantages", "f", advantages,
+                         "returns", "f", returns, "old_values", "f", old_values, "weights", "f", weights, "dvalues", "f",
+                         dvalues)
+    os_, = _vectors(logits, len(POLICY_STATS), "out_stats", "f", out_stats)
+    batch = _BATCH_PACK.pack(v.data_ptr(), v.stride(0), *rows, temperature, clip, value_clip, value_coef, entropy_coef,
+                             denominator, bool(normalize))
     dl, _, _, stride = _matrix(_tensor(dlogits, "dlogits", dev), "dlogits", N, A)
     if dlogits.dtype != logits.dtype:
         raise PicturaError(EINVAL, f"dlogits: dtype {dlogits.dtype}, the logits have {logits.dtype}")
-    dv = _vector(dvalues, "dvalues", f32, N, dev)
     need = ctypes.c_uint64()
     st = _lib.pictura_policy_loss_workspace(N, A, ctypes.addressof(need))
     if st != OK:
@@ -647,7 +641,7 @@ def pictura_grad_norm(table, max_norm: float, out, device):
     allocator."""
     import torch
     at, n = _table(table), len(table)
-    oo = _vector(out, "out", torch.float32, 2)
+    oo, = _vectors(out, 2, "out", "f", out)
     need = ctypes.c_uint64()
     st = _lib.pictura_grad_norm_workspace(at, n, ctypes.addressof(need))
     if st != OK:
@@ -661,9 +655,8 @@ def pictura_grad_norm(table, max_norm: float, out, device):
 def pictura_adamw_step(table, device, lr, betas, eps, weight_decay, step, bits=32, grad_factor=None):
     """One AdamW step of the tensors of a table (see pictura_grad_norm), on the
     current stream.  grad_factor: float32 tensor of one element on the device."""
-    import torch
     at = _table(table)
-    gf = 0 if grad_factor is None else _vector(grad_factor, "grad_factor", torch.float32, 1)
+    gf = 0 if grad_factor is None else _vectors(grad_factor, 1, "grad_factor", "f", grad_factor)[0]
     st = _call(device, _lib.pictura_adamw_step, _ADAMW_PACK.pack(lr, betas[0], betas[1], eps, weight_decay, step, bits, gf), at,
                len(table))
     if st != OK:
