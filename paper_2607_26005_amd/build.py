@@ -17,7 +17,11 @@ SOURCES = ["pictura_binner.hip", "pictura_render.hip", "pictura_encoder.hip", "p
 # and 2.5 % on the tile-shape-specialised instance and colour kernels, than
 # the next best setting, in A/B runs with identical images); the antialiased
 # kernel spills and slows under it, so it keeps the default scheduler.
+# The policy source is compiled once for the entries and once for the kernels of
+# each type of logits, side by side.
 UNITS = [(src, src.replace(".hip", ".o"), []) for src in SOURCES] + [
+    ("pictura_policy.hip", f"pictura_policy_{name}.o", [f"-DPICTURA_POLICY_TYPE={kind}"])
+    for name, kind in (("f32", "float"), ("bf16", "__bf16"), ("f16", "_Float16"))] + [
     ("pictura_render.hip", "pictura_render_plain.o",
      ["-DPICTURA_RENDER_PLAIN", "-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]),
     ("pictura_render.hip", "pictura_render_side.o",

@@ -4,34 +4,18 @@
 #include <type_traits>
 
 #include "pictura.h"
-#include "pictura_internal.h"
+#include "pictura_policy.h"
 
 #pragma clang fp contract(off)
 
 namespace pictura {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
+// This file is compiled once for each type of logits, PICTURA_POLICY_TYPE, for the
+// kernels, and once without for the entries.
+#ifdef PICTURA_POLICY_TYPE
+
 constexpr float kOne = 0x1p31f;           // weight of a row's largest logit
 constexpr int kMaxBlocks = 1 << 20;       // workgroups of a launch, which then take rows in turn
-
-struct Rows {
-    const void* data;
-    int64_t stride;
-    const uint8_t* mask;
-    int64_t mask_stride;
-    int64_t rows;
-    int32_t actions;
-};
-
-struct Sampling {
-    float temperature, top_p, min_p;
-    int32_t top_k;
-    const float* temperatures;
-    const float* top_ps;
-    const float* min_ps;
-    const int32_t* top_ks;
-};
 
 // One row as the kernels read it: fp32, -inf at a place that is not allowed.
 template <class T>
@@ -1063,27 +1047,6 @@ __global__ __launch_bounds__(kThreads) void sample_small_kernel(const Rows R, co
 // policy loss
 // ---------------------------------------------------------------------------
 
-struct Batch {
-    const float* values;
-    int64_t values_stride;
-    const int64_t* actions;
-    const float* old_logp;
-    const float* advantages;
-    const float* returns;
-    const float* old_values;
-    const float* weights;
-    float temperature, clip, value_clip, value_coef, entropy_coef, denominator;
-    int32_t normalize;
-    float* stats;
-    void* dlogits;
-    int64_t dstride;
-    float* dvalues;
-};
-
-constexpr int kMomentBlocks = 64;       // most partial sums of the weights and advantages: a lane each
-constexpr int kMomentRows = 1024;       // rows of a workgroup that sums them, at least
-constexpr int kSums = 5;                // sums over the rows: policy, value, entropy, KL, clipped
-
 // Over the workgroup; the array may be in use before.
 template <class V>
 __device__ __forceinline__ V loss_sum(V x, V* lds)
@@ -1108,7 +1071,7 @@ __device__ __forceinline__ float row_weight(const Batch& b, int64_t n, int32_t A
 
 // Sums of the weights, and of the advantages and their squares by weight; clears the
 // count of finished workgroups that the loss kernel keeps.
-__global__ __launch_bounds__(kThreads) void loss_moments_kernel(const Batch b, int64_t rows, int32_t A,
+static __global__ __launch_bounds__(kThreads) void loss_moments_kernel(const Batch b, int64_t rows, int32_t A,
                                                                 double* __restrict__ part, uint32_t* __restrict__ done)
 {
     __shared__ double lds[kWaves];
@@ -1158,27 +1121,42 @@ __device__ __forceinline__ Shared3 loss_shared(const Batch& b, const double* __r
     return o;
 }
 
+// What a row holds apart from its logits; w is 0 where it does not count.
+struct RowIn {
+    float w, advantage, old_logp, value, ret, old_value;
+    int32_t action;
+};
+
+__device__ __forceinline__ RowIn row_in(const Batch& b, int64_t n, int32_t A)
+{
+    const int64_t a = b.actions[n];
+    const float w = b.weights ? b.weights[n] : 1.0f;
+    const bool inside = a >= 0 && a < A;
+    return RowIn{inside ? w : 0.0f, b.advantages[n], b.old_logp[n], b.values[n * b.values_stride], b.returns[n],
+                 b.value_clip > 0.0f ? b.old_values[n] : 0.0f, inside ? (int32_t)a : 0};
+}
+
 // The terms of one row, given its log-probability and entropy: d loss / d log p[action]
 // and d loss / d v before weights, and what goes into the sums.
 struct RowTerms {
     float g, dv, sums[kSums];
 };
 
-__device__ __forceinline__ RowTerms row_terms(const Batch& b, const Shared3& s, int64_t n, float logp, float entropy)
+__device__ __forceinline__ RowTerms row_terms(const Batch& b, const Shared3& s, const RowIn& in, float logp, float entropy)
 {
     RowTerms o;
-    const float adv = (b.advantages[n] - s.mean) * s.rstd;
-    const float diff = logp - b.old_logp[n];
+    const float adv = (in.advantage - s.mean) * s.rstd;
+    const float diff = logp - in.old_logp;
     const float r = expf(diff);
     const float lo = 1.0f - b.clip, hi = 1.0f + b.clip;
     const float un = r * adv, cl = fminf(fmaxf(r, lo), hi) * adv;
     // (written so that a NaN stays one)
     o.sums[0] = un <= cl ? -un : cl < un ? -cl : un + cl;
     o.g = un <= cl ? -un : cl < un ? 0.0f : un + cl;
-    const float v = b.values[n * b.values_stride], R = b.returns[n];
+    const float v = in.value, R = in.ret;
     float err = v - R, dv = err;
     if (b.value_clip > 0.0f) {
-        const float old = b.old_values[n], move = v - old;
+        const float old = in.old_value, move = v - old;
         const float far = old + fminf(fmaxf(move, -b.value_clip), b.value_clip) - R;
         if (fabsf(move) > b.value_clip && fabsf(far) > fabsf(err)) {
             err = far;
@@ -1193,8 +1171,25 @@ __device__ __forceinline__ RowTerms row_terms(const Batch& b, const Shared3& s, 
     return o;
 }
 
+template <int NW>
+__device__ __forceinline__ void loss_stats(const Batch& b, const Shared3& s, const double* sums, int64_t blocks,
+                                           double (*lds)[NW])
+{
+    double x[kSums] = {};
+    for (int64_t i = threadIdx.x; i < blocks; i += NW * 64)
+#pragma unroll
+        for (int k = 0; k < kSums; ++k) x[k] += sums[i * kSums + k];
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) x[k] = block_sum<NW>(x[k], lds[k]) * (double)s.inv;
+    if (threadIdx.x == 0) {
+        b.stats[0] = (float)(x[0] + (double)b.value_coef * x[1] - (double)b.entropy_coef * x[2]);
+        for (int k = 0; k < kSums; ++k) b.stats[k + 1] = (float)x[k];
+    }
+}
+
 // Leave this workgroup's sums; the last workgroup to do so adds them all up, in the
-// order of the workgroups, and writes the statistics.
+// order of the workgroups, and writes the statistics.  (Where a launch writes much,
+// the fence that this takes in every workgroup costs more than another launch.)
 template <int NW>
 __device__ void loss_finish(const Batch& b, const Shared3& s, const double* acc, double* __restrict__ sums,
                             uint32_t* __restrict__ done)
@@ -1212,36 +1207,19 @@ __device__ void loss_finish(const Batch& b, const Shared3& s, const double* acc,
     __syncthreads();
     if (last != gridDim.x - 1) return;
     __threadfence();
-    double x[kSums] = {};
-    for (unsigned i = threadIdx.x; i < gridDim.x; i += NW * 64)
-#pragma unroll
-        for (int k = 0; k < kSums; ++k) x[k] += sums[(int64_t)i * kSums + k];
-#pragma unroll
-    for (int k = 0; k < kSums; ++k) x[k] = block_sum<NW>(x[k], lds[1][k]) * (double)s.inv;
-    if (threadIdx.x == 0) {
-        b.stats[0] = (float)(x[0] + (double)b.value_coef * x[1] - (double)b.entropy_coef * x[2]);
-        for (int k = 0; k < kSums; ++k) b.stats[k + 1] = (float)x[k];
-    }
+    loss_stats<NW>(b, s, sums, gridDim.x, lds[1]);
 }
-
-struct Work {
-    const double* part;   // sums of loss_moments_kernel
-    int32_t parts;
-    double* sums;
-    uint32_t* done;
-};
 
 // exp d for d <= 0.  d log2 e rounded once is off by up to 2^-24 of itself, which
 // the exponential of a large |d| shows; fp32 gradients take the rest of the product
 // along.
-template <class T>
+constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596299e-8f;   // log2 e is their sum
+
 __device__ __forceinline__ float exp_of(float d)
 {
-    constexpr float kLog2e = 1.44269502f, kRest = 1.92596299e-8f;   // log2 e = their sum
     const float h = d * kLog2e;
     const float e = __builtin_amdgcn_exp2f(h);
-    if constexpr (sizeof(T) == 2) return e;
-    const float l = fmaf(d, kRest, fmaf(d, kLog2e, -h));
+    const float l = fmaf(d, kLog2eRest, fmaf(d, kLog2e, -h));
     return fmaf(e, l * 0.693147182f, e);
 }
 
@@ -1259,13 +1237,14 @@ __global__ __launch_bounds__(kThreads) void loss_thread_kernel(const Rows R, con
     for (int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x; n < R.rows; n += (int64_t)gridDim.x * kThreads) {
         const Row<T> row(R, n);
         T* out = (T*)b.dlogits + n * b.dstride;
-        const float w = row_weight(b, n, A);
+        const RowIn in = row_in(b, n, A);
+        const float w = in.w;
         if (w == 0.0f) {
             for (int i = 0; i < A; ++i) out[i] = (T)0.0f;
             b.dvalues[n] = 0.0f;
             continue;
         }
-        const int a = (int)b.actions[n];
+        const int a = in.action;
         float x[kMax], top = -INFINITY, xa = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kMax; ++i) x[i] = i < A ? row(i) : -INFINITY;
@@ -1280,20 +1259,20 @@ __global__ __launch_bounds__(kThreads) void loss_thread_kernel(const Rows R, con
         for (int i = 0; i < kMax; ++i) {
             const float d = (x[i] - top) * rt;
             x[i] = d < -1e4f ? -1e4f : d;   // (an exponential of zero; a NaN stays one)
-            const float e = exp_of<float>(x[i]);
+            const float e = exp_of(x[i]);
             e0 += e;
             e1 = fmaf(e, x[i], e1);
         }
         const float logs = logf(e0), rs = 1.0f / e0;
         const float H = e0 > 0.0f ? logs - e1 * rs : e0 == 0.0f ? 0.0f : e0;
-        const RowTerms t = row_terms(b, s, n, e0 == 0.0f ? -INFINITY : (xa - top) * rt - logs, H);
+        const RowTerms t = row_terms(b, s, in, e0 == 0.0f ? -INFINITY : (xa - top) * rt - logs, H);
         const float scale = w * s.inv;
         const float k1 = e0 == 0.0f ? 0.0f : ce * rs * scale * rt;
         const float k0 = e0 == 0.0f ? 0.0f : (ce * (H - logs) - t.g) * rs * scale * rt;
         const float ga = t.g * scale * rt;
 #pragma unroll
         for (int i = 0; i < kMax; ++i)
-            if (i < A) out[i] = (T)(exp_of<float>(x[i]) * fmaf(x[i], k1, k0) + (i == a ? ga : 0.0f));
+            if (i < A) out[i] = (T)(exp_of(x[i]) * fmaf(x[i], k1, k0) + (i == a ? ga : 0.0f));
         b.dvalues[n] = t.dv * scale;
 #pragma unroll
         for (int q = 0; q < kSums; ++q) acc[q] += (double)w * (double)t.sums[q];
@@ -1314,11 +1293,12 @@ __global__ __launch_bounds__(kThreads) void loss_small_kernel(const Rows R, cons
         const int64_t n = n0 + threadIdx.x / G;
         const bool live = n < R.rows;
         const int64_t m = live ? n : R.rows - 1;
-        const float w = live ? row_weight(b, m, A) : 0.0f;
+        const RowIn in = row_in(b, m, A);
+        const float w = live ? in.w : 0.0f;
         const bool on = w != 0.0f;
         const Row<T> row(R, m);
         const float x = on && j < A ? row(j) : -INFINITY;
-        const int a = on ? (int)b.actions[m] : 0;
+        const int a = in.action;
         const float top = group_max<G>(x);
         const float d = x == -INFINITY ? -INFINITY : (x - top) / rt, e = expf(d);
         const float e0 = group_sum<G>(e), e1 = group_sum<G>(e != 0.0f ? e * d : 0.0f);
@@ -1328,7 +1308,7 @@ __global__ __launch_bounds__(kThreads) void loss_small_kernel(const Rows R, cons
         if (on) {
             const float logs = logf(e0), rs = 1.0f / e0;
             const float H = e0 > 0.0f ? logs - e1 * rs : e0 == 0.0f ? 0.0f : e0;
-            const RowTerms t = row_terms(b, s, m, e0 == 0.0f ? -INFINITY : da - logs, H);
+            const RowTerms t = row_terms(b, s, in, e0 == 0.0f ? -INFINITY : da - logs, H);
             const float scale = w * s.inv;
             if (e != 0.0f) y = e * rs * (ce * (d - logs + H) - t.g);
             if (j == a) y += t.g;
@@ -1348,7 +1328,8 @@ __global__ __launch_bounds__(kThreads) void loss_small_kernel(const Rows R, cons
 
 // Rows held in registers, as in sample_row_kernel: the logits are read once and the
 // gradient written once.  With e = exp d and S its sum, d loss / d logit of action i is
-// e_i (k1 d_i + k0), plus g at the action taken.
+// e_i (k1 d_i + k0), plus g at the action taken.  For 16-bit logits d is kept in units
+// of log 2, so that its exponential is one instruction.
 template <class T, int NW, int ITEMS>
 __global__ __launch_bounds__(NW * 64) void loss_row_kernel(const Rows R, const Batch b, const Work k)
 {
@@ -1358,15 +1339,21 @@ __global__ __launch_bounds__(NW * 64) void loss_row_kernel(const Rows R, const B
     const Shared3 s = loss_shared(b, k.part, k.parts);
     const int A = R.actions;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const float rt = 1.0f / b.temperature;
+    constexpr bool kHalf = sizeof(T) == 2;
+    constexpr float kUnit = kHalf ? 0.693147182f : 1.0f;
+    const float rt = 1.0f / b.temperature, rd = kHalf ? rt * kLog2e : rt;
+    auto expd = [](float d) { return kHalf ? __builtin_amdgcn_exp2f(d) : exp_of(d); };
     if (threadIdx.x == 0)
         for (int q = 0; q < kSums; ++q) acc[q] = 0.0;
+    RowIn next = (int64_t)blockIdx.x < R.rows ? row_in(b, blockIdx.x, A) : RowIn{};
     for (int64_t n = blockIdx.x; n < R.rows; n += gridDim.x) {
+        const RowIn in = next;   // (the next one's numbers come while this row is worked on)
+        if (n + gridDim.x < R.rows) next = row_in(b, n + gridDim.x, A);
         const VecRow<T, NW, NV> vr(R, n, wave, lane);
         const int per = vr.per;
-        const float w = same_in_wave(row_weight(b, n, A));
+        const float w = same_in_wave(in.w);
         const bool on = w != 0.0f;
-        const int a = on ? (int)same_in_wave((uint32_t)b.actions[n]) : 0;
+        const int a = (int)same_in_wave((uint32_t)in.action);
         uint32_t r[NV][V];
         float k1 = 0.0f, k0 = 0.0f, ga = 0.0f;
         if (on) {
@@ -1384,7 +1371,7 @@ __global__ __launch_bounds__(NW * 64) void loss_row_kernel(const Rows R, const B
             if (top == -INFINITY) top = 0.0f;   // nothing is allowed
             // (an exponential of zero is cut off there; a NaN stays one)
             auto dist = [&](float x) {
-                const float d = (x - top) * rt;
+                const float d = (x - top) * rd;
                 return d < -1e4f ? -1e4f : d;
             };
             float e0 = 0.0f, e1 = 0.0f;
@@ -1394,7 +1381,7 @@ __global__ __launch_bounds__(NW * 64) void loss_row_kernel(const Rows R, const B
                     renew(r[j]);
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        const float d = dist(__uint_as_float(r[j][v])), e = exp_of<T>(d);
+                        const float d = dist(__uint_as_float(r[j][v])), e = expd(d);
                         e0 += e;
                         e1 = fmaf(e, d, e1);
                         r[j][v] = __float_as_uint(d);
@@ -1412,10 +1399,10 @@ __global__ __launch_bounds__(NW * 64) void loss_row_kernel(const Rows R, const B
                 e1 = from_lane(lane_scan<NW>(sums[1][lane & (NW - 1)], 0.0f, Add{}), NW - 1);
             }
             const float logs = logf(e0), rs = 1.0f / e0;
-            const float H = e0 > 0.0f ? logs - e1 * rs : e0 == 0.0f ? 0.0f : e0;
-            const RowTerms t = row_terms(b, s, n, e0 == 0.0f ? -INFINITY : (xa - top) * rt - logs, H);
+            const float H = e0 > 0.0f ? logs - e1 * kUnit * rs : e0 == 0.0f ? 0.0f : e0;
+            const RowTerms t = row_terms(b, s, in, e0 == 0.0f ? -INFINITY : (xa - top) * rt - logs, H);
             const float scale = w * s.inv;
-            k1 = e0 == 0.0f ? 0.0f : b.entropy_coef * rs * scale * rt;
+            k1 = e0 == 0.0f ? 0.0f : b.entropy_coef * kUnit * rs * scale * rt;
             k0 = e0 == 0.0f ? 0.0f : (b.entropy_coef * (H - logs) - t.g) * rs * scale * rt;
             ga = t.g * scale * rt;
             if (threadIdx.x == 0) {
@@ -1435,13 +1422,18 @@ __global__ __launch_bounds__(NW * 64) void loss_row_kernel(const Rows R, const B
                 renew(r[j]);
                 const int i0 = vr.first(j);
                 Vec y;
+                float z[V];
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     const float d = __uint_as_float(r[j][v]);
-                    float z = on ? exp_of<T>(d) * fmaf(d, k1, k0) : 0.0f;
-                    if (on && i0 + v == a) z += ga;
-                    y.v[v] = (T)z;
+                    z[v] = on ? expd(d) * fmaf(d, k1, k0) : 0.0f;
                 }
+                if (on && a >= i0 && a < i0 + V) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) z[v] += i0 + v == a ? ga : 0.0f;
+                }
+#pragma unroll
+                for (int v = 0; v < V; ++v) y.v[v] = (T)z[v];
                 if (even && vr.whole(j)) {
                     *reinterpret_cast<Vec*>(out + i0) = y;
                 } else {
@@ -1452,10 +1444,8 @@ __global__ __launch_bounds__(NW * 64) void loss_row_kernel(const Rows R, const B
             }
         if constexpr (NW > 1) __syncthreads();
     }
-    __syncthreads();
-    double mine[kSums];
-    for (int q = 0; q < kSums; ++q) mine[q] = threadIdx.x == 0 ? acc[q] : 0.0;
-    loss_finish<NW>(b, s, mine, k.sums, k.done);
+    if (threadIdx.x == 0)
+        for (int q = 0; q < kSums; ++q) k.sums[(int64_t)blockIdx.x * kSums + q] = acc[q];
 }
 
 // One workgroup per row, the row read again for every pass.
@@ -1469,13 +1459,14 @@ __global__ __launch_bounds__(kThreads) void loss_long_kernel(const Rows R, const
     for (int64_t n = blockIdx.x; n < R.rows; n += gridDim.x) {
         const Row<T> row(R, n);
         T* out = (T*)b.dlogits + n * b.dstride;
-        const float w = row_weight(b, n, A);
+        const RowIn in = row_in(b, n, A);
+        const float w = in.w;
         if (w == 0.0f) {
             for (int i = threadIdx.x; i < A; i += kThreads) out[i] = (T)0.0f;
             if (threadIdx.x == 0) b.dvalues[n] = 0.0f;
             continue;
         }
-        const int a = (int)b.actions[n];
+        const int a = in.action;
         float top = -INFINITY;
         for (int i = threadIdx.x; i < A; i += kThreads) top = fmaxf(top, row(i));
         const float xa = row(a);
@@ -1493,7 +1484,7 @@ __global__ __launch_bounds__(kThreads) void loss_long_kernel(const Rows R, const
         e1 = loss_sum(e1, ldsf);
         const float logs = logf(e0), rs = 1.0f / e0;
         const float H = e0 > 0.0f ? logs - e1 * rs : e0 == 0.0f ? 0.0f : e0;
-        const RowTerms t = row_terms(b, s, n, e0 == 0.0f ? -INFINITY : dist(xa) - logs, H);
+        const RowTerms t = row_terms(b, s, in, e0 == 0.0f ? -INFINITY : dist(xa) - logs, H);
         const float scale = w * s.inv;
         const float ce = b.entropy_coef;
         for (int i = threadIdx.x; i < A; i += kThreads) {
@@ -1508,54 +1499,65 @@ __global__ __launch_bounds__(kThreads) void loss_long_kernel(const Rows R, const
         }
         __syncthreads();
     }
-    loss_finish<kWaves>(b, s, acc, k.sums, k.done);
+    if (threadIdx.x == 0)
+        for (int q = 0; q < kSums; ++q) k.sums[(int64_t)blockIdx.x * kSums + q] = acc[q];
+}
+
+// The statistics from the sums of `blocks` workgroups, in their order.
+static __global__ __launch_bounds__(kThreads) void loss_stats_kernel(const Batch b, const Work k, int64_t blocks)
+{
+    __shared__ double lds[kSums][kWaves];
+    loss_stats<kWaves>(b, loss_shared(b, k.part, k.parts), k.sums, blocks, lds);
 }
 
 // ---------------------------------------------------------------------------
-// host
+// launches
 // ---------------------------------------------------------------------------
 
 namespace {
 
-size_t size_of(int32_t t) { return t == PICTURA_F32 ? 4 : 2; }
-
-bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-
-bool logits_ok(const pictura_logits* l)
-{
-    if (!l || (l->dtype != PICTURA_F32 && l->dtype != PICTURA_BF16 && l->dtype != PICTURA_F16)) return false;
-    if (l->actions < 1 || l->actions > PICTURA_MAX_ACTIONS || l->rows < 0 || l->rows > 0x7FFFFFFFll) return false;
-    if (l->rows == 0) return true;
-    if (l->stride < l->actions && l->rows > 1) return false;
-    if (l->mask && l->mask_stride != 0 && l->mask_stride < l->actions && l->rows > 1) return false;
-    return l->data && aligned(l->data, size_of(l->dtype));
-}
-
-Rows rows_of(const pictura_logits& l) { return Rows{l.data, l.stride, l.mask, l.mask_stride, l.rows, l.actions}; }
-
 unsigned blocks_for(int64_t rows) { return (unsigned)(rows < kMaxBlocks ? rows : kMaxBlocks); }
 
-// Lanes that hold a row of up to 64 actions.
-int group_lanes(int32_t actions) { return actions <= 8 ? 8 : actions <= 16 ? 16 : actions <= 32 ? 32 : 64; }
+template <int N>
+using Int = std::integral_constant<int, N>;
 
-// Waves of a workgroup that holds a row of so many slots in its registers.
-int row_waves(int slots) { return slots <= 64 * 16 ? 1 : slots <= 4 * 64 * 32 ? 4 : 16; }
+// Waves and items of a workgroup that holds a row of so many slots in its registers.
+// With many rows few waves to a row: the row's reductions take fewer barriers, and
+// more rows are under way on a CU (2,047 rows of 16,381: 58 us with four waves, 77
+// with sixteen).  With fewer rows than CUs the waves are there anyway (one row of
+// 16,385: 15 us with sixteen, 25 with four).
+struct RowShape {
+    int waves, items;
+};
 
-// Workgroups of the loss: each leaves one set of partial sums, so there are no more
-// than fill the card a few times.
-constexpr int64_t kLossBlocks = 4096;
-
-int64_t loss_blocks(int64_t rows, int32_t actions)
+RowShape row_shape(int slots, int64_t rows)
 {
-    const int64_t per = actions <= 16 ? kThreads : actions <= 64 ? kThreads / group_lanes(actions) : 1;
-    const int64_t most = actions <= 64 ? 1024 : kLossBlocks / row_waves(actions);
-    const int64_t b = (rows + per - 1) / per;
-    return b < 1 ? 1 : b < most ? b : most;
+    const bool few = rows < 256;
+    if (slots <= 64 * 16 && !few) return {1, 16};
+    if (slots <= 64 * 32 && !few) return {1, 32};
+    if (slots <= 4 * 64 * 16) return {4, 16};
+    if (slots <= 4 * 64 * 32 && !few) return {4, 32};
+    if (slots <= 4 * 64 * 72 && !few) return {4, 72};
+    if (slots <= 16 * 64 * 16) return {16, 16};
+    if (slots <= 16 * 64 * 32) return {16, 32};
+    return {16, 72};
 }
 
-uint64_t loss_bytes(int64_t rows, int32_t actions)
+// go(waves, items) with both as constants.
+template <class F>
+void with_shape(RowShape s, F go)
 {
-    return sizeof(double) * (uint64_t)(kMomentBlocks * 3 + loss_blocks(rows, actions) * kSums) + 256;
+    auto at = [&](auto w, auto i) {
+        if (s.waves == decltype(w)::value && s.items == decltype(i)::value) go(w, i);
+    };
+    at(Int<1>{}, Int<16>{});
+    at(Int<1>{}, Int<32>{});
+    at(Int<4>{}, Int<16>{});
+    at(Int<4>{}, Int<32>{});
+    at(Int<4>{}, Int<72>{});
+    at(Int<16>{}, Int<16>{});
+    at(Int<16>{}, Int<32>{});
+    at(Int<16>{}, Int<72>{});
 }
 
 // Slots a row takes: rows that do not start at 16-byte addresses begin inside a vector.
@@ -1566,6 +1568,8 @@ int slots_of(const Rows& R)
     const bool even = aligned(R.data, 16) && (R.rows == 1 || R.stride % V == 0);
     return R.actions + (even ? 0 : V - 1);
 }
+
+}  // namespace
 
 template <class T>
 void launch_sample(const Rows& R, const Sampling& S, const float* uniform, int64_t* action, float* logp, hipStream_t s)
@@ -1590,50 +1594,85 @@ void launch_sample(const Rows& R, const Sampling& S, const float* uniform, int64
     }
     const bool filter = S.top_ks || S.top_ps || (S.top_k > 0 && S.top_k < R.actions) || S.top_p < 1.0f;
     const int slots = slots_of<T>(R);
+    if (slots > kMostSlots) {
+        hipLaunchKernelGGL(sample_long_kernel<T>, dim3(blocks_for(R.rows)), dim3(kLongWaves * 64), 0, s, R, S, uniform, action, logp);
+        return;
+    }
     const unsigned gx = blocks_for(R.rows);
-    const dim3 grid(gx, slots <= kMostSlots ? (unsigned)((R.rows + gx - 1) / gx) : 1u);
-    auto go = [&](auto kernel, int waves) {
-        hipLaunchKernelGGL(kernel, grid, dim3(waves * 64), 0, s, R, S, uniform, action, logp);
-    };
-    auto pick = [&](auto f) {
-        constexpr bool F = decltype(f)::value;
-        if (slots <= 64 * 16) go(sample_row_kernel<T, 1, 16, F>, 1);
-        else if (slots <= 4 * 64 * 16) go(sample_row_kernel<T, 4, 16, F>, 4);
-        else if (slots <= 4 * 64 * 32) go(sample_row_kernel<T, 4, 32, F>, 4);
-        else if (slots <= 16 * 64 * 16) go(sample_row_kernel<T, 16, 16, F>, 16);
-        else if (slots <= 16 * 64 * 32) go(sample_row_kernel<T, 16, 32, F>, 16);
-        else if (slots <= kMostSlots) go(sample_row_kernel<T, 16, 72, F>, 16);
-        else go(sample_long_kernel<T>, kLongWaves);
-    };
-    if (filter) pick(std::true_type{});
-    else pick(std::false_type{});
+    const dim3 grid(gx, (unsigned)((R.rows + gx - 1) / gx));
+    with_shape(row_shape(slots, R.rows), [&](auto w, auto i) {
+        constexpr int W = decltype(w)::value, I = decltype(i)::value;
+        if (filter) hipLaunchKernelGGL((sample_row_kernel<T, W, I, true>), grid, dim3(W * 64), 0, s, R, S, uniform, action, logp);
+        else hipLaunchKernelGGL((sample_row_kernel<T, W, I, false>), grid, dim3(W * 64), 0, s, R, S, uniform, action, logp);
+    });
 }
 
 template <class T>
 void launch_loss(const Rows& R, const Batch& b, const Work& k, hipStream_t s)
 {
     const dim3 grid((unsigned)loss_blocks(R.rows, R.actions)), block(kThreads);
+    hipLaunchKernelGGL(loss_moments_kernel, dim3((unsigned)k.parts), block, 0, s, b, R.rows, R.actions, k.part, k.done);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, R, b, k); };
     if (R.actions > 64) {
         const int slots = slots_of<T>(R);
-        auto row = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3(waves * 64), 0, s, R, b, k); };
-        if (slots <= 64 * 16) row(loss_row_kernel<T, 1, 16>, 1);
-        else if (slots <= 4 * 64 * 16) row(loss_row_kernel<T, 4, 16>, 4);
-        else if (slots <= 4 * 64 * 32) row(loss_row_kernel<T, 4, 32>, 4);
-        else if (slots <= 16 * 64 * 16) row(loss_row_kernel<T, 16, 16>, 16);
-        else if (slots <= 16 * 64 * 32) row(loss_row_kernel<T, 16, 32>, 16);
-        else if (slots <= kMostSlots) row(loss_row_kernel<T, 16, 72>, 16);
-        else go(loss_long_kernel<T>);
+        if (slots <= kMostSlots)
+            with_shape(row_shape(slots, R.rows), [&](auto w, auto i) {
+                constexpr int W = decltype(w)::value, I = decltype(i)::value;
+                hipLaunchKernelGGL((loss_row_kernel<T, W, I>), grid, dim3(W * 64), 0, s, R, b, k);
+            });
+        else
+            go(loss_long_kernel<T>);
+        hipLaunchKernelGGL(loss_stats_kernel, dim3(1), block, 0, s, b, k, (int64_t)grid.x);
     } else if (R.actions <= 16) go(loss_thread_kernel<T>);
     else if (group_lanes(R.actions) == 32) go(loss_small_kernel<T, 32>);
     else go(loss_small_kernel<T, 64>);
 }
 
+template void launch_sample<PICTURA_POLICY_TYPE>(const Rows&, const Sampling&, const float*, int64_t*, float*, hipStream_t);
+template void launch_loss<PICTURA_POLICY_TYPE>(const Rows&, const Batch&, const Work&, hipStream_t);
+
+#else   // the entries
+
+// Workgroups of the loss: each leaves one set of partial sums, so there are no more
+// than fill the card a few times.
+constexpr int64_t kLossBlocks = 8192;
+
+int64_t loss_blocks(int64_t rows, int32_t actions)
+{
+    const int64_t per = actions <= 16 ? kThreads : actions <= 64 ? kThreads / group_lanes(actions) : 1;
+    const int64_t most = actions <= 64 ? 1024 : kLossBlocks / (actions <= 64 * 32 ? 1 : 4);
+    const int64_t b = (rows + per - 1) / per;
+    return b < 1 ? 1 : b < most ? b : most;
+}
+
+namespace {
+
+size_t size_of(int32_t t) { return t == PICTURA_F32 ? 4 : 2; }
+
+bool logits_ok(const pictura_logits* l)
+{
+    if (!l || (l->dtype != PICTURA_F32 && l->dtype != PICTURA_BF16 && l->dtype != PICTURA_F16)) return false;
+    if (l->actions < 1 || l->actions > PICTURA_MAX_ACTIONS || l->rows < 0 || l->rows > 0x7FFFFFFFll) return false;
+    if (l->rows == 0) return true;
+    if (l->stride < l->actions && l->rows > 1) return false;
+    if (l->mask && l->mask_stride != 0 && l->mask_stride < l->actions && l->rows > 1) return false;
+    return l->data && aligned(l->data, size_of(l->dtype));
+}
+
+Rows rows_of(const pictura_logits& l) { return Rows{l.data, l.stride, l.mask, l.mask_stride, l.rows, l.actions}; }
+
+uint64_t loss_bytes(int64_t rows, int32_t actions)
+{
+    return sizeof(double) * (uint64_t)(kMomentBlocks * 3 + loss_blocks(rows, actions) * kSums) + 256;
+}
+
 pictura_status launched() { return hipGetLastError() == hipSuccess ? PICTURA_OK : PICTURA_EDEVICE; }
 
 }  // namespace
+#endif
 }  // namespace pictura
 
+#ifndef PICTURA_POLICY_TYPE
 using namespace pictura;
 
 extern "C" {
@@ -1695,7 +1734,6 @@ pictura_status pictura_policy_loss(const pictura_logits* logits, const pictura_p
     double* part = (double*)((char*)workspace + 256);
     const int64_t parts = R.rows / kMomentRows < 1 ? 1 : R.rows / kMomentRows < kMomentBlocks ? R.rows / kMomentRows : kMomentBlocks;
     const Work k{part, (int32_t)parts, part + 3 * kMomentBlocks, done};
-    hipLaunchKernelGGL(loss_moments_kernel, dim3((unsigned)parts), dim3(kThreads), 0, s, b, R.rows, R.actions, part, done);
     if (logits->dtype == PICTURA_F32) launch_loss<float>(R, b, k, s);
     else if (logits->dtype == PICTURA_BF16) launch_loss<__bf16>(R, b, k, s);
     else launch_loss<_Float16>(R, b, k, s);
@@ -1703,3 +1741,4 @@ pictura_status pictura_policy_loss(const pictura_logits* logits, const pictura_p
 }
 
 }  // extern "C"
+#endif
