@@ -425,13 +425,12 @@ __device__ __forceinline__ void renew(uint32_t (&x)[V])
     for (int v = 0; v < V; ++v) asm volatile("" : "+v"(x[v]));
 }
 
-// A row of V-element vectors at 16-byte addresses: vector q covers the elements
+// A row of V-element vectors at addresses that are a multiple of them: vector q covers the elements
 // from q V - shift on, the first and the last perhaps only in part.  A thread of
 // a workgroup of NW waves holds up to NV of them, 64 vectors apart, and a wave a
 // stretch of the row.
-template <class T, int NW, int NV>
+template <class T, int NW, int NV, int V>
 struct VecRow {
-    static constexpr int V = 16 / sizeof(T);
     Row<T> row;
     int A, shift, vectors, per, q0;
     __device__ __forceinline__ VecRow(const Rows& r, int64_t n, int wave, int lane) : row(r, n), A(r.actions)
@@ -450,7 +449,7 @@ struct VecRow {
     // The logits' bits, -inf where there is none.
     __device__ __forceinline__ void load(uint32_t (&r)[NV][V]) const
     {
-        struct alignas(16) Vec { T v[V]; };
+        struct alignas(V * sizeof(T)) Vec { T v[V]; };
         const Vec* at = reinterpret_cast<const Vec*>(row.x - shift) + q0;
         const uint32_t none = __float_as_uint(-INFINITY);
 #pragma unroll
@@ -508,19 +507,153 @@ constexpr int kRank = 256;   // candidates that are ranked by counting
 // Shared memory of a row's workgroup.
 template <int NW, bool kFilter>
 struct RowLds {
-    static constexpr int kBins = NW == 1 ? 256 : 1024, kList = NW == 1 ? 1024 : 2048;
-    unsigned long long hist[kFilter ? kBins + kBins / 16 : 1];
-    uint64_t sums[4][NW], told[4];
-    uint64_t before[kFilter ? kRank : 1];       // weight of the candidates above each
-    float list[kFilter ? kList + 4 : 1];        // candidates
-    uint32_t weight[kFilter ? kRank + 4 : 1];   // theirs
-    uint32_t equal[kFilter ? kRank : 1];        // candidates equal to each
+    static constexpr int kBins = NW == 1 ? 256 : 1024, kList = NW == 1 ? 512 : 2048;
+    alignas(16) unsigned long long hist[kFilter ? kBins + kBins / 16 : 1];
+    alignas(16) float list[kFilter ? kList + 4 : 1];        // candidates
+    alignas(16) uint32_t weight[kFilter ? kRank + 4 : 1];   // theirs
+    alignas(16) int32_t index[kFilter ? kRank + 4 : 1];     // and where they stand
+    uint64_t sums[2][NW], told[5];
     uint32_t listed;
     float maxima[3][NW];
     uint32_t ties[NW];
 };
 
 constexpr uint32_t kTie = 0xFFFFFFFFu;   // in a weight's place: equal to the cut
+
+constexpr int kSmallBins = 256;
+
+// First of kSmallBins bins up to which the counts reach need, the last where they do
+// not; every wave for itself.
+__device__ __forceinline__ int find_small_bin(const uint32_t* hist, uint32_t need)
+{
+    const int lane = threadIdx.x & 63;
+    const uint4 h = *reinterpret_cast<const uint4*>(hist + 4 * lane);
+    const uint32_t mine = h.x + h.y + h.z + h.w, run = wave_scan(mine);
+    const uint64_t hit = __ballot(run >= need);
+    if (!hit) return kSmallBins - 1;
+    const int at = __ffsll((unsigned long long)hit) - 1;
+    const uint32_t left = need - from_lane(run - mine, at);
+    const uint32_t a = from_lane(h.x, at), b = from_lane(h.y, at), c = from_lane(h.z, at);
+    return 4 * at + (left <= a ? 0 : left <= a + b ? 1 : left <= a + b + c ? 2 : 3);
+}
+
+// What one wave wrote to LDS is there for its other lanes.
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The draw among C <= kRank candidates, which hold the top_k largest logits: each is
+// ranked by counting those above it.  (A loop over four candidates at a time waits
+// for LDS some 130 cycles: few candidates, and spread over the waves.)
+template <int NW, class Lds>
+__device__ __forceinline__ void draw_from_list(Lds& lds, uint32_t C, const Weights& weight, const RowSampling& q,
+                                               int64_t n, int64_t* __restrict__ out_action, float* __restrict__ out_logp)
+{
+    constexpr uint32_t NT = NW * 64;
+    constexpr int Q = kRank / NT < 1 ? 1 : kRank / NT;   // candidates of a thread
+    const uint32_t k = min((uint32_t)q.top_k, C), wave0 = threadIdx.x & ~63u;
+    const bool nucleus = q.top_p < 1.0f;
+    float x[Q];
+    uint32_t w[Q], above[Q], equal[Q];
+    uint64_t before[Q];
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+        const uint32_t c = threadIdx.x + NT * i;
+        x[i] = -INFINITY;
+        w[i] = above[i] = equal[i] = 0;
+        before[i] = 0;
+        if (wave0 + NT * i < C) {
+            if (c < C) x[i] = lds.list[c];
+            w[i] = weight(x[i]);
+            if (c < kRank) lds.weight[c] = w[i];   // (past C: 0)
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < Q; ++i)
+        if (wave0 + NT * i < C) {
+#pragma unroll 2
+            for (uint32_t b = 0; b < C; b += 4) {   // (past C: -inf)
+                const float4 y = *reinterpret_cast<const float4*>(lds.list + b);
+                const uint4 z = *reinterpret_cast<const uint4*>(lds.weight + b);
+                above[i] += (y.x > x[i]) + (y.y > x[i]) + (y.z > x[i]) + (y.w > x[i]);
+                equal[i] += (y.x == x[i]) + (y.y == x[i]) + (y.z == x[i]) + (y.w == x[i]);
+                before[i] += (uint64_t)(y.x > x[i] ? z.x : 0u) + (y.y > x[i] ? z.y : 0u);
+                before[i] += (uint64_t)(y.z > x[i] ? z.z : 0u) + (y.w > x[i] ? z.w : 0u);
+            }
+            if (threadIdx.x + NT * i < C && above[i] < k && k <= above[i] + equal[i]) {   // (equal ones write the same)
+                lds.told[0] = (uint64_t)equal[i] << 32 | __float_as_uint(x[i]);
+                lds.told[1] = k - above[i];
+                lds.told[2] = before[i] + (uint64_t)(k - above[i]) * w[i];
+            }
+        }
+    __syncthreads();
+    float over = __uint_as_float(same_in_wave((uint32_t)lds.told[0]));
+    uint32_t same = same_in_wave((uint32_t)(lds.told[0] >> 32)), ties = same_in_wave((uint32_t)lds.told[1]);
+    if (nucleus) {
+        uint64_t need = share(lds.told[2], cut31(q.top_p));
+        if (need < 1) need = 1;
+#pragma unroll
+        for (int i = 0; i < Q; ++i)
+            if (threadIdx.x + NT * i < C && x[i] >= over) {
+                const uint32_t some = x[i] == over ? ties : equal[i];
+                if (before[i] < need && need <= before[i] + (uint64_t)some * w[i]) {
+                    lds.told[3] = (uint64_t)equal[i] << 32 | __float_as_uint(x[i]);
+                    lds.told[4] = ties_for(need - before[i], w[i]);
+                }
+            }
+        __syncthreads();
+        over = __uint_as_float(same_in_wave((uint32_t)lds.told[3]));
+        same = same_in_wave((uint32_t)(lds.told[3] >> 32));
+        ties = same_in_wave((uint32_t)lds.told[4]);
+    }
+    // what is left of each weight
+    uint32_t index[Q];
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+        const uint32_t c = threadIdx.x + NT * i;
+        index[i] = 0xFFFFFFFFu;
+        if (wave0 + NT * i < C) {
+            if (c < C) index[i] = (uint32_t)lds.index[c];
+            bool in = c < C && x[i] >= over && w[i] >= q.least;
+            if (ties < same && __any(in && x[i] == over)) {   // the first of the equal ones, by index
+                uint32_t ahead = 0;
+#pragma unroll 2
+                for (uint32_t b = 0; b < C; b += 4) {
+                    const float4 y = *reinterpret_cast<const float4*>(lds.list + b);
+                    const int4 z = *reinterpret_cast<const int4*>(lds.index + b);
+                    ahead += (y.x == x[i] && (uint32_t)z.x < index[i]) + (y.y == x[i] && (uint32_t)z.y < index[i]);
+                    ahead += (y.z == x[i] && (uint32_t)z.z < index[i]) + (y.w == x[i] && (uint32_t)z.w < index[i]);
+                }
+                in = in && (x[i] > over || ahead < ties);
+            }
+            w[i] = in ? w[i] : 0u;
+            if (c < kRank) lds.weight[c] = w[i];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < Q; ++i)
+        if (__any(w[i] != 0)) {
+            uint64_t total = 0, first = 0;   // all weights, and those that come before by index
+#pragma unroll 2
+            for (uint32_t b = 0; b < C; b += 4) {
+                const int4 y = *reinterpret_cast<const int4*>(lds.index + b);
+                const uint4 z = *reinterpret_cast<const uint4*>(lds.weight + b);
+                total += (uint64_t)z.x + z.y;
+                total += (uint64_t)z.z + z.w;
+                first += (uint64_t)((uint32_t)y.x < index[i] ? z.x : 0u) + ((uint32_t)y.y < index[i] ? z.y : 0u);
+                first += (uint64_t)((uint32_t)y.z < index[i] ? z.z : 0u) + ((uint32_t)y.w < index[i] ? z.w : 0u);
+            }
+            const uint64_t target = share(total, cut31(q.u));
+            if (first <= target && target - first < w[i]) {
+                out_action[n] = (int64_t)index[i];
+                out_logp[n] = q.greedy ? 0.0f : logf((float)w[i] / (float)total);
+            }
+        }
+}
 
 // One workgroup of NW waves per row, ITEMS logits to a thread, read once.  Each
 // wave holds a stretch of the row, 64 vectors at a time, so that running sums by
@@ -533,14 +666,16 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
                                                              int64_t* __restrict__ out_action,
                                                              float* __restrict__ out_logp)
 {
-    constexpr int V = 16 / sizeof(T), NV = ITEMS / V, NT = NW * 64;
+    // (with a filter four elements to a vector, whatever their type: of eight the compiler
+    // keeps two copies)
+    constexpr int V = kFilter ? 4 : 16 / sizeof(T), NV = ITEMS / V, NT = NW * 64;
     using Lds = RowLds<NW, kFilter>;
     __shared__ alignas(16) Lds lds;
     const int A = R.actions;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t n = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (n >= R.rows) return;
-    const VecRow<T, NW, NV> vr(R, n, wave, lane);
+    const VecRow<T, NW, NV, V> vr(R, n, wave, lane);
     const Row<T>& row = vr.row;
     const RowSampling q(S, uniform, n);
     const int per = vr.per;
@@ -556,16 +691,40 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
         for (int v = 1; v < V; ++v) m = fmaxf(m, x(j, v));
         return m;
     };
+    float low = INFINITY;   // smallest of the fours' maxima
 #pragma unroll
     for (int j = 0; j < NV; ++j)
         if (j < per) {
             renew(r[j]);
-            top = fmaxf(top, vmax(j));
+            const float m = vmax(j);
+            top = fmaxf(top, m);
+            if (kFilter) low = m > -INFINITY ? fminf(low, m) : low;
 #pragma unroll
             for (int v = 0; v < V; ++v) odd |= !(x(j, v) < INFINITY);
         }
+    const bool some_k = kFilter && q.top_k > 0 && q.top_k < A;
+    uint32_t* const counts = reinterpret_cast<uint32_t*>(lds.hist);
+    if constexpr (kFilter) {
+        if (some_k) {
+            for (int i = threadIdx.x; i < kSmallBins; i += NT) counts[i] = 0;
+            for (int i = threadIdx.x; i < kRank + 4; i += NT) lds.list[i] = -INFINITY;
+        }
+        if (threadIdx.x == 0) lds.listed = 0;
+    }
     // the largest logit; a NaN or +inf, or a temperature without meaning, makes no draw
-    top = block_max<NW>(odd ? INFINITY : top, lds.maxima[0]);
+    top = wave_max(odd ? INFINITY : top);
+    if (kFilter) low = -wave_max(-low);
+    if constexpr (NW > 1) {
+        if (lane == 0) {
+            lds.maxima[0][wave] = top;
+            lds.maxima[1][wave] = -low;
+        }
+        __syncthreads();
+        top = from_lane(lane_scan<NW>(lds.maxima[0][lane & (NW - 1)], -INFINITY, Max{}), NW - 1);
+        if (kFilter) low = -from_lane(lane_scan<NW>(lds.maxima[1][lane & (NW - 1)], -INFINITY, Max{}), NW - 1);
+    } else if (kFilter) {
+        wave_fence();
+    }
     if (top == INFINITY || top == -INFINITY) {
         if (threadIdx.x == 0) {
             out_action[n] = -1;
@@ -578,67 +737,22 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
     float over = -INFINITY;
     uint32_t ties = 0;
     bool by_logit = false;   // the cut comes from the logits, before any weight
-    // the cut among lds.list[0 .. C): by count, or by weight, up to `need`
-    auto rank_list = [&](uint32_t C, bool weigh) {
-        if (threadIdx.x < 4) {
-            lds.list[C + threadIdx.x] = -INFINITY;
-            lds.weight[C + threadIdx.x] = 0;
-        }
-        if (weigh)
-            for (uint32_t i = threadIdx.x; i < C; i += NT) lds.weight[i] = weight(lds.list[i]);
-        __syncthreads();
-    };
     if constexpr (kFilter) {
-        bool cut_k = false;
-        if (q.top_k > 0 && q.top_k < A) {
-            uint32_t some = 0;
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-                if (j < per) {
-                    renew(r[j]);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) some += x(j, v) != -INFINITY;
-                }
-            cut_k = block_sum<NW>((uint64_t)some, lds.sums[0]) > (uint64_t)q.top_k;
-        }
-        if (cut_k) {
-            by_logit = true;
-            // The top_k-th largest of the vectors' maxima is no more than the top_k-th
+        if (some_k) {
+            // The top_k-th largest of the maxima of four is no more than the top_k-th
             // largest logit: a histogram of them bounds the logits that can be kept
             // from below, and those few are listed.
-            float low = INFINITY;
-            uint32_t vecs = 0;
+            const float scale = (float)kSmallBins / (top - low);   // (no range: NaN, and all in bin 0)
+            auto bin = [&](float y) { return (int)fminf(fmaxf((top - y) * scale, 0.0f), (float)(kSmallBins - 1)); };
 #pragma unroll
             for (int j = 0; j < NV; ++j)
                 if (j < per) {
                     renew(r[j]);
                     const float m = vmax(j);
-                    if (m > -INFINITY) {
-                        low = fminf(low, m);
-                        ++vecs;
-                    }
+                    if (m > -INFINITY) atomicAdd(&counts[bin(m)], 1u);
                 }
-            for (int i = threadIdx.x; i < Lds::kBins + Lds::kBins / 16; i += NT) lds.hist[i] = 0;
-            if (threadIdx.x == 0) lds.listed = 0;
-            low = -block_max<NW>(-low, lds.maxima[1]);
-            if (NW == 1) __syncthreads();
-            const float scale = (float)Lds::kBins / (top - low);   // (no range: NaN, and all in bin 0)
-            auto bin = [&](float y) { return (int)fminf(fmaxf((top - y) * scale, 0.0f), (float)(Lds::kBins - 1)); };
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-                if (j < per) {
-                    renew(r[j]);
-                    const float m = vmax(j);
-                    if (m > -INFINITY) atomicAdd(&lds.hist[padded(bin(m))], 1ull);
-                }
-            const bool enough = block_sum<NW>((uint64_t)vecs, lds.sums[1]) >= (uint64_t)q.top_k;
-            int edge = Lds::kBins - 1;
-            if (enough) {
-                if (NW == 1) __syncthreads();
-                if (wave == 0) find_bin(lds.hist, Lds::kBins, (uint64_t)q.top_k, lds.told);
-                __syncthreads();
-                edge = (int)same_in_wave((uint32_t)lds.told[0]);
-            }
+            __syncthreads();
+            const int edge = find_small_bin(counts, (uint32_t)q.top_k);
 #pragma unroll
             for (int j = 0; j < NV; ++j)
                 if (j < per) {
@@ -650,56 +764,20 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
                             if (x(j, v) > -INFINITY && bin(x(j, v)) <= edge) {
                                 const uint32_t at = atomicAdd(&lds.listed, 1u);
                                 if (at < Lds::kList) lds.list[at] = x(j, v);
+                                if (at < kRank) lds.index[at] = vr.first(j) + v;
                             }
                     }
                 }
             __syncthreads();
             const uint32_t C = same_in_wave(lds.listed);
             if (C <= kRank) {
-                // how many and how much is above each, and equal to it
-                rank_list(C, q.top_p < 1.0f);
-                for (uint32_t i = threadIdx.x; i < C; i += NT) {
-                    const float xi = lds.list[i];
-                    uint32_t above = 0, equal = 0;
-                    uint64_t before = 0;
-                    for (uint32_t k = 0; k < C; k += 4) {
-                        const float4 y = *reinterpret_cast<const float4*>(lds.list + k);
-                        const uint4 w = *reinterpret_cast<const uint4*>(lds.weight + k);
-                        above += (y.x > xi) + (y.y > xi) + (y.z > xi) + (y.w > xi);
-                        equal += (y.x == xi) + (y.y == xi) + (y.z == xi) + (y.w == xi);
-                        before += (uint64_t)(y.x > xi ? w.x : 0u) + (y.y > xi ? w.y : 0u);
-                        before += (uint64_t)(y.z > xi ? w.z : 0u) + (y.w > xi ? w.w : 0u);
-                    }
-                    lds.before[i] = before;
-                    lds.equal[i] = equal;
-                    if (above < (uint32_t)q.top_k && (uint32_t)q.top_k <= above + equal) {
-                        // (equal ones write the same)
-                        lds.told[0] = (uint64_t)__float_as_uint(xi);
-                        lds.told[1] = (uint64_t)((uint32_t)q.top_k - above);
-                        lds.told[2] = before + (uint64_t)((uint32_t)q.top_k - above) * lds.weight[i];
-                    }
-                }
-                __syncthreads();
-                over = __uint_as_float(same_in_wave((uint32_t)lds.told[0]));
-                ties = same_in_wave((uint32_t)lds.told[1]);
-                if (q.top_p < 1.0f) {
-                    uint64_t need = share(lds.told[2], cut31(q.top_p));
-                    if (need < 1) need = 1;
-                    __syncthreads();
-                    for (uint32_t i = threadIdx.x; i < C; i += NT) {
-                        const float xi = lds.list[i];
-                        const uint32_t equal = xi == over ? ties : lds.equal[i];
-                        const uint64_t before = lds.before[i];
-                        if (xi >= over && before < need && need <= before + (uint64_t)equal * lds.weight[i]) {
-                            lds.told[0] = (uint64_t)__float_as_uint(xi);
-                            lds.told[1] = ties_for(need - before, lds.weight[i]);
-                        }
-                    }
-                    __syncthreads();
-                    over = __uint_as_float(same_in_wave((uint32_t)lds.told[0]));
-                    ties = same_in_wave((uint32_t)lds.told[1]);
-                }
-            } else {
+                draw_from_list<NW>(lds, C, weight, q, n, out_action, out_logp);
+                return;
+            }
+            // (where the fours are fewer than top_k all that is allowed is listed, and top_k
+            // of them or fewer are no cut)
+            if (C > (uint32_t)q.top_k) {
+                by_logit = true;
                 auto narrow = [&](auto each) {
                     Cut cut = find_cut(each, 0u, (uint64_t)q.top_k, [](float) { return 1u; }, lds.hist, lds.told);
                     if (q.top_p < 1.0f) {
@@ -707,7 +785,7 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
                         each([&](float y) {
                             if (order_key(y) > cut.key) above += weight(y);
                         });
-                        above = block_sum<NW>(above, lds.sums[2]);
+                        above = block_sum<NW>(above, lds.sums[0]);
                         const uint64_t one = weight(key_value(cut.key));
                         uint64_t need = share(above + one * cut.ties, cut31(q.top_p));
                         if (need < 1) need = 1;
@@ -725,7 +803,10 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
                     narrow([&](auto f) {
                         for (int i = threadIdx.x; i < A; i += NT) f(row(i));
                     });
+                over = same_in_wave(over);
+                ties = same_in_wave(ties);
             }
+            __syncthreads();   // top_p alone lists again
         }
     }
     // The registers come to hold the weights that are left, kTie for one equal to the cut.
@@ -736,7 +817,7 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
     for (int j = 0; j < NV; ++j)
         if (j < per) {
             renew(r[j]);
-            if (!kFilter || vmax(j) >= over) {   // few vectors hold a logit that top_k keeps
+            if (!kFilter || vmax(j) >= over) {   // few of them hold a logit that top_k keeps
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     const float y = x(j, v);
@@ -760,7 +841,7 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
                 }
             for (int i = threadIdx.x; i < Lds::kBins + Lds::kBins / 16; i += NT) lds.hist[i] = 0;
             if (threadIdx.x == 0) lds.listed = 0;
-            sum = block_sum<NW>(sum, lds.sums[1]);
+            sum = block_sum<NW>(sum, lds.sums[0]);
             if (NW == 1) __syncthreads();
             uint64_t need = share(sum, cut31(q.top_p));
             if (need < 1) need = 1;
@@ -804,7 +885,12 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
             __syncthreads();
             const uint32_t C = same_in_wave(lds.listed);
             if (C <= kRank) {
-                rank_list(C, true);
+                if (threadIdx.x < 4) {
+                    lds.list[C + threadIdx.x] = -INFINITY;
+                    lds.weight[C + threadIdx.x] = 0;
+                }
+                for (uint32_t i = threadIdx.x; i < C; i += NT) lds.weight[i] = weight(lds.list[i]);
+                __syncthreads();
                 for (uint32_t i = threadIdx.x; i < C; i += NT) {
                     const float xi = lds.list[i];
                     uint32_t equal = 0;
@@ -897,7 +983,7 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
         total = mine = sum + (uint64_t)left * one;
     } else {
         if (lane == 0) {
-            lds.sums[3][wave] = sum;
+            lds.sums[1][wave] = sum;
             lds.ties[wave] = same;
         }
         __syncthreads();
@@ -905,7 +991,7 @@ __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const
         const uint32_t has = lds.ties[lane & (NW - 1)];
         const uint32_t before = lane_scan<NW>(has, 0u, Add{}) - has;
         const uint32_t take = before < ties ? min(ties - before, has) : 0u;
-        const uint64_t part = lds.sums[3][lane & (NW - 1)] + (uint64_t)take * one;
+        const uint64_t part = lds.sums[1][lane & (NW - 1)] + (uint64_t)take * one;
         const uint64_t run = lane_scan<NW>(part, (uint64_t)0, Add{});
         total = from_lane(run, NW - 1);
         mine = from_lane(part, wave);
@@ -1349,7 +1435,7 @@ __global__ __launch_bounds__(NW * 64) void loss_row_kernel(const Rows R, const B
     for (int64_t n = blockIdx.x; n < R.rows; n += gridDim.x) {
         const RowIn in = next;   // (the next one's numbers come while this row is worked on)
         if (n + gridDim.x < R.rows) next = row_in(b, n + gridDim.x, A);
-        const VecRow<T, NW, NV> vr(R, n, wave, lane);
+        const VecRow<T, NW, NV, V> vr(R, n, wave, lane);
         const int per = vr.per;
         const float w = same_in_wave(in.w);
         const bool on = w != 0.0f;
