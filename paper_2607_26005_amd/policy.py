@@ -84,7 +84,8 @@ class _PolicyLoss(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dloss, _):
         dlogits, dvalues = ctx.saved_tensors
-        return dlogits * dloss.to(dlogits.dtype), dvalues * dloss, None, None
+        # (the product in fp32: a loss scale may be beyond what the logits' type holds)
+        return (dlogits.float() * dloss).to(dlogits.dtype), dvalues * dloss, None, None
 
 
 def policy_loss(logits, values, actions, old_logp, advantages, returns, **kwargs):

@@ -415,3 +415,18 @@ def test_draw_and_loss_in_a_graph(mods):
         torch.cuda.synchronize()
         for x, y in zip(got_now, want):
             assert torch.equal(x, y), k
+
+
+def test_loss_scales_beyond_the_logits_type(mods):
+    """The gradient that arrives at the loss may be a loss scale, and 2^17 is no number in
+    fp16: what it makes of the gradient still is one."""
+    torch, policy = mods
+    logits, z, b = _batch(torch, 300, 12, "float16", 4)
+    old = _old_logp(torch, z, b).cuda()
+    c = {k: v.cuda() for k, v in b.items()}
+    x, v = logits.clone().requires_grad_(), c["values"].clone().requires_grad_()
+    loss, _ = policy.policy_loss(x, v, c["actions"], old, c["advantages"], c["returns"])
+    (2.0 ** 17 * loss).backward()
+    out = policy.policy_gradient(logits, c["values"], c["actions"], old, c["advantages"], c["returns"])
+    assert torch.equal(x.grad, (out.dlogits.float() * 2.0 ** 17).half()) and x.grad.isfinite().all()
+    assert torch.equal(v.grad, out.dvalues * 2.0 ** 17)
