@@ -1,5 +1,24 @@
 // The policy's decisions: actions drawn from logits, and the clipped policy loss
 // over them with its gradient.
+//
+// Drawing.  The probabilities of a row are held as whole numbers, w = rint(2^31
+// exp((x - max) / T)): sums of them are exact, so a draw does not depend on the order
+// or the split of a sum, and a row draws alike alone and in any batch.  Weights below
+// 2^-32 of the largest vanish.  What is kept by top_k and top_p is a prefix in the
+// order of the logits, so a row needs the logit that the prefix ends with and not a
+// sort.
+//
+// Both work on rows from a few actions to 2^20.  Up to 16 (loss) or 64 (drawing)
+// actions a row takes a thread or a group of lanes; up to 73,728 it is held in the
+// registers of one to sixteen waves and read once; longer ones are read again for
+// every pass.
+//
+// Measured (a whole call among others; one MI355X, whose large copies run at 4,906
+// GB/s and whose launches take 3.8 us): 65,536 rows of 12 drawn in 11.8 us, one row
+// of 16,385 with top_k and top_p 10.4 us, 2,048 rows of 4,099 in bf16 with all three
+// filters 36.6 us, 512 rows of 65,536 with top_p 100 us (134 MB read: 27 us at a copy's
+// rate), without it 52 us; loss and gradient of 65,536 rows of 12 20.4 us, of 2,047
+// rows of 16,381 in bf16 64 us (134 MB read and written).
 #include <cmath>
 #include <type_traits>
 
@@ -285,7 +304,28 @@ struct RowSampling {
 // rows of any length: read again for every pass
 // ---------------------------------------------------------------------------
 
+// Sixteen waves to a row, eight loads of each thread under way: bound by the loads'
+// latency.  256 rows of 131,072 in fp32 are drawn in 87 us without filters and 238 with
+// top_p (170 and 437 with one load at a time), their loss and gradient take 112 us (571
+// with four waves and one load).  A row stays on one CU, however few rows there are: one
+// of 131,072 takes 230 us.
 constexpr int kLongWaves = 16;
+constexpr int kAhead = 8;   // loads of a thread that are under way together
+
+// f(i, x) for the logits of a row at i0, i0 + step, ... below i1, in that order.
+template <class T, class F>
+__device__ __forceinline__ void walk_row(const Row<T>& row, int i0, int i1, int step, F f)
+{
+    int i = i0;
+    for (; i < i1 - (kAhead - 1) * step; i += kAhead * step) {
+        float x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) x[u] = row(i + u * step);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) f(i + u * step, x[u]);
+    }
+    for (; i < i1; i += step) f(i, row(i));
+}
 
 template <class T>
 __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows R, const Sampling S,
@@ -303,9 +343,7 @@ __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows
     for (int64_t n = blockIdx.x; n < R.rows; n += gridDim.x) {
         const Row<T> row(R, n);
         const RowSampling q(S, uniform, n);
-        auto each = [&](auto f) {
-            for (int i = threadIdx.x; i < A; i += NT) f(row(i));
-        };
+        auto each = [&](auto f) { walk_row(row, threadIdx.x, A, NT, [&](int, float x) { f(x); }); };
         // the largest logit; a NaN or +inf, or a temperature without meaning, makes no draw
         float top = -INFINITY, bad = q.temp >= 0.0f ? 0.0f : 1.0f;
         each([&](float x) {
@@ -350,13 +388,12 @@ __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows
         const int per = ((A + NT - 1) / NT) * 64, i0 = min(A, wave * per), i1 = min(A, i0 + per);
         uint64_t sum = 0;
         uint32_t ties = 0;
-        for (int i = i0 + lane; i < i1; i += 64) {
-            const float x = row(i);
+        walk_row(row, i0 + lane, i1, 64, [&](int, float x) {
             const uint32_t key = order_key(x);
-            if (x == -INFINITY) continue;
+            if (x == -INFINITY) return;
             if (key > cut.key) sum += kept(x);
             ties += key == cut.key;
-        }
+        });
         sum = wave_sum(sum);
         ties = wave_sum(ties);
         const uint32_t one = cut.ties ? kept(key_value(cut.key)) : 0u;
@@ -381,25 +418,43 @@ __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows
         }
         const uint64_t target = share(total, cut31(q.u));
         if (base <= target && target - base < mine) {   // one wave: it walks through its part
-            for (int b = i0; b < i1; b += 64) {
-                const int i = b + lane;
-                const float x = i < i1 ? row(i) : -INFINITY;
-                const uint32_t key = order_key(x);
-                const bool tie = x != -INFINITY && key == cut.key;
-                const uint64_t same = __ballot(tie);
-                const uint32_t before = __popcll(same & ((1ull << lane) - 1ull));
-                const uint32_t w = x == -INFINITY ? 0u : key > cut.key || (tie && before < left) ? kept(x) : 0u;
-                const uint64_t run = wave_scan((uint64_t)w);
-                const uint64_t hit = __ballot(base + run > target);
-                if (hit) {
-                    if (lane == __ffsll((unsigned long long)hit) - 1) {
-                        out_action[n] = i;
-                        out_logp[n] = q.greedy ? 0.0f : logf((float)w / (float)total);
-                    }
-                    break;
+            for (int b = i0; b < i1; b += kAhead * 64) {
+                float x[kAhead];
+                uint32_t w[kAhead];
+                uint64_t some = 0;
+#pragma unroll
+                for (int v = 0; v < kAhead; ++v) {
+                    const int i = b + v * 64 + lane;
+                    x[v] = i < i1 ? row(i) : -INFINITY;
                 }
-                base += __shfl(run, 63);
-                left -= min(left, (uint32_t)__popcll(same));
+#pragma unroll
+                for (int v = 0; v < kAhead; ++v) {
+                    const uint32_t key = order_key(x[v]);
+                    const bool tie = x[v] != -INFINITY && key == cut.key;
+                    const uint64_t same = __ballot(tie);
+                    const uint32_t before = __popcll(same & ((1ull << lane) - 1ull));
+                    w[v] = x[v] == -INFINITY ? 0u : key > cut.key || (tie && before < left) ? kept(x[v]) : 0u;
+                    left -= min(left, (uint32_t)__popcll(same));
+                    some += w[v];
+                }
+                some = wave_sum(some);
+                if (base + some <= target) {
+                    base += some;
+                    continue;
+                }
+                bool found = false;
+#pragma unroll
+                for (int v = 0; v < kAhead; ++v) {
+                    const uint64_t run = wave_scan((uint64_t)w[v]);
+                    const uint64_t hit = __ballot(base + run > target);
+                    if (hit && !found && lane == __ffsll((unsigned long long)hit) - 1) {
+                        out_action[n] = b + v * 64 + lane;
+                        out_logp[n] = q.greedy ? 0.0f : logf((float)w[v] / (float)total);
+                    }
+                    found = found || hit;
+                    base += __shfl(run, 63);
+                }
+                break;
             }
         }
         __syncthreads();
@@ -660,14 +715,25 @@ __device__ __forceinline__ void draw_from_list(Lds& lds, uint32_t C, const Weigh
 // index go wave by wave.  A cut is found (the value that the kept prefix ends
 // with, and how many of the logits equal to it are kept), then the registers hold
 // the weights that are left, then the draw goes by their sums.
+//
+// top_k needs no exponentials but its candidates': a histogram of the maxima of four
+// bounds them from below, and most rows end with the few that are listed (2,048 rows
+// of 4,099 in fp32: 25 us with top_k 64, with or without top_p 0.95, and 15 without
+// filters).  top_p alone needs all weights, then a histogram by weight of those that
+// can matter (30 us).
+// 512 rows of 65,536 with top_p: 100 us, the vector unit issues in 63 % of it, 75
+// instructions for 64 logits.  A CU's registers hold one such row, so no loads run
+// under the arithmetic of another.  16-bit rows of over 32,768 logits with a filter
+// do not fit the 128 registers of a wave of sixteen as they are compiled, and spill (512 rows of 65,536 in bf16: 325 us
+// with top_p, 152 with top_k 64, 42 without; 1,024 of 32,768, which do not: 102).
 template <class T, int NW, int ITEMS, bool kFilter>
 __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const Sampling S,
                                                              const float* __restrict__ uniform,
                                                              int64_t* __restrict__ out_action,
                                                              float* __restrict__ out_logp)
 {
-    // (with a filter four elements to a vector, whatever their type: of eight the compiler
-    // keeps two copies)
+    // (with a filter four elements to a vector, whatever their type: eight take more
+    // registers)
     constexpr int V = kFilter ? 4 : 16 / sizeof(T), NV = ITEMS / V, NT = NW * 64;
     using Lds = RowLds<NW, kFilter>;
     __shared__ alignas(16) Lds lds;
@@ -1066,7 +1132,9 @@ __device__ __forceinline__ V group_sum(V x)
 }
 
 // Heads of up to 64 actions.  Each lane holds one action; where a filter is on, it
-// counts the actions and adds the weights that come before its own, A steps.
+// counts the actions and adds the weights that come before its own, A steps.  65,536
+// rows of 12: 8.4 us of kernel, 230 vector instructions for a wave's four rows; the
+// call takes 10 to 12 us, launch and binding included.
 template <class T, int G, bool kFilter>
 __global__ __launch_bounds__(kThreads) void sample_small_kernel(const Rows R, const Sampling S,
                                                                 const float* __restrict__ uniform,
@@ -1134,17 +1202,18 @@ __global__ __launch_bounds__(kThreads) void sample_small_kernel(const Rows R, co
 // ---------------------------------------------------------------------------
 
 // Over the workgroup; the array may be in use before.
-template <class V>
+template <int NW = kWaves, class V>
 __device__ __forceinline__ V loss_sum(V x, V* lds)
 {
     __syncthreads();
-    return block_sum<kWaves>(x, lds);
+    return block_sum<NW>(x, lds);
 }
 
+template <int NW>
 __device__ __forceinline__ float loss_max(float x, float* lds)
 {
     __syncthreads();
-    return block_max<kWaves>(x, lds);
+    return block_max<NW>(x, lds);
 }
 
 // Weight of row n, 0 where it does not count.
@@ -1275,7 +1344,8 @@ __device__ __forceinline__ void loss_stats(const Batch& b, const Shared3& s, con
 
 // Leave this workgroup's sums; the last workgroup to do so adds them all up, in the
 // order of the workgroups, and writes the statistics.  (Where a launch writes much,
-// the fence that this takes in every workgroup costs more than another launch.)
+// the fence that this takes in every workgroup costs more than another launch: 2,047
+// rows of 16,381 in bf16 78 us with it, 58 with loss_stats_kernel.)
 template <int NW>
 __device__ void loss_finish(const Batch& b, const Shared3& s, const double* acc, double* __restrict__ sums,
                             uint32_t* __restrict__ done)
@@ -1311,7 +1381,9 @@ __device__ __forceinline__ float exp_of(float d)
 
 // Heads of up to 16 actions: a row to a thread.  What a row takes apart from its
 // logits (the terms, two exponentials, a logarithm) is then done once for it, not by
-// every lane of a group.
+// every lane of a group: the calls for 65,536 rows of 12 take 20 us, and
+// took 42 in groups of 16 lanes (2,048 rows: 19 and 22).  17 us of it is this kernel,
+// one wave to a SIMD and bound by its latencies.
 template <class T>
 __global__ __launch_bounds__(kThreads) void loss_thread_kernel(const Rows R, const Batch b, const Work k)
 {
@@ -1415,7 +1487,9 @@ __global__ __launch_bounds__(kThreads) void loss_small_kernel(const Rows R, cons
 // Rows held in registers, as in sample_row_kernel: the logits are read once and the
 // gradient written once.  With e = exp d and S its sum, d loss / d logit of action i is
 // e_i (k1 d_i + k0), plus g at the action taken.  For 16-bit logits d is kept in units
-// of log 2, so that its exponential is one instruction.
+// of log 2, so that its exponential is one instruction.  2,047 rows of 16,381 in bf16:
+// 40 us of kernel (3.3 TB/s read and written, 25 vector instructions for 64 logits), 64
+// with the other launches; 4,096 of 8,191 in fp32 64 us with them (4.2 TB/s).
 template <class T, int NW, int ITEMS>
 __global__ __launch_bounds__(NW * 64) void loss_row_kernel(const Rows R, const Batch b, const Work k)
 {
@@ -1536,9 +1610,10 @@ __global__ __launch_bounds__(NW * 64) void loss_row_kernel(const Rows R, const B
 
 // One workgroup per row, the row read again for every pass.
 template <class T>
-__global__ __launch_bounds__(kThreads) void loss_long_kernel(const Rows R, const Batch b, const Work k)
+__global__ __launch_bounds__(kLongWaves * 64) void loss_long_kernel(const Rows R, const Batch b, const Work k)
 {
-    __shared__ float ldsf[kWaves];
+    constexpr int NT = kLongWaves * 64;
+    __shared__ float ldsf[kLongWaves];
     const Shared3 s = loss_shared(b, k.part, k.parts);
     const int A = R.actions;
     double acc[kSums] = {};
@@ -1548,37 +1623,37 @@ __global__ __launch_bounds__(kThreads) void loss_long_kernel(const Rows R, const
         const RowIn in = row_in(b, n, A);
         const float w = in.w;
         if (w == 0.0f) {
-            for (int i = threadIdx.x; i < A; i += kThreads) out[i] = (T)0.0f;
+            for (int i = threadIdx.x; i < A; i += NT) out[i] = (T)0.0f;
             if (threadIdx.x == 0) b.dvalues[n] = 0.0f;
             continue;
         }
         const int a = in.action;
         float top = -INFINITY;
-        for (int i = threadIdx.x; i < A; i += kThreads) top = fmaxf(top, row(i));
+        walk_row(row, threadIdx.x, A, NT, [&](int, float x) { top = fmaxf(top, x); });
         const float xa = row(a);
-        top = loss_max(top, ldsf);
+        top = loss_max<kLongWaves>(top, ldsf);
         const float rt = b.temperature;
         // d = (x - top) / T, sum of e = exp d, and of e d
         auto dist = [&](float x) { return x == -INFINITY ? -INFINITY : (x - top) / rt; };
         float e0 = 0.0f, e1 = 0.0f;
-        for (int i = threadIdx.x; i < A; i += kThreads) {
-            const float d = dist(row(i)), e = expf(d);
+        walk_row(row, threadIdx.x, A, NT, [&](int, float x) {
+            const float d = dist(x), e = expf(d);
             e0 += e;
             if (e != 0.0f) e1 += e * d;
-        }
-        e0 = loss_sum(e0, ldsf);
-        e1 = loss_sum(e1, ldsf);
+        });
+        e0 = loss_sum<kLongWaves>(e0, ldsf);
+        e1 = loss_sum<kLongWaves>(e1, ldsf);
         const float logs = logf(e0), rs = 1.0f / e0;
         const float H = e0 > 0.0f ? logs - e1 * rs : e0 == 0.0f ? 0.0f : e0;
         const RowTerms t = row_terms(b, s, in, e0 == 0.0f ? -INFINITY : dist(xa) - logs, H);
         const float scale = w * s.inv;
         const float ce = b.entropy_coef;
-        for (int i = threadIdx.x; i < A; i += kThreads) {
-            const float d = dist(row(i)), e = expf(d), p = e * rs;
+        walk_row(row, threadIdx.x, A, NT, [&](int i, float x) {
+            const float d = dist(x), e = expf(d), p = e * rs;
             float y = e != 0.0f ? p * (ce * (d - logs + H) - t.g) : 0.0f;
             if (i == a) y += t.g;
             out[i] = (T)(y * scale / rt);
-        }
+        });
         if (threadIdx.x == 0) {
             b.dvalues[n] = t.dv * scale;
             for (int q = 0; q < kSums; ++q) acc[q] += (double)w * (double)t.sums[q];
@@ -1611,7 +1686,7 @@ using Int = std::integral_constant<int, N>;
 // With many rows few waves to a row: the row's reductions take fewer barriers, and
 // more rows are under way on a CU (2,047 rows of 16,381: 58 us with four waves, 77
 // with sixteen).  With fewer rows than CUs the waves are there anyway (one row of
-// 16,385: 15 us with sixteen, 25 with four).
+// 16,385: 15 us with sixteen, 25 with four when this was chosen; 10 us now).
 struct RowShape {
     int waves, items;
 };
@@ -1707,7 +1782,7 @@ void launch_loss(const Rows& R, const Batch& b, const Work& k, hipStream_t s)
                 hipLaunchKernelGGL((loss_row_kernel<T, W, I>), grid, dim3(W * 64), 0, s, R, b, k);
             });
         else
-            go(loss_long_kernel<T>);
+            hipLaunchKernelGGL(loss_long_kernel<T>, grid, dim3(kLongWaves * 64), 0, s, R, b, k);
         hipLaunchKernelGGL(loss_stats_kernel, dim3(1), block, 0, s, b, k, (int64_t)grid.x);
     } else if (R.actions <= 16) go(loss_thread_kernel<T>);
     else if (group_lanes(R.actions) == 32) go(loss_small_kernel<T, 32>);

@@ -430,3 +430,59 @@ def test_loss_scales_beyond_the_logits_type(mods):
     out = policy.policy_gradient(logits, c["values"], c["actions"], old, c["advantages"], c["returns"])
     assert torch.equal(x.grad, (out.dlogits.float() * 2.0 ** 17).half()) and x.grad.isfinite().all()
     assert torch.equal(v.grad, out.dvalues * 2.0 ** 17)
+
+
+# Rows longer than a workgroup's registers.  A lane of such a row adds 131,075 / 1,024 =
+# 129 terms and then a tree of 10 steps: below 2^-16, as _close has it.
+
+@pytest.mark.parametrize("A", [73729, 81920, 131075])
+def test_loss_of_rows_that_registers_do_not_hold(mods, A):
+    torch, policy = mods
+    for dtype in DTYPES:
+        N = 4
+        logits, z, b = _batch(torch, N, A, dtype, A, pad=3)
+        mask = torch.rand(N, A, generator=torch.Generator().manual_seed(1)) < 0.5
+        mask.scatter_(1, b["actions"][:, None], True)
+        b["actions"][1] = -1                                 # a row that counts nothing, between others
+        zb = dict(b, actions=b["actions"].clamp(min=0))
+        for m in (None, mask):
+            out, ref = _run(torch, policy, logits, b, _old_logp(torch, z, zb, m), None if m is None else m.cuda(),
+                            entropy_coef=0.05, normalize=True)
+            _close(out, ref, dtype)
+            assert (out.dlogits[1] == 0).all() and out.dvalues[1] == 0
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("A", [73729, 74751, 90113, 262147])
+def test_long_draws_follow_the_rule_to_the_bit(mods, A, dtype):
+    """The whole-number rule of the sampler in int64: few distinct logits, so that ties
+    of the cut reach over all waves; random numbers that lead into every wave's part."""
+    torch, policy = mods
+    N = 6
+    g = torch.Generator().manual_seed(A)
+    x = (torch.randint(-24, 9, (N, A), generator=g) / 8.0).to(getattr(torch, dtype)).cuda()
+    x[3, ::2] = float("-inf")
+    u = torch.tensor([0.0, 0.1, 0.37, 0.5, 0.93, 1.0 - 2.0 ** -24])
+    for how in (dict(), dict(top_k=1000), dict(top_p=0.6), dict(top_k=5000, top_p=0.9), dict(min_p=0.2), dict(temperature=0.0)):
+        act, logp = policy.sample_actions(x, u.cuda(), **how)
+        for n in range(N):
+            row = x[n].float().cpu()
+            if how.get("temperature", 1.0) == 0.0:
+                assert int(act[n]) == int(row.argmax())
+                continue
+            w = (torch.exp(row.cuda() - row.max().item()) * 2.0 ** 31).round().long().cpu()
+            order = row.argsort(descending=True, stable=True)
+            kept = torch.zeros(A, dtype=torch.int64)
+            k = how.get("top_k", A)
+            first = order[:k]
+            ws = w[first]
+            if "top_p" in how:
+                need = max(int(ws.sum()) * int(np.floor(np.float32(how["top_p"]) * np.float32(2.0 ** 31))) >> 31, 1)
+                ws = torch.where(ws.cumsum(0) - ws < need, ws, 0)
+            kept[first] = ws
+            kept[kept < int(np.ceil(np.float32(how.get("min_p", 0.0)) * np.float32(2.0 ** 31)))] = 0
+            total = int(kept.sum())
+            target = total * int(np.floor(np.float32(u[n].item()) * np.float32(2.0 ** 31))) >> 31
+            want = int((kept.cumsum(0) > target).nonzero()[0])
+            assert int(act[n]) == want, (how, n, int(act[n]), want)
+            assert abs(float(logp[n]) - np.log(int(kept[want]) / total)) < 1e-5
