@@ -480,6 +480,9 @@ __device__ __forceinline__ void renew(uint32_t (&x)[V])
     for (int v = 0; v < V; ++v) asm volatile("" : "+v"(x[v]));
 }
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 // A row of V-element vectors at addresses that are a multiple of them: vector q covers the elements
 // from q V - shift on, the first and the last perhaps only in part.  A thread of
 // a workgroup of NW waves holds up to NV of them, 64 vectors apart, and a wave a
@@ -507,14 +510,37 @@ struct VecRow {
         struct alignas(V * sizeof(T)) Vec { T v[V]; };
         const Vec* at = reinterpret_cast<const Vec*>(row.x - shift) + q0;
         const uint32_t none = __float_as_uint(-INFINITY);
+        if constexpr (sizeof(T) == 2 && V == 4) {
+            // (converted four at a time, as registers that belong together: one by one the
+            // compiler keeps every logit twice)
+            const uint32_t half = (uint32_t)__builtin_bit_cast(uint16_t, (T)-INFINITY) * 0x10001u;
+            u32x2 raw[NV];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
+            for (int j = 0; j < NV; ++j) {
+                raw[j] = u32x2{half, half};
+                if (j < per && whole(j)) raw[j] = reinterpret_cast<const u32x2*>(at)[j * 64];
+            }
 #pragma unroll
-            for (int v = 0; v < V; ++v) r[j][v] = none;
-            if (j < per && whole(j)) {
-                const Vec t = at[j * 64];
+            for (int j = 0; j < NV; ++j) {
+                
+                const Vec t = __builtin_bit_cast(Vec, raw[j]);
+                u32x4 y;
 #pragma unroll
-                for (int v = 0; v < V; ++v) r[j][v] = __float_as_uint((float)t.v[v]);
+                for (int v = 0; v < V; ++v) y[v] = __float_as_uint((float)t.v[v]);
+                asm volatile("" : "+v"(y));
+#pragma unroll
+                for (int v = 0; v < V; ++v) r[j][v] = y[v];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) r[j][v] = none;
+                if (j < per && whole(j)) {
+                    const Vec t = at[j * 64];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) r[j][v] = __float_as_uint((float)t.v[v]);
+                }
             }
         }
         // the two ends, element by element
