@@ -7,7 +7,7 @@
 //
 // Bound by memory: 300 tensors of 50 M fp32 weights with bf16 gradients take four
 // launches of 67 us (1.3 GB at 4.8 TB/s; a large copy runs at 4.9) and 43 us for the
-// norm, which has to see every gradient before the first weight moves: 313 us the
+// norm, which has to see every gradient before the first weight moves: 316 us the
 // call.  64 tensors of 128 M bf16 weights with 8-bit moments take 290 us (1.28 GB at
 // 4.4 TB/s, 76 vector instructions for 64 weights), and their moments are decoded in
 // 228 us (1.28 GB at 5.6).  A step of 29 tensors is launches and the binding, 28 us.

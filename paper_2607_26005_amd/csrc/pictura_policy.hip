@@ -16,7 +16,7 @@
 // Measured (a whole call among others; one MI355X, whose large copies run at 4,906
 // GB/s and whose launches take 3.8 us): 65,536 rows of 12 drawn in 11.8 us, one row
 // of 16,385 with top_k and top_p 10.4 us, 2,048 rows of 4,099 in bf16 with all three
-// filters 36.6 us, 512 rows of 65,536 with top_p 100 us (134 MB read: 27 us at a copy's
+// filters 30.5 us, 512 rows of 65,536 with top_p 100 us (134 MB read: 27 us at a copy's
 // rate), without it 52 us; loss and gradient of 65,536 rows of 12 20.4 us, of 2,047
 // rows of 16,381 in bf16 64 us (134 MB read and written).
 #include <cmath>
@@ -305,12 +305,31 @@ struct RowSampling {
 // ---------------------------------------------------------------------------
 
 // Sixteen waves to a row, eight loads of each thread under way: bound by the loads'
-// latency.  256 rows of 131,072 in fp32 are drawn in 87 us without filters and 238 with
-// top_p (170 and 437 with one load at a time), their loss and gradient take 112 us (571
-// with four waves and one load).  A row stays on one CU, however few rows there are: one
-// of 131,072 takes 230 us.
+// latency.  256 rows of 131,072 in fp32 are drawn in 80 us without filters and 221 with
+// top_p (170 and 437 with one load at a time), their loss and gradient take 107 us (571
+// with four waves and one load; bf16 100).  A row stays on one CU, however few rows
+// there are: one of 131,072 with both filters takes 175 us.
 constexpr int kLongWaves = 16;
 constexpr int kAhead = 8;   // loads of a thread that are under way together
+
+// The logits at i, i + step, ...  Masked ones are loaded too: no load waits for another.
+template <class T>
+__device__ __forceinline__ void load_ahead(const Row<T>& row, int i, int step, float (&x)[kAhead])
+{
+    T t[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) t[u] = row.x[i + u * step];
+    if (row.mask) {
+        uint8_t m[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) m[u] = row.mask[i + u * step];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) x[u] = m[u] ? (float)t[u] : -INFINITY;
+    } else {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) x[u] = (float)t[u];
+    }
+}
 
 // f(i, x) for the logits of a row at i0, i0 + step, ... below i1, in that order.
 template <class T, class F>
@@ -319,8 +338,7 @@ __device__ __forceinline__ void walk_row(const Row<T>& row, int i0, int i1, int 
     int i = i0;
     for (; i < i1 - (kAhead - 1) * step; i += kAhead * step) {
         float x[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) x[u] = row(i + u * step);
+        load_ahead(row, i, step, x);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) f(i + u * step, x[u]);
     }
@@ -422,10 +440,14 @@ __global__ __launch_bounds__(kLongWaves * 64) void sample_long_kernel(const Rows
                 float x[kAhead];
                 uint32_t w[kAhead];
                 uint64_t some = 0;
+                if (b + kAhead * 64 <= i1) {
+                    load_ahead(row, b + lane, 64, x);
+                } else {
 #pragma unroll
-                for (int v = 0; v < kAhead; ++v) {
-                    const int i = b + v * 64 + lane;
-                    x[v] = i < i1 ? row(i) : -INFINITY;
+                    for (int v = 0; v < kAhead; ++v) {
+                        const int i = b + v * 64 + lane;
+                        x[v] = i < i1 ? row(i) : -INFINITY;
+                    }
                 }
 #pragma unroll
                 for (int v = 0; v < kAhead; ++v) {
@@ -749,9 +771,8 @@ __device__ __forceinline__ void draw_from_list(Lds& lds, uint32_t C, const Weigh
 // can matter (30 us).
 // 512 rows of 65,536 with top_p: 100 us, the vector unit issues in 63 % of it, 75
 // instructions for 64 logits.  A CU's registers hold one such row, so no loads run
-// under the arithmetic of another.  16-bit rows of over 32,768 logits with a filter
-// do not fit the 128 registers of a wave of sixteen as they are compiled, and spill (512 rows of 65,536 in bf16: 325 us
-// with top_p, 152 with top_k 64, 42 without; 1,024 of 32,768, which do not: 102).
+// under the arithmetic of another.
+// In bf16 the same takes 89 us; 1,024 rows of 32,768 take 90 and 93 (fp32).
 template <class T, int NW, int ITEMS, bool kFilter>
 __global__ __launch_bounds__(NW * 64) void sample_row_kernel(const Rows R, const Sampling S,
                                                              const float* __restrict__ uniform,
