@@ -502,7 +502,6 @@ __device__ __forceinline__ void renew(uint32_t (&x)[V])
     for (int v = 0; v < V; ++v) asm volatile("" : "+v"(x[v]));
 }
 
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // A row of V-element vectors at addresses that are a multiple of them: vector q covers the elements
@@ -532,26 +531,30 @@ struct VecRow {
         struct alignas(V * sizeof(T)) Vec { T v[V]; };
         const Vec* at = reinterpret_cast<const Vec*>(row.x - shift) + q0;
         const uint32_t none = __float_as_uint(-INFINITY);
-        if constexpr (sizeof(T) == 2 && V == 4) {
-            // (converted four at a time, as registers that belong together: one by one the
-            // compiler keeps every logit twice)
+        if constexpr (sizeof(T) == 2) {
+            // All loads first, then the conversions (a conversion next to its load waits for
+            // it before the next one leaves), four at a time as registers that belong
+            // together: one by one the compiler keeps every logit twice.
+            typedef uint32_t Words __attribute__((ext_vector_type(V / 2)));
             const uint32_t half = (uint32_t)__builtin_bit_cast(uint16_t, (T)-INFINITY) * 0x10001u;
-            u32x2 raw[NV];
+            Words raw[NV];
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                raw[j] = u32x2{half, half};
-                if (j < per && whole(j)) raw[j] = reinterpret_cast<const u32x2*>(at)[j * 64];
+                raw[j] = (Words)half;
+                if (j < per && whole(j)) raw[j] = reinterpret_cast<const Words*>(at)[j * 64];
             }
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                
                 const Vec t = __builtin_bit_cast(Vec, raw[j]);
-                u32x4 y;
 #pragma unroll
-                for (int v = 0; v < V; ++v) y[v] = __float_as_uint((float)t.v[v]);
-                asm volatile("" : "+v"(y));
+                for (int k = 0; k < V; k += 4) {
+                    u32x4 y;
 #pragma unroll
-                for (int v = 0; v < V; ++v) r[j][v] = y[v];
+                    for (int v = 0; v < 4; ++v) y[v] = __float_as_uint((float)t.v[k + v]);
+                    asm volatile("" : "+v"(y));
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) r[j][k + v] = y[v];
+                }
             }
         } else {
 #pragma unroll
