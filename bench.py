@@ -43,7 +43,7 @@ HBM_PEAK_GBS = 8000.0   # MI355X HBM3E peak
 # `traffic` is reported as null.
 TRAFFIC = {
     "config": 4,
-    "sources_sha256": "1861e6e0e0c1a4a94b8f4e6ba0aa85d577e1710aa85e0245d17ee356f18cf77a",
+    "sources_sha256": "f57204c5f8004a115e18e60c2d5a95c5e82a84f86e0e8eaaafbf5be163635c32",
     "fetch_bytes": 1.1530e9,
     "write_bytes": 5368709120,
 }

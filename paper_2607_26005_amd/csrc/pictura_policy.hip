@@ -16,9 +16,9 @@
 // Measured (a whole call among others; one MI355X, whose large copies run at 4,906
 // GB/s and whose launches take 3.8 us): 65,536 rows of 12 drawn in 11.8 us, one row
 // of 16,385 with top_k and top_p 10.4 us, 2,048 rows of 4,099 in bf16 with all three
-// filters 30.5 us, 512 rows of 65,536 with top_p 100 us (134 MB read: 27 us at a copy's
+// filters 30 us, 512 rows of 65,536 with top_p 96 us (134 MB read: 27 us at a copy's
 // rate), without it 52 us; loss and gradient of 65,536 rows of 12 20.4 us, of 2,047
-// rows of 16,381 in bf16 64 us (134 MB read and written).
+// rows of 16,381 in bf16 53 us (134 MB read and written).
 #include <cmath>
 #include <type_traits>
 
@@ -587,23 +587,54 @@ struct VecRow {
                 for (int v = 0; v < V; ++v) r[j][v] = j == je ? t[v] : r[j][v];
         }
         if (row.mask) {
-            struct alignas(V) Bytes { uint8_t v[V]; };
-            const bool even = ((reinterpret_cast<uintptr_t>(row.mask) - shift) & (V - 1)) == 0;
+            struct Bytes { uint8_t v[V]; };
+            if constexpr (V == 4) {
+                // four loads, at any address, before the first is waited for; more (and two
+                // of eight) take registers of which the kernels have none left
+                constexpr int kGroup = 4;
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
-                if (j < per) {
-                    const int i0 = first(j);
-                    if (even && whole(j)) {
-                        const Bytes k = *reinterpret_cast<const Bytes*>(row.mask + i0);
+                for (int j0 = 0; j0 < NV; j0 += kGroup) {
+                    uint32_t m[kGroup];
 #pragma unroll
-                        for (int v = 0; v < V; ++v) r[j][v] = k.v[v] ? r[j][v] : none;
-                    } else {
+                    for (int g = 0; g < kGroup; ++g) {
+                        const int j = j0 + g;
+                        m[g] = 0x01010101u;
+                        if (j < NV && j < per && whole(j)) __builtin_memcpy(&m[g], row.mask + first(j), V);
+                    }
 #pragma unroll
-                        for (int v = 0; v < V; ++v)
-                            if (i0 + v >= 0 && i0 + v < A && !row.mask[i0 + v]) r[j][v] = none;
+                    for (int g = 0; g < kGroup; ++g) {
+                        const int j = j0 + g;
+                        if (j < NV && j < per) {
+                            const Bytes k = __builtin_bit_cast(Bytes, m[g]);
+                            if (!whole(j)) mask_ends(j, r[j]);
+#pragma unroll
+                            for (int v = 0; v < V; ++v) r[j][v] = k.v[v] ? r[j][v] : none;
+                        }
                     }
                 }
+            } else {
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (j < per) {
+                        if (whole(j)) {
+                            Bytes k;
+                            __builtin_memcpy(&k, row.mask + first(j), V);
+#pragma unroll
+                            for (int v = 0; v < V; ++v) r[j][v] = k.v[v] ? r[j][v] : none;
+                        } else {
+                            mask_ends(j, r[j]);
+                        }
+                    }
+            }
         }
+    }
+    // a vector that the row covers only in part
+    __device__ __forceinline__ void mask_ends(int j, uint32_t (&x)[V]) const
+    {
+        const int i0 = first(j);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (i0 + v >= 0 && i0 + v < A && !row.mask[i0 + v]) x[v] = __float_as_uint(-INFINITY);
     }
 };
 
@@ -772,7 +803,7 @@ __device__ __forceinline__ void draw_from_list(Lds& lds, uint32_t C, const Weigh
 // of 4,099 in fp32: 25 us with top_k 64, with or without top_p 0.95, and 15 without
 // filters).  top_p alone needs all weights, then a histogram by weight of those that
 // can matter (30 us).
-// 512 rows of 65,536 with top_p: 100 us, the vector unit issues in 63 % of it, 75
+// 512 rows of 65,536 with top_p: 96 us, the vector unit issues in 63 % of it, 75
 // instructions for 64 logits.  A CU's registers hold one such row, so no loads run
 // under the arithmetic of another.
 // In bf16 the same takes 89 us; 1,024 rows of 32,768 take 90 and 93 (fp32).
@@ -1538,8 +1569,8 @@ __global__ __launch_bounds__(kThreads) void loss_small_kernel(const Rows R, cons
 // gradient written once.  With e = exp d and S its sum, d loss / d logit of action i is
 // e_i (k1 d_i + k0), plus g at the action taken.  For 16-bit logits d is kept in units
 // of log 2, so that its exponential is one instruction.  2,047 rows of 16,381 in bf16:
-// 40 us of kernel (3.3 TB/s read and written, 25 vector instructions for 64 logits), 64
-// with the other launches; 4,096 of 8,191 in fp32 64 us with them (4.2 TB/s).
+// 53 us with the other launches, which take 15 (64 when each load waited for the
+// conversion of the one before); 4,096 of 8,191 in fp32 64 us with them (4.2 TB/s).
 template <class T, int NW, int ITEMS>
 __global__ __launch_bounds__(NW * 64) void loss_row_kernel(const Rows R, const Batch b, const Work k)
 {
