@@ -440,8 +440,9 @@ typedef struct {
 } pictura_logits;
 
 /* How actions are drawn.  A pointer, where not NULL, holds a value for each row
- * in place of the scalar before it.  temperature >= 0 (0: the largest logit);
- * top_k <= 0, top_p >= 1 and min_p <= 0 are off, a NaN among top_ps or min_ps too. */
+ * in place of the scalar before it.  temperature >= 0 (0: the largest logit; +inf:
+ * every allowed action of finite logit weighs the same); top_k <= 0, top_p >= 1 and
+ * min_p <= 0 are off, a NaN among top_ps or min_ps too. */
 typedef struct {
     float temperature;
     int32_t top_k;
@@ -456,7 +457,8 @@ typedef struct {
 /* Draw one action per row from the random numbers uniform[rows] in [0, 1).
  * With l the allowed logits of a row, d = (l - max l) / temperature and the
  * weights w = rint(2^31 exp(d)) as whole numbers (fp32 up to the rounding, so
- * that no sum below depends on its order): order the actions by logit, largest
+ * that no sum below depends on its order; where l - max l is beyond fp32's range w
+ * is 0, at any temperature): order the actions by logit, largest
  * first, equal ones by index.  top_k keeps the first top_k of them; top_p of
  * those the shortest prefix whose weights reach max(1, floor(top_p * their sum));
  * min_p (1 at most) drops what weighs less than min_p * 2^31.  With W the sum that is left

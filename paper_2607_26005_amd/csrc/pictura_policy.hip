@@ -67,13 +67,14 @@ __device__ __forceinline__ float key_value(uint32_t k)
 // one more step rounds correctly (Markstein, "Computation of elementary functions on
 // the IBM RISC System/6000 processor", 1990).  Powers of two keep T and d where nothing
 // underflows that could show, and quotients below -200 (an exponential of zero) are
-// cut there, so that -inf gives weight 0.
+// cut there, so that -inf gives weight 0.  At T = +inf every finite difference has the
+// quotient 0: scale is 0 then, and -inf times 0 a NaN, which fmaxf drops for `least`.
 struct Weights {
     float top, scale, temp, y, least;
     __device__ __forceinline__ Weights(float top_, float t) : top(top_)
     {
-        scale = t < 0x1p-64f ? 0x1p100f : t > 0x1p64f ? 0x1p-64f : 1.0f;
-        temp = t * scale;
+        scale = t < 0x1p-64f ? 0x1p100f : t > 0x1p64f ? t == INFINITY ? 0.0f : 0x1p-64f : 1.0f;
+        temp = t == INFINITY ? 1.0f : t * scale;
         y = 1.0f / temp;
         least = -200.0f * temp;
     }

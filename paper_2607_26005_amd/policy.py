@@ -30,11 +30,12 @@ def sample_actions(logits: torch.Tensor, uniform: torch.Tensor, mask: Optional[t
     numbers give the same actions, whatever else is in the batch.
 
     mask (bool or uint8, [rows, actions] or [actions]): 0 where an action is not
-    allowed.  temperature (0: the largest logit), top_k, top_p and min_p are numbers
-    or tensors of one per row (float32; top_k int32); 0, 1 and 0 turn the filters
-    off.  A row without an allowed action, or with a NaN, gives -1 and NaN.  The
-    log-probability is that of the distribution drawn from, after temperature and
-    filters.  No gradient flows through a draw."""
+    allowed.  temperature (0: the largest logit; infinity: all allowed actions of
+    finite logit alike), top_k, top_p and min_p are numbers or tensors of one per row
+    (float32; top_k int32); 0, 1 and 0 turn the filters off.  A row without an allowed
+    action, or with a NaN, gives -1 and NaN.  The log-probability is that of the
+    distribution drawn from, after temperature and filters.  No gradient flows
+    through a draw."""
     N = logits.shape[0] if isinstance(logits, torch.Tensor) and logits.dim() == 2 else 0
     dev = logits.device if isinstance(logits, torch.Tensor) else None
     actions = torch.empty(N, dtype=torch.int64, device=dev)

@@ -1,0 +1,67 @@
+"""Draws, losses and steps at the ends of what their arguments allow."""
+import numpy as np
+import pytest
+
+from tests import policy_oracle as PO
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mods():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no HIP device")
+    from paper_2607_26005_amd import policy
+    return torch, policy
+
+
+def _draw_by_rule(torch, x, w, u, top_k=0, top_p=1.0, min_p=0.0):
+    """The drawing rule in whole numbers, given the weights (int64) of the logits."""
+    one = 1 << 31
+    cut = lambda v: (v.clamp(0.0, 1.0 - 2.0 ** -24) * float(one)).to(torch.int64)
+    share = lambda W, m: (W >> 32) * m * 2 + ((W & 0xFFFFFFFF) * m >> 31)
+    order = x.sort(dim=1, descending=True, stable=True).indices
+    ws = w.gather(1, order)
+    if top_k > 0:
+        ws[:, top_k:] = 0
+    if top_p < 1:
+        need = share(ws.sum(1, keepdim=True), cut(torch.tensor(top_p, dtype=torch.float32, device=x.device))).clamp_min(1)
+        ws = ws * (ws.cumsum(1) - ws < need)
+    ws = ws * (ws >= int(np.ceil(np.float32(min_p) * np.float32(one))))
+    c = torch.zeros_like(w).scatter_(1, order, ws).cumsum(1)
+    act = (c <= share(c[:, -1:], cut(u)[:, None])).sum(1)
+    return act, torch.zeros_like(w).scatter_(1, order, ws).gather(1, act[:, None])[:, 0], c[:, -1]
+
+
+@pytest.mark.parametrize("N, A", [(9, 1), (9, 12), (9, 40), (9, 300), (300, 300), (300, 2000), (9, 5000), (300, 5000), (4, 40000),
+                                  (4, 80000)])
+def test_an_infinite_temperature_draws_evenly(mods, N, A):
+    # every allowed action of finite logit weighs 2^31, whatever the logits: the rest of
+    # the rule (order, filters, the draw) is unchanged
+    torch, policy = mods
+    g = torch.Generator().manual_seed(A)
+    for dtype in (torch.float32, torch.bfloat16):
+        x = (torch.randn(N, A, generator=g) * 3).to(dtype).cuda()
+        mask = (torch.rand(N, A, generator=g) < 0.7).cuda()
+        mask[:, 0] = True
+        if A > 1:
+            x[:, 1] = float("-inf")
+        u = torch.rand(N, generator=g).cuda()
+        for m in (None, mask):
+            z = x.float() if m is None else x.float().masked_fill(~m, -float("inf"))
+            w = (z > -float("inf")).long() << 31
+            for how in (dict(), dict(top_k=3), dict(top_k=A // 2), dict(top_p=0.4), dict(top_k=700, top_p=0.6), dict(min_p=1.0, top_p=0.9)):
+                want, mine, total = _draw_by_rule(torch, z, w, u, **how)
+                per_row = torch.full((N,), float("inf"), device="cuda")
+                for t in (float("inf"), per_row):
+                    act, logp = policy.sample_actions(x, u, mask=m, temperature=t, **how)
+                    assert torch.equal(act, want), (dtype, how, (act != want).nonzero().flatten().tolist())
+                    # (the logarithm of the same quotient: a unit of it)
+                    ref = (mine.double() / total.double()).log()
+                    assert ((logp.double() - ref).abs() <= 2.0 ** -22 * ref.abs() + 2.0 ** -23).all(), how
+                # one such row leaves the others as they are
+                per_row[1:] = 0.8
+                act, logp = policy.sample_actions(x, u, mask=m, temperature=per_row, **how)
+                plain, plogp = policy.sample_actions(x, u, mask=m, temperature=0.8, **how)
+                assert act[0] == want[0] and torch.equal(act[1:], plain[1:]) and torch.equal(logp[1:], plogp[1:])
