@@ -62,7 +62,8 @@ uint64_t held(PyObject* state, const char* key, at::ScalarType kind, int64_t cou
     return (uint64_t)(uintptr_t)t.data_ptr();
 }
 
-// fill(params, grads, states, bits, table, steps) -> rows.  grads: a list (None: no
+// fill(params, grads, states, bits, table, steps) -> (rows, index of the first parameter
+// that took one, or -1): all that did are on that one's device.  grads: a list (None: no
 // gradient), True for the parameters' own, False for none needed; a parameter without
 // a gradient where one is needed takes no row.  states: dicts.  steps: int64, one for
 // each row.
@@ -82,7 +83,7 @@ PyObject* fill(PyObject*, PyObject* args)
             refuse("lists of different lengths");
         Row* out = static_cast<Row*>(table.buf);
         int64_t* step = static_cast<int64_t*>(steps.buf);
-        Py_ssize_t rows = 0;
+        Py_ssize_t rows = 0, first = -1;
         at::Device dev(at::kCPU);
         for (Py_ssize_t i = 0; i < count; ++i) {
             const at::Tensor& p = tensor(PyList_GET_ITEM(params, i), "parameter", i);
@@ -96,7 +97,10 @@ PyObject* fill(PyObject*, PyObject* args)
                 g = &p.grad();
                 if (!g->defined()) continue;
             }
-            if (rows == 0) dev = p.device();
+            if (rows == 0) {
+                dev = p.device();
+                first = i;
+            }
             if (p.device() != dev) refuse("parameter ", i, ": on ", p.device(), ", others on ", dev);
             if (p.layout() != at::kStrided || !p.is_contiguous() || p.is_neg()) refuse("parameter ", i, ": tensor is not contiguous");
             r.param_dtype = dtype_code(p, "parameter");
@@ -128,7 +132,7 @@ PyObject* fill(PyObject*, PyObject* args)
             step[rows] = at_step;
             out[rows++] = r;
         }
-        result = PyLong_FromSsize_t(rows);
+        result = Py_BuildValue("nn", rows, first);
     } catch (const std::exception& e) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, e.what());
     }

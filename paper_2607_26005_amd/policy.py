@@ -137,9 +137,9 @@ class AdamW(torch.optim.Optimizer):
         return len(self.state) == len(params) and all(map(operator.is_, self.state, params))
 
     def _table(self, params, grads):
-        """(rows of pictura_adamw_tensor, their steps) of the parameters that have a
-        gradient (grads: a list, or True for the parameters' own; False: of all that have
-        a state), everything checked that the kernels rely on."""
+        """(rows of pictura_adamw_tensor, their steps, the states, the device of all rows) of
+        the parameters that have a gradient (grads: a list, or True for the parameters' own;
+        False: of all that have a state), everything checked that the kernels rely on."""
         table, steps = np.empty(len(params), pictura.ADAMW_TENSOR), np.empty(len(params), np.int64)
         if self._in_order(params):
             states = list(self.state.values())
@@ -148,13 +148,15 @@ class AdamW(torch.optim.Optimizer):
         else:
             states = [self._state(p) if (p.grad if grads is True else g) is not None else None
                       for p, g in zip(params, params if grads is True else grads)]
-        if params:
-            pictura._check_device(params[0], "parameter 0", None)
         try:
-            n = _tensors.fill(params, grads, states, self.bits, table, steps)
+            n, first = _tensors.fill(params, grads, states, self.bits, table, steps)
         except ValueError as e:
             raise PicturaError(EINVAL, str(e)) from None
-        return table[:n], steps[:n], states
+        if not n:
+            return table[:0], steps[:0], states, None
+        # (of the first that takes part: parameters without a gradient may be anywhere)
+        pictura._check_device(params[first], f"parameter {first}", None)
+        return table[:n], steps[:n], states, params[first].device
 
     def step(self, closure=None, grads=None):
         if (self._optimizer_step_pre_hooks or self._optimizer_step_post_hooks or _optimizer._global_optimizer_pre_hooks
@@ -172,10 +174,9 @@ class AdamW(torch.optim.Optimizer):
         params = [p for group in self.param_groups for p in group["params"]]
         if grads is not None and len(grads) != len(params):
             raise PicturaError(EINVAL, f"grads: {len(grads)} of them for {len(params)} parameters")
-        table, steps, states = self._table(params, True if grads is None else list(grads))
-        if not len(table):
+        table, steps, states, dev = self._table(params, True if grads is None else list(grads))
+        if dev is None:
             return loss
-        dev = params[0].device
         factor = None
         if self.max_norm is not None:
             norm = torch.empty(2, dtype=torch.float32, device=dev)
@@ -212,15 +213,15 @@ class AdamW(torch.optim.Optimizer):
             params = [p for p in params if self.state.get(p)]
         if self.bits == 32:
             return [self.state[p]["exp_avg"] for p in params], [self.state[p]["exp_avg_sq"] for p in params]
-        table, _, _ = self._table(params, False)
+        table, _, _, dev = self._table(params, False)
         if out is None:
             out = tuple([torch.empty(p.numel(), dtype=torch.float32, device=p.device) for p in params] for _ in range(2))
         try:
             addresses = [_tensors.outputs(list(ts), params) for ts in out]
         except ValueError as e:
             raise PicturaError(EINVAL, str(e)) from None
-        if params:
-            pictura.pictura_adamw_moments(table, *(np.frombuffer(a, np.uint64) for a in addresses), params[0].device)
+        if dev is not None:
+            pictura.pictura_adamw_moments(table, *(np.frombuffer(a, np.uint64) for a in addresses), dev)
         return list(out[0]), list(out[1])
 
     def load_state_dict(self, state_dict):

@@ -1,0 +1,49 @@
+"""What the optimizer and the loss keep and check around their kernels: host tensors
+stand in for device ones, and a launch is recorded, not made (no GPU needed)."""
+import pytest
+import torch
+
+from paper_2607_26005_amd import pictura, policy
+
+
+@pytest.fixture
+def launches(monkeypatch):
+    """The devices of the launches that would have been made."""
+    made = []
+    monkeypatch.setattr(pictura, "_call", lambda device, fn, *args: made.append(device) or pictura.OK)
+    return made
+
+
+@pytest.fixture
+def any_device(monkeypatch):
+    monkeypatch.setattr(pictura, "_check_device", lambda t, name, ctx: None)
+
+
+def _param(*shape, device="cpu"):
+    return torch.nn.Parameter(torch.zeros(*shape, device=device))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("listed", [False, True])
+def test_a_step_refuses_host_weights_behind_a_frozen_one(launches, bits, listed):
+    # parameter 0 takes no part; parameter 1 is on the host: its address is none for a kernel
+    frozen, head = _param(4, device="meta"), _param(4)
+    head.grad = torch.ones(4)
+    opt = policy.AdamW([frozen, head], bits=bits, max_norm=1.0)
+    with pytest.raises(pictura.PicturaError, match="parameter 1: tensor on cpu, expected the HIP device"):
+        opt.step(grads=[None, torch.ones(4)] if listed else None)
+    assert launches == []
+
+
+def test_a_step_runs_on_the_device_of_the_weights_that_take_part(launches, any_device):
+    frozen, head = _param(4, device="meta"), _param(4)
+    head.grad = torch.ones(4)
+    policy.AdamW([frozen, head]).step()
+    assert launches == [head.device]
+    other = _param(4)
+    other.grad = torch.ones(4)
+    with pytest.raises(pictura.PicturaError, match="parameter 2: on meta, others on cpu"):
+        moved = _param(4, device="meta")
+        moved.grad = torch.ones(4, device="meta")
+        policy.AdamW([frozen, other, moved]).step()
+    assert launches == [head.device]
