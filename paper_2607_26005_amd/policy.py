@@ -61,7 +61,11 @@ def policy_gradient(logits, values, actions, old_logp, advantages, returns, *, o
     whose action is outside the head (-1 from sample_actions).  The loss is the mean
     by weight, or the sum over `denominator` where that is given: parts of a
     minibatch then add up.  normalize: advantages by the mean and deviation of the
-    rows given here.  value_clip > 0 needs old_values."""
+    rows given here.  value_clip > 0 needs old_values.
+
+    dlogits is cut to the logits' type here, before any factor of the caller's: in float16,
+    entries below 2^-24 are lost.  policy_loss keeps them; so does a denominator that
+    is smaller by the loss scale, with dlogits and dvalues that much larger."""
     if not isinstance(logits, torch.Tensor):
         raise PicturaError(EINVAL, f"logits: expected a torch tensor on the HIP device, got {type(logits).__name__}")
     stats = torch.empty(len(POLICY_STATS), dtype=torch.float32, device=logits.device)
@@ -76,7 +80,11 @@ def policy_gradient(logits, values, actions, old_logp, advantages, returns, *, o
 class _PolicyLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, values, args, kwargs):
-        out = policy_gradient(logits.detach(), values.detach(), *args, **kwargs)
+        # float16's range is too short for a gradient that a loss scale has yet to lift (of
+        # 65,536 rows of 12 a third of the entries would be 0): kept in float32 until then
+        x = logits.detach()
+        out = policy_gradient(x.float() if x.dtype == torch.float16 else x, values.detach(), *args, **kwargs)
+        ctx.dtype = x.dtype
         ctx.save_for_backward(out.dlogits, out.dvalues)
         ctx.mark_non_differentiable(out.stats)
         return out.stats[0].clone(), out.stats
@@ -86,12 +94,19 @@ class _PolicyLoss(torch.autograd.Function):
     def backward(ctx, dloss, _):
         dlogits, dvalues = ctx.saved_tensors
         # (the product in fp32: a loss scale may be beyond what the logits' type holds)
-        return (dlogits.float() * dloss).to(dlogits.dtype), dvalues * dloss, None, None
+        if ctx.dtype == torch.float32:
+            dx = dlogits * dloss
+        else:
+            dx = torch.empty(dlogits.shape, dtype=ctx.dtype, device=dlogits.device)
+            torch.mul(dlogits.float(), dloss, out=dx)
+        return dx, dvalues * dloss, None, None
 
 
 def policy_loss(logits, values, actions, old_logp, advantages, returns, **kwargs):
     """(loss, stats) for autograd: policy_gradient's loss, whose backward hands on the
-    gradient that the same pass computed.  Only logits and values get one."""
+    gradient that the same pass computed, times the factor that arrives (a loss scale).
+    Only logits and values get one.  Of float16 logits the gradient is kept in float32
+    for that: 8 bytes an entry between the two, with the logits' own float32 copy."""
     return _PolicyLoss.apply(logits, values, (actions, old_logp, advantages, returns), kwargs)
 
 

@@ -65,3 +65,45 @@ def test_an_infinite_temperature_draws_evenly(mods, N, A):
                 act, logp = policy.sample_actions(x, u, mask=m, temperature=per_row, **how)
                 plain, plogp = policy.sample_actions(x, u, mask=m, temperature=0.8, **how)
                 assert act[0] == want[0] and torch.equal(act[1:], plain[1:]) and torch.equal(logp[1:], plogp[1:])
+
+
+def _decisions(torch, N, A, dtype, seed):
+    """Logits and a batch of decisions, log-ratios away from the clip's edges."""
+    g = torch.Generator().manual_seed(seed)
+    rnd = lambda *s: torch.randn(*s, generator=g)
+    z = (rnd(N, A) * 1.5).to(dtype)
+    b = dict(actions=torch.randint(0, A, (N,), generator=g), advantages=rnd(N) + 0.2, values=rnd(N))
+    b["returns"] = b["values"] + rnd(N)
+    diff = rnd(N).double() * 0.3
+    r = diff.exp()
+    diff = torch.where(((r - 0.8).abs() < 1e-3) | ((r - 1.2).abs() < 1e-3), torch.full_like(diff, 0.01), diff)
+    b["old_logp"] = (z.double().log_softmax(1).gather(1, b["actions"][:, None])[:, 0] - diff).float()
+    return z, b
+
+
+def _oracle(z, b, **kw):
+    return PO.policy_loss(z.float().numpy(), *(b[k].numpy() for k in ("values", "actions", "old_logp", "advantages", "returns")), **kw)
+
+
+# what fp32 arithmetic before a rounding costs (as in tests/test_gpu_policy.py), and the
+# rounding: half a unit, in fp16 at least half of 2^-24
+ROUND = {"float32": (2.0 ** -16, 0.0), "bfloat16": (2.0 ** -16 + 2.0 ** -8, 0.0), "float16": (2.0 ** -16 + 2.0 ** -11, 2.0 ** -25)}
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+@pytest.mark.parametrize("N, A", [(300, 12), (4096, 12), (1500, 40), (700, 999), (33, 16381), (5, 80000)])
+def test_a_loss_scale_lifts_what_the_logits_type_could_not_hold(mods, N, A, dtype):
+    # the gradient under a scale is the 64-bit one times the scale, rounded once
+    torch, policy = mods
+    z, b = _decisions(torch, N, A, getattr(torch, dtype), N + A)
+    _, dz, dv = _oracle(z, b)
+    c = {k: v.cuda() for k, v in b.items()}
+    for scale in (2.0 ** 16, 2.0 ** 13, 1.0):
+        x, v = z.cuda().requires_grad_(), c["values"].clone().requires_grad_()
+        loss, stats = policy.policy_loss(x, v, c["actions"], c["old_logp"], c["advantages"], c["returns"])
+        (scale * loss).backward()
+        assert x.grad.dtype == x.dtype and stats.dtype == loss.dtype == torch.float32
+        want, got = dz * scale, x.grad.double().cpu().numpy()
+        rel, least = ROUND[dtype]
+        assert (np.abs(got - want) <= rel * np.abs(want) + 2.0 ** -20 * np.abs(want).max() + least).all()
+        assert (np.abs(v.grad.double().cpu().numpy() - dv * scale) <= 2.0 ** -20 * np.abs(dv * scale).max()).all()
