@@ -66,7 +66,8 @@ uint64_t held(PyObject* state, const char* key, at::ScalarType kind, int64_t cou
 // that took one, or -1): all that did are on that one's device.  grads: a list (None: no
 // gradient), True for the parameters' own, False for none needed; a parameter without
 // a gradient where one is needed takes no row.  states: dicts.  steps: int64, one for
-// each row.
+// each row.  Gradients mean a step, which writes the parameters of all rows: their
+// version goes up, so that autograd refuses a graph that saved them before.
 PyObject* fill(PyObject*, PyObject* args)
 {
     PyObject *params, *grads, *states;
@@ -131,6 +132,11 @@ PyObject* fill(PyObject*, PyObject* args)
             }
             step[rows] = at_step;
             out[rows++] = r;
+        }
+        for (Py_ssize_t i = first; rows > 0 && (listed || own) && i < count; ++i) {
+            const at::Tensor& p = THPVariable_Unpack(PyList_GET_ITEM(params, i));
+            const bool steps_too = listed ? PyList_GET_ITEM(grads, i) != Py_None : p.grad().defined();
+            if (steps_too && !p.is_inference()) p.unsafeGetTensorImpl()->bump_version();   // (those have none)
         }
         result = Py_BuildValue("nn", rows, first);
     } catch (const std::exception& e) {

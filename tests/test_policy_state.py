@@ -47,3 +47,25 @@ def test_a_step_runs_on_the_device_of_the_weights_that_take_part(launches, any_d
         moved.grad = torch.ones(4, device="meta")
         policy.AdamW([frozen, other, moved]).step()
     assert launches == [head.device]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_counts_as_a_change_of_the_weights(launches, any_device, bits):
+    # as torch's optimizers: a graph that saved the weights before the step is refused after it
+    w, still, x = _param(3), _param(3), torch.ones(3, requires_grad=True)
+    opt = policy.AdamW([still, w], bits=bits)
+    loss = (w * x).sum()
+    loss.backward(retain_graph=True)
+    before = w._version
+    opt.step()
+    assert (w._version, still._version) == (before + 1, 0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    opt.step(grads=[torch.ones(3), None])
+    assert (w._version, still._version) == (before + 1, 1)
+    opt.moments()
+    assert (w._version, still._version) == (before + 1, 1)
+    with torch.inference_mode():
+        p = torch.nn.Parameter(torch.zeros(3))
+    policy.AdamW([p]).step(grads=[torch.ones(3)])   # (such a tensor has no version)
+    assert len(launches) == 2 + (bits == 8) + 1
