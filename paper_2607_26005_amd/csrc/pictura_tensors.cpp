@@ -63,7 +63,8 @@ uint64_t held(PyObject* state, const char* key, at::ScalarType kind, int64_t cou
 }
 
 // fill(params, grads, states, bits, table, steps) -> (rows, index of the first parameter
-// that took one, or -1): all that did are on that one's device.  grads: a list (None: no
+// that took one, or -1): all that did are on that one's device.  None: a state that a
+// row needs has not begun (no "step").  grads: a list (None: no
 // gradient), True for the parameters' own, False for none needed; a parameter without
 // a gradient where one is needed takes no row.  states: dicts.  steps: int64, one for
 // each row.  Gradients mean a step, which writes the parameters of all rows: their
@@ -85,6 +86,7 @@ PyObject* fill(PyObject*, PyObject* args)
         Row* out = static_cast<Row*>(table.buf);
         int64_t* step = static_cast<int64_t*>(steps.buf);
         Py_ssize_t rows = 0, first = -1;
+        bool begun = true;
         at::Device dev(at::kCPU);
         for (Py_ssize_t i = 0; i < count; ++i) {
             const at::Tensor& p = tensor(PyList_GET_ITEM(params, i), "parameter", i);
@@ -116,6 +118,11 @@ PyObject* fill(PyObject*, PyObject* args)
             }
             PyObject* s = PyList_GET_ITEM(states, i);
             if (!PyDict_Check(s)) refuse("state of parameter ", i, ": no state");
+            PyObject* k = PyDict_GetItemString(s, "step");
+            if (!k) {
+                begun = false;
+                break;
+            }
             const bool small = bits == 8;
             r.exp_avg = held(s, "exp_avg", small ? at::kChar : at::kFloat, r.n, dev, i);
             r.exp_avg_sq = held(s, "exp_avg_sq", small ? at::kByte : at::kFloat, r.n, dev, i);
@@ -124,8 +131,7 @@ PyObject* fill(PyObject*, PyObject* args)
                 r.exp_avg_scale = held(s, "exp_avg_scale", at::kFloat, blocks, dev, i);
                 r.exp_avg_sq_scale = held(s, "exp_avg_sq_scale", at::kFloat, blocks, dev, i);
             }
-            PyObject* k = PyDict_GetItemString(s, "step");
-            const long long at_step = k && PyLong_Check(k) ? PyLong_AsLongLong(k) : -1;
+            const long long at_step = PyLong_Check(k) ? PyLong_AsLongLong(k) : -1;
             if (at_step < 0) {
                 PyErr_Clear();
                 refuse("state of parameter ", i, ": step is not a whole number");
@@ -133,12 +139,12 @@ PyObject* fill(PyObject*, PyObject* args)
             step[rows] = at_step;
             out[rows++] = r;
         }
-        for (Py_ssize_t i = first; rows > 0 && (listed || own) && i < count; ++i) {
+        for (Py_ssize_t i = first; begun && rows > 0 && (listed || own) && i < count; ++i) {
             const at::Tensor& p = THPVariable_Unpack(PyList_GET_ITEM(params, i));
             const bool steps_too = listed ? PyList_GET_ITEM(grads, i) != Py_None : p.grad().defined();
             if (steps_too && !p.is_inference()) p.unsafeGetTensorImpl()->bump_version();   // (those have none)
         }
-        result = Py_BuildValue("nn", rows, first);
+        result = begun ? Py_BuildValue("nn", rows, first) : Py_NewRef(Py_None);
     } catch (const std::exception& e) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, e.what());
     }

@@ -156,15 +156,17 @@ class AdamW(torch.optim.Optimizer):
         the parameters that have a gradient (grads: a list, or True for the parameters' own;
         False: of all that have a state), everything checked that the kernels rely on."""
         table, steps = np.empty(len(params), pictura.ADAMW_TENSOR), np.empty(len(params), np.int64)
-        if self._in_order(params):
-            states = list(self.state.values())
-        elif grads is False:
-            states = [self.state[p] for p in params]
-        else:
-            states = [self._state(p) if (p.grad if grads is True else g) is not None else None
-                      for p, g in zip(params, params if grads is True else grads)]
         try:
-            n, first = _tensors.fill(params, grads, states, self.bits, table, steps)
+            states = list(self.state.values()) if self._in_order(params) else None
+            got = _tensors.fill(params, grads, states, self.bits, table, steps) if states is not None else None
+            if got is None:   # (states that have not begun may be there, empty: to read one makes it)
+                if grads is False:
+                    states = [self.state[p] for p in params]
+                else:
+                    states = [self._state(p) if (p.grad if grads is True else g) is not None else None
+                              for p, g in zip(params, params if grads is True else grads)]
+                got = _tensors.fill(params, grads, states, self.bits, table, steps)
+            n, first = got
         except ValueError as e:
             raise PicturaError(EINVAL, str(e)) from None
         if not n:
@@ -224,8 +226,10 @@ class AdamW(torch.optim.Optimizer):
         lists of float32 tensors; with bits=8 what the codes stand for, written to
         the two lists of contiguous float32 tensors `out` where that is given."""
         params = [p for group in self.param_groups for p in group["params"]]
-        if not self._in_order(params) or not all(self.state.values()):
-            params = [p for p in params if self.state.get(p)]
+        if self._in_order(params):
+            params = [p for p, s in zip(params, self.state.values()) if "step" in s]
+        else:
+            params = [p for p in params if "step" in self.state.get(p, ())]
         if self.bits == 32:
             return [self.state[p]["exp_avg"] for p in params], [self.state[p]["exp_avg_sq"] for p in params]
         table, _, _, dev = self._table(params, False)

@@ -69,3 +69,20 @@ def test_a_step_counts_as_a_change_of_the_weights(launches, any_device, bits):
         p = torch.nn.Parameter(torch.zeros(3))
     policy.AdamW([p]).step(grads=[torch.ones(3)])   # (such a tensor has no version)
     assert len(launches) == 2 + (bits == 8) + 1
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("kept", [{}, {"mine": 1}])
+def test_a_state_that_was_read_before_the_first_step_is_begun_by_it(launches, any_device, bits, kept):
+    ps = [_param(3), _param(300)]
+    opt = policy.AdamW(ps, bits=bits)
+    for p in ps:
+        opt.state[p].update(kept)                            # reading makes an empty state
+    assert opt.moments() == ([], [])
+    opt.step(grads=[torch.ones(3), None])
+    assert opt.state[ps[0]]["step"] == 1 and opt.state[ps[0]]["exp_avg"].numel() == 3 and opt.state[ps[1]] == kept
+    assert [len(m) for m in opt.moments()] == [1, 1]
+    opt.step(grads=[torch.ones(3), torch.ones(300)])
+    assert [opt.state[p]["step"] for p in ps] == [2, 1]
+    assert [len(m) for m in opt.moments()] == [2, 2]
+    assert all(opt.state[p].items() >= kept.items() for p in ps)
