@@ -1856,9 +1856,13 @@ void launch_loss(const Rows& R, const Batch& b, const Work& k, hipStream_t s)
     const dim3 grid((unsigned)loss_blocks(R.rows, R.actions)), block(kThreads);
     hipLaunchKernelGGL(loss_moments_kernel, dim3((unsigned)k.parts), block, 0, s, b, R.rows, R.actions, k.part, k.done);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, R, b, k); };
+    // loss_thread_kernel and loss_row_kernel multiply by 1 / T, which below 2^-128 is
+    // infinite, and by which a gradient may leave fp32's range before the weight of an action
+    // makes it 0.  The other two divide, last: they take the temperatures that small.
+    const bool divide = b.temperature < 0x1p-64f;
     if (R.actions > 64) {
         const int slots = slots_of<T>(R);
-        if (slots <= kMostSlots)
+        if (slots <= kMostSlots && !divide)
             with_shape(row_shape(slots, R.rows), [&](auto w, auto i) {
                 constexpr int W = decltype(w)::value, I = decltype(i)::value;
                 hipLaunchKernelGGL((loss_row_kernel<T, W, I>), grid, dim3(W * 64), 0, s, R, b, k);
@@ -1866,8 +1870,8 @@ void launch_loss(const Rows& R, const Batch& b, const Work& k, hipStream_t s)
         else
             hipLaunchKernelGGL(loss_long_kernel<T>, grid, dim3(kLongWaves * 64), 0, s, R, b, k);
         hipLaunchKernelGGL(loss_stats_kernel, dim3(1), block, 0, s, b, k, (int64_t)grid.x);
-    } else if (R.actions <= 16) go(loss_thread_kernel<T>);
-    else if (group_lanes(R.actions) == 32) go(loss_small_kernel<T, 32>);
+    } else if (R.actions <= 16 && !divide) go(loss_thread_kernel<T>);
+    else if (group_lanes(R.actions) <= 32) go(loss_small_kernel<T, 32>);
     else go(loss_small_kernel<T, 64>);
 }
 

@@ -107,3 +107,32 @@ def test_a_loss_scale_lifts_what_the_logits_type_could_not_hold(mods, N, A, dtyp
         rel, least = ROUND[dtype]
         assert (np.abs(got - want) <= rel * np.abs(want) + 2.0 ** -20 * np.abs(want).max() + least).all()
         assert (np.abs(v.grad.double().cpu().numpy() - dv * scale) <= 2.0 ** -20 * np.abs(dv * scale).max()).all()
+
+
+@pytest.mark.parametrize("A", [1, 5, 12, 40, 300, 5000, 80000])
+@pytest.mark.parametrize("exponent", [-140, -127, -126, -90, -60])
+def test_loss_at_the_smallest_temperatures(mods, A, exponent):
+    # the softmax is one at the largest logit and zero elsewhere; in fp32 as in 64 bits
+    # no gradient is left of it, the ratio of any other action is 0, values learn as ever.
+    # (Row 0 may have drawn another action, of log-probability (z - top) / T: a number beyond
+    # where the oracle's exponential, and so its logarithm, has one.)
+    torch, policy = mods
+    N, T = 9, 2.0 ** exponent
+    z, b = _decisions(torch, N, A, torch.float32, A)
+    b["actions"][1:] = z[1:].argmax(1)
+    b["old_logp"] = torch.randn(N, generator=torch.Generator().manual_seed(1)) * 0.3
+    stats, dz, dv = _oracle(z, b, temperature=T, entropy_coef=0.3)
+    assert (dz == 0).all() and np.isfinite(stats[[0, 1, 2, 3, 5]]).all()
+    c = {k: v.cuda() for k, v in b.items()}
+    out = policy.policy_gradient(z.cuda(), c["values"], c["actions"], c["old_logp"], c["advantages"], c["returns"], temperature=T,
+                                 entropy_coef=0.3)
+    got = out.stats.cpu().double().numpy()
+    rest = [0, 1, 2, 3, 5]
+    assert np.abs(got[rest] - stats[rest]).max() <= 2.0 ** -16 * max(1.0, np.abs(stats[rest]).max()), (got, stats)
+    top = z.gather(1, b["actions"][:, None])[:, 0].double() - z.max(1).values.double()
+    diff = (top / T - b["old_logp"].double()).numpy()
+    with np.errstate(over="ignore"):
+        kl = np.where(np.abs(diff.astype(np.float32)) < np.inf, np.expm1(diff) - diff, np.inf).mean()
+    assert got[4] == kl if kl == np.inf else abs(got[4] - kl) <= 2.0 ** -16 * max(1.0, kl), (got[4], kl)
+    assert (out.dlogits == 0).all(), out.dlogits[out.dlogits != 0]
+    assert (np.abs(out.dvalues.cpu().double().numpy() - dv) <= 2.0 ** -20 * np.abs(dv).max()).all()
