@@ -510,7 +510,8 @@ pictura_status pictura_policy_loss_workspace(int64_t rows, int32_t actions, uint
  * mean of (r - 1) - log r, [5] the weight of rows with r outside 1 +- clip.
  * dlogits (the logits' type, dlogits_stride elements between rows) and dvalues
  * [rows] receive the gradient of the mean loss; it is 0 at actions of probability
- * zero.  If no row counts, all are 0.  Sums are taken in a fixed order.
+ * zero.  If no row counts, or the weights add up to 0 and there is no denominator, all are
+ * 0.  Sums are taken in a fixed order.
  * workspace: device memory, 256-byte aligned, in use until the call's work on the
  * stream is done.  dlogits may be the logits' own memory (same stride).  EINVAL: a null or
  * misaligned pointer, a value out of range, or a workspace too small. */

@@ -1346,8 +1346,9 @@ __device__ __forceinline__ Shared3 loss_shared(const Batch& b, const double* __r
 #pragma unroll
     for (int k = 0; k < 3; ++k) s[k] = wave_sum(s[k]);
     Shared3 o;
+    // (weights of both signs may add up to 0: no mean, but parts of a minibatch still count)
     const double den = b.denominator != 0.0f ? (double)b.denominator : s[0];
-    o.inv = s[0] != 0.0 ? (float)(1.0 / den) : 0.0f;
+    o.inv = den != 0.0 ? (float)(1.0 / den) : 0.0f;
     o.mean = 0.0f;
     o.rstd = 1.0f;
     if (b.normalize && s[0] != 0.0) {

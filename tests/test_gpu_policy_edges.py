@@ -136,3 +136,25 @@ def test_loss_at_the_smallest_temperatures(mods, A, exponent):
     assert got[4] == kl if kl == np.inf else abs(got[4] - kl) <= 2.0 ** -16 * max(1.0, kl), (got[4], kl)
     assert (out.dlogits == 0).all(), out.dlogits[out.dlogits != 0]
     assert (np.abs(out.dvalues.cpu().double().numpy() - dv) <= 2.0 ** -20 * np.abs(dv).max()).all()
+
+
+@pytest.mark.parametrize("A", [12, 40, 300, 80000])
+def test_a_part_whose_weights_cancel_still_counts(mods, A):
+    # weights of both signs that add up to 0 in one part of a minibatch: by the denominator
+    # of the whole its rows count like any others; without one there is no mean to take
+    torch, policy = mods
+    N = 6
+    z, b = _decisions(torch, N, A, torch.float32, 2 * A)
+    w = torch.tensor([0.5, -0.5, 1.25, -1.0, -0.25, 0.0])
+    c = {k: v.cuda() for k, v in b.items()}
+    run = lambda **kw: policy.policy_gradient(z.cuda(), c["values"], c["actions"], c["old_logp"], c["advantages"], c["returns"],
+                                              weights=w.cuda(), **kw)
+    stats, dz, dv = _oracle(z, b, weights=w.numpy(), denominator=8.0)
+    out = run(denominator=8.0)
+    assert np.abs(dz).max() > 1e-3
+    assert np.abs(out.stats.cpu().double().numpy() - stats).max() <= 2.0 ** -16
+    got = out.dlogits.cpu().double().numpy()
+    assert (np.abs(got - dz) <= 2.0 ** -16 * np.abs(dz) + 2.0 ** -20 * np.abs(dz).max()).all()
+    assert (np.abs(out.dvalues.cpu().double().numpy() - dv) <= 2.0 ** -20 * np.abs(dv).max()).all()
+    out = run()
+    assert (out.stats == 0).all() and (out.dlogits == 0).all() and (out.dvalues == 0).all()
