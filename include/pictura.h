@@ -562,7 +562,10 @@ pictura_status pictura_grad_norm(const pictura_adamw_tensor* tensors, int32_t co
  * the update uses m and v before they are cut: a block's scale is its largest
  * magnitude (0 if that is below 2^-90), m's code the sign and rint(127 sqrt(|m| / s)),
  * v's rint(255 (v / s)^(1/4)), at least 1 where v > 0.  A NaN makes its block's scale
- * NaN.  EINVAL: a null pointer where n > 0, a pointer not aligned to its elements,
+ * NaN.  With 8 bits and eps from 2^-40 on, the update's root and quotient are off by up to
+ * a unit of fp32 each.  A block's second moments below 2^-90 count as zero in the next
+ * step, where its first ones may not: gradients below 2^-40 take an eps above them.
+ * EINVAL: a null pointer where n > 0, a pointer not aligned to its elements,
  * n < 0, step < 1, betas outside [0, 1), or bits other than 32 and 8. */
 pictura_status pictura_adamw_step(const pictura_adamw* how, const pictura_adamw_tensor* tensors, int32_t count,
                                   void* stream);

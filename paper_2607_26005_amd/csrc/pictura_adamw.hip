@@ -23,6 +23,7 @@ namespace pictura {
 constexpr int kThreads = 256;
 constexpr int kChunk = 4096;                     // elements of one workgroup
 constexpr int kBlk = PICTURA_ADAMW_BLOCK;
+constexpr float kLeastEps = 0x1p-40f;            // from it on the hardware's root and reciprocal serve
 constexpr float kTiny = 0x1p-90f;                // below it a block's moments count as zero: 1 / scale stays finite
 static_assert(kChunk % kBlk == 0, "blocks do not straddle workgroups");
 
@@ -138,6 +139,8 @@ __device__ __forceinline__ void store4(void* p, int type, int64_t i, const float
 // m and v after the gradient g, and the parameter.  kFast: with the hardware's root
 // and reciprocal (a unit off each, where the correctly rounded ones take some 25
 // instructions): the 8-bit step is bound by instructions, the 32-bit one by memory.
+// Both instructions take subnormal numbers for 0, so the root is wrong below 2^-63 and
+// the reciprocal infinite: with eps from kLeastEps on, neither shows in m / den.
 template <bool kFast>
 __device__ __forceinline__ float adamw(const StepFactors& f, float p, float g, float& m, float& v)
 {
@@ -275,6 +278,7 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x)
 // are decoded, stepped and scaled again without leaving the registers.  Codes come from
 // the hardware's reciprocal and root, and from exact arithmetic where those leave the
 // rounding open.
+template <bool kFast>
 __global__ __launch_bounds__(kThreads) void adamw8_kernel(const Args<Step8Arg> a, const StepFactors f)
 {
     const Step8Arg t = a.t[tensor_of(a, (int)blockIdx.x)];
@@ -324,7 +328,7 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const Args<Step8Arg> a
         for (int k = 0; k < 4; ++k) {
             m[k] = m_value(qm.v[k], um);
             v[k] = v_value(qv.v[k], uv);
-            p[k] = adamw<true>(f, p[k], g[k] * gf, m[k], v[k]);
+            p[k] = adamw<kFast>(f, p[k], g[k] * gf, m[k], v[k]);
             mm = max(mm, __float_as_uint(fabsf(m[k])));
             vm = max(vm, __float_as_uint(fabsf(v[k])));
         }
@@ -626,7 +630,8 @@ pictura_status pictura_adamw_step(const pictura_adamw* how, const pictura_adamw_
             [&](const Args<StepArg>& a, unsigned blocks) {
                 hipLaunchKernelGGL(adamw32_kernel, dim3(blocks), dim3(kThreads), 0, s, a, f);
             });
-    else
+    else {
+        const auto kernel = f.eps >= kLeastEps ? adamw8_kernel<true> : adamw8_kernel<false>;
         for_launches<Step8Arg>(
             tensors, count, kChunk,
             [&](Step8Arg& t, int32_t k, int64_t at) {
@@ -634,8 +639,9 @@ pictura_status pictura_adamw_step(const pictura_adamw* how, const pictura_adamw_
                 fill_scales(t, tensors[k], at);
             },
             [&](const Args<Step8Arg>& a, unsigned blocks) {
-                hipLaunchKernelGGL(adamw8_kernel, dim3(blocks), dim3(kThreads), 0, s, a, f);
+                hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, s, a, f);
             });
+    }
     return launched();
 }
 

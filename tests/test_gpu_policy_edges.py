@@ -158,3 +158,24 @@ def test_a_part_whose_weights_cancel_still_counts(mods, A):
     assert (np.abs(out.dvalues.cpu().double().numpy() - dv) <= 2.0 ** -20 * np.abs(dv).max()).all()
     out = run()
     assert (out.stats == 0).all() and (out.dlogits == 0).all() and (out.dvalues == 0).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [0.0, 2.0 ** -140, 1e-30, 1e-20, 1e-15])
+def test_steps_with_next_to_no_epsilon(mods, bits, eps):
+    # v of gradients down to 1e-19 is 1e-40, a number of 17 bits in fp32: its root is off by
+    # 2^-18 of itself, and with it the update
+    torch, policy = mods
+    how = dict(lr=1e-3, betas=(0.9, 0.99), weight_decay=0.0)
+    g = torch.Generator().manual_seed(0)
+    n = 5000
+    sizes = 10.0 ** (torch.rand(n, generator=g) * 18 - 19)
+    grad = sizes * torch.where(torch.rand(n, generator=g) < 0.5, -1.0, 1.0)
+    if eps > 0:
+        grad[256:700] = 0.0                                  # whole blocks of nothing: 0 / eps
+    p = torch.nn.Parameter(torch.zeros(n).cuda())
+    policy.AdamW([p], **how, eps=eps, bits=bits).step(grads=[grad.cuda()])
+    eps32 = float(np.float32(eps))
+    want = PO.adamw(np.zeros(n), grad.double().numpy(), np.zeros(n), np.zeros(n), 1, how["lr"], how["betas"], eps32, 0.0)[0]
+    got = p.detach().double().cpu().numpy()
+    assert (np.abs(got - want) <= 2.0 ** -16 * how["lr"]).all(), np.abs(got - want).max() / how["lr"]
