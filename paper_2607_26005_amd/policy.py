@@ -132,6 +132,10 @@ class AdamW(torch.optim.Optimizer):
         self.grad_norm = None
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
 
+    def __getstate__(self):
+        # (what torch's own keeps of an optimizer in copies and pickles, and what this one adds)
+        return dict(super().__getstate__(), bits=self.bits, max_norm=self.max_norm, grad_norm=self.grad_norm)
+
     def _state(self, p):
         s = self.state[p]
         if "step" not in s:

@@ -1,5 +1,8 @@
 """What the optimizer and the loss keep and check around their kernels: host tensors
 stand in for device ones, and a launch is recorded, not made (no GPU needed)."""
+import copy
+import pickle
+
 import pytest
 import torch
 
@@ -86,3 +89,21 @@ def test_a_state_that_was_read_before_the_first_step_is_begun_by_it(launches, an
     assert [opt.state[p]["step"] for p in ps] == [2, 1]
     assert [len(m) for m in opt.moments()] == [2, 2]
     assert all(opt.state[p].items() >= kept.items() for p in ps)
+
+
+@pytest.mark.parametrize("bits, max_norm", [(32, None), (8, 0.5)])
+@pytest.mark.parametrize("how", [copy.deepcopy, lambda o: pickle.loads(pickle.dumps(o))], ids=["copy", "pickle"])
+@pytest.mark.parametrize("stepped", [False, True])
+def test_copies_of_an_optimizer_step_as_it_does(launches, any_device, bits, max_norm, how, stepped):
+    opt = policy.AdamW([_param(300)], lr=0.25, bits=bits, max_norm=max_norm)
+    if stepped:
+        opt.step(grads=[torch.ones(300)])
+    other = how(opt)
+    assert (other.bits, other.max_norm, other.param_groups[0]["lr"]) == (bits, max_norm, 0.25)
+    assert (other.grad_norm is None) == (opt.grad_norm is None)
+    del launches[:]
+    other.step(grads=[torch.ones(300)])
+    q = other.param_groups[0]["params"][0]
+    assert other.state[q]["step"] == 1 + stepped and opt.param_groups[0]["params"][0] is not q
+    assert other.state[q]["exp_avg"].dtype == (torch.float32 if bits == 32 else torch.int8)
+    assert len(launches) == 1 + (max_norm is not None)
