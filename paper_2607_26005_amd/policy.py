@@ -247,10 +247,18 @@ class AdamW(torch.optim.Optimizer):
             pictura.pictura_adamw_moments(table, *(np.frombuffer(a, np.uint64) for a in addresses), dev)
         return list(out[0]), list(out[1])
 
+    def state_dict(self):
+        """As torch's, with max_norm beside the groups."""
+        held = super().state_dict()
+        held["max_norm"] = self.max_norm
+        return held
+
     def load_state_dict(self, state_dict):
         """As torch's, with the moments' own types kept (torch would make them the
-        weights')."""
+        weights'), and with max_norm, as the rates of the groups, taken from the
+        dictionary where that has it."""
         super().load_state_dict(state_dict)
+        self.max_norm = state_dict.get("max_norm", self.max_norm)
         at = {}
         for mine, theirs in zip(self.param_groups, state_dict["param_groups"]):
             at.update(zip(theirs["params"], mine["params"]))

@@ -107,3 +107,20 @@ def test_copies_of_an_optimizer_step_as_it_does(launches, any_device, bits, max_
     assert other.state[q]["step"] == 1 + stepped and opt.param_groups[0]["params"][0] is not q
     assert other.state[q]["exp_avg"].dtype == (torch.float32 if bits == 32 else torch.int8)
     assert len(launches) == 1 + (max_norm is not None)
+
+
+def test_a_checkpoint_keeps_the_clipping_norm(launches, any_device):
+    opt = policy.AdamW([_param(300)], lr=0.25, max_norm=0.5)
+    opt.step(grads=[torch.ones(300)])
+    held = opt.state_dict()
+    for max_norm in (None, 2.0):
+        other = policy.AdamW([_param(300)], max_norm=max_norm)
+        other.load_state_dict(copy.deepcopy(held))
+        assert other.max_norm == 0.5 and other.param_groups[0]["lr"] == 0.25
+        # one that does not have it (torch's own, or an earlier one) leaves what the optimizer was made with
+        other = policy.AdamW([_param(300)], max_norm=max_norm)
+        other.load_state_dict({k: held[k] for k in ("state", "param_groups")})
+        assert other.max_norm == max_norm
+    off = policy.AdamW([_param(300)], max_norm=2.0)
+    off.load_state_dict(policy.AdamW([_param(300)]).state_dict())
+    assert off.max_norm is None
