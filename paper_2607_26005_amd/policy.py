@@ -257,7 +257,16 @@ class AdamW(torch.optim.Optimizer):
         """As torch's, with the moments' own types kept (torch would make them the
         weights'), and with max_norm, as the rates of the groups, taken from the
         dictionary where that has it."""
-        super().load_state_dict(state_dict)
+        made = []   # what the hooks before this one make of it; the hooks after see the result
+        hooks = (self.register_load_state_dict_pre_hook(lambda _, held: made.append(held)),
+                 self.register_load_state_dict_post_hook(lambda _: self._take(made[0]), prepend=True))
+        try:
+            super().load_state_dict(state_dict)
+        finally:
+            for hook in hooks:
+                hook.remove()
+
+    def _take(self, state_dict):
         self.max_norm = state_dict.get("max_norm", self.max_norm)
         at = {}
         for mine, theirs in zip(self.param_groups, state_dict["param_groups"]):

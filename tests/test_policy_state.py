@@ -124,3 +124,30 @@ def test_a_checkpoint_keeps_the_clipping_norm(launches, any_device):
     off = policy.AdamW([_param(300)], max_norm=2.0)
     off.load_state_dict(policy.AdamW([_param(300)]).state_dict())
     assert off.max_norm is None
+
+
+def test_hooks_of_a_load_are_heard(launches, any_device):
+    source, target = (policy.AdamW([torch.nn.Parameter(torch.zeros(4, dtype=torch.bfloat16))]) for _ in range(2))
+    q = target.param_groups[0]["params"][0]
+    source.step(grads=[torch.ones(4)])
+    held = source.state_dict()
+    precise = torch.full((4,), 1 + 2.0 ** -20)               # (no number in bfloat16, which torch would make it)
+
+    def before(opt, d):
+        return dict(d, state={0: dict(d["state"][0], exp_avg=precise, step=7)})
+
+    def after(opt):
+        assert torch.equal(opt.state[q]["exp_avg"], precise) and opt.state[q]["step"] == 7
+        opt.state[q]["step"] = 9
+
+    hooks = target.register_load_state_dict_pre_hook(before), target.register_load_state_dict_post_hook(after)
+    target.load_state_dict(held)
+    assert target.state[q]["step"] == 9 and torch.equal(target.state[q]["exp_avg"], precise)
+    for h in hooks:
+        h.remove()
+    assert not target._optimizer_load_state_dict_pre_hooks and not target._optimizer_load_state_dict_post_hooks
+    target.load_state_dict(held)
+    assert target.state[q]["step"] == 1 and torch.equal(target.state[q]["exp_avg"], torch.zeros(4))
+    with pytest.raises(ValueError):
+        target.load_state_dict({"state": {}, "param_groups": []})
+    assert not target._optimizer_load_state_dict_pre_hooks and not target._optimizer_load_state_dict_post_hooks
