@@ -151,3 +151,36 @@ def test_hooks_of_a_load_are_heard(launches, any_device):
     with pytest.raises(ValueError):
         target.load_state_dict({"state": {}, "param_groups": []})
     assert not target._optimizer_load_state_dict_pre_hooks and not target._optimizer_load_state_dict_post_hooks
+
+
+@pytest.mark.parametrize("name", ["temperature", "top_k", "top_p", "min_p"])
+@pytest.mark.parametrize("v", [10 ** 400, -10 ** 400])
+def test_sampling_refuses_numbers_beyond_its_types(launches, any_device, name, v):
+    n, a = 3, 5
+    if name == "top_k":
+        policy.sample_actions(torch.zeros(n, a), torch.zeros(n), top_k=v)   # any whole number: cut to what counts
+        assert len(launches) == 1
+        return
+    with pytest.raises(pictura.PicturaError, match=name) as e:
+        policy.sample_actions(torch.zeros(n, a), torch.zeros(n), **{name: v})
+    assert e.value.status == pictura.EINVAL and launches == []
+
+
+@pytest.mark.parametrize("name", ["temperature", "clip", "value_clip", "value_coef", "entropy_coef", "denominator"])
+@pytest.mark.parametrize("v", [10 ** 400, "much", None])
+def test_loss_refuses_numbers_beyond_its_types(launches, any_device, name, v):
+    n = 3
+    z, i = torch.zeros(n), torch.zeros(n, dtype=torch.int64)
+    with pytest.raises(pictura.PicturaError, match=f"{name}: ") as e:
+        policy.policy_gradient(torch.zeros(n, 5), z, i, z, z, z, **{name: v})
+    assert e.value.status == pictura.EINVAL and launches == []
+
+
+@pytest.mark.parametrize("name", ["lr", "eps", "weight_decay"])
+@pytest.mark.parametrize("v", [10 ** 400, "much"])
+def test_steps_refuse_numbers_beyond_their_types(launches, any_device, name, v):
+    opt = policy.AdamW([_param(3)])
+    opt.param_groups[0][name] = v
+    with pytest.raises(pictura.PicturaError, match=f"{name}: ") as e:
+        opt.step(grads=[torch.ones(3)])
+    assert e.value.status == pictura.EINVAL and launches == []
