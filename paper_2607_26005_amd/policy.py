@@ -217,9 +217,9 @@ class AdamW(torch.optim.Optimizer):
                 stop = begin + int(same.argmax()) if same.any() else end
                 pictura.pictura_adamw_step(table[begin:stop], dev, group["lr"], group["betas"], group["eps"],
                                            group["weight_decay"], int(steps[begin]) + 1, self.bits, factor)
+                for i in got[begin:stop]:   # (also where a later call is refused: these have moved)
+                    states[i]["step"] += 1
                 begin = stop
-        for i in got:
-            states[i]["step"] += 1
         return loss
 
     _hooked_step = torch.optim.Optimizer.profile_hook_step(_step)

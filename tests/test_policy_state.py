@@ -184,3 +184,16 @@ def test_steps_refuse_numbers_beyond_their_types(launches, any_device, name, v):
     with pytest.raises(pictura.PicturaError, match=f"{name}: ") as e:
         opt.step(grads=[torch.ones(3)])
     assert e.value.status == pictura.EINVAL and launches == []
+
+
+def test_groups_that_moved_before_a_refused_one_have_counted(launches, any_device, monkeypatch):
+    ps = [_param(3) for _ in range(4)]
+    opt = policy.AdamW([dict(params=ps[:2]), dict(params=ps[2:])])
+    opt.step(grads=[torch.ones(3)] * 4)
+    opt.param_groups[1]["betas"] = (0.9, 2.0)
+    call = pictura._call                                     # (the entry refuses such a beta before it launches)
+    monkeypatch.setattr(pictura, "_call", lambda device, fn, how, *args: pictura.EINVAL
+                        if pictura._ADAMW_PACK.unpack(how)[2] == 2.0 else call(device, fn, how, *args))
+    with pytest.raises(pictura.PicturaError):
+        opt.step(grads=[torch.ones(3), None, torch.ones(3), torch.ones(3)])
+    assert [opt.state[p]["step"] for p in ps] == [2, 1, 1, 1] and len(launches) == 3
