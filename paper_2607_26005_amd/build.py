@@ -54,12 +54,17 @@ def _tensors_command(out: str) -> list:
 
 
 def build(verbose: bool = False) -> str:
+    """Builds both.  The helper alone needs a host compiler and torch's C++ headers: without
+    them this raises once the library is there, with which the renderer and the encoder run."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    objs = []
-    tensors = _tensors_command(TENSORS + ".tmp")
-    if verbose:
-        print(" ".join(tensors))
-    procs = [subprocess.Popen(tensors)]
+    objs, procs = [], []
+    try:
+        tensors = _tensors_command(TENSORS + ".tmp")
+        if verbose:
+            print(" ".join(tensors))
+        helper = subprocess.Popen(tensors)
+    except (ImportError, OSError) as e:
+        helper, missing = None, e
     for src, oname, extra in UNITS:
         obj = os.path.join(CSRC, oname)
         cmd = [hipcc, *HIPCC_FLAGS, *extra, "-I", INCLUDE, "-c", os.path.join(CSRC, src), "-o", obj]
@@ -70,12 +75,15 @@ def build(verbose: bool = False) -> str:
     for p in procs:
         if p.wait() != 0:
             raise RuntimeError(f"{p.args[0]} failed")
-    os.replace(TENSORS + ".tmp", TENSORS)
     tmp = LIB + ".tmp"
     subprocess.check_call([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-Wl,--no-undefined", "-o", tmp, *objs])
     os.replace(tmp, LIB)
     for o in objs:
         os.remove(o)
+    if helper is None or helper.wait() != 0:
+        raise RuntimeError(f"{LIB} is built; {TENSORS}, which the policy's operators need, is not: " +
+                           (str(missing) if helper is None else f"{tensors[0]} failed"))
+    os.replace(TENSORS + ".tmp", TENSORS)
     return LIB
 
 
