@@ -502,18 +502,17 @@ def _call(device, fn, *args) -> int:
         return fn(*args, torch.cuda.current_stream().cuda_stream)
 
 
-def _pack(packer, names, numbers, *values) -> bytes:
-    """The struct of these values; a number that does not fit it is refused by its name
-    (looked for only then)."""
-    try:
-        return packer.pack(*values)
-    except (struct.error, OverflowError, TypeError) as e:
-        for name, v in zip(names, numbers):
-            try:
-                struct.pack("f" if packer is not _ADAMW_PACK else "d", v)
-            except (struct.error, OverflowError, TypeError):
-                raise PicturaError(EINVAL, f"{name}: {type(v).__name__}, expected a number within range") from None
-        raise PicturaError(EINVAL, str(e)) from None
+_NO_NUMBER = (struct.error, OverflowError, TypeError)   # what packing raises
+
+
+def _refuse(kind: str, names, numbers, e) -> None:
+    """By its name, the number that no struct could be packed with."""
+    for name, v in zip(names, numbers):
+        try:
+            struct.pack(kind, v)
+        except _NO_NUMBER:
+            raise PicturaError(EINVAL, f"{name}: {type(v).__name__}, expected a number within range") from None
+    raise PicturaError(EINVAL, str(e)) from None
 
 
 def _tensor(t, name: str, device=None):
@@ -602,7 +601,10 @@ def pictura_sample_actions(logits, uniform, out_action, out_logp, mask=None, tem
         named += (name, kind, row)
     *rows, iu, oa, ol = _vectors(logits, N, *named, "uniform", "f", uniform, "out_action", "l", out_action, "out_logp", "f",
                                  out_logp)
-    how = _pack(_SAMPLING_PACK, named[::3], scalars, *scalars, *rows)
+    try:
+        how = _SAMPLING_PACK.pack(*scalars, *rows)
+    except _NO_NUMBER as e:
+        _refuse("f", named[::3], scalars, e)
     st = _call(logits.device, _lib.pictura_sample_actions, l, how, iu, oa, ol)
     if st != OK:
         raise PicturaError(st, "sample_actions failed")
@@ -626,9 +628,12 @@ def pictura_policy_loss(logits, values, actions, old_logp, advantages, returns, 
                          "returns", "f", returns, "old_values", "f", old_values, "weights", "f", weights, "dvalues", "f",
                          dvalues)
     os_, = _vectors(logits, len(POLICY_STATS), "out_stats", "f", out_stats)
-    numbers = (temperature, clip, value_clip, value_coef, entropy_coef, denominator)
-    batch = _pack(_BATCH_PACK, ("temperature", "clip", "value_clip", "value_coef", "entropy_coef", "denominator"), numbers,
-                  v.data_ptr(), v.stride(0), *rows, *numbers, bool(normalize))
+    try:
+        batch = _BATCH_PACK.pack(v.data_ptr(), v.stride(0), *rows, temperature, clip, value_clip, value_coef, entropy_coef,
+                                 denominator, bool(normalize))
+    except _NO_NUMBER as e:
+        _refuse("f", ("temperature", "clip", "value_clip", "value_coef", "entropy_coef", "denominator"),
+                (temperature, clip, value_clip, value_coef, entropy_coef, denominator), e)
     if value_clip > 0 and old_values is None:
         raise PicturaError(EINVAL, "old_values: needed where value_clip > 0")
     dl, _, _, stride = _matrix(_tensor(dlogits, "dlogits", dev), "dlogits", N, A)
@@ -673,8 +678,10 @@ def pictura_adamw_step(table, device, lr, betas, eps, weight_decay, step, bits=3
     current stream.  grad_factor: float32 tensor of one element on the device."""
     at = _table(table)
     gf = 0 if grad_factor is None else _vectors(grad_factor, 1, "grad_factor", "f", grad_factor)[0]
-    numbers = (lr, betas[0], betas[1], eps, weight_decay)
-    how = _pack(_ADAMW_PACK, ("lr", "beta1", "beta2", "eps", "weight_decay"), numbers, *numbers, step, bits, gf)
+    try:
+        how = _ADAMW_PACK.pack(lr, betas[0], betas[1], eps, weight_decay, step, bits, gf)
+    except _NO_NUMBER as e:
+        _refuse("d", ("lr", "beta1", "beta2", "eps", "weight_decay"), (lr, *betas, eps, weight_decay), e)
     st = _call(device, _lib.pictura_adamw_step, how, at, len(table))
     if st != OK:
         raise PicturaError(st, "adamw_step: a value out of range")

@@ -175,8 +175,8 @@ class AdamW(torch.optim.Optimizer):
             raise PicturaError(EINVAL, str(e)) from None
         if not n:
             return table[:0], steps[:0], states, None
-        # (of the first that takes part: parameters without a gradient may be anywhere)
-        pictura._check_device(params[first], f"parameter {first}", None)
+        if not params[first].is_cuda:   # (the first that takes part: those without a gradient may be anywhere)
+            pictura._check_device(params[first], f"parameter {first}", None)
         return table[:n], steps[:n], states, params[first].device
 
     def step(self, closure=None, grads=None):
@@ -230,9 +230,7 @@ class AdamW(torch.optim.Optimizer):
         lists of float32 tensors; with bits=8 what the codes stand for, written to
         the two lists of contiguous float32 tensors `out` where that is given."""
         params = [p for group in self.param_groups for p in group["params"]]
-        if self._in_order(params):
-            params = [p for p, s in zip(params, self.state.values()) if "step" in s]
-        else:
+        if not self._in_order(params) or not all(["step" in s for s in self.state.values()]):
             params = [p for p in params if "step" in self.state.get(p, ())]
         if self.bits == 32:
             return [self.state[p]["exp_avg"] for p in params], [self.state[p]["exp_avg_sq"] for p in params]
