@@ -43,7 +43,7 @@ HBM_PEAK_GBS = 8000.0   # MI355X HBM3E peak
 # `traffic` is reported as null.
 TRAFFIC = {
     "config": 4,
-    "sources_sha256": "f57204c5f8004a115e18e60c2d5a95c5e82a84f86e0e8eaaafbf5be163635c32",
+    "sources_sha256": "2991bed528c94c068b883b66ecff028c592075c78410b2d3aab3a08e302c48ff",
     "fetch_bytes": 1.1530e9,
     "write_bytes": 5368709120,
 }
