@@ -415,8 +415,9 @@ pictura_status pictura_encode_views(const pictura_encoder* enc, const uint8_t* c
  * (paper Sec. 3.3 and App. A.3: categorical actions, clipped policy optimisation
  * with normalised advantages, AdamW).  Like pictura_encode_views these calls take
  * no context: they run on `stream` of the current device, allocate nothing and
- * do not synchronise, so they can be captured in a graph.  Errors are found on
- * the host before anything is launched. */
+ * do not synchronise, so they can be captured in a graph.  (Replays take the numbers
+ * that were captured; an AdamW step's among them is its number, so its bias correction
+ * is that of the capture.)  Errors are found on the host before anything is launched. */
 
 #define PICTURA_F32  0
 #define PICTURA_BF16 1

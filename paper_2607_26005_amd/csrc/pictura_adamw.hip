@@ -2,15 +2,16 @@
 // norm of all gradients together.
 //
 // The tensors' pointers travel in the kernel's arguments, up to 80 tensors to a
-// launch, so a step copies nothing to the device and can be captured in a graph.  A
+// launch (60 with 8-bit moments, 160 in the norm), so a step copies nothing to the device
+// and can be captured in a graph, in which its step number is the captured one.  A
 // workgroup takes kChunk elements of one tensor.
 //
 // Bound by memory: 300 tensors of 50 M fp32 weights with bf16 gradients take four
-// launches of 67 us (1.3 GB at 4.8 TB/s; a large copy runs at 4.9) and 43 us for the
+// launches of 50 to 77 us (1.3 GB at 4.9 TB/s; a large copy runs at 4.9) and 43 us for the
 // norm, which has to see every gradient before the first weight moves: 316 us the
-// call.  64 tensors of 128 M bf16 weights with 8-bit moments take 290 us (1.28 GB at
-// 4.4 TB/s, 76 vector instructions for 64 weights), and their moments are decoded in
-// 228 us (1.28 GB at 5.6).  A step of 29 tensors is launches and the binding, 28 us.
+// call.  64 tensors of 128 M bf16 weights with 8-bit moments take 255 to 290 us (1.27 GB at
+// 4.4 to 5.0 TB/s, 76 vector instructions for 64 weights), and their moments are decoded in
+// 220 to 228 us (1.26 GB at 5.6).  A step of 29 tensors is launches and the binding, 29 us.
 #include <cmath>
 
 #include "pictura.h"

@@ -1215,8 +1215,10 @@ __device__ __forceinline__ V group_sum(V x)
 
 // Heads of up to 64 actions.  Each lane holds one action; where a filter is on, it
 // counts the actions and adds the weights that come before its own, A steps.  65,536
-// rows of 12: 8.4 us of kernel, 230 vector instructions for a wave's four rows; the
-// call takes 10 to 12 us, launch and binding included.
+// rows of 12: 8.2 us of kernel; 16,384 waves of 234 vector instructions, whose issue
+// takes 6 us of it (some 3,700 instructions for each SIMD, four cycles each).  The
+// call takes 10 to 12 us, launch and binding included; 65,536 rows of 48 with top_p 88 us,
+// 48 steps each.
 template <class T, int G, bool kFilter>
 __global__ __launch_bounds__(kThreads) void sample_small_kernel(const Rows R, const Sampling S,
                                                                 const float* __restrict__ uniform,
@@ -1428,7 +1430,8 @@ __device__ __forceinline__ void loss_stats(const Batch& b, const Shared3& s, con
 // Leave this workgroup's sums; the last workgroup to do so adds them all up, in the
 // order of the workgroups, and writes the statistics.  (Where a launch writes much,
 // the fence that this takes in every workgroup costs more than another launch: 2,047
-// rows of 16,381 in bf16 78 us with it, 58 with loss_stats_kernel.)
+// rows of 16,381 in bf16 took 78 us with it and 58 with loss_stats_kernel when that was
+// chosen; they take 51 to 53 now.)
 template <int NW>
 __device__ void loss_finish(const Batch& b, const Shared3& s, const double* acc, double* __restrict__ sums,
                             uint32_t* __restrict__ done)
@@ -1522,7 +1525,9 @@ __global__ __launch_bounds__(kThreads) void loss_thread_kernel(const Rows R, con
     loss_finish<kWaves>(b, s, acc, k.sums, k.done);
 }
 
-// Heads of 17 to 64 actions: a row in a group of G lanes, one action each.
+// Heads of 17 to 64 actions: a row in a group of G lanes, one action each.  65,536 rows of
+// 17 take 46 us with their first launch, of 48 62 us: a row's logarithm, its two
+// exponentials of ratios and the terms are computed by all lanes of the group.
 template <class T, int G>
 __global__ __launch_bounds__(kThreads) void loss_small_kernel(const Rows R, const Batch b, const Work k)
 {
@@ -1771,9 +1776,18 @@ using Int = std::integral_constant<int, N>;
 
 // Waves and items of a workgroup that holds a row of so many slots in its registers.
 // With many rows few waves to a row: the row's reductions take fewer barriers, and
-// more rows are under way on a CU (2,047 rows of 16,381: 58 us with four waves, 77
-// with sixteen).  With fewer rows than CUs the waves are there anyway (one row of
-// 16,385: 15 us with sixteen, 25 with four when this was chosen; 10 us now).
+// more rows are under way on a CU.  With fewer rows than CUs the waves are there anyway.
+// fp32 in a graph, us (draws, draws with top_p, loss and gradient), by waves to a row:
+//     4,096 rows of 500      one 6, 12, 19       four 11, 23, 27      sixteen 35, 112, 93
+//     4,096 rows of 2,000    one 14, 28, 29      four 15, 30, 31
+//     4,096 rows of 8,000    four 39, 73, 59     sixteen 50, 148, 100
+//     1,024 rows of 2,000    one 7, 18, 16       four 7, 12, 15
+//     1,024 rows of 16,000   four 27, 62, 33     sixteen 23, 56, 47
+//       255 rows of 2,000    one 7, 16, 13       four 5, 9, 10
+//       255 rows of 16,000   four 12, 28, 19     sixteen 9, 16, 17
+// The 256 rows from which a row gets fewer waves are too few for draws: 256 to 512 rows
+// of 1,000 to 2,000 take 1.1 to 1.9 times as long with one wave as with four (256 of 2,000
+// with top_p 16.5 us and 8.8), 256 of 16,000 with top_p 29 us where sixteen take 16.
 struct RowShape {
     int waves, items;
 };

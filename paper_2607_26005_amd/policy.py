@@ -106,7 +106,7 @@ def policy_loss(logits, values, actions, old_logp, advantages, returns, **kwargs
     """(loss, stats) for autograd: policy_gradient's loss, whose backward hands on the
     gradient that the same pass computed, times the factor that arrives (a loss scale).
     Only logits and values get one.  Of float16 logits the gradient is kept in float32
-    for that: 8 bytes an entry between the two, with the logits' own float32 copy."""
+    for that, 4 bytes an entry (and 4 more for the logits' copy while it is computed)."""
     return _PolicyLoss.apply(logits, values, (actions, old_logp, advantages, returns), kwargs)
 
 
@@ -120,7 +120,10 @@ class AdamW(torch.optim.Optimizer):
     (None: no gradient) in place of the parameters' own .grad; they may be of another
     type than the weights.  After a step with max_norm, grad_norm is the norm before
     clipping, a tensor on the device.  With bits=8 a weight's state holds codes
-    (exp_avg int8, exp_avg_sq uint8) and scales; moments() gives what they stand for."""
+    (exp_avg int8, exp_avg_sq uint8) and scales; moments() gives what they stand for.
+
+    The step number is the host's: a step captured in a graph replays with the rate and
+    the bias correction that it was captured with, and counts once."""
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2,
                  bits: int = 32, max_norm: Optional[float] = None):
