@@ -10,7 +10,7 @@
 // launches of 50 to 77 us (1.3 GB at 4.9 TB/s; a large copy runs at 4.9) and 43 us for the
 // norm, which has to see every gradient before the first weight moves: 316 us the
 // call.  64 tensors of 128 M bf16 weights with 8-bit moments take 255 to 290 us (1.27 GB at
-// 4.4 to 5.0 TB/s, 76 vector instructions for 64 weights), and their moments are decoded in
+// 4.4 to 5.0 TB/s, 77 vector instructions for 64 weights), and their moments are decoded in
 // 220 to 228 us (1.26 GB at 5.6).  A step of 29 tensors is launches and the binding, 29 us.
 #include <cmath>
 
