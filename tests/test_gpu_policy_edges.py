@@ -179,3 +179,22 @@ def test_steps_with_next_to_no_epsilon(mods, bits, eps):
     want = PO.adamw(np.zeros(n), grad.double().numpy(), np.zeros(n), np.zeros(n), 1, how["lr"], how["betas"], eps32, 0.0)[0]
     got = p.detach().double().cpu().numpy()
     assert (np.abs(got - want) <= 2.0 ** -16 * how["lr"]).all(), np.abs(got - want).max() / how["lr"]
+
+
+@pytest.mark.parametrize("A", [12, 40, 300, 5000, 80000])
+@pytest.mark.parametrize("exponent", [-145, -127, -100, -65, -64, -63, 63, 64, 65, 100, 122])
+def test_temperatures_of_any_size_draw_by_their_quotients(mods, A, exponent):
+    # logits as large as the temperature: the correctly rounded quotient, to the bit
+    torch, policy = mods
+    N, g = 8, torch.Generator().manual_seed(A)
+    for T in (2.0 ** exponent, float(np.float32(1.37 * 2.0 ** exponent))):
+        x = (torch.randn(N, A, generator=g).double() * 2.5 * T).float().cuda()
+        u = torch.rand(N, generator=g).cuda()
+        t = torch.full((N, 1), T, dtype=torch.float32, device="cuda")
+        w = (((x - x.amax(1, keepdim=True)) / t).exp() * 2.0 ** 31).round().to(torch.int64)
+        for how in (dict(), dict(top_k=7), dict(top_p=0.8), dict(top_k=400, top_p=0.5), dict(min_p=0.3)):
+            want, mine, total = _draw_by_rule(torch, x, w, u, **how)
+            act, logp = policy.sample_actions(x, u, temperature=T, **how)
+            assert torch.equal(act, want), (T, how, (act != want).nonzero().flatten().tolist())
+            ref = (mine.double() / total.double()).log()
+            assert ((logp.double() - ref).abs() <= 2.0 ** -22 * ref.abs() + 2.0 ** -23).all(), how
