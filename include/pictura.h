@@ -576,6 +576,70 @@ pictura_status pictura_adamw_step(const pictura_adamw* how, const pictura_adamw_
 pictura_status pictura_adamw_moments(const pictura_adamw_tensor* tensors, int32_t count, float* const* exp_avg_out,
                                      float* const* exp_avg_sq_out, void* stream);
 
+/* ---- a memory over the steps of an episode ----------------------------------
+ * Layers for a policy that decides from what it saw before: a gated linear
+ * recurrence over sequences of steps, and the norm between such layers.  As the
+ * policy's calls above: no context, `stream` of the current device, no allocation,
+ * no synchronisation, errors found on the host before anything is launched. */
+
+#define PICTURA_SCAN_STEPS 16   /* steps between the states that a scan saves for its gradient */
+
+/* `batch` sequences of `steps` steps of `channels` channels.  Element (b, t, c) of gates
+ * is at gates[b * gates_batch + t * gates_step + c] (strides in elements, 0 or more),
+ * likewise inputs (both of `dtype`), and resets[b * resets_batch + t * resets_step],
+ * which is not 0 where step t begins anew: what sequence b remembers is forgotten
+ * before that step, a NaN too.  Sequences packed one behind the other are one sequence
+ * with resets.  state (or NULL: zeros): fp32 [batch][channels], what is remembered
+ * before the first step.  batch * channels < 2^31, steps < 2^31. */
+typedef struct {
+    const void* gates;
+    const void* inputs;
+    const float* state;
+    const uint8_t* resets;   /* or NULL: none */
+    int64_t gates_batch, gates_step;
+    int64_t inputs_batch, inputs_step;
+    int64_t resets_batch, resets_step;
+    int64_t batch, steps;
+    int32_t channels;        /* 1 or more */
+    int32_t dtype;           /* PICTURA_F32, PICTURA_BF16 or PICTURA_F16 */
+} pictura_sequences;
+
+/* Bytes of workspace that a scan of these sizes and its gradient take (reads batch,
+ * steps, channels and dtype alone). */
+pictura_status pictura_gated_scan_workspace(const pictura_sequences* sequences, uint64_t* bytes);
+
+/* Gated linear recurrence over whole sequences: with a = sigmoid(gates),
+ *   h_t = a_t h_(t-1) + (1 - a_t) inputs_t,
+ * h_(t-1) = 0 where step t is reset, in fp32 (a and 1 - a each to a few units of their
+ * own).  out (same type, strides of its own, no two elements at one place) receives h_t;
+ * last_state (or NULL) fp32 [batch][channels] the state after the last step; saved (or
+ * NULL), fp32 [ceil(steps / PICTURA_SCAN_STEPS)][batch][channels], what the gradient
+ * needs: the states before steps 0, 16, 32, ...  Results do not depend on what else runs;
+ * where few channels stand against many steps the steps are cut into segments, whose
+ * sums are taken in one order.  last_state must not overlap state, nor out the inputs.
+ * workspace: device memory, 256-byte aligned, in use until the call's work on the stream
+ * is done.  EINVAL: a null or misaligned pointer, sizes or strides out of range, or a
+ * workspace too small. */
+pictura_status pictura_gated_scan(const pictura_sequences* sequences, void* out, int64_t out_batch, int64_t out_step,
+                                  float* last_state, float* saved, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Gradient of pictura_gated_scan: from dout (of out; strides 0 or more) and dlast (of
+ * last_state; NULL: zeros), with the `saved` of that call (`state` is not read again)
+ *   G_t = dout_t + c_(t+1), c_(steps) = dlast, c_t = a_t G_t (0 where step t is reset),
+ *   dinputs_t = (1 - a_t) G_t, dgates_t = a_t (1 - a_t) (h_(t-1) - inputs_t) G_t,
+ * and dstate (or NULL) = c_0.  Each is rounded to its type once.  dgates and dinputs must
+ * not overlap what is read, nor each other.  Errors and workspace as pictura_gated_scan. */
+pictura_status pictura_gated_scan_gradient(const pictura_sequences* sequences, const float* saved, const void* dout,
+                                           int64_t dout_batch, int64_t dout_step, const float* dlast, void* dgates,
+                                           int64_t dgates_batch, int64_t dgates_step, void* dinputs, int64_t dinputs_batch,
+                                           int64_t dinputs_step, float* dstate, void* workspace, uint64_t workspace_bytes,
+                                           void* stream);
+
+/* One step of the recurrence (steps is 1, sequences->state not read): state fp32
+ * [batch][channels] is replaced by h, out[b * out_batch + c] receives it in the inputs'
+ * type and may be the inputs' or the gates' own memory (same stride). */
+pictura_status pictura_gated_step(const pictura_sequences* sequences, void* out, int64_t out_batch, float* state, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,640 @@
+// A memory over the steps of sequences: the gated linear recurrence
+//     a = sigmoid(g),  h_t = a_t h_(t-1) + (1 - a_t) x_t
+// per channel (h_(t-1) taken as 0 where a step is reset), its gradient, and one step
+// of it in place.
+//
+// Gradient.  With G_t the gradient of h_t, all later steps included, and c_t = a_t G_t
+// what step t hands back (0 at a reset):
+//     G_t = dout_t + c_(t+1),  dx_t = (1 - a_t) G_t,  dg_t = a_t (1 - a_t) (h_(t-1) - x_t) G_t,
+// the same recurrence backwards.  h_(t-1) is needed in fp32: the forward pass leaves the
+// state before every 16th step, and the steps between are computed again in registers
+// (0.25 byte an element instead of 4).
+//
+// A thread walks through the steps of one or two channels, 16 steps' loads under way at
+// once.  Where there are too few channels for the card, the steps are cut into segments:
+// what a segment does to a state is h -> P h + H, with P the product of its a.  One
+// launch computes P and H of every segment and of groups of 16, in the next every
+// segment begins by folding those before it, in their order, so results repeat to the bit.
+#include <cmath>
+
+#include "pictura.h"
+#include "pictura_internal.h"
+
+#pragma clang fp contract(off)
+
+namespace pictura {
+namespace {
+
+constexpr int kSteps = PICTURA_SCAN_STEPS;   // steps between saved states, and in registers at once
+constexpr int kFew = 8;                      // steps in registers of the summaries' 16 waves
+constexpr int kGroup = 16;                   // segments of a group
+
+template <class T, int V>
+struct alignas(V * sizeof(T)) Vec {
+    T v[V];
+};
+
+template <class T, int V>
+__device__ __forceinline__ Vec<T, V> load(const T* p) { return *reinterpret_cast<const Vec<T, V>*>(p); }
+
+template <class T, int V>
+__device__ __forceinline__ void store(T* p, const Vec<T, V>& x) { *reinterpret_cast<Vec<T, V>*>(p) = x; }
+
+// Element (b, t, c) of a sequence's tensor is at data[b * batch + t * step + c].
+template <class T>
+struct Tensor {
+    T* data;
+    int64_t batch, step;
+};
+
+template <class T>
+struct Sequences {
+    Tensor<const T> gates, inputs;
+    const float* state;                 // [batch][channels]
+    Tensor<const uint8_t> resets;       // one channel
+    int64_t threads, steps, segment;    // vectors of channels in all, steps, steps of a segment
+    int32_t vectors;                    // vectors of a sequence's channels
+    int32_t segments;
+};
+
+// The smaller one of a = sigmoid(g) and 1 - a, with the sign set where that is 1 - a:
+// the other one is 1 - |m| to half a unit.  e = exp(-|g|) with the product by log2(e) in
+// two terms; at 128 and beyond it is 0 in fp32.
+__device__ __forceinline__ float gate_of(float g)
+{
+    constexpr float kHi = 1.44269502f, kLo = 1.92596299e-8f, kLn2 = 0.693147182f;
+    const float z = fabsf(g) > 128.0f ? 128.0f : fabsf(g);   // (a NaN stays one)
+    const float hi = z * -kHi, lo = fmaf(z, -kHi, -hi) - z * kLo;
+    float e = __builtin_amdgcn_exp2f(hi);
+    e = fmaf(e * lo, kLn2, e);
+    const float d = 1.0f + e;
+    float r = __builtin_amdgcn_rcpf(d);
+    r = fmaf(fmaf(-d, r, 1.0f), r, r);
+    const float m = e * r;
+    return g < 0.0f ? m : -m;
+}
+
+// m as a and b = 1 - a.
+__device__ __forceinline__ void gate_parts(float m, float& a, float& b)
+{
+    const float s = fabsf(m), l = 1.0f - s;
+    const bool positive = __float_as_uint(m) >> 31;
+    a = positive ? l : s;
+    b = positive ? s : l;
+}
+
+// What steps do to a state, h -> P h + H.  A reset among them makes P -0 (every other
+// product is +0 or more): the state does not count then, even if it is a NaN.
+struct Map {
+    float P, H;
+};
+
+__device__ __forceinline__ float apply(const Map& f, float h)
+{
+    return __float_as_uint(f.P) == 0x80000000u ? f.H : fmaf(f.P, h, f.H);
+}
+
+// f, then g
+__device__ __forceinline__ Map then(const Map& f, const Map& g)
+{
+    return Map{__float_as_uint(g.P) == 0x80000000u ? g.P : g.P * f.P, apply(g, f.H)};
+}
+
+// Where a thread's channels begin in the tensors.
+template <class T, int V>
+struct Place {
+    int64_t b;
+    int32_t c;
+    __device__ __forceinline__ Place(int64_t thread, int32_t vectors)
+    {
+        if (thread >> 32 == 0) {   // (a 64-bit division takes some hundred instructions)
+            b = (uint32_t)thread / (uint32_t)vectors;
+            c = (int32_t)((uint32_t)thread % (uint32_t)vectors) * V;
+        } else {
+            b = thread / vectors;
+            c = (int32_t)(thread % vectors) * V;
+        }
+    }
+    template <class U>
+    __device__ __forceinline__ U* in(const Tensor<U>& x) const { return x.data + b * x.batch + c; }
+    __device__ __forceinline__ const uint8_t* flags(const Tensor<const uint8_t>& x) const { return x.data + b * x.batch; }
+};
+
+// Up to N steps of a tensor; those from n on are zeros.
+template <class T, int V, int N>
+__device__ __forceinline__ void load_steps(const T* p, int64_t step, int n, Vec<T, V> (&x)[N])
+{
+    if (n == N) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = load<T, V>(p + i * step);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            x[i] = Vec<T, V>{};
+            if (i < n) x[i] = load<T, V>(p + i * step);
+        }
+    }
+}
+
+template <bool kResets, int N>
+__device__ __forceinline__ uint32_t load_resets(const uint8_t* p, int64_t step, int n)
+{
+    uint32_t bits = 0;
+    if constexpr (kResets) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < n && p[i * step]) bits |= 1u << i;
+    }
+    return bits;
+}
+
+// Summaries of the segments and their groups: rows of `threads` vectors of maps.
+template <int V>
+struct alignas(8 * V) Maps {
+    Map v[V];
+};
+
+template <int V>
+struct Summaries {
+    Maps<V>* segments;   // [segments][threads]
+    Maps<V>* groups;     // [groups][threads]
+};
+
+// P and H of every segment (forwards), or of what it hands back (kBack: c -> P c + H).
+template <class T, int V, bool kResets, bool kBack>
+__global__ __launch_bounds__(64 * kGroup) void summary_kernel(const Sequences<T> q, const Tensor<const T> dout,
+                                                              const Summaries<V> out)
+{
+    __shared__ Maps<V> lds[kGroup][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t thread = (int64_t)blockIdx.x * 64 + lane;
+    const int32_t seg = blockIdx.y * kGroup + wave;
+    const bool on = thread < q.threads && seg < q.segments && seg != (kBack ? 0 : q.segments - 1);
+    Maps<V> f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) f.v[v] = Map{1.0f, 0.0f};
+    if (on) {
+        const Place<T, V> at(thread, q.vectors);
+        const int64_t t0 = seg * q.segment, t1 = min(q.steps, t0 + q.segment);
+        const T* g = at.in(q.gates);
+        const T* x = kBack ? at.in(dout) : at.in(q.inputs);
+        const int64_t xs = kBack ? dout.step : q.inputs.step;
+        const uint8_t* r = at.flags(q.resets);
+        const int64_t blocks = (t1 - t0 + kFew - 1) / kFew;
+        for (int64_t k = 0; k < blocks; ++k) {
+            const int64_t t = t0 + (kBack ? blocks - 1 - k : k) * kFew;
+            const int n = (int)min((int64_t)kFew, t1 - t);
+            Vec<T, V> gs[kFew], xs_[kFew];
+            load_steps<T, V>(g + t * q.gates.step, q.gates.step, n, gs);
+            load_steps<T, V>(x + t * xs, xs, n, xs_);
+            const uint32_t resets = load_resets<kResets, kFew>(r + t * q.resets.step, q.resets.step, n);
+#pragma unroll
+            for (int j = 0; j < kFew; ++j) {
+                const int i = kBack ? kFew - 1 - j : j;
+                if (i >= n) continue;
+                const bool reset = kResets && (resets >> i & 1u);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    float a, b;
+                    gate_parts(gate_of((float)gs[i].v[v]), a, b);
+                    Map& m = f.v[v];
+                    if constexpr (kBack) m.H = reset ? 0.0f : a * ((float)xs_[i].v[v] + m.H);
+                    else m.H = reset ? b * (float)xs_[i].v[v] : fmaf(a, m.H, b * (float)xs_[i].v[v]);
+                    m.P = reset ? -0.0f : __float_as_uint(m.P) == 0x80000000u ? m.P : a * m.P;
+                }
+            }
+        }
+        out.segments[(int64_t)seg * q.threads + thread] = f;
+    }
+    lds[wave][lane] = f;
+    __syncthreads();
+    if (wave == 0 && thread < q.threads) {
+#pragma unroll
+        for (int k = 1; k < kGroup; ++k) {
+            const Maps<V>& m = lds[kBack ? kGroup - 1 - k : k][lane];
+            if (k == 1) f = lds[kBack ? kGroup - 1 : 0][lane];
+#pragma unroll
+            for (int v = 0; v < V; ++v) f.v[v] = then(f.v[v], m.v[v]);
+        }
+        out.groups[(int64_t)blockIdx.y * q.threads + thread] = f;
+    }
+}
+
+// h through the maps of the segments before this one (kBack: those after it).
+template <int V, bool kBack>
+__device__ __forceinline__ void fold(const Summaries<V>& s, int64_t threads, int64_t thread, int32_t seg, int32_t segments,
+                                     float (&h)[V])
+{
+    auto through = [&](const Maps<V>* rows, int32_t from, int32_t count) {
+        constexpr int kAhead = 8;
+        for (int32_t k = 0; k < count; k += kAhead) {
+            Maps<V> m[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (k + i < count) m[i] = rows[(int64_t)(kBack ? from - k - i : from + k + i) * threads + thread];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (k + i < count) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) h[v] = apply(m[i].v[v], h[v]);
+                }
+        }
+    };
+    const int32_t group = seg / kGroup, groups = (segments + kGroup - 1) / kGroup;
+    if (kBack) {
+        through(s.groups, groups - 1, groups - 1 - group);
+        const int32_t last = min(segments, (group + 1) * kGroup) - 1;
+        through(s.segments, last, last - seg);
+    } else {
+        through(s.groups, 0, group);
+        through(s.segments, group * kGroup, seg - group * kGroup);
+    }
+}
+
+template <class T, int V, bool kResets>
+__global__ __launch_bounds__(256) void scan_kernel(const Sequences<T> q, const Tensor<T> out, float* __restrict__ last,
+                                                   float* __restrict__ saved, const Summaries<V> sums)
+{
+    const int64_t thread = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (thread >= q.threads) return;
+    const int32_t seg = blockIdx.y;
+    const Place<T, V> at(thread, q.vectors);
+    const int64_t t0 = seg * q.segment, t1 = min(q.steps, t0 + q.segment);
+    const T* g = at.in(q.gates);
+    const T* x = at.in(q.inputs);
+    const uint8_t* r = at.flags(q.resets);
+    T* y = at.in(out);
+    float h[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = q.state ? q.state[thread * V + v] : 0.0f;
+    if (seg > 0) fold<V, false>(sums, q.threads, thread, seg, q.segments, h);
+    auto steps = [&](int64_t t, int n) {
+        Vec<T, V> gs[kSteps], xs[kSteps];
+        load_steps<T, V>(g + t * q.gates.step, q.gates.step, n, gs);
+        load_steps<T, V>(x + t * q.inputs.step, q.inputs.step, n, xs);
+        const uint32_t resets = load_resets<kResets, kSteps>(r + t * q.resets.step, q.resets.step, n);
+        if (saved) {
+            Vec<float, V> s;
+#pragma unroll
+            for (int v = 0; v < V; ++v) s.v[v] = h[v];
+            store<float, V>(saved + ((t / kSteps) * q.threads + thread) * V, s);
+        }
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            if (i >= n) continue;
+            Vec<T, V> o;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float a, b;
+                gate_parts(gate_of((float)gs[i].v[v]), a, b);
+                const float add = b * (float)xs[i].v[v];
+                h[v] = kResets && (resets >> i & 1u) ? add : fmaf(a, h[v], add);
+                o.v[v] = (T)h[v];
+            }
+            store<T, V>(y + (t + i) * out.step, o);
+        }
+    };
+    int64_t t = t0;
+    for (; t + kSteps <= t1; t += kSteps) steps(t, kSteps);
+    if (t < t1) steps(t, (int)(t1 - t));
+    if (last && seg == q.segments - 1) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) last[thread * V + v] = h[v];
+    }
+}
+
+template <class T, int V, bool kResets>
+__global__ __launch_bounds__(256) void scan_gradient_kernel(const Sequences<T> q, const Tensor<const T> dout,
+                                                            const float* __restrict__ dlast, const float* __restrict__ saved,
+                                                            const Tensor<T> dgates, const Tensor<T> dinputs,
+                                                            float* __restrict__ dstate, const Summaries<V> sums)
+{
+    const int64_t thread = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (thread >= q.threads) return;
+    const int32_t seg = blockIdx.y;
+    const Place<T, V> at(thread, q.vectors);
+    const int64_t t0 = seg * q.segment, t1 = min(q.steps, t0 + q.segment);
+    const T* g = at.in(q.gates);
+    const T* x = at.in(q.inputs);
+    const T* dy = at.in(dout);
+    const uint8_t* r = at.flags(q.resets);
+    T* dg = at.in(dgates);
+    T* dx = at.in(dinputs);
+    float c[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) c[v] = dlast ? dlast[thread * V + v] : 0.0f;
+    if (seg < q.segments - 1) fold<V, true>(sums, q.threads, thread, seg, q.segments, c);
+    auto steps = [&](int64_t t, int n) {
+        Vec<T, V> gs[kSteps], xs[kSteps], dys[kSteps];
+        load_steps<T, V>(g + t * q.gates.step, q.gates.step, n, gs);
+        load_steps<T, V>(x + t * q.inputs.step, q.inputs.step, n, xs);
+        load_steps<T, V>(dy + t * dout.step, dout.step, n, dys);
+        const uint32_t resets = load_resets<kResets, kSteps>(r + t * q.resets.step, q.resets.step, n);
+        const Vec<float, V> s = load<float, V>(saved + ((t / kSteps) * q.threads + thread) * V);
+        float h[V], m[kSteps][V], d[kSteps][V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = s.v[v];
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float xi = (float)xs[i].v[v];
+                float a, b;
+                m[i][v] = gate_of((float)gs[i].v[v]);
+                gate_parts(m[i][v], a, b);
+                if (kResets && (resets >> i & 1u)) h[v] = 0.0f;
+                d[i][v] = h[v] - xi;
+                h[v] = fmaf(a, h[v], b * xi);
+            }
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+            const int i = kSteps - 1 - j;
+            if (i >= n) continue;
+            Vec<T, V> og, ox;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float a, b;
+                gate_parts(m[i][v], a, b);
+                const float G = (float)dys[i].v[v] + c[v], bG = b * G;
+                ox.v[v] = (T)bG;
+                og.v[v] = (T)(a * bG * d[i][v]);
+                c[v] = kResets && (resets >> i & 1u) ? 0.0f : a * G;
+            }
+            store<T, V>(dg + (t + i) * dgates.step, og);
+            store<T, V>(dx + (t + i) * dinputs.step, ox);
+        }
+    };
+    int64_t t = t1;
+    if ((t1 - t0) % kSteps) {
+        t -= (t1 - t0) % kSteps;
+        steps(t, (int)(t1 - t));
+    }
+    for (; t > t0; t -= kSteps) steps(t - kSteps, kSteps);
+    if (dstate && seg == 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) dstate[thread * V + v] = c[v];
+    }
+}
+
+// One step in place: as many channels a thread as 16 bytes hold, at any address.
+template <class T, int V>
+__global__ __launch_bounds__(256) void step_kernel(const Sequences<T> q, T* __restrict__ out, int64_t out_batch,
+                                                   float* __restrict__ state)
+{
+    const int64_t thread = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (thread >= q.threads) return;
+    const Place<T, V> at(thread, q.vectors);
+    struct Bits { T v[V]; };
+    struct States { float v[V]; };
+    Bits g, x, o;
+    States h;
+    __builtin_memcpy(&g, at.in(q.gates), sizeof(g));
+    __builtin_memcpy(&x, at.in(q.inputs), sizeof(x));
+    __builtin_memcpy(&h, state + thread * V, sizeof(h));
+    const bool reset = q.resets.data && q.resets.data[at.b * q.resets.batch];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        float a, b;
+        gate_parts(gate_of((float)g.v[v]), a, b);
+        const float add = b * (float)x.v[v];
+        h.v[v] = reset ? add : fmaf(a, h.v[v], add);
+        o.v[v] = (T)h.v[v];
+    }
+    __builtin_memcpy(state + thread * V, &h, sizeof(h));
+    __builtin_memcpy(out + at.b * out_batch + at.c, &o, sizeof(o));
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+size_t size_of(int32_t t) { return t == PICTURA_F32 ? 4 : 2; }
+
+constexpr int64_t kWavesWanted = 4096;   // waves that fill the card
+constexpr int64_t kLeastSegment = 64;
+
+// Channels of a thread, and how the steps are cut.
+struct Shape {
+    int32_t vec, segments;
+    int64_t threads, segment;
+};
+
+Shape shape_of(const pictura_sequences& q, int32_t vec)
+{
+    Shape s{vec, 1, q.batch * (q.channels / vec), q.steps};
+    const int64_t waves = (s.threads + 63) / 64;
+    int64_t segments = waves ? kWavesWanted / waves : 1;
+    if (segments > q.steps / kLeastSegment) segments = q.steps / kLeastSegment;
+    if (segments > kGroup * 32) segments = kGroup * 32;
+    if (segments < 2) return s;
+    s.segment = ((q.steps + segments - 1) / segments + kSteps - 1) / kSteps * kSteps;
+    s.segments = (int32_t)((q.steps + s.segment - 1) / s.segment);
+    return s;
+}
+
+uint64_t summary_bytes(const Shape& s)
+{
+    if (s.segments < 2) return 0;
+    return (uint64_t)(s.segments + (s.segments + kGroup - 1) / kGroup) * s.threads * s.vec * sizeof(Map);
+}
+
+// The most that any alignment of the tensors takes.
+uint64_t workspace_bytes_of(const pictura_sequences& q)
+{
+    const uint64_t one = summary_bytes(shape_of(q, 1)), two = q.dtype == PICTURA_F32 || q.channels % 2 ? 0 : summary_bytes(shape_of(q, 2));
+    return 256 + (one > two ? one : two);
+}
+
+constexpr int64_t kMostChannels = (1ll << 31) - 1;   // of all sequences together
+
+bool sizes_ok(const pictura_sequences* q)
+{
+    return q && (q->dtype == PICTURA_F32 || q->dtype == PICTURA_BF16 || q->dtype == PICTURA_F16) && q->batch >= 0 &&
+           q->steps >= 0 && q->steps <= 0x7FFFFFFFll && q->channels >= 1 && q->batch <= kMostChannels / q->channels;
+}
+
+bool strides_ok(int64_t batch, int64_t step) { return batch >= 0 && step >= 0; }
+
+// Written tensors: no two elements at one place.
+bool apart(const pictura_sequences& q, int64_t batch, int64_t step)
+{
+    if (!strides_ok(batch, step)) return false;
+    const bool many = q.batch > 1, more = q.steps > 1;
+    if ((many && batch < q.channels) || (more && step < q.channels)) return false;
+    return !many || !more || batch / step >= q.steps || step / batch >= q.batch;   // one spans all of the other
+}
+
+bool inputs_ok(const pictura_sequences& q)
+{
+    const size_t e = size_of(q.dtype);
+    return q.gates && q.inputs && aligned(q.gates, e) && aligned(q.inputs, e) && aligned(q.state, 4) &&
+           strides_ok(q.gates_batch, q.gates_step) && strides_ok(q.inputs_batch, q.inputs_step) &&
+           strides_ok(q.resets_batch, q.resets_step);
+}
+
+pictura_status launched() { return hipGetLastError() == hipSuccess ? PICTURA_OK : PICTURA_EDEVICE; }
+
+template <class T>
+Sequences<T> sequences_of(const pictura_sequences& q, const Shape& s)
+{
+    return Sequences<T>{{(const T*)q.gates, q.gates_batch, q.gates_step}, {(const T*)q.inputs, q.inputs_batch, q.inputs_step},
+                        q.state, {q.resets, q.resets_batch, q.resets_step}, s.threads, q.steps, s.segment,
+                        q.channels / s.vec, s.segments};
+}
+
+// Whether pairs of channels can be loaded as one from a tensor of elements of e bytes.
+bool pairs(const pictura_sequences& q, const void* p, int64_t batch, int64_t step, size_t e)
+{
+    return aligned(p, 2 * e) && (q.batch < 2 || batch % 2 == 0) && (q.steps < 2 || step % 2 == 0);
+}
+
+template <int V>
+Summaries<V> summaries_of(void* workspace, const Shape& s)
+{
+    Maps<V>* segments = (Maps<V>*)workspace;
+    return Summaries<V>{segments, segments + (int64_t)s.segments * s.threads};
+}
+
+// go(T{}, constant V, constant whether there are resets)
+template <bool B>
+struct Bool {
+    static constexpr bool value = B;
+};
+template <int N>
+struct Int {
+    static constexpr int value = N;
+};
+
+template <class F>
+void with_kinds(const pictura_sequences& q, int32_t vec, F go)
+{
+    auto resets = [&](auto t, auto v) {
+        if (q.resets) go(t, v, Bool<true>{});
+        else go(t, v, Bool<false>{});
+    };
+    auto typed = [&](auto t) {
+        if constexpr (sizeof(t) == 2)
+            if (vec == 2) return resets(t, Int<2>{});
+        resets(t, Int<1>{});
+    };
+    if (q.dtype == PICTURA_F32) typed(float{});
+    else if (q.dtype == PICTURA_BF16) typed((__bf16)0.0f);
+    else typed((_Float16)0.0f);
+}
+
+dim3 grid_of(const Shape& s) { return dim3((unsigned)((s.threads + 255) / 256), (unsigned)s.segments); }
+
+dim3 summary_grid(const Shape& s) { return dim3((unsigned)((s.threads + 63) / 64), (unsigned)((s.segments + kGroup - 1) / kGroup)); }
+
+}  // namespace
+}  // namespace pictura
+
+using namespace pictura;
+
+extern "C" {
+
+pictura_status pictura_gated_scan_workspace(const pictura_sequences* q, uint64_t* bytes)
+{
+    if (!sizes_ok(q) || !bytes) return PICTURA_EINVAL;
+    *bytes = workspace_bytes_of(*q);
+    return PICTURA_OK;
+}
+
+pictura_status pictura_gated_scan(const pictura_sequences* q, void* out, int64_t out_batch, int64_t out_step,
+                                  float* last_state, float* saved, void* workspace, uint64_t workspace_bytes, void* stream)
+{
+    if (!sizes_ok(q)) return PICTURA_EINVAL;
+    if (q->batch == 0) return PICTURA_OK;
+    const size_t e = size_of(q->dtype);
+    if (!aligned(last_state, 4) || !aligned(q->state, 4) || (q->steps == 0 && !last_state)) return PICTURA_EINVAL;
+    if (q->steps > 0) {
+        if (!inputs_ok(*q) || !out || !aligned(out, e) || !apart(*q, out_batch, out_step) || !aligned(saved, 4))
+            return PICTURA_EINVAL;
+        if (!workspace || !aligned(workspace, 256) || workspace_bytes < workspace_bytes_of(*q)) return PICTURA_EINVAL;
+    }
+    const bool two = e == 2 && q->channels % 2 == 0 && pairs(*q, q->gates, q->gates_batch, q->gates_step, e) &&
+                     pairs(*q, q->inputs, q->inputs_batch, q->inputs_step, e) && pairs(*q, out, out_batch, out_step, e) &&
+                     aligned(saved, 8);
+    const Shape s = shape_of(*q, two ? 2 : 1);
+    hipStream_t st = (hipStream_t)stream;
+    with_kinds(*q, s.vec, [&](auto t, auto v, auto resets) {
+        using T = decltype(t);
+        constexpr int V = decltype(v)::value;
+        constexpr bool R = decltype(resets)::value;
+        const Sequences<T> seq = sequences_of<T>(*q, s);
+        const Summaries<V> sums = summaries_of<V>(workspace, s);
+        if (s.segments > 1)
+            hipLaunchKernelGGL((summary_kernel<T, V, R, false>), summary_grid(s), dim3(64 * kGroup), 0, st, seq,
+                               Tensor<const T>{}, sums);
+        hipLaunchKernelGGL((scan_kernel<T, V, R>), grid_of(s), dim3(256), 0, st, seq, Tensor<T>{(T*)out, out_batch, out_step},
+                           last_state, saved, sums);
+    });
+    return launched();
+}
+
+pictura_status pictura_gated_scan_gradient(const pictura_sequences* q, const float* saved, const void* dout, int64_t dout_batch,
+                                           int64_t dout_step, const float* dlast, void* dgates, int64_t dgates_batch,
+                                           int64_t dgates_step, void* dinputs, int64_t dinputs_batch, int64_t dinputs_step,
+                                           float* dstate, void* workspace, uint64_t workspace_bytes, void* stream)
+{
+    if (!sizes_ok(q)) return PICTURA_EINVAL;
+    if (q->batch == 0) return PICTURA_OK;
+    const size_t e = size_of(q->dtype);
+    if (!aligned(dlast, 4) || !aligned(dstate, 4) || (q->steps == 0 && !dstate)) return PICTURA_EINVAL;
+    if (q->steps > 0) {
+        if (!inputs_ok(*q) || !saved || !aligned(saved, 4) || !dout || !aligned(dout, e) || !strides_ok(dout_batch, dout_step))
+            return PICTURA_EINVAL;
+        if (!dgates || !dinputs || !aligned(dgates, e) || !aligned(dinputs, e) || !apart(*q, dgates_batch, dgates_step) ||
+            !apart(*q, dinputs_batch, dinputs_step))
+            return PICTURA_EINVAL;
+        if (!workspace || !aligned(workspace, 256) || workspace_bytes < workspace_bytes_of(*q)) return PICTURA_EINVAL;
+    }
+    const bool two = e == 2 && q->channels % 2 == 0 && pairs(*q, q->gates, q->gates_batch, q->gates_step, e) &&
+                     pairs(*q, q->inputs, q->inputs_batch, q->inputs_step, e) && pairs(*q, dout, dout_batch, dout_step, e) &&
+                     pairs(*q, dgates, dgates_batch, dgates_step, e) && pairs(*q, dinputs, dinputs_batch, dinputs_step, e) &&
+                     aligned(saved, 8);
+    const Shape s = shape_of(*q, two ? 2 : 1);
+    hipStream_t st = (hipStream_t)stream;
+    with_kinds(*q, s.vec, [&](auto t, auto v, auto resets) {
+        using T = decltype(t);
+        constexpr int V = decltype(v)::value;
+        constexpr bool R = decltype(resets)::value;
+        const Sequences<T> seq = sequences_of<T>(*q, s);
+        const Summaries<V> sums = summaries_of<V>(workspace, s);
+        const Tensor<const T> dy{(const T*)dout, dout_batch, dout_step};
+        if (s.segments > 1)
+            hipLaunchKernelGGL((summary_kernel<T, V, R, true>), summary_grid(s), dim3(64 * kGroup), 0, st, seq, dy, sums);
+        hipLaunchKernelGGL((scan_gradient_kernel<T, V, R>), grid_of(s), dim3(256), 0, st, seq, dy, dlast, saved,
+                           Tensor<T>{(T*)dgates, dgates_batch, dgates_step}, Tensor<T>{(T*)dinputs, dinputs_batch, dinputs_step},
+                           dstate, sums);
+    });
+    return launched();
+}
+
+pictura_status pictura_gated_step(const pictura_sequences* q, void* out, int64_t out_batch, float* state, void* stream)
+{
+    if (!sizes_ok(q) || q->steps != 1) return PICTURA_EINVAL;
+    if (q->batch == 0) return PICTURA_OK;
+    const size_t e = size_of(q->dtype);
+    if (!inputs_ok(*q) || !out || !aligned(out, e) || !apart(*q, out_batch, 0) || !state || !aligned(state, 4)) return PICTURA_EINVAL;
+    auto go = [&](auto t) {
+        using T = decltype(t);
+        constexpr int V = 16 / sizeof(T);
+        const Shape s{q->channels % V ? 1 : V, 1, q->batch * (q->channels / (q->channels % V ? 1 : V)), 1};
+        const dim3 grid((unsigned)((s.threads + 255) / 256));
+        if (s.vec == 1)
+            hipLaunchKernelGGL((step_kernel<T, 1>), grid, dim3(256), 0, (hipStream_t)stream, sequences_of<T>(*q, s), (T*)out,
+                               out_batch, state);
+        else
+            hipLaunchKernelGGL((step_kernel<T, V>), grid, dim3(256), 0, (hipStream_t)stream, sequences_of<T>(*q, s), (T*)out,
+                               out_batch, state);
+    };
+    if (q->dtype == PICTURA_F32) go(float{});
+    else if (q->dtype == PICTURA_BF16) go((__bf16)0.0f);
+    else go((_Float16)0.0f);
+    return launched();
+}
+
+}  // extern "C"

@@ -9,6 +9,8 @@
 #include <cstdint>
 #include <sstream>
 #include <stdexcept>
+#include <string>
+#include <vector>
 
 namespace {
 
@@ -228,8 +230,141 @@ PyObject* outputs(PyObject*, PyObject* args)
     return nullptr;
 }
 
+// pictura_sequences (include/pictura.h)
+struct Sequences {
+    uint64_t gates, inputs, state, resets;
+    int64_t gates_batch, gates_step, inputs_batch, inputs_step, resets_batch, resets_step, batch, steps;
+    int32_t channels, dtype;
+};
+static_assert(sizeof(Sequences) == 104, "pictura_sequences");
+
+struct Place {
+    uint64_t at = 0;
+    int64_t batch = 0, step = 0;
+};
+
+void strided(const at::Tensor& t, const char* name, const at::Device& dev)
+{
+    if (t.layout() != at::kStrided || t.is_neg()) refuse(name, ": expected a plain strided tensor");
+    if (t.device() != dev) refuse(name, ": tensor on ", t.device(), ", the others are on ", dev);
+}
+
+// A tensor [batch, steps, channels] (step: [batch, channels]) whose channels are neighbours.
+Place place(const at::Tensor& t, const char* name, const at::Tensor& like, bool whole)
+{
+    strided(t, name, like.device());
+    if (t.scalar_type() != like.scalar_type()) refuse(name, ": dtype ", t.scalar_type(), ", the gates have ", like.scalar_type());
+    if (t.sizes() != like.sizes()) refuse(name, ": shape ", t.sizes(), ", the gates have ", like.sizes());
+    if (t.size(-1) > 1 && t.stride(-1) != 1) refuse(name, ": strides ", t.strides(), ": a step's channels have to be contiguous");
+    return Place{(uint64_t)(uintptr_t)t.data_ptr(), t.stride(0), whole ? t.stride(1) : 0};
+}
+
+bool apart(const Sequences& q, const Place& p)
+{
+    const bool many = q.batch > 1, more = q.steps > 1;
+    if ((many && p.batch < q.channels) || (more && p.step < q.channels)) return false;
+    return !many || !more || p.batch / p.step >= q.steps || p.step / p.batch >= q.batch;
+}
+
+const at::Tensor& given(PyObject* o, const char* name)
+{
+    if (!THPVariable_Check(o)) refuse(name, ": expected a torch tensor on the HIP device, got ", Py_TYPE(o)->tp_name);
+    return THPVariable_Unpack(o);
+}
+
+// sequences(whole, gates, inputs, state, resets, (name, kind, tensor), ...) -> (packed
+// pictura_sequences, then for each tensor its address and, of kind "s" (the gates' shape
+// and type), its two strides).  Kind "f": float32 [batch, channels], contiguous, or None: 0;
+// "w": the same and written, so that its version goes up; "c": the states that a scan
+// saves.  whole: [batch, steps, channels], else one step, [batch, channels].
+PyObject* sequences(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    constexpr int64_t kSaved = 16;   // PICTURA_SCAN_STEPS
+    if (n < 5 || (n - 5) % 3) {
+        PyErr_SetString(PyExc_TypeError, "sequences(whole, gates, inputs, state, resets, name, kind, tensor, ...)");
+        return nullptr;
+    }
+    PyObject* result = nullptr;
+    try {
+        const bool whole = args[0] == Py_True;
+        const at::Tensor& gates = given(args[1], "gates");
+        const at::Tensor& inputs = given(args[2], "inputs");
+        if (gates.dim() != (whole ? 3 : 2) || gates.size(-1) < 1)
+            refuse("gates: shape ", gates.sizes(), ", expected ", whole ? "[batch, steps, channels]" : "[batch, channels]");
+        const at::Device dev = gates.device();
+        Sequences q{};
+        q.dtype = dtype_code(gates, "gates");
+        q.batch = gates.size(0);
+        q.steps = whole ? gates.size(1) : 1;
+        const int64_t channels = gates.size(-1);
+        if (channels > 0x7FFFFFFF || q.batch > 0x7FFFFFFF / channels || q.steps > 0x7FFFFFFF)
+            refuse("gates: shape ", gates.sizes(), ": batch times channels, and steps, have to be below 2^31");
+        q.channels = (int32_t)channels;
+        const Place g = place(gates, "gates", gates, whole), x = place(inputs, "inputs", gates, whole);
+        q.gates = g.at, q.gates_batch = g.batch, q.gates_step = g.step;
+        q.inputs = x.at, q.inputs_batch = x.batch, q.inputs_step = x.step;
+        auto floats = [&](PyObject* o, const char* name, int64_t rows) -> uint64_t {
+            if (o == Py_None) return 0;
+            const at::Tensor& t = given(o, name);
+            strided(t, name, dev);
+            const bool saved = rows >= 0;
+            if (t.scalar_type() != at::kFloat || t.dim() != (saved ? 3 : 2) || (saved && t.size(0) != rows) ||
+                t.size(saved) != q.batch || t.size(saved + 1) != channels || !t.is_contiguous())
+                refuse(name, ": ", t.scalar_type(), " ", t.sizes(), " with strides ", t.strides(), ", expected contiguous float32 [",
+                       saved ? std::to_string(rows) + ", " : "", q.batch, ", ", channels, "]");
+            return (uint64_t)(uintptr_t)t.data_ptr();
+        };
+        q.state = floats(args[3], "state", -1);
+        if (args[4] != Py_None) {
+            const at::Tensor& r = given(args[4], "resets");
+            strided(r, "resets", dev);
+            if (r.scalar_type() != at::kBool && r.scalar_type() != at::kByte)
+                refuse("resets: dtype ", r.scalar_type(), ", expected bool or uint8");
+            if (r.dim() != (whole ? 2 : 1) || r.size(0) != q.batch || (whole && r.size(1) != q.steps))
+                refuse("resets: shape ", r.sizes(), ", expected [", q.batch, whole ? ", " + std::to_string(q.steps) : "", "]");
+            q.resets = (uint64_t)(uintptr_t)r.data_ptr();
+            q.resets_batch = r.stride(0);
+            q.resets_step = whole ? r.stride(1) : 0;
+        }
+        std::vector<uint64_t> values;
+        for (Py_ssize_t k = 5; k < n; k += 3) {
+            const char* name = PyUnicode_AsUTF8(args[k]);
+            const char* kind = PyUnicode_AsUTF8(args[k + 1]);
+            if (!name || !kind) refuse("a name is no text");
+            if (*kind == 's' || *kind == 'o') {
+                const Place p = place(given(args[k + 2], name), name, gates, whole);
+                if (*kind == 'o' && !apart(q, p))
+                    refuse(name, ": strides ", THPVariable_Unpack(args[k + 2]).strides(), ": elements overlap");
+                values.insert(values.end(), {p.at, (uint64_t)p.batch, (uint64_t)p.step});
+            } else {
+                values.push_back(floats(args[k + 2], name, *kind == 'c' ? (q.steps + kSaved - 1) / kSaved : -1));
+            }
+        }
+        for (Py_ssize_t k = 5; k < n; k += 3)
+            if (*PyUnicode_AsUTF8(args[k + 1]) == 'w' && args[k + 2] != Py_None) {
+                const at::Tensor& t = THPVariable_Unpack(args[k + 2]);
+                if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+            }
+        result = PyTuple_New(1 + (Py_ssize_t)values.size());
+        PyObject* packed = PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&q), sizeof(q));
+        if (!result || !packed) refuse("out of memory");
+        PyTuple_SET_ITEM(result, 0, packed);
+        for (size_t k = 0; k < values.size(); ++k) {
+            PyObject* o = PyLong_FromUnsignedLongLong(values[k]);
+            if (!o) refuse("out of memory");
+            PyTuple_SET_ITEM(result, 1 + (Py_ssize_t)k, o);
+        }
+        return result;
+    } catch (const std::exception& e) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, e.what());
+    }
+    Py_XDECREF(result);
+    return nullptr;
+}
+
 PyMethodDef methods[] = {{"outputs", outputs, METH_VARARGS, "Addresses of fp32 tensors of the parameters' sizes."},
                          {"vectors", (PyCFunction)(void (*)())vectors, METH_FASTCALL, "Addresses of vectors of one length."},
+                         {"sequences", (PyCFunction)(void (*)())sequences, METH_FASTCALL, "A packed pictura_sequences."},
                          {"fill", fill, METH_VARARGS, "Fill a table of pictura_adamw_tensor from lists of tensors."},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -106,6 +106,7 @@ ADAMW_TENSOR = np.dtype([(n, np.uint64) for n in ("param", "grad", "exp_avg", "e
                         [("n", np.int64), ("param_dtype", np.int32), ("grad_dtype", np.int32)], align=True)
 ADAMW_BLOCK = 256
 MAX_ACTIONS = 1 << 20
+SCAN_STEPS = 16   # steps between the states that a scan saves
 POLICY_STATS = ("loss", "policy_loss", "value_loss", "entropy", "approx_kl", "clip_fraction")
 
 
@@ -167,6 +168,15 @@ _lib.pictura_adamw_step.argtypes = [_P, _P, ctypes.c_int32, _P]
 _lib.pictura_adamw_step.restype = ctypes.c_int32
 _lib.pictura_adamw_moments.argtypes = [_P, ctypes.c_int32, _P, _P, _P]
 _lib.pictura_adamw_moments.restype = ctypes.c_int32
+_lib.pictura_gated_scan_workspace.argtypes = [_P, _P]
+_lib.pictura_gated_scan_workspace.restype = ctypes.c_int32
+_lib.pictura_gated_scan.argtypes = [_P, _P, ctypes.c_int64, ctypes.c_int64, _P, _P, _P, ctypes.c_uint64, _P]
+_lib.pictura_gated_scan.restype = ctypes.c_int32
+_lib.pictura_gated_scan_gradient.argtypes = [_P, _P] + [_P, ctypes.c_int64, ctypes.c_int64, _P] + \
+    [_P, ctypes.c_int64, ctypes.c_int64] * 2 + [_P, _P, ctypes.c_uint64, _P]
+_lib.pictura_gated_scan_gradient.restype = ctypes.c_int32
+_lib.pictura_gated_step.argtypes = [_P, _P, ctypes.c_int64, _P, _P]
+_lib.pictura_gated_step.restype = ctypes.c_int32
 
 EXPORTED = ["pictura_create", "pictura_destroy", "pictura_last_error", "pictura_scene_upload",
             "pictura_bin_scene", "pictura_render_views", "pictura_agents_step", "pictura_bins_info",
@@ -175,7 +185,8 @@ EXPORTED = ["pictura_create", "pictura_destroy", "pictura_last_error", "pictura_
             "pictura_device_errors", "pictura_selftest_rcp_noalloc", "pictura_store_probe",
             "pictura_encoder_workspace", "pictura_encode_views", "pictura_sample_actions",
             "pictura_policy_loss_workspace", "pictura_policy_loss", "pictura_grad_norm_workspace", "pictura_grad_norm",
-            "pictura_adamw_step", "pictura_adamw_moments"]
+            "pictura_adamw_step", "pictura_adamw_moments", "pictura_gated_scan_workspace", "pictura_gated_scan",
+            "pictura_gated_scan_gradient", "pictura_gated_step"]
 DEVERR_RING_WAIT = 1
 
 STAT_NAMES = ["view_tiles", "cells_in_rect", "cells_prefiltered", "cells_visible", "cand_tris", "boxes_visible",
@@ -697,6 +708,65 @@ def pictura_adamw_moments(table, exp_avg_out, exp_avg_sq_out, device):
     st = _call(device, _lib.pictura_adamw_moments, at, len(table), exp_avg_out.ctypes.data, exp_avg_sq_out.ctypes.data)
     if st != OK:
         raise PicturaError(st, "adamw_moments: a value out of range")
+
+
+# --- a memory over the steps of an episode ------------------------------------------
+
+def _sequences(whole, gates, inputs, state, resets, *named):
+    """(packed pictura_sequences, addresses and strides of `named`), everything checked
+    that the kernels rely on."""
+    from paper_2607_26005_amd import _tensors
+    try:
+        out = _tensors.sequences(whole, gates, inputs, state, resets, *named)
+    except ValueError as e:
+        raise PicturaError(EINVAL, str(e)) from None
+    if not gates.is_cuda:
+        _check_device(gates, "gates", None)
+    return out
+
+
+def _scan_workspace(q, device):
+    import torch
+    need = ctypes.c_uint64()
+    st = _lib.pictura_gated_scan_workspace(q, ctypes.addressof(need))
+    if st != OK:
+        raise PicturaError(st, "gated_scan_workspace: sizes out of range")
+    return torch.empty(need.value, dtype=torch.uint8, device=device), need.value
+
+
+def pictura_gated_scan(gates, inputs, out, last_state, saved=None, state=None, resets=None):
+    """Gated linear recurrence over sequences: gates, inputs and out [batch, steps,
+    channels] of one type (float32, bfloat16 or float16), channels contiguous, the other
+    strides their own; state and last_state float32 [batch, channels]; resets bool or
+    uint8 [batch, steps]; saved float32 [ceil(steps / SCAN_STEPS), batch, channels] where
+    a gradient is wanted.  On the current stream in a workspace of the caching allocator."""
+    q, *o, la, sa = _sequences(True, gates, inputs, state, resets, "out", "o", out, "last_state", "f", last_state,
+                               "saved", "c", saved)
+    ws, size = _scan_workspace(q, gates.device)
+    st = _call(gates.device, _lib.pictura_gated_scan, q, *o, la, sa, ws.data_ptr(), size)
+    if st != OK:
+        raise PicturaError(st, "gated_scan failed")
+
+
+def pictura_gated_scan_gradient(gates, inputs, saved, dout, dlast, dgates, dinputs, dstate, resets=None):
+    """Gradient of pictura_gated_scan with the `saved` of that call: dout, dgates and
+    dinputs as gates, dlast (or None: zeros) and dstate (or None: not wanted) float32
+    [batch, channels]."""
+    q, sa, *d = _sequences(True, gates, inputs, None, resets, "saved", "c", saved, "dout", "s", dout, "dlast", "f", dlast,
+                           "dgates", "o", dgates, "dinputs", "o", dinputs, "dstate", "f", dstate)
+    ws, size = _scan_workspace(q, gates.device)
+    st = _call(gates.device, _lib.pictura_gated_scan_gradient, q, sa, *d, ws.data_ptr(), size)
+    if st != OK:
+        raise PicturaError(st, "gated_scan_gradient failed")
+
+
+def pictura_gated_step(gates, inputs, out, state, resets=None):
+    """One step of the recurrence: gates, inputs and out [batch, channels], state float32
+    [batch, channels] replaced by what is remembered after it, resets [batch]."""
+    q, oo, ob, _, sa = _sequences(False, gates, inputs, None, resets, "out", "o", out, "state", "w", state)
+    st = _call(gates.device, _lib.pictura_gated_step, q, oo, ob, sa)
+    if st != OK:
+        raise PicturaError(st, "gated_step failed")
 
 
 # --- device-resident agents ------------------------------------------------------

@@ -1,0 +1,67 @@
+"""Plain 64-bit forms of the memory's operators on the host, step by step, with bounds of
+the error that fp32 arithmetic may leave.
+
+The bounds are running ones, u = 2^-24: a rounded operation adds u of its result, the
+gate's two parts come to within 10 u of their own (a hardware exponential off by up to a
+unit, 2 u; two roundings of its correction; 1 + e, the refined reciprocal, their product
+and the difference from 1, with the exponential's error passed on), and errors travel
+through the recurrence with the factors of the values.  Magnitudes stand for values, so
+that the bounds hold for any split of the steps."""
+import torch
+
+U = 2.0 ** -24
+GATE = 10
+
+
+def half_step(t, dtype):
+    """Half a unit of `dtype` at values t: what one rounding may change (subnormals too)."""
+    info = torch.finfo(dtype)
+    return t.abs() * (info.eps / 2) + info.smallest_normal * info.eps / 2
+
+
+def scan(gates, inputs, state=None, resets=None):
+    """(h, last, bound of h, bound of last) of [batch, steps, channels] tensors."""
+    g, x = gates.detach().cpu().double(), inputs.detach().cpu().double()
+    B, T, C = x.shape
+    h = torch.zeros(B, C, dtype=torch.float64) if state is None else state.detach().cpu().double()
+    A, e = h.abs(), torch.zeros_like(h)
+    out, bound, mags = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    for t in range(T):
+        a, b = g[:, t].sigmoid(), (-g[:, t]).sigmoid()
+        if resets is not None:
+            began = resets.cpu().bool()[:, t, None]
+            h, A, e = (torch.where(began, torch.zeros_like(v), v) for v in (h, A, e))
+        e = a * e + U * ((GATE + 4) * a * A + (GATE + 4) * b * x[:, t].abs())
+        h, A = a * h + b * x[:, t], a * A + b * x[:, t].abs()
+        e = e + U * A
+        out[:, t], bound[:, t], mags[:, t] = h, e, A
+    return out, h, bound, e
+
+
+def scan_gradient(gates, inputs, state, resets, dout, dlast):
+    """(dgates, dinputs, dstate) and the bounds of the three."""
+    g, x, dy = (t.detach().cpu().double() for t in (gates, inputs, dout))
+    B, T, C = x.shape
+    h, last, eh, _ = scan(gates, inputs, state, resets)
+    mag = scan(gates, inputs.abs(), None if state is None else state.abs(), resets)[0]
+    first = torch.zeros(B, C, dtype=torch.float64) if state is None else state.detach().cpu().double()
+    c = torch.zeros(B, C, dtype=torch.float64) if dlast is None else dlast.detach().cpu().double()
+    cm, ec = c.abs(), torch.zeros_like(c)
+    dg, dx, bg, bx = (torch.empty_like(x) for _ in range(4))
+    zero = torch.zeros_like(c)
+    for t in range(T - 1, -1, -1):
+        a, b = g[:, t].sigmoid(), (-g[:, t]).sigmoid()
+        G, Gm = dy[:, t] + c, dy[:, t].abs() + cm
+        eG = ec + U * Gm
+        before, bm, eb = (h[:, t - 1], mag[:, t - 1], eh[:, t - 1]) if t else (first, first.abs(), zero)
+        if resets is not None:
+            began = resets.cpu().bool()[:, t, None]
+            before, bm, eb = (torch.where(began, zero, v) for v in (before, bm, eb))
+        d, dm = before - x[:, t], bm + x[:, t].abs()
+        dx[:, t], bx[:, t] = b * G, b * eG + (GATE + 2) * U * b * Gm
+        dg[:, t] = a * b * G * d
+        bg[:, t] = a * b * (dm * eG + Gm * (eb + U * dm) + (2 * GATE + 4) * U * Gm * dm)
+        c, cm, ec = a * G, a * Gm, a * eG + (GATE + 4) * U * a * Gm
+        if resets is not None:
+            c, cm, ec = (torch.where(began, zero, v) for v in (c, cm, ec))
+    return (dg, dx, c), (bg, bx, ec)

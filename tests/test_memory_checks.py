@@ -1,0 +1,143 @@
+"""The memory's operators refuse what their kernels could not use safely, before any
+device work: host tensors stand in for device ones (no GPU needed)."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2607_26005_amd import memory, pictura
+
+B, T, C = 2, 5, 6
+
+
+@pytest.fixture(autouse=True)
+def host_is_device(request, monkeypatch):
+    if "device" not in request.node.name:
+        monkeypatch.setattr(pictura, "_check_device", lambda t, name, ctx: None)
+
+
+def _raises(match, fn, *a, **k):
+    with pytest.raises(pictura.PicturaError, match=match) as e:
+        fn(*a, **k)
+    assert e.value.status == pictura.EINVAL
+
+
+z = torch.zeros
+
+
+@pytest.mark.parametrize("match, bad", [
+    ("gates: expected a torch tensor", dict(gates=[[0.0]])),
+    ("inputs: expected a torch tensor", dict(inputs=None)),
+    ("gates: shape", dict(gates=z(T, C))),
+    ("inputs: shape", dict(inputs=z(T, C))),
+    ("gates: dtype", dict(gates=z(B, T, C).double(), inputs=z(B, T, C).double())),
+    ("gates: shape", dict(gates=z(B, T, 0), inputs=z(B, T, 0))),
+    ("gates: strides", dict(gates=z(B, C, T).transpose(1, 2))),
+    ("gates: expected a plain", dict(gates=torch._neg_view(z(B, T, C)))),
+    ("inputs: dtype", dict(inputs=z(B, T, C).half())),
+    ("inputs: shape", dict(inputs=z(B, T + 1, C))),
+    ("inputs: strides", dict(inputs=z(B, T, 2 * C)[..., ::2])),
+    ("state: ", dict(state=z(B, C).half())),
+    ("state: ", dict(state=z(B, C + 1))),
+    ("state: ", dict(state=z(C, B).t())),
+    ("state: expected a torch tensor", dict(state=0.0)),
+    ("resets: dtype", dict(resets=z(B, T))),
+    ("resets: shape", dict(resets=z(B, T + 1, dtype=torch.bool))),
+    ("resets: shape", dict(resets=z(T, dtype=torch.bool))),
+])
+def test_scan_refuses(match, bad):
+    _raises(match, memory.gated_scan, **dict(dict(gates=z(B, T, C), inputs=z(B, T, C)), **bad))
+    if "inputs" not in bad:   # and where a gradient is wanted
+        _raises(match, memory.gated_scan, **dict(dict(gates=z(B, T, C), inputs=z(B, T, C, requires_grad=True)), **bad))
+
+
+@pytest.mark.parametrize("match, bad", [
+    ("gates: shape", dict(gates=z(B, T, C))),
+    ("inputs: dtype", dict(inputs=z(B, C).half())),
+    ("inputs: expected a torch tensor", dict(inputs=None)),
+    ("state: ", dict(state=z(B, C).half())),
+    ("state: ", dict(state=z(B, 2 * C)[:, :C])),
+    ("resets: shape", dict(resets=z(B, T, dtype=torch.bool))),
+    ("out: dtype", dict(out=z(B, C).half())),
+    ("out: shape", dict(out=z(B + 1, C))),
+    ("out: strides", dict(out=z(1, C).expand(B, C))),
+])
+def test_step_refuses(match, bad):
+    _raises(match, memory.gated_step, **dict(dict(gates=z(B, C), inputs=z(B, C), state=z(B, C)), **bad))
+
+
+def test_outputs_of_the_scan_are_checked():
+    ok = lambda: dict(gates=z(B, T, C), inputs=z(B, T, C), out=z(B, T, C), last_state=z(B, C))
+    _raises("out: shape", pictura.pictura_gated_scan, **dict(ok(), out=z(B, T, C + 1)))
+    _raises("last_state: ", pictura.pictura_gated_scan, **dict(ok(), last_state=z(B)))
+    _raises("saved: ", pictura.pictura_gated_scan, **dict(ok(), saved=z(2, B, C)))
+    _raises("out: strides .* overlap", pictura.pictura_gated_scan, **dict(ok(), out=z(B, 1, C).expand(B, T, C)))
+    _raises("out: strides .* overlap", pictura.pictura_gated_scan, **dict(ok(), out=z(20 * C).as_strided((B, T, C), (C, C, 1))))
+    g = lambda **k: dict(dict(gates=z(B, T, C), inputs=z(B, T, C), saved=z(1, B, C), dout=z(B, T, C), dlast=z(B, C),
+                              dgates=z(B, T, C), dinputs=z(B, T, C), dstate=z(B, C)), **k)
+    _raises("dout: dtype", pictura.pictura_gated_scan_gradient, **g(dout=z(B, T, C).half()))
+    _raises("dlast: ", pictura.pictura_gated_scan_gradient, **g(dlast=z(B, C + 1)))
+    _raises("dgates: shape", pictura.pictura_gated_scan_gradient, **g(dgates=z(B, C)))
+    _raises("dinputs: strides .* overlap", pictura.pictura_gated_scan_gradient, **g(dinputs=z(1, T, C).expand(B, T, C)))
+    _raises("dstate: ", pictura.pictura_gated_scan_gradient, **g(dstate=z(B, C).half()))
+
+
+def test_host_tensors_are_refused_for_their_device():
+    _raises("expected the HIP device", memory.gated_scan, z(B, T, C), z(B, T, C))
+    _raises("expected the HIP device", memory.gated_step, z(B, C), z(B, C), z(B, C))
+
+
+# --- the C entries themselves: bad arguments come back as a status, before any launch
+
+class _Sequences(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("gates", "inputs", "state", "resets")] + \
+               [(n, ctypes.c_int64) for n in ("gates_batch", "gates_step", "inputs_batch", "inputs_step", "resets_batch",
+                                              "resets_step", "batch", "steps")] + \
+               [("channels", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+def _q(**over):
+    q = _Sequences(64, 64, None, None, T * C, C, T * C, C, 0, 0, B, T, C, 0)
+    for k, v in over.items():
+        setattr(q, k, v)
+    return q
+
+
+def test_c_entries_refuse():
+    L, ref = pictura._lib, ctypes.byref
+    scan = lambda q=None, out=64, ob=T * C, os_=C, last=64, saved=64, ws=256, n=1 << 40: \
+        L.pictura_gated_scan(ref(q or _q()), out, ob, os_, last, saved, ws, n, None)
+    grad = lambda q=None, saved=64, dout=64, db=T * C, dlast=64, dg=64, gb=T * C, dx=64, xs=C, ds=64, ws=256, n=1 << 40: \
+        L.pictura_gated_scan_gradient(ref(q or _q()), saved, dout, db, C, dlast, dg, gb, C, dx, T * C, xs, ds, ws, n, None)
+    step = lambda q=None, out=64, ob=C, state=64: L.pictura_gated_step(ref(q or _q(steps=1)), out, ob, state, None)
+    sizes = [dict(dtype=3), dict(batch=-1), dict(steps=-1), dict(steps=1 << 31), dict(channels=0), dict(batch=1 << 31)]
+    inputs = [dict(gates=None), dict(inputs=None), dict(gates=66), dict(inputs=65), dict(state=66), dict(gates_step=-1),
+              dict(inputs_batch=-1), dict(resets_step=-1)]
+    for over in sizes + inputs:
+        assert scan(_q(**over)) == pictura.EINVAL, over
+        assert grad(_q(**over)) == pictura.EINVAL, over
+        assert step(_q(**dict(dict(steps=1), **over))) == pictura.EINVAL, over
+    for k in (dict(out=None), dict(out=66), dict(ob=T * C - 1), dict(os_=C - 1), dict(last=66), dict(saved=66), dict(ws=None),
+              dict(ws=128), dict(n=8)):
+        assert scan(**k) == pictura.EINVAL, k
+    for k in (dict(saved=None), dict(saved=66), dict(dout=None), dict(dout=66), dict(db=-1), dict(dlast=66), dict(dg=None), dict(dg=66),
+              dict(gb=T * C - 1), dict(dx=None), dict(xs=0), dict(ds=66), dict(ws=None), dict(n=8)):
+        assert grad(**k) == pictura.EINVAL, k
+    for k in (dict(out=None), dict(out=66), dict(ob=C - 1), dict(state=None), dict(state=66), dict(q=_q())):
+        assert step(**k) == pictura.EINVAL, k
+    assert L.pictura_gated_scan(None, 64, T * C, C, 64, 64, 256, 1 << 40, None) == pictura.EINVAL
+    out = ctypes.c_uint64()
+    assert L.pictura_gated_scan_workspace(None, ctypes.addressof(out)) == pictura.EINVAL
+    assert L.pictura_gated_scan_workspace(ref(_q()), None) == pictura.EINVAL
+    assert scan(_q(batch=0, gates=None)) == pictura.OK
+
+
+def test_workspace_covers_every_split():
+    """However the steps are cut, maps of all segments and groups fit."""
+    L = pictura._lib
+    need = ctypes.c_uint64()
+    for batch, steps, channels in ((1, 1, 1), (1, 10 ** 6, 1), (1, 65521, 1024), (3, 8191, 331), (2048, 128, 512),
+                                   (1, 2 ** 31 - 1, 2), (2 ** 20, 3, 2047)):
+        q = _q(batch=batch, steps=steps, channels=channels)
+        assert L.pictura_gated_scan_workspace(ctypes.byref(q), ctypes.addressof(need)) == pictura.OK
+        assert need.value <= 256 + (512 + 32) * 8 * max(batch * channels, 64 * 4096)
