@@ -640,6 +640,61 @@ pictura_status pictura_gated_scan_gradient(const pictura_sequences* sequences, c
  * type and may be the inputs' or the gates' own memory (same stride). */
 pictura_status pictura_gated_step(const pictura_sequences* sequences, void* out, int64_t out_batch, float* state, void* stream);
 
+#define PICTURA_MAX_NORM (1 << 16)   /* most elements of a normed row */
+
+/* Kinds of 8-bit codes. */
+#define PICTURA_INT8 0   /* two's complement, -127..127 */
+#define PICTURA_E4M3 1   /* sign, 4 bits of exponent, 3 of mantissa, no infinities, 448 at most (OCP e4m3fn) */
+
+/* Rows to be normed: row n has `width` values of `dtype` from x + n * x_stride on (in
+ * elements; 0: the same row for all), and from residual + n * residual_stride where
+ * that is not NULL.  weight: [width] of weight_dtype, `dtype` or PICTURA_F32. */
+typedef struct {
+    const void* x;
+    const void* residual;
+    const void* weight;
+    int64_t x_stride, residual_stride;
+    int64_t rows;          /* 0..2^31 - 1 */
+    int32_t width;         /* 1..PICTURA_MAX_NORM */
+    int32_t dtype;         /* PICTURA_F32, PICTURA_BF16 or PICTURA_F16 */
+    int32_t weight_dtype;
+    float eps;             /* 0 or more, finite */
+} pictura_norm;
+
+/* Root-mean-square norm with the residual's addition: s = x + residual, rounded to dtype,
+ * q = 1 / sqrt(mean(s^2) + eps), out = (s q) weight, rounded to dtype once.  The mean is
+ * taken in fp64 and q rounded to fp32.  sum (or NULL) receives s and may be x's or
+ * residual's own memory (same stride), as may out; factors (or NULL), fp32 [rows], receives
+ * q.  EINVAL: a null or misaligned pointer, or a value out of range. */
+pictura_status pictura_rms_norm(const pictura_norm* norm, void* sum, int64_t sum_stride, void* out, int64_t out_stride,
+                                float* factors, void* stream);
+
+/* The norm with an output in 8 bits: with y = (s q) weight in fp32, M the largest |y| of the
+ * row and L the kind's largest value (127 or 448), scales[n] = M / L and the codes are
+ * y (L (1 / M)), every operation rounded to fp32, then to the nearest of the kind, ties to
+ * even: they stand for code * scales[n].  A row whose M is below 2^-100 gets scale 0 and codes 0; an infinity or a NaN
+ * makes the values of its row NaN.  codes: one byte each, rows codes_stride apart. */
+pictura_status pictura_rms_norm_codes(const pictura_norm* norm, int32_t kind, void* sum, int64_t sum_stride, void* codes,
+                                      int64_t codes_stride, float* scales, void* stream);
+
+/* What codes stand for, in fp32: out[n * out_stride + i] = code * scales[n]. */
+pictura_status pictura_row_values(const void* codes, int64_t codes_stride, const float* scales, int32_t kind, int64_t rows,
+                                  int32_t width, float* out, int64_t out_stride, void* stream);
+
+/* Bytes of workspace that the gradient takes (reads rows, width and the types alone). */
+pictura_status pictura_rms_norm_gradient_workspace(const pictura_norm* norm, uint64_t* bytes);
+
+/* Gradient of pictura_rms_norm: norm->x is its sum (what it normed), residual NULL, factors
+ * its factors; from dout (of out) and dsum (of sum; or NULL: zeros), with k = dout weight
+ * and u = x q, dx = q (k - u mean(k u)) + dsum, the gradient of x and of the residual
+ * alike, rounded to dtype once, and dweight = sum over the rows of dout u, in the weight's
+ * type, summed in a fixed order.  dx may be dout's or dsum's own memory (same stride).
+ * With no rows dweight is 0.  Errors as pictura_rms_norm; workspace: device memory,
+ * 256-byte aligned, in use until the call's work on the stream is done. */
+pictura_status pictura_rms_norm_gradient(const pictura_norm* norm, const float* factors, const void* dout, int64_t dout_stride,
+                                         const void* dsum, int64_t dsum_stride, void* dx, int64_t dx_stride, void* dweight,
+                                         void* workspace, uint64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,6 +10,8 @@
 #include <sstream>
 #include <stdexcept>
 #include <string>
+#include <tuple>
+#include <utility>
 #include <vector>
 
 namespace {
@@ -362,9 +364,117 @@ PyObject* sequences(PyObject*, PyObject* const* args, Py_ssize_t n)
     return nullptr;
 }
 
+// pictura_norm (include/pictura.h)
+struct Norm {
+    uint64_t x, residual, weight;
+    int64_t x_stride, residual_stride, rows;
+    int32_t width, dtype, weight_dtype;
+    float eps;
+};
+static_assert(sizeof(Norm) == 64, "pictura_norm");
+
+// (address, elements between rows) of a [rows, width] tensor whose rows are contiguous; written: and apart.
+std::pair<uint64_t, int64_t> rows_at(const at::Tensor& t, const char* name, const at::Tensor& like, bool written)
+{
+    strided(t, name, like.device());
+    if (t.sizes() != like.sizes()) refuse(name, ": shape ", t.sizes(), ", expected ", like.sizes());
+    const int64_t stride = t.size(0) > 1 ? t.stride(0) : t.size(1);
+    if ((t.size(1) > 1 && t.stride(1) != 1) || (written && stride < t.size(1)))
+        refuse(name, ": strides ", t.strides(), ": a row has to be contiguous", written ? ", and apart from the next" : "");
+    return {(uint64_t)(uintptr_t)t.data_ptr(), stride};
+}
+
+// norm(x, weight, residual, eps, (name, kind, tensor), ...) -> (packed pictura_norm, then
+// for each tensor its address and, of kinds "s" (x's shape and type), "o" (the same,
+// written) and "b" (one byte each, written), the elements between its rows).  Kind "f":
+// float32 [rows]; "w": the weight's shape and type.  None: 0, except of kind "o".
+PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    constexpr int64_t kMost = 1 << 16;   // PICTURA_MAX_NORM
+    if (n < 4 || (n - 4) % 3) {
+        PyErr_SetString(PyExc_TypeError, "norm(x, weight, residual, eps, name, kind, tensor, ...)");
+        return nullptr;
+    }
+    PyObject* result = nullptr;
+    try {
+        const at::Tensor& x = given(args[0], "x");
+        const at::Tensor& weight = given(args[1], "weight");
+        Norm q{};
+        q.dtype = dtype_code(x, "x");
+        if (x.dim() != 2 || x.size(1) < 1 || x.size(1) > kMost || x.size(0) > 0x7FFFFFFF)
+            refuse("x: shape ", x.sizes(), ": rows of 1 to ", kMost, " elements, fewer than 2^31 of them");
+        q.rows = x.size(0);
+        q.width = (int32_t)x.size(1);
+        std::tie(q.x, q.x_stride) = rows_at(x, "x", x, false);
+        strided(weight, "weight", x.device());
+        q.weight_dtype = dtype_code(weight, "weight");
+        if (weight.dim() != 1 || weight.size(0) != q.width || !weight.is_contiguous() ||
+            (weight.scalar_type() != x.scalar_type() && weight.scalar_type() != at::kFloat))
+            refuse("weight: ", weight.scalar_type(), " ", weight.sizes(), " with strides ", weight.strides(), ", expected contiguous ",
+                   x.scalar_type(), " or float32 [", q.width, "]");
+        q.weight = (uint64_t)(uintptr_t)weight.data_ptr();
+        auto same = [&](const at::Tensor& t, const char* name) {
+            if (t.scalar_type() != x.scalar_type()) refuse(name, ": dtype ", t.scalar_type(), ", the others have ", x.scalar_type());
+        };
+        if (args[2] != Py_None) {
+            const at::Tensor& r = given(args[2], "residual");
+            same(r, "residual");
+            std::tie(q.residual, q.residual_stride) = rows_at(r, "residual", x, false);
+        }
+        const double eps = PyFloat_AsDouble(args[3]);
+        if (PyErr_Occurred() || !(eps >= 0) || eps > 3e38) {
+            PyErr_Clear();
+            refuse("eps: expected a finite number, 0 or more");
+        }
+        q.eps = (float)eps;
+        std::vector<uint64_t> values;
+        for (Py_ssize_t k = 4; k < n; k += 3) {
+            const char* name = PyUnicode_AsUTF8(args[k]);
+            const char* kind = PyUnicode_AsUTF8(args[k + 1]);
+            if (!name || !kind) refuse("a name is no text");
+            const bool vector = *kind == 'f' || *kind == 'w';
+            if (args[k + 2] == Py_None && *kind != 'o') {
+                values.push_back(0);
+                if (!vector) values.push_back(0);
+                continue;
+            }
+            const at::Tensor& t = given(args[k + 2], name);
+            if (vector) {
+                strided(t, name, x.device());
+                const int64_t count = *kind == 'f' ? q.rows : q.width;
+                const at::ScalarType type = *kind == 'f' ? at::kFloat : weight.scalar_type();
+                if (t.scalar_type() != type || t.dim() != 1 || t.size(0) != count || !t.is_contiguous())
+                    refuse(name, ": ", t.scalar_type(), " ", t.sizes(), ", expected contiguous ", type, " [", count, "]");
+                values.push_back((uint64_t)(uintptr_t)t.data_ptr());
+                continue;
+            }
+            if (*kind != 'b') same(t, name);
+            else if (t.scalar_type() != at::kChar && t.scalar_type() != at::kFloat8_e4m3fn)
+                refuse(name, ": dtype ", t.scalar_type(), ", expected int8 or float8_e4m3fn");
+            const auto at = rows_at(t, name, x, *kind != 's');
+            values.insert(values.end(), {at.first, (uint64_t)at.second});
+        }
+        result = PyTuple_New(1 + (Py_ssize_t)values.size());
+        PyObject* packed = PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&q), sizeof(q));
+        if (!result || !packed) refuse("out of memory");
+        PyTuple_SET_ITEM(result, 0, packed);
+        for (size_t k = 0; k < values.size(); ++k) {
+            PyObject* o = PyLong_FromUnsignedLongLong(values[k]);
+            if (!o) refuse("out of memory");
+            PyTuple_SET_ITEM(result, 1 + (Py_ssize_t)k, o);
+        }
+        return result;
+    } catch (const std::exception& e) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, e.what());
+    }
+    Py_XDECREF(result);
+    return nullptr;
+}
+
 PyMethodDef methods[] = {{"outputs", outputs, METH_VARARGS, "Addresses of fp32 tensors of the parameters' sizes."},
                          {"vectors", (PyCFunction)(void (*)())vectors, METH_FASTCALL, "Addresses of vectors of one length."},
                          {"sequences", (PyCFunction)(void (*)())sequences, METH_FASTCALL, "A packed pictura_sequences."},
+                         {"norm", (PyCFunction)(void (*)())norm, METH_FASTCALL, "A packed pictura_norm."},
                          {"fill", fill, METH_VARARGS, "Fill a table of pictura_adamw_tensor from lists of tensors."},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,16 +1,16 @@
 """What a policy remembers over the steps of an episode, on the device: a gated linear
-recurrence.
+recurrence, and the root-mean-square norm between its layers.
 
 The paper's policy decides from the views of one step (Sec. 3.3); a policy that should
 know what it saw before carries a state from step to step.  These functions are the
 layers of one: in training they run over whole sequences of steps (rollouts, recorded
 drives, several of either packed behind one another), when acting one step at a time on
 a state that stays on the device.  Every one runs in the library's kernels
-(csrc/pictura_memory.hip) on the current stream and never waits for the device.
+(csrc/pictura_memory.hip, csrc/pictura_norm.hip) on the current stream and never waits for the device.
 """
 from __future__ import annotations
 
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -97,3 +97,107 @@ def gated_step(gates: torch.Tensor, inputs: torch.Tensor, state: torch.Tensor, r
         out = torch.empty(inputs.shape, dtype=inputs.dtype, device=inputs.device)
     pictura.pictura_gated_step(gates, inputs, out, state, resets)
     return out
+
+
+def _rows(t, name: str, like=None) -> torch.Tensor:
+    """t [..., width] as rows (a copy where its strides allow no view of them)."""
+    if not isinstance(t, torch.Tensor) or t.dim() < 1:
+        raise PicturaError(EINVAL, f"{name}: expected a torch tensor [..., width] on the HIP device, got {type(t).__name__}")
+    if like is not None and t.shape != like.shape:
+        raise PicturaError(EINVAL, f"{name}: shape {tuple(t.shape)}, x has {tuple(like.shape)}")
+    if t.dim() == 2 and t.stride(1) == 1:
+        return t
+    if t.shape[-1] == 0:
+        raise PicturaError(EINVAL, f"{name}: shape {tuple(t.shape)}: rows of 1 to {pictura.MAX_NORM} elements")
+    t = t.reshape(t.numel() // t.shape[-1], t.shape[-1])
+    return t if t.stride(1) == 1 or t.shape[1] == 1 else t.clone(memory_format=torch.contiguous_format)
+
+
+def _normed(x, weight, residual, eps, save):
+    rows = _rows(x, "x")
+    out = torch.empty(rows.shape, dtype=x.dtype, device=x.device)
+    total = res = None
+    if residual is not None:
+        res, total = _rows(residual, "residual", x), torch.empty_like(out)
+    factors = torch.empty(rows.shape[0], dtype=torch.float32, device=x.device) if save else None
+    pictura.pictura_rms_norm(rows, weight, out, total, res, eps, factors)
+    return rows if total is None else total, out, factors
+
+
+class _RMSNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        total, out, factors = _normed(x.detach(), weight.detach(), None if residual is None else residual.detach(), eps, True)
+        ctx.set_materialize_grads(False)
+        ctx.shape = x.shape
+        if residual is None:
+            ctx.save_for_backward(weight, factors, x)
+            return out.view(x.shape)
+        total = total.view(x.shape)
+        ctx.save_for_backward(weight, factors, total)
+        return out.view(x.shape), total
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, dsum=None):
+        weight, factors, total = ctx.saved_tensors
+        if dout is None:
+            if dsum is None:
+                return None, None, None, None
+            return dsum, torch.zeros_like(weight) if ctx.needs_input_grad[1] else None, dsum, None
+        rows = _rows(total, "x")
+        dx, dw = torch.empty(rows.shape, dtype=rows.dtype, device=rows.device), torch.empty_like(weight)
+        pictura.pictura_rms_norm_gradient(rows, weight, factors, _rows(dout.resolve_neg(), "dout"), dx, dw,
+                                          None if dsum is None else _rows(dsum.resolve_neg(), "dsum"))
+        dx = dx.view(ctx.shape)
+        return dx, dw, dx if ctx.needs_input_grad[2] else None, None
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6):
+    """y = s / sqrt(mean(s^2) + eps) * weight over the last dimension of s = x + residual.
+    Returns y, or with a residual (y, s): s, rounded to the type, is the residual that goes on.
+
+    x and residual: float32, bfloat16 or float16, rows of 1 to 65,536 (tensors whose rows do
+    not stand at one distance are copied first); weight of that type or float32.  The mean is
+    taken in 64 bits, the rest in float32.  Gradients flow to x, residual and weight."""
+    for name, t in (("x", x), ("weight", weight), ("residual", residual)):
+        if not isinstance(t, torch.Tensor) and (t is not None or name != "residual"):
+            raise PicturaError(EINVAL, f"{name}: expected a torch tensor on the HIP device, got {type(t).__name__}")
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (residual is not None and residual.requires_grad)):
+        return _RMSNorm.apply(x, weight, residual, eps)
+    total, out, _ = _normed(x, weight, residual, eps, False)
+    return out.view(x.shape) if residual is None else (out.view(x.shape), total.view(x.shape))
+
+
+class RowCodes(NamedTuple):
+    """Rows in 8 bits: what a code stands for is its value times the scale of its row."""
+    codes: torch.Tensor            # int8 or float8_e4m3fn, the input's shape
+    scales: torch.Tensor           # float32 [...], one for each row
+    sum: Optional[torch.Tensor]    # x + residual, where there is a residual
+
+    def values(self, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """What the codes stand for, float32 (in `out`, contiguous, where that is given)."""
+        rows = _rows(self.codes, "codes")
+        if out is None:
+            out = torch.empty(self.codes.shape, dtype=torch.float32, device=self.codes.device)
+        elif not isinstance(out, torch.Tensor) or out.shape != self.codes.shape or not out.is_contiguous():
+            raise PicturaError(EINVAL, f"out: expected a contiguous tensor of shape {tuple(self.codes.shape)}")
+        pictura.pictura_row_values(rows, self.scales.reshape(-1), out.view(rows.shape))
+        return out
+
+
+def rms_norm_8bit(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  dtype: torch.dtype = torch.float8_e4m3fn) -> RowCodes:
+    """rms_norm with an output in 8 bits, for layers that multiply in them: codes of `dtype`
+    (float8_e4m3fn or int8) and a scale for each row, its largest magnitude over 448 or 127.
+    Codes are the nearest ones of the float32 result, to the bit.  No gradient flows through."""
+    if dtype not in (torch.int8, torch.float8_e4m3fn):
+        raise PicturaError(EINVAL, f"dtype: {dtype}, expected float8_e4m3fn or int8")
+    rows = _rows(x, "x")
+    codes = torch.empty(rows.shape, dtype=dtype, device=x.device)
+    scales = torch.empty(rows.shape[0], dtype=torch.float32, device=x.device)
+    total = res = None
+    if residual is not None:
+        res, total = _rows(residual, "residual", x), torch.empty(rows.shape, dtype=x.dtype, device=x.device)
+    pictura.pictura_rms_norm_codes(rows, weight, codes, scales, total, res, eps)
+    return RowCodes(codes.view(x.shape), scales.view(x.shape[:-1]), None if total is None else total.view(x.shape))

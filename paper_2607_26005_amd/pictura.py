@@ -106,6 +106,7 @@ ADAMW_TENSOR = np.dtype([(n, np.uint64) for n in ("param", "grad", "exp_avg", "e
                         [("n", np.int64), ("param_dtype", np.int32), ("grad_dtype", np.int32)], align=True)
 ADAMW_BLOCK = 256
 MAX_ACTIONS = 1 << 20
+MAX_NORM = 1 << 16
 SCAN_STEPS = 16   # steps between the states that a scan saves
 POLICY_STATS = ("loss", "policy_loss", "value_loss", "entropy", "approx_kl", "clip_fraction")
 
@@ -177,6 +178,16 @@ _lib.pictura_gated_scan_gradient.argtypes = [_P, _P] + [_P, ctypes.c_int64, ctyp
 _lib.pictura_gated_scan_gradient.restype = ctypes.c_int32
 _lib.pictura_gated_step.argtypes = [_P, _P, ctypes.c_int64, _P, _P]
 _lib.pictura_gated_step.restype = ctypes.c_int32
+_lib.pictura_rms_norm.argtypes = [_P, _P, ctypes.c_int64, _P, ctypes.c_int64, _P, _P]
+_lib.pictura_rms_norm.restype = ctypes.c_int32
+_lib.pictura_rms_norm_codes.argtypes = [_P, ctypes.c_int32, _P, ctypes.c_int64, _P, ctypes.c_int64, _P, _P]
+_lib.pictura_rms_norm_codes.restype = ctypes.c_int32
+_lib.pictura_row_values.argtypes = [_P, ctypes.c_int64, _P, ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, _P, ctypes.c_int64, _P]
+_lib.pictura_row_values.restype = ctypes.c_int32
+_lib.pictura_rms_norm_gradient_workspace.argtypes = [_P, _P]
+_lib.pictura_rms_norm_gradient_workspace.restype = ctypes.c_int32
+_lib.pictura_rms_norm_gradient.argtypes = [_P, _P] + [_P, ctypes.c_int64] * 3 + [_P, _P, ctypes.c_uint64, _P]
+_lib.pictura_rms_norm_gradient.restype = ctypes.c_int32
 
 EXPORTED = ["pictura_create", "pictura_destroy", "pictura_last_error", "pictura_scene_upload",
             "pictura_bin_scene", "pictura_render_views", "pictura_agents_step", "pictura_bins_info",
@@ -186,7 +197,8 @@ EXPORTED = ["pictura_create", "pictura_destroy", "pictura_last_error", "pictura_
             "pictura_encoder_workspace", "pictura_encode_views", "pictura_sample_actions",
             "pictura_policy_loss_workspace", "pictura_policy_loss", "pictura_grad_norm_workspace", "pictura_grad_norm",
             "pictura_adamw_step", "pictura_adamw_moments", "pictura_gated_scan_workspace", "pictura_gated_scan",
-            "pictura_gated_scan_gradient", "pictura_gated_step"]
+            "pictura_gated_scan_gradient", "pictura_gated_step", "pictura_rms_norm", "pictura_rms_norm_codes",
+            "pictura_row_values", "pictura_rms_norm_gradient_workspace", "pictura_rms_norm_gradient"]
 DEVERR_RING_WAIT = 1
 
 STAT_NAMES = ["view_tiles", "cells_in_rect", "cells_prefiltered", "cells_visible", "cand_tris", "boxes_visible",
@@ -767,6 +779,81 @@ def pictura_gated_step(gates, inputs, out, state, resets=None):
     st = _call(gates.device, _lib.pictura_gated_step, q, oo, ob, sa)
     if st != OK:
         raise PicturaError(st, "gated_step failed")
+
+
+# --- the norm between layers ----------------------------------------------------------
+
+def _norm(x, weight, residual, eps, *named):
+    """(packed pictura_norm, addresses and strides of `named`), everything checked that the
+    kernels rely on."""
+    from paper_2607_26005_amd import _tensors
+    try:
+        out = _tensors.norm(x, weight, residual, eps, *named)
+    except ValueError as e:
+        raise PicturaError(EINVAL, str(e)) from None
+    if not x.is_cuda:
+        _check_device(x, "x", None)
+    return out
+
+
+def _code_kind(t, name: str) -> int:
+    import torch
+    if t.dtype not in (torch.int8, torch.float8_e4m3fn):
+        raise PicturaError(EINVAL, f"{name}: dtype {t.dtype}, expected int8 or float8_e4m3fn")
+    return 0 if t.dtype == torch.int8 else 1
+
+
+def pictura_rms_norm(x, weight, out, sum=None, residual=None, eps=1e-6, factors=None):
+    """Root-mean-square norm of the rows of x + residual, [rows, width] of float32, bfloat16 or
+    float16 (rows contiguous, any distance apart): weight [width] of that type or float32, out
+    and sum (the rows that were normed) as x, factors float32 [rows].  On the current stream."""
+    q, *at, fa = _norm(x, weight, residual, eps, "sum", "s" if sum is None else "o", sum, "out", "o", out, "factors", "f", factors)
+    st = _call(x.device, _lib.pictura_rms_norm, q, *at, fa)
+    if st != OK:
+        raise PicturaError(st, "rms_norm failed")
+
+
+def pictura_rms_norm_codes(x, weight, codes, scales, sum=None, residual=None, eps=1e-6):
+    """pictura_rms_norm with an output in 8 bits: codes int8 or float8_e4m3fn [rows, width],
+    scales float32 [rows]."""
+    q, *at, sc = _norm(x, weight, residual, eps, "sum", "s" if sum is None else "o", sum, "codes", "b", codes, "scales", "f", scales)
+    st = _call(x.device, _lib.pictura_rms_norm_codes, q, _code_kind(codes, "codes"), *at, sc)
+    if st != OK:
+        raise PicturaError(st, "rms_norm_codes failed")
+
+
+def pictura_row_values(codes, scales, out):
+    """What codes [rows, width] with scales [rows] stand for, into out float32 [rows, width]."""
+    import torch
+    c = _tensor(codes, "codes")
+    kind = _code_kind(c, "codes")
+    cp, N, C, cs = _matrix(c, "codes")
+    if not 1 <= C <= MAX_NORM or N > 0x7FFFFFFF:
+        raise PicturaError(EINVAL, f"codes: shape {tuple(c.shape)}: rows of 1 to {MAX_NORM} elements, fewer than 2^31 of them")
+    op, _, _, os_ = _matrix(_tensor(out, "out", c.device), "out", N, C)
+    if out.dtype != torch.float32:
+        raise PicturaError(EINVAL, f"out: dtype {out.dtype}, expected float32")
+    sp, = _vectors(codes, N, "scales", "f", scales)
+    st = _call(c.device, _lib.pictura_row_values, cp, cs, sp, kind, N, C, op, os_)
+    if st != OK:
+        raise PicturaError(st, "row_values failed")
+
+
+def pictura_rms_norm_gradient(x, weight, factors, dout, dx, dweight, dsum=None):
+    """Gradient of pictura_rms_norm: x is its sum (or its x, without a residual) and factors
+    its factors; dout, dsum (or None: zeros) and dx as x, dweight as the weight.  In a
+    workspace of the caching allocator."""
+    import torch
+    q, fa, *at, dw = _norm(x, weight, None, 0.0, "factors", "f", factors, "dout", "s", dout, "dsum", "s", dsum, "dx", "o", dx,
+                           "dweight", "w", dweight)
+    need = ctypes.c_uint64()
+    st = _lib.pictura_rms_norm_gradient_workspace(q, ctypes.addressof(need))
+    if st != OK:
+        raise PicturaError(st, "rms_norm_gradient_workspace: sizes out of range")
+    ws = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+    st = _call(x.device, _lib.pictura_rms_norm_gradient, q, fa, *at, dw, ws.data_ptr(), need.value)
+    if st != OK:
+        raise PicturaError(st, "rms_norm_gradient failed")
 
 
 # --- device-resident agents ------------------------------------------------------

@@ -65,3 +65,43 @@ def scan_gradient(gates, inputs, state, resets, dout, dlast):
         if resets is not None:
             c, cm, ec = (torch.where(began, zero, v) for v in (c, cm, ec))
     return (dg, dx, c), (bg, bx, ec)
+
+
+# --- the norm ---------------------------------------------------------------------
+
+def norm(x, weight, residual=None, eps=1e-6):
+    """(what is normed in x's type, y, factor q [rows, 1]) of [rows, width] tensors."""
+    s = x.detach().cpu()
+    if residual is not None:
+        s = (s.float() + residual.detach().cpu().float()).to(s.dtype)
+    q = 1 / (s.double().pow(2).mean(1, keepdim=True) + eps).sqrt()
+    return s, s.double() * q * weight.detach().cpu().double(), q
+
+
+def norm_codes(x, weight, residual, eps, dtype):
+    """(codes, scales) by the operator's own fp32 steps, of a mean in 64 bits."""
+    s, _, q = norm(x, weight, residual, eps)
+    y = (s.float() * q.float()) * weight.cpu().float()
+    most = 127.0 if dtype == torch.int8 else 448.0
+    top = y.abs().amax(1)
+    none = top < 2.0 ** -100
+    up = torch.where(none, torch.zeros_like(top), top.reciprocal() * most)
+    code = y * up[:, None]
+    code = code.round().to(torch.int8) if dtype == torch.int8 else code.to(dtype)
+    return code, torch.where(none, torch.zeros_like(top), top / most)
+
+
+def norm_gradient(s, weight, eps, dout, dsum):
+    """(dx, dweight) and their bounds.  The kernels' sums are of 70 terms one after the other
+    at most, and of 10 levels of lanes and waves; those over rows of all rows at most."""
+    s, w, dy = (t.detach().cpu().double() for t in (s, weight, dout))
+    q = 1 / (s.pow(2).mean(1, keepdim=True) + eps).sqrt()
+    u, k = s * q, dy * w
+    c, cm = (k * u).mean(1, keepdim=True), (k * u).abs().mean(1, keepdim=True)
+    dx = q * (k - u * c)
+    size = q * (k.abs() + u.abs() * c.abs())
+    bound = 8 * U * size + q * u.abs() * 90 * U * cm
+    if dsum is not None:
+        dx = dx + dsum.detach().cpu().double()
+    bound = bound + U * dx.abs()
+    return (dx, (dy * u).sum(0)), (bound, (s.shape[0] + 6) * U * (dy * u).abs().sum(0))

@@ -141,3 +141,111 @@ def test_workspace_covers_every_split():
         q = _q(batch=batch, steps=steps, channels=channels)
         assert L.pictura_gated_scan_workspace(ctypes.byref(q), ctypes.addressof(need)) == pictura.OK
         assert need.value <= 256 + (512 + 32) * 8 * max(batch * channels, 64 * 4096)
+
+
+# --- the norm ---------------------------------------------------------------------
+
+N, W = 4, 6
+
+
+@pytest.mark.parametrize("match, bad", [
+    ("x: expected a torch tensor", dict(x=[[0.0]])),
+    ("x: expected a torch tensor", dict(x=torch.zeros(()))),
+    ("x: dtype", dict(x=z(N, W).double())),
+    ("x: shape", dict(x=z(N, 0))),
+    ("x: shape", dict(x=z(1, 65537), weight=z(65537))),
+    ("x: expected a plain", dict(x=torch._neg_view(z(N, W)))),
+    ("weight: expected a torch tensor", dict(weight=1.0)),
+    ("weight: ", dict(weight=z(W + 1))),
+    ("weight: ", dict(weight=z(1, W))),
+    ("weight: ", dict(weight=z(2 * W)[::2])),
+    ("weight: ", dict(weight=z(W).half())),
+    ("weight: dtype", dict(weight=z(W).double())),
+    ("residual: expected a torch tensor", dict(residual=0)),
+    ("residual: dtype", dict(residual=z(N, W).half())),
+    ("residual: shape", dict(residual=z(N + 1, W))),
+    ("eps: ", dict(eps=-1.0)),
+    ("eps: ", dict(eps=float("nan"))),
+    ("eps: ", dict(eps=float("inf"))),
+    ("eps: ", dict(eps="small")),
+])
+def test_norm_refuses(match, bad):
+    a = dict(dict(x=z(N, W), weight=z(W)), **bad)
+    _raises(match, memory.rms_norm, **a)
+    _raises(match, memory.rms_norm_8bit, **a)
+    if "weight" not in bad:
+        _raises(match, memory.rms_norm, **dict(a, weight=z(W, requires_grad=True)))
+
+
+def test_the_norms_other_arguments_are_checked():
+    x, w, f, s = z(N, W), z(W), z(N), pictura
+    _raises("dtype: ", memory.rms_norm_8bit, x, w, dtype=torch.uint8)
+    _raises("out: shape", s.pictura_rms_norm, x, w, z(N, W + 1))
+    _raises("out: dtype", s.pictura_rms_norm, x, w, z(N, W).half())
+    _raises("out: strides", s.pictura_rms_norm, x, w, z(1, W).expand(N, W))
+    _raises("out: strides", s.pictura_rms_norm, x, w, z(W, N).t())
+    _raises("sum: shape", s.pictura_rms_norm, x, w, x, z(N, W + 1))
+    _raises("sum: strides", s.pictura_rms_norm, x, w, x, z(1, W).expand(N, W))
+    _raises("factors: ", s.pictura_rms_norm, x, w, x, None, None, 1e-6, z(N + 1))
+    _raises("codes: dtype", s.pictura_rms_norm_codes, x, w, z(N, W), f)
+    _raises("codes: shape", s.pictura_rms_norm_codes, x, w, z(N, W + 1, dtype=torch.int8), f)
+    _raises("scales: ", s.pictura_rms_norm_codes, x, w, z(N, W, dtype=torch.int8), z(N).half())
+    _raises("dout: shape", s.pictura_rms_norm_gradient, x, w, f, z(N, W + 1), x, w)
+    _raises("dsum: dtype", s.pictura_rms_norm_gradient, x, w, f, x, x, w, x.half())
+    _raises("dx: strides", s.pictura_rms_norm_gradient, x, w, f, x, z(1, W).expand(N, W), w)
+    _raises("dweight: ", s.pictura_rms_norm_gradient, x, w, f, x, x, w.half())
+    _raises("codes: dtype", s.pictura_row_values, x, f, x)
+    _raises("out: dtype", s.pictura_row_values, z(N, W, dtype=torch.int8), f, x.half())
+    _raises("out: shape", s.pictura_row_values, z(N, W, dtype=torch.int8), f, z(N, W + 1))
+    _raises("scales: shape", s.pictura_row_values, z(N, W, dtype=torch.int8), z(N + 1), x)
+    _raises("out: expected a contiguous", memory.RowCodes(z(N, W, dtype=torch.int8), f, None).values, z(W, N).t())
+
+
+def test_the_norm_refuses_host_tensors_for_their_device():
+    _raises("expected the HIP device", memory.rms_norm, z(N, W), z(W))
+    _raises("expected the HIP device", memory.rms_norm_8bit, z(N, W), z(W))
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "residual", "weight")] + \
+               [(n, ctypes.c_int64) for n in ("x_stride", "residual_stride", "rows")] + \
+               [(n, ctypes.c_int32) for n in ("width", "dtype", "weight_dtype")] + [("eps", ctypes.c_float)]
+
+
+def test_the_norms_c_entries_refuse():
+    L, ref = pictura._lib, ctypes.byref
+
+    def q(**over):
+        n = _Norm(64, None, 64, W, W, N, W, 0, 0, 1e-6)
+        for k, v in over.items():
+            setattr(n, k, v)
+        return n
+
+    norm = lambda n=None, sum=None, ss=W, out=64, os_=W, f=None: L.pictura_rms_norm(ref(n or q()), sum, ss, out, os_, f, None)
+    codes = lambda n=None, kind=0, sum=None, ss=W, c=64, cs=W, s=64: \
+        L.pictura_rms_norm_codes(ref(n or q()), kind, sum, ss, c, cs, s, None)
+    grad = lambda n=None, f=64, dy=64, dys=W, ds=None, dss=W, dx=64, dxs=W, dw=64, ws=256, size=1 << 30: \
+        L.pictura_rms_norm_gradient(ref(n or q()), f, dy, dys, ds, dss, dx, dxs, dw, ws, size, None)
+    sizes = [dict(dtype=3), dict(weight_dtype=1), dict(rows=-1), dict(rows=1 << 31), dict(width=0), dict(width=65537), dict(eps=-1.0),
+             dict(eps=float("nan")), dict(eps=float("inf"))]
+    operands = [dict(x=None), dict(x=66), dict(weight=None), dict(weight=66), dict(x_stride=-1)]
+    for over in sizes + operands:
+        assert norm(q(**over)) == codes(q(**over)) == grad(q(**over)) == pictura.EINVAL, over
+    for over in (dict(residual=66), dict(residual=64, residual_stride=-1)):
+        assert norm(q(**over)) == codes(q(**over)) == pictura.EINVAL, over
+    for k in (dict(out=None), dict(out=66), dict(os_=W - 1), dict(sum=66), dict(sum=64, ss=W - 1), dict(f=66)):
+        assert norm(**k) == pictura.EINVAL, k
+    for k in (dict(kind=2), dict(c=None), dict(cs=W - 1), dict(s=None), dict(s=66), dict(sum=66)):
+        assert codes(**k) == pictura.EINVAL, k
+    for k in (dict(n=q(residual=64)), dict(f=None), dict(f=66), dict(dy=None), dict(dy=66), dict(dys=-1), dict(ds=66), dict(ds=64, dss=-1),
+              dict(dx=None), dict(dxs=0), dict(dw=None), dict(dw=66), dict(ws=None), dict(ws=128), dict(size=8)):
+        assert grad(**k) == pictura.EINVAL, k
+    values = lambda c=64, cs=W, s=64, kind=0, rows=N, width=W, out=64, os_=W: \
+        L.pictura_row_values(c, cs, s, kind, rows, width, out, os_, None)
+    for k in (dict(c=None), dict(cs=-1), dict(s=None), dict(s=66), dict(kind=2), dict(rows=-1), dict(width=0), dict(out=None), dict(out=66),
+              dict(os_=W - 1)):
+        assert values(**k) == pictura.EINVAL, k
+    assert norm(q(rows=0, x=None)) == codes(q(rows=0)) == values(rows=0) == pictura.OK
+    out = ctypes.c_uint64()
+    assert L.pictura_rms_norm_gradient_workspace(None, ctypes.addressof(out)) == pictura.EINVAL
+    assert L.pictura_rms_norm_gradient_workspace(ref(q()), None) == pictura.EINVAL
