@@ -520,6 +520,46 @@ pictura_status pictura_policy_loss(const pictura_logits* logits, const pictura_p
                                    uint64_t workspace_bytes, float* out_stats, void* dlogits, int64_t dlogits_stride,
                                    float* dvalues, void* stream);
 
+/* Pairs of sequences of decisions, device arrays.  Sequence s is rows offsets[s] to
+ * offsets[s + 1] - 1 of the logits; of pair p sequence 2p is preferred to sequence 2p + 1.
+ * offsets do not decrease and lie within 0..rows (they are cut to that; a sequence may be
+ * empty).  Rows whose action is outside 0..actions - 1 (padding, or what
+ * pictura_sample_actions gives a row without actions), rows that allow nothing and rows
+ * outside all sequences count nothing: their gradient is 0. */
+typedef struct {
+    const int64_t* actions;      /* [rows] */
+    const int64_t* offsets;      /* [2 pairs + 1] */
+    const float* ref_logp;       /* [rows], log-probabilities by the reference policy; NULL: 0 */
+    const float* weights;        /* [pairs]; NULL: all 1.  A pair of weight 0 is not looked at */
+    int64_t pairs;               /* 0..2^23 */
+    float beta;                  /* > 0 */
+    float smoothing;             /* 0 or more, below 1: how likely a pair stands the other way round */
+    float denominator;           /* 0: the sum of the weights; else what sums are divided by */
+    int32_t average;             /* 1: mean over a sequence's rows that count, 0: sum */
+} pictura_preferences;
+
+#define PICTURA_PREFERENCE_STATS 4   /* loss, reward of the preferred, of the others, how often it is larger */
+
+/* Bytes of workspace pictura_preference_loss takes. */
+pictura_status pictura_preference_loss_workspace(int64_t rows, int32_t actions, int64_t pairs, uint64_t* bytes);
+
+/* Preference loss by paired log ratios, and its gradient.  With l the logarithm of the
+ * softmax of the allowed logits at a row's action, D_s = sum (or mean) of l - ref_logp over
+ * the rows of sequence s, m = beta (D_2p - D_2p+1),
+ *   loss = -(1 - smoothing) log sigmoid(m) - smoothing log sigmoid(-m),
+ * and out_stats holds the means by weight over the pairs of the loss, of beta D_2p, of
+ * beta D_2p+1 and of m > 0; out_ratios [2 pairs] the D_s.  dlogits (the logits' type,
+ * dlogits_stride elements between rows, apart from the logits) receives the gradient of the
+ * mean loss; it is 0 at actions of probability zero.  Sums over rows and pairs are taken in
+ * fp64 in a fixed order.  If the weights add up to 0 and there is no denominator, the
+ * statistics and the gradient are 0.  A NaN or +inf at an allowed place makes its pair NaN.
+ * workspace: device memory, 256-byte aligned, in use until the call's work on the stream is
+ * done.  EINVAL: a null or misaligned pointer, a value out of range, or a workspace too
+ * small. */
+pictura_status pictura_preference_loss(const pictura_logits* logits, const pictura_preferences* pairs, void* workspace,
+                                       uint64_t workspace_bytes, float* out_stats, float* out_ratios, void* dlogits,
+                                       int64_t dlogits_stride, void* stream);
+
 #define PICTURA_ADAMW_BLOCK 256   /* elements that share a scale of an 8-bit moment */
 
 /* One tensor of an optimizer step: n elements each, contiguous.  With 32 bits

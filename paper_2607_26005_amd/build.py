@@ -9,7 +9,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libpictura.so")
 TENSORS = os.path.join(HERE, "_tensors.so")
 SOURCES = ["pictura_binner.hip", "pictura_render.hip", "pictura_encoder.hip", "pictura_policy.hip", "pictura_adamw.hip",
-           "pictura_memory.hip", "pictura_norm.hip", "pictura_abi.hip"]
+           "pictura_memory.hip", "pictura_norm.hip", "pictura_prefer.hip",
+           "pictura_abi.hip"]
 # (source, object name, extra flags): the render source is compiled three
 # times.  One object holds only the production class/depth kernels, one the
 # production instance and one-sample colour kernels, both scheduled by LLVM's

@@ -1,4 +1,4 @@
-// Exchanges between the lanes of a wave and the waves of a workgroup.
+// Exchanges between the lanes of a wave and the waves of a workgroup, and an exponential.
 #pragma once
 
 #include "pictura_internal.h"
@@ -101,6 +101,20 @@ __device__ __forceinline__ float block_max(float x, float* lds)
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
     return from_lane(lane_scan<NW>(lds[threadIdx.x & (NW - 1)], -INFINITY, Max{}), NW - 1);
+}
+
+// exp d for d <= 0.  d log2 e rounded once is off by up to 2^-24 of itself, which
+// the exponential of a large |d| shows; fp32 gradients take the rest of the product
+// along: that of d with a constant of two terms, the first product's rounding by an fma
+// (Dekker, "A floating-point technique for extending the available precision", 1971).
+constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596299e-8f;   // log2 e is their sum
+
+__device__ __forceinline__ float exp_of(float d)
+{
+    const float h = d * kLog2e;
+    const float e = __builtin_amdgcn_exp2f(h);
+    const float l = fmaf(d, kLog2eRest, fmaf(d, kLog2e, -h));
+    return fmaf(e, l * 0.693147182f, e);
 }
 
 }  // namespace pictura

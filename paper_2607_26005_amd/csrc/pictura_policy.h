@@ -1,6 +1,7 @@
 // What the policy's entries hand to the kernels of each type of logits.
 #pragma once
 
+#include "pictura.h"
 #include "pictura_internal.h"
 
 namespace pictura {
@@ -64,5 +65,20 @@ int64_t loss_blocks(int64_t rows, int32_t actions);
 inline int group_lanes(int32_t actions) { return actions <= 8 ? 8 : actions <= 16 ? 16 : actions <= 32 ? 32 : 64; }
 
 inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+// What the entries check.
+inline size_t size_of(int32_t t) { return t == PICTURA_F32 ? 4 : 2; }
+
+inline bool logits_ok(const pictura_logits* l)
+{
+    if (!l || (l->dtype != PICTURA_F32 && l->dtype != PICTURA_BF16 && l->dtype != PICTURA_F16)) return false;
+    if (l->actions < 1 || l->actions > PICTURA_MAX_ACTIONS || l->rows < 0 || l->rows > 0x7FFFFFFFll) return false;
+    if (l->rows == 0) return true;
+    if (l->stride < l->actions && l->rows > 1) return false;
+    if (l->mask && l->mask_stride != 0 && l->mask_stride < l->actions && l->rows > 1) return false;
+    return l->data && aligned(l->data, size_of(l->dtype));
+}
+
+inline Rows rows_of(const pictura_logits& l) { return Rows{l.data, l.stride, l.mask, l.mask_stride, l.rows, l.actions}; }
 
 }  // namespace pictura

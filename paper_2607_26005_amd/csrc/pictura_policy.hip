@@ -1355,20 +1355,6 @@ __device__ void loss_finish(const Batch& b, const Shared3& s, const double* acc,
     loss_stats<NW>(b, s, sums, gridDim.x, lds[1]);
 }
 
-// exp d for d <= 0.  d log2 e rounded once is off by up to 2^-24 of itself, which
-// the exponential of a large |d| shows; fp32 gradients take the rest of the product
-// along: that of d with a constant of two terms, the first product's rounding by an fma
-// (Dekker, "A floating-point technique for extending the available precision", 1971).
-constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596299e-8f;   // log2 e is their sum
-
-__device__ __forceinline__ float exp_of(float d)
-{
-    const float h = d * kLog2e;
-    const float e = __builtin_amdgcn_exp2f(h);
-    const float l = fmaf(d, kLog2eRest, fmaf(d, kLog2e, -h));
-    return fmaf(e, l * 0.693147182f, e);
-}
-
 // Heads of up to 16 actions: a row to a thread.  What a row takes apart from its
 // logits (the terms, two exponentials, a logarithm) is then done once for it, not by
 // every lane of a group: the calls for 65,536 rows of 12 take 20 us, and
@@ -1815,20 +1801,6 @@ int64_t loss_blocks(int64_t rows, int32_t actions)
 }
 
 namespace {
-
-size_t size_of(int32_t t) { return t == PICTURA_F32 ? 4 : 2; }
-
-bool logits_ok(const pictura_logits* l)
-{
-    if (!l || (l->dtype != PICTURA_F32 && l->dtype != PICTURA_BF16 && l->dtype != PICTURA_F16)) return false;
-    if (l->actions < 1 || l->actions > PICTURA_MAX_ACTIONS || l->rows < 0 || l->rows > 0x7FFFFFFFll) return false;
-    if (l->rows == 0) return true;
-    if (l->stride < l->actions && l->rows > 1) return false;
-    if (l->mask && l->mask_stride != 0 && l->mask_stride < l->actions && l->rows > 1) return false;
-    return l->data && aligned(l->data, size_of(l->dtype));
-}
-
-Rows rows_of(const pictura_logits& l) { return Rows{l.data, l.stride, l.mask, l.mask_stride, l.rows, l.actions}; }
 
 uint64_t loss_bytes(int64_t rows, int32_t actions)
 {

@@ -1,0 +1,570 @@
+// A preference loss over pairs of sequences of decisions, and its gradient.
+//
+// Per row l = log softmax(x)[action]; per sequence D = sum (l - ref) over its rows (or their
+// mean); per pair m = beta (D_preferred - D_other) and
+//     loss = -(1 - eps) log sigmoid(m) - eps log sigmoid(-m),
+//     dloss/dx_i = +-c (delta_ia - p_i),  c = w beta (eps sigmoid(m) - (1 - eps) sigmoid(-m)),
+// for the rows of the preferred sequence (+) and the other (-).  A row's gradient hangs on
+// all rows of its pair.
+//
+// Heads of up to 64 actions: a workgroup to a pair, which keeps its rows in registers
+// between the sums and the gradient (pairs of more than 256 rows of 16 actions, or 32 of 64,
+// read them again).  Larger heads: one launch for the rows' log-probabilities, one for the
+// pairs, one for the gradient, which reads the logits again.
+#include <cmath>
+
+#include "pictura.h"
+#include "pictura_lanes.h"
+#include "pictura_policy.h"
+
+#pragma clang fp contract(off)
+
+namespace pictura {
+namespace {
+
+struct Pairs {
+    const int64_t* actions;
+    const int64_t* offsets;   // [2 count + 1], of rows
+    const float* ref;         // or null: zeros
+    const float* weights;     // or null: ones
+    int64_t count;
+    float beta, smoothing, denominator;
+    int32_t average;
+    float* stats;
+    float* ratios;            // [2 count]
+    void* dlogits;
+    int64_t dstride;
+};
+
+constexpr int kTerms = 4;               // of a pair: loss, rewards, whether the preferred one's is larger
+constexpr int64_t kFewPairs = 2048;     // weights of so many are added up by every workgroup that needs their sum
+
+struct Scratch {
+    double* omega;     // the sum of the weights, where there are more pairs than that
+    double* terms;     // [count][kTerms], times the weight
+    float2* softmax;   // [rows]: largest logit, 1 / sum of exponentials
+    float* ratio;      // [rows]: l - ref
+    float* factor;     // [rows]: 1 or 0 (whether the row counts), then its c
+};
+
+template <int G, class V>
+__device__ __forceinline__ V group_sum(V x)
+{
+    if constexpr (G > 1) x = x + lanes<0xB1, 0xf>((V)0, x);
+    if constexpr (G > 2) x = x + lanes<0x4E, 0xf>((V)0, x);
+    if constexpr (G > 4) x = x + lanes<0x141, 0xf>((V)0, x);
+    if constexpr (G > 8) x = x + lanes<0x140, 0xf>((V)0, x);
+    if constexpr (G > 16) x = x + __shfl_xor(x, 16);
+    if constexpr (G > 32) x = x + __shfl_xor(x, 32);
+    return x;
+}
+
+template <int G>
+__device__ __forceinline__ float group_max(float x)
+{
+    if constexpr (G > 1) x = fmaxf(x, lanes<0xB1, 0xf>(x, x));
+    if constexpr (G > 2) x = fmaxf(x, lanes<0x4E, 0xf>(x, x));
+    if constexpr (G > 4) x = fmaxf(x, lanes<0x141, 0xf>(x, x));
+    if constexpr (G > 8) x = fmaxf(x, lanes<0x140, 0xf>(x, x));
+    if constexpr (G > 16) x = fmaxf(x, __shfl_xor(x, 16));
+    if constexpr (G > 32) x = fmaxf(x, __shfl_xor(x, 32));
+    return x;
+}
+
+// exp(x - top), 0 for -inf; a NaN stays one.  top is finite, or infinite with a NaN to come.
+__device__ __forceinline__ float weight_of(float x, float top)
+{
+    const float d = x - top;
+    return exp_of(d < -200.0f ? -200.0f : d);
+}
+
+// The rows of sequence s, [first, second), whatever the offsets say.
+__device__ __forceinline__ int64_t bound_of(const Pairs& q, int64_t i, int64_t rows)
+{
+    const int64_t o = q.offsets[i];
+    return o < 0 ? 0 : o > rows ? rows : o;
+}
+
+// 1 / sum of the weights: of the pairs, given, or 0 where that is 0.
+template <int NT>
+__device__ double inverse_weight(const Pairs& q, const Scratch& k, double* lds)
+{
+    double sum;
+    if (q.denominator != 0.0f) sum = q.denominator;
+    else if (!q.weights) sum = (double)q.count;
+    else if (q.count > kFewPairs) sum = *k.omega;
+    else {
+        double x = 0.0;
+        for (int64_t i = threadIdx.x; i < q.count; i += NT) x += (double)q.weights[i];
+        sum = block_sum<NT / 64>(x, lds);
+    }
+    return sum != 0.0 ? 1.0 / sum : 0.0;
+}
+
+// What a pair's sums (of ratios and of rows that count) make of it.
+struct PairTerms {
+    double t[kTerms];
+    double ratio[2];   // D of both
+    float c[2];        // factor of their rows
+};
+
+__device__ __forceinline__ PairTerms pair_terms(const Pairs& q, int64_t p, const double (&sum)[2], const double (&rows)[2], double inverse)
+{
+    PairTerms r{};
+    double part[2];
+    for (int i = 0; i < 2; ++i) {
+        part[i] = q.average && rows[i] > 1.0 ? 1.0 / rows[i] : 1.0;
+        r.ratio[i] = sum[i] * part[i];
+    }
+    const double w = q.weights ? (double)q.weights[p] : 1.0;
+    if (w == 0.0) return r;   // (its numbers are not looked at)
+    const double beta = (double)q.beta, eps = (double)q.smoothing, m = beta * (r.ratio[0] - r.ratio[1]);
+    const double e = exp(-fabs(m)), near = log1p(e);                  // log sigmoid(-+m) = -(max(+-m, 0) + near)
+    const double lose = fmax(-m, 0.0) + near, win = fmax(m, 0.0) + near;
+    const double up = (m > 0.0 ? e : 1.0) / (1.0 + e), down = (m > 0.0 ? 1.0 : e) / (1.0 + e);   // sigmoid(-m), sigmoid(m)
+    double loss = (1.0 - eps) * lose;
+    if (eps > 0.0) loss += eps * win;
+    if (m != m) loss = m;
+    r.t[0] = w * loss;
+    r.t[1] = w * (beta * r.ratio[0]);
+    r.t[2] = w * (beta * r.ratio[1]);
+    r.t[3] = m > 0.0 ? w : 0.0;
+    const double c = m != m ? m : w * inverse * beta * (eps * down - (1.0 - eps) * up);
+    r.c[0] = (float)(c * part[0]);
+    r.c[1] = (float)(-c * part[1]);
+    return r;
+}
+
+// Sum of the weights of many pairs, in a fixed order.
+static __global__ __launch_bounds__(1024) void weight_sum_kernel(const Pairs q, const Scratch k)
+{
+    __shared__ double lds[16];
+    double x = 0.0;
+    for (int64_t i = threadIdx.x; i < q.count; i += 1024) x += (double)q.weights[i];
+    x = block_sum<16>(x, lds);
+    if (threadIdx.x == 0) *k.omega = x;
+}
+
+// Means of the pairs' terms, by one workgroup of NT threads.
+template <int NT>
+__device__ void write_stats(const Pairs& q, const Scratch& k, double inverse, double (*lds)[NT / 64])
+{
+    double t[kTerms] = {};
+    for (int64_t i = threadIdx.x; i < q.count; i += NT) {
+#pragma unroll
+        for (int j = 0; j < kTerms; ++j) t[j] += k.terms[i * kTerms + j];
+    }
+#pragma unroll
+    for (int j = 0; j < kTerms; ++j) {
+        const double x = block_sum<NT / 64>(t[j], lds[j]);
+        if (threadIdx.x == 0) q.stats[j] = (float)(x * inverse);
+    }
+}
+
+static __global__ __launch_bounds__(256) void stats_kernel(const Pairs q, const Scratch k)
+{
+    __shared__ double lds[kTerms + 1][4];
+    const double inverse = inverse_weight<256>(q, k, lds[kTerms]);
+    write_stats<256>(q, k, inverse, lds);
+}
+
+// ---------------------------------------------------------------------------
+// heads of up to 64 actions
+// ---------------------------------------------------------------------------
+
+// A row in a group of G lanes, E actions each.
+template <class T, int G, int E>
+struct SmallRow {
+    float x[E];          // logits, then exponentials
+    float top, inverse;  // of the row
+    float logp;
+    bool counts;
+
+    __device__ __forceinline__ void read(const Rows& R, const Pairs& q, int64_t n, int member)
+    {
+        const int A = R.actions, i0 = member * E;
+        const T* data = (const T*)R.data + n * R.stride;
+        const uint8_t* mask = R.mask ? R.mask + n * R.mask_stride : nullptr;
+        const int64_t action = q.actions[n];
+        counts = action >= 0 && action < A;
+        logp = 0.0f;
+        inverse = 0.0f;
+        if (!counts) return;   // (the whole group)
+        T t[E];
+        uint8_t m[E];
+        const T* from = data + i0;
+#pragma unroll
+        for (int k = 0; k < E; k += 4) {
+            if (i0 + k + 4 <= A) {
+                __builtin_memcpy(t + k, from + k, 4 * sizeof(T));
+                if (mask) __builtin_memcpy(m + k, mask + i0 + k, 4);
+            } else {
+#pragma unroll
+                for (int j = k; j < k + 4; ++j) {
+                    t[j] = (T)-INFINITY;
+                    m[j] = 1;
+                    if (i0 + j < A) {
+                        t[j] = from[j];
+                        if (mask) m[j] = mask[i0 + j];
+                    }
+                }
+            }
+        }
+        const float taken = mask && !mask[action] ? -INFINITY : (float)data[action];
+        float largest = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            x[j] = mask && !m[j] ? -INFINITY : (float)t[j];
+            largest = fmaxf(largest, x[j]);
+        }
+        top = group_max<G>(largest);
+        const float base = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            x[j] = weight_of(x[j], base);
+            sum += x[j];
+        }
+        sum = group_sum<G>(sum);
+        if (sum == 0.0f) {   // nothing is allowed
+            counts = false;
+            return;
+        }
+        inverse = 1.0f / sum;
+        logp = (taken - base) - logf(sum);
+    }
+
+    // c (delta - p), 0 at actions of probability zero
+    __device__ __forceinline__ void write(const Rows& R, const Pairs& q, int64_t n, int member, float c) const
+    {
+        const int A = R.actions, i0 = member * E;
+        T* out = (T*)q.dlogits + n * q.dstride + i0;
+        const int action = counts && logp != -INFINITY ? (int)q.actions[n] : -1;
+        const float f = counts ? -c * inverse : 0.0f;
+        T t[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) t[j] = (T)(counts ? fmaf(f, x[j], i0 + j == action ? c : 0.0f) : 0.0f);
+#pragma unroll
+        for (int k = 0; k < E; k += 4) {
+            if (i0 + k + 4 <= A) {
+                __builtin_memcpy(out + k, t + k, 4 * sizeof(T));
+            } else {
+#pragma unroll
+                for (int j = k; j < k + 4; ++j)
+                    if (i0 + j < A) out[j] = t[j];
+            }
+        }
+    }
+};
+
+constexpr int kOutside = 64;   // workgroups that clear the gradient of rows outside all sequences
+
+// A workgroup to a pair.
+template <class T, int G, int E>
+__global__ __launch_bounds__(256) void pair_kernel(const Rows R, const Pairs q, const Scratch k)
+{
+    constexpr int kRows = 256 / G;   // of a workgroup at a time
+    __shared__ double lds[5][4];
+    const int member = threadIdx.x % G, mine = threadIdx.x / G;
+    SmallRow<T, G, E> row;
+    if ((int64_t)blockIdx.x >= q.count) {
+        const int64_t from = bound_of(q, 0, R.rows), to = bound_of(q, 2 * q.count, R.rows);
+        row.counts = false;
+        for (int64_t n = ((int64_t)blockIdx.x - q.count) * kRows + mine; n < R.rows; n += kOutside * kRows)
+            if (n < from || n >= to) row.write(R, q, n, member, 0.0f);
+        return;
+    }
+    const int64_t p = blockIdx.x;
+    const int64_t first = bound_of(q, 2 * p, R.rows), middle = max(first, bound_of(q, 2 * p + 1, R.rows)),
+                  last = max(middle, bound_of(q, 2 * p + 2, R.rows));
+    double sum[2] = {}, rows[2] = {};
+    for (int64_t n = first + mine; n < last; n += kRows) {
+        row.read(R, q, n, member);
+        if (row.counts && member == 0) {
+            const double d = (double)(row.logp - (q.ref ? q.ref[n] : 0.0f));
+            if (n < middle) sum[0] += d, rows[0] += 1.0;
+            else sum[1] += d, rows[1] += 1.0;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        sum[i] = block_sum<4>(sum[i], lds[2 * i]);
+        rows[i] = block_sum<4>(rows[i], lds[2 * i + 1]);
+    }
+    const PairTerms t = pair_terms(q, p, sum, rows, inverse_weight<256>(q, k, lds[4]));
+    if (threadIdx.x == 0) {
+        q.ratios[2 * p] = (float)t.ratio[0];
+        q.ratios[2 * p + 1] = (float)t.ratio[1];
+        for (int j = 0; j < kTerms; ++j) k.terms[p * kTerms + j] = t.t[j];
+    }
+    const bool again = last - first > kRows;
+    for (int64_t n = first + mine; n < last; n += kRows) {
+        if (again) row.read(R, q, n, member);
+        const float c = t.c[n < middle ? 0 : 1];
+        if (c == 0.0f) row.counts = false;   // (a pair of weight 0 may hold what is no number)
+        row.write(R, q, n, member, c);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// larger heads
+// ---------------------------------------------------------------------------
+
+// V elements of a row from i on, -inf where nothing is allowed.
+template <class T, int V>
+struct Piece {
+    T t[V];
+    uint8_t m[V];
+    __device__ __forceinline__ void load(const T* data, const uint8_t* mask, int i)
+    {
+        __builtin_memcpy(t, data + i, sizeof(t));
+        if (mask) __builtin_memcpy(m, mask + i, sizeof(m));
+    }
+    __device__ __forceinline__ float operator()(const uint8_t* mask, int v) const { return mask && !m[v] ? -INFINITY : (float)t[v]; }
+};
+
+// Largest logit and sum of exponentials of every row, by teams of NW waves, a row read once
+// in vectors of 16 bytes at any address; the last one begins earlier where a row's length
+// is no multiple of them, and its first elements are skipped.
+template <class T, int NW>
+__global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void row_kernel(const Rows R, const Pairs q, const Scratch k)
+{
+    constexpr int V = 16 / sizeof(T), kAhead = 4, kLanes = NW * 64, kTeams = NW == 1 ? 4 : 1;
+    __shared__ float maxima[NW], sums[NW];
+    const int member = NW == 1 ? threadIdx.x & 63 : threadIdx.x, team = NW == 1 ? threadIdx.x >> 6 : 0;
+    const int A = R.actions;
+    const int64_t from = bound_of(q, 0, R.rows), to = bound_of(q, 2 * q.count, R.rows);
+    for (int64_t n = (int64_t)blockIdx.x * kTeams + team; n < R.rows; n += (int64_t)gridDim.x * kTeams) {
+        const int64_t action = q.actions[n];
+        const bool on = action >= 0 && action < A && n >= from && n < to;
+        if (!on) {   // (the whole team)
+            if (member == 0) {
+                k.factor[n] = 0.0f;
+                k.ratio[n] = 0.0f;
+            }
+            continue;
+        }
+        const T* data = (const T*)R.data + n * R.stride;
+        const uint8_t* mask = R.mask ? R.mask + n * R.mask_stride : nullptr;
+        float top = -INFINITY, sum = 0.0f;
+        for (int i = member * V; i < A; i += kLanes * V * kAhead) {
+            Piece<T, V> x[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int at = i + u * kLanes * V;
+                if (at < A) x[u].load(data, mask, at + V <= A ? at : A - V);
+            }
+            float largest = -INFINITY;
+            float y[kAhead][V];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int at = i + u * kLanes * V, skip = at + V <= A ? 0 : at + V - A;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    y[u][v] = at < A && v >= skip ? x[u](mask, v) : -INFINITY;
+                    largest = fmaxf(largest, y[u][v]);
+                }
+            }
+            if (largest > top) {
+                sum *= weight_of(top, largest);
+                top = largest;
+            }
+            const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int v = 0; v < V; ++v) sum += weight_of(y[u][v], base);
+        }
+        float all = group_max<64>(top);
+        if constexpr (NW > 1) {
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) maxima[threadIdx.x >> 6] = all;
+            __syncthreads();
+            all = group_max<NW>(maxima[threadIdx.x & (NW - 1)]);
+        }
+        const float base = all == -INFINITY ? 0.0f : all;
+        if (top != all) sum *= weight_of(top, base);
+        sum = group_sum<64>(sum);
+        if constexpr (NW > 1) {
+            if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+            __syncthreads();
+            sum = group_sum<NW>(sums[threadIdx.x & (NW - 1)]);
+        }
+        if (member == 0) {
+            const float taken = mask && !mask[action] ? -INFINITY : (float)data[action];
+            k.softmax[n] = make_float2(base, 1.0f / sum);
+            k.factor[n] = sum == 0.0f ? 0.0f : 1.0f;   // nothing is allowed
+            k.ratio[n] = sum == 0.0f ? 0.0f : (taken - base) - logf(sum) - (q.ref ? q.ref[n] : 0.0f);
+        }
+    }
+}
+
+// A workgroup to a pair: its sums, and the factors of its rows.
+static __global__ __launch_bounds__(256) void terms_kernel(const Pairs q, const Scratch k, int64_t all)
+{
+    __shared__ double lds[5][4];
+    for (int64_t p = blockIdx.x; p < q.count; p += gridDim.x) {
+        const int64_t first = bound_of(q, 2 * p, all), middle = max(first, bound_of(q, 2 * p + 1, all)),
+                      last = max(middle, bound_of(q, 2 * p + 2, all));
+        double sum[2] = {}, rows[2] = {};
+        for (int64_t n = first + threadIdx.x; n < last; n += 256) {
+            const double f = (double)k.factor[n], d = (double)k.ratio[n];
+            if (n < middle) sum[0] += d, rows[0] += f;
+            else sum[1] += d, rows[1] += f;
+        }
+        __syncthreads();   // (lds may still be read from before)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            sum[i] = block_sum<4>(sum[i], lds[2 * i]);
+            rows[i] = block_sum<4>(rows[i], lds[2 * i + 1]);
+        }
+        const PairTerms t = pair_terms(q, p, sum, rows, inverse_weight<256>(q, k, lds[4]));
+        if (threadIdx.x == 0) {
+            q.ratios[2 * p] = (float)t.ratio[0];
+            q.ratios[2 * p + 1] = (float)t.ratio[1];
+            for (int j = 0; j < kTerms; ++j) k.terms[p * kTerms + j] = t.t[j];
+        }
+        for (int64_t n = first + threadIdx.x; n < last; n += 256) k.factor[n] = k.factor[n] != 0.0f ? t.c[n < middle ? 0 : 1] : 0.0f;
+    }
+}
+
+// c (delta - p) of every row, by teams as in row_kernel; the first workgroup writes the
+// statistics too.
+template <class T, int NW>
+__global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void gradient_kernel(const Rows R, const Pairs q, const Scratch k)
+{
+    constexpr int V = 16 / sizeof(T), kLanes = NW * 64, kTeams = NW == 1 ? 4 : 1, NT = NW == 1 ? 256 : NW * 64;
+    __shared__ double lds[kTerms + 1][NT / 64];
+    if (blockIdx.x == 0) write_stats<NT>(q, k, inverse_weight<NT>(q, k, lds[kTerms]), lds);
+    const int member = NW == 1 ? threadIdx.x & 63 : threadIdx.x, team = NW == 1 ? threadIdx.x >> 6 : 0;
+    const int A = R.actions;
+    for (int64_t n = (int64_t)blockIdx.x * kTeams + team; n < R.rows; n += (int64_t)gridDim.x * kTeams) {
+        const T* data = (const T*)R.data + n * R.stride;
+        const uint8_t* mask = R.mask ? R.mask + n * R.mask_stride : nullptr;
+        T* out = (T*)q.dlogits + n * q.dstride;
+        const float c = k.factor[n];
+        const bool on = c != 0.0f;
+        const float2 s = on ? k.softmax[n] : make_float2(0.0f, 0.0f);
+        const float f = -c * s.y;
+        int action = -1;
+        if (on) {
+            action = (int)q.actions[n];
+            if ((mask && !mask[action]) || (float)data[action] == -INFINITY) action = -1;
+        }
+        for (int i = member * V; i < A; i += kLanes * V) {
+            const int at = i + V <= A ? i : A - V;
+            Piece<T, V> x;
+            T y[V];
+            if (on) x.load(data, mask, at);
+#pragma unroll
+            for (int v = 0; v < V; ++v) y[v] = (T)(on ? fmaf(f, weight_of(x(mask, v), s.x), at + v == action ? c : 0.0f) : 0.0f);
+            __builtin_memcpy(out + at, y, sizeof(y));
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+
+constexpr int kSmallHead = 64;
+
+uint64_t rounded(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+uint64_t scratch_bytes(int64_t rows, int32_t actions, int64_t pairs)
+{
+    return 256 + rounded(pairs * kTerms * sizeof(double)) + (actions > kSmallHead ? rounded(rows * 8) + 2 * rounded(rows * 4) : 0);
+}
+
+Scratch scratch_of(void* workspace, int64_t rows, int64_t pairs)
+{
+    char* at = (char*)workspace;
+    Scratch k;
+    k.omega = (double*)at;
+    k.terms = (double*)(at += 256);
+    k.softmax = (float2*)(at += rounded(pairs * kTerms * sizeof(double)));
+    k.ratio = (float*)(at += rounded(rows * 8));
+    k.factor = (float*)(at += rounded(rows * 4));
+    return k;
+}
+
+template <int N>
+struct Int {
+    static constexpr int value = N;
+};
+
+template <class T>
+void launch(const Rows& R, const Pairs& q, const Scratch& k, hipStream_t st)
+{
+    if (q.weights && q.denominator == 0.0f && q.count > kFewPairs)
+        hipLaunchKernelGGL(weight_sum_kernel, dim3(1), dim3(1024), 0, st, q, k);
+    if (R.actions <= kSmallHead) {
+        const dim3 grid((unsigned)(q.count + kOutside));
+        if (R.actions <= 16) hipLaunchKernelGGL((pair_kernel<T, 1, 16>), grid, dim3(256), 0, st, R, q, k);
+        else hipLaunchKernelGGL((pair_kernel<T, 8, 8>), grid, dim3(256), 0, st, R, q, k);
+        hipLaunchKernelGGL(stats_kernel, dim3(1), dim3(256), 0, st, q, k);
+        return;
+    }
+    constexpr int V = 16 / sizeof(T);
+    const int64_t vectors = (R.actions + V - 1) / V;
+    auto go = [&](auto waves) {
+        constexpr int NW = decltype(waves)::value, kTeams = NW == 1 ? 4 : 1, NT = NW == 1 ? 256 : NW * 64;
+        const int64_t all = (R.rows + kTeams - 1) / kTeams, most = 1 << 20;
+        const dim3 grid((unsigned)(all < 1 ? 1 : all < most ? all : most));
+        hipLaunchKernelGGL((row_kernel<T, NW>), grid, dim3(NT), 0, st, R, q, k);
+        if (q.count > 0)
+            hipLaunchKernelGGL(terms_kernel, dim3((unsigned)(q.count < most ? q.count : most)), dim3(256), 0, st, q, k, R.rows);
+        hipLaunchKernelGGL((gradient_kernel<T, NW>), grid, dim3(NT), 0, st, R, q, k);
+    };
+    if (vectors <= 256) go(Int<1>{});
+    else if (vectors <= 4096) go(Int<4>{});
+    else go(Int<16>{});
+}
+
+constexpr int64_t kMostPairs = 1 << 23;   // (a launch has fewer than 2^32 threads)
+
+pictura_status launched() { return hipGetLastError() == hipSuccess ? PICTURA_OK : PICTURA_EDEVICE; }
+
+}  // namespace
+}  // namespace pictura
+
+using namespace pictura;
+
+extern "C" {
+
+pictura_status pictura_preference_loss_workspace(int64_t rows, int32_t actions, int64_t pairs, uint64_t* bytes)
+{
+    if (!bytes || rows < 0 || rows > 0x7FFFFFFFll || actions < 1 || actions > PICTURA_MAX_ACTIONS || pairs < 0 || pairs > kMostPairs)
+        return PICTURA_EINVAL;
+    *bytes = scratch_bytes(rows, actions, pairs);
+    return PICTURA_OK;
+}
+
+pictura_status pictura_preference_loss(const pictura_logits* logits, const pictura_preferences* p, void* workspace,
+                                       uint64_t workspace_bytes, float* out_stats, float* out_ratios, void* dlogits,
+                                       int64_t dlogits_stride, void* stream)
+{
+    if (!logits_ok(logits) || !p || p->pairs < 0 || p->pairs > kMostPairs || !out_stats || !aligned(out_stats, 4)) return PICTURA_EINVAL;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < scratch_bytes(logits->rows, logits->actions, p->pairs))
+        return PICTURA_EINVAL;
+    if (!(p->beta > 0.0f) || !std::isfinite(p->beta) || !(p->smoothing >= 0.0f && p->smoothing < 1.0f) || !(p->denominator >= 0.0f) ||
+        !std::isfinite(p->denominator))
+        return PICTURA_EINVAL;
+    if (!p->offsets || !aligned(p->offsets, 8) || !aligned(p->ref_logp, 4) || !aligned(p->weights, 4)) return PICTURA_EINVAL;
+    if (p->pairs > 0 && (!out_ratios || !aligned(out_ratios, 4))) return PICTURA_EINVAL;
+    if (logits->rows > 0) {
+        if (!p->actions || !aligned(p->actions, 8) || !dlogits || !aligned(dlogits, size_of(logits->dtype))) return PICTURA_EINVAL;
+        if (dlogits_stride < logits->actions && logits->rows > 1) return PICTURA_EINVAL;
+    }
+    const Rows R = rows_of(*logits);
+    const Pairs q{p->actions, p->offsets, p->ref_logp, p->weights, p->pairs, p->beta, p->smoothing, p->denominator,
+                  p->average ? 1 : 0, out_stats, out_ratios, dlogits, dlogits_stride};
+    const Scratch k = scratch_of(workspace, R.rows, p->pairs);
+    hipStream_t st = (hipStream_t)stream;
+    if (logits->dtype == PICTURA_F32) launch<float>(R, q, k, st);
+    else if (logits->dtype == PICTURA_BF16) launch<__bf16>(R, q, k, st);
+    else launch<_Float16>(R, q, k, st);
+    return launched();
+}
+
+}  // extern "C"

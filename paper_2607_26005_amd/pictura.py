@@ -89,6 +89,11 @@ class _PolicyBatch(ctypes.Structure):
                                               "denominator")] + [("normalize", ctypes.c_int32)]
 
 
+class _Preferences(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("actions", "offsets", "ref_logp", "weights")] + [("pairs", ctypes.c_int64)] + \
+               [(n, ctypes.c_float) for n in ("beta", "smoothing", "denominator")] + [("average", ctypes.c_int32)]
+
+
 class _AdamW(ctypes.Structure):
     _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + \
                [("step", ctypes.c_int64), ("bits", ctypes.c_int32), ("grad_factor", ctypes.c_void_p)]
@@ -97,8 +102,9 @@ class _AdamW(ctypes.Structure):
 # The same structs packed: a tenth of the time of filling a ctypes one, in calls of a few microseconds
 _LOGITS_PACK, _SAMPLING_PACK = struct.Struct("@PiiqqPq"), struct.Struct("@fiffPPPP")
 _BATCH_PACK, _ADAMW_PACK = struct.Struct("@PqPPPPPPffffffi4x"), struct.Struct("@dddddqi4xP")
-assert [p.size for p in (_LOGITS_PACK, _SAMPLING_PACK, _BATCH_PACK, _ADAMW_PACK)] == \
-    [ctypes.sizeof(c) for c in (_Logits, _Sampling, _PolicyBatch, _AdamW)]
+_PREFERENCES_PACK = struct.Struct("@PPPPqfffi")
+assert [p.size for p in (_LOGITS_PACK, _SAMPLING_PACK, _BATCH_PACK, _ADAMW_PACK, _PREFERENCES_PACK)] == \
+    [ctypes.sizeof(c) for c in (_Logits, _Sampling, _PolicyBatch, _AdamW, _Preferences)]
 
 # pictura_adamw_tensor, as a row of a table: a step fills the columns
 ADAMW_TENSOR = np.dtype([(n, np.uint64) for n in ("param", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale",
@@ -106,6 +112,7 @@ ADAMW_TENSOR = np.dtype([(n, np.uint64) for n in ("param", "grad", "exp_avg", "e
                         [("n", np.int64), ("param_dtype", np.int32), ("grad_dtype", np.int32)], align=True)
 ADAMW_BLOCK = 256
 MAX_ACTIONS = 1 << 20
+PREFERENCE_STATS = ("loss", "reward", "other_reward", "accuracy")
 MAX_NORM = 1 << 16
 SCAN_STEPS = 16   # steps between the states that a scan saves
 POLICY_STATS = ("loss", "policy_loss", "value_loss", "entropy", "approx_kl", "clip_fraction")
@@ -169,6 +176,10 @@ _lib.pictura_adamw_step.argtypes = [_P, _P, ctypes.c_int32, _P]
 _lib.pictura_adamw_step.restype = ctypes.c_int32
 _lib.pictura_adamw_moments.argtypes = [_P, ctypes.c_int32, _P, _P, _P]
 _lib.pictura_adamw_moments.restype = ctypes.c_int32
+_lib.pictura_preference_loss_workspace.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int64, _P]
+_lib.pictura_preference_loss_workspace.restype = ctypes.c_int32
+_lib.pictura_preference_loss.argtypes = [_P, _P, _P, ctypes.c_uint64, _P, _P, _P, ctypes.c_int64, _P]
+_lib.pictura_preference_loss.restype = ctypes.c_int32
 _lib.pictura_gated_scan_workspace.argtypes = [_P, _P]
 _lib.pictura_gated_scan_workspace.restype = ctypes.c_int32
 _lib.pictura_gated_scan.argtypes = [_P, _P, ctypes.c_int64, ctypes.c_int64, _P, _P, _P, ctypes.c_uint64, _P]
@@ -196,7 +207,8 @@ EXPORTED = ["pictura_create", "pictura_destroy", "pictura_last_error", "pictura_
             "pictura_device_errors", "pictura_selftest_rcp_noalloc", "pictura_store_probe",
             "pictura_encoder_workspace", "pictura_encode_views", "pictura_sample_actions",
             "pictura_policy_loss_workspace", "pictura_policy_loss", "pictura_grad_norm_workspace", "pictura_grad_norm",
-            "pictura_adamw_step", "pictura_adamw_moments", "pictura_gated_scan_workspace", "pictura_gated_scan",
+            "pictura_adamw_step", "pictura_adamw_moments", "pictura_preference_loss_workspace",
+            "pictura_preference_loss", "pictura_gated_scan_workspace", "pictura_gated_scan",
             "pictura_gated_scan_gradient", "pictura_gated_step", "pictura_rms_norm", "pictura_rms_norm_codes",
             "pictura_row_values", "pictura_rms_norm_gradient_workspace", "pictura_rms_norm_gradient"]
 DEVERR_RING_WAIT = 1
@@ -670,6 +682,43 @@ def pictura_policy_loss(logits, values, actions, old_logp, advantages, returns, 
     st = _call(dev, _lib.pictura_policy_loss, l, batch, ws.data_ptr(), need.value, os_, dl, stride, dv)
     if st != OK:
         raise PicturaError(st, "policy_loss: a value out of range")
+
+
+def pictura_preference_loss(logits, actions, offsets, out_stats, out_ratios, dlogits, ref_logp=None, weights=None, mask=None,
+                            beta=0.1, smoothing=0.0, average=False, denominator=0.0):
+    """Preference loss over pairs of sequences and its gradient: logits and mask as in
+    pictura_sample_actions, actions int64 [rows], offsets int64 [2 pairs + 1], ref_logp float32
+    [rows], weights float32 [pairs].  Writes out_stats float32 [4] (PREFERENCE_STATS),
+    out_ratios float32 [2 pairs] and dlogits (the logits' type and shape, rows contiguous,
+    apart from the logits), on the current stream in a workspace of the caching allocator."""
+    import torch
+    l, N, A = _logits(logits, mask)
+    dev = logits.device
+    o = _tensor(offsets, "offsets", dev)
+    if o.dim() != 1 or o.shape[0] % 2 == 0:
+        raise PicturaError(EINVAL, f"offsets: shape {tuple(o.shape)}, expected [2 pairs + 1]")
+    P = o.shape[0] // 2
+    ac, rf = _vectors(logits, N, "actions", "l", actions, "ref_logp", "f", ref_logp)
+    of, = _vectors(logits, 2 * P + 1, "offsets", "l", offsets)
+    we, = _vectors(logits, P, "weights", "f", weights)
+    os_, = _vectors(logits, len(PREFERENCE_STATS), "out_stats", "f", out_stats)
+    ra, = _vectors(logits, 2 * P, "out_ratios", "f", out_ratios)
+    for name, v, ok in (("beta", beta, lambda v: 0 < v < 3e38), ("smoothing", smoothing, lambda v: 0 <= v < 1),
+                        ("denominator", denominator, lambda v: 0 <= v < 3e38)):
+        if isinstance(v, bool) or not isinstance(v, (int, float)) or not ok(v):
+            raise PicturaError(EINVAL, f"{name}: {v!r}, expected a number within range")
+    how = _PREFERENCES_PACK.pack(ac, of, rf, we, P, beta, smoothing, denominator, bool(average))
+    dl, _, _, stride = _matrix(_tensor(dlogits, "dlogits", dev), "dlogits", N, A)
+    if dlogits.dtype != logits.dtype:
+        raise PicturaError(EINVAL, f"dlogits: dtype {dlogits.dtype}, the logits have {logits.dtype}")
+    need = ctypes.c_uint64()
+    st = _lib.pictura_preference_loss_workspace(N, A, P, ctypes.addressof(need))
+    if st != OK:
+        raise PicturaError(st, "preference_loss_workspace: sizes out of range")
+    ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+    st = _call(dev, _lib.pictura_preference_loss, l, how, ws.data_ptr(), need.value, os_, ra, dl, stride)
+    if st != OK:
+        raise PicturaError(st, "preference_loss: a value out of range")
 
 
 def _table(table, name="tensors") -> int:
