@@ -41,17 +41,19 @@ HIPCC_FLAGS = [
 
 
 def _tensors_command(out: str) -> list:
-    """The host compiler's command for the helper that reads lists of torch tensors."""
+    """The host compiler's command for the helper that reads torch tensors and makes the calls that take them."""
     import sysconfig
 
     import torch
     root = os.path.dirname(torch.__file__)
     inc = os.path.join(root, "include")
-    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
-            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-isystem", inc, "-isystem",
-            os.path.join(inc, "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
-            os.path.join(CSRC, "pictura_tensors.cpp"), "-o", out, "-L", os.path.join(root, "lib"), "-ltorch_python",
-            "-ltorch", "-ltorch_cpu", "-lc10"]
+    rocm = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wno-unused-function",
+            "-D__HIP_PLATFORM_AMD__", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-isystem", inc,
+            "-isystem", os.path.join(inc, "torch", "csrc", "api", "include"), "-isystem", rocm, "-I", INCLUDE, "-I",
+            sysconfig.get_paths()["include"], os.path.join(CSRC, "pictura_tensors.cpp"),
+            os.path.join(CSRC, "pictura_calls.cpp"), "-o", out, "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch",
+            "-ltorch_cpu", "-lc10", "-lc10_hip"]
 
 
 def build(verbose: bool = False) -> str:

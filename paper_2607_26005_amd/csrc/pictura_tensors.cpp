@@ -2,17 +2,7 @@
 // keeps a kernel inside its buffers.  In Python those checks take 0.5 us a vector and
 // some 4 us an optimizer's tensor (29 tensors of the policy: 115 us a step, ten times
 // the step's kernels); here 0.1 us.
-#include <Python.h>
-
-#include <torch/csrc/autograd/python_variable.h>
-
-#include <cstdint>
-#include <sstream>
-#include <stdexcept>
-#include <string>
-#include <tuple>
-#include <utility>
-#include <vector>
+#include "pictura_tensors.h"
 
 namespace {
 
@@ -26,32 +16,10 @@ static_assert(sizeof(Row) == 64, "one row of the table");
 
 constexpr int64_t kBlock = 256;   // PICTURA_ADAMW_BLOCK
 
-struct Refused : std::runtime_error {
-    using std::runtime_error::runtime_error;
-};
-
-template <class... A>
-[[noreturn]] void refuse(const A&... a)
-{
-    std::ostringstream s;
-    (void)(s << ... << a);
-    throw Refused(s.str());
-}
-
 const at::Tensor& tensor(PyObject* o, const char* what, Py_ssize_t i)
 {
     if (!THPVariable_Check(o)) refuse(what, " ", i, ": expected a torch tensor, got ", Py_TYPE(o)->tp_name);
     return THPVariable_Unpack(o);
-}
-
-int32_t dtype_code(const at::Tensor& t, const char* what)
-{
-    switch (t.scalar_type()) {
-    case at::kFloat: return 0;
-    case at::kBFloat16: return 1;
-    case at::kHalf: return 2;
-    default: refuse(what, ": dtype ", t.scalar_type(), ", expected float32, bfloat16 or float16");
-    }
 }
 
 // Address of one of a parameter's moments or scales.
@@ -232,48 +200,6 @@ PyObject* outputs(PyObject*, PyObject* args)
     return nullptr;
 }
 
-// pictura_sequences (include/pictura.h)
-struct Sequences {
-    uint64_t gates, inputs, state, resets;
-    int64_t gates_batch, gates_step, inputs_batch, inputs_step, resets_batch, resets_step, batch, steps;
-    int32_t channels, dtype;
-};
-static_assert(sizeof(Sequences) == 104, "pictura_sequences");
-
-struct Place {
-    uint64_t at = 0;
-    int64_t batch = 0, step = 0;
-};
-
-void strided(const at::Tensor& t, const char* name, const at::Device& dev)
-{
-    if (t.layout() != at::kStrided || t.is_neg()) refuse(name, ": expected a plain strided tensor");
-    if (t.device() != dev) refuse(name, ": tensor on ", t.device(), ", the others are on ", dev);
-}
-
-// A tensor [batch, steps, channels] (step: [batch, channels]) whose channels are neighbours.
-Place place(const at::Tensor& t, const char* name, const at::Tensor& like, bool whole)
-{
-    strided(t, name, like.device());
-    if (t.scalar_type() != like.scalar_type()) refuse(name, ": dtype ", t.scalar_type(), ", the gates have ", like.scalar_type());
-    if (t.sizes() != like.sizes()) refuse(name, ": shape ", t.sizes(), ", the gates have ", like.sizes());
-    if (t.size(-1) > 1 && t.stride(-1) != 1) refuse(name, ": strides ", t.strides(), ": a step's channels have to be contiguous");
-    return Place{(uint64_t)(uintptr_t)t.data_ptr(), t.stride(0), whole ? t.stride(1) : 0};
-}
-
-bool apart(const Sequences& q, const Place& p)
-{
-    const bool many = q.batch > 1, more = q.steps > 1;
-    if ((many && p.batch < q.channels) || (more && p.step < q.channels)) return false;
-    return !many || !more || p.batch / p.step >= q.steps || p.step / p.batch >= q.batch;
-}
-
-const at::Tensor& given(PyObject* o, const char* name)
-{
-    if (!THPVariable_Check(o)) refuse(name, ": expected a torch tensor on the HIP device, got ", Py_TYPE(o)->tp_name);
-    return THPVariable_Unpack(o);
-}
-
 // sequences(whole, gates, inputs, state, resets, (name, kind, tensor), ...) -> (packed
 // pictura_sequences, then for each tensor its address and, of kind "s" (the gates' shape
 // and type), its two strides).  Kind "f": float32 [batch, channels], contiguous, or None: 0;
@@ -281,7 +207,6 @@ const at::Tensor& given(PyObject* o, const char* name)
 // saves.  whole: [batch, steps, channels], else one step, [batch, channels].
 PyObject* sequences(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
-    constexpr int64_t kSaved = 16;   // PICTURA_SCAN_STEPS
     if (n < 5 || (n - 5) % 3) {
         PyErr_SetString(PyExc_TypeError, "sequences(whole, gates, inputs, state, resets, name, kind, tensor, ...)");
         return nullptr;
@@ -290,44 +215,7 @@ PyObject* sequences(PyObject*, PyObject* const* args, Py_ssize_t n)
     try {
         const bool whole = args[0] == Py_True;
         const at::Tensor& gates = given(args[1], "gates");
-        const at::Tensor& inputs = given(args[2], "inputs");
-        if (gates.dim() != (whole ? 3 : 2) || gates.size(-1) < 1)
-            refuse("gates: shape ", gates.sizes(), ", expected ", whole ? "[batch, steps, channels]" : "[batch, channels]");
-        const at::Device dev = gates.device();
-        Sequences q{};
-        q.dtype = dtype_code(gates, "gates");
-        q.batch = gates.size(0);
-        q.steps = whole ? gates.size(1) : 1;
-        const int64_t channels = gates.size(-1);
-        if (channels > 0x7FFFFFFF || q.batch > 0x7FFFFFFF / channels || q.steps > 0x7FFFFFFF)
-            refuse("gates: shape ", gates.sizes(), ": batch times channels, and steps, have to be below 2^31");
-        q.channels = (int32_t)channels;
-        const Place g = place(gates, "gates", gates, whole), x = place(inputs, "inputs", gates, whole);
-        q.gates = g.at, q.gates_batch = g.batch, q.gates_step = g.step;
-        q.inputs = x.at, q.inputs_batch = x.batch, q.inputs_step = x.step;
-        auto floats = [&](PyObject* o, const char* name, int64_t rows) -> uint64_t {
-            if (o == Py_None) return 0;
-            const at::Tensor& t = given(o, name);
-            strided(t, name, dev);
-            const bool saved = rows >= 0;
-            if (t.scalar_type() != at::kFloat || t.dim() != (saved ? 3 : 2) || (saved && t.size(0) != rows) ||
-                t.size(saved) != q.batch || t.size(saved + 1) != channels || !t.is_contiguous())
-                refuse(name, ": ", t.scalar_type(), " ", t.sizes(), " with strides ", t.strides(), ", expected contiguous float32 [",
-                       saved ? std::to_string(rows) + ", " : "", q.batch, ", ", channels, "]");
-            return (uint64_t)(uintptr_t)t.data_ptr();
-        };
-        q.state = floats(args[3], "state", -1);
-        if (args[4] != Py_None) {
-            const at::Tensor& r = given(args[4], "resets");
-            strided(r, "resets", dev);
-            if (r.scalar_type() != at::kBool && r.scalar_type() != at::kByte)
-                refuse("resets: dtype ", r.scalar_type(), ", expected bool or uint8");
-            if (r.dim() != (whole ? 2 : 1) || r.size(0) != q.batch || (whole && r.size(1) != q.steps))
-                refuse("resets: shape ", r.sizes(), ", expected [", q.batch, whole ? ", " + std::to_string(q.steps) : "", "]");
-            q.resets = (uint64_t)(uintptr_t)r.data_ptr();
-            q.resets_batch = r.stride(0);
-            q.resets_step = whole ? r.stride(1) : 0;
-        }
+        const Sequences q = sequences_of(whole, gates, given(args[2], "inputs"), optional(args[3], "state"), optional(args[4], "resets"));
         std::vector<uint64_t> values;
         for (Py_ssize_t k = 5; k < n; k += 3) {
             const char* name = PyUnicode_AsUTF8(args[k]);
@@ -339,7 +227,8 @@ PyObject* sequences(PyObject*, PyObject* const* args, Py_ssize_t n)
                     refuse(name, ": strides ", THPVariable_Unpack(args[k + 2]).strides(), ": elements overlap");
                 values.insert(values.end(), {p.at, (uint64_t)p.batch, (uint64_t)p.step});
             } else {
-                values.push_back(floats(args[k + 2], name, *kind == 'c' ? (q.steps + kSaved - 1) / kSaved : -1));
+                const at::Tensor* t = optional(args[k + 2], name);
+                values.push_back(t ? floats(q, gates, *t, name, *kind == 'c') : 0);
             }
         }
         for (Py_ssize_t k = 5; k < n; k += 3)
@@ -364,33 +253,12 @@ PyObject* sequences(PyObject*, PyObject* const* args, Py_ssize_t n)
     return nullptr;
 }
 
-// pictura_norm (include/pictura.h)
-struct Norm {
-    uint64_t x, residual, weight;
-    int64_t x_stride, residual_stride, rows;
-    int32_t width, dtype, weight_dtype;
-    float eps;
-};
-static_assert(sizeof(Norm) == 64, "pictura_norm");
-
-// (address, elements between rows) of a [rows, width] tensor whose rows are contiguous; written: and apart.
-std::pair<uint64_t, int64_t> rows_at(const at::Tensor& t, const char* name, const at::Tensor& like, bool written)
-{
-    strided(t, name, like.device());
-    if (t.sizes() != like.sizes()) refuse(name, ": shape ", t.sizes(), ", expected ", like.sizes());
-    const int64_t stride = t.size(0) > 1 ? t.stride(0) : t.size(1);
-    if ((t.size(1) > 1 && t.stride(1) != 1) || (written && stride < t.size(1)))
-        refuse(name, ": strides ", t.strides(), ": a row has to be contiguous", written ? ", and apart from the next" : "");
-    return {(uint64_t)(uintptr_t)t.data_ptr(), stride};
-}
-
 // norm(x, weight, residual, eps, (name, kind, tensor), ...) -> (packed pictura_norm, then
 // for each tensor its address and, of kinds "s" (x's shape and type), "o" (the same,
 // written) and "b" (one byte each, written), the elements between its rows).  Kind "f":
 // float32 [rows]; "w": the weight's shape and type.  None: 0, except of kind "o".
 PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
-    constexpr int64_t kMost = 1 << 16;   // PICTURA_MAX_NORM
     if (n < 4 || (n - 4) % 3) {
         PyErr_SetString(PyExc_TypeError, "norm(x, weight, residual, eps, name, kind, tensor, ...)");
         return nullptr;
@@ -399,34 +267,12 @@ PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t n)
     try {
         const at::Tensor& x = given(args[0], "x");
         const at::Tensor& weight = given(args[1], "weight");
-        Norm q{};
-        q.dtype = dtype_code(x, "x");
-        if (x.dim() != 2 || x.size(1) < 1 || x.size(1) > kMost || x.size(0) > 0x7FFFFFFF)
-            refuse("x: shape ", x.sizes(), ": rows of 1 to ", kMost, " elements, fewer than 2^31 of them");
-        q.rows = x.size(0);
-        q.width = (int32_t)x.size(1);
-        std::tie(q.x, q.x_stride) = rows_at(x, "x", x, false);
-        strided(weight, "weight", x.device());
-        q.weight_dtype = dtype_code(weight, "weight");
-        if (weight.dim() != 1 || weight.size(0) != q.width || !weight.is_contiguous() ||
-            (weight.scalar_type() != x.scalar_type() && weight.scalar_type() != at::kFloat))
-            refuse("weight: ", weight.scalar_type(), " ", weight.sizes(), " with strides ", weight.strides(), ", expected contiguous ",
-                   x.scalar_type(), " or float32 [", q.width, "]");
-        q.weight = (uint64_t)(uintptr_t)weight.data_ptr();
-        auto same = [&](const at::Tensor& t, const char* name) {
-            if (t.scalar_type() != x.scalar_type()) refuse(name, ": dtype ", t.scalar_type(), ", the others have ", x.scalar_type());
-        };
-        if (args[2] != Py_None) {
-            const at::Tensor& r = given(args[2], "residual");
-            same(r, "residual");
-            std::tie(q.residual, q.residual_stride) = rows_at(r, "residual", x, false);
-        }
         const double eps = PyFloat_AsDouble(args[3]);
-        if (PyErr_Occurred() || !(eps >= 0) || eps > 3e38) {
+        if (PyErr_Occurred()) {
             PyErr_Clear();
             refuse("eps: expected a finite number, 0 or more");
         }
-        q.eps = (float)eps;
+        const Norm q = norm_of(x, weight, optional(args[2], "residual"), eps);
         std::vector<uint64_t> values;
         for (Py_ssize_t k = 4; k < n; k += 3) {
             const char* name = PyUnicode_AsUTF8(args[k]);
@@ -448,7 +294,7 @@ PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t n)
                 values.push_back((uint64_t)(uintptr_t)t.data_ptr());
                 continue;
             }
-            if (*kind != 'b') same(t, name);
+            if (*kind != 'b') same_type(t, name, x);
             else if (t.scalar_type() != at::kChar && t.scalar_type() != at::kFloat8_e4m3fn)
                 refuse(name, ": dtype ", t.scalar_type(), ", expected int8 or float8_e4m3fn");
             const auto at = rows_at(t, name, x, *kind != 's');
@@ -481,4 +327,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__tensors() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__tensors()
+{
+    PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddFunctions(m, pictura_calls) < 0) Py_CLEAR(m);
+    return m;
+}

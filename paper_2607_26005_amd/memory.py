@@ -14,53 +14,10 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from paper_2607_26005_amd import pictura
+from paper_2607_26005_amd import _tensors, pictura
 from paper_2607_26005_amd.pictura import EINVAL, PicturaError
 
-
-def _steps_first(t: torch.Tensor) -> bool:
-    return t.stride(1) > t.stride(0)
-
-
-def _like(t: torch.Tensor) -> torch.Tensor:
-    """An uninitialised [batch, steps, channels] tensor in t's order of batch and steps."""
-    B, T, C = t.shape
-    if _steps_first(t):
-        return torch.empty(T, B, C, dtype=t.dtype, device=t.device).transpose(0, 1)
-    return torch.empty(B, T, C, dtype=t.dtype, device=t.device)
-
-
-def _scan(gates, inputs, state, resets, save):
-    B, T, C = inputs.shape
-    f32 = dict(dtype=torch.float32, device=inputs.device)
-    out, last = _like(inputs), torch.empty(B, C, **f32)
-    saved = torch.empty(-(-T // pictura.SCAN_STEPS), B, C, **f32) if save else None
-    pictura.pictura_gated_scan(gates, inputs, out, last, saved, state, resets)
-    return out, last, saved
-
-
-class _GatedScan(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, gates, inputs, state, resets):
-        out, last, saved = _scan(gates.detach(), inputs.detach(), None if state is None else state.detach(), resets, True)
-        ctx.save_for_backward(gates, inputs, saved, resets)
-        ctx.set_materialize_grads(False)
-        return out, last
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dout, dlast):
-        gates, inputs, saved, resets = ctx.saved_tensors
-        if dout is None:
-            dout = torch.zeros(inputs.shape[2], dtype=inputs.dtype, device=inputs.device).expand(inputs.shape)
-        elif dout.is_neg() or (dout.shape[2] > 1 and dout.stride(2) != 1):
-            dout = dout.resolve_neg().clone(memory_format=torch.contiguous_format)
-        if dlast is not None:
-            dlast = dlast.resolve_neg().contiguous()
-        dgates, dinputs = _like(gates), _like(inputs)
-        dstate = torch.empty(saved.shape[1:], dtype=torch.float32, device=saved.device) if ctx.needs_input_grad[2] else None
-        pictura.pictura_gated_scan_gradient(gates, inputs, saved, dout, dlast, dgates, dinputs, dstate, resets)
-        return dgates, dinputs, dstate, None
+pictura._bind_helper(_tensors)
 
 
 def gated_scan(gates: torch.Tensor, inputs: torch.Tensor, state: Optional[torch.Tensor] = None,
@@ -75,14 +32,10 @@ def gated_scan(gates: torch.Tensor, inputs: torch.Tensor, state: Optional[torch.
     episode begins with that step, and what came before is forgotten.
 
     Gradients flow to gates, inputs and state."""
-    for name, t in (("gates", gates), ("inputs", inputs), ("state", state)):
-        if not isinstance(t, torch.Tensor) and (t is not None or name != "state"):
-            raise PicturaError(EINVAL, f"{name}: expected a torch tensor on the HIP device, got {type(t).__name__}")
-    if inputs.dim() != 3:
-        raise PicturaError(EINVAL, f"inputs: shape {tuple(inputs.shape)}, expected [batch, steps, channels]")
-    if torch.is_grad_enabled() and (gates.requires_grad or inputs.requires_grad or (state is not None and state.requires_grad)):
-        return _GatedScan.apply(gates, inputs, state, resets)
-    return _scan(gates, inputs, state, resets, False)[:2]
+    try:
+        return _tensors.gated_scan(gates, inputs, state, resets)
+    except ValueError as e:
+        raise PicturaError(EINVAL, str(e)) from None
 
 
 def gated_step(gates: torch.Tensor, inputs: torch.Tensor, state: torch.Tensor, resets: Optional[torch.Tensor] = None,
@@ -91,66 +44,10 @@ def gated_step(gates: torch.Tensor, inputs: torch.Tensor, state: torch.Tensor, r
     acts: `state` (float32) is replaced by what is remembered after the step, and returned in
     the inputs' type (in `out`, where that is given; it may be the inputs or the gates).
     resets: [batch].  No gradient flows through it."""
-    if out is None:
-        if not isinstance(inputs, torch.Tensor):
-            raise PicturaError(EINVAL, f"inputs: expected a torch tensor on the HIP device, got {type(inputs).__name__}")
-        out = torch.empty(inputs.shape, dtype=inputs.dtype, device=inputs.device)
-    pictura.pictura_gated_step(gates, inputs, out, state, resets)
-    return out
-
-
-def _rows(t, name: str, like=None) -> torch.Tensor:
-    """t [..., width] as rows (a copy where its strides allow no view of them)."""
-    if not isinstance(t, torch.Tensor) or t.dim() < 1:
-        raise PicturaError(EINVAL, f"{name}: expected a torch tensor [..., width] on the HIP device, got {type(t).__name__}")
-    if like is not None and t.shape != like.shape:
-        raise PicturaError(EINVAL, f"{name}: shape {tuple(t.shape)}, x has {tuple(like.shape)}")
-    if t.dim() == 2 and t.stride(1) == 1:
-        return t
-    if t.shape[-1] == 0:
-        raise PicturaError(EINVAL, f"{name}: shape {tuple(t.shape)}: rows of 1 to {pictura.MAX_NORM} elements")
-    t = t.reshape(t.numel() // t.shape[-1], t.shape[-1])
-    return t if t.stride(1) == 1 or t.shape[1] == 1 else t.clone(memory_format=torch.contiguous_format)
-
-
-def _normed(x, weight, residual, eps, save):
-    rows = _rows(x, "x")
-    out = torch.empty(rows.shape, dtype=x.dtype, device=x.device)
-    total = res = None
-    if residual is not None:
-        res, total = _rows(residual, "residual", x), torch.empty_like(out)
-    factors = torch.empty(rows.shape[0], dtype=torch.float32, device=x.device) if save else None
-    pictura.pictura_rms_norm(rows, weight, out, total, res, eps, factors)
-    return rows if total is None else total, out, factors
-
-
-class _RMSNorm(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x, weight, residual, eps):
-        total, out, factors = _normed(x.detach(), weight.detach(), None if residual is None else residual.detach(), eps, True)
-        ctx.set_materialize_grads(False)
-        ctx.shape = x.shape
-        if residual is None:
-            ctx.save_for_backward(weight, factors, x)
-            return out.view(x.shape)
-        total = total.view(x.shape)
-        ctx.save_for_backward(weight, factors, total)
-        return out.view(x.shape), total
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dout, dsum=None):
-        weight, factors, total = ctx.saved_tensors
-        if dout is None:
-            if dsum is None:
-                return None, None, None, None
-            return dsum, torch.zeros_like(weight) if ctx.needs_input_grad[1] else None, dsum, None
-        rows = _rows(total, "x")
-        dx, dw = torch.empty(rows.shape, dtype=rows.dtype, device=rows.device), torch.empty_like(weight)
-        pictura.pictura_rms_norm_gradient(rows, weight, factors, _rows(dout.resolve_neg(), "dout"), dx, dw,
-                                          None if dsum is None else _rows(dsum.resolve_neg(), "dsum"))
-        dx = dx.view(ctx.shape)
-        return dx, dw, dx if ctx.needs_input_grad[2] else None, None
+    try:
+        return _tensors.gated_step(gates, inputs, state, resets, out)
+    except ValueError as e:
+        raise PicturaError(EINVAL, str(e)) from None
 
 
 def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6):
@@ -160,13 +57,10 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Ten
     x and residual: float32, bfloat16 or float16, rows of 1 to 65,536 (tensors whose rows do
     not stand at one distance are copied first); weight of that type or float32.  The mean is
     taken in 64 bits, the rest in float32.  Gradients flow to x, residual and weight."""
-    for name, t in (("x", x), ("weight", weight), ("residual", residual)):
-        if not isinstance(t, torch.Tensor) and (t is not None or name != "residual"):
-            raise PicturaError(EINVAL, f"{name}: expected a torch tensor on the HIP device, got {type(t).__name__}")
-    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (residual is not None and residual.requires_grad)):
-        return _RMSNorm.apply(x, weight, residual, eps)
-    total, out, _ = _normed(x, weight, residual, eps, False)
-    return out.view(x.shape) if residual is None else (out.view(x.shape), total.view(x.shape))
+    try:
+        return _tensors.rms_norm(x, weight, residual, eps)
+    except ValueError as e:
+        raise PicturaError(EINVAL, str(e)) from None
 
 
 class RowCodes(NamedTuple):
@@ -177,13 +71,10 @@ class RowCodes(NamedTuple):
 
     def values(self, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """What the codes stand for, float32 (in `out`, contiguous, where that is given)."""
-        rows = _rows(self.codes, "codes")
-        if out is None:
-            out = torch.empty(self.codes.shape, dtype=torch.float32, device=self.codes.device)
-        elif not isinstance(out, torch.Tensor) or out.shape != self.codes.shape or not out.is_contiguous():
-            raise PicturaError(EINVAL, f"out: expected a contiguous tensor of shape {tuple(self.codes.shape)}")
-        pictura.pictura_row_values(rows, self.scales.reshape(-1), out.view(rows.shape))
-        return out
+        try:
+            return _tensors.row_values(self.codes, self.scales, out)
+        except ValueError as e:
+            raise PicturaError(EINVAL, str(e)) from None
 
 
 def rms_norm_8bit(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -193,11 +84,7 @@ def rms_norm_8bit(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torc
     Codes are the nearest ones of the float32 result, to the bit.  No gradient flows through."""
     if dtype not in (torch.int8, torch.float8_e4m3fn):
         raise PicturaError(EINVAL, f"dtype: {dtype}, expected float8_e4m3fn or int8")
-    rows = _rows(x, "x")
-    codes = torch.empty(rows.shape, dtype=dtype, device=x.device)
-    scales = torch.empty(rows.shape[0], dtype=torch.float32, device=x.device)
-    total = res = None
-    if residual is not None:
-        res, total = _rows(residual, "residual", x), torch.empty(rows.shape, dtype=x.dtype, device=x.device)
-    pictura.pictura_rms_norm_codes(rows, weight, codes, scales, total, res, eps)
-    return RowCodes(codes.view(x.shape), scales.view(x.shape[:-1]), None if total is None else total.view(x.shape))
+    try:
+        return RowCodes(*_tensors.rms_norm_8bit(x, weight, residual, eps, dtype is not torch.int8))
+    except ValueError as e:
+        raise PicturaError(EINVAL, str(e)) from None

@@ -213,6 +213,17 @@ EXPORTED = ["pictura_create", "pictura_destroy", "pictura_last_error", "pictura_
             "pictura_row_values", "pictura_rms_norm_gradient_workspace", "pictura_rms_norm_gradient"]
 DEVERR_RING_WAIT = 1
 
+
+
+def _bind_helper(helper) -> None:
+    """Hands the library's entries to the native helper that makes the calls of memory and
+    policy (torch has to be imported before it, and what only renders imports neither)."""
+    helper.bind(*(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in (
+        "pictura_gated_scan_workspace", "pictura_gated_scan", "pictura_gated_scan_gradient", "pictura_gated_step",
+        "pictura_rms_norm", "pictura_rms_norm_codes", "pictura_row_values", "pictura_rms_norm_gradient_workspace",
+        "pictura_rms_norm_gradient", "pictura_preference_loss_workspace", "pictura_preference_loss")))
+
+
 STAT_NAMES = ["view_tiles", "cells_in_rect", "cells_prefiltered", "cells_visible", "cand_tris", "boxes_visible",
               "box_tris", "first_pass_survivors", "exact_batches", "clipped", "raster_tris", "lane_tris",
               "lane_px", "record_tris", "record_tris_fp64", "blocks_tested", "blocks_passed", "first_pass_chunks",

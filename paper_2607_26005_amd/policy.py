@@ -21,6 +21,8 @@ from torch.optim import optimizer as _optimizer
 from paper_2607_26005_amd import _tensors, pictura
 from paper_2607_26005_amd.pictura import EINVAL, PicturaError
 
+pictura._bind_helper(_tensors)
+
 POLICY_STATS = pictura.POLICY_STATS
 PREFERENCE_STATS = pictura.PREFERENCE_STATS
 
@@ -136,46 +138,23 @@ def preference_gradient(logits, actions, offsets, ref_logp=None, *, weights=None
 
     dlogits is cut to the logits' type here, before any factor of the caller's; preference_loss
     keeps what float16 would lose."""
-    if not isinstance(logits, torch.Tensor):
-        raise PicturaError(EINVAL, f"logits: expected a torch tensor on the HIP device, got {type(logits).__name__}")
-    if not isinstance(offsets, torch.Tensor):
-        raise PicturaError(EINVAL, f"offsets: expected a torch tensor on the HIP device, got {type(offsets).__name__}")
-    stats = torch.empty(len(PREFERENCE_STATS), dtype=torch.float32, device=logits.device)
-    ratios = torch.empty(max(offsets.numel() - 1, 0), dtype=torch.float32, device=logits.device)
-    dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    pictura.pictura_preference_loss(logits, actions, offsets, stats, ratios, dlogits, ref_logp, weights, mask, beta,
-                                    smoothing, average, denominator)
-    return PreferenceGradient(stats, dlogits, ratios)
+    try:
+        return PreferenceGradient(*_tensors.preference_gradient(logits, actions, offsets, ref_logp, weights, mask, beta,
+                                                                smoothing, average, denominator))
+    except ValueError as e:
+        raise PicturaError(EINVAL, str(e)) from None
 
 
-class _PreferenceLoss(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, logits, args, kwargs):
-        x = logits.detach()
-        out = preference_gradient(x.float() if x.dtype == torch.float16 else x, *args, **kwargs)
-        ctx.dtype = x.dtype
-        ctx.save_for_backward(out.dlogits)
-        ctx.mark_non_differentiable(out.stats, out.ratios)
-        return out.stats[0].clone(), out.stats, out.ratios
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dloss, *_):
-        dlogits, = ctx.saved_tensors
-        if ctx.dtype == torch.float32:
-            return dlogits * dloss, None, None
-        dx = torch.empty(dlogits.shape, dtype=ctx.dtype, device=dlogits.device)
-        torch.mul(dlogits.float(), dloss, out=dx)
-        return dx, None, None
-
-
-def preference_loss(logits, actions, offsets, ref_logp=None, **kwargs):
+def preference_loss(logits, actions, offsets, ref_logp=None, *, weights=None, mask=None, beta: float = 0.1,
+                    smoothing: float = 0.0, average: bool = False, denominator: float = 0.0):
     """(loss, stats, ratios) for autograd: preference_gradient's loss, whose backward hands
     on the gradient that the same call computed, times the factor that arrives (a loss
     scale).  Of float16 logits the gradient is kept in float32 for that."""
-    if not isinstance(logits, torch.Tensor):
-        raise PicturaError(EINVAL, f"logits: expected a torch tensor on the HIP device, got {type(logits).__name__}")
-    return _PreferenceLoss.apply(logits, (actions, offsets, ref_logp), kwargs)
+    try:
+        return _tensors.preference_loss(logits, actions, offsets, ref_logp, weights, mask, beta, smoothing, average,
+                                        denominator)
+    except ValueError as e:
+        raise PicturaError(EINVAL, str(e)) from None
 
 
 class AdamW(torch.optim.Optimizer):
