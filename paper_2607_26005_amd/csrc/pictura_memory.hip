@@ -55,6 +55,7 @@ struct Sequences {
     int64_t threads, steps, segment;    // vectors of channels in all, steps, steps of a segment
     int32_t vectors;                    // vectors of a sequence's channels
     int32_t segments;
+    bool one;                           // a wave's are of one sequence
 };
 
 // The smaller one of a = sigmoid(g) and 1 - a, with the sign set where that is 1 - a:
@@ -100,6 +101,20 @@ __device__ __forceinline__ Map then(const Map& f, const Map& g)
     return Map{__float_as_uint(g.P) == 0x80000000u ? g.P : g.P * f.P, apply(g, f.H)};
 }
 
+// Says that x may be new from here on, and in this order: what is computed from it is not
+// computed earlier, where it would take registers for longer.
+__device__ __forceinline__ void hold(float& x) { asm volatile("" : "+v"(x)); }
+
+template <class T, int V>
+__device__ __forceinline__ void hold(Vec<T, V>& x)
+{
+    if constexpr (sizeof(x) == 4) {
+        uint32_t w = __builtin_bit_cast(uint32_t, x);
+        asm volatile("" : "+v"(w));
+        x = __builtin_bit_cast(Vec<T, V>, w);
+    }
+}
+
 // Where a thread's channels begin in the tensors.
 template <class T, int V>
 struct Place {
@@ -136,11 +151,17 @@ __device__ __forceinline__ void load_steps(const T* p, int64_t step, int n, Vec<
     }
 }
 
+// Bit i: whether step i of n is reset.  Where a wave's channels are all of one sequence,
+// each of its lanes looks at one step.
 template <bool kResets, int N>
-__device__ __forceinline__ uint32_t load_resets(const uint8_t* p, int64_t step, int n)
+__device__ __forceinline__ uint32_t load_resets(const uint8_t* p, int64_t step, int n, bool one)
 {
     uint32_t bits = 0;
     if constexpr (kResets) {
+        if (one) {
+            const int lane = threadIdx.x & 63;
+            return (uint32_t)__ballot(lane < n && p[lane * step] != 0);
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (i < n && p[i * step]) bits |= 1u << i;
@@ -187,7 +208,7 @@ __global__ __launch_bounds__(64 * kGroup) void summary_kernel(const Sequences<T>
             Vec<T, V> gs[kFew], xs_[kFew];
             load_steps<T, V>(g + t * q.gates.step, q.gates.step, n, gs);
             load_steps<T, V>(x + t * xs, xs, n, xs_);
-            const uint32_t resets = load_resets<kResets, kFew>(r + t * q.resets.step, q.resets.step, n);
+            const uint32_t resets = load_resets<kResets, kFew>(r + t * q.resets.step, q.resets.step, n, q.one);
 #pragma unroll
             for (int j = 0; j < kFew; ++j) {
                 const int i = kBack ? kFew - 1 - j : j;
@@ -272,7 +293,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const Sequences<T> q, const T
         Vec<T, V> gs[kSteps], xs[kSteps];
         load_steps<T, V>(g + t * q.gates.step, q.gates.step, n, gs);
         load_steps<T, V>(x + t * q.inputs.step, q.inputs.step, n, xs);
-        const uint32_t resets = load_resets<kResets, kSteps>(r + t * q.resets.step, q.resets.step, n);
+        const uint32_t resets = load_resets<kResets, kSteps>(r + t * q.resets.step, q.resets.step, n, q.one);
         if (saved) {
             Vec<float, V> s;
 #pragma unroll
@@ -304,7 +325,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const Sequences<T> q, const T
 }
 
 template <class T, int V, bool kResets>
-__global__ __launch_bounds__(256) void scan_gradient_kernel(const Sequences<T> q, const Tensor<const T> dout,
+__global__ __launch_bounds__(256, 4) void scan_gradient_kernel(const Sequences<T> q, const Tensor<const T> dout,
                                                             const float* __restrict__ dlast, const float* __restrict__ saved,
                                                             const Tensor<T> dgates, const Tensor<T> dinputs,
                                                             float* __restrict__ dstate, const Summaries<V> sums)
@@ -329,7 +350,7 @@ __global__ __launch_bounds__(256) void scan_gradient_kernel(const Sequences<T> q
         load_steps<T, V>(g + t * q.gates.step, q.gates.step, n, gs);
         load_steps<T, V>(x + t * q.inputs.step, q.inputs.step, n, xs);
         load_steps<T, V>(dy + t * dout.step, dout.step, n, dys);
-        const uint32_t resets = load_resets<kResets, kSteps>(r + t * q.resets.step, q.resets.step, n);
+        const uint32_t resets = load_resets<kResets, kSteps>(r + t * q.resets.step, q.resets.step, n, q.one);
         const Vec<float, V> s = load<float, V>(saved + ((t / kSteps) * q.threads + thread) * V);
         float h[V], m[kSteps][V], d[kSteps][V];
 #pragma unroll
@@ -345,11 +366,14 @@ __global__ __launch_bounds__(256) void scan_gradient_kernel(const Sequences<T> q
                 if (kResets && (resets >> i & 1u)) h[v] = 0.0f;
                 d[i][v] = h[v] - xi;
                 h[v] = fmaf(a, h[v], b * xi);
+                hold(m[i][v]);
+                hold(d[i][v]);
             }
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
             const int i = kSteps - 1 - j;
             if (i >= n) continue;
+            hold(dys[i]);
             Vec<T, V> og, ox;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -481,7 +505,7 @@ Sequences<T> sequences_of(const pictura_sequences& q, const Shape& s)
 {
     return Sequences<T>{{(const T*)q.gates, q.gates_batch, q.gates_step}, {(const T*)q.inputs, q.inputs_batch, q.inputs_step},
                         q.state, {q.resets, q.resets_batch, q.resets_step}, s.threads, q.steps, s.segment,
-                        q.channels / s.vec, s.segments};
+                        q.channels / s.vec, s.segments, q.channels / s.vec % 64 == 0};
 }
 
 // Whether pairs of channels can be loaded as one from a tensor of elements of e bytes.

@@ -263,7 +263,7 @@ struct Gradient {
     const float* factors;
     const void* weight;
     T* dx;
-    float* part;     // [parts][width]: sums over the rows of each team
+    float* part;     // [parts][width]: sums over the rows of each workgroup
     int64_t s_stride, dout_stride, dsum_stride, dx_stride, rows;
     int32_t width;
 };
@@ -319,15 +319,33 @@ __global__ __launch_bounds__(Tm::kThreads) void norm_gradient_kernel(const Gradi
             store<T, V>(R.dx + n * R.dx_stride + at.first, o);
         }
     }
-    float* part = R.part + ((int64_t)blockIdx.x * Tm::kRows + Tm::row()) * C;
+    float* part = R.part + (int64_t)blockIdx.x * C;
+    if constexpr (Tm::kRows == 1) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const Span<V, Tm::kLanes> at(Tm::member(), j, C);
-        if (!at.on) continue;
-        Vec<float, V> o;
+        for (int j = 0; j < NV; ++j) {
+            const Span<V, Tm::kLanes> at(Tm::member(), j, C);
+            if (!at.on) continue;
+            Vec<float, V> o;
 #pragma unroll
-        for (int v = 0; v < V; ++v) o.v[v] = dw[j][v];
-        store<float, V>(part + at.first, o);
+            for (int v = 0; v < V; ++v) o.v[v] = dw[j][v];
+            store<float, V>(part + at.first, o);
+        }
+    } else {   // the workgroup's teams are added up, in their order
+        constexpr int kSlots = Tm::kLanes * V;
+        __shared__ float all[Tm::kRows][kSlots + 1];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < V; ++v) all[Tm::row()][Tm::member() * V + v] = dw[j][v];
+            __syncthreads();
+            for (int i = threadIdx.x; i < kSlots; i += Tm::kThreads) {
+                float x = 0.0f;
+                for (int k = 0; k < Tm::kRows; ++k) x += all[k][i];
+                const Span<V, Tm::kLanes> at(i / V, j, C);
+                if (at.on) part[at.first + i % V] = x;   // (what two vectors hold is the same in both)
+            }
+        }
     }
 }
 
@@ -341,8 +359,16 @@ __global__ __launch_bounds__(kColumns * kDeep) void weight_gradient_kernel(const
     const int c = threadIdx.x % kColumns, d = threadIdx.x / kColumns;
     const int column = blockIdx.x * kColumns + c;
     double x = 0.0;
-    if (column < width)
-        for (int k = d; k < parts; k += kDeep) x += (double)part[(int64_t)k * width + column];
+    if (column < width) {
+        constexpr int kAhead = 8;   // loads under way
+        for (int k = d; k < parts; k += kDeep * kAhead) {
+            float y[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) y[u] = k + u * kDeep < parts ? part[(int64_t)(k + u * kDeep) * width + column] : 0.0f;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) x += (double)y[u];
+        }
+    }
     lds[d][c] = x;
     __syncthreads();
     for (int half = kDeep / 2; half > 0; half /= 2) {
@@ -474,7 +500,7 @@ int64_t gradient_parts(const pictura_norm& n)
     int64_t parts = 0;
     auto count = [&](auto, auto, auto team) {
         using Tm = decltype(team);
-        parts = gradient_blocks<Tm>(n.rows) * Tm::kRows;
+        parts = gradient_blocks<Tm>(n.rows);
     };
     if (n.dtype == PICTURA_F32) with_team<float>(n.width, count);
     else with_team<_Float16>(n.width, count);

@@ -22,6 +22,11 @@
 namespace pictura {
 namespace {
 
+template <int N>
+struct Int {
+    static constexpr int value = N;
+};
+
 struct Pairs {
     const int64_t* actions;
     const int64_t* offsets;   // [2 count + 1], of rows
@@ -72,9 +77,13 @@ __device__ __forceinline__ float group_max(float x)
 }
 
 // exp(x - top), 0 for -inf; a NaN stays one.  top is finite, or infinite with a NaN to come.
+// For 16-bit logits the product with log2 e is rounded once, off by up to 2^-24 of x - top:
+// far below what their gradient's rounding takes.
+template <class T>
 __device__ __forceinline__ float weight_of(float x, float top)
 {
     const float d = x - top;
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(d * kLog2e);
     return exp_of(d < -200.0f ? -200.0f : d);
 }
 
@@ -85,19 +94,23 @@ __device__ __forceinline__ int64_t bound_of(const Pairs& q, int64_t i, int64_t r
     return o < 0 ? 0 : o > rows ? rows : o;
 }
 
-// 1 / sum of the weights: of the pairs, given, or 0 where that is 0.
+// This thread's part of the sum of the weights, where every workgroup adds them up.
 template <int NT>
-__device__ double inverse_weight(const Pairs& q, const Scratch& k, double* lds)
+__device__ __forceinline__ double weight_part(const Pairs& q)
 {
-    double sum;
+    double x = 0.0;
+    if (q.weights && q.denominator == 0.0f && q.count <= kFewPairs)
+        for (int64_t i = threadIdx.x; i < q.count; i += NT) x += (double)q.weights[i];
+    return x;
+}
+
+// 1 / sum of the weights: of the pairs (sum: where every workgroup adds them up), given, or
+// 0 where that is 0.
+__device__ __forceinline__ double inverse_weight(const Pairs& q, const Scratch& k, double sum)
+{
     if (q.denominator != 0.0f) sum = q.denominator;
     else if (!q.weights) sum = (double)q.count;
     else if (q.count > kFewPairs) sum = *k.omega;
-    else {
-        double x = 0.0;
-        for (int64_t i = threadIdx.x; i < q.count; i += NT) x += (double)q.weights[i];
-        sum = block_sum<NT / 64>(x, lds);
-    }
     return sum != 0.0 ? 1.0 / sum : 0.0;
 }
 
@@ -119,7 +132,9 @@ __device__ __forceinline__ PairTerms pair_terms(const Pairs& q, int64_t p, const
     const double w = q.weights ? (double)q.weights[p] : 1.0;
     if (w == 0.0) return r;   // (its numbers are not looked at)
     const double beta = (double)q.beta, eps = (double)q.smoothing, m = beta * (r.ratio[0] - r.ratio[1]);
-    const double e = exp(-fabs(m)), near = log1p(e);                  // log sigmoid(-+m) = -(max(+-m, 0) + near)
+    // (fp32: these two are off by a few units, and all four waves' fp64 ones take 6 us)
+    const float ef = expf(-(float)fabs(m));
+    const double e = ef, near = log1pf(ef);                           // log sigmoid(-+m) = -(max(+-m, 0) + near)
     const double lose = fmax(-m, 0.0) + near, win = fmax(m, 0.0) + near;
     const double up = (m > 0.0 ? e : 1.0) / (1.0 + e), down = (m > 0.0 ? 1.0 : e) / (1.0 + e);   // sigmoid(-m), sigmoid(m)
     double loss = (1.0 - eps) * lose;
@@ -147,25 +162,66 @@ static __global__ __launch_bounds__(1024) void weight_sum_kernel(const Pairs q, 
 
 // Means of the pairs' terms, by one workgroup of NT threads.
 template <int NT>
-__device__ void write_stats(const Pairs& q, const Scratch& k, double inverse, double (*lds)[NT / 64])
+__device__ void write_stats(const Pairs& q, const Scratch& k)
 {
-    double t[kTerms] = {};
+    __shared__ double lds[NT / 64][kTerms + 1];
+    double t[kTerms + 1] = {};
     for (int64_t i = threadIdx.x; i < q.count; i += NT) {
 #pragma unroll
         for (int j = 0; j < kTerms; ++j) t[j] += k.terms[i * kTerms + j];
     }
+    t[kTerms] = weight_part<NT>(q);
 #pragma unroll
-    for (int j = 0; j < kTerms; ++j) {
-        const double x = block_sum<NT / 64>(t[j], lds[j]);
-        if (threadIdx.x == 0) q.stats[j] = (float)(x * inverse);
+    for (int j = 0; j <= kTerms; ++j) {
+        t[j] = wave_sum(t[j]);
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6][j] = t[j];
+    }
+    __syncthreads();
+    if (threadIdx.x < kTerms) {
+        double x = 0.0, w = 0.0;
+        for (int i = 0; i < NT / 64; ++i) {
+            x += lds[i][threadIdx.x];
+            w += lds[i][kTerms];
+        }
+        q.stats[threadIdx.x] = (float)(x * inverse_weight(q, k, w));
     }
 }
 
-static __global__ __launch_bounds__(256) void stats_kernel(const Pairs q, const Scratch k)
+static __global__ __launch_bounds__(256) void stats_kernel(const Pairs q, const Scratch k) { write_stats<256>(q, k); }
+
+// The sums of a pair over a workgroup of four waves, its terms by the first wave, and the
+// factors of its rows for all: two barriers.
+__device__ __forceinline__ void finish_pair(const Pairs& q, const Scratch& k, int64_t p, const double (&sum)[2],
+                                            const uint32_t (&rows)[2], float (&c)[2])
 {
-    __shared__ double lds[kTerms + 1][4];
-    const double inverse = inverse_weight<256>(q, k, lds[kTerms]);
-    write_stats<256>(q, k, inverse, lds);
+    __shared__ double parts[4][5];
+    __shared__ float factors[2];
+    const int wave = threadIdx.x >> 6;
+    const double t[5] = {wave_sum(sum[0]), wave_sum(sum[1]), (double)wave_sum(rows[0]), (double)wave_sum(rows[1]),
+                         wave_sum(weight_part<256>(q))};
+    __syncthreads();   // (what stands there may still be read from before)
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+        for (int j = 0; j < 5; ++j) parts[wave][j] = t[j];
+    }
+    __syncthreads();
+    if (wave == 0) {
+        double x[5];
+#pragma unroll
+        for (int j = 0; j < 5; ++j) x[j] = ((parts[0][j] + parts[1][j]) + parts[2][j]) + parts[3][j];
+        const double all[2] = {x[0], x[1]}, count[2] = {x[2], x[3]};
+        const PairTerms r = pair_terms(q, p, all, count, inverse_weight(q, k, x[4]));
+        if (threadIdx.x == 0) {
+            q.ratios[2 * p] = (float)r.ratio[0];
+            q.ratios[2 * p + 1] = (float)r.ratio[1];
+            for (int j = 0; j < kTerms; ++j) k.terms[p * kTerms + j] = r.t[j];
+            factors[0] = r.c[0];
+            factors[1] = r.c[1];
+        }
+    }
+    __syncthreads();
+    c[0] = factors[0];
+    c[1] = factors[1];
 }
 
 // ---------------------------------------------------------------------------
@@ -177,7 +233,8 @@ template <class T, int G, int E>
 struct SmallRow {
     float x[E];          // logits, then exponentials
     float top, inverse;  // of the row
-    float logp;
+    float logp, ref;
+    int at;              // the action, -1 where its probability is zero
     bool counts;
 
     __device__ __forceinline__ void read(const Rows& R, const Pairs& q, int64_t n, int member)
@@ -185,11 +242,8 @@ struct SmallRow {
         const int A = R.actions, i0 = member * E;
         const T* data = (const T*)R.data + n * R.stride;
         const uint8_t* mask = R.mask ? R.mask + n * R.mask_stride : nullptr;
-        const int64_t action = q.actions[n];
-        counts = action >= 0 && action < A;
-        logp = 0.0f;
-        inverse = 0.0f;
-        if (!counts) return;   // (the whole group)
+        const int64_t action = q.actions[n];   // (no load waits for it)
+        ref = q.ref ? q.ref[n] : 0.0f;
         T t[E];
         uint8_t m[E];
         const T* from = data + i0;
@@ -210,19 +264,24 @@ struct SmallRow {
                 }
             }
         }
-        const float taken = mask && !mask[action] ? -INFINITY : (float)data[action];
-        float largest = -INFINITY;
+        float largest = -INFINITY, taken = -INFINITY;
 #pragma unroll
         for (int j = 0; j < E; ++j) {
             x[j] = mask && !m[j] ? -INFINITY : (float)t[j];
             largest = fmaxf(largest, x[j]);
+            taken = i0 + j == action ? x[j] : taken;
         }
+        counts = action >= 0 && action < A;
+        at = counts ? (int)action : -1;
+        logp = inverse = 0.0f;
+        if (!counts) return;   // (the whole group)
         top = group_max<G>(largest);
+        if constexpr (G > 1) taken = __shfl(taken, (threadIdx.x & 63 & ~(G - 1)) + at / E);
         const float base = top == -INFINITY ? 0.0f : top;
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            x[j] = weight_of(x[j], base);
+            x[j] = weight_of<T>(x[j], base);
             sum += x[j];
         }
         sum = group_sum<G>(sum);
@@ -232,6 +291,7 @@ struct SmallRow {
         }
         inverse = 1.0f / sum;
         logp = (taken - base) - logf(sum);
+        if (logp == -INFINITY) at = -1;
     }
 
     // c (delta - p), 0 at actions of probability zero
@@ -239,11 +299,10 @@ struct SmallRow {
     {
         const int A = R.actions, i0 = member * E;
         T* out = (T*)q.dlogits + n * q.dstride + i0;
-        const int action = counts && logp != -INFINITY ? (int)q.actions[n] : -1;
         const float f = counts ? -c * inverse : 0.0f;
         T t[E];
 #pragma unroll
-        for (int j = 0; j < E; ++j) t[j] = (T)(counts ? fmaf(f, x[j], i0 + j == action ? c : 0.0f) : 0.0f);
+        for (int j = 0; j < E; ++j) t[j] = (T)(counts ? fmaf(f, x[j], i0 + j == at ? c : 0.0f) : 0.0f);
 #pragma unroll
         for (int k = 0; k < E; k += 4) {
             if (i0 + k + 4 <= A) {
@@ -264,7 +323,6 @@ template <class T, int G, int E>
 __global__ __launch_bounds__(256) void pair_kernel(const Rows R, const Pairs q, const Scratch k)
 {
     constexpr int kRows = 256 / G;   // of a workgroup at a time
-    __shared__ double lds[5][4];
     const int member = threadIdx.x % G, mine = threadIdx.x / G;
     SmallRow<T, G, E> row;
     if ((int64_t)blockIdx.x >= q.count) {
@@ -277,30 +335,22 @@ __global__ __launch_bounds__(256) void pair_kernel(const Rows R, const Pairs q, 
     const int64_t p = blockIdx.x;
     const int64_t first = bound_of(q, 2 * p, R.rows), middle = max(first, bound_of(q, 2 * p + 1, R.rows)),
                   last = max(middle, bound_of(q, 2 * p + 2, R.rows));
-    double sum[2] = {}, rows[2] = {};
+    double sum[2] = {};
+    uint32_t rows[2] = {};
     for (int64_t n = first + mine; n < last; n += kRows) {
         row.read(R, q, n, member);
         if (row.counts && member == 0) {
-            const double d = (double)(row.logp - (q.ref ? q.ref[n] : 0.0f));
-            if (n < middle) sum[0] += d, rows[0] += 1.0;
-            else sum[1] += d, rows[1] += 1.0;
+            const double d = (double)(row.logp - row.ref);
+            if (n < middle) sum[0] += d, ++rows[0];
+            else sum[1] += d, ++rows[1];
         }
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        sum[i] = block_sum<4>(sum[i], lds[2 * i]);
-        rows[i] = block_sum<4>(rows[i], lds[2 * i + 1]);
-    }
-    const PairTerms t = pair_terms(q, p, sum, rows, inverse_weight<256>(q, k, lds[4]));
-    if (threadIdx.x == 0) {
-        q.ratios[2 * p] = (float)t.ratio[0];
-        q.ratios[2 * p + 1] = (float)t.ratio[1];
-        for (int j = 0; j < kTerms; ++j) k.terms[p * kTerms + j] = t.t[j];
-    }
+    float factors[2];
+    finish_pair(q, k, p, sum, rows, factors);
     const bool again = last - first > kRows;
     for (int64_t n = first + mine; n < last; n += kRows) {
         if (again) row.read(R, q, n, member);
-        const float c = t.c[n < middle ? 0 : 1];
+        const float c = factors[n < middle ? 0 : 1];
         if (c == 0.0f) row.counts = false;   // (a pair of weight 0 may hold what is no number)
         row.write(R, q, n, member, c);
     }
@@ -347,12 +397,13 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void row_kernel(const Rows
         const T* data = (const T*)R.data + n * R.stride;
         const uint8_t* mask = R.mask ? R.mask + n * R.mask_stride : nullptr;
         float top = -INFINITY, sum = 0.0f;
-        for (int i = member * V; i < A; i += kLanes * V * kAhead) {
+        auto add = [&](int i, auto whole) {   // whole: all of the vectors stand in the row
+            constexpr bool kWhole = decltype(whole)::value;
             Piece<T, V> x[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int at = i + u * kLanes * V;
-                if (at < A) x[u].load(data, mask, at + V <= A ? at : A - V);
+                if (kWhole || at < A) x[u].load(data, mask, kWhole || at + V <= A ? at : A - V);
             }
             float largest = -INFINITY;
             float y[kAhead][V];
@@ -361,20 +412,26 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void row_kernel(const Rows
                 const int at = i + u * kLanes * V, skip = at + V <= A ? 0 : at + V - A;
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    y[u][v] = at < A && v >= skip ? x[u](mask, v) : -INFINITY;
+                    y[u][v] = kWhole || (at < A && v >= skip) ? x[u](mask, v) : -INFINITY;
                     largest = fmaxf(largest, y[u][v]);
                 }
             }
             if (largest > top) {
-                sum *= weight_of(top, largest);
+                sum *= weight_of<T>(top, largest);
                 top = largest;
             }
             const float base = top == -INFINITY ? 0.0f : top;
+            float some = 0.0f;
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
 #pragma unroll
-                for (int v = 0; v < V; ++v) sum += weight_of(y[u][v], base);
-        }
+                for (int v = 0; v < V; ++v) some += weight_of<T>(y[u][v], base);
+            sum += some;
+        };
+        constexpr int kChunk = kLanes * V * kAhead;
+        int i = member * V;
+        for (; i - member * V + kChunk <= A; i += kChunk) add(i, Int<true>{});
+        if (i < A) add(i, Int<false>{});
         float all = group_max<64>(top);
         if constexpr (NW > 1) {
             __syncthreads();
@@ -383,7 +440,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void row_kernel(const Rows
             all = group_max<NW>(maxima[threadIdx.x & (NW - 1)]);
         }
         const float base = all == -INFINITY ? 0.0f : all;
-        if (top != all) sum *= weight_of(top, base);
+        if (top != all) sum *= weight_of<T>(top, base);
         sum = group_sum<64>(sum);
         if constexpr (NW > 1) {
             if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
@@ -402,29 +459,21 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void row_kernel(const Rows
 // A workgroup to a pair: its sums, and the factors of its rows.
 static __global__ __launch_bounds__(256) void terms_kernel(const Pairs q, const Scratch k, int64_t all)
 {
-    __shared__ double lds[5][4];
     for (int64_t p = blockIdx.x; p < q.count; p += gridDim.x) {
         const int64_t first = bound_of(q, 2 * p, all), middle = max(first, bound_of(q, 2 * p + 1, all)),
                       last = max(middle, bound_of(q, 2 * p + 2, all));
-        double sum[2] = {}, rows[2] = {};
+        double sum[2] = {};
+        uint32_t rows[2] = {};
         for (int64_t n = first + threadIdx.x; n < last; n += 256) {
-            const double f = (double)k.factor[n], d = (double)k.ratio[n];
-            if (n < middle) sum[0] += d, rows[0] += f;
-            else sum[1] += d, rows[1] += f;
+            const uint32_t counts = k.factor[n] != 0.0f;
+            const double d = (double)k.ratio[n];
+            if (n < middle) sum[0] += d, rows[0] += counts;
+            else sum[1] += d, rows[1] += counts;
         }
-        __syncthreads();   // (lds may still be read from before)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            sum[i] = block_sum<4>(sum[i], lds[2 * i]);
-            rows[i] = block_sum<4>(rows[i], lds[2 * i + 1]);
-        }
-        const PairTerms t = pair_terms(q, p, sum, rows, inverse_weight<256>(q, k, lds[4]));
-        if (threadIdx.x == 0) {
-            q.ratios[2 * p] = (float)t.ratio[0];
-            q.ratios[2 * p + 1] = (float)t.ratio[1];
-            for (int j = 0; j < kTerms; ++j) k.terms[p * kTerms + j] = t.t[j];
-        }
-        for (int64_t n = first + threadIdx.x; n < last; n += 256) k.factor[n] = k.factor[n] != 0.0f ? t.c[n < middle ? 0 : 1] : 0.0f;
+        float c[2];
+        finish_pair(q, k, p, sum, rows, c);
+        for (int64_t n = first + threadIdx.x; n < last; n += 256)
+            if (k.factor[n] != 0.0f) k.factor[n] = c[n < middle ? 0 : 1];
     }
 }
 
@@ -434,8 +483,7 @@ template <class T, int NW>
 __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void gradient_kernel(const Rows R, const Pairs q, const Scratch k)
 {
     constexpr int V = 16 / sizeof(T), kLanes = NW * 64, kTeams = NW == 1 ? 4 : 1, NT = NW == 1 ? 256 : NW * 64;
-    __shared__ double lds[kTerms + 1][NT / 64];
-    if (blockIdx.x == 0) write_stats<NT>(q, k, inverse_weight<NT>(q, k, lds[kTerms]), lds);
+    if (blockIdx.x == 0) write_stats<NT>(q, k);
     const int member = NW == 1 ? threadIdx.x & 63 : threadIdx.x, team = NW == 1 ? threadIdx.x >> 6 : 0;
     const int A = R.actions;
     for (int64_t n = (int64_t)blockIdx.x * kTeams + team; n < R.rows; n += (int64_t)gridDim.x * kTeams) {
@@ -457,7 +505,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void gradient_kernel(const
             T y[V];
             if (on) x.load(data, mask, at);
 #pragma unroll
-            for (int v = 0; v < V; ++v) y[v] = (T)(on ? fmaf(f, weight_of(x(mask, v), s.x), at + v == action ? c : 0.0f) : 0.0f);
+            for (int v = 0; v < V; ++v) y[v] = (T)(on ? fmaf(f, weight_of<T>(x(mask, v), s.x), at + v == action ? c : 0.0f) : 0.0f);
             __builtin_memcpy(out + at, y, sizeof(y));
         }
     }
@@ -487,11 +535,6 @@ Scratch scratch_of(void* workspace, int64_t rows, int64_t pairs)
     k.factor = (float*)(at += rounded(rows * 4));
     return k;
 }
-
-template <int N>
-struct Int {
-    static constexpr int value = N;
-};
 
 template <class T>
 void launch(const Rows& R, const Pairs& q, const Scratch& k, hipStream_t st)
