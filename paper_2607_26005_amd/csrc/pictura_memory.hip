@@ -26,8 +26,6 @@ namespace pictura {
 namespace {
 
 constexpr int kSteps = PICTURA_SCAN_STEPS;   // steps between saved states, and in registers at once
-constexpr int kFew = 8;                      // steps in registers of the summaries' 16 waves
-constexpr int kGroup = 16;                   // segments of a group
 
 template <class T, int V>
 struct alignas(V * sizeof(T)) Vec {
@@ -52,9 +50,8 @@ struct Sequences {
     Tensor<const T> gates, inputs;
     const float* state;                 // [batch][channels]
     Tensor<const uint8_t> resets;       // one channel
-    int64_t threads, steps, segment;    // vectors of channels in all, steps, steps of a segment
+    int64_t threads, steps;             // vectors of channels in all, steps
     int32_t vectors;                    // vectors of a sequence's channels
-    int32_t segments;
     bool one;                           // a wave's are of one sequence
 };
 
@@ -169,118 +166,332 @@ __device__ __forceinline__ uint32_t load_resets(const uint8_t* p, int64_t step, 
     return bits;
 }
 
-// Summaries of the segments and their groups: rows of `threads` vectors of maps.
 template <int V>
 struct alignas(8 * V) Maps {
     Map v[V];
 };
 
-template <int V>
-struct Summaries {
-    Maps<V>* segments;   // [segments][threads]
-    Maps<V>* groups;     // [groups][threads]
+// ---------------------------------------------------------------------------
+// few channels: the steps cut into tiles, a workgroup each
+// ---------------------------------------------------------------------------
+
+// What workgroups tell one another: a 64-bit word that holds a value together with the
+// fact that it is there, so that it needs no fence.  `tiles` has P and H of every tile, with
+// P in the lower half, which is kEmpty before; `groups` the state after every kGroup tiles in
+// the upper half of a word whose lower half is kEmpty before.
+constexpr uint32_t kEmpty = 0xFFFFFFFFu;
+constexpr int kTileWaves = 16;                   // waves of a tile, kSteps steps each
+constexpr int kTile = kTileWaves * kSteps;
+constexpr int kGroup = 16;                       // tiles of a group
+constexpr int kPolls = 1 << 20;                  // of a wait, a second or more
+
+typedef unsigned long long Word;
+
+struct Chain {
+    uint32_t* ticket;
+    Word* tiles;    // [tiles][threads][V]
+    Word* groups;   // [groups][threads][V]
+    int64_t words;  // of both
+    int32_t count;  // tiles
 };
 
-// P and H of every segment (forwards), or of what it hands back (kBack: c -> P c + H).
-template <class T, int V, bool kResets, bool kBack>
-__global__ __launch_bounds__(64 * kGroup) void summary_kernel(const Sequences<T> q, const Tensor<const T> dout,
-                                                              const Summaries<V> out)
+__device__ __forceinline__ void tell(Word* at, uint32_t low, float high)
 {
-    __shared__ Maps<V> lds[kGroup][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t thread = (int64_t)blockIdx.x * 64 + lane;
-    const int32_t seg = blockIdx.y * kGroup + wave;
-    const bool on = thread < q.threads && seg < q.segments && seg != (kBack ? 0 : q.segments - 1);
-    Maps<V> f;
+    __hip_atomic_store(at, (Word)__float_as_uint(high) << 32 | low, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ void tell(Word* at, const Map& m)
+{
+    const uint32_t p = __float_as_uint(m.P);
+    tell(at, p == kEmpty ? 0x7FC00000u : p, m.H);   // (a NaN of that pattern: any other)
+}
+
+// Waits until the V words are there.  A workgroup waits only for such with smaller tickets,
+// which have started before it and in turn wait only for smaller ones: every wait ends.
+// (If one did not, its values would be taken as they are, NaNs.)
+template <int V>
+__device__ __forceinline__ void await(const Word* at, bool on, Word (&w)[V])
+{
+    for (int i = 0; i < kPolls; ++i) {
+        bool there = true;
 #pragma unroll
-    for (int v = 0; v < V; ++v) f.v[v] = Map{1.0f, 0.0f};
-    if (on) {
-        const Place<T, V> at(thread, q.vectors);
-        const int64_t t0 = seg * q.segment, t1 = min(q.steps, t0 + q.segment);
-        const T* g = at.in(q.gates);
-        const T* x = kBack ? at.in(dout) : at.in(q.inputs);
-        const int64_t xs = kBack ? dout.step : q.inputs.step;
-        const uint8_t* r = at.flags(q.resets);
-        const int64_t blocks = (t1 - t0 + kFew - 1) / kFew;
-        for (int64_t k = 0; k < blocks; ++k) {
-            const int64_t t = t0 + (kBack ? blocks - 1 - k : k) * kFew;
-            const int n = (int)min((int64_t)kFew, t1 - t);
-            Vec<T, V> gs[kFew], xs_[kFew];
-            load_steps<T, V>(g + t * q.gates.step, q.gates.step, n, gs);
-            load_steps<T, V>(x + t * xs, xs, n, xs_);
-            const uint32_t resets = load_resets<kResets, kFew>(r + t * q.resets.step, q.resets.step, n, q.one);
-#pragma unroll
-            for (int j = 0; j < kFew; ++j) {
-                const int i = kBack ? kFew - 1 - j : j;
-                if (i >= n) continue;
-                const bool reset = kResets && (resets >> i & 1u);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    float a, b;
-                    gate_parts(gate_of((float)gs[i].v[v]), a, b);
-                    Map& m = f.v[v];
-                    if constexpr (kBack) m.H = reset ? 0.0f : a * ((float)xs_[i].v[v] + m.H);
-                    else m.H = reset ? b * (float)xs_[i].v[v] : fmaf(a, m.H, b * (float)xs_[i].v[v]);
-                    m.P = reset ? -0.0f : __float_as_uint(m.P) == 0x80000000u ? m.P : a * m.P;
-                }
-            }
+        for (int v = 0; v < V; ++v) {
+            w[v] = on ? __hip_atomic_load(at + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+            there = there && (uint32_t)w[v] != kEmpty;
         }
-        out.segments[(int64_t)seg * q.threads + thread] = f;
-    }
-    lds[wave][lane] = f;
-    __syncthreads();
-    if (wave == 0 && thread < q.threads) {
-#pragma unroll
-        for (int k = 1; k < kGroup; ++k) {
-            const Maps<V>& m = lds[kBack ? kGroup - 1 - k : k][lane];
-            if (k == 1) f = lds[kBack ? kGroup - 1 : 0][lane];
-#pragma unroll
-            for (int v = 0; v < V; ++v) f.v[v] = then(f.v[v], m.v[v]);
-        }
-        out.groups[(int64_t)blockIdx.y * q.threads + thread] = f;
+        if (__all(there)) return;
+        __builtin_amdgcn_s_sleep(1);
     }
 }
 
-// h through the maps of the segments before this one (kBack: those after it).
-template <int V, bool kBack>
-__device__ __forceinline__ void fold(const Summaries<V>& s, int64_t threads, int64_t thread, int32_t seg, int32_t segments,
-                                     float (&h)[V])
+// Clears what the workgroups of one call tell one another.
+static __global__ __launch_bounds__(256) void chain_kernel(const Chain c)
 {
-    auto through = [&](const Maps<V>* rows, int32_t from, int32_t count) {
-        constexpr int kAhead = 8;
-        for (int32_t k = 0; k < count; k += kAhead) {
-            Maps<V> m[kAhead];
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i == 0) *c.ticket = 0;
+    if (i < c.words) c.tiles[i] = ~0ull;
+}
+
+template <int V>
+struct TileLds {
+    Maps<V> waves[kTileWaves][64];    // of this tile
+    Maps<V> before[kTileWaves][64];   // of the tiles before it in its group; the last row: the state before those
+    uint32_t ticket;
+};
+
+// This workgroup's tile and channels, in the order in which workgroups start: all channels
+// of a tile before the next one.
+template <int V>
+__device__ __forceinline__ int32_t take_ticket(const Chain& c, TileLds<V>& lds, int32_t blocks, int32_t& block)
+{
+    if (threadIdx.x == 0) lds.ticket = atomicAdd(c.ticket, 1u);
+    __syncthreads();
+    block = (int32_t)(lds.ticket % (uint32_t)blocks);
+    return (int32_t)(lds.ticket / (uint32_t)blocks);
+}
+
+// The state before this wave's steps.  k: the tile in the order of the recurrence, w: the
+// wave in that order, f: what its steps do; first: the state before tile 0.
+template <int V>
+__device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, int64_t threads, int64_t thread, bool on, int32_t k,
+                                             int w, const Maps<V>& f, const float (&first)[V], float (&h)[V])
+{
+    const int lane = threadIdx.x & 63;
+    const int32_t g = k / kGroup, r = k % kGroup;
+    lds.waves[w][lane] = f;
+    __syncthreads();
+    if (w == kTileWaves - 1 && r < kGroup - 1 && k < c.count - 1) {   // what the whole tile does
+        Maps<V> all = lds.waves[0][lane];
+#pragma unroll 2
+        for (int i = 1; i < kTileWaves; ++i) {
+            const Maps<V> m = lds.waves[i][lane];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (k + i < count) m[i] = rows[(int64_t)(kBack ? from - k - i : from + k + i) * threads + thread];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (k + i < count) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) h[v] = apply(m[i].v[v], h[v]);
-                }
+            for (int v = 0; v < V; ++v) all.v[v] = then(all.v[v], m.v[v]);
         }
-    };
-    const int32_t group = seg / kGroup, groups = (segments + kGroup - 1) / kGroup;
-    if (kBack) {
-        through(s.groups, groups - 1, groups - 1 - group);
-        const int32_t last = min(segments, (group + 1) * kGroup) - 1;
-        through(s.segments, last, last - seg);
-    } else {
-        through(s.groups, 0, group);
-        through(s.segments, group * kGroup, seg - group * kGroup);
+        if (on) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) tell(c.tiles + ((int64_t)k * threads + thread) * V + v, all.v[v]);
+        }
+    }
+    // each wave waits for one of the tiles before, the last one for the group before
+    Maps<V> m;
+    if (w < r) {
+        Word x[V];
+        await<V>(c.tiles + ((int64_t)(g * kGroup + w) * threads + thread) * V, on, x);
+#pragma unroll
+        for (int v = 0; v < V; ++v) m.v[v] = Map{__uint_as_float((uint32_t)x[v]), __uint_as_float((uint32_t)(x[v] >> 32))};
+        lds.before[w][lane] = m;
+    } else if (w == kTileWaves - 1) {
+        if (g > 0) {
+            Word x[V];
+            await<V>(c.groups + ((int64_t)(g - 1) * threads + thread) * V, on, x);
+#pragma unroll
+            for (int v = 0; v < V; ++v) m.v[v].H = __uint_as_float((uint32_t)(x[v] >> 32));
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) m.v[v].H = first[v];
+        }
+        lds.before[w][lane] = m;
+    }
+    __syncthreads();
+    m = lds.before[kTileWaves - 1][lane];
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = m.v[v].H;
+    for (int i = 0; i < r; ++i) {
+        m = lds.before[i][lane];
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = apply(m.v[v], h[v]);
+    }
+    for (int i = 0; i < w; ++i) {
+        m = lds.waves[i][lane];
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = apply(m.v[v], h[v]);
+    }
+    if (w == kTileWaves - 1 && r == kGroup - 1 && k < c.count - 1 && on) {   // the state after the group
+#pragma unroll
+        for (int v = 0; v < V; ++v) tell(c.groups + ((int64_t)g * threads + thread) * V + v, 0u, apply(f.v[v], h[v]));
     }
 }
+
+// Forwards over one tile: a and (1 - a) x of a wave's 16 steps stay in registers while it
+// waits for the state before them, so that everything is read once.
+template <class T, int V, bool kResets>
+__global__ __launch_bounds__(kTileWaves * 64, 4) void tile_kernel(const Sequences<T> q, const Tensor<T> out, float* __restrict__ last,
+                                                                  float* __restrict__ saved, const Chain chain)
+{
+    __shared__ TileLds<V> lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int32_t block;
+    const int32_t tile = take_ticket<V>(chain, lds, (int32_t)((q.threads + 63) / 64), block);
+    const int64_t thread = (int64_t)block * 64 + lane;
+    const bool on = thread < q.threads;
+    const Place<T, V> at(on ? thread : 0, q.vectors);   // (lanes beyond the last channel read the first ones' and write nothing)
+    const int64_t t = (int64_t)tile * kTile + wave * kSteps;
+    const int n = (int)max((int64_t)0, min((int64_t)kSteps, q.steps - t));
+    float a[kSteps][V], add[kSteps][V], first[V], h[V];
+    uint32_t resets;
+    Maps<V> f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        f.v[v] = Map{1.0f, 0.0f};
+        first[v] = q.state && on ? q.state[thread * V + v] : 0.0f;
+    }
+    {
+        Vec<T, V> gs[kSteps], xs[kSteps];
+        load_steps<T, V>(at.in(q.gates) + t * q.gates.step, q.gates.step, n, gs);
+        load_steps<T, V>(at.in(q.inputs) + t * q.inputs.step, q.inputs.step, n, xs);
+        resets = load_resets<kResets, kSteps>(at.flags(q.resets) + t * q.resets.step, q.resets.step, n, q.one);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float b;
+                gate_parts(gate_of((float)gs[i].v[v]), a[i][v], b);
+                add[i][v] = b * (float)xs[i].v[v];
+                const bool reset = kResets && (resets >> i & 1u);
+                Map& m = f.v[v];
+                if (i < n) {
+                    m.H = reset ? add[i][v] : fmaf(a[i][v], m.H, add[i][v]);
+                    m.P = reset ? -0.0f : a[i][v] * m.P;   // (-0 stays -0)
+                }
+                hold(a[i][v]);
+                hold(add[i][v]);
+            }
+    }
+    state_before<V>(chain, lds, q.threads, thread, on, tile, wave, f, first, h);
+    if (!on || n == 0) return;
+    if (saved) {
+        Vec<float, V> s;
+#pragma unroll
+        for (int v = 0; v < V; ++v) s.v[v] = h[v];
+        store<float, V>(saved + ((t / kSteps) * q.threads + thread) * V, s);
+    }
+    T* y = at.in(out) + t * out.step;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        if (i >= n) continue;
+        Vec<T, V> o;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            h[v] = kResets && (resets >> i & 1u) ? add[i][v] : fmaf(a[i][v], h[v], add[i][v]);
+            o.v[v] = (T)h[v];
+        }
+        store<T, V>(y + i * out.step, o);
+    }
+    if (last && t + n == q.steps) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) last[thread * V + v] = h[v];
+    }
+}
+
+// Backwards over one tile, from the last one on.
+template <class T, int V, bool kResets>
+__global__ __launch_bounds__(kTileWaves * 64, 4) void tile_gradient_kernel(const Sequences<T> q, const Tensor<const T> dout,
+                                                                           const float* __restrict__ dlast,
+                                                                           const float* __restrict__ saved, const Tensor<T> dgates,
+                                                                           const Tensor<T> dinputs, float* __restrict__ dstate,
+                                                                           const Chain chain)
+{
+    __shared__ TileLds<V> lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int32_t block;
+    const int32_t k = take_ticket<V>(chain, lds, (int32_t)((q.threads + 63) / 64), block);
+    const int64_t thread = (int64_t)block * 64 + lane;
+    const bool on = thread < q.threads;
+    const Place<T, V> at(on ? thread : 0, q.vectors);
+    const int64_t t = (int64_t)(chain.count - 1 - k) * kTile + (kTileWaves - 1 - wave) * kSteps;
+    const int n = (int)max((int64_t)0, min((int64_t)kSteps, q.steps - t));
+    float m[kSteps][V], d[kSteps][V], first[V], c[V];
+    Vec<T, V> dys[kSteps];
+    uint32_t resets;
+    Maps<V> f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        f.v[v] = Map{1.0f, 0.0f};
+        first[v] = dlast && on ? dlast[thread * V + v] : 0.0f;
+    }
+    {
+        Vec<T, V> gs[kSteps], xs[kSteps];
+        load_steps<T, V>(at.in(q.gates) + t * q.gates.step, q.gates.step, n, gs);
+        load_steps<T, V>(at.in(q.inputs) + t * q.inputs.step, q.inputs.step, n, xs);
+        load_steps<T, V>(at.in(dout) + t * dout.step, dout.step, n, dys);
+        resets = load_resets<kResets, kSteps>(at.flags(q.resets) + t * q.resets.step, q.resets.step, n, q.one);
+        float h[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = 0.0f;
+        if (on && n > 0) {
+            const Vec<float, V> s = load<float, V>(saved + ((t / kSteps) * q.threads + thread) * V);
+#pragma unroll
+            for (int v = 0; v < V; ++v) h[v] = s.v[v];
+        }
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float x = (float)xs[i].v[v];
+                float a, b;
+                m[i][v] = gate_of((float)gs[i].v[v]);
+                gate_parts(m[i][v], a, b);
+                if (kResets && (resets >> i & 1u)) h[v] = 0.0f;
+                d[i][v] = h[v] - x;
+                h[v] = fmaf(a, h[v], b * x);
+                hold(m[i][v]);
+                hold(d[i][v]);
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+        const int i = kSteps - 1 - j;
+        if (i >= n) continue;
+        hold(dys[i]);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float a, b;
+            gate_parts(m[i][v], a, b);
+            const bool reset = kResets && (resets >> i & 1u);
+            f.v[v].H = reset ? 0.0f : a * ((float)dys[i].v[v] + f.v[v].H);
+            f.v[v].P = reset ? -0.0f : a * f.v[v].P;
+        }
+    }
+    state_before<V>(chain, lds, q.threads, thread, on, k, wave, f, first, c);
+    if (!on) return;
+    T* dg = at.in(dgates) + t * dgates.step;
+    T* dx = at.in(dinputs) + t * dinputs.step;
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+        const int i = kSteps - 1 - j;
+        if (i >= n) continue;
+        hold(dys[i]);
+        Vec<T, V> og, ox;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float a, b;
+            gate_parts(m[i][v], a, b);
+            const float G = (float)dys[i].v[v] + c[v], bG = b * G;
+            ox.v[v] = (T)bG;
+            og.v[v] = (T)(a * bG * d[i][v]);
+            c[v] = kResets && (resets >> i & 1u) ? 0.0f : a * G;
+        }
+        store<T, V>(dg + i * dgates.step, og);
+        store<T, V>(dx + i * dinputs.step, ox);
+    }
+    if (dstate && t == 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) dstate[thread * V + v] = c[v];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// many channels: a thread walks through all steps of its own
+// ---------------------------------------------------------------------------
 
 template <class T, int V, bool kResets>
 __global__ __launch_bounds__(256) void scan_kernel(const Sequences<T> q, const Tensor<T> out, float* __restrict__ last,
-                                                   float* __restrict__ saved, const Summaries<V> sums)
+                                                   float* __restrict__ saved)
 {
     const int64_t thread = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (thread >= q.threads) return;
-    const int32_t seg = blockIdx.y;
     const Place<T, V> at(thread, q.vectors);
-    const int64_t t0 = seg * q.segment, t1 = min(q.steps, t0 + q.segment);
     const T* g = at.in(q.gates);
     const T* x = at.in(q.inputs);
     const uint8_t* r = at.flags(q.resets);
@@ -288,7 +499,6 @@ __global__ __launch_bounds__(256) void scan_kernel(const Sequences<T> q, const T
     float h[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = q.state ? q.state[thread * V + v] : 0.0f;
-    if (seg > 0) fold<V, false>(sums, q.threads, thread, seg, q.segments, h);
     auto steps = [&](int64_t t, int n) {
         Vec<T, V> gs[kSteps], xs[kSteps];
         load_steps<T, V>(g + t * q.gates.step, q.gates.step, n, gs);
@@ -315,10 +525,10 @@ __global__ __launch_bounds__(256) void scan_kernel(const Sequences<T> q, const T
             store<T, V>(y + (t + i) * out.step, o);
         }
     };
-    int64_t t = t0;
-    for (; t + kSteps <= t1; t += kSteps) steps(t, kSteps);
-    if (t < t1) steps(t, (int)(t1 - t));
-    if (last && seg == q.segments - 1) {
+    int64_t t = 0;
+    for (; t + kSteps <= q.steps; t += kSteps) steps(t, kSteps);
+    if (t < q.steps) steps(t, (int)(q.steps - t));
+    if (last) {
 #pragma unroll
         for (int v = 0; v < V; ++v) last[thread * V + v] = h[v];
     }
@@ -328,13 +538,11 @@ template <class T, int V, bool kResets>
 __global__ __launch_bounds__(256, 4) void scan_gradient_kernel(const Sequences<T> q, const Tensor<const T> dout,
                                                             const float* __restrict__ dlast, const float* __restrict__ saved,
                                                             const Tensor<T> dgates, const Tensor<T> dinputs,
-                                                            float* __restrict__ dstate, const Summaries<V> sums)
+                                                            float* __restrict__ dstate)
 {
     const int64_t thread = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (thread >= q.threads) return;
-    const int32_t seg = blockIdx.y;
     const Place<T, V> at(thread, q.vectors);
-    const int64_t t0 = seg * q.segment, t1 = min(q.steps, t0 + q.segment);
     const T* g = at.in(q.gates);
     const T* x = at.in(q.inputs);
     const T* dy = at.in(dout);
@@ -344,7 +552,6 @@ __global__ __launch_bounds__(256, 4) void scan_gradient_kernel(const Sequences<T
     float c[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) c[v] = dlast ? dlast[thread * V + v] : 0.0f;
-    if (seg < q.segments - 1) fold<V, true>(sums, q.threads, thread, seg, q.segments, c);
     auto steps = [&](int64_t t, int n) {
         Vec<T, V> gs[kSteps], xs[kSteps], dys[kSteps];
         load_steps<T, V>(g + t * q.gates.step, q.gates.step, n, gs);
@@ -388,13 +595,13 @@ __global__ __launch_bounds__(256, 4) void scan_gradient_kernel(const Sequences<T
             store<T, V>(dx + (t + i) * dinputs.step, ox);
         }
     };
-    int64_t t = t1;
-    if ((t1 - t0) % kSteps) {
-        t -= (t1 - t0) % kSteps;
-        steps(t, (int)(t1 - t));
+    int64_t t = q.steps;
+    if (t % kSteps) {
+        t -= t % kSteps;
+        steps(t, (int)(q.steps - t));
     }
-    for (; t > t0; t -= kSteps) steps(t - kSteps, kSteps);
-    if (dstate && seg == 0) {
+    for (; t > 0; t -= kSteps) steps(t - kSteps, kSteps);
+    if (dstate) {
 #pragma unroll
         for (int v = 0; v < V; ++v) dstate[thread * V + v] = c[v];
     }
@@ -436,39 +643,32 @@ bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) 
 
 size_t size_of(int32_t t) { return t == PICTURA_F32 ? 4 : 2; }
 
-constexpr int64_t kWavesWanted = 4096;   // waves that fill the card
-constexpr int64_t kLeastSegment = 64;
+constexpr int64_t kManyWaves = 2048;   // waves that fill the card
 
-// Channels of a thread, and how the steps are cut.
+// Channels of a thread, and the tiles that the steps are cut into (0: not cut).
 struct Shape {
-    int32_t vec, segments;
-    int64_t threads, segment;
+    int32_t vec, tiles;
+    int64_t threads;
 };
 
 Shape shape_of(const pictura_sequences& q, int32_t vec)
 {
-    Shape s{vec, 1, q.batch * (q.channels / vec), q.steps};
+    Shape s{vec, 0, q.batch * (q.channels / vec)};
     const int64_t waves = (s.threads + 63) / 64;
-    int64_t segments = waves ? kWavesWanted / waves : 1;
-    if (segments > q.steps / kLeastSegment) segments = q.steps / kLeastSegment;
-    if (segments > kGroup * 32) segments = kGroup * 32;
-    if (segments < 2) return s;
-    s.segment = ((q.steps + segments - 1) / segments + kSteps - 1) / kSteps * kSteps;
-    s.segments = (int32_t)((q.steps + s.segment - 1) / s.segment);
+    const int64_t tiles = (q.steps + kTile - 1) / kTile;
+    // (a launch has fewer than 2^32 threads)
+    if (waves < kManyWaves && q.steps >= 2 * kTile && waves * tiles <= 1 << 21) s.tiles = (int32_t)tiles;
     return s;
 }
 
-uint64_t summary_bytes(const Shape& s)
-{
-    if (s.segments < 2) return 0;
-    return (uint64_t)(s.segments + (s.segments + kGroup - 1) / kGroup) * s.threads * s.vec * sizeof(Map);
-}
+int64_t chain_words(const Shape& s) { return (int64_t)(s.tiles + (s.tiles + kGroup - 1) / kGroup) * s.threads * s.vec; }
 
 // The most that any alignment of the tensors takes.
 uint64_t workspace_bytes_of(const pictura_sequences& q)
 {
-    const uint64_t one = summary_bytes(shape_of(q, 1)), two = q.dtype == PICTURA_F32 || q.channels % 2 ? 0 : summary_bytes(shape_of(q, 2));
-    return 256 + (one > two ? one : two);
+    const int64_t one = chain_words(shape_of(q, 1)),
+                  two = q.dtype == PICTURA_F32 || q.channels % 2 ? 0 : chain_words(shape_of(q, 2));
+    return 256 + sizeof(Word) * (uint64_t)(one > two ? one : two);
 }
 
 constexpr int64_t kMostChannels = (1ll << 31) - 1;   // of all sequences together
@@ -504,8 +704,8 @@ template <class T>
 Sequences<T> sequences_of(const pictura_sequences& q, const Shape& s)
 {
     return Sequences<T>{{(const T*)q.gates, q.gates_batch, q.gates_step}, {(const T*)q.inputs, q.inputs_batch, q.inputs_step},
-                        q.state, {q.resets, q.resets_batch, q.resets_step}, s.threads, q.steps, s.segment,
-                        q.channels / s.vec, s.segments, q.channels / s.vec % 64 == 0};
+                        q.state, {q.resets, q.resets_batch, q.resets_step}, s.threads, q.steps,
+                        q.channels / s.vec, q.channels / s.vec % 64 == 0};
 }
 
 // Whether pairs of channels can be loaded as one from a tensor of elements of e bytes.
@@ -514,11 +714,15 @@ bool pairs(const pictura_sequences& q, const void* p, int64_t batch, int64_t ste
     return aligned(p, 2 * e) && (q.batch < 2 || batch % 2 == 0) && (q.steps < 2 || step % 2 == 0);
 }
 
-template <int V>
-Summaries<V> summaries_of(void* workspace, const Shape& s)
+Chain chain_of(void* workspace, const Shape& s)
 {
-    Maps<V>* segments = (Maps<V>*)workspace;
-    return Summaries<V>{segments, segments + (int64_t)s.segments * s.threads};
+    Word* words = (Word*)((char*)workspace + 256);
+    return Chain{(uint32_t*)workspace, words, words + (int64_t)s.tiles * s.threads * s.vec, chain_words(s), s.tiles};
+}
+
+void clear(const Chain& c, hipStream_t st)
+{
+    hipLaunchKernelGGL(chain_kernel, dim3((unsigned)((c.words + 255) / 256)), dim3(256), 0, st, c);
 }
 
 // go(T{}, constant V, constant whether there are resets)
@@ -548,9 +752,10 @@ void with_kinds(const pictura_sequences& q, int32_t vec, F go)
     else typed((_Float16)0.0f);
 }
 
-dim3 grid_of(const Shape& s) { return dim3((unsigned)((s.threads + 255) / 256), (unsigned)s.segments); }
-
-dim3 summary_grid(const Shape& s) { return dim3((unsigned)((s.threads + 63) / 64), (unsigned)((s.segments + kGroup - 1) / kGroup)); }
+dim3 grid_of(const Shape& s)
+{
+    return s.tiles ? dim3((unsigned)((s.threads + 63) / 64 * s.tiles)) : dim3((unsigned)((s.threads + 255) / 256));
+}
 
 }  // namespace
 }  // namespace pictura
@@ -588,12 +793,14 @@ pictura_status pictura_gated_scan(const pictura_sequences* q, void* out, int64_t
         constexpr int V = decltype(v)::value;
         constexpr bool R = decltype(resets)::value;
         const Sequences<T> seq = sequences_of<T>(*q, s);
-        const Summaries<V> sums = summaries_of<V>(workspace, s);
-        if (s.segments > 1)
-            hipLaunchKernelGGL((summary_kernel<T, V, R, false>), summary_grid(s), dim3(64 * kGroup), 0, st, seq,
-                               Tensor<const T>{}, sums);
-        hipLaunchKernelGGL((scan_kernel<T, V, R>), grid_of(s), dim3(256), 0, st, seq, Tensor<T>{(T*)out, out_batch, out_step},
-                           last_state, saved, sums);
+        const Tensor<T> y{(T*)out, out_batch, out_step};
+        if (s.tiles) {
+            const Chain c = chain_of(workspace, s);
+            clear(c, st);
+            hipLaunchKernelGGL((tile_kernel<T, V, R>), grid_of(s), dim3(kTileWaves * 64), 0, st, seq, y, last_state, saved, c);
+        } else {
+            hipLaunchKernelGGL((scan_kernel<T, V, R>), grid_of(s), dim3(256), 0, st, seq, y, last_state, saved);
+        }
     });
     return launched();
 }
@@ -626,13 +833,16 @@ pictura_status pictura_gated_scan_gradient(const pictura_sequences* q, const flo
         constexpr int V = decltype(v)::value;
         constexpr bool R = decltype(resets)::value;
         const Sequences<T> seq = sequences_of<T>(*q, s);
-        const Summaries<V> sums = summaries_of<V>(workspace, s);
         const Tensor<const T> dy{(const T*)dout, dout_batch, dout_step};
-        if (s.segments > 1)
-            hipLaunchKernelGGL((summary_kernel<T, V, R, true>), summary_grid(s), dim3(64 * kGroup), 0, st, seq, dy, sums);
-        hipLaunchKernelGGL((scan_gradient_kernel<T, V, R>), grid_of(s), dim3(256), 0, st, seq, dy, dlast, saved,
-                           Tensor<T>{(T*)dgates, dgates_batch, dgates_step}, Tensor<T>{(T*)dinputs, dinputs_batch, dinputs_step},
-                           dstate, sums);
+        const Tensor<T> dg{(T*)dgates, dgates_batch, dgates_step}, dx{(T*)dinputs, dinputs_batch, dinputs_step};
+        if (s.tiles) {
+            const Chain c = chain_of(workspace, s);
+            clear(c, st);
+            hipLaunchKernelGGL((tile_gradient_kernel<T, V, R>), grid_of(s), dim3(kTileWaves * 64), 0, st, seq, dy, dlast, saved, dg,
+                               dx, dstate, c);
+        } else {
+            hipLaunchKernelGGL((scan_gradient_kernel<T, V, R>), grid_of(s), dim3(256), 0, st, seq, dy, dlast, saved, dg, dx, dstate);
+        }
     });
     return launched();
 }
@@ -646,7 +856,7 @@ pictura_status pictura_gated_step(const pictura_sequences* q, void* out, int64_t
     auto go = [&](auto t) {
         using T = decltype(t);
         constexpr int V = 16 / sizeof(T);
-        const Shape s{q->channels % V ? 1 : V, 1, q->batch * (q->channels / (q->channels % V ? 1 : V)), 1};
+        const Shape s{q->channels % V ? 1 : V, 0, q->batch * (q->channels / (q->channels % V ? 1 : V))};
         const dim3 grid((unsigned)((s.threads + 255) / 256));
         if (s.vec == 1)
             hipLaunchKernelGGL((step_kernel<T, 1>), grid, dim3(256), 0, (hipStream_t)stream, sequences_of<T>(*q, s), (T*)out,
