@@ -55,30 +55,26 @@ struct Sequences {
     bool one;                           // a wave's are of one sequence
 };
 
-// The smaller one of a = sigmoid(g) and 1 - a, with the sign set where that is 1 - a:
-// the other one is 1 - |m| to half a unit.  e = exp(-|g|) with the product by log2(e) in
-// two terms; at 128 and beyond it is 0 in fp32.
+// The smaller one of a = sigmoid(g) and 1 - a, with g's sign: the other one is 1 - |m| to half
+// a unit.  e = exp(-|g|) with the product by log2(e) in two terms; at 128 and beyond it is 0
+// in fp32.  e is off by up to 3.5 u (u = 2^-24), the reciprocal by 4.5 u, m by 8.5 u.
 __device__ __forceinline__ float gate_of(float g)
 {
     constexpr float kHi = 1.44269502f, kLo = 1.92596299e-8f, kLn2 = 0.693147182f;
     const float z = fabsf(g) > 128.0f ? 128.0f : fabsf(g);   // (a NaN stays one)
-    const float hi = z * -kHi, lo = fmaf(z, -kHi, -hi) - z * kLo;
+    const float hi = z * -kHi, lo = fmaf(z, -kLo, fmaf(z, -kHi, -hi));
     float e = __builtin_amdgcn_exp2f(hi);
     e = fmaf(e * lo, kLn2, e);
-    const float d = 1.0f + e;
-    float r = __builtin_amdgcn_rcpf(d);
-    r = fmaf(fmaf(-d, r, 1.0f), r, r);
-    const float m = e * r;
-    return g < 0.0f ? m : -m;
+    return copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), g);
 }
 
 // m as a and b = 1 - a.
 __device__ __forceinline__ void gate_parts(float m, float& a, float& b)
 {
     const float s = fabsf(m), l = 1.0f - s;
-    const bool positive = __float_as_uint(m) >> 31;
-    a = positive ? l : s;
-    b = positive ? s : l;
+    const bool negative = __float_as_uint(m) >> 31;
+    a = negative ? s : l;
+    b = negative ? l : s;
 }
 
 // What steps do to a state, h -> P h + H.  A reset among them makes P -0 (every other
@@ -166,6 +162,13 @@ __device__ __forceinline__ uint32_t load_resets(const uint8_t* p, int64_t step, 
     return bits;
 }
 
+// Waves of a tile, kSteps steps each: two channels a thread leave registers for two
+// workgroups of eight on a CU (one of 65,536 steps of 1,024 in bf16: forward 120 us, gradient
+// 173; with sixteen 120 and 180, with four 158 and 237), one channel for two of sixteen
+// (three of 8,192 of 330 in fp32: 30 and 43 us; with eight 37 and 45).
+constexpr int tile_waves(int vec) { return vec == 2 ? 8 : 16; }
+constexpr int tile_steps(int vec) { return tile_waves(vec) * kSteps; }
+
 template <int V>
 struct alignas(8 * V) Maps {
     Map v[V];
@@ -180,8 +183,6 @@ struct alignas(8 * V) Maps {
 // P in the lower half, which is kEmpty before; `groups` the state after every kGroup tiles in
 // the upper half of a word whose lower half is kEmpty before.
 constexpr uint32_t kEmpty = 0xFFFFFFFFu;
-constexpr int kTileWaves = 16;                   // waves of a tile, kSteps steps each
-constexpr int kTile = kTileWaves * kSteps;
 constexpr int kGroup = 16;                       // tiles of a group
 constexpr int kPolls = 1 << 20;                  // of a wait, a second or more
 
@@ -206,19 +207,30 @@ __device__ __forceinline__ void tell(Word* at, const Map& m)
     tell(at, p == kEmpty ? 0x7FC00000u : p, m.H);   // (a NaN of that pattern: any other)
 }
 
-// Waits until the V words are there.  A workgroup waits only for such with smaller tickets,
-// which have started before it and in turn wait only for smaller ones: every wait ends.
-// (If one did not, its values would be taken as they are, NaNs.)
 template <int V>
-__device__ __forceinline__ void await(const Word* at, bool on, Word (&w)[V])
+constexpr int kItems = kGroup / tile_waves(V);   // tiles of its group that a wave waits for
+
+// Waits until the words of up to kItems<V> tiles are there, `apart` of them apart.  A workgroup
+// waits only for such with smaller tickets, which have started before it and in turn wait
+// only for smaller ones: every wait ends.  (If one did not, its values would be taken as they
+// are, NaNs.)
+template <int V>
+__device__ __forceinline__ void await(const Word* at, int64_t apart, int items, bool on, Word (&w)[kItems<V>][V])
 {
     for (int i = 0; i < kPolls; ++i) {
         bool there = true;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            w[v] = on ? __hip_atomic_load(at + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
-            there = there && (uint32_t)w[v] != kEmpty;
-        }
+        for (int k = 0; k < kItems<V>; ++k)
+            if (k < items) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) w[k][v] = on ? __hip_atomic_load(at + k * apart + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+            }
+#pragma unroll
+        for (int k = 0; k < kItems<V>; ++k)
+            if (k < items) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) there = there && (uint32_t)w[k][v] != kEmpty;
+            }
         if (__all(there)) return;
         __builtin_amdgcn_s_sleep(1);
     }
@@ -234,8 +246,8 @@ static __global__ __launch_bounds__(256) void chain_kernel(const Chain c)
 
 template <int V>
 struct TileLds {
-    Maps<V> waves[kTileWaves][64];    // of this tile
-    Maps<V> before[kTileWaves][64];   // of the tiles before it in its group; the last row: the state before those
+    Maps<V> waves[tile_waves(V)][64];   // of this tile
+    Maps<V> before[kGroup][64];      // of the tiles before it in its group; the last row: the state before those
     uint32_t ticket;
 };
 
@@ -260,10 +272,10 @@ __device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, in
     const int32_t g = k / kGroup, r = k % kGroup;
     lds.waves[w][lane] = f;
     __syncthreads();
-    if (w == kTileWaves - 1 && r < kGroup - 1 && k < c.count - 1) {   // what the whole tile does
+    if (w == tile_waves(V) - 1 && r < kGroup - 1 && k < c.count - 1) {   // what the whole tile does
         Maps<V> all = lds.waves[0][lane];
 #pragma unroll 2
-        for (int i = 1; i < kTileWaves; ++i) {
+        for (int i = 1; i < tile_waves(V); ++i) {
             const Maps<V> m = lds.waves[i][lane];
 #pragma unroll
             for (int v = 0; v < V; ++v) all.v[v] = then(all.v[v], m.v[v]);
@@ -273,41 +285,43 @@ __device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, in
             for (int v = 0; v < V; ++v) tell(c.tiles + ((int64_t)k * threads + thread) * V + v, all.v[v]);
         }
     }
-    // each wave waits for one of the tiles before, the last one for the group before
+    // each wave waits for some of the tiles before, the last one for the group before as well
     Maps<V> m;
-    if (w < r) {
-        Word x[V];
-        await<V>(c.tiles + ((int64_t)(g * kGroup + w) * threads + thread) * V, on, x);
+    Word x[kItems<V>][V];
+    const int mine = min(kItems<V>, r - w * kItems<V>);
+    if (mine > 0) {
+        await<V>(c.tiles + ((int64_t)(g * kGroup + w * kItems<V>) * threads + thread) * V, threads * V, mine, on, x);
 #pragma unroll
-        for (int v = 0; v < V; ++v) m.v[v] = Map{__uint_as_float((uint32_t)x[v]), __uint_as_float((uint32_t)(x[v] >> 32))};
-        lds.before[w][lane] = m;
-    } else if (w == kTileWaves - 1) {
-        if (g > 0) {
-            Word x[V];
-            await<V>(c.groups + ((int64_t)(g - 1) * threads + thread) * V, on, x);
+        for (int i = 0; i < kItems<V>; ++i)
+            if (i < mine) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) m.v[v].H = __uint_as_float((uint32_t)(x[v] >> 32));
-        } else {
+                for (int v = 0; v < V; ++v) m.v[v] = Map{__uint_as_float((uint32_t)x[i][v]), __uint_as_float((uint32_t)(x[i][v] >> 32))};
+                lds.before[w * kItems<V> + i][lane] = m;
+            }
+    }
+    if (w == tile_waves(V) - 1) {
+        if (g > 0) await<V>(c.groups + ((int64_t)(g - 1) * threads + thread) * V, 0, 1, on, x);
 #pragma unroll
-            for (int v = 0; v < V; ++v) m.v[v].H = first[v];
-        }
-        lds.before[w][lane] = m;
+        for (int v = 0; v < V; ++v) m.v[v].H = g > 0 ? __uint_as_float((uint32_t)(x[0][v] >> 32)) : first[v];
+        lds.before[kGroup - 1][lane] = m;
     }
     __syncthreads();
-    m = lds.before[kTileWaves - 1][lane];
+    m = lds.before[kGroup - 1][lane];
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = m.v[v].H;
+#pragma unroll 4
     for (int i = 0; i < r; ++i) {
         m = lds.before[i][lane];
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = apply(m.v[v], h[v]);
     }
+#pragma unroll 4
     for (int i = 0; i < w; ++i) {
         m = lds.waves[i][lane];
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = apply(m.v[v], h[v]);
     }
-    if (w == kTileWaves - 1 && r == kGroup - 1 && k < c.count - 1 && on) {   // the state after the group
+    if (w == tile_waves(V) - 1 && r == kGroup - 1 && k < c.count - 1 && on) {   // the state after the group
 #pragma unroll
         for (int v = 0; v < V; ++v) tell(c.groups + ((int64_t)g * threads + thread) * V + v, 0u, apply(f.v[v], h[v]));
     }
@@ -316,7 +330,7 @@ __device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, in
 // Forwards over one tile: a and (1 - a) x of a wave's 16 steps stay in registers while it
 // waits for the state before them, so that everything is read once.
 template <class T, int V, bool kResets>
-__global__ __launch_bounds__(kTileWaves * 64, 4) void tile_kernel(const Sequences<T> q, const Tensor<T> out, float* __restrict__ last,
+__global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_kernel(const Sequences<T> q, const Tensor<T> out, float* __restrict__ last,
                                                                   float* __restrict__ saved, const Chain chain)
 {
     __shared__ TileLds<V> lds;
@@ -326,7 +340,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 4) void tile_kernel(const Sequence
     const int64_t thread = (int64_t)block * 64 + lane;
     const bool on = thread < q.threads;
     const Place<T, V> at(on ? thread : 0, q.vectors);   // (lanes beyond the last channel read the first ones' and write nothing)
-    const int64_t t = (int64_t)tile * kTile + wave * kSteps;
+    const int64_t t = (int64_t)tile * tile_steps(V) + wave * kSteps;
     const int n = (int)max((int64_t)0, min((int64_t)kSteps, q.steps - t));
     float a[kSteps][V], add[kSteps][V], first[V], h[V];
     uint32_t resets;
@@ -386,7 +400,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 4) void tile_kernel(const Sequence
 
 // Backwards over one tile, from the last one on.
 template <class T, int V, bool kResets>
-__global__ __launch_bounds__(kTileWaves * 64, 4) void tile_gradient_kernel(const Sequences<T> q, const Tensor<const T> dout,
+__global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_gradient_kernel(const Sequences<T> q, const Tensor<const T> dout,
                                                                            const float* __restrict__ dlast,
                                                                            const float* __restrict__ saved, const Tensor<T> dgates,
                                                                            const Tensor<T> dinputs, float* __restrict__ dstate,
@@ -399,7 +413,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 4) void tile_gradient_kernel(const
     const int64_t thread = (int64_t)block * 64 + lane;
     const bool on = thread < q.threads;
     const Place<T, V> at(on ? thread : 0, q.vectors);
-    const int64_t t = (int64_t)(chain.count - 1 - k) * kTile + (kTileWaves - 1 - wave) * kSteps;
+    const int64_t t = (int64_t)(chain.count - 1 - k) * tile_steps(V) + (tile_waves(V) - 1 - wave) * kSteps;
     const int n = (int)max((int64_t)0, min((int64_t)kSteps, q.steps - t));
     float m[kSteps][V], d[kSteps][V], first[V], c[V];
     Vec<T, V> dys[kSteps];
@@ -643,7 +657,10 @@ bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) 
 
 size_t size_of(int32_t t) { return t == PICTURA_F32 ? 4 : 2; }
 
-constexpr int64_t kManyWaves = 2048;   // waves that fill the card
+// Waves from which on every thread walks through all steps.  Walking against tiles, us (bf16,
+// 64 M elements, 512 steps): 512 waves forward 139 and 97, gradient 372 and 151; 1,024 waves 82
+// and 103, 219 and 161; 1,600 waves (105 M) 136 and 141, 265 and 226.
+constexpr int64_t kManyWaves = 1024, kManyBack = 2048;
 
 // Channels of a thread, and the tiles that the steps are cut into (0: not cut).
 struct Shape {
@@ -651,13 +668,12 @@ struct Shape {
     int64_t threads;
 };
 
-Shape shape_of(const pictura_sequences& q, int32_t vec)
+Shape shape_of(const pictura_sequences& q, int32_t vec, bool back)
 {
     Shape s{vec, 0, q.batch * (q.channels / vec)};
-    const int64_t waves = (s.threads + 63) / 64;
-    const int64_t tiles = (q.steps + kTile - 1) / kTile;
+    const int64_t waves = (s.threads + 63) / 64, tile = tile_steps(vec), tiles = (q.steps + tile - 1) / tile;
     // (a launch has fewer than 2^32 threads)
-    if (waves < kManyWaves && q.steps >= 2 * kTile && waves * tiles <= 1 << 21) s.tiles = (int32_t)tiles;
+    if (waves < (back ? kManyBack : kManyWaves) && q.steps >= 2 * tile && waves * tiles <= 1 << 21) s.tiles = (int32_t)tiles;
     return s;
 }
 
@@ -666,8 +682,8 @@ int64_t chain_words(const Shape& s) { return (int64_t)(s.tiles + (s.tiles + kGro
 // The most that any alignment of the tensors takes.
 uint64_t workspace_bytes_of(const pictura_sequences& q)
 {
-    const int64_t one = chain_words(shape_of(q, 1)),
-                  two = q.dtype == PICTURA_F32 || q.channels % 2 ? 0 : chain_words(shape_of(q, 2));
+    const int64_t one = chain_words(shape_of(q, 1, true)),
+                  two = q.dtype == PICTURA_F32 || q.channels % 2 ? 0 : chain_words(shape_of(q, 2, true));
     return 256 + sizeof(Word) * (uint64_t)(one > two ? one : two);
 }
 
@@ -786,7 +802,7 @@ pictura_status pictura_gated_scan(const pictura_sequences* q, void* out, int64_t
     const bool two = e == 2 && q->channels % 2 == 0 && pairs(*q, q->gates, q->gates_batch, q->gates_step, e) &&
                      pairs(*q, q->inputs, q->inputs_batch, q->inputs_step, e) && pairs(*q, out, out_batch, out_step, e) &&
                      aligned(saved, 8);
-    const Shape s = shape_of(*q, two ? 2 : 1);
+    const Shape s = shape_of(*q, two ? 2 : 1, false);
     hipStream_t st = (hipStream_t)stream;
     with_kinds(*q, s.vec, [&](auto t, auto v, auto resets) {
         using T = decltype(t);
@@ -797,7 +813,7 @@ pictura_status pictura_gated_scan(const pictura_sequences* q, void* out, int64_t
         if (s.tiles) {
             const Chain c = chain_of(workspace, s);
             clear(c, st);
-            hipLaunchKernelGGL((tile_kernel<T, V, R>), grid_of(s), dim3(kTileWaves * 64), 0, st, seq, y, last_state, saved, c);
+            hipLaunchKernelGGL((tile_kernel<T, V, R>), grid_of(s), dim3(tile_waves(V) * 64), 0, st, seq, y, last_state, saved, c);
         } else {
             hipLaunchKernelGGL((scan_kernel<T, V, R>), grid_of(s), dim3(256), 0, st, seq, y, last_state, saved);
         }
@@ -826,7 +842,7 @@ pictura_status pictura_gated_scan_gradient(const pictura_sequences* q, const flo
                      pairs(*q, q->inputs, q->inputs_batch, q->inputs_step, e) && pairs(*q, dout, dout_batch, dout_step, e) &&
                      pairs(*q, dgates, dgates_batch, dgates_step, e) && pairs(*q, dinputs, dinputs_batch, dinputs_step, e) &&
                      aligned(saved, 8);
-    const Shape s = shape_of(*q, two ? 2 : 1);
+    const Shape s = shape_of(*q, two ? 2 : 1, true);
     hipStream_t st = (hipStream_t)stream;
     with_kinds(*q, s.vec, [&](auto t, auto v, auto resets) {
         using T = decltype(t);
@@ -838,7 +854,7 @@ pictura_status pictura_gated_scan_gradient(const pictura_sequences* q, const flo
         if (s.tiles) {
             const Chain c = chain_of(workspace, s);
             clear(c, st);
-            hipLaunchKernelGGL((tile_gradient_kernel<T, V, R>), grid_of(s), dim3(kTileWaves * 64), 0, st, seq, dy, dlast, saved, dg,
+            hipLaunchKernelGGL((tile_gradient_kernel<T, V, R>), grid_of(s), dim3(tile_waves(V) * 64), 0, st, seq, dy, dlast, saved, dg,
                                dx, dstate, c);
         } else {
             hipLaunchKernelGGL((scan_gradient_kernel<T, V, R>), grid_of(s), dim3(256), 0, st, seq, dy, dlast, saved, dg, dx, dstate);
