@@ -13,6 +13,7 @@ from __future__ import annotations
 from typing import NamedTuple, Optional
 
 import torch
+import torch.nn as nn
 
 from paper_2607_26005_amd import _tensors, pictura
 from paper_2607_26005_amd.pictura import EINVAL, PicturaError
@@ -88,3 +89,54 @@ def rms_norm_8bit(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torc
         return RowCodes(*_tensors.rms_norm_8bit(x, weight, residual, eps, dtype is not torch.int8))
     except ValueError as e:
         raise PicturaError(EINVAL, str(e)) from None
+
+
+class MemoryLayer(nn.Module):
+    """A layer of a policy that remembers: norm, one projection to gates and inputs, the gated
+    recurrence, and a projection back, beside the residual stream.
+
+    x is what the layer before put out and `residual` the stream before that was added (None
+    for the first layer): their sum is taken by the norm."""
+
+    def __init__(self, width: int, eps: float = 1e-6):
+        super().__init__()
+        self.width, self.eps = width, eps
+        self.norm = nn.Parameter(torch.ones(width))
+        self.project = nn.Linear(width, 2 * width)
+        self.out = nn.Linear(width, width)
+        with torch.no_grad():   # gates that keep for some ten steps
+            self.project.bias[:width] = 2.0
+
+    def _split(self, x, residual, y):
+        return y if residual is not None else (y, x)
+
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, state: Optional[torch.Tensor] = None,
+                resets: Optional[torch.Tensor] = None):
+        """x [batch, steps, width] -> (output, residual stream, state after the last step)."""
+        y, stream = self._split(x, residual, rms_norm(x, self.norm, residual, self.eps))
+        gates, inputs = self.project(y).chunk(2, -1)
+        h, state = gated_scan(gates, inputs, state, resets)
+        return self.out(h), stream, state
+
+    def quantized(self):
+        """The projection's weights in 8 bits, for `step`: (codes [2 width, width], scales)."""
+        w = self.project.weight.detach()
+        scales = w.abs().amax(1, keepdim=True).clamp(min=1e-30).float() / 448.0
+        return (w.float() / scales).to(torch.float8_e4m3fn), scales.t().contiguous()
+
+    @torch.no_grad()
+    def step(self, x: torch.Tensor, residual: Optional[torch.Tensor], state: torch.Tensor,
+             resets: Optional[torch.Tensor] = None, codes=None):
+        """One step of [batch, width] on `state` (float32, replaced) -> (output, residual
+        stream).  codes (of `quantized`): the projection multiplies in 8 bits (width a multiple
+        of 16)."""
+        if codes is None:
+            y, stream = self._split(x, residual, rms_norm(x, self.norm, residual, self.eps))
+            both = self.project(y)
+        else:
+            held = rms_norm_8bit(x, self.norm, residual, self.eps)
+            stream = x if residual is None else held.sum
+            both = torch._scaled_mm(held.codes, codes[0].t(), scale_a=held.scales[:, None], scale_b=codes[1],
+                                    out_dtype=torch.bfloat16).to(x.dtype) + self.project.bias
+        gates, inputs = both.chunk(2, -1)
+        return self.out(gated_step(gates, inputs, state, resets)), stream
