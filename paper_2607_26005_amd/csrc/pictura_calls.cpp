@@ -9,7 +9,7 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
-#include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/variable.h>
 
 #include "pictura.h"
@@ -102,21 +102,22 @@ void check_capture(std::initializer_list<std::pair<const Tensor*, const char*>> 
     }
 }
 
-// What a backward returns can not be differentiated again: trying to is an error.
-variable_list once(const variable_list& grads, variable_list out)
+// What a backward returns can not be differentiated again.  Where a graph of it is wanted,
+// it hangs on what it was computed from by a node that raises.
+struct Twice : torch::autograd::Node {
+    variable_list apply(variable_list&&) override
+    {
+        throw std::runtime_error("trying to differentiate twice a function of this library, whose gradients have none");
+    }
+};
+
+variable_list once(const variable_list& from, variable_list out)
 {
-    bool again = false;
-    for (const Tensor& g : grads) again = again || (g.defined() && g.requires_grad());
-    if (!again) return out;
-    variable_list some;
+    if (!at::GradMode::is_enabled()) return out;
+    const auto node = std::make_shared<Twice>();
+    node->set_next_edges(torch::autograd::collect_next_edges(from));
     for (Tensor& t : out)
-        if (t.defined()) some.push_back(t.detach().requires_grad_());
-    const auto error = std::make_shared<torch::autograd::DelayedError>(
-        "trying to differentiate twice a function of this library", static_cast<int64_t>(some.size()));
-    some = (*error)(std::move(some));
-    size_t k = 0;
-    for (Tensor& t : out)
-        if (t.defined()) t = some[k++];
+        if (t.defined()) torch::autograd::set_history(t, node);
     return out;
 }
 
@@ -125,6 +126,10 @@ template <class F>
 PyObject* guarded(F f)
 {
     HANDLE_TH_ERRORS
+    if (!entries.scan) {
+        PyErr_SetString(PyExc_RuntimeError, "the library's entries are not bound: import memory or policy");
+        return nullptr;
+    }
     try {
         return f();
     } catch (const Refused& e) {
@@ -243,7 +248,7 @@ struct GatedScan : torch::autograd::Function<GatedScan> {
                                         (uint64_t)ws.numel(), stream_of(gates)),
                   "gated_scan_gradient");
         }
-        return once(grads, std::move(out));
+        return once({gates, inputs, saved, grads[0], grads[1]}, std::move(out));
     }
 };
 
@@ -271,6 +276,8 @@ PyObject* gated_step(PyObject*, PyObject* const* args, Py_ssize_t n)
         arguments(n, 5, "gated_step");
         const Tensor &gates = given(args[0], "gates"), &inputs = given(args[1], "inputs"), &state = given(args[2], "state");
         const Sequences q = sequences_of(false, gates, inputs, &state, optional(args[3], "resets"));
+        if (wants_gradient({&gates, &inputs, &state}))
+            refuse("gated_step hands on no gradient: call it under torch.no_grad(), or gated_scan");
         const Tensor* given_out = optional(args[4], "out");
         if (given_out && !apart(q, place(*given_out, "out", gates, false)))
             refuse("out: strides ", given_out->strides(), ": elements overlap");
@@ -338,7 +345,7 @@ struct RMSNorm : torch::autograd::Function<RMSNorm> {
         const Tensor dsum = grads.size() > 1 ? grads[1] : Tensor();
         variable_list out(4);
         if (!grads[0].defined()) {
-            out[0] = out[2] = dsum;   // (both undefined without a residual)
+            out[0] = out[2] = dsum;   // (both undefined without a residual; linear, so nothing is lost)
             return out;
         }
         {
@@ -362,9 +369,10 @@ struct RMSNorm : torch::autograd::Function<RMSNorm> {
                   "rms_norm_gradient");
             out[0] = dx;
             out[1] = dw;
-            if (grads.size() > 1) out[2] = dx;   // (there is a residual)
         }
-        return once(grads, std::move(out));
+        out = once({total, weight, grads[0], dsum}, std::move(out));
+        if (grads.size() > 1) out[2] = out[0];   // (there is a residual)
+        return out;
     }
 };
 
@@ -518,7 +526,7 @@ variable_list preferred(const Tensor& logits, const Preferences& p)
     q.weights = (const float*)vector(p.weights, "weights", at::kFloat, q.pairs, logits);
     if (!(p.beta > 0 && p.beta < 3e38) || (float)p.beta == 0.0f) refuse("beta: ", p.beta, ", expected a number within range");
     if (!(p.smoothing >= 0 && (float)p.smoothing < 1.0f)) refuse("smoothing: ", p.smoothing, ", expected a number within range");
-    if (!(p.denominator >= 0 && p.denominator < 3e38)) refuse("denominator: ", p.denominator, ", expected a number within range");
+    if (!(p.denominator >= 0 && p.denominator < 3e38) || (p.denominator > 0 && (float)p.denominator == 0.0f)) refuse("denominator: ", p.denominator, ", expected a number within range");
     q.beta = (float)p.beta;
     q.smoothing = (float)p.smoothing;
     q.denominator = (float)p.denominator;
@@ -565,7 +573,7 @@ struct PreferenceLoss : torch::autograd::Function<PreferenceLoss> {
                 at::mul_out(out[0], dlogits.to(at::kFloat), grads[0]);
             }
         }
-        return once(grads, std::move(out));
+        return once({grads[0]}, std::move(out));   // (the logits are not kept for this)
     }
 };
 

@@ -9,7 +9,7 @@
 //
 // Heads of up to 64 actions: a workgroup to a pair, which keeps its rows in registers
 // between the sums and the gradient (pairs of more than 256 rows of 16 actions, or 32 of 64,
-// read them again).  Larger heads: one launch for the rows' log-probabilities, one for the
+// read them again; pairs of thousands of rows take the three launches of larger heads).  Larger heads: one launch for the rows' log-probabilities, one for the
 // pairs, one for the gradient, which reads the logits again.
 #include <cmath>
 
@@ -41,6 +41,7 @@ struct Pairs {
     int64_t dstride;
 };
 
+constexpr int kPairThreads = 256;       // of a workgroup that sums up a pair
 constexpr int kTerms = 4;               // of a pair: loss, rewards, whether the preferred one's is larger
 constexpr int64_t kFewPairs = 2048;     // weights of so many are added up by every workgroup that needs their sum
 
@@ -356,6 +357,39 @@ __global__ __launch_bounds__(256) void pair_kernel(const Rows R, const Pairs q, 
     }
 }
 
+// Sequences too long for a workgroup to a pair: every row's log-probability, ...
+template <class T, int G, int E>
+__global__ __launch_bounds__(256) void small_row_kernel(const Rows R, const Pairs q, const Scratch k)
+{
+    constexpr int kRows = 256 / G;
+    const int member = threadIdx.x % G, mine = threadIdx.x / G;
+    const int64_t from = bound_of(q, 0, R.rows), to = bound_of(q, 2 * q.count, R.rows);
+    SmallRow<T, G, E> row;
+    for (int64_t n = (int64_t)blockIdx.x * kRows + mine; n < R.rows; n += (int64_t)gridDim.x * kRows) {
+        row.read(R, q, n, member);
+        const bool on = row.counts && n >= from && n < to;
+        if (member == 0) {
+            k.factor[n] = on ? 1.0f : 0.0f;
+            k.ratio[n] = on ? row.logp - row.ref : 0.0f;
+        }
+    }
+}
+
+// ... and, after terms_kernel, its gradient.
+template <class T, int G, int E>
+__global__ __launch_bounds__(256) void small_gradient_kernel(const Rows R, const Pairs q, const Scratch k)
+{
+    constexpr int kRows = 256 / G;
+    const int member = threadIdx.x % G, mine = threadIdx.x / G;
+    SmallRow<T, G, E> row;
+    for (int64_t n = (int64_t)blockIdx.x * kRows + mine; n < R.rows; n += (int64_t)gridDim.x * kRows) {
+        const float c = k.factor[n];
+        row.read(R, q, n, member);
+        if (c == 0.0f) row.counts = false;
+        row.write(R, q, n, member, c);
+    }
+}
+
 // ---------------------------------------------------------------------------
 // larger heads
 // ---------------------------------------------------------------------------
@@ -457,22 +491,34 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void row_kernel(const Rows
 }
 
 // A workgroup to a pair: its sums, and the factors of its rows.
-static __global__ __launch_bounds__(256) void terms_kernel(const Pairs q, const Scratch k, int64_t all)
+static __global__ __launch_bounds__(kPairThreads) void terms_kernel(const Pairs q, const Scratch k, int64_t all)
 {
+    constexpr int kAhead = 4;   // loads under way
     for (int64_t p = blockIdx.x; p < q.count; p += gridDim.x) {
         const int64_t first = bound_of(q, 2 * p, all), middle = max(first, bound_of(q, 2 * p + 1, all)),
                       last = max(middle, bound_of(q, 2 * p + 2, all));
         double sum[2] = {};
         uint32_t rows[2] = {};
-        for (int64_t n = first + threadIdx.x; n < last; n += 256) {
-            const uint32_t counts = k.factor[n] != 0.0f;
-            const double d = (double)k.ratio[n];
-            if (n < middle) sum[0] += d, rows[0] += counts;
-            else sum[1] += d, rows[1] += counts;
+        for (int64_t n = first + threadIdx.x; n < last; n += kAhead * kPairThreads) {
+            float f[kAhead], d[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int64_t i = n + u * kPairThreads;
+                f[u] = i < last ? k.factor[i] : 0.0f;
+                d[u] = i < last ? k.ratio[i] : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const bool other = n + u * kPairThreads >= middle;
+                sum[0] += other ? 0.0 : (double)d[u];
+                sum[1] += other ? (double)d[u] : 0.0;
+                rows[0] += !other && f[u] != 0.0f;
+                rows[1] += other && f[u] != 0.0f;
+            }
         }
         float c[2];
         finish_pair(q, k, p, sum, rows, c);
-        for (int64_t n = first + threadIdx.x; n < last; n += 256)
+        for (int64_t n = first + threadIdx.x; n < last; n += kPairThreads)
             if (k.factor[n] != 0.0f) k.factor[n] = c[n < middle ? 0 : 1];
     }
 }
@@ -516,12 +562,17 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void gradient_kernel(const
 // ---------------------------------------------------------------------------
 
 constexpr int kSmallHead = 64;
+// Rows of a pair, on average, from which on its sequences are spread over workgroups: one
+// alone walks through 4,096 rows of 12 in some 50 us.
+constexpr int64_t kLongPair = 4096;
+
+bool by_pairs(int64_t rows, int32_t actions, int64_t pairs) { return actions <= kSmallHead && rows <= kLongPair * pairs; }
 
 uint64_t rounded(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 uint64_t scratch_bytes(int64_t rows, int32_t actions, int64_t pairs)
 {
-    return 256 + rounded(pairs * kTerms * sizeof(double)) + (actions > kSmallHead ? rounded(rows * 8) + 2 * rounded(rows * 4) : 0);
+    return 256 + rounded(pairs * kTerms * sizeof(double)) + (by_pairs(rows, actions, pairs) ? 0 : rounded(rows * 8) + 2 * rounded(rows * 4));
 }
 
 Scratch scratch_of(void* workspace, int64_t rows, int64_t pairs)
@@ -541,10 +592,30 @@ void launch(const Rows& R, const Pairs& q, const Scratch& k, hipStream_t st)
 {
     if (q.weights && q.denominator == 0.0f && q.count > kFewPairs)
         hipLaunchKernelGGL(weight_sum_kernel, dim3(1), dim3(1024), 0, st, q, k);
-    if (R.actions <= kSmallHead) {
+    auto with_rows = [&](auto go) {   // lanes of a row, elements of a lane
+        if (R.actions <= 16) go(Int<1>{}, Int<16>{});
+        else go(Int<8>{}, Int<8>{});
+    };
+    auto terms = [&] {
+        if (q.count > 0) hipLaunchKernelGGL(terms_kernel, dim3((unsigned)q.count), dim3(kPairThreads), 0, st, q, k, R.rows);
+    };
+    if (by_pairs(R.rows, R.actions, q.count)) {
         const dim3 grid((unsigned)(q.count + kOutside));
-        if (R.actions <= 16) hipLaunchKernelGGL((pair_kernel<T, 1, 16>), grid, dim3(256), 0, st, R, q, k);
-        else hipLaunchKernelGGL((pair_kernel<T, 8, 8>), grid, dim3(256), 0, st, R, q, k);
+        with_rows([&](auto g, auto e) {
+            hipLaunchKernelGGL((pair_kernel<T, decltype(g)::value, decltype(e)::value>), grid, dim3(256), 0, st, R, q, k);
+        });
+        hipLaunchKernelGGL(stats_kernel, dim3(1), dim3(256), 0, st, q, k);
+        return;
+    }
+    if (R.actions <= kSmallHead) {
+        with_rows([&](auto g, auto e) {
+            constexpr int G = decltype(g)::value, E = decltype(e)::value;
+            const int64_t all = (R.rows * G + 255) / 256, most = 1 << 20;
+            const dim3 grid((unsigned)(all < most ? all : most));
+            hipLaunchKernelGGL((small_row_kernel<T, G, E>), grid, dim3(256), 0, st, R, q, k);
+            terms();
+            hipLaunchKernelGGL((small_gradient_kernel<T, G, E>), grid, dim3(256), 0, st, R, q, k);
+        });
         hipLaunchKernelGGL(stats_kernel, dim3(1), dim3(256), 0, st, q, k);
         return;
     }
@@ -555,8 +626,7 @@ void launch(const Rows& R, const Pairs& q, const Scratch& k, hipStream_t st)
         const int64_t all = (R.rows + kTeams - 1) / kTeams, most = 1 << 20;
         const dim3 grid((unsigned)(all < 1 ? 1 : all < most ? all : most));
         hipLaunchKernelGGL((row_kernel<T, NW>), grid, dim3(NT), 0, st, R, q, k);
-        if (q.count > 0)
-            hipLaunchKernelGGL(terms_kernel, dim3((unsigned)(q.count < most ? q.count : most)), dim3(256), 0, st, q, k, R.rows);
+        terms();
         hipLaunchKernelGGL((gradient_kernel<T, NW>), grid, dim3(NT), 0, st, R, q, k);
     };
     if (vectors <= 256) go(Int<1>{});

@@ -30,7 +30,9 @@ def gated_scan(gates: torch.Tensor, inputs: torch.Tensor, state: Optional[torch.
     rollout's [steps, batch, channels] transposed is as good), channels contiguous.  The
     recurrence runs in float32; out has the inputs' type.  state: what is remembered before
     the first step (None: nothing).  resets, bool or uint8 [batch, steps]: where true, an
-    episode begins with that step, and what came before is forgotten.
+    episode begins with that step, and what came before is forgotten.  Sequences packed one
+    behind the other are one with resets; padding behind a sequence changes nothing before
+    it (with a reset where it begins also if it holds no numbers), but is in the last state.
 
     Gradients flow to gates, inputs and state."""
     try:
@@ -44,7 +46,7 @@ def gated_step(gates: torch.Tensor, inputs: torch.Tensor, state: torch.Tensor, r
     """One step of gated_scan's recurrence for [batch, channels], the policy's form when it
     acts: `state` (float32) is replaced by what is remembered after the step, and returned in
     the inputs' type (in `out`, where that is given; it may be the inputs or the gates).
-    resets: [batch].  No gradient flows through it."""
+    resets: [batch].  No gradient flows through it: where one is wanted it is refused."""
     try:
         return _tensors.gated_step(gates, inputs, state, resets, out)
     except ValueError as e:

@@ -715,7 +715,7 @@ def pictura_preference_loss(logits, actions, offsets, out_stats, out_ratios, dlo
     os_, = _vectors(logits, len(PREFERENCE_STATS), "out_stats", "f", out_stats)
     ra, = _vectors(logits, 2 * P, "out_ratios", "f", out_ratios)
     for name, v, ok in (("beta", beta, lambda v: 0 < v < 3e38), ("smoothing", smoothing, lambda v: 0 <= v < 1),
-                        ("denominator", denominator, lambda v: 0 <= v < 3e38)):
+                        ("denominator", denominator, lambda v: v == 0 or 1e-38 < v < 3e38)):
         if isinstance(v, bool) or not isinstance(v, (int, float)) or not ok(v):
             raise PicturaError(EINVAL, f"{name}: {v!r}, expected a number within range")
     how = _PREFERENCES_PACK.pack(ac, of, rf, we, P, beta, smoothing, denominator, bool(average))

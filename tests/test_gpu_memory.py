@@ -348,3 +348,86 @@ def test_offsets_beyond_32_bits():
     want, last = memory.gated_scan(g, x, s)
     got, last2 = memory.gated_scan(g2, view, s)
     assert torch.equal(got, want) and torch.equal(last, last2)
+
+
+def test_padding_behind_a_reset_may_hold_anything():
+    from paper_2607_26005_amd import memory
+    for T, n in ((30, 17), (900, 500)):
+        g, x, s, _ = _inputs(1, T, 6, torch.float32)
+        resets = torch.zeros(1, T, dtype=torch.bool, device="cuda")
+        resets[0, n] = True
+        leaves = [t.clone().requires_grad_() for t in (g[:, :n], x[:, :n], s)]
+        out, _ = memory.gated_scan(*leaves)
+        dout = _rand(3, 1, n, 6).cuda()
+        want = torch.autograd.grad(out, leaves, dout)
+        with torch.no_grad():
+            g[:, n:], x[:, n:] = float("nan"), float("inf")
+        padded = [t.clone().requires_grad_() for t in (g, x, s)]
+        got, _ = memory.gated_scan(*padded, resets)
+        # (cut into tiles or not: the same to a few units)
+        assert torch.allclose(got[:, :n], out, rtol=1e-5, atol=1e-6)
+        grads = torch.autograd.grad(got, padded, torch.cat([dout, torch.zeros(1, T - n, 6, device="cuda")], 1))
+        for a, b in zip(grads[:2], want[:2]):
+            assert torch.allclose(a[:, :n], b, rtol=1e-4, atol=1e-6)
+        assert torch.allclose(grads[2], want[2], rtol=1e-4, atol=1e-6)
+
+
+def test_gradients_are_not_differentiated_again():
+    from paper_2607_26005_amd import memory, policy
+    g, x, s, _ = _inputs(2, 9, 4, torch.float32)
+    x.requires_grad_()
+    w = torch.ones(4, device="cuda", requires_grad=True)
+    l = torch.randn(4, 5, device="cuda", requires_grad=True)
+    a, o = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.tensor([0, 2, 4]).cuda()
+    for f, t in ((lambda: memory.gated_scan(g, x, s)[0], x), (lambda: memory.rms_norm(x, w), x),
+                 (lambda: memory.rms_norm(x, w, x.detach())[0], x), (lambda: policy.preference_loss(l, a, o)[0], l)):
+        once, = torch.autograd.grad(f().sum(), t, create_graph=True)
+        plain, = torch.autograd.grad(f().sum(), t)
+        assert torch.equal(once, plain)
+        with pytest.raises(RuntimeError, match="differentiate twice"):
+            once.pow(2).sum().backward()
+        if t is not l:   # (that loss does not keep its logits: they are told to be unused)
+            once, = torch.autograd.grad(f().sum(), t, create_graph=True)
+            with pytest.raises(RuntimeError, match="differentiate twice"):
+                torch.autograd.grad(once.pow(2).sum() + t.sum(), t)
+
+
+def test_a_graph_can_be_gone_through_again():
+    from paper_2607_26005_amd import memory
+    g, x, s, r = _inputs(2, 600, 4, torch.float32, resets=0.01)
+    x.requires_grad_()
+    out, _ = memory.gated_scan(g, x, s, r)
+    a, = torch.autograd.grad(out.sum(), x, retain_graph=True)
+    b, = torch.autograd.grad(out.sum(), x)
+    assert torch.equal(a, b)
+    with torch.no_grad():
+        x.add_(1)
+    out, _ = memory.gated_scan(g, x, s, r)
+    with torch.no_grad():
+        x.add_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        out.sum().backward()
+
+
+def test_a_capture_refuses_leaves_that_an_eager_graph_holds():
+    from paper_2607_26005_amd import memory, pictura
+    x, w = torch.randn(6, 16, device="cuda"), torch.ones(16, device="cuda", requires_grad=True)
+    held = w * 1   # an eager graph of the leaf, on the default stream
+    memory.rms_norm(x, w)
+    graph = torch.cuda.CUDAGraph()
+    with pytest.raises(pictura.PicturaError, match="weight: a graph recorded on another stream"):
+        with torch.cuda.graph(graph):
+            memory.rms_norm(x, w)
+    del held
+    torch.cuda.synchronize()
+    # without one the backward is captured
+    graph = torch.cuda.CUDAGraph()
+    dy = torch.randn_like(x)
+    with torch.cuda.graph(graph):
+        dw, = torch.autograd.grad(memory.rms_norm(x, w), w, dy)
+    for _ in range(3):
+        x.copy_(torch.randn_like(x))
+        dw.zero_()
+        graph.replay()
+        want, = torch.autograd.grad(memory.rms_norm(x, w), w, dy)
+        assert torch.equal(dw, want)

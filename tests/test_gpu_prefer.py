@@ -280,3 +280,11 @@ def test_rows_beyond_32_bits():
         got, want = policy.preference_gradient(view, a, o, r), policy.preference_gradient(l, a, o, r)
         assert all(map(torch.equal, got, want))
         del base, view
+
+
+@pytest.mark.parametrize("A, dtype", [(3, torch.float32), (12, torch.bfloat16), (50, torch.float16), (100, torch.float32)])
+def test_long_sequences(A, dtype):
+    l, a, o, r, m = _inputs([9000, 3000], A, dtype, mask=0.7, unused=0.1, outside=50)
+    got = _check(l, a, o, r, mask=m, beta=0.02)
+    assert (got.dlogits[:50] == 0).all() and (got.dlogits[-50:] == 0).all()
+    _check(l, a, o, r, mask=m, average=True, weights=torch.tensor([2.0]).cuda(), denominator=3.0)

@@ -66,6 +66,13 @@ def test_step_refuses(match, bad):
     _raises(match, memory.gated_step, **dict(dict(gates=z(B, C), inputs=z(B, C), state=z(B, C)), **bad))
 
 
+def test_a_step_refuses_to_lose_a_gradient():
+    for name in ("gates", "inputs", "state"):
+        a = dict(gates=z(B, C), inputs=z(B, C), state=z(B, C))
+        a[name].requires_grad_()
+        _raises("no gradient", memory.gated_step, **a)
+
+
 def test_outputs_of_the_scan_are_checked():
     ok = lambda: dict(gates=z(B, T, C), inputs=z(B, T, C), out=z(B, T, C), last_state=z(B, C))
     _raises("out: shape", pictura.pictura_gated_scan, **dict(ok(), out=z(B, T, C + 1)))

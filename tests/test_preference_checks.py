@@ -53,6 +53,7 @@ def _args(**over):
     ("smoothing", dict(smoothing=-0.1)),
     ("denominator", dict(denominator=-1.0)),
     ("denominator", dict(denominator=1e39)),
+    ("denominator", dict(denominator=1e-60)),
 ])
 def test_preferences_refuse(match, bad):
     _raises(match, policy.preference_gradient, **_args(**bad))
