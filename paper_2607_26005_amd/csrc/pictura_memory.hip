@@ -56,15 +56,25 @@ struct Sequences {
 };
 
 // The smaller one of a = sigmoid(g) and 1 - a, with g's sign: the other one is 1 - |m| to half
-// a unit.  e = exp(-|g|) with the product by log2(e) in two terms; at 128 and beyond it is 0
-// in fp32.  e is off by up to 3.5 u (u = 2^-24), the reciprocal by 4.5 u, m by 8.5 u.
+// a unit.  For fp32, e = exp(-|g|) takes the product by log2(e) in two terms (at 128 and
+// beyond it is 0): e is off by up to 3.5 u (u = 2^-24), the reciprocal by 4.5 u, m by 8.5 u.
+// 16-bit gates take the product in one, off by 1.3 |g| u more: where |g| is large m is small,
+// so that a and 1 - a stay within half a unit of 1, and their inputs are rounded to 2^-9 or
+// 2^-12 of themselves.  Tiles of bf16 are bound by the vector unit: forward over one of 65,536
+// steps of 1,024 channels takes 121 us with two terms.
+template <class T>
 __device__ __forceinline__ float gate_of(float g)
 {
     constexpr float kHi = 1.44269502f, kLo = 1.92596299e-8f, kLn2 = 0.693147182f;
-    const float z = fabsf(g) > 128.0f ? 128.0f : fabsf(g);   // (a NaN stays one)
-    const float hi = z * -kHi, lo = fmaf(z, -kLo, fmaf(z, -kHi, -hi));
-    float e = __builtin_amdgcn_exp2f(hi);
-    e = fmaf(e * lo, kLn2, e);
+    float e;
+    if constexpr (sizeof(T) == 2) {
+        e = __builtin_amdgcn_exp2f(fabsf(g) * -kHi);
+    } else {
+        const float z = fabsf(g) > 128.0f ? 128.0f : fabsf(g);   // (a NaN stays one)
+        const float hi = z * -kHi, lo = fmaf(z, -kLo, fmaf(z, -kHi, -hi));
+        e = __builtin_amdgcn_exp2f(hi);
+        e = fmaf(e * lo, kLn2, e);
+    }
     return copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), g);
 }
 
@@ -247,7 +257,8 @@ static __global__ __launch_bounds__(256) void chain_kernel(const Chain c)
 template <int V>
 struct TileLds {
     Maps<V> waves[tile_waves(V)][64];   // of this tile
-    Maps<V> before[kGroup][64];      // of the tiles before it in its group; the last row: the state before those
+    Maps<V> before[kGroup][64];         // of the tiles before it in its group
+    float start[64][V];                 // the state before the group
     uint32_t ticket;
 };
 
@@ -268,6 +279,7 @@ template <int V>
 __device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, int64_t threads, int64_t thread, bool on, int32_t k,
                                              int w, const Maps<V>& f, const float (&first)[V], float (&h)[V])
 {
+    constexpr int W = tile_waves(V);
     const int lane = threadIdx.x & 63;
     const int32_t g = k / kGroup, r = k % kGroup;
     lds.waves[w][lane] = f;
@@ -285,11 +297,11 @@ __device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, in
             for (int v = 0; v < V; ++v) tell(c.tiles + ((int64_t)k * threads + thread) * V + v, all.v[v]);
         }
     }
-    // each wave waits for some of the tiles before, the last one for the group before as well
+    // each wave waits for some of the tiles before
     Maps<V> m;
-    Word x[kItems<V>][V];
     const int mine = min(kItems<V>, r - w * kItems<V>);
     if (mine > 0) {
+        Word x[kItems<V>][V];
         await<V>(c.tiles + ((int64_t)(g * kGroup + w * kItems<V>) * threads + thread) * V, threads * V, mine, on, x);
 #pragma unroll
         for (int i = 0; i < kItems<V>; ++i)
@@ -299,16 +311,33 @@ __device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, in
                 lds.before[w * kItems<V> + i][lane] = m;
             }
     }
-    if (w == tile_waves(V) - 1) {
+    __syncthreads();
+    // The last wave waits for the state before the group.  In a group's last tile it has joined
+    // all of the group by then: from one group to the next there is one wait and one product.
+    if (w == W - 1) {
+        const bool ends = r == kGroup - 1 && k < c.count - 1;
+        if (ends) {
+            m = lds.before[0][lane];
+#pragma unroll 4
+            for (int i = 1; i < kGroup - 1 + W; ++i) {
+                const Maps<V> n = i < kGroup - 1 ? lds.before[i][lane] : lds.waves[i - (kGroup - 1)][lane];
+#pragma unroll
+                for (int v = 0; v < V; ++v) m.v[v] = then(m.v[v], n.v[v]);
+            }
+        }
+        float start[V];
+        Word x[kItems<V>][V];
         if (g > 0) await<V>(c.groups + ((int64_t)(g - 1) * threads + thread) * V, 0, 1, on, x);
 #pragma unroll
-        for (int v = 0; v < V; ++v) m.v[v].H = g > 0 ? __uint_as_float((uint32_t)(x[0][v] >> 32)) : first[v];
-        lds.before[kGroup - 1][lane] = m;
+        for (int v = 0; v < V; ++v) {
+            start[v] = g > 0 ? __uint_as_float((uint32_t)(x[0][v] >> 32)) : first[v];
+            if (ends && on) tell(c.groups + ((int64_t)g * threads + thread) * V + v, 0u, apply(m.v[v], start[v]));
+            lds.start[lane][v] = start[v];
+        }
     }
     __syncthreads();
-    m = lds.before[kGroup - 1][lane];
 #pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = m.v[v].H;
+    for (int v = 0; v < V; ++v) h[v] = lds.start[lane][v];
 #pragma unroll 4
     for (int i = 0; i < r; ++i) {
         m = lds.before[i][lane];
@@ -320,10 +349,6 @@ __device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, in
         m = lds.waves[i][lane];
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = apply(m.v[v], h[v]);
-    }
-    if (w == tile_waves(V) - 1 && r == kGroup - 1 && k < c.count - 1 && on) {   // the state after the group
-#pragma unroll
-        for (int v = 0; v < V; ++v) tell(c.groups + ((int64_t)g * threads + thread) * V + v, 0u, apply(f.v[v], h[v]));
     }
 }
 
@@ -360,7 +385,7 @@ __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_kernel(const Seque
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 float b;
-                gate_parts(gate_of((float)gs[i].v[v]), a[i][v], b);
+                gate_parts(gate_of<T>((float)gs[i].v[v]), a[i][v], b);
                 add[i][v] = b * (float)xs[i].v[v];
                 const bool reset = kResets && (resets >> i & 1u);
                 Map& m = f.v[v];
@@ -444,7 +469,7 @@ __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_gradient_kernel(co
             for (int v = 0; v < V; ++v) {
                 const float x = (float)xs[i].v[v];
                 float a, b;
-                m[i][v] = gate_of((float)gs[i].v[v]);
+                m[i][v] = gate_of<T>((float)gs[i].v[v]);
                 gate_parts(m[i][v], a, b);
                 if (kResets && (resets >> i & 1u)) h[v] = 0.0f;
                 d[i][v] = h[v] - x;
@@ -531,7 +556,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const Sequences<T> q, const T
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 float a, b;
-                gate_parts(gate_of((float)gs[i].v[v]), a, b);
+                gate_parts(gate_of<T>((float)gs[i].v[v]), a, b);
                 const float add = b * (float)xs[i].v[v];
                 h[v] = kResets && (resets >> i & 1u) ? add : fmaf(a, h[v], add);
                 o.v[v] = (T)h[v];
@@ -582,7 +607,7 @@ __global__ __launch_bounds__(256, 4) void scan_gradient_kernel(const Sequences<T
             for (int v = 0; v < V; ++v) {
                 const float xi = (float)xs[i].v[v];
                 float a, b;
-                m[i][v] = gate_of((float)gs[i].v[v]);
+                m[i][v] = gate_of<T>((float)gs[i].v[v]);
                 gate_parts(m[i][v], a, b);
                 if (kResets && (resets >> i & 1u)) h[v] = 0.0f;
                 d[i][v] = h[v] - xi;
@@ -640,7 +665,7 @@ __global__ __launch_bounds__(256) void step_kernel(const Sequences<T> q, T* __re
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         float a, b;
-        gate_parts(gate_of((float)g.v[v]), a, b);
+        gate_parts(gate_of<T>((float)g.v[v]), a, b);
         const float add = b * (float)x.v[v];
         h.v[v] = reset ? add : fmaf(a, h.v[v], add);
         o.v[v] = (T)h.v[v];

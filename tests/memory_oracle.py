@@ -3,14 +3,23 @@ the error that fp32 arithmetic may leave.
 
 The bounds are running ones, u = 2^-24: a rounded operation adds u of its result, the
 gate's two parts come to within 10 u of their own (a hardware exponential off by up to a
-unit, 2 u; two roundings of its correction; 1 + e, the refined reciprocal, their product
-and the difference from 1, with the exponential's error passed on), and errors travel
-through the recurrence with the factors of the values.  Magnitudes stand for values, so
-that the bounds hold for any split of the steps."""
+unit, 2 u; two roundings of its correction; 1 + e, the reciprocal off by a unit, their
+product and the difference from 1, with the exponential's error passed on), and errors
+travel through the recurrence with the factors of the values.  Magnitudes stand for
+values, so that the bounds hold for any split of the steps.
+
+Gates of 16 bits: the product |g| log2 e is rounded once, by u of itself, and the constant
+by 0.23 u, which in exp(-|g|) is a relative 1.23 |g| u, and no more than that in either part
+(the larger one, 1 - m, has it times m / (1 - m) <= 1)."""
 import torch
 
 U = 2.0 ** -24
 GATE = 10
+
+
+def _gate(g, dtype):
+    """Units that a gate's parts may be off by."""
+    return GATE if dtype == torch.float32 else GATE + 1.23 * g.abs()
 
 
 def half_step(t, dtype):
@@ -31,7 +40,8 @@ def scan(gates, inputs, state=None, resets=None):
         if resets is not None:
             began = resets.cpu().bool()[:, t, None]
             h, A, e = (torch.where(began, torch.zeros_like(v), v) for v in (h, A, e))
-        e = a * e + U * ((GATE + 4) * a * A + (GATE + 4) * b * x[:, t].abs())
+        off = _gate(g[:, t], gates.dtype)
+        e = a * e + U * ((off + 4) * a * A + (off + 4) * b * x[:, t].abs())
         h, A = a * h + b * x[:, t], a * A + b * x[:, t].abs()
         e = e + U * A
         out[:, t], bound[:, t], mags[:, t] = h, e, A
@@ -58,10 +68,11 @@ def scan_gradient(gates, inputs, state, resets, dout, dlast):
             began = resets.cpu().bool()[:, t, None]
             before, bm, eb = (torch.where(began, zero, v) for v in (before, bm, eb))
         d, dm = before - x[:, t], bm + x[:, t].abs()
-        dx[:, t], bx[:, t] = b * G, b * eG + (GATE + 2) * U * b * Gm
+        off = _gate(g[:, t], gates.dtype)
+        dx[:, t], bx[:, t] = b * G, b * eG + (off + 2) * U * b * Gm
         dg[:, t] = a * b * G * d
-        bg[:, t] = a * b * (dm * eG + Gm * (eb + U * dm) + (2 * GATE + 4) * U * Gm * dm)
-        c, cm, ec = a * G, a * Gm, a * eG + (GATE + 4) * U * a * Gm
+        bg[:, t] = a * b * (dm * eG + Gm * (eb + U * dm) + (2 * off + 4) * U * Gm * dm)
+        c, cm, ec = a * G, a * Gm, a * eG + (off + 4) * U * a * Gm
         if resets is not None:
             c, cm, ec = (torch.where(began, zero, v) for v in (c, cm, ec))
     return (dg, dx, c), (bg, bx, ec)
