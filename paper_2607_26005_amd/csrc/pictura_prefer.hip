@@ -407,15 +407,25 @@ struct Piece {
     __device__ __forceinline__ float operator()(const uint8_t* mask, int v) const { return mask && !m[v] ? -INFINITY : (float)t[v]; }
 };
 
-// Largest logit and sum of exponentials of every row, by teams of NW waves, a row read once
-// in vectors of 16 bytes at any address; the last one begins earlier where a row's length
-// is no multiple of them, and its first elements are skipped.
-template <class T, int NW>
-__global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void row_kernel(const Rows R, const Pairs q, const Scratch k)
+// The L lanes that work on a row: 16 (four rows a wave), a wave, or a workgroup of waves.
+template <int L>
+struct Team {
+    static constexpr int kThreads = L < 256 ? 256 : L, kTeams = kThreads / L, kWaves = L < 64 ? 1 : L / 64;
+    static constexpr int kInWave = L < 64 ? L : 64;
+    __device__ __forceinline__ static int member() { return threadIdx.x % L; }
+    __device__ __forceinline__ static int team() { return threadIdx.x / L; }
+};
+
+// Largest logit and sum of exponentials of every row, read once in vectors of 16 bytes at
+// any address; the last one begins earlier where a row's length is no multiple of them, and
+// its first elements are skipped.
+template <class T, int L>
+__global__ __launch_bounds__(Team<L>::kThreads) void row_kernel(const Rows R, const Pairs q, const Scratch k)
 {
-    constexpr int V = 16 / sizeof(T), kAhead = 4, kLanes = NW * 64, kTeams = NW == 1 ? 4 : 1;
+    using Tm = Team<L>;
+    constexpr int V = 16 / sizeof(T), kAhead = 4, kTeams = Tm::kTeams, NW = Tm::kWaves;
     __shared__ float maxima[NW], sums[NW];
-    const int member = NW == 1 ? threadIdx.x & 63 : threadIdx.x, team = NW == 1 ? threadIdx.x >> 6 : 0;
+    const int member = Tm::member(), team = Tm::team();
     const int A = R.actions;
     const int64_t from = bound_of(q, 0, R.rows), to = bound_of(q, 2 * q.count, R.rows);
     for (int64_t n = (int64_t)blockIdx.x * kTeams + team; n < R.rows; n += (int64_t)gridDim.x * kTeams) {
@@ -436,14 +446,14 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void row_kernel(const Rows
             Piece<T, V> x[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int at = i + u * kLanes * V;
+                const int at = i + u * L * V;
                 if (kWhole || at < A) x[u].load(data, mask, kWhole || at + V <= A ? at : A - V);
             }
             float largest = -INFINITY;
             float y[kAhead][V];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int at = i + u * kLanes * V, skip = at + V <= A ? 0 : at + V - A;
+                const int at = i + u * L * V, skip = at + V <= A ? 0 : at + V - A;
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     y[u][v] = kWhole || (at < A && v >= skip) ? x[u](mask, v) : -INFINITY;
@@ -462,11 +472,11 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void row_kernel(const Rows
                 for (int v = 0; v < V; ++v) some += weight_of<T>(y[u][v], base);
             sum += some;
         };
-        constexpr int kChunk = kLanes * V * kAhead;
+        constexpr int kChunk = L * V * kAhead;
         int i = member * V;
         for (; i - member * V + kChunk <= A; i += kChunk) add(i, Int<true>{});
         if (i < A) add(i, Int<false>{});
-        float all = group_max<64>(top);
+        float all = group_max<Tm::kInWave>(top);
         if constexpr (NW > 1) {
             __syncthreads();
             if ((threadIdx.x & 63) == 0) maxima[threadIdx.x >> 6] = all;
@@ -475,7 +485,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void row_kernel(const Rows
         }
         const float base = all == -INFINITY ? 0.0f : all;
         if (top != all) sum *= weight_of<T>(top, base);
-        sum = group_sum<64>(sum);
+        sum = group_sum<Tm::kInWave>(sum);
         if constexpr (NW > 1) {
             if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
             __syncthreads();
@@ -525,12 +535,13 @@ static __global__ __launch_bounds__(kPairThreads) void terms_kernel(const Pairs 
 
 // c (delta - p) of every row, by teams as in row_kernel; the first workgroup writes the
 // statistics too.
-template <class T, int NW>
-__global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void gradient_kernel(const Rows R, const Pairs q, const Scratch k)
+template <class T, int L>
+__global__ __launch_bounds__(Team<L>::kThreads) void gradient_kernel(const Rows R, const Pairs q, const Scratch k)
 {
-    constexpr int V = 16 / sizeof(T), kLanes = NW * 64, kTeams = NW == 1 ? 4 : 1, NT = NW == 1 ? 256 : NW * 64;
-    if (blockIdx.x == 0) write_stats<NT>(q, k);
-    const int member = NW == 1 ? threadIdx.x & 63 : threadIdx.x, team = NW == 1 ? threadIdx.x >> 6 : 0;
+    using Tm = Team<L>;
+    constexpr int V = 16 / sizeof(T), kTeams = Tm::kTeams;
+    if (blockIdx.x == 0) write_stats<Tm::kThreads>(q, k);
+    const int member = Tm::member(), team = Tm::team();
     const int A = R.actions;
     for (int64_t n = (int64_t)blockIdx.x * kTeams + team; n < R.rows; n += (int64_t)gridDim.x * kTeams) {
         const T* data = (const T*)R.data + n * R.stride;
@@ -545,7 +556,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void gradient_kernel(const
             action = (int)q.actions[n];
             if ((mask && !mask[action]) || (float)data[action] == -INFINITY) action = -1;
         }
-        for (int i = member * V; i < A; i += kLanes * V) {
+        for (int i = member * V; i < A; i += L * V) {
             const int at = i + V <= A ? i : A - V;
             Piece<T, V> x;
             T y[V];
@@ -562,9 +573,10 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void gradient_kernel(const
 // ---------------------------------------------------------------------------
 
 constexpr int kSmallHead = 64;
-// Rows of a pair, on average, from which on its sequences are spread over workgroups: one
-// alone walks through 4,096 rows of 12 in some 50 us.
-constexpr int64_t kLongPair = 4096;
+// Rows of a pair, on average, from which on its sequences are spread over workgroups: two
+// pairs of 4,096 rows of 12 take 43 us by a workgroup each and 20 spread, four of 2,000 rows
+// 24 by a workgroup each.
+constexpr int64_t kLongPair = 1024;
 
 bool by_pairs(int64_t rows, int32_t actions, int64_t pairs) { return actions <= kSmallHead && rows <= kLongPair * pairs; }
 
@@ -593,7 +605,10 @@ void launch(const Rows& R, const Pairs& q, const Scratch& k, hipStream_t st)
     if (q.weights && q.denominator == 0.0f && q.count > kFewPairs)
         hipLaunchKernelGGL(weight_sum_kernel, dim3(1), dim3(1024), 0, st, q, k);
     auto with_rows = [&](auto go) {   // lanes of a row, elements of a lane
-        if (R.actions <= 16) go(Int<1>{}, Int<16>{});
+        if (R.actions <= 4) go(Int<1>{}, Int<4>{});
+        else if (R.actions <= 8) go(Int<1>{}, Int<8>{});
+        else if (R.actions <= 12) go(Int<1>{}, Int<12>{});
+        else if (R.actions <= 16) go(Int<1>{}, Int<16>{});
         else go(Int<8>{}, Int<8>{});
     };
     auto terms = [&] {
@@ -621,17 +636,19 @@ void launch(const Rows& R, const Pairs& q, const Scratch& k, hipStream_t st)
     }
     constexpr int V = 16 / sizeof(T);
     const int64_t vectors = (R.actions + V - 1) / V;
-    auto go = [&](auto waves) {
-        constexpr int NW = decltype(waves)::value, kTeams = NW == 1 ? 4 : 1, NT = NW == 1 ? 256 : NW * 64;
-        const int64_t all = (R.rows + kTeams - 1) / kTeams, most = 1 << 20;
-        const dim3 grid((unsigned)(all < 1 ? 1 : all < most ? all : most));
-        hipLaunchKernelGGL((row_kernel<T, NW>), grid, dim3(NT), 0, st, R, q, k);
+    auto go = [&](auto lanes) {
+        using Tm = Team<decltype(lanes)::value>;
+        constexpr int L = decltype(lanes)::value;
+        const int64_t all = (R.rows + Tm::kTeams - 1) / Tm::kTeams, most = 1 << 20;
+        const dim3 grid((unsigned)(all < 1 ? 1 : all < most ? all : most)), block(Tm::kThreads);
+        hipLaunchKernelGGL((row_kernel<T, L>), grid, block, 0, st, R, q, k);
         terms();
-        hipLaunchKernelGGL((gradient_kernel<T, NW>), grid, dim3(NT), 0, st, R, q, k);
+        hipLaunchKernelGGL((gradient_kernel<T, L>), grid, block, 0, st, R, q, k);
     };
-    if (vectors <= 256) go(Int<1>{});
-    else if (vectors <= 4096) go(Int<4>{});
-    else go(Int<16>{});
+    if (vectors <= 96) go(Int<16>{});
+    else if (vectors <= 512) go(Int<64>{});
+    else if (vectors <= 4096) go(Int<256>{});
+    else go(Int<1024>{});
 }
 
 constexpr int64_t kMostPairs = 1 << 23;   // (a launch has fewer than 2^32 threads)
