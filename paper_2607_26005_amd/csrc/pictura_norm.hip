@@ -419,21 +419,35 @@ struct Int {
 };
 
 // go(V, NV, Team): the lanes and registers of a row.  Rows shorter than a vector take
-// single elements.
-template <class T, class F>
+// single elements.  Two vectors a lane, so that a wave has more rows or bytes under way,
+// are as good as one or better up to a wave's width (131,072 rows of 300 in bf16: forward 68
+// us and 74, gradient 73 and 81; 262,144 of 512: 192 and 196, 199 and 208), except where codes
+// come out and most lanes have a vector (65,536 of 512 to e4m3 and back: 82.7 and 80.4).
+// Wider rows of 16 bits take one a lane and more waves, whose registers then hold all of
+// a row in fp32 (32,768 rows of 2,048 by one wave or four: forward 111 and 98 us, codes 109 and
+// 97, gradient 128 and 109); fp32 rows four (32,768 of 1,024: 94 and 99, 81 and 83, 105 and 120).
+template <class T, bool kCodes, class F>
 void with_team(int32_t width, F go)
 {
     constexpr int V = 16 / sizeof(T);
     const int vectors = (width + V - 1) / V;
     if (width < V) return go(Int<1>{}, Int<1>{}, Team<8, 1>{});
     if (vectors <= 8) return go(Int<V>{}, Int<1>{}, Team<8, 1>{});
-    if (vectors <= 16) return go(Int<V>{}, Int<1>{}, Team<16, 1>{});
-    if (vectors <= 32) return go(Int<V>{}, Int<1>{}, Team<32, 1>{});
-    if (vectors <= 64) return go(Int<V>{}, Int<1>{}, Team<64, 1>{});
+    if (vectors <= 16) return go(Int<V>{}, Int<2>{}, Team<8, 1>{});
+    if (vectors <= 32) return go(Int<V>{}, Int<2>{}, Team<16, 1>{});
+    if constexpr (kCodes)
+        if (vectors > 48 && vectors <= 64) return go(Int<V>{}, Int<1>{}, Team<64, 1>{});
+    if (vectors <= 64) return go(Int<V>{}, Int<2>{}, Team<32, 1>{});
     if (vectors <= 128) return go(Int<V>{}, Int<2>{}, Team<64, 1>{});
-    if (vectors <= 256) return go(Int<V>{}, Int<4>{}, Team<64, 1>{});
-    if (vectors <= 512) return go(Int<V>{}, Int<2>{}, Team<64, 4>{});
-    if (vectors <= 1024) return go(Int<V>{}, Int<4>{}, Team<64, 4>{});
+    if constexpr (V == 8) {
+        if (vectors <= 256) return go(Int<V>{}, Int<1>{}, Team<64, 4>{});
+        if (vectors <= 512) return go(Int<V>{}, Int<1>{}, Team<64, 8>{});
+        if (vectors <= 1024) return go(Int<V>{}, Int<1>{}, Team<64, 16>{});
+    } else {
+        if (vectors <= 256) return go(Int<V>{}, Int<4>{}, Team<64, 1>{});
+        if (vectors <= 512) return go(Int<V>{}, Int<2>{}, Team<64, 4>{});
+        if (vectors <= 1024) return go(Int<V>{}, Int<4>{}, Team<64, 4>{});
+    }
     if (vectors <= 2048) return go(Int<V>{}, Int<2>{}, Team<64, 16>{});
     if (vectors <= 4096) return go(Int<V>{}, Int<4>{}, Team<64, 16>{});
     if constexpr (V == 8) return go(Int<V>{}, Int<8>{}, Team<64, 16>{});
@@ -476,7 +490,7 @@ void launch_norm(const pictura_norm& n, void* sum, int64_t sum_stride, void* out
     with_types(n, [&](auto t, auto w) {
         using T = decltype(t);
         using W = decltype(w);
-        with_team<T>(n.width, [&](auto v, auto nv, auto team) {
+        with_team<T, kCodes>(n.width, [&](auto v, auto nv, auto team) {
             using Tm = decltype(team);
             hipLaunchKernelGGL((norm_kernel<T, W, decltype(v)::value, decltype(nv)::value, Tm, kCodes>),
                                dim3(blocks_for<Tm>(n.rows)), dim3(Tm::kThreads), 0, st, rows_of<T>(n),
@@ -485,13 +499,13 @@ void launch_norm(const pictura_norm& n, void* sum, int64_t sum_stride, void* out
     });
 }
 
-// Workgroups of the gradient, and the parts of dweight that they leave.
-constexpr int64_t kBlocks = 1024;
+// Waves of the gradient, whose workgroups leave a part of dweight each.
+constexpr int64_t kWaves = 4096;
 
 template <class Tm>
 int64_t gradient_blocks(int64_t rows)
 {
-    const int64_t b = (rows + Tm::kRows - 1) / Tm::kRows, most = Tm::NW == 1 ? kBlocks : Tm::NW == 4 ? kBlocks / 2 : kBlocks / 4;
+    const int64_t b = (rows + Tm::kRows - 1) / Tm::kRows, most = Tm::NW == 1 ? kWaves / 4 : kWaves / Tm::NW;
     return b < most ? b : most;
 }
 
@@ -502,8 +516,8 @@ int64_t gradient_parts(const pictura_norm& n)
         using Tm = decltype(team);
         parts = gradient_blocks<Tm>(n.rows);
     };
-    if (n.dtype == PICTURA_F32) with_team<float>(n.width, count);
-    else with_team<_Float16>(n.width, count);
+    if (n.dtype == PICTURA_F32) with_team<float, false>(n.width, count);
+    else with_team<_Float16, false>(n.width, count);
     return parts;
 }
 
@@ -598,7 +612,7 @@ pictura_status pictura_rms_norm_gradient(const pictura_norm* n, const float* fac
         using T = decltype(t);
         using W = decltype(w);
         if (n->rows > 0)
-            with_team<T>(n->width, [&](auto v, auto nv, auto team) {
+            with_team<T, false>(n->width, [&](auto v, auto nv, auto team) {
                 using Tm = decltype(team);
                 const Gradient<T> g{(const T*)n->x, (const T*)dout, (const T*)dsum, factors, n->weight, (T*)dx, (float*)workspace,
                                     n->x_stride, dout_stride, dsum_stride, dx_stride, n->rows, n->width};
