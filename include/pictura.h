@@ -650,13 +650,13 @@ pictura_status pictura_gated_scan_workspace(const pictura_sequences* sequences, 
 
 /* Gated linear recurrence over whole sequences: with a = sigmoid(gates),
  *   h_t = a_t h_(t-1) + (1 - a_t) inputs_t,
- * h_(t-1) = 0 where step t is reset, in fp32 (a and 1 - a each to a few units of their
- * own).  out (same type, strides of its own, no two elements at one place) receives h_t;
+ * h_(t-1) = 0 where step t is reset, in fp32 (a and 1 - a each to 10 units of 2^-24 of their
+ * own, with gates of 16 bits to 10 + 1.3 |gate|).  out (same type, strides of its own, no two elements at one place) receives h_t;
  * last_state (or NULL) fp32 [batch][channels] the state after the last step; saved (or
  * NULL), fp32 [ceil(steps / PICTURA_SCAN_STEPS)][batch][channels], what the gradient
- * needs: the states before steps 0, 16, 32, ...  Results do not depend on what else runs;
- * where few channels stand against many steps the steps are cut into segments, whose
- * sums are taken in one order.  last_state must not overlap state, nor out the inputs.
+ * needs: the states before steps 0, 16, 32, ...  The same call gives the same bits; where few
+ * channels stand against many steps the steps are cut into tiles, which rounds states in
+ * another order.  last_state must not overlap state, nor out the inputs.
  * workspace: device memory, 256-byte aligned, in use until the call's work on the stream
  * is done.  EINVAL: a null or misaligned pointer, sizes or strides out of range, or a
  * workspace too small. */

@@ -11,10 +11,17 @@
 // (0.25 byte an element instead of 4).
 //
 // A thread walks through the steps of one or two channels, 16 steps' loads under way at
-// once.  Where there are too few channels for the card, the steps are cut into segments:
-// what a segment does to a state is h -> P h + H, with P the product of its a.  One
-// launch computes P and H of every segment and of groups of 16, in the next every
-// segment begins by folding those before it, in their order, so results repeat to the bit.
+// once.  Where there are too few channels for the card, the steps are cut into tiles, a
+// workgroup each: what a tile's steps do to a state is h -> P h + H, with P the product of
+// their a, which every workgroup tells those behind it; it keeps a and (1 - a) x in registers
+// until it knows the state before its own.  Everything is read and written once, and joined in
+// one order, so that results repeat to the bit.
+//
+// Measured (one MI355X, large copies at 5,150 GB/s): 2,048 x 128 steps of 512 channels in bf16
+// forward 182 us, gradient 296 (838 and 1,376 MB with the saved states: 4.6 TB/s each); one
+// of 65,521 steps of 1,024 forward 111 us, gradient 158 (419 and 688 MB: 3.8 and 4.4 TB/s), of
+// which a launch that sums the segments up first and one that reads them again took 152 and 221;
+// single steps of 65,536 x 512 in bf16 68 us (470 MB: 6.9 TB/s, some of it from the caches).
 #include <cmath>
 
 #include "pictura.h"
@@ -284,10 +291,10 @@ __device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, in
     const int32_t g = k / kGroup, r = k % kGroup;
     lds.waves[w][lane] = f;
     __syncthreads();
-    if (w == tile_waves(V) - 1 && r < kGroup - 1 && k < c.count - 1) {   // what the whole tile does
+    if (w == W - 1 && r < kGroup - 1 && k < c.count - 1) {   // what the whole tile does
         Maps<V> all = lds.waves[0][lane];
 #pragma unroll 2
-        for (int i = 1; i < tile_waves(V); ++i) {
+        for (int i = 1; i < W; ++i) {
             const Maps<V> m = lds.waves[i][lane];
 #pragma unroll
             for (int v = 0; v < V; ++v) all.v[v] = then(all.v[v], m.v[v]);
@@ -352,8 +359,9 @@ __device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, in
     }
 }
 
-// Forwards over one tile: a and (1 - a) x of a wave's 16 steps stay in registers while it
-// waits for the state before them, so that everything is read once.
+// Forwards over one tile.  Of bf16 it takes 1,090 vector instructions a wave, 64 % of the time
+// it has; workgroups that take several tiles, and the next ticket ahead, are slower (169 us and
+// 121), as tickets wait for workgroups that are not ready.
 template <class T, int V, bool kResets>
 __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_kernel(const Sequences<T> q, const Tensor<T> out, float* __restrict__ last,
                                                                   float* __restrict__ saved, const Chain chain)
@@ -682,10 +690,16 @@ bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) 
 
 size_t size_of(int32_t t) { return t == PICTURA_F32 ? 4 : 2; }
 
-// Waves from which on every thread walks through all steps.  Walking against tiles, us (bf16,
-// 64 M elements, 512 steps): 512 waves forward 139 and 97, gradient 372 and 151; 1,024 waves 82
-// and 103, 219 and 161; 1,600 waves (105 M) 136 and 141, 265 and 226.
-constexpr int64_t kManyWaves = 1024, kManyBack = 2048;
+// Waves from which on every thread walks through all steps.  Walking against tiles, us (512
+// steps):
+//     bf16      512 waves forward 139 and 97, gradient 372 and 151 (64 M elements)
+//             1,024 waves 82 and 102, 151 and 157 (of 2,048 steps 329 and 357, 604 and 549)
+//             1,600 waves 136 and 141, 265 and 226
+//     fp32      512 waves 42 and 41, 83 and 75
+//             1,024 waves 80 and 86, 130 and 132 (of 2,048 steps 316 and 324, 522 and 499)
+//             4,096 waves 309 and 299, 514 and 467
+constexpr int64_t kManyWaves = 1024;
+constexpr int64_t many_back(int vec) { return vec == 2 ? 2048 : 8192; }
 
 // Channels of a thread, and the tiles that the steps are cut into (0: not cut).
 struct Shape {
@@ -698,7 +712,7 @@ Shape shape_of(const pictura_sequences& q, int32_t vec, bool back)
     Shape s{vec, 0, q.batch * (q.channels / vec)};
     const int64_t waves = (s.threads + 63) / 64, tile = tile_steps(vec), tiles = (q.steps + tile - 1) / tile;
     // (a launch has fewer than 2^32 threads)
-    if (waves < (back ? kManyBack : kManyWaves) && q.steps >= 2 * tile && waves * tiles <= 1 << 21) s.tiles = (int32_t)tiles;
+    if (waves < (back ? many_back(vec) : kManyWaves) && q.steps >= 2 * tile && waves * tiles <= 1 << 21) s.tiles = (int32_t)tiles;
     return s;
 }
 
