@@ -34,16 +34,22 @@ namespace {
 
 constexpr int kSteps = PICTURA_SCAN_STEPS;   // steps between saved states, and in registers at once
 
+// Neighbouring channels, loaded and stored as one at any address.
 template <class T, int V>
-struct alignas(V * sizeof(T)) Vec {
+struct Vec {
     T v[V];
 };
 
 template <class T, int V>
-__device__ __forceinline__ Vec<T, V> load(const T* p) { return *reinterpret_cast<const Vec<T, V>*>(p); }
+__device__ __forceinline__ Vec<T, V> load(const T* p)
+{
+    Vec<T, V> x;
+    __builtin_memcpy(&x, p, sizeof(x));
+    return x;
+}
 
 template <class T, int V>
-__device__ __forceinline__ void store(T* p, const Vec<T, V>& x) { *reinterpret_cast<Vec<T, V>*>(p) = x; }
+__device__ __forceinline__ void store(T* p, const Vec<T, V>& x) { __builtin_memcpy(p, &x, sizeof(x)); }
 
 // Element (b, t, c) of a sequence's tensor is at data[b * batch + t * step + c].
 template <class T>
@@ -58,7 +64,8 @@ struct Sequences {
     const float* state;                 // [batch][channels]
     Tensor<const uint8_t> resets;       // one channel
     int64_t threads, steps;             // vectors of channels in all, steps
-    int32_t vectors;                    // vectors of a sequence's channels
+    int64_t states;                     // channels in all
+    int32_t channels, vectors;          // of a sequence, and the vectors that cover them
     bool one;                           // a wave's are of one sequence
 };
 
@@ -125,20 +132,25 @@ __device__ __forceinline__ void hold(Vec<T, V>& x)
     }
 }
 
-// Where a thread's channels begin in the tensors.
+// Where a thread's channels begin in the tensors, and among all channels.  Where a sequence's
+// channels are no multiple of V the last vector begins earlier, and two threads compute
+// and write the same for what both hold.
 template <class T, int V>
 struct Place {
-    int64_t b;
+    int64_t b, flat;
     int32_t c;
-    __device__ __forceinline__ Place(int64_t thread, int32_t vectors)
+    __device__ __forceinline__ Place(int64_t thread, int32_t vectors, int32_t channels)
     {
+        int32_t i;
         if (thread >> 32 == 0) {   // (a 64-bit division takes some hundred instructions)
             b = (uint32_t)thread / (uint32_t)vectors;
-            c = (int32_t)((uint32_t)thread % (uint32_t)vectors) * V;
+            i = (int32_t)((uint32_t)thread % (uint32_t)vectors);
         } else {
             b = thread / vectors;
-            c = (int32_t)(thread % vectors) * V;
+            i = (int32_t)(thread % vectors);
         }
+        c = min(i * V, channels - V);
+        flat = b * channels + c;
     }
     template <class U>
     __device__ __forceinline__ U* in(const Tensor<U>& x) const { return x.data + b * x.batch + c; }
@@ -372,7 +384,7 @@ __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_kernel(const Seque
     const int32_t tile = take_ticket<V>(chain, lds, (int32_t)((q.threads + 63) / 64), block);
     const int64_t thread = (int64_t)block * 64 + lane;
     const bool on = thread < q.threads;
-    const Place<T, V> at(on ? thread : 0, q.vectors);   // (lanes beyond the last channel read the first ones' and write nothing)
+    const Place<T, V> at(on ? thread : 0, q.vectors, q.channels);   // (lanes beyond the last channel read the first ones' and write nothing)
     const int64_t t = (int64_t)tile * tile_steps(V) + wave * kSteps;
     const int n = (int)max((int64_t)0, min((int64_t)kSteps, q.steps - t));
     float a[kSteps][V], add[kSteps][V], first[V], h[V];
@@ -381,7 +393,7 @@ __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_kernel(const Seque
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         f.v[v] = Map{1.0f, 0.0f};
-        first[v] = q.state && on ? q.state[thread * V + v] : 0.0f;
+        first[v] = q.state && on ? q.state[at.flat + v] : 0.0f;
     }
     {
         Vec<T, V> gs[kSteps], xs[kSteps];
@@ -411,7 +423,7 @@ __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_kernel(const Seque
         Vec<float, V> s;
 #pragma unroll
         for (int v = 0; v < V; ++v) s.v[v] = h[v];
-        store<float, V>(saved + ((t / kSteps) * q.threads + thread) * V, s);
+        store<float, V>(saved + (t / kSteps) * q.states + at.flat, s);
     }
     T* y = at.in(out) + t * out.step;
 #pragma unroll
@@ -427,7 +439,7 @@ __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_kernel(const Seque
     }
     if (last && t + n == q.steps) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) last[thread * V + v] = h[v];
+        for (int v = 0; v < V; ++v) last[at.flat + v] = h[v];
     }
 }
 
@@ -445,7 +457,7 @@ __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_gradient_kernel(co
     const int32_t k = take_ticket<V>(chain, lds, (int32_t)((q.threads + 63) / 64), block);
     const int64_t thread = (int64_t)block * 64 + lane;
     const bool on = thread < q.threads;
-    const Place<T, V> at(on ? thread : 0, q.vectors);
+    const Place<T, V> at(on ? thread : 0, q.vectors, q.channels);
     const int64_t t = (int64_t)(chain.count - 1 - k) * tile_steps(V) + (tile_waves(V) - 1 - wave) * kSteps;
     const int n = (int)max((int64_t)0, min((int64_t)kSteps, q.steps - t));
     float m[kSteps][V], d[kSteps][V], first[V], c[V];
@@ -455,7 +467,7 @@ __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_gradient_kernel(co
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         f.v[v] = Map{1.0f, 0.0f};
-        first[v] = dlast && on ? dlast[thread * V + v] : 0.0f;
+        first[v] = dlast && on ? dlast[at.flat + v] : 0.0f;
     }
     {
         Vec<T, V> gs[kSteps], xs[kSteps];
@@ -467,7 +479,7 @@ __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_gradient_kernel(co
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = 0.0f;
         if (on && n > 0) {
-            const Vec<float, V> s = load<float, V>(saved + ((t / kSteps) * q.threads + thread) * V);
+            const Vec<float, V> s = load<float, V>(saved + (t / kSteps) * q.states + at.flat);
 #pragma unroll
             for (int v = 0; v < V; ++v) h[v] = s.v[v];
         }
@@ -524,7 +536,7 @@ __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_gradient_kernel(co
     }
     if (dstate && t == 0) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) dstate[thread * V + v] = c[v];
+        for (int v = 0; v < V; ++v) dstate[at.flat + v] = c[v];
     }
 }
 
@@ -538,14 +550,14 @@ __global__ __launch_bounds__(256) void scan_kernel(const Sequences<T> q, const T
 {
     const int64_t thread = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (thread >= q.threads) return;
-    const Place<T, V> at(thread, q.vectors);
+    const Place<T, V> at(thread, q.vectors, q.channels);
     const T* g = at.in(q.gates);
     const T* x = at.in(q.inputs);
     const uint8_t* r = at.flags(q.resets);
     T* y = at.in(out);
     float h[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = q.state ? q.state[thread * V + v] : 0.0f;
+    for (int v = 0; v < V; ++v) h[v] = q.state ? q.state[at.flat + v] : 0.0f;
     auto steps = [&](int64_t t, int n) {
         Vec<T, V> gs[kSteps], xs[kSteps];
         load_steps<T, V>(g + t * q.gates.step, q.gates.step, n, gs);
@@ -555,7 +567,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const Sequences<T> q, const T
             Vec<float, V> s;
 #pragma unroll
             for (int v = 0; v < V; ++v) s.v[v] = h[v];
-            store<float, V>(saved + ((t / kSteps) * q.threads + thread) * V, s);
+            store<float, V>(saved + (t / kSteps) * q.states + at.flat, s);
         }
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
@@ -577,7 +589,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const Sequences<T> q, const T
     if (t < q.steps) steps(t, (int)(q.steps - t));
     if (last) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) last[thread * V + v] = h[v];
+        for (int v = 0; v < V; ++v) last[at.flat + v] = h[v];
     }
 }
 
@@ -589,7 +601,7 @@ __global__ __launch_bounds__(256, 4) void scan_gradient_kernel(const Sequences<T
 {
     const int64_t thread = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (thread >= q.threads) return;
-    const Place<T, V> at(thread, q.vectors);
+    const Place<T, V> at(thread, q.vectors, q.channels);
     const T* g = at.in(q.gates);
     const T* x = at.in(q.inputs);
     const T* dy = at.in(dout);
@@ -598,14 +610,14 @@ __global__ __launch_bounds__(256, 4) void scan_gradient_kernel(const Sequences<T
     T* dx = at.in(dinputs);
     float c[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) c[v] = dlast ? dlast[thread * V + v] : 0.0f;
+    for (int v = 0; v < V; ++v) c[v] = dlast ? dlast[at.flat + v] : 0.0f;
     auto steps = [&](int64_t t, int n) {
         Vec<T, V> gs[kSteps], xs[kSteps], dys[kSteps];
         load_steps<T, V>(g + t * q.gates.step, q.gates.step, n, gs);
         load_steps<T, V>(x + t * q.inputs.step, q.inputs.step, n, xs);
         load_steps<T, V>(dy + t * dout.step, dout.step, n, dys);
         const uint32_t resets = load_resets<kResets, kSteps>(r + t * q.resets.step, q.resets.step, n, q.one);
-        const Vec<float, V> s = load<float, V>(saved + ((t / kSteps) * q.threads + thread) * V);
+        const Vec<float, V> s = load<float, V>(saved + (t / kSteps) * q.states + at.flat);
         float h[V], m[kSteps][V], d[kSteps][V];
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = s.v[v];
@@ -650,7 +662,7 @@ __global__ __launch_bounds__(256, 4) void scan_gradient_kernel(const Sequences<T
     for (; t > 0; t -= kSteps) steps(t - kSteps, kSteps);
     if (dstate) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) dstate[thread * V + v] = c[v];
+        for (int v = 0; v < V; ++v) dstate[at.flat + v] = c[v];
     }
 }
 
@@ -661,14 +673,14 @@ __global__ __launch_bounds__(256) void step_kernel(const Sequences<T> q, T* __re
 {
     const int64_t thread = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (thread >= q.threads) return;
-    const Place<T, V> at(thread, q.vectors);
+    const Place<T, V> at(thread, q.vectors, q.channels);
     struct Bits { T v[V]; };
     struct States { float v[V]; };
     Bits g, x, o;
     States h;
     __builtin_memcpy(&g, at.in(q.gates), sizeof(g));
     __builtin_memcpy(&x, at.in(q.inputs), sizeof(x));
-    __builtin_memcpy(&h, state + thread * V, sizeof(h));
+    __builtin_memcpy(&h, state + at.flat, sizeof(h));
     const bool reset = q.resets.data && q.resets.data[at.b * q.resets.batch];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -678,7 +690,7 @@ __global__ __launch_bounds__(256) void step_kernel(const Sequences<T> q, T* __re
         h.v[v] = reset ? add : fmaf(a, h.v[v], add);
         o.v[v] = (T)h.v[v];
     }
-    __builtin_memcpy(state + thread * V, &h, sizeof(h));
+    __builtin_memcpy(state + at.flat, &h, sizeof(h));
     __builtin_memcpy(out + at.b * out_batch + at.c, &o, sizeof(o));
 }
 
@@ -701,6 +713,9 @@ size_t size_of(int32_t t) { return t == PICTURA_F32 ? 4 : 2; }
 constexpr int64_t kManyWaves = 1024;
 constexpr int64_t many_back(int vec) { return vec == 2 ? 2048 : 8192; }
 
+// Channels of a thread: two of 16 bits, as one load.
+int32_t vector_of(const pictura_sequences& q) { return q.dtype != PICTURA_F32 && q.channels > 1 ? 2 : 1; }
+
 // Channels of a thread, and the tiles that the steps are cut into (0: not cut).
 struct Shape {
     int32_t vec, tiles;
@@ -709,7 +724,7 @@ struct Shape {
 
 Shape shape_of(const pictura_sequences& q, int32_t vec, bool back)
 {
-    Shape s{vec, 0, q.batch * (q.channels / vec)};
+    Shape s{vec, 0, q.batch * ((q.channels + vec - 1) / vec)};
     const int64_t waves = (s.threads + 63) / 64, tile = tile_steps(vec), tiles = (q.steps + tile - 1) / tile;
     // (a launch has fewer than 2^32 threads)
     if (waves < (back ? many_back(vec) : kManyWaves) && q.steps >= 2 * tile && waves * tiles <= 1 << 21) s.tiles = (int32_t)tiles;
@@ -718,12 +733,9 @@ Shape shape_of(const pictura_sequences& q, int32_t vec, bool back)
 
 int64_t chain_words(const Shape& s) { return (int64_t)(s.tiles + (s.tiles + kGroup - 1) / kGroup) * s.threads * s.vec; }
 
-// The most that any alignment of the tensors takes.
 uint64_t workspace_bytes_of(const pictura_sequences& q)
 {
-    const int64_t one = chain_words(shape_of(q, 1, true)),
-                  two = q.dtype == PICTURA_F32 || q.channels % 2 ? 0 : chain_words(shape_of(q, 2, true));
-    return 256 + sizeof(Word) * (uint64_t)(one > two ? one : two);
+    return 256 + sizeof(Word) * (uint64_t)chain_words(shape_of(q, vector_of(q), true));
 }
 
 constexpr int64_t kMostChannels = (1ll << 31) - 1;   // of all sequences together
@@ -760,13 +772,7 @@ Sequences<T> sequences_of(const pictura_sequences& q, const Shape& s)
 {
     return Sequences<T>{{(const T*)q.gates, q.gates_batch, q.gates_step}, {(const T*)q.inputs, q.inputs_batch, q.inputs_step},
                         q.state, {q.resets, q.resets_batch, q.resets_step}, s.threads, q.steps,
-                        q.channels / s.vec, q.channels / s.vec % 64 == 0};
-}
-
-// Whether pairs of channels can be loaded as one from a tensor of elements of e bytes.
-bool pairs(const pictura_sequences& q, const void* p, int64_t batch, int64_t step, size_t e)
-{
-    return aligned(p, 2 * e) && (q.batch < 2 || batch % 2 == 0) && (q.steps < 2 || step % 2 == 0);
+                        q.batch * q.channels, q.channels, (q.channels + s.vec - 1) / s.vec, (q.channels + s.vec - 1) / s.vec % 64 == 0};
 }
 
 Chain chain_of(void* workspace, const Shape& s)
@@ -838,10 +844,7 @@ pictura_status pictura_gated_scan(const pictura_sequences* q, void* out, int64_t
             return PICTURA_EINVAL;
         if (!workspace || !aligned(workspace, 256) || workspace_bytes < workspace_bytes_of(*q)) return PICTURA_EINVAL;
     }
-    const bool two = e == 2 && q->channels % 2 == 0 && pairs(*q, q->gates, q->gates_batch, q->gates_step, e) &&
-                     pairs(*q, q->inputs, q->inputs_batch, q->inputs_step, e) && pairs(*q, out, out_batch, out_step, e) &&
-                     aligned(saved, 8);
-    const Shape s = shape_of(*q, two ? 2 : 1, false);
+    const Shape s = shape_of(*q, vector_of(*q), false);
     hipStream_t st = (hipStream_t)stream;
     with_kinds(*q, s.vec, [&](auto t, auto v, auto resets) {
         using T = decltype(t);
@@ -877,11 +880,7 @@ pictura_status pictura_gated_scan_gradient(const pictura_sequences* q, const flo
             return PICTURA_EINVAL;
         if (!workspace || !aligned(workspace, 256) || workspace_bytes < workspace_bytes_of(*q)) return PICTURA_EINVAL;
     }
-    const bool two = e == 2 && q->channels % 2 == 0 && pairs(*q, q->gates, q->gates_batch, q->gates_step, e) &&
-                     pairs(*q, q->inputs, q->inputs_batch, q->inputs_step, e) && pairs(*q, dout, dout_batch, dout_step, e) &&
-                     pairs(*q, dgates, dgates_batch, dgates_step, e) && pairs(*q, dinputs, dinputs_batch, dinputs_step, e) &&
-                     aligned(saved, 8);
-    const Shape s = shape_of(*q, two ? 2 : 1, true);
+    const Shape s = shape_of(*q, vector_of(*q), true);
     hipStream_t st = (hipStream_t)stream;
     with_kinds(*q, s.vec, [&](auto t, auto v, auto resets) {
         using T = decltype(t);
