@@ -666,21 +666,35 @@ __global__ __launch_bounds__(256, 4) void scan_gradient_kernel(const Sequences<T
     }
 }
 
-// One step in place: as many channels a thread as 16 bytes hold, at any address.
-template <class T, int V>
+// One step in place: as many channels a thread as 16 bytes hold, at any address.  (The last
+// ones of a sequence one by one: a state is read before it is replaced, so no two threads
+// may hold a channel.)
+template <class T>
 __global__ __launch_bounds__(256) void step_kernel(const Sequences<T> q, T* __restrict__ out, int64_t out_batch,
                                                    float* __restrict__ state)
 {
+    constexpr int V = 16 / sizeof(T);
     const int64_t thread = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (thread >= q.threads) return;
-    const Place<T, V> at(thread, q.vectors, q.channels);
-    struct Bits { T v[V]; };
-    struct States { float v[V]; };
-    Bits g, x, o;
-    States h;
-    __builtin_memcpy(&g, at.in(q.gates), sizeof(g));
-    __builtin_memcpy(&x, at.in(q.inputs), sizeof(x));
-    __builtin_memcpy(&h, state + at.flat, sizeof(h));
+    const Place<T, 1> at(thread, q.vectors, q.vectors);   // (at.c: the vector)
+    const int32_t c = at.c * V, n = min(V, q.channels - c);
+    const T* gates = q.gates.data + at.b * q.gates.batch + c;
+    const T* inputs = q.inputs.data + at.b * q.inputs.batch + c;
+    float* states = state + at.b * q.channels + c;
+    T* to = out + at.b * out_batch + c;
+    Vec<T, V> g, x, o;
+    Vec<float, V> h;
+    if (n == V) {
+        g = load<T, V>(gates);
+        x = load<T, V>(inputs);
+        h = load<float, V>(states);
+    } else {
+        g = x = Vec<T, V>{};
+        h = Vec<float, V>{};
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < n) g.v[v] = gates[v], x.v[v] = inputs[v], h.v[v] = states[v];
+    }
     const bool reset = q.resets.data && q.resets.data[at.b * q.resets.batch];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -690,8 +704,14 @@ __global__ __launch_bounds__(256) void step_kernel(const Sequences<T> q, T* __re
         h.v[v] = reset ? add : fmaf(a, h.v[v], add);
         o.v[v] = (T)h.v[v];
     }
-    __builtin_memcpy(state + at.flat, &h, sizeof(h));
-    __builtin_memcpy(out + at.b * out_batch + at.c, &o, sizeof(o));
+    if (n == V) {
+        store<float, V>(states, h);
+        store<T, V>(to, o);
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < n) states[v] = h.v[v], to[v] = o.v[v];
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -910,14 +930,9 @@ pictura_status pictura_gated_step(const pictura_sequences* q, void* out, int64_t
     auto go = [&](auto t) {
         using T = decltype(t);
         constexpr int V = 16 / sizeof(T);
-        const Shape s{q->channels % V ? 1 : V, 0, q->batch * (q->channels / (q->channels % V ? 1 : V))};
-        const dim3 grid((unsigned)((s.threads + 255) / 256));
-        if (s.vec == 1)
-            hipLaunchKernelGGL((step_kernel<T, 1>), grid, dim3(256), 0, (hipStream_t)stream, sequences_of<T>(*q, s), (T*)out,
-                               out_batch, state);
-        else
-            hipLaunchKernelGGL((step_kernel<T, V>), grid, dim3(256), 0, (hipStream_t)stream, sequences_of<T>(*q, s), (T*)out,
-                               out_batch, state);
+        const Shape s{V, 0, q->batch * ((q->channels + V - 1) / V)};
+        hipLaunchKernelGGL(step_kernel<T>, dim3((unsigned)((s.threads + 255) / 256)), dim3(256), 0, (hipStream_t)stream,
+                           sequences_of<T>(*q, s), (T*)out, out_batch, state);
     };
     if (q->dtype == PICTURA_F32) go(float{});
     else if (q->dtype == PICTURA_BF16) go((__bf16)0.0f);

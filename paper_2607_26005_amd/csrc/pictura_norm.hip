@@ -226,13 +226,18 @@ __global__ __launch_bounds__(Tm::kThreads) void norm_kernel(const Rows<T> R, T* 
     }
 }
 
-// What codes stand for.
-template <int V>
-__global__ __launch_bounds__(256) void values_kernel(const uint8_t* __restrict__ codes, int64_t stride,
-                                                     const float* __restrict__ scales, int32_t kind, int64_t rows,
-                                                     int32_t width, float* __restrict__ out, int64_t out_stride)
+// What codes stand for, four a thread at any address, the last ones of a row one by one.
+__device__ __forceinline__ float value_of(uint8_t code, int32_t kind)
 {
-    const int32_t per = width / V;
+    return kind == PICTURA_E4M3 ? __builtin_amdgcn_cvt_f32_fp8((int)code, 0) : (float)(int8_t)code;
+}
+
+static __global__ __launch_bounds__(256) void values_kernel(const uint8_t* __restrict__ codes, int64_t stride,
+                                                            const float* __restrict__ scales, int32_t kind, int64_t rows,
+                                                            int32_t width, float* __restrict__ out, int64_t out_stride)
+{
+    constexpr int V = 4;
+    const int32_t per = (width + V - 1) / V;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= rows * per) return;
     int64_t n;
@@ -245,14 +250,17 @@ __global__ __launch_bounds__(256) void values_kernel(const uint8_t* __restrict__
         c = (int32_t)(i % per) * V;
     }
     const float scale = scales[n];
-    const Vec<uint8_t, V> q = load<uint8_t, V>(codes + n * stride + c);
-    Vec<float, V> y;
+    codes += n * stride + c;
+    out += n * out_stride + c;
+    if (c + V <= width) {
+        const Vec<uint8_t, V> q = load<uint8_t, V>(codes);
+        Vec<float, V> y;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const float z = kind == PICTURA_E4M3 ? __builtin_amdgcn_cvt_f32_fp8((int)q.v[v], 0) : (float)(int8_t)q.v[v];
-        y.v[v] = z * scale;
+        for (int v = 0; v < V; ++v) y.v[v] = value_of(q.v[v], kind) * scale;
+        store<float, V>(out, y);
+    } else {
+        for (int v = 0; v < width - c; ++v) out[v] = value_of(codes[v], kind) * scale;
     }
-    store<float, V>(out + n * out_stride + c, y);
 }
 
 template <class T>
@@ -563,26 +571,14 @@ pictura_status pictura_row_values(const void* codes, int64_t codes_stride, const
     if (!codes || !scales || !out || !aligned(scales, 4) || !aligned(out, 4) || !stride_ok(codes_stride, rows, width, false) ||
         !stride_ok(out_stride, rows, width, true))
         return PICTURA_EINVAL;
-    auto go = [&](auto v) {
-        constexpr int V = decltype(v)::value;
-        const int64_t threads = rows * (width / V), blocks = (threads + 255) / 256;
-        // (a launch has fewer than 2^32 threads)
-        constexpr int64_t kMost = 1 << 23;
-        if (blocks <= kMost) {
-            hipLaunchKernelGGL(values_kernel<V>, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, (const uint8_t*)codes,
-                               codes_stride, scales, kind, rows, width, out, out_stride);
-            return;
-        }
-        const int64_t part = kMost * 256 / (width / V);
-        for (int64_t n = 0; n < rows; n += part) {
-            const int64_t some = rows - n < part ? rows - n : part;
-            hipLaunchKernelGGL(values_kernel<V>, dim3((unsigned)((some * (width / V) + 255) / 256)), dim3(256), 0,
-                               (hipStream_t)stream, (const uint8_t*)codes + n * codes_stride, codes_stride, scales + n, kind, some,
-                               width, out + n * out_stride, out_stride);
-        }
-    };
-    if (width % 4 == 0) go(Int<4>{});
-    else go(Int<1>{});
+    // (a launch has fewer than 2^32 threads)
+    const int64_t per = (width + 3) / 4, part = (1ll << 31) / per;
+    for (int64_t n = 0; n < rows; n += part) {
+        const int64_t some = rows - n < part ? rows - n : part;
+        hipLaunchKernelGGL(values_kernel, dim3((unsigned)((some * per + 255) / 256)), dim3(256), 0, (hipStream_t)stream,
+                           (const uint8_t*)codes + n * codes_stride, codes_stride, scales + n, kind, some, width,
+                           out + n * out_stride, out_stride);
+    }
     return launched();
 }
 
