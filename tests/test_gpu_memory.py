@@ -90,6 +90,12 @@ def test_steps_cut_into_segments(B, T, C, resets, dtype):
     _check(*_inputs(B, T, C, dtype, resets=resets, keep=4.0))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B, T, C, order", [(1, 1500, 7, "batch"), (2, 700, 131, "odd"), (3, 515, 129, "time"), (1, 600, 1, "batch")])
+def test_tiles_of_odd_channels(B, T, C, order, dtype):
+    _check(*_inputs(B, T, C, dtype, order=order, resets=0.003, keep=4.0))
+
+
 def test_one_long_sequence_of_few_channels():
     # 512 segments in 32 groups
     _check(*_inputs(1, 40003, 2, torch.float32, resets=0.0005, keep=7.0))
