@@ -18,10 +18,10 @@
 // one order, so that results repeat to the bit.
 //
 // Measured (one MI355X, large copies at 5,150 GB/s): 2,048 x 128 steps of 512 channels in bf16
-// forward 182 us, gradient 296 (838 and 1,376 MB with the saved states: 4.6 TB/s each); one
-// of 65,521 steps of 1,024 forward 111 us, gradient 158 (419 and 688 MB: 3.8 and 4.4 TB/s), of
+// forward 173 us, gradient 294 (838 and 1,376 MB with the saved states: 4.8 and 4.7 TB/s); one
+// of 65,521 steps of 1,024 forward 112 us, gradient 160 (419 and 688 MB: 3.7 and 4.3 TB/s), of
 // which a launch that sums the segments up first and one that reads them again took 152 and 221;
-// single steps of 65,536 x 512 in bf16 68 us (470 MB: 6.9 TB/s, some of it from the caches).
+// single steps of 65,536 x 512 in bf16 69 us (470 MB: 6.8 TB/s, some of it from the caches).
 #include <cmath>
 
 #include "pictura.h"
@@ -193,7 +193,8 @@ __device__ __forceinline__ uint32_t load_resets(const uint8_t* p, int64_t step, 
 
 // Waves of a tile, kSteps steps each: two channels a thread leave registers for two
 // workgroups of eight on a CU (one of 65,536 steps of 1,024 in bf16: forward 120 us, gradient
-// 173; with sixteen 120 and 180, with four 158 and 237), one channel for two of sixteen
+// 173; with sixteen 120 and 180, with four 158 and 237; all before gates of 16
+// bits took their exponential in one product), one channel for two of sixteen
 // (three of 8,192 of 330 in fp32: 30 and 43 us; with eight 37 and 45).
 constexpr int tile_waves(int vec) { return vec == 2 ? 8 : 16; }
 constexpr int tile_steps(int vec) { return tile_waves(vec) * kSteps; }
@@ -371,8 +372,8 @@ __device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, in
     }
 }
 
-// Forwards over one tile.  Of bf16 it takes 1,090 vector instructions a wave, 64 % of the time
-// it has; workgroups that take several tiles, and the next ticket ahead, are slower (169 us and
+// Forwards over one tile.  Of bf16 it takes 940 vector instructions a wave, and the vector units
+// are busy for 54 % of its time (backwards 1,520 and 60 %); workgroups that take several tiles, and the next ticket ahead, are slower (169 us and
 // 121), as tickets wait for workgroups that are not ready.
 template <class T, int V, bool kResets>
 __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_kernel(const Sequences<T> q, const Tensor<T> out, float* __restrict__ last,

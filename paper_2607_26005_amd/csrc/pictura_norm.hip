@@ -12,6 +12,13 @@
 // The mean is summed in 64 bits and q rounded once, so that it hangs neither on how a row
 // is split nor on the order of a sum; the codes of an 8-bit output, which change by a whole
 // step at a border, then repeat to the bit.
+//
+// Bound by memory.  Measured (one MI355X, large copies at 5,150 GB/s): 262,144 rows of 512 in
+// bf16 with residual forward 181 us, gradient 203 and the sums of dw 7 (1,074 MB each: 5.9 and
+// 5.3 TB/s, some of it from the caches); 65,536 of 512 to e4m3 51 us, their values 25; 4,095
+// of 8,197 in fp32 99, 111 and 7 us (537 MB each: 5.4 and 4.8 TB/s).  Rows of more than 16,384
+// elements of 16 bits have more sums of dw than registers: 2,048 of 32,768 forward 117 us,
+// gradient 315.
 #include <cmath>
 
 #include "pictura.h"
