@@ -43,7 +43,7 @@ HBM_PEAK_GBS = 8000.0   # MI355X HBM3E peak
 # `traffic` is reported as null.
 TRAFFIC = {
     "config": 4,
-    "sources_sha256": "2991bed528c94c068b883b66ecff028c592075c78410b2d3aab3a08e302c48ff",
+    "sources_sha256": "35b74acca91e98b75e736dfa16dd8aa67ea9c7c11cdea8713950fe6ad75d94b7",
     "fetch_bytes": 1.1530e9,
     "write_bytes": 5368709120,
 }
