@@ -605,8 +605,11 @@ PyObject* preference_loss(PyObject*, PyObject* const* args, Py_ssize_t n)
     return guarded([&]() -> PyObject* {
         arguments(n, 10, "preference_loss");
         const Tensor& logits = given(args[0], "logits");
+        const Preferences p = preferences(args);
+        if (wants_gradient({or_null(p.ref)})) refuse("ref_logp: wants a gradient, and there is no gradient of it: detach it");
+        if (wants_gradient({or_null(p.weights)})) refuse("weights: want a gradient, and there is no gradient of them: detach them");
         if (wants_gradient({&logits})) check_capture({{&logits, "logits"}});
-        return tuple(PreferenceLoss::apply(logits, preferences(args)));
+        return tuple(PreferenceLoss::apply(logits, p));
     });
 }
 

@@ -149,7 +149,8 @@ def preference_loss(logits, actions, offsets, ref_logp=None, *, weights=None, ma
                     smoothing: float = 0.0, average: bool = False, denominator: float = 0.0):
     """(loss, stats, ratios) for autograd: preference_gradient's loss, whose backward hands
     on the gradient that the same call computed, times the factor that arrives (a loss
-    scale).  Of float16 logits the gradient is kept in float32 for that."""
+    scale).  Only the logits get one: a ref_logp or weights that want a gradient are refused.
+    Of float16 logits the gradient is kept in float32 for that."""
     try:
         return _tensors.preference_loss(logits, actions, offsets, ref_logp, weights, mask, beta, smoothing, average,
                                         denominator)

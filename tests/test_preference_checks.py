@@ -95,3 +95,16 @@ def test_the_c_entry_refuses():
     assert L.pictura_preference_loss_workspace(-1, 3, 1, ctypes.addressof(out)) == pictura.EINVAL
     assert L.pictura_preference_loss_workspace(1, 3, (1 << 23) + 1, ctypes.addressof(out)) == pictura.EINVAL
     assert L.pictura_preference_loss_workspace(1, 3, 1, None) == pictura.EINVAL
+
+
+@pytest.mark.parametrize("name", ["ref_logp", "weights"])
+def test_tensors_without_a_gradient_that_want_one(name):
+    from paper_2607_26005_amd import policy
+    from paper_2607_26005_amd.pictura import PicturaError
+    a = dict(logits=torch.zeros(4, 3, requires_grad=True), actions=torch.zeros(4, dtype=torch.int64),
+             offsets=torch.tensor([0, 2, 4]), ref_logp=torch.zeros(4), weights=torch.ones(1))
+    a[name].requires_grad_()
+    with pytest.raises(PicturaError, match=f"{name}: .*no gradient"):
+        policy.preference_loss(**a)
+    with torch.no_grad(), pytest.raises(PicturaError, match="expected the HIP device"):   # (the next check)
+        policy.preference_loss(**a)
