@@ -656,7 +656,8 @@ pictura_status pictura_gated_scan_workspace(const pictura_sequences* sequences, 
  * NULL), fp32 [ceil(steps / PICTURA_SCAN_STEPS)][batch][channels], what the gradient
  * needs: the states before steps 0, 16, 32, ...  The same call gives the same bits; where few
  * channels stand against many steps the steps are cut into tiles, which rounds states in
- * another order.  last_state must not overlap state, nor out the inputs.
+ * another order.  last_state must not overlap state, nor out the inputs.  Of no steps
+ * last_state is state (or zeros).
  * workspace: device memory, 256-byte aligned, in use until the call's work on the stream
  * is done.  EINVAL: a null or misaligned pointer, sizes or strides out of range, or a
  * workspace too small. */

@@ -859,7 +859,8 @@ pictura_status pictura_gated_scan(const pictura_sequences* q, void* out, int64_t
     if (!sizes_ok(q)) return PICTURA_EINVAL;
     if (q->batch == 0) return PICTURA_OK;
     const size_t e = size_of(q->dtype);
-    if (!aligned(last_state, 4) || !aligned(q->state, 4) || (q->steps == 0 && !last_state)) return PICTURA_EINVAL;
+    if (!aligned(last_state, 4) || !aligned(q->state, 4)) return PICTURA_EINVAL;
+    if (q->steps == 0 && !last_state) return PICTURA_OK;   // (nothing to write)
     if (q->steps > 0) {
         if (!inputs_ok(*q) || !out || !aligned(out, e) || !apart(*q, out_batch, out_step) || !aligned(saved, 4))
             return PICTURA_EINVAL;
@@ -892,7 +893,8 @@ pictura_status pictura_gated_scan_gradient(const pictura_sequences* q, const flo
     if (!sizes_ok(q)) return PICTURA_EINVAL;
     if (q->batch == 0) return PICTURA_OK;
     const size_t e = size_of(q->dtype);
-    if (!aligned(dlast, 4) || !aligned(dstate, 4) || (q->steps == 0 && !dstate)) return PICTURA_EINVAL;
+    if (!aligned(dlast, 4) || !aligned(dstate, 4)) return PICTURA_EINVAL;
+    if (q->steps == 0 && !dstate) return PICTURA_OK;   // (nothing to write)
     if (q->steps > 0) {
         if (!inputs_ok(*q) || !saved || !aligned(saved, 4) || !dout || !aligned(dout, e) || !strides_ok(dout_batch, dout_step))
             return PICTURA_EINVAL;

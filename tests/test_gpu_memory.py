@@ -253,6 +253,19 @@ def test_nothing_to_do():
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("given", [True, False])
+def test_the_gradient_of_no_steps(given, dtype):
+    """A rollout of no steps has gradients too, whether or not its state wants one."""
+    from paper_2607_26005_amd import memory
+    g, x = (torch.zeros(3, 0, 4, device="cuda", dtype=dtype, requires_grad=True) for _ in range(2))
+    s = torch.randn(3, 4, device="cuda") if given else None
+    out, last = memory.gated_scan(g, x, s)
+    assert out.shape == (3, 0, 4) and torch.equal(last, s if given else torch.zeros_like(last))
+    dg, dx = torch.autograd.grad(out.sum() + (last * 2).sum(), (g, x))
+    assert dg.shape == dx.shape == (3, 0, 4) and dg.dtype == dx.dtype == dtype
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("B, C", [(1, 1), (5, 7), (8, 128), (300, 40), (3, 513)])
 def test_single_steps_are_the_scan(B, C, dtype):
     from paper_2607_26005_amd import memory

@@ -139,6 +139,15 @@ def test_c_entries_refuse():
     assert scan(_q(batch=0, gates=None)) == pictura.OK
 
 
+def test_c_entries_of_no_steps_have_nothing_to_write():
+    """Without steps all that a scan or its gradient could write is the state's side."""
+    L, q = pictura._lib, ctypes.byref(_q(steps=0, gates=None, inputs=None))
+    assert L.pictura_gated_scan(q, None, 0, 0, None, None, None, 0, None) == pictura.OK
+    assert L.pictura_gated_scan_gradient(q, None, None, 0, 0, 64, None, 0, 0, None, 0, 0, None, None, 0, None) == pictura.OK
+    assert L.pictura_gated_scan(q, None, 0, 0, 66, None, None, 0, None) == pictura.EINVAL
+    assert L.pictura_gated_scan_gradient(q, None, None, 0, 0, 66, None, 0, 0, None, 0, 0, None, None, 0, None) == pictura.EINVAL
+
+
 def test_workspace_covers_every_split():
     """However the steps are cut, maps of all segments and groups fit."""
     L = pictura._lib
