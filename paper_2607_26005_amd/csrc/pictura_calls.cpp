@@ -5,7 +5,11 @@
 // gradient: 69 to 71).
 #include "pictura_tensors.h"
 
+#include <ATen/TracerMode.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/impl/LocalDispatchKeySet.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -122,9 +126,28 @@ variable_list once(const variable_list& from, variable_list out)
     return out;
 }
 
+// The calls are no operators of torch: what records or transforms a program by its operators
+// sees only the outputs' allocation, and would take what comes out for a constant.
+void check_seen(const char* call)
+{
+    const char* by = at::tracer::impl::is_dispatch_enabled()                                                               ? "torch.jit.trace"
+                     : c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode) ? "torch.func"
+                     : c10::impl::TorchDispatchModeTLS::any_modes_set()                                          ? "a dispatch mode"
+                                                                                                                 : nullptr;
+    if (by) refuse(call, ": called under ", by, ", which would not see it");
+}
+
+// Forward-mode differentiation: a dual tensor need not want a gradient to have a tangent.
+void check_tangents(std::initializer_list<std::pair<const Tensor*, const char*>> ts)
+{
+    if (!c10::AutogradState::get_tls_state().get_fw_grad_mode()) return;
+    for (const auto& [t, name] : ts)
+        if (t && t->defined() && t->_fw_grad(0).defined()) refuse(name, ": has a tangent, and this call hands on none");
+}
+
 // f() with what it refuses as a ValueError, and torch's own errors as torch has them.
 template <class F>
-PyObject* guarded(F f)
+PyObject* guarded(const char* call, F f)
 {
     HANDLE_TH_ERRORS
     if (!entries.scan) {
@@ -132,6 +155,7 @@ PyObject* guarded(F f)
         return nullptr;
     }
     try {
+        check_seen(call);
         return f();
     } catch (const Refused& e) {
         PyErr_SetString(PyExc_ValueError, e.what());
@@ -228,6 +252,8 @@ struct GatedScan : torch::autograd::Function<GatedScan> {
         const variable_list held = ctx->get_saved_variables();
         const Tensor &gates = held[0], &inputs = held[1], &saved = held[2], &resets = held[3];
         variable_list out(4);
+        check_seen("the gradient of gated_scan");
+        check_tangents({{&grads[0], "the gradient of out"}, {&grads[1], "the gradient of the state"}});
         {
             const at::AutoGradMode off(false);
             const c10::DeviceGuard guard(gates.device());
@@ -256,10 +282,11 @@ struct GatedScan : torch::autograd::Function<GatedScan> {
 // gated_scan(gates, inputs, state, resets) -> (out, last state)
 PyObject* gated_scan(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
-    return guarded([&]() -> PyObject* {
+    return guarded("gated_scan", [&]() -> PyObject* {
         arguments(n, 4, "gated_scan");
         const Tensor &gates = given(args[0], "gates"), &inputs = given(args[1], "inputs");
         const Tensor *state = optional(args[2], "state"), *resets = optional(args[3], "resets");
+        check_tangents({{&gates, "gates"}, {&inputs, "inputs"}, {state, "state"}});
         if (wants_gradient({&gates, &inputs, state})) {
             check_capture({{&gates, "gates"}, {&inputs, "inputs"}, {state, "state"}});
             return tuple(GatedScan::apply(gates, inputs, or_none(state), or_none(resets)));
@@ -273,13 +300,14 @@ PyObject* gated_scan(PyObject*, PyObject* const* args, Py_ssize_t n)
 // gated_step(gates, inputs, state, resets, out) -> out
 PyObject* gated_step(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
-    return guarded([&]() -> PyObject* {
+    return guarded("gated_step", [&]() -> PyObject* {
         arguments(n, 5, "gated_step");
         const Tensor &gates = given(args[0], "gates"), &inputs = given(args[1], "inputs"), &state = given(args[2], "state");
         const Sequences q = sequences_of(false, gates, inputs, &state, optional(args[3], "resets"));
         if (wants_gradient({&gates, &inputs, &state}))
             refuse("gated_step hands on no gradient: call it under torch.no_grad(), or gated_scan");
         const Tensor* given_out = optional(args[4], "out");
+        check_tangents({{&gates, "gates"}, {&inputs, "inputs"}, {&state, "state"}, {given_out, "out"}});
         if (given_out && !apart(q, place(*given_out, "out", gates, false)))
             refuse("out: strides ", given_out->strides(), ": elements overlap");
         on_device(gates, "gates");
@@ -349,6 +377,8 @@ struct RMSNorm : torch::autograd::Function<RMSNorm> {
             out[0] = out[2] = dsum;   // (both undefined without a residual; linear, so nothing is lost)
             return out;
         }
+        check_seen("the gradient of rms_norm");
+        check_tangents({{&grads[0], "the gradient of y"}, {&dsum, "the gradient of the sum"}});
         {
             const at::AutoGradMode off(false);
             const c10::DeviceGuard guard(total.device());
@@ -380,11 +410,12 @@ struct RMSNorm : torch::autograd::Function<RMSNorm> {
 // rms_norm(x, weight, residual, eps) -> y, or (y, x + residual)
 PyObject* rms_norm(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
-    return guarded([&]() -> PyObject* {
+    return guarded("rms_norm", [&]() -> PyObject* {
         arguments(n, 4, "rms_norm");
         const Tensor &x = given(args[0], "x"), &weight = given(args[1], "weight");
         const Tensor* residual = optional(args[2], "residual");
         const double eps = number(args[3], "eps");
+        check_tangents({{&x, "x"}, {&weight, "weight"}, {residual, "residual"}});
         variable_list r;
         if (wants_gradient({&x, &weight, residual})) {
             check_capture({{&x, "x"}, {&weight, "weight"}, {residual, "residual"}});
@@ -408,11 +439,12 @@ int32_t code_kind(const Tensor& t, const char* name)
 // rms_norm_8bit(x, weight, residual, eps, whether e4m3) -> (codes, scales, x + residual or None)
 PyObject* rms_norm_8bit(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
-    return guarded([&]() -> PyObject* {
+    return guarded("rms_norm_8bit", [&]() -> PyObject* {
         arguments(n, 5, "rms_norm_8bit");
         const at::AutoGradMode off(false);
         const Tensor &x = given(args[0], "x"), &weight = given(args[1], "weight");
         const Tensor* residual = optional(args[2], "residual");
+        check_tangents({{&x, "x"}, {&weight, "weight"}, {residual, "residual"}});
         const Tensor r = rows_of(x, "x"), res = residual_rows(residual, x);
         const Norm q = norm_of(r, weight, or_null(res), number(args[3], "eps"));
         on_device(x, "x");
@@ -432,11 +464,12 @@ PyObject* rms_norm_8bit(PyObject*, PyObject* const* args, Py_ssize_t n)
 // row_values(codes, scales, out or None) -> out
 PyObject* row_values(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
-    return guarded([&]() -> PyObject* {
+    return guarded("row_values", [&]() -> PyObject* {
         arguments(n, 3, "row_values");
         const at::AutoGradMode off(false);
         const Tensor &codes = given(args[0], "codes"), &scales = given(args[1], "scales");
         const Tensor* given_out = optional(args[2], "out");
+        check_tangents({{&codes, "codes"}, {&scales, "scales"}, {given_out, "out"}});
         const int32_t kind = code_kind(codes, "codes");
         const Tensor r = rows_of(codes, "codes");
         if (r.size(1) > PICTURA_MAX_NORM || r.size(0) > 0x7FFFFFFF)
@@ -591,21 +624,24 @@ Preferences preferences(PyObject* const* args)
 // average, denominator) -> (stats, dlogits, ratios)
 PyObject* preference_gradient(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
-    return guarded([&]() -> PyObject* {
+    return guarded("preference_gradient", [&]() -> PyObject* {
         arguments(n, 10, "preference_gradient");
         const at::AutoGradMode off(false);
         const Tensor& logits = given(args[0], "logits");
-        return tuple(preferred(logits, preferences(args)));
+        const Preferences p = preferences(args);
+        check_tangents({{&logits, "logits"}, {or_null(p.ref), "ref_logp"}, {or_null(p.weights), "weights"}});
+        return tuple(preferred(logits, p));
     });
 }
 
 // preference_loss(the same) -> (loss, stats, ratios)
 PyObject* preference_loss(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
-    return guarded([&]() -> PyObject* {
+    return guarded("preference_loss", [&]() -> PyObject* {
         arguments(n, 10, "preference_loss");
         const Tensor& logits = given(args[0], "logits");
         const Preferences p = preferences(args);
+        check_tangents({{&logits, "logits"}, {or_null(p.ref), "ref_logp"}, {or_null(p.weights), "weights"}});
         if (wants_gradient({or_null(p.ref)})) refuse("ref_logp: wants a gradient, and there is no gradient of it: detach it");
         if (wants_gradient({or_null(p.weights)})) refuse("weights: want a gradient, and there is no gradient of them: detach them");
         if (wants_gradient({&logits})) check_capture({{&logits, "logits"}});

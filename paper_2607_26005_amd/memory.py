@@ -7,6 +7,10 @@ layers of one: in training they run over whole sequences of steps (rollouts, rec
 drives, several of either packed behind one another), when acting one step at a time on
 a state that stays on the device.  Every one runs in the library's kernels
 (csrc/pictura_memory.hip, csrc/pictura_norm.hip) on the current stream and never waits for the device.
+
+They are no operators of torch.  What would not see them, and so lose what they compute,
+is refused: torch.jit.trace, torch.func's transforms, dispatch modes, and tensors with a
+tangent (forward-mode differentiation).
 """
 from __future__ import annotations
 

@@ -137,7 +137,8 @@ def preference_gradient(logits, actions, offsets, ref_logp=None, *, weights=None
     over its rows in place of the sum.  smoothing: labels are wrong that often.
 
     dlogits is cut to the logits' type here, before any factor of the caller's; preference_loss
-    keeps what float16 would lose."""
+    keeps what float16 would lose.  Both are refused where they would not be seen: under
+    torch.jit.trace, torch.func's transforms and dispatch modes, and for tensors with a tangent."""
     try:
         return PreferenceGradient(*_tensors.preference_gradient(logits, actions, offsets, ref_logp, weights, mask, beta,
                                                                 smoothing, average, denominator))

@@ -450,3 +450,29 @@ def test_a_capture_refuses_leaves_that_an_eager_graph_holds():
         graph.replay()
         want, = torch.autograd.grad(memory.rms_norm(x, w), w, dy)
         assert torch.equal(dw, want)
+
+
+def test_gradients_with_a_tangent_or_not_seen():
+    """What arrives in the backward is looked at as what goes in."""
+    import torch.autograd.forward_ad as forward_ad
+    from torch.utils._python_dispatch import TorchDispatchMode
+    from paper_2607_26005_amd import memory
+
+    class Mode(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            return func(*args, **(kwargs or {}))
+
+    g, x, s, r = _inputs(2, 9, 4, torch.float32, resets=0.1)
+    x.requires_grad_()
+    w = torch.ones(4, device="cuda")
+    for f, name in ((lambda: memory.gated_scan(g, x, s, r)[0], "gated_scan"), (lambda: memory.rms_norm(x, w), "rms_norm"),
+                    (lambda: memory.rms_norm(x, w, x.detach())[0], "rms_norm")):
+        y = f()
+        with forward_ad.dual_level():
+            dy = forward_ad.make_dual(torch.ones_like(y), torch.ones_like(y))
+            with pytest.raises(RuntimeError, match="has a tangent"):
+                torch.autograd.grad(y, x, dy, retain_graph=True)
+        dy = torch.ones_like(y)
+        with Mode(), pytest.raises(RuntimeError, match=f"gradient of {name}: called under a dispatch mode"):
+            torch.autograd.grad(y, x, dy, retain_graph=True)
+        assert torch.equal(torch.autograd.grad(y, x, dy)[0], torch.autograd.grad(f(), x, dy)[0])
