@@ -145,6 +145,27 @@ void check_tangents(std::initializer_list<std::pair<const Tensor*, const char*>>
         if (t && t->defined() && t->_fw_grad(0).defined()) refuse(name, ": has a tangent, and this call hands on none");
 }
 
+// Outputs that have no gradient, of a call that wants one: it is not lost without a word, but
+// raises where it would arrive.
+struct Refuses : torch::autograd::Node {
+    explicit Refuses(const char* what) : what_(what) {}
+    variable_list apply(variable_list&&) override { throw std::runtime_error(what_); }
+    const char* what_;
+};
+
+void refuse_gradient(const char* what, const variable_list& from, const variable_list& out)
+{
+    const auto node = std::make_shared<Refuses>(what);
+    node->set_next_edges(torch::autograd::collect_next_edges(from));
+    for (const Tensor& t : out)
+        if (t.is_floating_point()) torch::autograd::set_history(t, node);
+}
+
+// The gradient of a sum: what arrives, for both terms.
+struct SumOfTwo : torch::autograd::Node {
+    variable_list apply(variable_list&& grads) override { return {grads[0], grads[0]}; }
+};
+
 // f() with what it refuses as a ValueError, and torch's own errors as torch has them.
 template <class F>
 PyObject* guarded(const char* call, F f)
@@ -441,10 +462,12 @@ PyObject* rms_norm_8bit(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
     return guarded("rms_norm_8bit", [&]() -> PyObject* {
         arguments(n, 5, "rms_norm_8bit");
-        const at::AutoGradMode off(false);
         const Tensor &x = given(args[0], "x"), &weight = given(args[1], "weight");
         const Tensor* residual = optional(args[2], "residual");
         check_tangents({{&x, "x"}, {&weight, "weight"}, {residual, "residual"}});
+        const bool wanted = wants_gradient({&x, &weight, residual}), through = wants_gradient({&x, residual});
+        if (through) check_capture({{&x, "x"}, {residual, "residual"}});
+        const at::AutoGradMode off(false);
         const Tensor r = rows_of(x, "x"), res = residual_rows(residual, x);
         const Norm q = norm_of(r, weight, or_null(res), number(args[3], "eps"));
         on_device(x, "x");
@@ -457,6 +480,14 @@ PyObject* rms_norm_8bit(PyObject*, PyObject* const* args, Py_ssize_t n)
         check(entries.norm_codes(c(q), e4m3 ? PICTURA_E4M3 : PICTURA_INT8, data<void>(total), q.width, codes.data_ptr(), q.width,
                                  data<float>(scales), stream_of(x)),
               "rms_norm_codes");
+        if (wanted)
+            refuse_gradient("rms_norm_8bit: its codes and scales have no gradient: detach them, or call rms_norm",
+                            {x, weight, residual ? *residual : Tensor()}, {codes, scales});
+        if (residual && through) {   // (the stream that goes on)
+            const auto node = std::make_shared<SumOfTwo>();
+            node->set_next_edges(torch::autograd::collect_next_edges(x, *residual));
+            torch::autograd::set_history(total, node);
+        }
         return tuple({codes, scales, total});
     });
 }
@@ -466,10 +497,12 @@ PyObject* row_values(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
     return guarded("row_values", [&]() -> PyObject* {
         arguments(n, 3, "row_values");
-        const at::AutoGradMode off(false);
         const Tensor &codes = given(args[0], "codes"), &scales = given(args[1], "scales");
         const Tensor* given_out = optional(args[2], "out");
         check_tangents({{&codes, "codes"}, {&scales, "scales"}, {given_out, "out"}});
+        const bool wanted = wants_gradient({&codes, &scales, given_out});
+        if (wanted && given_out) refuse("out: hands on no gradient, and one is wanted: detach the codes and scales");
+        const at::AutoGradMode off(false);
         const int32_t kind = code_kind(codes, "codes");
         const Tensor r = rows_of(codes, "codes");
         if (r.size(1) > PICTURA_MAX_NORM || r.size(0) > 0x7FFFFFFF)
@@ -492,6 +525,7 @@ PyObject* row_values(PyObject*, PyObject* const* args, Py_ssize_t n)
         check(entries.row_values((const void*)at, stride, data<float>(scales), kind, r.size(0), (int32_t)r.size(1), data<float>(out),
                                  r.size(1), stream_of(codes)),
               "row_values");
+        if (wanted) refuse_gradient("the values of 8-bit codes have no gradient: detach the codes and scales", {codes, scales}, {out});
         if (given_out && !out.is_inference()) out.unsafeGetTensorImpl()->bump_version();
         return THPVariable_Wrap(out);
     });

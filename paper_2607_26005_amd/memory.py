@@ -77,7 +77,8 @@ class RowCodes(NamedTuple):
     sum: Optional[torch.Tensor]    # x + residual, where there is a residual
 
     def values(self, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """What the codes stand for, float32 (in `out`, contiguous, where that is given)."""
+        """What the codes stand for, float32 (in `out`, contiguous, where that is given).  Has
+        no gradient, as the codes."""
         try:
             return _tensors.row_values(self.codes, self.scales, out)
         except ValueError as e:
@@ -88,7 +89,9 @@ def rms_norm_8bit(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torc
                   dtype: torch.dtype = torch.float8_e4m3fn) -> RowCodes:
     """rms_norm with an output in 8 bits, for layers that multiply in them: codes of `dtype`
     (float8_e4m3fn or int8) and a scale for each row, its largest magnitude over 448 or 127.
-    Codes are the nearest ones of the float32 result, to the bit.  No gradient flows through."""
+    Codes are the nearest ones of the float32 result, to the bit.  Codes and scales have no
+    gradient: where one is wanted it raises when it would reach them (detach them to go
+    without).  `sum` hands on its own, to x and the residual."""
     if dtype not in (torch.int8, torch.float8_e4m3fn):
         raise PicturaError(EINVAL, f"dtype: {dtype}, expected float8_e4m3fn or int8")
     try:

@@ -322,3 +322,41 @@ def test_offsets_beyond_32_bits():
     view = torch.as_strided(base, (2, 96), (far, 1))
     view.copy_(x)
     assert torch.equal(memory.rms_norm(view, w), memory.rms_norm(x, w))
+
+
+@pytest.mark.parametrize("kind", [torch.float8_e4m3fn, torch.int8])
+def test_codes_lose_no_gradient_without_a_word(kind):
+    """The sum of a norm to 8 bits hands on its gradient; its codes, which have none, raise
+    where one would arrive."""
+    from paper_2607_26005_amd import memory
+    x, w, r = (_rand(k, *s).cuda() for k, s in ((1, (6, 40)), (2, (40,)), (3, (6, 40))))
+    want = memory.rms_norm_8bit(x, w, r, dtype=kind)
+    assert not any(t.requires_grad for t in want) and not want.values().requires_grad
+    wants = [t.clone().requires_grad_() for t in (x, w, r)]
+    x1, w1, r1 = wants
+    dy = _rand(4, 6, 40).cuda()
+    held = memory.rms_norm_8bit(x1, w1, r1, dtype=kind)
+    assert torch.equal(held.codes.detach().view(torch.uint8), want.codes.view(torch.uint8))
+    assert torch.equal(held.scales, want.scales) and torch.equal(held.sum, want.sum)
+    dx, dr = torch.autograd.grad(held.sum, (x1, r1), dy)
+    assert torch.equal(dx, dy) and torch.equal(dr, dy)
+    both, = torch.autograd.grad(memory.rms_norm_8bit(x1, w, x1, dtype=kind).sum, x1, dy)   # the same tensor twice
+    assert torch.equal(both, 2 * dy)
+    twice = torch.autograd.grad(memory.rms_norm_8bit(x1 * 1, w, r, dtype=kind).sum.pow(3).sum(), x1, create_graph=True)[0]
+    again, = torch.autograd.grad(twice.sum(), x1)
+    assert torch.allclose(again, 6 * (x + r), rtol=1e-5, atol=1e-6)
+    for a in ((x1, w, r), (x, w1, r), (x, w, r1), (x1, w1, None)):
+        held = memory.rms_norm_8bit(*a, dtype=kind)
+        assert a[2] is None or held.sum.requires_grad == (a[1] is w)
+        with pytest.raises(RuntimeError, match="codes and scales have no gradient"):
+            held.scales.sum().backward()
+        with pytest.raises(RuntimeError, match="have no gradient"):
+            held.values().sum().backward()
+        if kind is torch.float8_e4m3fn:
+            with pytest.raises(RuntimeError, match="codes and scales have no gradient"):
+                held.codes.float().sum().backward()
+        free = memory.RowCodes(held.codes.detach(), held.scales.detach(), None).values()
+        assert torch.equal(free, held.values()) and not free.requires_grad
+    assert all(t.grad is None for t in wants)
+    with torch.no_grad():
+        assert not any(t is not None and t.requires_grad for t in memory.rms_norm_8bit(x1, w1, r1, dtype=kind))

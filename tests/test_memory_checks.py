@@ -217,6 +217,14 @@ def test_the_norms_other_arguments_are_checked():
     _raises("out: expected a contiguous", memory.RowCodes(z(N, W, dtype=torch.int8), f, None).values, z(W, N).t())
 
 
+def test_values_refuse_to_lose_a_gradient():
+    codes, scales, out = z(N, W, dtype=torch.int8), z(N), z(N, W)
+    _raises("out: hands on no gradient", memory.RowCodes(codes, scales.requires_grad_(), None).values, out)
+    _raises("out: hands on no gradient", memory.RowCodes(codes, z(N), None).values, z(N, W, requires_grad=True))
+    with torch.no_grad():   # (the next check)
+        _raises("expected the HIP device", memory.RowCodes(codes, scales, None).values, out)
+
+
 def test_the_norm_refuses_host_tensors_for_their_device():
     _raises("expected the HIP device", memory.rms_norm, z(N, W), z(W))
     _raises("expected the HIP device", memory.rms_norm_8bit, z(N, W), z(W))
