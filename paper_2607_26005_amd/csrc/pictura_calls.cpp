@@ -325,9 +325,9 @@ PyObject* gated_step(PyObject*, PyObject* const* args, Py_ssize_t n)
         arguments(n, 5, "gated_step");
         const Tensor &gates = given(args[0], "gates"), &inputs = given(args[1], "inputs"), &state = given(args[2], "state");
         const Sequences q = sequences_of(false, gates, inputs, &state, optional(args[3], "resets"));
-        if (wants_gradient({&gates, &inputs, &state}))
-            refuse("gated_step hands on no gradient: call it under torch.no_grad(), or gated_scan");
         const Tensor* given_out = optional(args[4], "out");
+        if (wants_gradient({&gates, &inputs, &state, given_out}))
+            refuse("gated_step hands on no gradient: call it under torch.no_grad(), or gated_scan");
         check_tangents({{&gates, "gates"}, {&inputs, "inputs"}, {&state, "state"}, {given_out, "out"}});
         if (given_out && !apart(q, place(*given_out, "out", gates, false)))
             refuse("out: strides ", given_out->strides(), ": elements overlap");

@@ -73,6 +73,14 @@ def test_a_step_refuses_to_lose_a_gradient():
         _raises("no gradient", memory.gated_step, **a)
 
 
+def test_a_step_into_what_wants_a_gradient():
+    """An `out` with a graph would keep that of what the step replaced."""
+    for out in (z(B, C, requires_grad=True), z(B, C, requires_grad=True) * 2):
+        _raises("no gradient", memory.gated_step, z(B, C), z(B, C), z(B, C), out=out)
+        with torch.no_grad():   # (the next check)
+            _raises("expected the HIP device", memory.gated_step, z(B, C), z(B, C), z(B, C), out=out)
+
+
 def test_outputs_of_the_scan_are_checked():
     ok = lambda: dict(gates=z(B, T, C), inputs=z(B, T, C), out=z(B, T, C), last_state=z(B, C))
     _raises("out: shape", pictura.pictura_gated_scan, **dict(ok(), out=z(B, T, C + 1)))
