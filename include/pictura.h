@@ -678,7 +678,8 @@ pictura_status pictura_gated_scan_gradient(const pictura_sequences* sequences, c
 
 /* One step of the recurrence (steps is 1, sequences->state not read): state fp32
  * [batch][channels] is replaced by h, out[b * out_batch + c] receives it in the inputs'
- * type and may be the inputs' or the gates' own memory (same stride). */
+ * type.  out and the state may each be the inputs' or the gates' own rows (same type, address
+ * and stride), and out the state's; any other memory that is written and also read is EINVAL. */
 pictura_status pictura_gated_step(const pictura_sequences* sequences, void* out, int64_t out_batch, float* state, void* stream);
 
 #define PICTURA_MAX_NORM (1 << 16)   /* most elements of a normed row */

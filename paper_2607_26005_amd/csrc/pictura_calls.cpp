@@ -329,8 +329,9 @@ PyObject* gated_step(PyObject*, PyObject* const* args, Py_ssize_t n)
         if (wants_gradient({&gates, &inputs, &state, given_out}))
             refuse("gated_step hands on no gradient: call it under torch.no_grad(), or gated_scan");
         check_tangents({{&gates, "gates"}, {&inputs, "inputs"}, {&state, "state"}, {given_out, "out"}});
-        if (given_out && !apart(q, place(*given_out, "out", gates, false)))
-            refuse("out: strides ", given_out->strides(), ": elements overlap");
+        const Place o = given_out ? place(*given_out, "out", gates, false) : Place{};
+        if (given_out && !apart(q, o)) refuse("out: strides ", given_out->strides(), ": elements overlap");
+        check_step(q, (int64_t)gates.element_size(), o, q.state);
         on_device(gates, "gates");
         const c10::DeviceGuard guard(gates.device());
         const Tensor out = given_out ? *given_out : empty(inputs.sizes(), inputs.scalar_type(), inputs);

@@ -26,6 +26,7 @@
 
 #include "pictura.h"
 #include "pictura_internal.h"
+#include "pictura_overlap.h"
 
 #pragma clang fp contract(off)
 
@@ -778,6 +779,19 @@ bool apart(const pictura_sequences& q, int64_t batch, int64_t step)
     return !many || !more || batch / step >= q.steps || step / batch >= q.batch;   // one spans all of the other
 }
 
+// What a step writes is either a thread's own operands or apart from all that is read: threads
+// run in any order.
+bool step_apart(const pictura_sequences& q, const void* out, int64_t out_batch, const float* state)
+{
+    const int64_t e = (int64_t)size_of(q.dtype);
+    auto rows = [&](const void* p, int64_t batch) { return region(p, q.batch, q.channels * e, batch * e); };
+    const Region y = rows(out, out_batch), h = region(state, q.batch, q.channels * 4ll, q.channels * 4ll);
+    for (const Region& r : {rows(q.gates, q.gates_batch), rows(q.inputs, q.inputs_batch)})
+        if ((overlap(r, y) && !same(r, y)) || (overlap(r, h) && !same(r, h))) return false;
+    const Region flags = region(q.resets, q.batch, 1, q.resets_batch);
+    return !(overlap(y, h) && !same(y, h)) && !overlap(flags, y) && !overlap(flags, h);
+}
+
 bool inputs_ok(const pictura_sequences& q)
 {
     const size_t e = size_of(q.dtype);
@@ -930,6 +944,7 @@ pictura_status pictura_gated_step(const pictura_sequences* q, void* out, int64_t
     if (q->batch == 0) return PICTURA_OK;
     const size_t e = size_of(q->dtype);
     if (!inputs_ok(*q) || !out || !aligned(out, e) || !apart(*q, out_batch, 0) || !state || !aligned(state, 4)) return PICTURA_EINVAL;
+    if (!step_apart(*q, out, out_batch, state)) return PICTURA_EINVAL;
     auto go = [&](auto t) {
         using T = decltype(t);
         constexpr int V = 16 / sizeof(T);

@@ -217,6 +217,8 @@ PyObject* sequences(PyObject*, PyObject* const* args, Py_ssize_t n)
         const at::Tensor& gates = given(args[1], "gates");
         const Sequences q = sequences_of(whole, gates, given(args[2], "inputs"), optional(args[3], "state"), optional(args[4], "resets"));
         std::vector<uint64_t> values;
+        Place written;   // of one step
+        uint64_t state = 0;
         for (Py_ssize_t k = 5; k < n; k += 3) {
             const char* name = PyUnicode_AsUTF8(args[k]);
             const char* kind = PyUnicode_AsUTF8(args[k + 1]);
@@ -226,11 +228,14 @@ PyObject* sequences(PyObject*, PyObject* const* args, Py_ssize_t n)
                 if (*kind == 'o' && !apart(q, p))
                     refuse(name, ": strides ", THPVariable_Unpack(args[k + 2]).strides(), ": elements overlap");
                 values.insert(values.end(), {p.at, (uint64_t)p.batch, (uint64_t)p.step});
+                if (*kind == 'o') written = p;
             } else {
                 const at::Tensor* t = optional(args[k + 2], name);
                 values.push_back(t ? floats(q, gates, *t, name, *kind == 'c') : 0);
+                if (*kind == 'w') state = values.back();
             }
         }
+        if (!whole) check_step(q, (int64_t)gates.element_size(), written, state);
         for (Py_ssize_t k = 5; k < n; k += 3)
             if (*PyUnicode_AsUTF8(args[k + 1]) == 'w' && args[k + 2] != Py_None) {
                 const at::Tensor& t = THPVariable_Unpack(args[k + 2]);

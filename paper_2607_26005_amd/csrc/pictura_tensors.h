@@ -14,6 +14,8 @@
 #include <utility>
 #include <vector>
 
+#include "pictura_overlap.h"
+
 extern PyMethodDef pictura_calls[];   // pictura_calls.cpp
 
 namespace {
@@ -126,6 +128,24 @@ Sequences sequences_of(bool whole, const at::Tensor& gates, const at::Tensor& in
         q.resets_step = whole ? r.stride(1) : 0;
     }
     return q;
+}
+
+// What a step writes, `out` and the state, may be an operand's own rows and nothing else that is
+// read or written.
+void check_step(const Sequences& q, int64_t size, const Place& out, uint64_t state)
+{
+    using namespace pictura;
+    auto rows = [&](uint64_t at, int64_t batch) { return region((const void*)at, q.batch, q.channels * size, batch * size); };
+    const Region y = rows(out.at, out.batch), h = region((const void*)state, q.batch, q.channels * 4ll, q.channels * 4ll),
+                 flags = region((const void*)q.resets, q.batch, 1, q.resets_batch);
+    const std::pair<Region, const char*> read[] = {{rows(q.gates, q.gates_batch), "the gates"}, {rows(q.inputs, q.inputs_batch), "the inputs"}};
+    for (const auto& [r, name] : read) {
+        if (overlap(r, y) && !same(r, y)) refuse("out: overlaps ", name, ", and is not the same rows");
+        if (overlap(r, h) && !same(r, h)) refuse("state: overlaps ", name, ", and is not the same rows");
+    }
+    if (overlap(y, h) && !same(y, h)) refuse("out: overlaps the state, and is not the same rows");
+    if (overlap(flags, y)) refuse("out: overlaps the resets");
+    if (overlap(flags, h)) refuse("state: overlaps the resets");
 }
 
 // pictura_norm (include/pictura.h)

@@ -49,7 +49,8 @@ def gated_step(gates: torch.Tensor, inputs: torch.Tensor, state: torch.Tensor, r
                out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """One step of gated_scan's recurrence for [batch, channels], the policy's form when it
     acts: `state` (float32) is replaced by what is remembered after the step, and returned in
-    the inputs' type (in `out`, where that is given; it may be the inputs or the gates).
+    the inputs' type (in `out`, where that is given; it may be the inputs or the gates, and is
+    refused where it overlaps them, the state or the resets in another way).
     resets: [batch].  No gradient flows through it: where one is wanted it is refused."""
     try:
         return _tensors.gated_step(gates, inputs, state, resets, out)

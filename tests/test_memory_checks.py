@@ -81,6 +81,86 @@ def test_a_step_into_what_wants_a_gradient():
             _raises("expected the HIP device", memory.gated_step, z(B, C), z(B, C), z(B, C), out=out)
 
 
+def _steps():
+    """What a step may write over, and what not: (match or None, arguments)."""
+    both, half, held, row = z(4, 48), z(4, 48, dtype=torch.bfloat16), z(5, 16), z(64)
+    a = dict(gates=both[:, :16], inputs=both[:, 16:32], state=z(4, 16))
+    b = dict(gates=z(4, 16, dtype=torch.bfloat16), inputs=half[:, 16:32], state=z(4, 16))
+    flat, last = both.view(-1), both.view(torch.bool).view(4, -1)[:, -1]
+    for out in (None, a["gates"], a["inputs"], both[:, 32:], a["state"], z(4, 16)):   # its own rows, or rows between
+        yield None, dict(a, out=out)
+    yield None, dict(a, inputs=a["state"])
+    yield None, dict(a, resets=last)
+    yield "out: overlaps the gates", dict(a, out=both[:, 8:24])                            # shifted
+    yield "out: overlaps the gates", dict(a, out=both[:, 1:17])
+    yield "out: overlaps the inputs", dict(a, out=both[:, 31:47])
+    yield "out: overlaps the gates", dict(a, out=flat[:64].view(4, 16))                   # another stride
+    yield "out: overlaps the gates", dict(a, out=flat[-65:-1].view(4, 16))   # (the inputs too)
+    yield "out: overlaps the gates", dict(a, gates=row[:16].expand(4, 16), out=row.view(4, 16))
+    yield "out: overlaps the state", dict(a, state=held[:4], out=held[1:])
+    yield "out: overlaps the state", dict(b, out=b["state"].view(torch.bfloat16)[:, :16])
+    yield "state: overlaps the gates", dict(a, gates=held[1:], state=held[:4])
+    yield "state: overlaps the inputs", dict(a, inputs=flat[8:72].view(4, 16), state=flat[:64].view(4, 16), gates=z(4, 16))
+    yield "state: overlaps the inputs", dict(b, state=half.view(-1)[:128].view(torch.float32).view(4, 16))
+    yield "out: overlaps the resets", dict(a, out=both[:, 32:], resets=last)
+    yield "state: overlaps the resets", dict(a, resets=a["state"].view(torch.bool)[:, 3])
+
+
+def test_a_step_writes_over_its_own_operands_alone():
+    """Threads run in any order: what one writes over another's operands is right or wrong by chance."""
+    for match, a in _steps():
+        _raises(match or "expected the HIP device", memory.gated_step, **a)
+        if match:
+            _raises(match, pictura.pictura_gated_step, **dict(dict(out=z(4, 16, dtype=a["gates"].dtype)), **a))
+
+
+def test_the_step_entry_refuses_the_same():
+    L, ref = pictura._lib, ctypes.byref
+    q = lambda **k: ref(_q(**dict(dict(steps=1, batch=4, channels=16, gates=4096, inputs=4096 + 64, gates_batch=48, inputs_batch=48), **k)))
+    step = lambda out=1 << 16, stride=16, state=1 << 20, **k: L.pictura_gated_step(q(**k), out, stride, state, None)
+    for k in (dict(out=4096 + 4, stride=48), dict(out=4096, stride=16), dict(out=4096 - 252), dict(out=4096 + 3 * 192 + 60),
+              dict(state=4096), dict(state=4096 + 640 - 4), dict(out=(1 << 20) + 4), dict(out=(1 << 20) - 252, stride=16),
+              dict(resets=(1 << 16) + 252, resets_batch=1), dict(resets=(1 << 20) - 3, resets_batch=1), dict(dtype=1, out=1 << 20)):
+        assert step(**k) == pictura.EINVAL, k
+
+
+def test_overlap_is_exact(tmp_path):
+    """pictura_overlap.h against every byte of small regions."""
+    import os
+    import subprocess
+    source = tmp_path / "overlap.cpp"
+    source.write_text(r"""
+#include <cstdio>
+#include <set>
+#include "pictura_overlap.h"
+using namespace pictura;
+int main()
+{
+    int both = 0, wrong = 0;
+    std::set<uintptr_t> held;
+    for (int64_t ra = 1; ra < 5; ++ra) for (int64_t na = 1; na < 4; ++na) for (int64_t sa = 0; sa < 9; ++sa) {
+        const Region a{100, ra, na, sa};
+        held.clear();
+        for (int64_t i = 0; i < ra; ++i) for (int64_t j = 0; j < na; ++j) held.insert(100 + i * sa + j);
+        for (uintptr_t at = 70; at < 140; ++at) for (int64_t rb = 1; rb < 5; ++rb) for (int64_t nb = 1; nb < 4; ++nb)
+            for (int64_t sb = 0; sb < 9; ++sb) {
+                bool want = false;
+                for (int64_t i = 0; i < rb && !want; ++i) for (int64_t j = 0; j < nb; ++j) want = want || held.count(at + i * sb + j);
+                both += want;
+                wrong += want != overlap(a, Region{at, rb, nb, sb});
+            }
+    }
+    const Region none{0, 4, 4, 4}, empty{100, 0, 4, 4}, some{100, 4, 4, 4};
+    wrong += overlap(none, some) + overlap(empty, some) + overlap(some, empty) + !same(some, some) + same(some, Region{100, 4, 4, 8});
+    printf("%d %d\n", both, wrong);
+}
+""")
+    csrc = os.path.join(os.path.dirname(pictura.__file__), "csrc")
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-I", csrc, str(source), "-o", str(tmp_path / "overlap")])
+    both, wrong = map(int, subprocess.check_output([str(tmp_path / "overlap")]).split())
+    assert both > 10000 and wrong == 0
+
+
 def test_outputs_of_the_scan_are_checked():
     ok = lambda: dict(gates=z(B, T, C), inputs=z(B, T, C), out=z(B, T, C), last_state=z(B, C))
     _raises("out: shape", pictura.pictura_gated_scan, **dict(ok(), out=z(B, T, C + 1)))
