@@ -719,7 +719,8 @@ pictura_status pictura_rms_norm(const pictura_norm* norm, void* sum, int64_t sum
 pictura_status pictura_rms_norm_codes(const pictura_norm* norm, int32_t kind, void* sum, int64_t sum_stride, void* codes,
                                       int64_t codes_stride, float* scales, void* stream);
 
-/* What codes stand for, in fp32: out[n * out_stride + i] = code * scales[n]. */
+/* What codes stand for, in fp32: out[n * out_stride + i] = code * scales[n].  EINVAL also where
+ * out overlaps the codes or the scales. */
 pictura_status pictura_row_values(const void* codes, int64_t codes_stride, const float* scales, int32_t kind, int64_t rows,
                                   int32_t width, float* out, int64_t out_stride, void* stream);
 

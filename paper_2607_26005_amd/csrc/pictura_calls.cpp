@@ -519,6 +519,10 @@ PyObject* row_values(PyObject*, PyObject* const* args, Py_ssize_t n)
             if (given_out->scalar_type() != at::kFloat) refuse("out: dtype ", given_out->scalar_type(), ", expected float32");
             if (given_out->sizes() != codes.sizes() || !given_out->is_contiguous())
                 refuse("out: expected a contiguous tensor of shape ", codes.sizes());
+            using namespace pictura;
+            const Region y = region(given_out->data_ptr(), r.size(0), r.size(1) * 4, r.size(1) * 4);
+            if (overlap(y, region((const void*)at, r.size(0), r.size(1), stride))) refuse("out: overlaps the codes");
+            if (overlap(y, region(scales.data_ptr(), r.size(0), 4, 4))) refuse("out: overlaps the scales");
         }
         on_device(codes, "codes");
         const c10::DeviceGuard guard(codes.device());

@@ -23,6 +23,7 @@
 
 #include "pictura.h"
 #include "pictura_lanes.h"
+#include "pictura_overlap.h"
 
 #pragma clang fp contract(off)
 
@@ -578,6 +579,8 @@ pictura_status pictura_row_values(const void* codes, int64_t codes_stride, const
     if (!codes || !scales || !out || !aligned(scales, 4) || !aligned(out, 4) || !stride_ok(codes_stride, rows, width, false) ||
         !stride_ok(out_stride, rows, width, true))
         return PICTURA_EINVAL;
+    const Region y = region(out, rows, width * 4ll, out_stride * 4);   // (threads run in any order)
+    if (overlap(y, region(codes, rows, width, codes_stride)) || overlap(y, region(scales, rows, 4, 4))) return PICTURA_EINVAL;
     // (a launch has fewer than 2^32 threads)
     const int64_t per = (width + 3) / 4, part = (1ll << 31) / per;
     for (int64_t n = 0; n < rows; n += part) {

@@ -896,7 +896,7 @@ def pictura_row_values(codes, scales, out):
     sp, = _vectors(codes, N, "scales", "f", scales)
     st = _call(c.device, _lib.pictura_row_values, cp, cs, sp, kind, N, C, op, os_)
     if st != OK:
-        raise PicturaError(st, "row_values failed")
+        raise PicturaError(st, "row_values failed" if st != EINVAL else "row_values: out overlaps the codes or the scales")
 
 
 def pictura_rms_norm_gradient(x, weight, factors, dout, dx, dweight, dsum=None):

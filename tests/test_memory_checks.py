@@ -305,6 +305,20 @@ def test_the_norms_other_arguments_are_checked():
     _raises("out: expected a contiguous", memory.RowCodes(z(N, W, dtype=torch.int8), f, None).values, z(W, N).t())
 
 
+def test_values_are_apart_from_their_codes():
+    out = z(4, 16)
+    codes = out.view(torch.int8)
+    for c in (codes[:, :16], codes[:, 48:], codes.view(-1)[100:164].view(4, 16)):
+        _raises("out: overlaps the codes", memory.RowCodes(c, z(4), None).values, out)
+    _raises("out: overlaps the scales", memory.RowCodes(z(4, 16, dtype=torch.int8), out.view(-1)[3:7], None).values, out)
+    held = z(5, 16)   # beside one another
+    _raises("expected the HIP device", memory.RowCodes(held.view(torch.int8)[:4, :16], held[4, :4], None).values, z(4, 16))
+    _raises("expected the HIP device", memory.RowCodes(held.view(torch.int8)[4:, :16], held[4, 15:], None).values, held[3:4])
+    values = lambda c=1 << 16, cs=16, s=1 << 20, out=4096, os_=16: pictura._lib.pictura_row_values(c, cs, s, 0, 4, 16, out, os_, None)
+    for k in (dict(c=4096 + 240), dict(c=4096 - 63), dict(s=4096 + 252), dict(s=4096 - 12)):
+        assert values(**k) == pictura.EINVAL, k
+
+
 def test_values_refuse_to_lose_a_gradient():
     codes, scales, out = z(N, W, dtype=torch.int8), z(N), z(N, W)
     _raises("out: hands on no gradient", memory.RowCodes(codes, scales.requires_grad_(), None).values, out)
