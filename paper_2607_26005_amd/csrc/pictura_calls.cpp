@@ -650,13 +650,23 @@ struct PreferenceLoss : torch::autograd::Function<PreferenceLoss> {
     }
 };
 
+bool truth(PyObject* o, const char* name)
+{
+    const int is = PyObject_IsTrue(o);
+    if (is < 0) {
+        PyErr_Clear();
+        refuse(name, ": ", Py_TYPE(o)->tp_name, ", expected a bool");
+    }
+    return is == 1;
+}
+
 Preferences preferences(PyObject* const* args)
 {
     auto or_undefined = [](const Tensor* t) { return t ? *t : Tensor(); };
     return Preferences{given(args[1], "actions"), given(args[2], "offsets"), or_undefined(optional(args[3], "ref_logp")),
                        or_undefined(optional(args[4], "weights")), or_undefined(optional(args[5], "mask")),
                        number(args[6], "beta"), number(args[7], "smoothing"), number(args[9], "denominator"),
-                       PyObject_IsTrue(args[8]) == 1};
+                       truth(args[8], "average")};
 }
 
 // preference_gradient(logits, actions, offsets, ref_logp, weights, mask, beta, smoothing,

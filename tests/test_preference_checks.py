@@ -60,6 +60,16 @@ def test_preferences_refuse(match, bad):
     _raises(match, policy.preference_loss, **_args(**bad))
 
 
+def test_an_average_that_is_no_truth_value():
+    class Odd:
+        def __bool__(self):
+            raise KeyError("neither")
+
+    for bad in (Odd(), z(2)):
+        _raises("average: ", policy.preference_gradient, **_args(average=bad))
+        _raises("average: ", policy.preference_loss, **_args(average=bad))
+
+
 def test_output_buffers_are_checked():
     ok = lambda **k: dict(_args(), out_stats=z(4), out_ratios=z(2 * P), dlogits=z(N, A), **k)
     _raises("out_stats: shape", pictura.pictura_preference_loss, **dict(ok(), out_stats=z(6)))
