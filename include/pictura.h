@@ -651,7 +651,10 @@ pictura_status pictura_gated_scan_workspace(const pictura_sequences* sequences, 
 /* Gated linear recurrence over whole sequences: with a = sigmoid(gates),
  *   h_t = a_t h_(t-1) + (1 - a_t) inputs_t,
  * h_(t-1) = 0 where step t is reset, in fp32 (a and 1 - a each to 10 units of 2^-24 of their
- * own, with gates of 16 bits to 10 + 1.3 |gate|).  out (same type, strides of its own, no two elements at one place) receives h_t;
+ * own, with gates of 16 bits to 10 + 1.3 |gate|; 0 below 2^-126, from gates of 88 on).  An
+ * infinite state stays infinite until a reset; a step whose a is 0 makes it a NaN, or, where the
+ * steps are cut into tiles, only within its tile.  out (same type, strides of its own, no two
+ * elements at one place) receives h_t;
  * last_state (or NULL) fp32 [batch][channels] the state after the last step; saved (or
  * NULL), fp32 [ceil(steps / PICTURA_SCAN_STEPS)][batch][channels], what the gradient
  * needs: the states before steps 0, 16, 32, ...  The same call gives the same bits; where few

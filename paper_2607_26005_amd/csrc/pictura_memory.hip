@@ -119,6 +119,12 @@ __device__ __forceinline__ Map then(const Map& f, const Map& g)
     return Map{__float_as_uint(g.P) == 0x80000000u ? g.P : g.P * f.P, apply(g, f.H)};
 }
 
+// A product of gates as others may use it: what fp32 does not reach is 2^-149, the smallest number
+// above 0, and not 0.  An infinite state then stays infinite, as it does through the steps one by
+// one, where 0 times infinity is a NaN; of a finite one it is off by 2^-149, as products next to it
+// are.  (As whole numbers: -0 and NaN are larger.)
+__device__ __forceinline__ float kept(float P) { return __uint_as_float(max(__float_as_uint(P), 1u)); }
+
 // Says that x may be new from here on, and in this order: what is computed from it is not
 // computed earlier, where it would take registers for longer.
 __device__ __forceinline__ void hold(float& x) { asm volatile("" : "+v"(x)); }
@@ -315,7 +321,7 @@ __device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, in
         }
         if (on) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) tell(c.tiles + ((int64_t)k * threads + thread) * V + v, all.v[v]);
+            for (int v = 0; v < V; ++v) tell(c.tiles + ((int64_t)k * threads + thread) * V + v, Map{kept(all.v[v].P), all.v[v].H});
         }
     }
     // each wave waits for some of the tiles before
@@ -352,7 +358,7 @@ __device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, in
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             start[v] = g > 0 ? __uint_as_float((uint32_t)(x[0][v] >> 32)) : first[v];
-            if (ends && on) tell(c.groups + ((int64_t)g * threads + thread) * V + v, 0u, apply(m.v[v], start[v]));
+            if (ends && on) tell(c.groups + ((int64_t)g * threads + thread) * V + v, 0u, apply(Map{kept(m.v[v].P), m.v[v].H}, start[v]));
             lds.start[lane][v] = start[v];
         }
     }
@@ -419,6 +425,8 @@ __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_kernel(const Seque
                 hold(add[i][v]);
             }
     }
+#pragma unroll
+    for (int v = 0; v < V; ++v) f.v[v].P = kept(f.v[v].P);
     state_before<V>(chain, lds, q.threads, thread, on, tile, wave, f, first, h);
     if (!on || n == 0) return;
     if (saved) {
@@ -514,6 +522,8 @@ __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_gradient_kernel(co
             f.v[v].P = reset ? -0.0f : a * f.v[v].P;
         }
     }
+#pragma unroll
+    for (int v = 0; v < V; ++v) f.v[v].P = kept(f.v[v].P);
     state_before<V>(chain, lds, q.threads, thread, on, k, wave, f, first, c);
     if (!on) return;
     T* dg = at.in(dgates) + t * dgates.step;

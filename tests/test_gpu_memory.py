@@ -170,6 +170,41 @@ def test_a_reset_forgets_what_is_no_number(T):
     assert dx[0, cut:cut + 5].isnan().all() and dx[0, :4].isfinite().all() and (dx[0, 4:cut] == 0).all()
 
 
+def _kind(t):
+    """0 of what is finite, 1 and -1 of the infinities, 2 of NaN."""
+    t = t.detach().cpu().double()
+    return torch.where(t.isnan(), torch.full_like(t, 2.0), torch.where(t.isinf(), t.sign(), torch.zeros_like(t)))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B, T, C, resets", [(1, 40, 6, 0.0), (1, 1500, 6, 0.0), (2, 1500, 5, 0.003), (1, 9000, 2, 0.0)])
+def test_infinities_stay_as_the_formula_has_them(B, T, C, resets, dtype):
+    """An infinite state remains one until a reset, however many steps lie behind and however they
+    are cut: the product of their gates is below fp32's range, and not 0."""
+    from paper_2607_26005_amd import memory
+    inf = float("inf")
+    g, x, s, r = _inputs(B, T, C, dtype, resets=resets, keep=0.0)
+    x[0, 9, 0], x[0, 11, 1] = inf, -inf
+    x[0, T // 2, 1] = inf    # against the one before: no number from here on
+    x[-1, T - 20, -1] = -inf
+    s[0, 0] = -inf           # against step 9's
+    if B > 1:
+        s[1, 1] = inf
+    want, last, *_ = O.scan(g, x, s, r)
+    out, after = memory.gated_scan(g, x, s, r)
+    assert torch.equal(_kind(out), _kind(want)) and torch.equal(_kind(after), _kind(last))
+    assert (_kind(want) == 1).any() or resets == 0.0
+    # and backwards
+    g, x, s, _ = _inputs(B, T, C, dtype, seed=5, keep=0.0)
+    dout, dlast = _rand(7, B, T, C).to("cuda", dtype), _rand(8, B, C).cuda()
+    dout[0, T - 9, 0], dout[0, T - 11, 1], dout[0, T // 2, 1], dlast[0, 0] = inf, -inf, inf, -inf
+    leaves = [t.requires_grad_() for t in (g, x, s)]
+    got = torch.autograd.grad(memory.gated_scan(*leaves, r), leaves, (dout, dlast))
+    grads, _ = O.scan_gradient(g, x, s, r, dout, dlast)
+    for name, a, w in zip(("dgates", "dinputs", "dstate"), got, grads):
+        assert torch.equal(_kind(a), _kind(w)), name
+
+
 def test_gates_at_their_ends():
     from paper_2607_26005_amd import memory
     inf = float("inf")
