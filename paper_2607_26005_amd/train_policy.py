@@ -11,8 +11,8 @@ pattern for a trainer, not a reproduction of the paper's results.
 
 With --memory the policy remembers the steps of an episode (memory.MemoryLayer): it acts
 one step at a time on states that stay on the device and learns from whole rollouts.  With
---prefer it also learns from pairs of agents, of which the one with the larger return is
-preferred.
+--prefer it also learns from pairs of agents, of which the one with the larger return over an
+episode's steps is preferred in them.
 
     python -m paper_2607_26005_amd.train_policy --iterations 4 --bits 8
     python -m paper_2607_26005_amd.train_policy --memory 2 --act-bits 8 --prefer 0.1
@@ -87,6 +87,23 @@ def advantages(rewards, values, last_value, gamma: float = 0.999, lam: float = 0
         run = rewards[t] + gamma * after - values[t] + gamma * lam * run
         out[t] = run
     return out, out + values
+
+
+def preferred(returns: torch.Tensor, resets: torch.Tensor):
+    """Pairs for the preference loss from [agents, steps] of a rollout, of every episode in it its
+    own: (rows of the [agents * steps] decisions, one sequence behind the other; offsets).  The
+    agent with the larger return over an episode's steps comes first.  All agents' episodes begin
+    together."""
+    n, steps = returns.shape
+    half, began = n // 2, resets[:1].any(0).tolist()
+    starts = [t for t in range(steps) if t == 0 or began[t]]
+    rows, lengths = [], [0]
+    for a, b in zip(starts, starts[1:] + [steps]):
+        order = returns[:, a].argsort(descending=True)
+        pairs = torch.stack([order[:half], order[n - half:]], 1).reshape(-1, 1)
+        rows.append((pairs * steps + torch.arange(a, b, device=returns.device)).reshape(-1))
+        lengths += [b - a] * (2 * half)
+    return torch.cat(rows), torch.tensor(lengths, device=returns.device).cumsum(0)
 
 
 class Trainer:
@@ -175,17 +192,13 @@ class Trainer:
 
     def remembered_update(self, batch, epochs: int = 2, prefer: float = 0.0):
         """The whole rollout as a minibatch, once an epoch; with prefer also that much of the
-        preference loss over pairs of agents.  Returns the last statistics of both."""
+        preference loss over pairs of agents, episode by episode.  Returns the last statistics of both."""
         seen, resets, before, actions, logp, values, adv, returns = batch
         n, steps = actions.shape
         flat = lambda t: t.reshape(-1)
-        pairs = None
         if prefer:
-            # the agent with the larger return first
-            order = returns[:, 0].argsort(descending=True)
-            half = n // 2
-            pairs = torch.stack([order[:half], order[n - half:]], 1).reshape(-1)
-            offsets = torch.arange(2 * half + 1, device=actions.device) * steps
+            rows_of, offsets = preferred(returns, resets)
+            did, before_logp = flat(actions)[rows_of], flat(logp)[rows_of]
         stats = liked = None
         for _ in range(epochs):
             out = self.net.sequence(seen, before, resets)
@@ -193,8 +206,7 @@ class Trainer:
             loss, stats = policy.policy_loss(rows[:, :ACTIONS], rows[:, ACTIONS], flat(actions), flat(logp), flat(adv),
                                              flat(returns), old_values=flat(values), clip=0.2, value_clip=0.2, normalize=True)
             if prefer:
-                some = out[pairs].reshape(-1, ACTIONS + 1)
-                other, liked, _ = policy.preference_loss(some[:, :ACTIONS], flat(actions[pairs]), offsets, flat(logp[pairs]))
+                other, liked, _ = policy.preference_loss(rows[rows_of, :ACTIONS], did, offsets, before_logp)
                 loss = loss + prefer * other
             self.opt.zero_grad()
             loss.backward()
