@@ -117,13 +117,17 @@ class MemoryLayer(nn.Module):
         with torch.no_grad():   # gates that keep for some ten steps
             self.project.bias[:width] = 2.0
 
-    def _split(self, x, residual, y):
-        return y if residual is not None else (y, x)
+    def _normed(self, x, residual):
+        """(what is projected, the stream): the norm, and x as the stream goes on."""
+        if residual is None:
+            return rms_norm(x, self.norm, None, self.eps), x
+        # (under autocast the layer before puts out its products' type, and the stream keeps its own)
+        return rms_norm(x.to(residual.dtype), self.norm, residual, self.eps)
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, state: Optional[torch.Tensor] = None,
                 resets: Optional[torch.Tensor] = None):
         """x [batch, steps, width] -> (output, residual stream, state after the last step)."""
-        y, stream = self._split(x, residual, rms_norm(x, self.norm, residual, self.eps))
+        y, stream = self._normed(x, residual)
         gates, inputs = self.project(y).chunk(2, -1)
         h, state = gated_scan(gates, inputs, state, resets)
         return self.out(h), stream, state
@@ -141,9 +145,10 @@ class MemoryLayer(nn.Module):
         stream).  codes (of `quantized`): the projection multiplies in 8 bits (width a multiple
         of 16)."""
         if codes is None:
-            y, stream = self._split(x, residual, rms_norm(x, self.norm, residual, self.eps))
+            y, stream = self._normed(x, residual)
             both = self.project(y)
         else:
+            x = x if residual is None else x.to(residual.dtype)
             held = rms_norm_8bit(x, self.norm, residual, self.eps)
             stream = x if residual is None else held.sum
             both = torch._scaled_mm(held.codes, codes[0].t(), scale_a=held.scales[:, None], scale_b=codes[1],

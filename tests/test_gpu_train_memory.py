@@ -86,6 +86,56 @@ def test_gradients_of_layers_against_differences():
         assert abs(got - want) <= 1e-3 + 1e-2 * g.double().norm(), (tuple(p.shape), got.item(), want.item())
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_layers_under_autocast(dtype):
+    """Products in 16 bits, the stream between the layers in its own type: bit for bit what the same
+    layers do by hand."""
+    from paper_2607_26005_amd import memory
+    layers = _layers(48, 3)
+    gen = torch.Generator().manual_seed(4)
+    x = torch.randn(2, 9, 48, generator=gen).cuda().requires_grad_()
+    dy = torch.randn(2, 9, 48, generator=gen).cuda()
+    params = [x] + [p for layer in layers for p in layer.parameters()]
+
+    def by_hand(x):
+        cut = lambda m, t: torch.nn.functional.linear(t.to(dtype), m.weight.to(dtype), m.bias.to(dtype))
+        stream, y = None, x
+        for layer in layers:
+            if stream is None:
+                normed, stream = memory.rms_norm(y, layer.norm), y
+            else:
+                normed, stream = memory.rms_norm(y.float(), layer.norm, stream)
+            gates, inputs = cut(layer.project, normed).chunk(2, -1)
+            y = cut(layer.out, memory.gated_scan(gates, inputs, torch.zeros(2, 48, device="cuda"))[0])
+        return y, stream
+
+    y, stream = by_hand(x)
+    want = torch.autograd.grad((y.float() + stream, ), params, dy)
+    with torch.autocast("cuda", dtype=dtype):
+        got, went = x, None
+        for layer in layers:
+            got, went, _ = layer(got, went, torch.zeros(2, 48, device="cuda"))
+    assert got.dtype == dtype and went.dtype == torch.float32 and torch.equal(got, y) and torch.equal(went, stream)
+    grads = torch.autograd.grad((got.float() + went, ), params, dy)
+    assert all(map(torch.equal, grads, want))
+    # and step by step (matrix products of other shapes add up in another order: a unit of the type
+    # in each of six products of values of some 2)
+    states = [torch.zeros(2, 48, device="cuda") for _ in layers]
+    codes = [layer.quantized() for layer in layers]
+    for t in range(9):
+        for how in (None, codes):
+            held = states if how is None else [s.clone() for s in states]
+            with torch.autocast("cuda", dtype=dtype):
+                z, r = x.detach()[:, t], None
+                for i, layer in enumerate(layers):
+                    z, r = layer.step(z, r, held[i], None, how and how[i])
+            assert z.dtype == dtype and r.dtype == torch.float32
+            if how is None:
+                assert torch.allclose(z.float() + r, (y.float() + stream)[:, t], atol=24 * torch.finfo(dtype).eps)
+            else:
+                assert z.isfinite().all() and r.isfinite().all()
+
+
 def test_projection_in_8_bits():
     from paper_2607_26005_amd import memory
     layer, = _layers(64, 1)
