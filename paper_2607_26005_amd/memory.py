@@ -134,9 +134,9 @@ class MemoryLayer(nn.Module):
 
     def quantized(self):
         """The projection's weights in 8 bits, for `step`: (codes [2 width, width], scales)."""
-        w = self.project.weight.detach()
-        scales = w.abs().amax(1, keepdim=True).clamp(min=1e-30).float() / 448.0
-        return (w.float() / scales).to(torch.float8_e4m3fn), scales.t().contiguous()
+        w = self.project.weight.detach().float()   # (1e-30 is 0 in float16)
+        scales = w.abs().amax(1, keepdim=True).clamp(min=1e-30) / 448.0
+        return (w / scales).to(torch.float8_e4m3fn), scales.t().contiguous()
 
     @torch.no_grad()
     def step(self, x: torch.Tensor, residual: Optional[torch.Tensor], state: torch.Tensor,

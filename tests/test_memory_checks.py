@@ -375,3 +375,21 @@ def test_the_norms_c_entries_refuse():
     out = ctypes.c_uint64()
     assert L.pictura_rms_norm_gradient_workspace(None, ctypes.addressof(out)) == pictura.EINVAL
     assert L.pictura_rms_norm_gradient_workspace(ref(q()), None) == pictura.EINVAL
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_weights_in_8_bits(dtype):
+    """Codes stand for the weights to half a step of e4m3, rows of zeros and of the smallest numbers too."""
+    layer = memory.MemoryLayer(32)
+    w = torch.randn(64, 32, generator=torch.Generator().manual_seed(1))
+    w[3], w[5], w[7] = 0, w[5] * 2.0 ** -20, torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+    with torch.no_grad():
+        layer.project.weight.copy_(w)
+    layer = layer.to(dtype)
+    w = layer.project.weight.detach().double()
+    codes, scales = layer.quantized()
+    assert codes.shape == (64, 32) and scales.shape == (1, 64) and scales.dtype == torch.float32 and (scales > 0).all()
+    values, half = codes.double() * scales.double().t(), torch.maximum(w.abs() * 2.0 ** -4, scales.double().t() * 2.0 ** -10)
+    # (a row whose largest magnitude is below 1e-30 is taken for zeros; the quotient is rounded to fp32)
+    held = w.abs().amax(1) >= 1e-30
+    assert ((values - w).abs() <= half * (1 + 2.0 ** -20))[held].all() and (values[~held].abs() <= 1e-30).all() and (values[3] == 0).all()
