@@ -754,9 +754,11 @@ struct Shape {
     int64_t threads;
 };
 
+int64_t vectors_of(int32_t channels, int32_t vec) { return ((int64_t)channels + vec - 1) / vec; }
+
 Shape shape_of(const pictura_sequences& q, int32_t vec, bool back)
 {
-    Shape s{vec, 0, q.batch * ((q.channels + vec - 1) / vec)};
+    Shape s{vec, 0, q.batch * vectors_of(q.channels, vec)};
     const int64_t waves = (s.threads + 63) / 64, tile = tile_steps(vec), tiles = (q.steps + tile - 1) / tile;
     // (a launch has fewer than 2^32 threads)
     if (waves < (back ? many_back(vec) : kManyWaves) && q.steps >= 2 * tile && waves * tiles <= 1 << 21) s.tiles = (int32_t)tiles;
@@ -815,9 +817,10 @@ pictura_status launched() { return hipGetLastError() == hipSuccess ? PICTURA_OK 
 template <class T>
 Sequences<T> sequences_of(const pictura_sequences& q, const Shape& s)
 {
+    const int64_t vectors = vectors_of(q.channels, s.vec);
     return Sequences<T>{{(const T*)q.gates, q.gates_batch, q.gates_step}, {(const T*)q.inputs, q.inputs_batch, q.inputs_step},
                         q.state, {q.resets, q.resets_batch, q.resets_step}, s.threads, q.steps,
-                        q.batch * q.channels, q.channels, (q.channels + s.vec - 1) / s.vec, (q.channels + s.vec - 1) / s.vec % 64 == 0};
+                        q.batch * q.channels, q.channels, (int32_t)vectors, vectors % 64 == 0};
 }
 
 Chain chain_of(void* workspace, const Shape& s)
@@ -958,7 +961,7 @@ pictura_status pictura_gated_step(const pictura_sequences* q, void* out, int64_t
     auto go = [&](auto t) {
         using T = decltype(t);
         constexpr int V = 16 / sizeof(T);
-        const Shape s{V, 0, q->batch * ((q->channels + V - 1) / V)};
+        const Shape s{V, 0, q->batch * vectors_of(q->channels, V)};
         hipLaunchKernelGGL(step_kernel<T>, dim3((unsigned)((s.threads + 255) / 256)), dim3(256), 0, (hipStream_t)stream,
                            sequences_of<T>(*q, s), (T*)out, out_batch, state);
     };

@@ -247,6 +247,16 @@ def test_workspace_covers_every_split():
         assert need.value <= 256 + (512 + 32) * 8 * max(batch * channels, 64 * 4096)
 
 
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("channels", [2 ** 31 - 1, 2 ** 31 - 2, 2 ** 31 - 8])
+def test_as_many_channels_as_there_may_be(channels, dtype):
+    """Their count of threads does not leave 32 bits: such scans are not cut, and need no words for tiles."""
+    need = ctypes.c_uint64()
+    q = _q(batch=1, steps=1 << 20, channels=channels, dtype=dtype)
+    assert pictura._lib.pictura_gated_scan_workspace(ctypes.byref(q), ctypes.addressof(need)) == pictura.OK
+    assert need.value == 256
+
+
 # --- the norm ---------------------------------------------------------------------
 
 N, W = 4, 6
