@@ -257,6 +257,20 @@ def test_as_many_channels_as_there_may_be(channels, dtype):
     assert need.value == 256
 
 
+def test_a_workspace_holds_the_words_of_its_tiles():
+    """Pairs of channels of 16 bits are cut into tiles of 128 steps, single channels into tiles of 256; each tile
+    tells a word of 8 bytes a channel, and every 16 of them one more, behind 256 bytes for the tickets."""
+    need = ctypes.c_uint64()
+    for dtype, batch, steps, channels in ((0, 1, 65521, 1024), (1, 1, 65521, 1024), (2, 3, 8191, 331), (0, 3, 8191, 331), (1, 5, 512, 1),
+                                          (1, 1, 2 ** 31 - 1, 2), (0, 1, 511, 8), (0, 1, 512, 8), (1, 1, 255, 8), (1, 1, 256, 8)):
+        q = _q(batch=batch, steps=steps, channels=channels, dtype=dtype)
+        assert pictura._lib.pictura_gated_scan_workspace(ctypes.byref(q), ctypes.addressof(need)) == pictura.OK
+        pair, tile = (2, 128) if dtype and channels > 1 else (1, 256)
+        threads, tiles = batch * -(-channels // pair), -(-steps // tile)
+        cut = steps >= 2 * tile and (threads + 63) // 64 * tiles <= 1 << 21
+        assert need.value == 256 + (8 * threads * pair * (tiles + -(-tiles // 16)) if cut else 0), (dtype, batch, steps, channels)
+
+
 # --- the norm ---------------------------------------------------------------------
 
 N, W = 4, 6
