@@ -680,10 +680,9 @@ __global__ __launch_bounds__(256, 4) void scan_gradient_kernel(const Sequences<T
 
 // One step in place: as many channels a thread as 16 bytes hold, at any address.  (The last
 // ones of a sequence one by one: a state is read before it is replaced, so no two threads
-// may hold a channel.)
+// may hold a channel.  out and state may be a thread's own operands: no __restrict__.)
 template <class T>
-__global__ __launch_bounds__(256) void step_kernel(const Sequences<T> q, T* __restrict__ out, int64_t out_batch,
-                                                   float* __restrict__ state)
+__global__ __launch_bounds__(256) void step_kernel(const Sequences<T> q, T* out, int64_t out_batch, float* state)
 {
     constexpr int V = 16 / sizeof(T);
     const int64_t thread = (int64_t)blockIdx.x * 256 + threadIdx.x;

@@ -135,7 +135,8 @@ __device__ __forceinline__ float factor(double sum, int32_t width, float eps)
     return (float)(1.0 / __builtin_sqrt(sum / (double)width + (double)eps));
 }
 
-// out: T, or 8-bit codes with a scale for each row.
+// out: T, or 8-bit codes with a scale for each row.  sum and out may be the rows that are read (all of
+// a row is before any of it is written): no __restrict__.
 struct Codes {
     void* codes;
     int64_t stride;
@@ -144,8 +145,8 @@ struct Codes {
 };
 
 template <class T, class W, int V, int NV, class Tm, bool kCodes>
-__global__ __launch_bounds__(Tm::kThreads) void norm_kernel(const Rows<T> R, T* __restrict__ sum, int64_t sum_stride,
-                                                            T* __restrict__ out, int64_t out_stride,
+__global__ __launch_bounds__(Tm::kThreads) void norm_kernel(const Rows<T> R, T* sum, int64_t sum_stride,
+                                                            T* out, int64_t out_stride,
                                                             float* __restrict__ factors, const Codes codes)
 {
     __shared__ double ldsd[Tm::NW];

@@ -319,6 +319,30 @@ def test_single_steps_are_the_scan(B, C, dtype):
         assert memory.gated_step(g[:, 0], a, b, out=a) is a and torch.equal(a, want)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B, C", [(1, 1), (5, 7), (300, 40), (3, 513), (64, 2050)])
+def test_a_step_in_place(B, C, dtype):
+    """What a step writes may be its own operands' memory."""
+    from paper_2607_26005_amd import memory
+    g, x, s, r = (t[:, 0] if t.dim() == 3 else t for t in _inputs(B, 1, C, dtype, resets=0.3))
+    r = r[:, 0]
+    held = s.clone()
+    want = memory.gated_step(g, x, held, r)
+    both = torch.cat([g, x, torch.zeros_like(g)], 1)
+    for k in range(3):   # over the gates, over the inputs, between them
+        rows, state = both.clone(), s.clone()
+        got = memory.gated_step(rows[:, :C], rows[:, C:2 * C], state, r, rows[:, k * C:(k + 1) * C])
+        assert torch.equal(got, want) and torch.equal(state, held)
+        left = [i for i in range(3) if i != k]
+        assert all(torch.equal(rows[:, i * C:(i + 1) * C], both[:, i * C:(i + 1) * C]) for i in left)
+    if dtype == torch.float32:
+        state = s.clone()
+        assert memory.gated_step(g, x, state, r, state) is state and torch.equal(state, held)
+        state = x.clone()   # the inputs are the state
+        want = memory.gated_step(g, x, x.clone(), r)
+        assert torch.equal(memory.gated_step(g, state, state, r), want) and torch.equal(state, want)
+
+
 def test_rows_and_channels_beyond_are_left():
     from paper_2607_26005_amd import memory, pictura
     g, x, s, _ = _inputs(2, 20, 6, torch.float32)
