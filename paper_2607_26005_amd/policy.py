@@ -130,7 +130,8 @@ def preference_gradient(logits, actions, offsets, ref_logp=None, *, weights=None
     offsets[s] on up to offsets[s + 1] (int64 [2 pairs + 1], on the device), and of pair p
     sequence 2p is the one preferred to sequence 2p + 1.  ref_logp [rows]: the actions'
     log-probabilities by the policy that is not to be left too far (None: 0).  Padded
-    sequences are ones whose further rows have action -1.
+    sequences are ones whose further rows have action -1.  Sequences are best of like lengths:
+    with heads of up to 64 actions one pair far longer than the others is a workgroup's alone.
 
     weights [pairs]; the loss is the mean by weight, or the sum over `denominator` where that
     is given: parts of a minibatch then add up.  average: a sequence's log ratio is the mean

@@ -110,6 +110,17 @@ def test_many_pairs(pairs):
         _check(l, a, o, r, weights=w)
 
 
+@pytest.mark.parametrize("A", [3, 12, 50])
+@pytest.mark.parametrize("longest", [(40, 20001), (399, 20001), (0, 7000)])
+def test_one_long_pair_among_many_short_ones(longest, A):
+    """Lengths far from their mean: a pair of thousands of rows is one workgroup's where there are pairs enough."""
+    g = torch.Generator().manual_seed(A)
+    lengths = torch.randint(0, 5, (400,), generator=g).tolist()
+    lengths[longest[0]] = longest[1]
+    l, a, o, r, _ = _inputs(lengths, A, unused=0.1, outside=5)
+    _check(l, a, o, r, weights=torch.rand(200, generator=g).cuda(), average=True, beta=0.5)
+
+
 @pytest.mark.parametrize("A", [12, 100])
 def test_rows_outside_the_sequences(A):
     l, a, o, r, _ = _inputs([4, 9], A, outside=300)
