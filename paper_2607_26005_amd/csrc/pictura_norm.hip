@@ -439,7 +439,9 @@ struct Int {
 // single elements.  Two vectors a lane, so that a wave has more rows or bytes under way,
 // are as good as one or better up to a wave's width (131,072 rows of 300 in bf16: forward 68
 // us and 74, gradient 73 and 81; 262,144 of 512: 192 and 196, 199 and 208), except where codes
-// come out and most lanes have a vector (65,536 of 512 to e4m3 and back: 82.7 and 80.4).
+// of 16-bit rows come out and most lanes have a vector (65,536 to e4m3 with a residual, two a
+// lane and one: of 400 38.1 and 37.2, 448 39.1 and 36.3, 480 40.4 and 38.5, 512 42.7 and 41.7;
+// but in fp32 of 224 30.2 and 32.4, of 256 33.6 and 36.4).
 // Wider rows of 16 bits take one a lane and more waves, whose registers then hold all of
 // a row in fp32 (32,768 rows of 2,048 by one wave or four: forward 111 and 98 us, codes 109 and
 // 97, gradient 128 and 109); fp32 rows four (32,768 of 1,024: 94 and 99, 81 and 83, 105 and 120).
@@ -452,7 +454,7 @@ void with_team(int32_t width, F go)
     if (vectors <= 8) return go(Int<V>{}, Int<1>{}, Team<8, 1>{});
     if (vectors <= 16) return go(Int<V>{}, Int<2>{}, Team<8, 1>{});
     if (vectors <= 32) return go(Int<V>{}, Int<2>{}, Team<16, 1>{});
-    if constexpr (kCodes)
+    if constexpr (kCodes && V == 8)
         if (vectors > 48 && vectors <= 64) return go(Int<V>{}, Int<1>{}, Team<64, 1>{});
     if (vectors <= 64) return go(Int<V>{}, Int<2>{}, Team<32, 1>{});
     if (vectors <= 128) return go(Int<V>{}, Int<2>{}, Team<64, 1>{});
