@@ -663,7 +663,8 @@ pictura_status pictura_gated_scan_workspace(const pictura_sequences* sequences, 
  * needs: the states before steps 0, 16, 32, ...  The same call gives the same bits; where few
  * channels stand against many steps the steps are cut into tiles, which rounds states in
  * another order.  last_state must not overlap state, nor out the inputs.  Of no steps
- * last_state is state (or zeros).
+ * last_state is state (or zeros).  A tile waits for those before it, which have started before
+ * it; should the device not run them for a second, the states behind are NaN up to a reset.
  * workspace: device memory, 256-byte aligned, in use until the call's work on the stream
  * is done.  EINVAL: a null or misaligned pointer, sizes or strides out of range, or a
  * workspace too small. */
@@ -737,7 +738,8 @@ pictura_status pictura_rms_norm_gradient_workspace(const pictura_norm* norm, uin
  * its factors; from dout (of out) and dsum (of sum; or NULL: zeros), with k = dout weight
  * and u = x q, dx = q (k - u mean(k u)) + dsum, the gradient of x and of the residual
  * alike, rounded to dtype once, and dweight = sum over the rows of dout u, in the weight's
- * type, summed in a fixed order.  dx may be dout's or dsum's own memory (same stride).
+ * type, summed in a fixed order (a workgroup's rows in fp32, the
+ * workgroups in fp64).  dx may be dout's or dsum's own memory (same stride).
  * With no rows dweight is 0.  Errors as pictura_rms_norm; workspace: device memory,
  * 256-byte aligned, in use until the call's work on the stream is done. */
 pictura_status pictura_rms_norm_gradient(const pictura_norm* norm, const float* factors, const void* dout, int64_t dout_stride,

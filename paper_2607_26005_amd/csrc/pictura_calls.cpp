@@ -1,8 +1,8 @@
 // The calls of memory.py and of the preference loss, with their autograd: checks, outputs
 // and workspaces from the caching allocator, one call of the library.  From Python, by
 // ctypes and a Python autograd function, the same took 12 to 19 us of the host a call and
-// 138 us for a scan with its gradient; here 5 to 10 us and 78 (torch's own layer norm with its
-// gradient: 69 to 71).
+// 138 us for a scan with its gradient; here 4 to 10 us and 55 to 78 (torch's own layer norm with
+// its gradient: 69 to 71, its silu 45).
 #include "pictura_tensors.h"
 
 #include <ATen/TracerMode.h>
@@ -130,10 +130,10 @@ variable_list once(const variable_list& from, variable_list out)
 // sees only the outputs' allocation, and would take what comes out for a constant.
 void check_seen(const char* call)
 {
-    const char* by = at::tracer::impl::is_dispatch_enabled()                                                               ? "torch.jit.trace"
-                     : c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode) ? "torch.func"
-                     : c10::impl::TorchDispatchModeTLS::any_modes_set()                                          ? "a dispatch mode"
-                                                                                                                 : nullptr;
+    const char* by = nullptr;
+    if (at::tracer::impl::is_dispatch_enabled()) by = "torch.jit.trace";
+    else if (c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode)) by = "torch.func";
+    else if (c10::impl::TorchDispatchModeTLS::any_modes_set()) by = "a dispatch mode";
     if (by) refuse(call, ": called under ", by, ", which would not see it");
 }
 
@@ -641,7 +641,8 @@ struct PreferenceLoss : torch::autograd::Function<PreferenceLoss> {
             if (dlogits.scalar_type() == at::kFloat) {
                 out[0] = dlogits.mul(grads[0]);
                 if (half) out[0] = out[0].to(at::kHalf);
-            } else {   // (the product in fp32: a loss scale may be beyond what the type holds)
+            } else {   // (the product in fp32: a loss scale may be beyond what the type holds.  bfloat16 is rounded
+                       // before it too, half a step more: its range loses nothing, and fp32 takes twice the memory)
                 out[0] = at::empty_like(dlogits);
                 at::mul_out(out[0], dlogits.to(at::kFloat), grads[0]);
             }

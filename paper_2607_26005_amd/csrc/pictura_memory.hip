@@ -14,12 +14,15 @@
 // once.  Where there are too few channels for the card, the steps are cut into tiles, a
 // workgroup each: what a tile's steps do to a state is h -> P h + H, with P the product of
 // their a, which every workgroup tells those behind it; it keeps a and (1 - a) x in registers
-// until it knows the state before its own.  Everything is read and written once, and joined in
-// one order, so that results repeat to the bit.
+// until it knows the state before its own (a scan in one pass with a look back: Merrill and
+// Garland, "Single-pass parallel prefix scan with decoupled look-back", 2016; here by groups of
+// tiles, and values that carry their own flag).  Everything is read and written once, and joined
+// in one order, so that results repeat to the bit.
 //
 // Measured (one MI355X, large copies at 5,150 GB/s): 2,048 x 128 steps of 512 channels in bf16
-// forward 173 us, gradient 294 (838 and 1,376 MB with the saved states: 4.8 and 4.7 TB/s); one
-// of 65,521 steps of 1,024 forward 112 us, gradient 160 (419 and 688 MB: 3.7 and 4.3 TB/s), of
+// forward 173 to 179 us, gradient 294 (838 and 1,376 MB with the saved states: 4.7 and 4.7 TB/s,
+// the gradient with four registers spilled where there are no resets); one
+// of 65,521 steps of 1,024 forward 109 us, gradient 160 (419 and 688 MB: 3.8 and 4.3 TB/s), of
 // which a launch that sums the segments up first and one that reads them again took 152 and 221;
 // single steps of 65,536 x 512 in bf16 69 us (470 MB: 6.8 TB/s, some of it from the caches).
 #include <cmath>
@@ -249,8 +252,8 @@ constexpr int kItems = kGroup / tile_waves(V);   // tiles of its group that a wa
 
 // Waits until the words of up to kItems<V> tiles are there, `apart` of them apart.  A workgroup
 // waits only for such with smaller tickets, which have started before it and in turn wait
-// only for smaller ones: every wait ends.  (If one did not, its values would be taken as they
-// are, NaNs.)
+// only for smaller ones: every wait ends, long before kPolls.  (If one did not, its values would
+// be taken as they are: NaN states from there to the next reset, as the header says.)
 template <int V>
 __device__ __forceinline__ void await(const Word* at, int64_t apart, int items, bool on, Word (&w)[kItems<V>][V])
 {
@@ -380,7 +383,7 @@ __device__ __forceinline__ void state_before(const Chain& c, TileLds<V>& lds, in
 }
 
 // Forwards over one tile.  Of bf16 it takes 940 vector instructions a wave, and the vector units
-// are busy for 54 % of its time (backwards 1,520 and 60 %); workgroups that take several tiles, and the next ticket ahead, are slower (169 us and
+// are busy for 55 % of its time (backwards 1,520 and 60 %); workgroups that take several tiles, and the next ticket ahead, are slower (169 us and
 // 121), as tickets wait for workgroups that are not ready.
 template <class T, int V, bool kResets>
 __global__ __launch_bounds__(tile_waves(V) * 64, 4) void tile_kernel(const Sequences<T> q, const Tensor<T> out, float* __restrict__ last,

@@ -16,9 +16,10 @@
 // Bound by memory.  Measured (one MI355X, large copies at 5,150 GB/s): 262,144 rows of 512 in
 // bf16 with residual forward 181 us, gradient 203 and the sums of dw 7 (1,074 MB each: 5.9 and
 // 5.3 TB/s, some of it from the caches); 65,536 of 512 to e4m3 51 us, their values 25; 4,095
-// of 8,197 in fp32 99, 111 and 7 us (537 MB each: 5.4 and 4.8 TB/s).  Rows of more than 16,384
-// elements of 16 bits have more sums of dw than registers: 2,048 of 32,768 forward 117 us,
-// gradient 315.
+// of 8,197 in fp32 98, 110 and 7 us (537 MB each: 5.5 and 4.9 TB/s).  In rows of more than 16,384
+// elements the gradient spills 110 to 160 registers, of more than 32,768 some 520 to 610 (and the
+// forward 60 to 80): in bf16 2,048 of 32,768 forward 118 us, gradient 319, 1,024 of 65,536 230 and
+// 630; in fp32 1,024 of 32,768 108 and 280, 512 of 65,536 200 and 476.
 #include <cmath>
 
 #include "pictura.h"
@@ -286,7 +287,9 @@ struct Gradient {
 };
 
 // Teams take rows in turn, one workgroup's the same distance apart, and keep the sums of
-// dy (s q) of their columns in registers.
+// dy (s q) of their columns in registers: in fp32, as fp64 would take twice the
+// registers.  A team adds up some 16 rows (4,095 of 8,197 in fp32: dw is off by 9e-8, and by 5e-8
+// if summed in 64 bits) to 32 (262,144 of 512), the workgroups' sums are added up in fp64.
 template <class T, class W, int V, int NV, class Tm>
 __global__ __launch_bounds__(Tm::kThreads) void norm_gradient_kernel(const Gradient<T> R)
 {

@@ -89,8 +89,9 @@ class RowCodes(NamedTuple):
 def rms_norm_8bit(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
                   dtype: torch.dtype = torch.float8_e4m3fn) -> RowCodes:
     """rms_norm with an output in 8 bits, for layers that multiply in them: codes of `dtype`
-    (float8_e4m3fn or int8) and a scale for each row, its largest magnitude over 448 or 127.
-    Codes are the nearest ones of the float32 result, to the bit.  Codes and scales have no
+    (float8_e4m3fn or int8) and a scale for each row, its largest magnitude M over 448 or 127.
+    A code is the nearest one of the float32 result y times 448 (1 / M) or 127 (1 / M), each
+    operation rounded to float32.  Codes and scales have no
     gradient: where one is wanted it raises when it would reach them (detach them to go
     without).  `sum` hands on its own, to x and the residual."""
     if dtype not in (torch.int8, torch.float8_e4m3fn):

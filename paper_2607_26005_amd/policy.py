@@ -152,7 +152,8 @@ def preference_loss(logits, actions, offsets, ref_logp=None, *, weights=None, ma
     """(loss, stats, ratios) for autograd: preference_gradient's loss, whose backward hands
     on the gradient that the same call computed, times the factor that arrives (a loss
     scale).  Only the logits get one: a ref_logp or weights that want a gradient are refused.
-    Of float16 logits the gradient is kept in float32 for that."""
+    Of float16 logits the gradient is kept in float32 for that; of bfloat16 ones in bfloat16, so
+    that a factor rounds it once more."""
     try:
         return _tensors.preference_loss(logits, actions, offsets, ref_logp, weights, mask, beta, smoothing, average,
                                         denominator)
